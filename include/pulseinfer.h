@@ -328,6 +328,109 @@ int pi_append_kv_devstep(pi_ctx* ctx, int layer, int batch, const uint32_t* step
                          int32_t* block_table_dev, int32_t* slot_block_dev, uint32_t* slot_stamp_dev,
                          void* digest_dev, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------
+ * The path on a cache in 4 bits, and what feeds it.  (The paper keeps its cache in 16 bits and starts at
+ * the queries and keys; these calls exist for the library's users.)  The recall path is bound by the bytes
+ * that cross the host link; a 4-bit block has 20480 bytes where the bf16 block has 65536 (B = 16, Hkv = 8).
+ * Selection and diff do not touch the cache and are used unchanged: score_select_diff -> pi_recall_kv4 ->
+ * pi_sparse_decode_attn_kv4, with pi_append_kv4 before them.
+ * These calls make the context's device current for the launch and put the caller's back.
+ *
+ * 4-bit block: [Hkv][B/16 tiles][2560 bytes], rounded up to a multiple of 4096 bytes (pi_kv4_block_bytes;
+ * the padding is never read as data).  A tile holds 16 tokens of one KV head:
+ *   bytes    0..1023 K codes [16][64], 1024..2047 V codes [16][64],
+ *         2048..2303 K scales [16][4]{scale, minimum} bf16, 2304..2559 V scales likewise.
+ * Each row of 128 channels is cut into 4 groups of 32: minimum = min x, scale = bf16((max x - min x) / 15)
+ * computed in fp32, code = (x - minimum) / scale rounded half to even and clamped to 0..15 (0 where the
+ * scale is 0); the value is scale * code + minimum.  K row: channel 32 j + 8 c + i is nibble i of the
+ * little-endian 32-bit word at byte 16 c + 4 j; V row: channel 32 j + 4 r + i is nibble i of the 16-bit
+ * word at byte 8 r + 2 j.  An infinite or NaN input, or a group whose spread overflows fp32, makes that
+ * group of that row read back as NaN. */
+
+/* Bytes of a 4-bit block of this context's shape (> 0), or a negative PI_ERR_* code. */
+int64_t pi_kv4_block_bytes(pi_ctx* ctx);
+
+/* Page table and slot map from request lengths, for a paged store (block-sized pages, 16 or 4 bits).  Every
+ * sequence goes from old_len to new_len tokens: one that grows takes the pages its new blocks need, one that
+ * shrinks (retired: new_len 0; drafts rolled back) gives the pages behind its new last block back.
+ *   old_len_dev, new_len_dev  [batch] int32, >= 0
+ *   page_table_dev   [batch][page_table_seq_stride] int32 (in/out): page of each block; entries given back
+ *                    become -1, all others stay as they are
+ *   free_pages_dev   [n_pages] int32 ring of free pages (in/out);  free_state_dev int64[4] (in/out): [0] pages
+ *                    taken and [1] pages given back since the start (free pages are ring entries [0]..[1]-1
+ *                    modulo n_pages: start with 0 and the number of free pages, entries in order from 0),
+ *                    [2] must be 0 (used during the call), [3] unused
+ *   token_start_dev  NULL or [batch + 1] int32 (out): new tokens before each sequence, the total last
+ *   n_tokens         capacity of the two maps of the packed batch of new tokens (sequence after sequence, in
+ *                    order of position):
+ *   slot_map_dev     NULL or [n_tokens] int64 (out): page * B + position % B;  positions_dev NULL or [n_tokens]
+ *                    int32 (out).  Entries behind the last new token become -1, which pi_kv4_store and
+ *                    pi_qk_norm_rope skip: a captured graph may keep one capacity.
+ * All or nothing: a length that is negative or needs more blocks than the row or max_blocks holds
+ * (PI_ERR_INDEX_RANGE: sequence, old, new), too few free pages (PI_ERR_POOL_TOO_SMALL: -1, wanted, free), more
+ * pages given back than the ring has places or more tokens than n_tokens (PI_ERR_CAPACITY), or a damaged
+ * free_state (PI_ERR_INDEX_RANGE) sets the status word with stage 7, changes no table, ring or counter, and
+ * fills the maps with -1 and token_start with 0.  A page outside [0, n_pages) found in the ring or the table
+ * is reported likewise; its table entry and its tokens' slots become -1.
+ * The caller orders calls that share a ring or a table; each sequence may appear in a batch once. */
+int pi_assign_pages(pi_ctx* ctx, int batch, const int32_t* old_len_dev, const int32_t* new_len_dev, int32_t* page_table_dev,
+                    int64_t page_table_seq_stride, int32_t* free_pages_dev, int32_t n_pages, int64_t* free_state_dev,
+                    int32_t* token_start_dev, int64_t n_tokens, int64_t* slot_map_dev, int32_t* positions_dev, void* stream);
+
+/* RMS norm of every query and key head and the rotation by position, from the projections to the q, k_new and
+ * k that the other calls take (bf16), in one pass:
+ *   y = x * rsqrt(mean(x^2) + eps) * weight    (both weights NULL: y = x)
+ *   pair (a, b) of the first rot_dim channels -> (a cos - b sin, b cos + a sin) at positions[t] * inv_freq[pair],
+ *   the angle computed in 64 bits;  pairs are (i, i + rot_dim/2), or (2i, 2i + 1) if interleaved.
+ *   dtype             PI_DTYPE_* of q_dev and k_dev: [n_tokens][Hq][D] and [n_tokens][Hkv][D], rows of a token
+ *                     contiguous, tokens q_token_stride / k_token_stride ELEMENTS apart (multiples of 16 bytes;
+ *                     so slices of one fused projection can be passed)
+ *   positions_dev     [n_tokens] int32; a token with a negative position is padding: its output rows stay as they were
+ *   q_weight_dev, k_weight_dev [D] float;  inv_freq_dev [rot_dim/2] float;  rot_dim even, 0..128
+ *   q_out_dev, k_out_dev  bf16 [n_tokens][Hq][D], [n_tokens][Hkv][D]; may be the inputs themselves if those are
+ *                     bf16 and contiguous */
+#define PI_DTYPE_BF16 0
+#define PI_DTYPE_FP16 1
+#define PI_DTYPE_FP32 2
+int pi_qk_norm_rope(pi_ctx* ctx, int64_t n_tokens, int dtype, const void* q_dev, int64_t q_token_stride, const void* k_dev,
+                    int64_t k_token_stride, const int32_t* positions_dev, const float* q_weight_dev, const float* k_weight_dev,
+                    float eps, const float* inv_freq_dev, int rot_dim, int interleaved, void* q_out_dev, void* k_out_dev, void* stream);
+
+/* Tokens into 4-bit blocks.  Token t, KV head h has its K row at k_dev + (t / inner_tokens) * k_outer_stride +
+ * (t % inner_tokens) * k_token_stride + h * k_head_stride (in bf16 ELEMENTS, multiples of 8; inner_tokens 0: one
+ * run of tokens), V likewise; it goes to token slot_map_dev[t] % B of block slot_map_dev[t] / B of `store`
+ * (device memory, or pinned host memory; n_blocks blocks).  slot_map_dev NULL: token t to slot t.  A negative slot
+ * is skipped, one beyond the store sets PI_ERR_INDEX_RANGE (stage 6: token, head, slot) and is skipped; all other
+ * bytes of the store stay as they are.  Two tokens of one call must not name the same slot. */
+int pi_kv4_store(pi_ctx* ctx, int64_t n_tokens, const void* k_dev, int64_t k_token_stride, int64_t k_head_stride,
+                 int64_t k_outer_stride, const void* v_dev, int64_t v_token_stride, int64_t v_head_stride,
+                 int64_t v_outer_stride, int64_t inner_tokens, const int64_t* slot_map_dev, void* store, int64_t n_blocks,
+                 void* stream);
+/* 4-bit blocks back to bf16: block blocks_dev[i] (NULL: i) of `store` to kv_dev [n_out][Hkv][2][B][D].  A block
+ * outside [0, n_blocks) sets PI_ERR_INDEX_RANGE (stage 6) and its output stays as it was. */
+int pi_kv4_load(pi_ctx* ctx, int64_t n_out, const void* store, int64_t n_blocks, const int32_t* blocks_dev, void* kv_dev, void* stream);
+
+/* pi_append_kv for pool and host store in 4 bits; slots, tables, stamps, digest (of the key as given) and errors as
+ * there.  step_dev NULL: `step` (>= 1) is the stamp, else *step_dev is read when the kernel runs.  page_table_dev
+ * NULL: block-major store [batch][NB] of 4-bit blocks, host_seq_stride_bytes apart; else an arena of 4-bit pages. */
+int pi_append_kv4(pi_ctx* ctx, int layer, int batch, uint32_t step, const uint32_t* step_dev, const void* k_new_dev,
+                  const void* v_new_dev, const int32_t* ctx_len_dev, void* host_kv4_pinned, int64_t host_seq_stride_bytes,
+                  const int32_t* page_table_dev, int64_t page_table_seq_stride, int32_t n_pages, void* pool4_dev,
+                  int32_t* block_table_dev, int32_t* slot_block_dev, uint32_t* slot_stamp_dev, void* digest_dev, void* stream);
+
+/* pi_recall_gather_scatter(_paged) with a 4-bit block as the unit: one list per sequence, pool4_dev [batch][C]
+ * 4-bit blocks.  Errors and skipped units as there, against C and NB blocks. */
+int pi_recall_kv4(pi_ctx* ctx, int layer, int batch, const void* host_kv4_pinned, int64_t host_seq_stride_bytes,
+                  const int32_t* page_table_dev, int64_t page_table_seq_stride, int32_t n_pages, void* pool4_dev,
+                  const pi_extent* recall_list_dev, int32_t list_capacity, const int32_t* recall_count_dev, void* stream);
+
+/* pi_sparse_decode_attn over a pool of 4-bit blocks ([batch][C]); any Hkv and G of the context.  Bytes of tokens
+ * beyond ctx_len in a selected block are ignored whatever they are.  A sequence without a single token to attend
+ * to gets zeros, and lse -inf. */
+int pi_sparse_decode_attn_kv4(pi_ctx* ctx, int layer, int batch, const void* q_dev, const void* pool4_dev,
+                              const int32_t* sel_slots_dev, const int32_t* sel_blocks_dev, const int32_t* sel_count_dev,
+                              const int32_t* ctx_len_dev, void* out_dev, float* lse_dev, void* stream);
+
 /* Helpers around the path (input preparation and measurement; not hot calls).
  * pi_build_digests: channel-wise min / max of the keys of head solo_head[layer] over the
  *   valid tokens of each block; kv may be device memory or pinned host memory laid out
@@ -357,7 +460,7 @@ int pi_middle_attention_mass(pi_ctx* ctx, int batch, const float* lse_mid_dev, c
 int pi_empty_launch(int n_ctas, int n_threads, void* stream);
 
 /* Sticky device status.  out[0] = first PI_ERR_* code seen by a kernel (0 = none),
- * out[1] = stage (1 score/select, 2 diff, 3 recall, 4 attention, 5 append), out[2..4] = sequence
+ * out[1] = stage (1 score/select, 2 diff, 3 recall, 4 attention, 5 append, 6 4-bit store / load, 7 page assignment), out[2..4] = sequence
  * or list, position, offending value.  Reads a pinned mirror: call after the stream
  * has been synchronised.  pi_clear_status resets it. */
 int pi_get_status(pi_ctx* ctx, int32_t out[8]);

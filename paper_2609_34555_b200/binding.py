@@ -24,7 +24,10 @@ EXTENT_DTYPE = torch.int32      # a pi_extent is four int32: src_unit, dst_unit,
 
 EXPORTS = ["pi_create", "pi_destroy", "pi_score_select", "pi_score_select_diff", "pi_score_select_diff_devstep", "pi_score_select_noalloc", "pi_score_select_strategy", "pi_diff_misses", "pi_diff_misses_devstep", "pi_recall_gather_scatter",
            "pi_recall_gather_scatter_paged", "pi_sparse_decode_attn", "pi_sparse_decode_attn_headwise", "pi_sparse_decode_attn_resident", "pi_sparse_decode_attn_recalled", "pi_attn_state_bytes", "pi_append_kv", "pi_append_kv_paged", "pi_append_kv_devstep", "pi_build_digests", "pi_build_digests_all", "pi_table_init", "pi_h2d_copy_ms", "pi_empty_launch", "pi_middle_attention_mass",
-           "pi_get_status", "pi_get_stats", "pi_clear_status", "pi_strerror"]
+           "pi_get_status", "pi_get_stats", "pi_clear_status", "pi_strerror",
+           "pi_kv4_block_bytes", "pi_assign_pages", "pi_qk_norm_rope", "pi_kv4_store", "pi_kv4_load", "pi_append_kv4", "pi_recall_kv4",
+           "pi_sparse_decode_attn_kv4"]
+DTYPE_CODES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}      # PI_DTYPE_*
 
 
 class PiConfig(ctypes.Structure):
@@ -85,12 +88,22 @@ def load_library(rebuild: bool = False) -> ctypes.CDLL:
     lib.pi_get_status.argtypes = [c_void_p, POINTER(c_int32 * 8)]
     lib.pi_get_stats.argtypes = [c_void_p, POINTER(c_int64 * 4), c_int]
     lib.pi_clear_status.argtypes = [c_void_p]
+    lib.pi_kv4_block_bytes.argtypes = [c_void_p]
+    lib.pi_assign_pages.argtypes = [c_void_p, c_int, i32p, i32p, i32p, c_int64, i32p, c_int32, vp, i32p, c_int64, vp, i32p, vp]
+    lib.pi_qk_norm_rope.argtypes = [c_void_p, c_int64, c_int, vp, c_int64, vp, c_int64, i32p, vp, vp, c_float, vp, c_int, c_int, vp, vp, vp]
+    lib.pi_kv4_store.argtypes = [c_void_p, c_int64, vp, c_int64, c_int64, c_int64, vp, c_int64, c_int64, c_int64, c_int64, vp, vp, c_int64, vp]
+    lib.pi_kv4_load.argtypes = [c_void_p, c_int64, vp, c_int64, i32p, vp, vp]
+    lib.pi_append_kv4.argtypes = [c_void_p, c_int, c_int, c_uint32, u32p, vp, vp, i32p, vp, c_int64, i32p, c_int64, c_int32, vp, i32p,
+                                  i32p, u32p, vp, vp]
+    lib.pi_recall_kv4.argtypes = [c_void_p, c_int, c_int, vp, c_int64, i32p, c_int64, c_int32, vp, vp, c_int32, i32p, vp]
+    lib.pi_sparse_decode_attn_kv4.argtypes = [c_void_p, c_int, c_int, vp, vp, i32p, i32p, i32p, i32p, vp, vp, vp]
     lib.pi_strerror.argtypes = [c_int]
     lib.pi_strerror.restype = c_char_p
     for name in EXPORTS:
         if name != "pi_strerror":
             getattr(lib, name).restype = c_int
     lib.pi_attn_state_bytes.restype = c_int64
+    lib.pi_kv4_block_bytes.restype = c_int64
     _lib = lib
     return lib
 
@@ -167,6 +180,8 @@ class PulseInfer:
         _check("pi_create", self._lib.pi_create(ctypes.byref(self.cfg), ctypes.byref(self._ctx)))
         self.frag_bytes = block_tokens * head_dim * 2 * 2
         self.block_bytes = self.frag_bytes * n_kv_heads
+        self.kv4_block_bytes = int(self._lib.pi_kv4_block_bytes(self._ctx))       # bytes of one block in 4 bits
+        self.device = torch.device("cuda", torch.cuda.current_device())
 
     @classmethod
     def from_workload(cls, cfg, max_batch: Optional[int] = None, **kw) -> "PulseInfer":
@@ -284,8 +299,8 @@ class PulseInfer:
         """headwise=True: sel_slots / sel_blocks are [batch][Hkv][K] (or [batch*Hkv][K]) and sel_count
         [batch][Hkv]: every KV head attends over its own selection."""
         batch = q.shape[0]
-        if not pool.is_cuda or not pool.is_contiguous():
-            raise TypeError("pool: expected a contiguous CUDA tensor")
+        if not pool.is_cuda or not pool.is_contiguous() or pool.dtype == torch.uint8:
+            raise TypeError("pool: expected a contiguous CUDA tensor of bf16 blocks (4-bit blocks: sparse_decode_attn_kv4)")
         fn = self._lib.pi_sparse_decode_attn_headwise if headwise else self._lib.pi_sparse_decode_attn
         _check("pi_sparse_decode_attn_headwise" if headwise else "pi_sparse_decode_attn", fn(
             self._ctx, layer, batch, _dev(q, torch.bfloat16, "q"), pool.data_ptr(),
@@ -306,8 +321,8 @@ class PulseInfer:
         """First half of the attention split around the recall: the selected blocks the step's recall list
         does not touch; may run beside recall_gather_scatter.  Leaves its softmax state in `state`."""
         batch = q.shape[0]
-        if not pool.is_cuda or not pool.is_contiguous():
-            raise TypeError("pool: expected a contiguous CUDA tensor")
+        if not pool.is_cuda or not pool.is_contiguous() or pool.dtype == torch.uint8:
+            raise TypeError("pool: expected a contiguous CUDA tensor of bf16 blocks (4-bit blocks: sparse_decode_attn_kv4)")
         _check("pi_sparse_decode_attn_resident", self._lib.pi_sparse_decode_attn_resident(
             self._ctx, layer, batch, _dev(q, torch.bfloat16, "q"), pool.data_ptr(),
             _dev(sel_slots, torch.int32, "sel_slots"), _dev(sel_blocks, torch.int32, "sel_blocks"),
@@ -320,8 +335,8 @@ class PulseInfer:
         """Second half: the blocks the recall brought in, merged with `state`; writes `out`.  The caller
         orders it after the first half and after the recall."""
         batch = q.shape[0]
-        if not pool.is_cuda or not pool.is_contiguous():
-            raise TypeError("pool: expected a contiguous CUDA tensor")
+        if not pool.is_cuda or not pool.is_contiguous() or pool.dtype == torch.uint8:
+            raise TypeError("pool: expected a contiguous CUDA tensor of bf16 blocks (4-bit blocks: sparse_decode_attn_kv4)")
         _check("pi_sparse_decode_attn_recalled", self._lib.pi_sparse_decode_attn_recalled(
             self._ctx, layer, batch, _dev(q, torch.bfloat16, "q"), pool.data_ptr(),
             _dev(sel_slots, torch.int32, "sel_slots"), _dev(sel_blocks, torch.int32, "sel_blocks"),
@@ -367,6 +382,183 @@ class PulseInfer:
             _dev(ctx_len, torch.int32, "ctx_len"), host_kv.data_ptr(), hs, pool.data_ptr(),
             _dev(block_table, torch.int32, "block_table"), _dev(slot_block, torch.int32, "slot_block"),
             _dev(slot_stamp, torch.int32, "slot_stamp"), _dev(digest, torch.bfloat16, "digest"), _stream(stream)))
+
+    # ------------------------------------------------------------------ the path on a cache in 4 bits, and what feeds it
+    def _on(self, t, dtype, name: str, shape=None, rows: Optional[int] = None) -> int:
+        """Address of a contiguous tensor of `dtype` on the context's device; shape: exact, rows: at least so many values."""
+        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()):
+            raise TypeError(f"{name}: expected a contiguous CUDA tensor of {dtype}")
+        if t.device != self.device:
+            raise ValueError(f"{name}: on {t.device}, the context is on {self.device}")
+        if shape is not None and tuple(t.shape) != shape:
+            raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+        if rows is not None and t.numel() < rows:
+            raise ValueError(f"{name}: expected at least {rows} values, got {t.numel()}")
+        return t.data_ptr()
+
+    def _stream4(self, stream) -> int:
+        if stream is None:
+            return torch.cuda.current_stream(self.device).cuda_stream
+        return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+    def _blocks4(self, t, name: str, call: str, host: bool = False) -> tuple:
+        """Address and number of 4-bit blocks of a contiguous uint8 tensor [..., kv4_block_bytes] (device; with `host` also pinned)."""
+        if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or not t.is_contiguous() or t.dim() < 2 or t.shape[-1] != self.kv4_block_bytes:
+            raise TypeError(f"{name}: expected a contiguous uint8 tensor [..., {self.kv4_block_bytes}] of 4-bit blocks")
+        if t.is_cuda:
+            if t.device != self.device:
+                raise ValueError(f"{name}: on {t.device}, the context is on {self.device}")
+        elif not host:
+            raise TypeError(f"{name}: expected a CUDA tensor")
+        elif not t.is_pinned():
+            raise PiError(call, -5, strerror(-5))
+        return t.data_ptr(), t.numel() // self.kv4_block_bytes
+
+    def assign_pages(self, old_len, new_len, page_table, free_pages, free_state, token_start=None, slot_map=None, positions=None,
+                     stream=None) -> None:
+        """Takes pages for the sequences that grow from old_len to new_len tokens and gives back those of the sequences that
+        shrink; writes slot and position of every new token (maps of one capacity, -1 behind the last token).
+        page_table: int32 [batch][NB]; free_pages: int32 ring; free_state: int64 [4] (see free_page_ring)."""
+        batch = old_len.shape[0]
+        if page_table.dim() != 2 or page_table.shape[0] < batch:
+            raise ValueError("page_table: expected [batch][blocks]")
+        if slot_map is not None and positions is not None and slot_map.shape[0] != positions.shape[0]:
+            raise ValueError("slot_map and positions have different lengths")
+        n = slot_map.shape[0] if slot_map is not None else positions.shape[0] if positions is not None else 0
+        _check("pi_assign_pages", self._lib.pi_assign_pages(
+            self._ctx, batch, self._on(old_len, torch.int32, "old_len", (batch,)), self._on(new_len, torch.int32, "new_len", (batch,)),
+            self._on(page_table, torch.int32, "page_table"), page_table.shape[1], self._on(free_pages, torch.int32, "free_pages"),
+            free_pages.numel(), self._on(free_state, torch.int64, "free_state", (4,)),
+            None if token_start is None else self._on(token_start, torch.int32, "token_start", (batch + 1,)), n,
+            None if slot_map is None else self._on(slot_map, torch.int64, "slot_map", (n,)),
+            None if positions is None else self._on(positions, torch.int32, "positions", (n,)), self._stream4(stream)))
+
+    def free_page_ring(self, n_pages: int) -> tuple:
+        """(free_pages, free_state) of an arena none of whose pages is taken."""
+        ring = torch.arange(n_pages, dtype=torch.int32, device=self.device)
+        return ring, torch.tensor([0, n_pages, 0, 0], dtype=torch.int64, device=self.device)
+
+    def qk_norm_rope(self, q, k, positions, inv_freq, q_out, k_out, q_weight=None, k_weight=None, eps: float = 1e-6,
+                     interleaved: bool = False, stream=None) -> None:
+        """Per-head RMS norm (when weights are given) and rotation of q [T][Hq][D] and k [T][Hkv][D] (bf16, fp16 or fp32; may be
+        slices of one fused projection) into q_out and k_out (bf16).  inv_freq: float32 [rot_dim / 2] (None: no rotation);
+        tokens with a negative position are padding and leave their output rows alone."""
+        c = self.cfg
+        T = q.shape[0]
+        for t, heads, name in ((q, c.n_q_heads, "q"), (k, c.n_kv_heads, "k")):
+            if not (t.is_cuda and t.dtype in DTYPE_CODES and t.dtype == q.dtype):
+                raise TypeError(f"{name}: expected a CUDA tensor of bfloat16, float16 or float32, both of one type")
+            if t.device != self.device:
+                raise ValueError(f"{name}: on {t.device}, the context is on {self.device}")
+            if t.shape != (T, heads, c.head_dim):
+                raise ValueError(f"{name}: expected shape {(T, heads, c.head_dim)}, got {tuple(t.shape)}")
+            if T and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != c.head_dim)):
+                raise ValueError(f"{name}: the rows of a token must be contiguous")
+        # (the token stride of a single token means nothing, and torch may report any)
+        qs, ks = (q.stride(0), k.stride(0)) if T > 1 else (c.n_q_heads * c.head_dim, c.n_kv_heads * c.head_dim)
+        rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+        _check("pi_qk_norm_rope", self._lib.pi_qk_norm_rope(
+            self._ctx, T, DTYPE_CODES[q.dtype], q.data_ptr(), qs, k.data_ptr(), ks, self._on(positions, torch.int32, "positions", (T,)),
+            None if q_weight is None else self._on(q_weight, torch.float32, "q_weight", (c.head_dim,)),
+            None if k_weight is None else self._on(k_weight, torch.float32, "k_weight", (c.head_dim,)), eps,
+            None if inv_freq is None else self._on(inv_freq, torch.float32, "inv_freq"), rot, int(interleaved),
+            self._on(q_out, torch.bfloat16, "q_out", (T, c.n_q_heads, c.head_dim)),
+            self._on(k_out, torch.bfloat16, "k_out", (T, c.n_kv_heads, c.head_dim)), self._stream4(stream)))
+
+    def kv4_store(self, k, v, store, slot_map=None, stream=None) -> None:
+        """Rounds the tokens k, v (bf16 [T][Hkv][D], or [N][M][Hkv][D] for N runs of M tokens; any strides with contiguous rows)
+        to 4 bits and writes token t to slot slot_map[t] (int64; None: t) of `store` (uint8 [..., kv4_block_bytes], device or
+        pinned).  Negative slots are skipped."""
+        c = self.cfg
+        runs = k.dim() == 4
+        for t, name in ((k, "k"), (v, "v")):
+            if not (t.is_cuda and t.dtype == torch.bfloat16):
+                raise TypeError(f"{name}: expected a CUDA tensor of torch.bfloat16")
+            if t.device != self.device:
+                raise ValueError(f"{name}: on {t.device}, the context is on {self.device}")
+            if t.dim() not in (3, 4) or t.shape != k.shape or tuple(t.shape[-2:]) != (c.n_kv_heads, c.head_dim):
+                raise ValueError(f"{name}: expected [tokens][{c.n_kv_heads}][{c.head_dim}] or [runs][tokens][{c.n_kv_heads}][{c.head_dim}], k and v alike")
+            if t.numel() and t.stride(-1) != 1:
+                raise ValueError(f"{name}: rows must be contiguous")
+        n = k.shape[0] * k.shape[1] if runs else k.shape[0]
+
+        def strides(t):       # {token, head, run}; of an axis of one entry the stride means nothing, and torch may report any
+            one = [0 if size <= 1 else st for size, st in zip(t.shape, t.stride())]
+            return one[-3], one[-2], one[0] if runs else 0
+
+        ptr, blocks = self._blocks4(store, "store", "pi_kv4_store", host=True)
+        _check("pi_kv4_store", self._lib.pi_kv4_store(
+            self._ctx, n, k.data_ptr(), *strides(k), v.data_ptr(), *strides(v), k.shape[1] if runs else 0,
+            None if slot_map is None else self._on(slot_map, torch.int64, "slot_map", (n,)), ptr, blocks, self._stream4(stream)))
+
+    def kv4_load(self, store, out, blocks=None, stream=None) -> None:
+        """Block blocks[i] (int32; None: i) of `store` as bf16 into out [n][Hkv][2][B][D]."""
+        c = self.cfg
+        n = out.shape[0] if blocks is None else blocks.numel()
+        ptr, held = self._blocks4(store, "store", "pi_kv4_load", host=True)
+        _check("pi_kv4_load", self._lib.pi_kv4_load(
+            self._ctx, n, ptr, held, None if blocks is None else self._on(blocks, torch.int32, "blocks"),
+            self._on(out, torch.bfloat16, "out", (n, c.n_kv_heads, 2, c.block_tokens, c.head_dim)), self._stream4(stream)))
+
+    def _store4(self, host_kv4, page_table, batch: int, call: str) -> tuple:
+        """(address, sequence stride, page table, its stride, pages) of a block-major or paged 4-bit store."""
+        ptr, blocks = self._blocks4(host_kv4, "host_kv4", call, host=True)
+        if page_table is not None:
+            if page_table.dim() != 2 or page_table.shape[0] < batch:
+                raise ValueError("page_table: expected [batch][blocks]")
+            return ptr, 0, self._on(page_table, torch.int32, "page_table"), page_table.shape[1], blocks
+        if blocks < batch * self.cfg.max_blocks:
+            raise ValueError(f"host_kv4: expected [batch][{self.cfg.max_blocks}] blocks")
+        return ptr, self.cfg.max_blocks * self.kv4_block_bytes, None, 0, 0
+
+    def _tables4(self, batch: int, block_table, slot_block, slot_stamp, digest) -> tuple:
+        c = self.cfg
+        return (self._on(block_table, torch.int32, "block_table", rows=batch * c.max_blocks),
+                self._on(slot_block, torch.int32, "slot_block", rows=batch * c.pool_slots),
+                self._on(slot_stamp, torch.int32, "slot_stamp", rows=batch * c.pool_slots),
+                self._on(digest, torch.bfloat16, "digest", rows=batch * c.max_blocks * 2 * c.head_dim))
+
+    def _pool4(self, pool4, batch: int, call: str) -> int:
+        ptr, blocks = self._blocks4(pool4, "pool4", call)
+        if blocks < batch * self.cfg.pool_slots:
+            raise ValueError(f"pool4: expected [batch][{self.cfg.pool_slots}] blocks")
+        return ptr
+
+    def append_kv4(self, layer: int, step, k_new, v_new, ctx_len, host_kv4, pool4, block_table, slot_block, slot_stamp, digest,
+                   page_table=None, stream=None) -> None:
+        """append_kv for a pool and a host store in 4 bits.  step: a positive int, or a one-element int32 CUDA tensor."""
+        c = self.cfg
+        batch = ctx_len.shape[0]
+        shape = (batch, c.n_kv_heads, c.head_dim)
+        dev_step = isinstance(step, torch.Tensor)
+        _check("pi_append_kv4", self._lib.pi_append_kv4(
+            self._ctx, layer, batch, 0 if dev_step else step, self._on(step, torch.int32, "step", rows=1) if dev_step else None,
+            self._on(k_new, torch.bfloat16, "k_new", shape), self._on(v_new, torch.bfloat16, "v_new", shape),
+            self._on(ctx_len, torch.int32, "ctx_len"), *self._store4(host_kv4, page_table, batch, "pi_append_kv4"),
+            self._pool4(pool4, batch, "pi_append_kv4"), *self._tables4(batch, block_table, slot_block, slot_stamp, digest),
+            self._stream4(stream)))
+
+    def recall_kv4(self, layer: int, host_kv4, pool4, recall_list, recall_count, page_table=None, stream=None) -> None:
+        """recall_gather_scatter with a 4-bit block as the unit."""
+        batch = recall_count.shape[0]
+        if recall_list.dim() != 3 or recall_list.shape[0] != batch or recall_list.shape[2] != 4:
+            raise ValueError("recall_list: expected [batch][capacity][4]")
+        _check("pi_recall_kv4", self._lib.pi_recall_kv4(
+            self._ctx, layer, batch, *self._store4(host_kv4, page_table, batch, "pi_recall_kv4"), self._pool4(pool4, batch, "pi_recall_kv4"),
+            self._on(recall_list, EXTENT_DTYPE, "recall_list"), recall_list.shape[1], self._on(recall_count, torch.int32, "recall_count"),
+            self._stream4(stream)))
+
+    def sparse_decode_attn_kv4(self, layer: int, q, pool4, sel_slots, sel_blocks, sel_count, ctx_len, out, lse=None, stream=None) -> None:
+        """sparse_decode_attn over a pool of 4-bit blocks (uint8 [batch][C][kv4_block_bytes])."""
+        c = self.cfg
+        batch = q.shape[0]
+        shape, lists = (batch, c.n_q_heads, c.head_dim), (batch, c.budget_blocks)
+        _check("pi_sparse_decode_attn_kv4", self._lib.pi_sparse_decode_attn_kv4(
+            self._ctx, layer, batch, self._on(q, torch.bfloat16, "q", shape), self._pool4(pool4, batch, "pi_sparse_decode_attn_kv4"),
+            self._on(sel_slots, torch.int32, "sel_slots", lists), self._on(sel_blocks, torch.int32, "sel_blocks", lists),
+            self._on(sel_count, torch.int32, "sel_count", (batch,)), self._on(ctx_len, torch.int32, "ctx_len", (batch,)),
+            self._on(out, torch.bfloat16, "out", shape),
+            None if lse is None else self._on(lse, torch.float32, "lse", (batch, c.n_q_heads)), self._stream4(stream)))
 
     # ------------------------------------------------------------------ helpers
     def build_digests(self, layer: int, kv, ctx_len, digest, kv_seq_stride: Optional[int] = None, stream=None) -> None:

@@ -15,7 +15,7 @@ INCLUDE = PKG.parent / "include"
 LIB = PKG / "libpulseinfer_b200.so"
 
 SOURCES = ["pi_api.cu", "pi_score_select.cu", "pi_select_diff.cu", "pi_diff_misses.cu", "pi_recall.cu", "pi_attn.cu", "pi_attn_headmajor.cu",
-           "pi_helpers.cu", "pi_append.cu"]
+           "pi_helpers.cu", "pi_append.cu", "pi_api_kv4.cu", "pi_kv4.cu", "pi_rope.cu", "pi_pages.cu", "pi_attn_kv4.cu"]
 
 
 def sources() -> list[Path]:

@@ -253,6 +253,7 @@ static int recall_call(pi_ctx* ctx, int layer, int n_lists, int lists_per_seq, c
     return pi_launch_recall(ctx, n_lists, lists_per_seq, src, host_seq_stride_bytes, pool_dev,
                             pool_seq_stride_bytes, recall_list_dev, list_capacity, recall_count_dev,
                             unit_bytes, unit_stride_bytes, list_offset_bytes, page_table, page_stride, n_pages,
+                            static_cast<int64_t>(ctx->cfg.n_kv_heads) * ctx->cfg.block_tokens * PI_HEAD_DIM * 4,
                             static_cast<cudaStream_t>(stream));
 }
 
@@ -387,7 +388,7 @@ static int append_call(pi_ctx* ctx, int layer, int batch, uint32_t step, const u
     }
     return pi_launch_append(ctx, ctx->solo_head[layer], batch, step, k_new_dev, v_new_dev, ctx_len_dev, dst,
                             host_seq_stride_bytes, pool_dev, block_table_dev, slot_block_dev, slot_stamp_dev,
-                            digest_dev, page_table, page_stride, n_pages, step_dev, static_cast<cudaStream_t>(stream));
+                            digest_dev, page_table, page_stride, n_pages, step_dev, 0, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" int pi_append_kv(pi_ctx* ctx, int layer, int batch, uint32_t step, const void* k_new_dev,

@@ -2,7 +2,7 @@
 // and, through the mapped pinned pointer, into the host store; running min / max of the
 // retrieval head's digest; a pool slot for a block that has just been opened.  One CTA per
 // sequence; a few KB per sequence, latency-bound.
-#include "pi_common.cuh"
+#include "pi_kv4.cuh"
 
 namespace {
 
@@ -26,9 +26,13 @@ struct AppendParams {
     int n_pages;
     const uint32_t* step_dev;      // when set, the stamp is read from device memory (graph replay)
     uint32_t step;
+    long long block_bytes;
     int B, Hkv, C, n_sink, n_local, max_blocks, h_star;
 };
 
+// KV4: pool and store hold blocks in 4 bits; the token's rows are rounded on their way there (the digest takes the
+// key as it came).
+template <bool KV4>
 __global__ void __launch_bounds__(APPEND_THREADS)
 append_kernel(AppendParams p) {
     __shared__ unsigned long long warp_min[APPEND_WARPS];
@@ -46,7 +50,7 @@ append_kernel(AppendParams p) {
     int32_t* table = p.table + static_cast<size_t>(seq) * p.max_blocks;
     int32_t* slot_block = p.slot_block + static_cast<size_t>(seq) * p.C;
     uint32_t* slot_stamp = p.slot_stamp + static_cast<size_t>(seq) * p.C;
-    const long long block_bytes = static_cast<long long>(p.Hkv) * 2 * p.B * PI_HEAD_DIM * 2;
+    const long long block_bytes = p.block_bytes;
     int slot = table[b];
     long long host_off = seq * p.host_stride + b * block_bytes;
     if (p.page) {
@@ -108,6 +112,18 @@ append_kernel(AppendParams p) {
         __syncthreads();                                   // zeros land before the rows below
     }
     if (tid == 0) slot_stamp[slot] = p.step_dev ? *p.step_dev : p.step;
+    if (KV4) {
+        // half a warp a row: the K row of a head in lanes 0..15, its V row in lanes 16..31
+        const bool is_v = lane >> 4;
+        const int l = lane & 15;
+        for (int h = warp; h < p.Hkv; h += APPEND_WARPS) {
+            uint32_t codes, sz;
+            kv4_quantise((is_v ? p.v_new : p.k_new)[(static_cast<size_t>(seq) * p.Hkv + h) * 16 + l], codes, sz);
+            const long long off = (static_cast<long long>(h) * (p.B >> 4) + (t >> 4)) * KV4_TILE_BYTES;
+            kv4_write_row(pool_blk + off, t & 15, is_v, l, codes, sz, true);
+            kv4_write_row(host_blk + off, t & 15, is_v, l, codes, sz, true);
+        }
+    } else
     // rows: [Hkv][2][B][D]; one head row is 256 B = 16 uint4
     for (int i = tid; i < p.Hkv * 32; i += APPEND_THREADS) {
         const int h = i >> 5, kv = (i >> 4) & 1, c = i & 15;
@@ -134,7 +150,7 @@ append_kernel(AppendParams p) {
 int pi_launch_append(pi_ctx* c, int h_star, int batch, uint32_t step, const void* k_new, const void* v_new,
                      const int32_t* ctx_len, void* host_kv, int64_t host_stride, void* pool, int32_t* table,
                      int32_t* slot_block, uint32_t* slot_stamp, void* digest, const int32_t* page_table,
-                     int64_t page_stride, int32_t n_pages, const uint32_t* step_dev, cudaStream_t stream) {
+                     int64_t page_stride, int32_t n_pages, const uint32_t* step_dev, int kv4, cudaStream_t stream) {
     AppendParams p;
     p.step_dev = step_dev;
     p.page = page_table; p.page_stride = page_stride; p.n_pages = n_pages;
@@ -147,12 +163,14 @@ int pi_launch_append(pi_ctx* c, int h_star, int batch, uint32_t step, const void
     p.digest = static_cast<__nv_bfloat16*>(digest);
     p.st = pi_status_of(c);
     p.host_stride = host_stride;
-    p.pool_stride = static_cast<long long>(c->cfg.pool_slots) * c->cfg.n_kv_heads * 2 * c->cfg.block_tokens * PI_HEAD_DIM * 2;
+    p.block_bytes = kv4 ? kv4_block_bytes(c->cfg.n_kv_heads, c->cfg.block_tokens)
+                        : static_cast<long long>(c->cfg.n_kv_heads) * 2 * c->cfg.block_tokens * PI_HEAD_DIM * 2;
+    p.pool_stride = c->cfg.pool_slots * p.block_bytes;
     p.step = step;
     p.B = c->cfg.block_tokens; p.Hkv = c->cfg.n_kv_heads; p.C = c->cfg.pool_slots;
     p.n_sink = c->cfg.n_sink_blocks; p.n_local = c->cfg.n_local_blocks; p.max_blocks = c->cfg.max_blocks;
     p.h_star = h_star;
-    PI_CUDA_TRY(pi_launch_pdl(append_kernel, dim3(batch), dim3(APPEND_THREADS), 0, stream, p));
+    PI_CUDA_TRY(pi_launch_pdl(kv4 ? append_kernel<true> : append_kernel<false>, dim3(batch), dim3(APPEND_THREADS), 0, stream, p));
     PI_CUDA_TRY(cudaGetLastError());
     return PI_OK;
 }

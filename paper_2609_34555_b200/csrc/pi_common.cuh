@@ -13,6 +13,8 @@
 #define PI_STAGE_RECALL 3
 #define PI_STAGE_ATTN   4
 #define PI_STAGE_APPEND 5
+#define PI_STAGE_KV4    6
+#define PI_STAGE_PAGES  7
 
 // Programmatic dependent launch.  Every kernel of the path is launched with programmatic stream
 // serialization: its grid may be scheduled while the kernel before it in the stream is still
@@ -137,7 +139,7 @@ int pi_launch_diff(pi_ctx*, int batch, uint32_t step, const uint32_t* step_dev, 
 int pi_launch_recall(pi_ctx*, int n_lists, int lists_per_seq, const void* host_kv, int64_t host_stride,
                      void* pool, int64_t pool_stride, const pi_extent* list, int32_t cap,
                      const int32_t* count, int64_t unit_bytes, int64_t unit_stride, int64_t list_offset,
-                     const int32_t* page_table, int64_t page_stride, int32_t n_pages, cudaStream_t);
+                     const int32_t* page_table, int64_t page_stride, int32_t n_pages, int64_t block_bytes, cudaStream_t);
 int pi_launch_attn(pi_ctx*, int batch, const void* q, const void* pool, const int32_t* sel_slots,
                    const int32_t* sel_blocks, const int32_t* sel_count, const int32_t* ctx_len,
                    void* out, float* lse, int headwise, cudaStream_t);
@@ -161,10 +163,22 @@ int pi_launch_attn_headmajor(pi_ctx*, int batch, const void* q, const void* pool
 int pi_launch_append(pi_ctx*, int h_star, int batch, uint32_t step, const void* k_new, const void* v_new,
                      const int32_t* ctx_len, void* host_kv, int64_t host_stride, void* pool, int32_t* table,
                      int32_t* slot_block, uint32_t* slot_stamp, void* digest, const int32_t* page_table,
-                     int64_t page_stride, int32_t n_pages, const uint32_t* step_dev, cudaStream_t);
+                     int64_t page_stride, int32_t n_pages, const uint32_t* step_dev, int kv4, cudaStream_t);
 int pi_launch_build_digests_all(pi_ctx*, int batch, const void* kv, int64_t stride, const int32_t* ctx_len,
                                 void* digest_all, cudaStream_t);
 int pi_launch_build_digests(pi_ctx*, int h_star, int batch, const void* kv, int64_t stride,
                             const int32_t* ctx_len, void* digest, cudaStream_t);
 int pi_launch_table_init(pi_ctx*, int batch, const int32_t* resident, int32_t* table,
                          int32_t* slot_block, uint32_t* slot_stamp, cudaStream_t);
+int pi_launch_assign_pages(pi_ctx*, int batch, const int32_t* old_len, const int32_t* new_len, int32_t* table, int64_t row_stride,
+                           int32_t n_pages, int32_t* ring, int64_t* state, int32_t* starts, int64_t n_tokens, int64_t* slots,
+                           int32_t* positions, cudaStream_t);
+int pi_launch_qk_norm_rope(pi_ctx*, int n_tokens, int dtype, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                           const int32_t* pos, const float* wq, const float* wk, float eps, const float* inv_freq, int rot_dim,
+                           int interleaved, void* q_out, void* k_out, cudaStream_t);
+// strides of k and v in elements: {token, head, outer}; inner > 0: token t is row t % inner of the outer index t / inner
+int pi_launch_kv4_store(pi_ctx*, int64_t n_tokens, const void* k, const int64_t (&k_strides)[3], const void* v,
+                        const int64_t (&v_strides)[3], int inner, const int64_t* slots, void* store, int64_t n_blocks, cudaStream_t);
+int pi_launch_kv4_load(pi_ctx*, int64_t n_out, const void* store, int64_t n_blocks, const int32_t* blocks, void* out, cudaStream_t);
+int pi_launch_attn_kv4(pi_ctx*, int batch, const void* q, const void* pool, const int32_t* sel_slots, const int32_t* sel_blocks,
+                       const int32_t* sel_count, const int32_t* ctx_len, void* out, float* lse, cudaStream_t);

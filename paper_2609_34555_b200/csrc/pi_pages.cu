@@ -1,0 +1,215 @@
+// Page tables and slot maps from request lengths: pages taken for the sequences that grow, given back for those that
+// shrink, and the slot and position of every new token, in one launch.
+//
+// The free pages are a ring: pages are taken at `head` and given back at `tail` (both counted up without end), so one
+// call can do both without the two meeting.  Which page a sequence gets follows from an exclusive scan of the growth
+// over the sequences, which every CTA computes for itself in shared memory (at most 4096 sequences, 32 KB out of L2):
+// no CTA waits for another, and a token's page is read from the ring directly rather than from the table row that
+// another CTA may still be writing.  The ring's counters move once, by whichever CTA finishes last (a ticket beside
+// them), when every CTA has read them.  Writes 12 bytes a token and 4 a page: bound by HBM for prompts, by latency for
+// decode steps.
+#include "pi_common.cuh"
+
+namespace {
+
+constexpr int PAGES_THREADS = 256;
+constexpr int PAGES_WARPS = PAGES_THREADS / 32;
+
+struct PagesParams {
+    const int32_t* old_len;
+    const int32_t* new_len;
+    int32_t* table;
+    int32_t* ring;
+    long long* state;              // head, tail, ticket, unused
+    int32_t* starts;
+    int64_t* slots;
+    int32_t* positions;
+    pi_status_ref st;
+    long long row_stride, n_tokens;
+    int batch, n_pages, row_limit, shift;
+};
+
+// Block-wide exclusive scan, continued from `run`; all threads call.
+__device__ __forceinline__ long long scan_from(long long v, long long* warp_tot, long long& run) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    long long inc = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long t = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += t;
+    }
+    __syncthreads();
+    if (lane == 31) warp_tot[warp] = inc;
+    __syncthreads();
+    long long base = run, tot = 0;
+#pragma unroll
+    for (int i = 0; i < PAGES_WARPS; ++i) {
+        if (i < warp) base += warp_tot[i];
+        tot += warp_tot[i];
+    }
+    run += tot;
+    return base + inc - v;
+}
+
+// Last s with pref[s] <= i, for an ascending pref[0 .. n] with pref[0] = 0 and i < pref[n].
+__device__ __forceinline__ int owner_of(const int* pref, int n, int i) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (pref[mid] <= i) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+__global__ void __launch_bounds__(PAGES_THREADS)
+assign_pages_kernel(PagesParams p) {
+    extern __shared__ int s_dyn[];
+    int* s_old = s_dyn;                                  // [batch]
+    int* s_tok = s_old + p.batch;                        // [batch + 1] new tokens before each sequence
+    int* s_grow = s_tok + p.batch + 1;                   // [batch + 1] pages taken before it
+    int* s_shrink = s_grow + p.batch + 1;                // [batch + 1] pages given back before it
+    __shared__ long long warp_tot[PAGES_WARPS];
+    __shared__ int s_bad;
+    const int tid = threadIdx.x, B = 1 << p.shift;
+    if (tid == 0) s_bad = -1;
+    pi_grid_dependency_wait();
+    pi_launch_dependents();
+    const long long head = *reinterpret_cast<volatile long long*>(p.state), tail = *reinterpret_cast<volatile long long*>(p.state + 1);
+    long long tokens = 0, grown = 0, shrunk = 0;
+    for (int s0 = 0; s0 < p.batch; s0 += PAGES_THREADS) {
+        const int s = s0 + tid;
+        int add = 0, g = 0, r = 0, o = 0;
+        bool bad = false;
+        if (s < p.batch) {
+            o = p.old_len[s];
+            const int n = p.new_len[s];
+            bad = o < 0 || n < 0 || ((static_cast<long long>(max(o, n)) + B - 1) >> p.shift) > p.row_limit;
+            if (!bad) {
+                const int ob = static_cast<int>((static_cast<long long>(o) + B - 1) >> p.shift), nb = static_cast<int>((static_cast<long long>(n) + B - 1) >> p.shift);
+                add = max(n - o, 0); g = max(nb - ob, 0); r = max(ob - nb, 0);
+            }
+        }
+        const long long t0 = scan_from(add, warp_tot, tokens), g0 = scan_from(g, warp_tot, grown), r0 = scan_from(r, warp_tot, shrunk);
+        if (s < p.batch) {
+            if (bad) atomicMax(&s_bad, s);
+            s_old[s] = o;
+            // (a total beyond 32 bits is refused below, before these are used)
+            s_tok[s] = static_cast<int>(t0); s_grow[s] = static_cast<int>(g0); s_shrink[s] = static_cast<int>(r0);
+        }
+    }
+    if (tid == 0) { s_tok[p.batch] = static_cast<int>(tokens); s_grow[p.batch] = static_cast<int>(grown); s_shrink[p.batch] = static_cast<int>(shrunk); }
+    __syncthreads();
+
+    // all or nothing: every CTA comes to the same verdict
+    const long long room = tail - head;
+    int code = PI_OK, ca = 0, cb = 0, cc = 0;
+    if (s_bad >= 0) { code = PI_ERR_INDEX_RANGE; ca = s_bad; cb = p.old_len[s_bad]; cc = p.new_len[s_bad]; }
+    else if (head < 0 || room < 0 || room > p.n_pages) { code = PI_ERR_INDEX_RANGE; ca = -1; cb = static_cast<int>(head); cc = static_cast<int>(tail); }
+    else if (grown > room) { code = PI_ERR_POOL_TOO_SMALL; ca = -1; cb = static_cast<int>(min(grown, 0x7fffffffLL)); cc = static_cast<int>(room); }
+    else if (room + shrunk > p.n_pages) { code = PI_ERR_CAPACITY; ca = -1; cb = static_cast<int>(min(shrunk, 0x7fffffffLL)); cc = p.n_pages; }
+    else if (tokens > 0x7fffffffLL || ((p.slots || p.positions) && tokens > p.n_tokens)) { code = PI_ERR_CAPACITY; ca = -2; cb = static_cast<int>(min(tokens, 0x7fffffffLL)); cc = static_cast<int>(min(p.n_tokens, 0x7fffffffLL)); }
+    const bool ok = code == PI_OK;
+    if (!ok) {
+        if (blockIdx.x == 0 && tid == 0) pi_report(p.st, code, PI_STAGE_PAGES, ca, cb, cc);
+        tokens = 0; grown = 0; shrunk = 0;
+    }
+    const long long me = static_cast<long long>(blockIdx.x) * PAGES_THREADS + tid, all = static_cast<long long>(gridDim.x) * PAGES_THREADS;
+    if (p.starts)
+        for (long long s = me; s <= p.batch; s += all) p.starts[s] = ok ? s_tok[s] : 0;
+
+    // place of the i-th page from a counter in the ring (i <= n_pages): one division per call, none per page
+    const unsigned n = static_cast<unsigned>(p.n_pages);
+    const unsigned head_at = ok ? static_cast<unsigned>(head % p.n_pages) : 0u, tail_at = ok ? static_cast<unsigned>(tail % p.n_pages) : 0u;
+    auto ring_at = [&](unsigned from, long long i) { const unsigned x = from + static_cast<unsigned>(i); return x < n ? x : x - n; };
+    // pages taken
+    for (long long i = me; i < grown; i += all) {
+        const int s = owner_of(s_grow, p.batch, static_cast<int>(i));
+        const int ob = (s_old[s] + B - 1) >> p.shift;
+        int pg = p.ring[ring_at(head_at, i)];
+        if (pg < 0 || pg >= p.n_pages) { pi_report(p.st, PI_ERR_INDEX_RANGE, PI_STAGE_PAGES, s, static_cast<int>(i), pg); pg = -1; }
+        p.table[s * p.row_stride + ob + (i - s_grow[s])] = pg;
+    }
+    // pages given back
+    for (long long i = me; i < shrunk; i += all) {
+        const int s = owner_of(s_shrink, p.batch, static_cast<int>(i));
+        const int keep = ((s_old[s] + B - 1) >> p.shift) - (s_shrink[s + 1] - s_shrink[s]);
+        int32_t* e = p.table + s * p.row_stride + keep + (i - s_shrink[s]);
+        const int pg = *e;
+        if (pg < 0 || pg >= p.n_pages) pi_report(p.st, PI_ERR_INDEX_RANGE, PI_STAGE_PAGES, s, static_cast<int>(i), pg);
+        p.ring[ring_at(tail_at, i)] = pg;
+        *e = -1;
+    }
+    // slot and position of every new token; four consecutive tokens a thread
+    if (p.slots || p.positions) {
+        for (long long t0 = me * 4; t0 < p.n_tokens; t0 += all * 4) {
+            int64_t slot[4];
+            int32_t pos[4];
+            int s = t0 < tokens ? owner_of(s_tok, p.batch, static_cast<int>(t0)) : p.batch;
+            int block = -1, pg = -1;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const long long t = t0 + u;
+                slot[u] = -1; pos[u] = -1;
+                if (t >= tokens) continue;
+                while (t >= s_tok[s + 1]) { ++s; block = -1; }
+                const int at = s_old[s] + static_cast<int>(t - s_tok[s]);
+                pos[u] = at;
+                if ((at >> p.shift) != block) {
+                    block = at >> p.shift;
+                    const int ob = (s_old[s] + B - 1) >> p.shift;
+                    pg = block < ob ? p.table[s * p.row_stride + block] : p.ring[ring_at(head_at, s_grow[s] + (block - ob))];
+                }
+                if (pg >= 0 && pg < p.n_pages) slot[u] = (static_cast<int64_t>(pg) << p.shift) + (at & (B - 1));
+                else pi_report(p.st, PI_ERR_INDEX_RANGE, PI_STAGE_PAGES, s, at, pg);
+            }
+            if (t0 + 4 <= p.n_tokens) {
+                if (p.slots) {
+                    reinterpret_cast<longlong2*>(p.slots + t0)[0] = make_longlong2(slot[0], slot[1]);
+                    reinterpret_cast<longlong2*>(p.slots + t0)[1] = make_longlong2(slot[2], slot[3]);
+                }
+                if (p.positions) *reinterpret_cast<int4*>(p.positions + t0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+            } else {
+                for (int u = 0; u < 4 && t0 + u < p.n_tokens; ++u) {
+                    if (p.slots) p.slots[t0 + u] = slot[u];
+                    if (p.positions) p.positions[t0 + u] = pos[u];
+                }
+            }
+        }
+    }
+    // the last CTA moves the ring's counters: by then every CTA has read them
+    __syncthreads();
+    if (tid == 0) {
+        __threadfence();
+        const unsigned long long v = atomicAdd(reinterpret_cast<unsigned long long*>(p.state + 2), 1ull);
+        if (v >= gridDim.x) pi_report(p.st, PI_ERR_INDEX_RANGE, PI_STAGE_PAGES, -3, static_cast<int>(v), static_cast<int>(gridDim.x));
+        else if (v == gridDim.x - 1) {
+            p.state[0] = head + grown;
+            p.state[1] = tail + shrunk;
+            p.state[2] = 0;
+        }
+    }
+}
+
+}  // namespace
+
+int pi_launch_assign_pages(pi_ctx* c, int batch, const int32_t* old_len, const int32_t* new_len, int32_t* table, int64_t row_stride,
+                           int32_t n_pages, int32_t* ring, int64_t* state, int32_t* starts, int64_t n_tokens, int64_t* slots,
+                           int32_t* positions, cudaStream_t stream) {
+    PagesParams p;
+    p.old_len = old_len; p.new_len = new_len; p.table = table; p.ring = ring;
+    p.state = reinterpret_cast<long long*>(state);
+    p.starts = starts; p.slots = slots; p.positions = positions;
+    p.st = pi_status_of(c);
+    p.row_stride = row_stride; p.n_tokens = n_tokens;
+    p.batch = batch; p.n_pages = n_pages;
+    p.row_limit = static_cast<int>(row_stride < c->cfg.max_blocks ? row_stride : c->cfg.max_blocks);
+    p.shift = c->cfg.block_tokens == 16 ? 4 : c->cfg.block_tokens == 32 ? 5 : 6;
+    // enough CTAs for the token maps (four tokens a thread) and for a batch whose rows all change, at most two per SM
+    const long long work = (n_tokens + 3) / 4 > static_cast<long long>(batch) * p.row_limit / 8 ? (n_tokens + 3) / 4 : static_cast<long long>(batch) * p.row_limit / 8;
+    long long grid = (work + PAGES_THREADS - 1) / PAGES_THREADS;
+    grid = grid < 1 ? 1 : grid > 2ll * c->n_sms ? 2ll * c->n_sms : grid;
+    const size_t smem = (4 * static_cast<size_t>(batch) + 3) * sizeof(int);
+    if (smem > 40 * 1024) PI_CUDA_TRY(cudaFuncSetAttribute(assign_pages_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    PI_CUDA_TRY(pi_launch_pdl(assign_pages_kernel, dim3(static_cast<unsigned>(grid)), dim3(PAGES_THREADS), smem, stream, p));
+    return PI_OK;
+}

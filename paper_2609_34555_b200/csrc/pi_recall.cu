@@ -225,7 +225,7 @@ recall_kernel(RecallParams p) {
 int pi_launch_recall(pi_ctx* c, int n_lists, int lists_per_seq, const void* host_kv, int64_t host_stride,
                      void* pool, int64_t pool_stride, const pi_extent* list, int32_t cap,
                      const int32_t* count, int64_t unit_bytes, int64_t unit_stride, int64_t list_offset,
-                     const int32_t* page_table, int64_t page_stride, int32_t n_pages, cudaStream_t stream) {
+                     const int32_t* page_table, int64_t page_stride, int32_t n_pages, int64_t block_bytes, cudaStream_t stream) {
     RecallParams p;
     p.page = page_table; p.page_stride = page_stride; p.n_pages = n_pages;
     p.host = static_cast<const unsigned char*>(host_kv);
@@ -237,7 +237,6 @@ int pi_launch_recall(pi_ctx* c, int n_lists, int lists_per_seq, const void* host
     p.list_offset = list_offset;
     p.n_lists = n_lists; p.lists_per_seq = lists_per_seq; p.cap = cap;
     // capacities of one sequence's regions in units (pool: C blocks, host: NB blocks of block_bytes)
-    const long long block_bytes = static_cast<long long>(c->cfg.n_kv_heads) * c->cfg.block_tokens * PI_HEAD_DIM * 4;
     p.pool_units = static_cast<long long>(c->cfg.pool_slots) * block_bytes / p.unit_stride;
     p.host_units = static_cast<long long>(c->cfg.max_blocks) * block_bytes / p.unit_stride;
     // shared memory: two prefix arrays over the lists + the extent cache

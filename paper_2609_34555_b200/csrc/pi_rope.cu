@@ -1,0 +1,210 @@
+// Norm of every query and key head and the position rotation, from the projections to the tensors the path takes.
+//
+//   y = x * rsqrt(mean(x^2) + eps) * w          (no weights given: y = x)
+//   (y_a, y_b) -> (y_a cos - y_b sin, y_b cos + y_a sin)   for the pairs of the first rot_dim channels, at the angle
+//   position * inv_freq[pair]; one rounding, to bf16, at the end.
+//
+// Streams each row once; bound by HBM from a few thousand tokens on, by latency below.  A warp works on one token, four
+// rows at a time: eight lanes a row, 16 channels a lane (two runs of 8, 64 channels apart, so that both members of a
+// pair are in one lane for the usual pairing i / i + 64 and for neighbouring pairs alike).  The token's angles are
+// taken once per warp, two per lane, and shared through shared memory: the product position * inv_freq in 64 bits
+// (32 lose a far position's angle: at 131072 radians their spacing is 2^-7), reduced to a fraction of a turn there,
+// the sine and cosine of the rest in 32.
+#include <cuda_fp16.h>
+
+#include "pi_common.cuh"
+
+namespace {
+
+constexpr int ROPE_THREADS = 128;
+constexpr int ROPE_WARPS = ROPE_THREADS / 32;
+
+struct RopeParams {
+    const void* q;
+    const void* k;
+    long long q_stride, k_stride;                  // elements between tokens
+    const int32_t* pos;
+    const float* wq;
+    const float* wk;
+    const float* inv_freq;
+    __nv_bfloat16* q_out;
+    __nv_bfloat16* k_out;
+    float eps;
+    int n_tokens, Hq, Hkv, half, parts;            // half = rot_dim / 2; parts = warps a token is cut into
+};
+
+template <typename T> struct Raw;                  // eight values as they are loaded
+template <> struct Raw<__nv_bfloat16> { uint4 a; };
+template <> struct Raw<__half> { uint4 a; };
+template <> struct Raw<float> { uint4 a, b; };
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, Raw<T>& r) {
+    r.a = reinterpret_cast<const uint4*>(p)[0];
+    if constexpr (sizeof(T) == 4) r.b = reinterpret_cast<const uint4*>(p)[1];
+}
+template <typename T>
+__device__ __forceinline__ void widen8(const Raw<T>& r, float* f) {
+    const uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            const uint32_t w2[4] = {r.b.x, r.b.y, r.b.z, r.b.w};
+            f[i] = __uint_as_float(w[i]);
+            f[4 + i] = __uint_as_float(w2[i]);
+        } else if constexpr (std::is_same<T, __half>::value) {
+            const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+            f[2 * i] = v.x; f[2 * i + 1] = v.y;
+        } else {
+            f[2 * i] = __uint_as_float(w[i] << 16);
+            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+}
+__device__ __forceinline__ uint4 narrow8(const float* f) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+enum { PAIR_HALVES_FULL = 0, PAIR_NEIGHBOURS = 1, PAIR_HALVES_PART = 2 };
+
+template <typename T, int PAIR>
+__global__ void __launch_bounds__(ROPE_THREADS)
+qk_norm_rope_kernel(RopeParams p) {
+    __shared__ float2 s_cs[ROPE_WARPS][64];                                    // cos, sin of the token's angles
+    __shared__ float s_row[PAIR == PAIR_HALVES_PART ? ROPE_WARPS : 1][4][128];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane >> 3, l = lane & 7;
+    const long long unit = static_cast<long long>(blockIdx.x) * ROPE_WARPS + warp;
+    pi_grid_dependency_wait();
+    pi_launch_dependents();
+    if (unit >= static_cast<long long>(p.n_tokens) * p.parts) return;
+    const int t = static_cast<int>(unit / p.parts), part = static_cast<int>(unit - static_cast<long long>(t) * p.parts);
+    const int pos = p.pos[t];
+    if (pos < 0) return;                                                       // a padding token: its rows stay as they were
+    const int H = p.Hq + p.Hkv, n_quads = (H + 3) >> 2;
+    const T* q = static_cast<const T*>(p.q) + t * p.q_stride;
+    const T* k = static_cast<const T*>(p.k) + t * p.k_stride;
+
+    auto src = [&](int row) { return row < p.Hq ? q + row * PI_HEAD_DIM : k + (row - p.Hq) * PI_HEAD_DIM; };
+    Raw<T> a = {}, b = {};
+    int quad = part;
+    int row = quad * 4 + sub;
+    if (row < H) { load8(src(row) + 8 * l, a); load8(src(row) + 64 + 8 * l, b); }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int f = lane + 32 * i;
+        float2 cs = make_float2(1.f, 0.f);                                     // channels beyond rot_dim are not turned
+        if (f < p.half) {
+            double turns = static_cast<double>(pos) * static_cast<double>(p.inv_freq[f]) * 0.15915494309189533577;   // 1 / (2 pi)
+            turns -= rint(turns);
+            sincospif(2.f * static_cast<float>(turns), &cs.y, &cs.x);
+        }
+        s_cs[warp][f] = cs;
+    }
+    __syncwarp();
+    float2 cs[8];                                                              // this lane's eight angles
+#pragma unroll
+    for (int e = 0; e < 8; ++e) cs[e] = s_cs[warp][PAIR == PAIR_NEIGHBOURS ? (e < 4 ? 4 * l + e : 32 + 4 * l + e - 4) : 8 * l + e];
+
+    int have = -1;                                                             // whose weights are in w: 0 queries, 1 keys
+    float w[16];
+    for (; quad < n_quads; quad += p.parts) {
+        row = quad * 4 + sub;
+        float x[16];
+        widen8(a, x);
+        widen8(b, x + 8);
+        const int next = row + 4 * p.parts;
+        if (next < H) { load8(src(next) + 8 * l, a); load8(src(next) + 64 + 8 * l, b); }
+        if (p.wq) {
+            const int is_k = row >= p.Hq;
+            if (is_k != have) {
+                have = is_k;
+                const float4* g = reinterpret_cast<const float4*>(is_k ? p.wk : p.wq);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float4 v = __ldg(g + (i < 2 ? 2 * l + i : 16 + 2 * l + i - 2));
+                    w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+                }
+            }
+            float ss = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) ss = fmaf(x[i], x[i], ss);
+            ss += __shfl_xor_sync(0xffffffffu, ss, 1);
+            ss += __shfl_xor_sync(0xffffffffu, ss, 2);
+            ss += __shfl_xor_sync(0xffffffffu, ss, 4);
+            const float r = rsqrtf(ss * (1.f / PI_HEAD_DIM) + p.eps);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] *= r * w[i];
+        }
+        if (PAIR == PAIR_HALVES_FULL) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float u = x[e], v = x[8 + e];
+                x[e] = u * cs[e].x - v * cs[e].y;
+                x[8 + e] = v * cs[e].x + u * cs[e].y;
+            }
+        } else if (PAIR == PAIR_NEIGHBOURS) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if ((e < 4 ? 4 * l + e : 32 + 4 * l + e - 4) >= p.half) continue;
+                const float u = x[2 * e], v = x[2 * e + 1];
+                x[2 * e] = u * cs[e].x - v * cs[e].y;
+                x[2 * e + 1] = v * cs[e].x + u * cs[e].y;
+            }
+        } else {
+            // the members of a pair are rot_dim / 2 channels apart, in whichever lanes: through shared memory
+            float* sr = s_row[warp][sub];
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sr[(i < 8 ? 0 : 56) + 8 * l + i] = x[i];
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int d = (i < 8 ? 0 : 56) + 8 * l + i;
+                if (d < p.half) { const float2 z = s_cs[warp][d]; x[i] = x[i] * z.x - sr[d + p.half] * z.y; }
+                else if (d < 2 * p.half) { const float2 z = s_cs[warp][d - p.half]; x[i] = x[i] * z.x + sr[d - p.half] * z.y; }
+            }
+        }
+        if (row < H) {
+            uint4* dst = reinterpret_cast<uint4*>(row < p.Hq ? p.q_out + (static_cast<size_t>(t) * p.Hq + row) * PI_HEAD_DIM
+                                                             : p.k_out + (static_cast<size_t>(t) * p.Hkv + row - p.Hq) * PI_HEAD_DIM);
+            dst[l] = narrow8(x);
+            dst[8 + l] = narrow8(x + 8);
+        }
+    }
+}
+
+template <typename T>
+int launch(const RopeParams& p, int interleaved, cudaStream_t stream) {
+    const long long units = static_cast<long long>(p.n_tokens) * p.parts;
+    const dim3 grid(static_cast<unsigned>((units + ROPE_WARPS - 1) / ROPE_WARPS)), block(ROPE_THREADS);
+    if (interleaved) PI_CUDA_TRY(pi_launch_pdl(qk_norm_rope_kernel<T, PAIR_NEIGHBOURS>, grid, block, 0, stream, p));
+    else if (p.half == 64) PI_CUDA_TRY(pi_launch_pdl(qk_norm_rope_kernel<T, PAIR_HALVES_FULL>, grid, block, 0, stream, p));
+    else PI_CUDA_TRY(pi_launch_pdl(qk_norm_rope_kernel<T, PAIR_HALVES_PART>, grid, block, 0, stream, p));
+    return PI_OK;
+}
+
+}  // namespace
+
+int pi_launch_qk_norm_rope(pi_ctx* c, int n_tokens, int dtype, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                           const int32_t* pos, const float* wq, const float* wk, float eps, const float* inv_freq, int rot_dim,
+                           int interleaved, void* q_out, void* k_out, cudaStream_t stream) {
+    RopeParams p;
+    p.q = q; p.k = k; p.q_stride = q_stride; p.k_stride = k_stride;
+    p.pos = pos; p.wq = wq; p.wk = wk; p.inv_freq = inv_freq;
+    p.q_out = static_cast<__nv_bfloat16*>(q_out); p.k_out = static_cast<__nv_bfloat16*>(k_out);
+    p.eps = eps; p.n_tokens = n_tokens; p.Hq = c->cfg.n_q_heads; p.Hkv = c->cfg.n_kv_heads; p.half = rot_dim / 2;
+    // few tokens: a token's rows are spread over several warps, down to four rows each
+    const long long want = static_cast<long long>(c->n_sms) * 16;
+    const int quads = (p.Hq + p.Hkv + 3) / 4;
+    long long parts = (want + n_tokens - 1) / n_tokens;
+    p.parts = static_cast<int>(parts < 1 ? 1 : parts > quads ? quads : parts);
+    if (dtype == PI_DTYPE_BF16) return launch<__nv_bfloat16>(p, interleaved, stream);
+    if (dtype == PI_DTYPE_FP16) return launch<__half>(p, interleaved, stream);
+    return launch<float>(p, interleaved, stream);
+}

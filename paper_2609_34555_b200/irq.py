@@ -180,6 +180,8 @@ class CudaOffload:
 
     def __init__(self, sess, q_all, ffn, split_attention: bool = False):
         import torch
+        if split_attention and sess.kv_bits != 16:
+            raise ValueError("the attention is split around the recall for bf16 blocks only")
         self.torch, self.sess, self.q_all, self.ffn = torch, sess, q_all, ffn
         self.split = split_attention
         self._state = sess.pi.attn_state(sess.batch, sess.device) if split_attention else None
@@ -204,7 +206,7 @@ class CudaOffload:
         pi.score_select_diff(l, self.step, q, b.digest, s.ctx_len, b.sel_blocks, b.sel_count, b.block_table, b.slot_block,
                              b.slot_stamp, b.sel_slots, b.recall_list, b.recall_count, stream=s.side)
         d = self.torch.cuda.Event(); d.record(s.side); s.side2.wait_event(d)
-        pi.recall_gather_scatter(l, s.host_region(l), b.pool, b.recall_list, b.recall_count, stream=s.side2)
+        s._path.recall(l, b, s.host_region(l), b.recall_list, b.recall_count, page_table=s.page_table(l), stream=s.side2)
         io = self.torch.cuda.Event(enable_timing=True)
         io.record(s.side2)
         if self.split:
@@ -227,8 +229,7 @@ class CudaOffload:
             pi.sparse_decode_attn_recalled(l, q, b.pool, b.sel_slots, b.sel_blocks, b.sel_count, s.ctx_len,
                                            b.recall_list, b.recall_count, self._state, s.out[l], stream=self.compute_stream)
         else:
-            pi.sparse_decode_attn(l, q, b.pool, b.sel_slots, b.sel_blocks, b.sel_count, s.ctx_len, s.out[l], None,
-                                  stream=self.compute_stream)
+            s._path.attention(l, b, q, s.ctx_len, s.out[l], stream=self.compute_stream)
         self.ffn()
 
     def drain(self) -> None:

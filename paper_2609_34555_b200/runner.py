@@ -13,18 +13,25 @@ from .binding import PulseInfer
 
 
 class LayerBuffers:
-    """Everything one layer keeps on the device for a batch of offloaded sequences."""
+    """Everything one layer keeps on the device for a batch of offloaded sequences.  kv_bits: 16, or 4 for a
+    pool of 4-bit blocks (uint8 [batch][C][pi.kv4_block_bytes])."""
 
-    def __init__(self, pi: PulseInfer, batch: int, device="cuda", keep_scores: bool = False):
+    def __init__(self, pi: PulseInfer, batch: int, device="cuda", keep_scores: bool = False, kv_bits: int = 16):
         c = pi.cfg
+        if kv_bits not in (4, 16):
+            raise ValueError("kv_bits: 16 or 4")
+        self.kv_bits = kv_bits
         i32 = dict(dtype=torch.int32, device=device)
         self.batch = batch
         self.digest = torch.zeros((batch, c.max_blocks, 2, c.head_dim), dtype=torch.bfloat16, device=device)
         self.block_table = torch.full((batch, c.max_blocks), -1, **i32)
         self.slot_block = torch.full((batch, c.pool_slots), -1, **i32)
         self.slot_stamp = torch.zeros((batch, c.pool_slots), **i32)
-        self.pool = torch.zeros((batch, c.pool_slots, c.n_kv_heads, 2, c.block_tokens, c.head_dim),
-                                dtype=torch.bfloat16, device=device)
+        if kv_bits == 4:
+            self.pool = torch.zeros((batch, c.pool_slots, pi.kv4_block_bytes), dtype=torch.uint8, device=device)
+        else:
+            self.pool = torch.zeros((batch, c.pool_slots, c.n_kv_heads, 2, c.block_tokens, c.head_dim),
+                                    dtype=torch.bfloat16, device=device)
         self.sel_blocks = torch.full((batch, c.budget_blocks), -1, **i32)
         self.sel_count = torch.zeros((batch,), **i32)
         self.sel_slots = torch.full((batch, c.budget_blocks), -1, **i32)
@@ -42,6 +49,19 @@ class RecallPath:
         self._ev_in = torch.cuda.Event()
         self._ev_recall = torch.cuda.Event()
 
+    def recall(self, layer: int, buf: LayerBuffers, host_kv: torch.Tensor, recall_list, recall_count,
+               page_table: Optional[torch.Tensor] = None, stream=None) -> None:
+        """The lists' blocks from the host store into the pool, in whichever form the buffers keep them."""
+        call = self.pi.recall_kv4 if buf.kv_bits == 4 else self.pi.recall_gather_scatter
+        call(layer, host_kv, buf.pool, recall_list, recall_count, page_table=page_table, stream=stream)
+
+    def append(self, layer: int, step, buf: LayerBuffers, k_new, v_new, ctx_len, host_kv: torch.Tensor,
+               page_table: Optional[torch.Tensor] = None, stream=None) -> None:
+        """The step's token into pool, host store and digest."""
+        call = self.pi.append_kv4 if buf.kv_bits == 4 else self.pi.append_kv
+        call(layer, step, k_new, v_new, ctx_len, host_kv, buf.pool, buf.block_table, buf.slot_block, buf.slot_stamp,
+             buf.digest, page_table=page_table, stream=stream)
+
     def prepare_layer(self, layer: int, buf: LayerBuffers, host_kv: torch.Tensor, ctx_len: torch.Tensor,
                       resident: torch.Tensor, kv_for_digest: Optional[torch.Tensor] = None,
                       page_table: Optional[torch.Tensor] = None) -> None:
@@ -50,6 +70,8 @@ class RecallPath:
         host store needs kv_for_digest (the keys in logical block order)."""
         if page_table is not None and kv_for_digest is None:
             raise ValueError("a paged host store cannot be read in block order: pass kv_for_digest")
+        if buf.kv_bits == 4 and kv_for_digest is None:
+            raise ValueError("digests are built from the keys in bf16: pass kv_for_digest")
         pi = self.pi
         pi.build_digests(layer, host_kv if kv_for_digest is None else kv_for_digest, ctx_len, buf.digest)
         pi.table_init(resident, buf.block_table, buf.slot_block, buf.slot_stamp)
@@ -62,7 +84,7 @@ class RecallPath:
         fill[:, :, 1] = order.to(torch.int32)
         fill[:, :, 2] = 1
         fill[:, :, 3] = torch.arange(C, dtype=torch.int32, device=resident.device)
-        pi.recall_gather_scatter(layer, host_kv, buf.pool, fill.contiguous(), n.contiguous(), page_table=page_table)
+        self.recall(layer, buf, host_kv, fill.contiguous(), n.contiguous(), page_table=page_table)
 
     def select_and_recall(self, layer: int, step: int, buf: LayerBuffers, q: torch.Tensor, ctx_len: torch.Tensor,
                           host_kv: torch.Tensor, stream=None, fused: bool = True) -> None:
@@ -76,12 +98,12 @@ class RecallPath:
             pi.score_select(layer, q, buf.digest, ctx_len, buf.sel_blocks, buf.sel_count, buf.scores, stream=stream)
             pi.diff_misses(layer, step, ctx_len, buf.sel_blocks, buf.sel_count, buf.block_table, buf.slot_block,
                            buf.slot_stamp, buf.sel_slots, buf.recall_list, buf.recall_count, stream=stream)
-        pi.recall_gather_scatter(layer, host_kv, buf.pool, buf.recall_list, buf.recall_count, stream=stream)
+        self.recall(layer, buf, host_kv, buf.recall_list, buf.recall_count, stream=stream)
 
     def attention(self, layer: int, buf: LayerBuffers, q: torch.Tensor, ctx_len: torch.Tensor, out: torch.Tensor,
                   lse: Optional[torch.Tensor] = None, stream=None) -> None:
-        self.pi.sparse_decode_attn(layer, q, buf.pool, buf.sel_slots, buf.sel_blocks, buf.sel_count, ctx_len, out,
-                                   lse, stream=stream)
+        call = self.pi.sparse_decode_attn_kv4 if buf.kv_bits == 4 else self.pi.sparse_decode_attn
+        call(layer, q, buf.pool, buf.sel_slots, buf.sel_blocks, buf.sel_count, ctx_len, out, lse, stream=stream)
 
     def layer_step(self, layer: int, step: int, buf: LayerBuffers, q: torch.Tensor, ctx_len: torch.Tensor,
                    host_kv: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor] = None,
@@ -111,6 +133,8 @@ class RecallPath:
         stream, the resident blocks' share of the attention beside the recall on the side stream, the recalled
         blocks' share on the current stream once the recall has landed."""
         pi = self.pi
+        if buf.kv_bits != 16:
+            raise ValueError("the attention is split around the recall for bf16 blocks only")
         main = torch.cuda.current_stream()
         if fused:
             pi.score_select_diff(layer, step, q, buf.digest, ctx_len, buf.sel_blocks, buf.sel_count, buf.block_table,
@@ -238,12 +262,20 @@ class DecodeSession:
 
     `recall_streams`: the recall launches of consecutive layers rotate over this many streams, so
     the fixed cost of one launch (launch gap, list scan, first round trip over the host link,
-    drain) is covered by the transfer of the next."""
+    drain) is covered by the transfer of the next.
+
+    `kv_bits=4` keeps the host store and the pools in 4-bit blocks (pi.kv4_block_bytes each): load_layer rounds the
+    layer's keys and values, appended tokens are rounded as they come, the recall moves 4-bit blocks and the
+    attention reads them.  Digests, and with them the selection, are built from the keys as given."""
 
     def __init__(self, pi: PulseInfer, batch: int, n_layers: int, host_layers: Optional[int] = None,
                  device="cuda", keep_scores: bool = False, paged: bool = False, page_seed: int = 0,
-                 recall_streams: int = 2, fused_select_diff: bool = True, split_attention: bool = False):
+                 recall_streams: int = 2, fused_select_diff: bool = True, split_attention: bool = False,
+                 kv_bits: int = 16):
         c = pi.cfg
+        if kv_bits == 4 and split_attention:
+            raise ValueError("the attention is split around the recall for bf16 blocks only")
+        self.kv_bits = kv_bits
         # attention split around the recall: the resident blocks' share runs beside the recall (in the serial
         # form on a stream of its own), the recalled blocks' share after it
         self.split_attention = split_attention
@@ -251,9 +283,12 @@ class DecodeSession:
         self.pi, self.batch, self.n_layers = pi, batch, n_layers
         self.host_layers = n_layers if host_layers is None else max(1, min(host_layers, n_layers))
         self.device = torch.device(device)
-        self.bufs = [LayerBuffers(pi, batch, device, keep_scores) for _ in range(n_layers)]
+        self.bufs = [LayerBuffers(pi, batch, device, keep_scores, kv_bits) for _ in range(n_layers)]
         shape = (batch, c.max_blocks, c.n_kv_heads, 2, c.block_tokens, c.head_dim)
-        self.host_kv = [torch.empty(shape, dtype=torch.bfloat16, pin_memory=True) for _ in range(self.host_layers)]
+        if kv_bits == 4:
+            shape = (batch, c.max_blocks, pi.kv4_block_bytes)
+        self.host_kv = [torch.empty(shape, dtype=torch.uint8 if kv_bits == 4 else torch.bfloat16, pin_memory=True)
+                        for _ in range(self.host_layers)]
         self.page_tables = None
         if paged:
             g = torch.Generator().manual_seed(page_seed)
@@ -302,15 +337,25 @@ class DecodeSession:
         host = self.host_region(layer)
         pt = self.page_table(layer)
         if kv_dev is not None and store:
+            blocks = self.pack_blocks(kv_dev) if self.kv_bits == 4 else kv_dev
             if pt is None:
-                host.copy_(kv_dev, non_blocking=False)
+                host.copy_(blocks, non_blocking=False)
             else:
-                scattered = torch.empty_like(kv_dev)
-                scattered.view((-1,) + tuple(kv_dev.shape[2:]))[pt.view(-1).long()] = kv_dev.view((-1,) + tuple(kv_dev.shape[2:]))
+                scattered = torch.empty_like(blocks)
+                scattered.view((-1,) + tuple(blocks.shape[2:]))[pt.view(-1).long()] = blocks.view((-1,) + tuple(blocks.shape[2:]))
                 host.copy_(scattered, non_blocking=False)
                 del scattered
+            del blocks
         self._path.prepare_layer(layer, self.bufs[layer], host, self.ctx_len, resident,
                                  kv_for_digest=kv_dev, page_table=pt)
+
+    def pack_blocks(self, kv_dev: torch.Tensor) -> torch.Tensor:
+        """Whole blocks [batch][NB][Hkv][2][B][D] bf16 -> 4-bit blocks [batch][NB][kv4_block_bytes] uint8."""
+        n = kv_dev.shape[0] * kv_dev.shape[1]
+        rows = kv_dev.reshape((n,) + tuple(kv_dev.shape[2:])).transpose(1, 3)          # [block][token][K, V][head][D]
+        out = torch.zeros((kv_dev.shape[0], kv_dev.shape[1], self.pi.kv4_block_bytes), dtype=torch.uint8, device=kv_dev.device)
+        self.pi.kv4_store(rows[:, :, 0], rows[:, :, 1], out)
+        return out
 
     def decode_step(self, q: torch.Tensor, overlapped: bool = True, timer: Optional[StageTimer] = None,
                     resident_script: Optional[torch.Tensor] = None, new_kv=None,
@@ -366,8 +411,7 @@ class DecodeSession:
                 pi.table_init(resident_script[l], b.block_table, b.slot_block, b.slot_stamp, stream=sel_s)
             if new_kv is not None:
                 ta = tm.mark(sel_s) if tm and tm.wants("append") else None
-                pi.append_kv(l, step, new_kv[0][l], new_kv[1][l], self.ctx_prev, host, b.pool, b.block_table,
-                             b.slot_block, b.slot_stamp, b.digest, page_table=pt, stream=sel_s)
+                self._path.append(l, step, b, new_kv[0][l], new_kv[1][l], self.ctx_prev, host, page_table=pt, stream=sel_s)
                 if ta is not None:
                     tm.add("append", ta, tm.mark(sel_s))
             if self.fused_select_diff:
@@ -408,7 +452,7 @@ class DecodeSession:
                     evs = torch.cuda.Event() if capturing else self._ev_res[l]
                     evs.record(res_s)
             t2r = tm.mark(rec_s) if tm and tm.wants("recall") else None
-            pi.recall_gather_scatter(l, host, b.pool, b.recall_list, b.recall_count, page_table=pt, stream=rec_s)
+            self._path.recall(l, b, host, b.recall_list, b.recall_count, page_table=pt, stream=rec_s)
             t3 = tm.mark(rec_s) if tm and tm.wants("recall") else None
             if overlapped:
                 evr.record(rec_s)
@@ -420,8 +464,7 @@ class DecodeSession:
                 pi.sparse_decode_attn_recalled(l, q[l], b.pool, b.sel_slots, b.sel_blocks, b.sel_count, self.ctx_len,
                                                b.recall_list, b.recall_count, self._attn_state, out[l], stream=main)
             else:
-                pi.sparse_decode_attn(l, q[l], b.pool, b.sel_slots, b.sel_blocks, b.sel_count, self.ctx_len,
-                                      out[l], None, stream=main)
+                self._path.attention(l, b, q[l], self.ctx_len, out[l], stream=main)
             t5 = tm.mark(main) if tm and tm.wants("attn") else None
             if overlapped:
                 eva.record(main)
