@@ -3,24 +3,24 @@
 //
 // 160 bytes a (token, KV head) for 4 G D operations: the pool's bytes are what the call cannot do without.  On the way
 // to them stands the arithmetic of taking the codes apart, so that is kept out of the wide loops:
-//   * a code becomes a bf16 number by two logical operations per PAIR: 0x4300 | code is 128 + code exactly, and the
-//     format's nibble order makes (word >> 4 n) & 0x000f000f a pair that the matrix instruction takes as it is;
+//   * a code becomes an fp16 number by one logical operation and one fused multiply-add per PAIR (code_pairs), and the
+//     format's nibble order makes the pairs what the matrix instruction takes as they are;
 //   * scales and minima never meet the codes.  For K they are applied to the products: with the channels of a group
-//     contracted by themselves,  q.k = sum over groups  scale * (q . code) + minimum * (sum of q),  two fused
-//     multiply-adds per (token, head, group) instead of one per channel.  For V they are applied to the weights:
-//     the contraction over tokens takes p * scale, one set per group, and the minima's part is a separate sum of
-//     p * minimum per (head, group).
+//     contracted by themselves,  q.k = sum over groups  scale * (q . code) + minimum * (sum of q);  the minima's part is
+//     one more small product.  For V the scales are applied to the weights, one set per group, and the minima's part is
+//     again one product, of the weights and the minima.
 // The contractions run on mma.sync (tokens or channels on M, up to 8 query heads on N): with G <= 16 query heads per
 // KV head a 128-row tcgen05 tile would be nearly empty, and the codes have to pass through registers anyway.
-// q and the codes are exact in bf16; p * scale is split into a bf16 head and a bf16 remainder (2^-17 together), so
-// that the weights add nothing to the one rounding of the output.  With G <= 4 the two halves of N carry the head and
-// the remainder, and the split costs no second instruction.
+// Codes are exact in fp16, queries after a power of two per head; weights times scales are rounded to 11 bits, each an
+// eighth of the output's own rounding and of random sign; all sums are in 32 bits.
 //
-// One (sequence, KV head) per cluster of S CTAs of 8 warps (S = 1, 2, 4 or 8 by the launcher's rule).  The item's
+// One (sequence, KV head) per cluster of S CTAs of 4 warps (S = 1, 2, 4 or 8 by the launcher's rule).  The item's
 // 16-token tiles are dealt out to its warps in turn; a warp streams its own tiles through its own ring of shared-memory
 // stages with 16-byte asynchronous copies (a tile is 2560 contiguous bytes), so no warp waits for another until the
 // end.  Every warp keeps its own running maximum and sum; the states are merged once, through shared memory, and
 // across the cluster through distributed shared memory: one launch, no partials in global memory.
+#include <cuda_fp16.h>
+
 #include "pi_attn_core.cuh"
 #include "pi_kv4.cuh"
 
@@ -28,9 +28,12 @@ namespace {
 
 using namespace pi_attn;
 
-constexpr int A4_WARPS = 8;
+constexpr int A4_WARPS = 4;
 constexpr int A4_THREADS = A4_WARPS * 32;
 constexpr int A4_STAGES = 4;
+constexpr int a4_ctas_per_sm(int NT) { return NT == 1 ? 4 : 2; }    // what the registers allow
+constexpr float A4_NO_UNIT = 0x1p120f;             // before a group's first product: every product but 0 leaves fp16
+constexpr float A4_NO_MAX = -1e30f;                // stands for -infinity in the running maximum: differences stay numbers
 
 struct Attn4Params {
     const __nv_bfloat16* q;
@@ -60,19 +63,78 @@ __device__ __forceinline__ uint2 lds64(uint32_t a) {
     asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
     return v;
 }
-// Pair n of a word: nibbles n (low half) and n + 4 (high half), each as the bf16 number 128 + nibble.
-__device__ __forceinline__ uint32_t code_pair(uint32_t w, int n) { return ((w >> (4 * n)) & 0x000f000fu) | 0x43004300u; }
-// 128 + code -> code - 8, exactly.
-__device__ __forceinline__ uint32_t less_136(uint32_t x) {
-    const __nv_bfloat162 c = __halves2bfloat162(__ushort_as_bfloat16(0x4308), __ushort_as_bfloat16(0x4308));
-    const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), c);
-    return *reinterpret_cast<const uint32_t*>(&r);
+// The four pairs of a word, nibbles n (low half) and n + 4 (high half), as fp16 numbers.  0x6400 | nibble is 1024 + nibble
+// and 0x6400 | 16 nibble is 1024 + 16 nibble, so two of the four need no shift; what brings them back to 0..15 is exact and
+// runs beside the logical operations, on the pipe that has room.
+__device__ __forceinline__ void code_pairs(uint32_t w, uint32_t (&p)[4]) {
+    const __half2 low = __halves2half2(__ushort_as_half(0xe400), __ushort_as_half(0xe400));        // -1024
+    const __half2 sixteenth = __halves2half2(__ushort_as_half(0x2c00), __ushort_as_half(0x2c00));  // 1 / 16
+    const __half2 high = __halves2half2(__ushort_as_half(0xd400), __ushort_as_half(0xd400));       // -64
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t v = i ? w >> 8 : w, a = (v & 0x000f000fu) | 0x64006400u, b = (v & 0x00f000f0u) | 0x64006400u;
+        const __half2 x = __hadd2(*reinterpret_cast<const __half2*>(&a), low), y = __hfma2(*reinterpret_cast<const __half2*>(&b), sixteenth, high);
+        p[2 * i] = *reinterpret_cast<const uint32_t*>(&x);
+        p[2 * i + 1] = *reinterpret_cast<const uint32_t*>(&y);
+    }
+}
+// d = a b
+__device__ __forceinline__ void mma_f16_zero(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ void mma_bf16_zero(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// 1 / x and 2^k for powers of two well inside the range
+__device__ __forceinline__ float inverse_power(float x) { return __uint_as_float(0x7f000000u - __float_as_uint(x)); }
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t max_f16x2(uint32_t a, uint32_t b) {
+    const __half2 v = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ float4 ld_shared_cluster_f32x4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+// The power of two at or below |x|, at least the smallest normal number.
+__device__ __forceinline__ float power_of(float x) { return __uint_as_float(max(__float_as_uint(x) & 0x7f800000u, 0x00800000u)); }
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ void sts128_zero(uint32_t a) { asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(a), "r"(0u) : "memory"); }
+__device__ __forceinline__ void ldsm_x2_t(uint32_t addr, uint32_t& a, uint32_t& b) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0,%1}, [%2];" : "=r"(a), "=r"(b) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 __device__ __forceinline__ uint32_t word_of(const uint4& v, int j) { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; }
 
-// NT: tiles of 8 query heads; DUP (G <= 4): columns 4..7 repeat heads 0..3 and carry the weights' remainders.
-template <int NT, bool DUP>
-__global__ void __launch_bounds__(A4_THREADS, NT == 1 ? 2 : 1)
+// NT: tiles of 8 query heads.
+template <int NT>
+__global__ void __launch_bounds__(A4_THREADS, a4_ctas_per_sm(NT))
 attn_kv4_kernel(Attn4Params p) {
     extern __shared__ __align__(128) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
@@ -82,6 +144,15 @@ attn_kv4_kernel(Attn4Params p) {
     pi_grid_dependency_wait();
     pi_launch_dependents();
 
+    // the entries of the warp's first 32 tiles are fetched beside the list's length, whatever that turns out to be
+    const int first = rank * A4_WARPS + warp, stride = A4_WARPS * S, log_sub = 31 - __clz(SUB);
+    const int32_t* slots = p.sel_slots + static_cast<size_t>(seq) * p.K;
+    const int32_t* blocks = p.sel_blocks + static_cast<size_t>(seq) * p.K;
+    auto entry_of = [&](int n) -> int2 {
+        const int j = (first + n * stride) >> log_sub;
+        return j < p.K ? make_int2(slots[j], blocks[j]) : make_int2(0, -1);
+    };
+    const int2 entry = entry_of(lane);
     const int ctx = p.ctx_len[seq];
     int cnt = p.sel_count[seq];
     if (cnt < 0 || cnt > p.K) {
@@ -89,194 +160,292 @@ attn_kv4_kernel(Attn4Params p) {
         cnt = 0;
     }
     const int n_tiles = cnt * SUB;
-    const int first = rank * A4_WARPS + warp, stride = A4_WARPS * S;
     const int n_mine = first < n_tiles ? (n_tiles - first + stride - 1) / stride : 0;
 
-    // {slot, sub-tile << 16, valid tokens << 20} of the warp's n-th tile (one per lane, 32 at a time)
-    auto meta_of = [&](int n) -> uint32_t {
-        if (n >= n_mine) return 0u;
-        const int t = first + n * stride, j = t / SUB, sub = t - j * SUB;
-        const int slot = p.sel_slots[static_cast<size_t>(seq) * p.K + j], blk = p.sel_blocks[static_cast<size_t>(seq) * p.K + j];
-        if (blk < 0) return 0u;
-        if (slot < 0 || slot >= p.C) {
-            if (h == 0) pi_report(p.st, PI_ERR_INDEX_RANGE, PI_STAGE_ATTN, seq, j, slot);
-            return 0u;
+    // The warp's n-th tile: byte offset from the head's first one (a sequence's pool is below 2^31 bytes), valid tokens.
+    auto meta_of = [&](int n, int2 e) -> uint2 {
+        if (n >= n_mine || e.y < 0) return make_uint2(0u, 0u);
+        const int t = first + n * stride, sub = t & (SUB - 1);
+        if (e.x < 0 || e.x >= p.C) {
+            if (h == 0) pi_report(p.st, PI_ERR_INDEX_RANGE, PI_STAGE_ATTN, seq, t >> log_sub, e.x);
+            return make_uint2(0u, 0u);
         }
-        const long long left = static_cast<long long>(ctx) - (static_cast<long long>(blk) * p.B + sub * 16);
-        const int nvalid = left < 0 ? 0 : left > 16 ? 16 : static_cast<int>(left);
-        return static_cast<uint32_t>(slot) | (static_cast<uint32_t>(sub) << 16) | (static_cast<uint32_t>(nvalid) << 20);
+        const long long left = static_cast<long long>(ctx) - (static_cast<long long>(e.y) * p.B + sub * 16);
+        return make_uint2(static_cast<uint32_t>(e.x * p.block_bytes) + sub * KV4_TILE_BYTES, left < 0 ? 0u : left > 16 ? 16u : static_cast<uint32_t>(left));
     };
-    uint32_t meta = meta_of(lane), meta_next = 0u;
+    uint2 meta = meta_of(lane, entry), meta_next = make_uint2(0u, 0u);     // of tiles 32 i + lane, and of the 32 after those
+    unsigned some = __ballot_sync(0xffffffffu, meta.y != 0u), whole = __ballot_sync(0xffffffffu, meta.y == 16u), some_next = 0u;
 
-    const unsigned char* head_base = p.pool + static_cast<long long>(seq) * p.C * p.block_bytes + static_cast<long long>(h) * SUB * KV4_TILE_BYTES;
+    const unsigned char* head_base = p.pool + static_cast<long long>(seq) * p.C * p.block_bytes + static_cast<long long>(h) * SUB * KV4_TILE_BYTES + lane * 16;
     const uint32_t ring = smem_u32(smem) + warp * (A4_STAGES * KV4_TILE_BYTES);
     const unsigned long long policy = pi_l2_stream_policy();
-    auto issue = [&](int n, uint32_t md) {             // tile n into its stage; one commit per tile, also for what is skipped
-        if (n < n_mine && (md >> 20)) {
-            const unsigned char* src = head_base + static_cast<long long>(md & 0xffffu) * p.block_bytes + ((md >> 16) & 15u) * KV4_TILE_BYTES + lane * 16;
-            const uint32_t dst = ring + (n % A4_STAGES) * KV4_TILE_BYTES + lane * 16;
+    uint32_t fill = 0u;                                  // stage of the next tile
+    auto issue = [&](bool has, uint32_t offset) {        // a tile into its stage; one commit per tile, also for what is skipped
+        if (has) {
+            const unsigned char* src = head_base + offset;
+            const uint32_t dst = ring + fill + lane * 16;
 #pragma unroll
             for (int i = 0; i < KV4_TILE_BYTES / 512; ++i) copy16(dst + i * 512, src + i * 512, policy);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
+        fill = fill == (A4_STAGES - 1) * KV4_TILE_BYTES ? 0u : fill + KV4_TILE_BYTES;
     };
 #pragma unroll
-    for (int n = 0; n < A4_STAGES - 1; ++n) issue(n, __shfl_sync(0xffffffffu, meta, n));
+    for (int n = 0; n < A4_STAGES - 1; ++n) issue((some >> n) & 1u, __shfl_sync(0xffffffffu, meta.x, n));
 
-    // ---- the queries as B operands, in the channel order of the K codes, and their sums over each group of channels
-    uint32_t bq[NT][4][2][2];
-    float qs[NT][4][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int g = DUP ? (r & 3) : nt * 8 + r;
+    // ---- the queries as B operands, in the channel order of the K codes, as fp16 numbers: every head is scaled by a power of
+    // two so that its largest channel lies in [1, 2); what is below 2^-14 of that is rounded at 2^-25 of it, less than the
+    // sums below round.  With them, for the minima's own products, lane (r, c)'s {0, sum} of head r over the channels of
+    // group c, as three bf16 numbers (2^-25 together).  One warp prepares a group of channels for all.
+    uint4* s_bq = reinterpret_cast<uint4*>(smem + A4_WARPS * A4_STAGES * KV4_TILE_BYTES);       // [NT][4 groups][32 lanes]
+    uint32_t* s_bz = reinterpret_cast<uint32_t*>(s_bq + NT * 4 * 32);                            // [NT][3][32]
+    float* s_scale = reinterpret_cast<float*>(s_bz + NT * 3 * 32);                               // [NT][8 heads]
+    for (int part = warp; part < 4 * NT; part += A4_WARPS) {
+        const int nt = part >> 2, mine = part & 3, g = nt * 8 + r;
         const bool real = g < p.G;
         const __nv_bfloat16* qg = p.q + (static_cast<size_t>(seq) * p.Hq + static_cast<size_t>(h) * p.G + (real ? g : 0)) * PI_HEAD_DIM;
+        uint4 own = make_uint4(0, 0, 0, 0);
+        __nv_bfloat162 top2 = __float2bfloat162_rn(0.f);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const uint4 x = real ? __ldg(reinterpret_cast<const uint4*>(qg + 32 * j + 8 * c)) : make_uint4(0, 0, 0, 0);
-            // pair n = channels (n, n + 4) of the eight
-            bq[nt][j][0][0] = __byte_perm(x.x, x.z, 0x5410);
-            bq[nt][j][0][1] = __byte_perm(x.x, x.z, 0x7632);
-            bq[nt][j][1][0] = __byte_perm(x.y, x.w, 0x5410);
-            bq[nt][j][1][1] = __byte_perm(x.y, x.w, 0x7632);
-            float s[4] = {0.f, 0.f, 0.f, 0.f};
-            const uint32_t ones[4] = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-            mma_bf16(s, ones, bq[nt][j][0][0], bq[nt][j][0][1]);
-            mma_bf16(s, ones, bq[nt][j][1][0], bq[nt][j][1][1]);
-            qs[nt][j][0] = s[0];
-            qs[nt][j][1] = s[1];
+            if (j == mine) own = x;
+            const __nv_bfloat162* y = reinterpret_cast<const __nv_bfloat162*>(&x);
+            top2 = __hmax2(__hmax2(__hmax2(__habs2(y[0]), __habs2(y[1])), __hmax2(__habs2(y[2]), __habs2(y[3]))), top2);
+        }
+        float top = fmaxf(__low2float(top2), __high2float(top2));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        top = power_of(top);
+        const float inv = 1.f / top;
+        const uint32_t xs[4] = {own.x, own.y, own.z, own.w};
+        float f[8], sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __uint_as_float(xs[i] << 16) * inv;
+            f[2 * i + 1] = __uint_as_float(xs[i] & 0xffff0000u) * inv;
+            sum += f[2 * i] + f[2 * i + 1];
+        }
+        // pair n = channels (n, n + 4) of the eight
+        s_bq[part * 32 + lane] = make_uint4(pack_f16(f[0], f[4]), pack_f16(f[1], f[5]), pack_f16(f[2], f[6]), pack_f16(f[3], f[7]));
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        if (c == mine) {
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                const float hi = __bfloat162float(__float2bfloat16_rn(sum));
+                s_bz[(nt * 3 + i) * 32 + lane] = pack_bf16(0.f, hi);
+                sum -= hi;
+            }
+            if (mine == 0) s_scale[nt * 8 + r] = p.scale_log2 * top;
         }
     }
-
-    // ---- running state: o[j][mt] = channels 32 j + 4 r + 2 mt (+ 1 in the upper two) of heads 2 c, 2 c + 1; zo: the
-    // minima's share of group j for this lane's tokens; m, l as usual (exp2 domain)
-    float o[NT][4][2][4], zo[NT][4][2], m[NT][2], l[NT][2];
+    __syncthreads();
+    uint32_t bq[NT][4][2][2], bz[NT][3];
+    float scale[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-        m[nt][0] = m[nt][1] = -INFINITY;
-        l[nt][0] = l[nt][1] = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            zo[nt][j][0] = zo[nt][j][1] = 0.f;
+            const uint4 x = s_bq[(nt * 4 + j) * 32 + lane];
+            bq[nt][j][0][0] = x.x; bq[nt][j][0][1] = x.y; bq[nt][j][1][0] = x.z; bq[nt][j][1][1] = x.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 3; ++i) bz[nt][i] = s_bz[(nt * 3 + i) * 32 + lane];
+        scale[nt][0] = s_scale[nt * 8 + 2 * c];
+        scale[nt][1] = s_scale[nt * 8 + 2 * c + 1];
+    }
+
+    // ---- running state: o[j][mt] = channels 32 j + 4 r + 2 mt (+ 1 in the upper two) of heads 2 c, 2 c + 1, times unit[j];
+    // z = row r of {scale, minimum} of the four groups, weighted, for the same heads; m (exp2 domain) and l as usual
+    float o[NT][4][2][4], z[NT][4], m[NT][2], l[NT][2], unit[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) unit[j] = A4_NO_UNIT;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        m[nt][0] = m[nt][1] = A4_NO_MAX;
+        l[nt][0] = l[nt][1] = 0.f;
+        z[nt][0] = z[nt][1] = z[nt][2] = z[nt][3] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[nt][j][0][e] = o[nt][j][1][e] = 0.f;
-        }
     }
     // Row r of a tile's products is token pr (row r + 8: pr + 8): then the four tokens that a lane needs of V, rows 2 c,
     // 2 c + 1, 2 c + 8, 2 c + 9, are c, c + 4, c + 8, c + 12, and the lanes of one load read neighbouring rows.
     const int pr = (r >> 1) + 4 * (r & 1);
+    const int pl = ((lane & 7) >> 1) + 4 * (lane & 1) + (lane & 8);     // the token whose scales this lane names to ldmatrix
 
-    for (int n = 0; n < n_mine; ++n) {
-        if ((n & 31) == 0) {
-            if (n) meta = meta_next;
-            meta_next = meta_of(n + 32 + lane);
+    uint32_t tile = ring;                                // stage of the tile at hand
+    for (int n = 0; n < n_mine; ++n, tile = tile == ring + (A4_STAGES - 1) * KV4_TILE_BYTES ? ring : tile + KV4_TILE_BYTES) {
+        const int i = n & 31;
+        if (i == 0) {
+            if (n) {
+                meta = meta_next;
+                some = some_next;
+                whole = __ballot_sync(0xffffffffu, meta.y == 16u);
+            }
+            some_next = 0u;
+            if (n + 32 < n_mine) {
+                meta_next = meta_of(n + 32 + lane, entry_of(n + 32 + lane));
+                some_next = __ballot_sync(0xffffffffu, meta_next.y != 0u);
+            }
         }
         asm volatile("cp.async.wait_group %0;" ::"n"(A4_STAGES - 2) : "memory");
         __syncwarp();                                   // the stage is filled by all lanes, and the previous one read by all
-        {
-            const int nn = n + A4_STAGES - 1;
-            // (meta_next is not touched before it is needed: its loads have 29 tiles' time to arrive)
-            issue(nn, (nn >> 5) == (n >> 5) ? __shfl_sync(0xffffffffu, meta, nn & 31) : __shfl_sync(0xffffffffu, meta_next, nn & 31));
-        }
-        const int nvalid = static_cast<int>(__shfl_sync(0xffffffffu, meta, n & 31) >> 20);
-        if (nvalid == 0) continue;
-        const uint32_t tile = ring + (n % A4_STAGES) * KV4_TILE_BYTES;
-        // ---- S^T = K q^T, group by group
+        if (i + A4_STAGES - 1 < 32) issue((some >> (i + A4_STAGES - 1)) & 1u, __shfl_sync(0xffffffffu, meta.x, i + A4_STAGES - 1));
+        else issue((some_next >> (i + A4_STAGES - 1 - 32)) & 1u, __shfl_sync(0xffffffffu, meta_next.x, i + A4_STAGES - 1 - 32));
+        if (!((some >> i) & 1u)) continue;
+        // ---- S^T = K q^T: the minima's products first, then the codes' group by group
         float s[NT][4];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
         {
             const uint4 ka = lds128(tile + pr * 64 + c * 16), kb = lds128(tile + (pr + 8) * 64 + c * 16);
             const uint4 za = lds128(tile + KV4_K_SCALES + pr * 16), zb = lds128(tile + KV4_K_SCALES + (pr + 8) * 16);
+            const uint32_t ya = lds32(tile + KV4_K_SCALES + pr * 16 + c * 4), yb = lds32(tile + KV4_K_SCALES + (pr + 8) * 16 + c * 4);
+            const uint32_t az[4] = {ya, yb, ya, yb};    // {scale, minimum} of group c: places 2 c, 2 c + 1 (and + 8)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                mma_bf16_zero(s[nt], az, bz[nt][2], 0u);
+                mma_bf16(s[nt], az, bz[nt][0], bz[nt][1]);
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint32_t wa = word_of(ka, j), wb = word_of(kb, j);
-                const uint32_t a0[4] = {code_pair(wa, 0), code_pair(wb, 0), code_pair(wa, 1), code_pair(wb, 1)};
-                const uint32_t a1[4] = {code_pair(wa, 2), code_pair(wb, 2), code_pair(wa, 3), code_pair(wb, 3)};
+                uint32_t a[4], b[4];
+                code_pairs(word_of(ka, j), a);
+                code_pairs(word_of(kb, j), b);
                 const float sa = kv4_scale_of(word_of(za, j)), sb = kv4_scale_of(word_of(zb, j));
-                // the products hold 128 q beside code q: taken off with the minimum
-                const float ma = fmaf(-128.f, sa, kv4_min_of(word_of(za, j))), mb = fmaf(-128.f, sb, kv4_min_of(word_of(zb, j)));
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    float x[4] = {0.f, 0.f, 0.f, 0.f};
-                    mma_bf16(x, a0, bq[nt][j][0][0], bq[nt][j][0][1]);
-                    mma_bf16(x, a1, bq[nt][j][1][0], bq[nt][j][1][1]);
+                    float x[4];
+                    mma_f16_zero(x, a[0], b[0], a[1], b[1], bq[nt][j][0][0], bq[nt][j][0][1]);
+                    mma_f16(x, a[2], b[2], a[3], b[3], bq[nt][j][1][0], bq[nt][j][1][1]);
+                    s[nt][0] = fmaf(sa, x[0], s[nt][0]); s[nt][1] = fmaf(sa, x[1], s[nt][1]);
+                    s[nt][2] = fmaf(sb, x[2], s[nt][2]); s[nt][3] = fmaf(sb, x[3], s[nt][3]);
+                }
+            }
+        }
+        if (!((whole >> i) & 1u)) {                     // what lies behind the last token may be anything, NaN among it
+            const int nvalid = static_cast<int>(__shfl_sync(0xffffffffu, meta.y, i));
+            if (lane < 16 && lane >= nvalid) sts128_zero(tile + KV4_V_SCALES + lane * 16);
+            __syncwarp();
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        s[nt][e] = fmaf(sa, x[e], fmaf(ma, qs[nt][j][e], s[nt][e]));
-                        s[nt][2 + e] = fmaf(sb, x[2 + e], fmaf(mb, qs[nt][j][e], s[nt][2 + e]));
+            for (int nt = 0; nt < NT; ++nt) {
+                if (pr >= nvalid) s[nt][0] = s[nt][1] = -INFINITY;
+                if (pr + 8 >= nvalid) s[nt][2] = s[nt][3] = -INFINITY;
+            }
+        }
+        // ---- online softmax over the tile's tokens.  The reference m moves only when a score exceeds it by 8 (a factor of
+        // 256, far from any overflow), so that most tiles neither reduce a maximum across lanes nor touch the sums.
+        float w[NT][4];
+        bool over = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[nt][e] = fmaf(s[nt][e], scale[nt][e & 1], -m[nt][e & 1]);
+            over |= max3(fmaxf(w[nt][0], w[nt][1]), w[nt][2], w[nt][3]) > 8.f;
+        }
+        if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float mx = fmaxf(s[nt][e], s[nt][2 + e]) * scale[nt][e];
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                    const float m_new = fmaxf(m[nt][e], mx), alpha = ex2(m[nt][e] - m_new);
+                    m[nt][e] = m_new;
+                    l[nt][e] *= alpha;
+                    z[nt][e] *= alpha;
+                    w[nt][e] = fmaf(s[nt][e], scale[nt][e], -m_new);
+                    w[nt][2 + e] = fmaf(s[nt][2 + e], scale[nt][e], -m_new);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        o[nt][j][0][e] *= alpha; o[nt][j][0][2 + e] *= alpha;
+                        o[nt][j][1][e] *= alpha; o[nt][j][1][2 + e] *= alpha;
                     }
                 }
-            }
         }
-        // ---- online softmax over the tile's tokens
-        float w[NT][4];
+        // ---- the weights; with them the minima's share of the result, for all four groups in one product.  Minima and
+        // scales are bf16, so the weights take part as a bf16 head (the upper half of the number) and a bf16 remainder.
+        uint32_t az[4];
+        ldsm_x2_t(tile + KV4_V_SCALES + pl * 16, az[0], az[2]);
+        az[1] = az[3] = 0u;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
+            float rest[4];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float s0 = pr < nvalid ? s[nt][e] * p.scale_log2 : -INFINITY;
-                const float s1 = pr + 8 < nvalid ? s[nt][2 + e] * p.scale_log2 : -INFINITY;
-                float mx = fmaxf(s0, s1);
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                const float m_new = fmaxf(m[nt][e], mx);
-                float alpha = 1.f, p0 = 0.f, p1 = 0.f;
-                if (m_new != -INFINITY) {
-                    alpha = exp2f(m[nt][e] - m_new);
-                    p0 = exp2f(s0 - m_new);
-                    p1 = exp2f(s1 - m_new);
+            for (int e = 0; e < 4; ++e) {
+                w[nt][e] = ex2(w[nt][e]);
+                rest[e] = w[nt][e] - __uint_as_float(__float_as_uint(w[nt][e]) & 0xffff0000u);
+            }
+            l[nt][0] += w[nt][0] + w[nt][2];
+            l[nt][1] += w[nt][1] + w[nt][3];
+            mma_bf16(z[nt], az, movm_t(pack_bf16(rest[0], rest[1])), movm_t(pack_bf16(rest[2], rest[3])));
+            mma_bf16(z[nt], az, movm_t(__byte_perm(__float_as_uint(w[nt][0]), __float_as_uint(w[nt][1]), 0x7632)),
+                     movm_t(__byte_perm(__float_as_uint(w[nt][2]), __float_as_uint(w[nt][3]), 0x7632)));
+        }
+        // ---- weight times scale, one set per group, in fp16: 11 bits, where bf16 would need two numbers.  Its narrow range is
+        // covered by a power of two per group (`unit`), set by the first tile so that the largest product is about 2^8 and
+        // moved when a later one leaves the range.
+        const uint4 va = lds128(tile + KV4_V_SCALES + pr * 16), vb = lds128(tile + KV4_V_SCALES + (pr + 8) * 16);
+        uint32_t pw[NT][4][2];
+        auto products = [&]() {
+            uint32_t top = 0u;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float sa = kv4_scale_of(word_of(va, j)) * unit[j], sb = kv4_scale_of(word_of(vb, j)) * unit[j];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    pw[nt][j][0] = pack_f16(w[nt][0] * sa, w[nt][1] * sa);
+                    pw[nt][j][1] = pack_f16(w[nt][2] * sb, w[nt][3] * sb);
+                    top = max_f16x2(top, max_f16x2(pw[nt][j][0], pw[nt][j][1]));
                 }
-                m[nt][e] = m_new;
-                l[nt][e] = l[nt][e] * alpha + p0 + p1;
-                w[nt][e] = p0; w[nt][2 + e] = p1;
+            }
+            return top;
+        };
+        {
+            const uint32_t top = products();
+            const __half2 t = *reinterpret_cast<const __half2*>(&top);
+            if (__any_sync(0xffffffffu, __hgt(__hmax(__low2half(t), __high2half(t)), __ushort_as_half(0x7800)))) {      // 2^15
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    zo[nt][j][e] *= alpha;
-                    o[nt][j][0][e] *= alpha; o[nt][j][0][2 + e] *= alpha;
-                    o[nt][j][1][e] *= alpha; o[nt][j][1][2 + e] *= alpha;
+                    // the largest product of the group in the tile (2^-20 of it: the product itself may leave fp32)
+                    const float sa = kv4_scale_of(word_of(va, j)) * 0x1p-20f, sb = kv4_scale_of(word_of(vb, j)) * 0x1p-20f;
+                    float mx = 0.f;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+                        mx = fmaxf(mx, fmaxf(fmaxf(w[nt][0], w[nt][1]) * sa, fmaxf(w[nt][2], w[nt][3]) * sb));
+                    // exponents: of 2^8 / (2^20 mx), from which the product of the largest weight and scale is 2^8 and more
+                    const int top_exp = min(static_cast<int>(__reduce_max_sync(0xffffffffu, __float_as_uint(mx)) >> 23), 239);
+                    const int want = 242 - top_exp, have = static_cast<int>(__float_as_uint(unit[j]) >> 23);
+                    if (top_exp > 0 && want < have) {
+                        const float f = have - want < 127 ? __uint_as_float(static_cast<uint32_t>(127 + want - have) << 23) : 0.f;
+                        unit[j] = __uint_as_float(static_cast<uint32_t>(want) << 23);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) { o[nt][j][0][e] *= f; o[nt][j][1][e] *= f; }
+                    }
                 }
+                products();
             }
-        // ---- O^T += V^T (p scale), group by group
-        uint4 va = lds128(tile + KV4_V_SCALES + pr * 16), vb = lds128(tile + KV4_V_SCALES + (pr + 8) * 16);
-        if (nvalid < 16) {                              // what lies behind the last token may be anything, NaN among it
-            if (pr >= nvalid) va = make_uint4(0, 0, 0, 0);
-            if (pr + 8 >= nvalid) vb = make_uint4(0, 0, 0, 0);
         }
+        // ---- O^T += V^T (weight scale), group by group
         uint2 x[4];
 #pragma unroll
         for (int a = 0; a < 4; ++a) x[a] = lds64(tile + KV4_V_CODES + (4 * a + c) * 64 + r * 8);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const unsigned sel = (j & 1) ? 0x7632u : 0x5410u;
-            const uint32_t y01 = __byte_perm(j < 2 ? x[0].x : x[0].y, j < 2 ? x[1].x : x[1].y, sel);
-            const uint32_t y23 = __byte_perm(j < 2 ? x[2].x : x[2].y, j < 2 ? x[3].x : x[3].y, sel);
-            const uint32_t a0[4] = {less_136(code_pair(y01, 0)), less_136(code_pair(y01, 1)), less_136(code_pair(y23, 0)), less_136(code_pair(y23, 1))};
-            const uint32_t a1[4] = {less_136(code_pair(y01, 2)), less_136(code_pair(y01, 3)), less_136(code_pair(y23, 2)), less_136(code_pair(y23, 3))};
-            const float sa = kv4_scale_of(word_of(va, j)), sb = kv4_scale_of(word_of(vb, j));
-            const float ma = fmaf(8.f, sa, kv4_min_of(word_of(va, j))), mb = fmaf(8.f, sb, kv4_min_of(word_of(vb, j)));
+            uint32_t a[4], b[4];
+            code_pairs(__byte_perm(j < 2 ? x[0].x : x[0].y, j < 2 ? x[1].x : x[1].y, sel), a);
+            code_pairs(__byte_perm(j < 2 ? x[2].x : x[2].y, j < 2 ? x[3].x : x[3].y, sel), b);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                zo[nt][j][0] = fmaf(w[nt][0], ma, fmaf(w[nt][2], mb, zo[nt][j][0]));
-                zo[nt][j][1] = fmaf(w[nt][1], ma, fmaf(w[nt][3], mb, zo[nt][j][1]));
-                const float p0 = w[nt][0] * sa, p1 = w[nt][1] * sa, p2 = w[nt][2] * sb, p3 = w[nt][3] * sb;
-                uint32_t h01 = pack_bf16(p0, p1), h23 = pack_bf16(p2, p3);
-                const float2 f01 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&h01));
-                const float2 f23 = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&h23));
-                const uint32_t r01 = pack_bf16(p0 - f01.x, p1 - f01.y), r23 = pack_bf16(p2 - f23.x, p3 - f23.y);
-                if (DUP) {
-                    if (c >= 2) { h01 = r01; h23 = r23; }
-                    const uint32_t b0 = movm_t(h01), b1 = movm_t(h23);
-                    mma_bf16(o[nt][j][0], a0, b0, b1);
-                    mma_bf16(o[nt][j][1], a1, b0, b1);
-                } else {
-                    const uint32_t b0 = movm_t(h01), b1 = movm_t(h23), d0 = movm_t(r01), d1 = movm_t(r23);
-                    mma_bf16(o[nt][j][0], a0, b0, b1);
-                    mma_bf16(o[nt][j][1], a1, b0, b1);
-                    mma_bf16(o[nt][j][0], a0, d0, d1);
-                    mma_bf16(o[nt][j][1], a1, d0, d1);
-                }
+                const uint32_t b0 = movm_t(pw[nt][j][0]), b1 = movm_t(pw[nt][j][1]);
+                mma_f16(o[nt][j][0], a[0], a[1], b[0], b[1], b0, b1);
+                mma_f16(o[nt][j][1], a[2], a[3], b[2], b[3], b0, b1);
             }
         }
     }
@@ -294,68 +463,72 @@ attn_kv4_kernel(Attn4Params p) {
             float sum = l[nt][e];
 #pragma unroll
             for (int d = 4; d <= 16; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-            float z[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                z[j] = zo[nt][j][e];
-#pragma unroll
-                for (int d = 4; d <= 16; d <<= 1) z[j] += __shfl_xor_sync(0xffffffffu, z[j], d);
-            }
             const int g = nt * 8 + 2 * c + e;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                float4 v = make_float4(o[nt][j][0][e], o[nt][j][0][2 + e], o[nt][j][1][e], o[nt][j][1][2 + e]);
-                if (DUP) {                              // the remainders' columns belong to the head four columns before
-                    v.x += __shfl_xor_sync(0xffffffffu, v.x, 2); v.y += __shfl_xor_sync(0xffffffffu, v.y, 2);
-                    v.z += __shfl_xor_sync(0xffffffffu, v.z, 2); v.w += __shfl_xor_sync(0xffffffffu, v.w, 2);
-                }
-                v.x += z[j]; v.y += z[j]; v.z += z[j]; v.w += z[j];
-                if (g < p.G && (!DUP || c < 2)) *reinterpret_cast<float4*>(s_o + (warp * p.G + g) * PI_HEAD_DIM + 32 * j + 4 * r) = v;
+                // the minima's share is in the lanes that hold row 2 j + 1
+                const float f = inverse_power(unit[j]), zj = __shfl_sync(0xffffffffu, z[nt][e], 8 * j + 4 + c);
+                const float4 v = make_float4(fmaf(o[nt][j][0][e], f, zj), fmaf(o[nt][j][0][2 + e], f, zj), fmaf(o[nt][j][1][e], f, zj), fmaf(o[nt][j][1][2 + e], f, zj));
+                if (g < p.G) *reinterpret_cast<float4*>(s_o + (warp * p.G + g) * PI_HEAD_DIM + 32 * j + 4 * r) = v;
             }
-            if (g < p.G && (!DUP || c < 2) && r == 0) { s_m[warp * p.G + g] = m[nt][e]; s_l[warp * p.G + g] = sum; }
+            if (g < p.G && r == 0) { s_m[warp * p.G + g] = m[nt][e]; s_l[warp * p.G + g] = sum; }
         }
     __syncthreads();
 
-    // ---- the eight warps' states into one: s_o [0][G][128] of this CTA, s_m / s_l [0][G]
-    const int n_out = p.G * PI_HEAD_DIM;
-    auto write_out = [&](int i, float M, float L, float v) {
-        const int g = i >> 7, d = i & 127;
-        const size_t row = static_cast<size_t>(seq) * p.Hq + static_cast<size_t>(h) * p.G + g;
-        p.out[row * PI_HEAD_DIM + d] = __float2bfloat16_rn(L > 0.f ? v / L : 0.f);
-        if (p.lse && d == 0) p.lse[row] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
-    };
-    for (int i = tid; i < n_out; i += A4_THREADS) {
-        const int g = i >> 7;
-        float M = -INFINITY, L = 0.f, v = 0.f;
+    // ---- the warps' states into one: their factors first, once per head, then four channels a thread.  The result goes
+    // out, or, where a cluster shares the item, to s_o [0][G][128] (a thread's own places of warp 0's part, which nobody else
+    // reads) with the maximum and the sum in s_m / s_l behind the warps'.
+    const int n_quads = p.G * (PI_HEAD_DIM / 4);
+    for (int g = warp; g < p.G; g += A4_WARPS) {
+        const float mk = lane < A4_WARPS ? s_m[lane * p.G + g] : A4_NO_MAX;
+        float M = mk;
 #pragma unroll
-        for (int k = 0; k < A4_WARPS; ++k) M = fmaxf(M, s_m[k * p.G + g]);
+        for (int d = A4_WARPS / 2; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+        const float a = lane < A4_WARPS ? ex2(mk - M) : 0.f;
+        float L = lane < A4_WARPS ? a * s_l[lane * p.G + g] : 0.f;
+#pragma unroll
+        for (int d = A4_WARPS / 2; d; d >>= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
+        __syncwarp();
+        if (lane < A4_WARPS) s_m[lane * p.G + g] = a;
+        if (lane == 0) { s_l[A4_WARPS * p.G + g] = M; s_l[A4_WARPS * p.G + p.G + g] = L; }
+    }
+    __syncthreads();
+    auto write_out = [&](int i, float M, float L, float4 v) {
+        const int g = i >> 5, d = 4 * (i & 31);
+        const size_t row = static_cast<size_t>(seq) * p.Hq + static_cast<size_t>(h) * p.G + g;
+        const float f = L > 0.f ? 1.f / L : 0.f;
+        // (a NaN among the sums has to come through: 0 only where nothing was summed)
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x * f, v.y * f), hi = __floats2bfloat162_rn(v.z * f, v.w * f);
+        *reinterpret_cast<uint2*>(p.out + row * PI_HEAD_DIM + d) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+        if (p.lse && d == 0) p.lse[row] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : L == 0.f ? -INFINITY : L;
+    };
+    for (int i = tid; i < n_quads; i += A4_THREADS) {
+        const int g = i >> 5;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int k = 0; k < A4_WARPS; ++k) {
-            const float a = M == -INFINITY ? 0.f : exp2f(s_m[k * p.G + g] - M);
-            L = fmaf(s_l[k * p.G + g], a, L);
-            v = fmaf(s_o[k * n_out + i], a, v);
+            const float a = s_m[k * p.G + g];
+            const float4 x = reinterpret_cast<const float4*>(s_o)[k * n_quads + i];
+            v.x = fmaf(x.x, a, v.x); v.y = fmaf(x.y, a, v.y); v.z = fmaf(x.z, a, v.z); v.w = fmaf(x.w, a, v.w);
         }
-        if (S == 1) write_out(i, M, L, v);
-        else {
-            // one thread's own places of warp 0's part, which only it reads; M and L behind all parts
-            s_o[i] = v;
-            if ((i & 127) == 0) { s_l[A4_WARPS * p.G + g] = M; s_l[A4_WARPS * p.G + p.G + g] = L; }
-        }
+        if (S == 1) write_out(i, s_l[A4_WARPS * p.G + g], s_l[A4_WARPS * p.G + p.G + g], v);
+        else reinterpret_cast<float4*>(s_o)[i] = v;
     }
     if (S == 1) return;
     __syncwarp();
     // ---- and the cluster's: every CTA concludes its share of the outputs, reading the others' shared memory
     cluster_sync_all();
     const uint32_t at_o = smem_u32(s_o), at_m = smem_u32(s_l + A4_WARPS * p.G), at_l = at_m + 4 * p.G;
-    for (int i = rank * A4_THREADS + tid; i < n_out; i += S * A4_THREADS) {
-        const int g = i >> 7;
-        float M = -INFINITY, L = 0.f, v = 0.f;
+    for (int i = rank * A4_THREADS + tid; i < n_quads; i += S * A4_THREADS) {
+        const int g = i >> 5;
+        float M = A4_NO_MAX, L = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int k = 0; k < S; ++k) M = fmaxf(M, ld_shared_cluster_f32(map_shared_rank(at_m + 4 * g, k)));
         for (int k = 0; k < S; ++k) {
-            const float mk = ld_shared_cluster_f32(map_shared_rank(at_m + 4 * g, k));
-            const float a = M == -INFINITY ? 0.f : exp2f(mk - M);
+            const float a = ex2(ld_shared_cluster_f32(map_shared_rank(at_m + 4 * g, k)) - M);
             L = fmaf(ld_shared_cluster_f32(map_shared_rank(at_l + 4 * g, k)), a, L);
-            v = fmaf(ld_shared_cluster_f32(map_shared_rank(at_o + 4 * i, k)), a, v);
+            const float4 x = ld_shared_cluster_f32x4(map_shared_rank(at_o + 16 * i, k));
+            v.x = fmaf(x.x, a, v.x); v.y = fmaf(x.y, a, v.y); v.z = fmaf(x.z, a, v.z); v.w = fmaf(x.w, a, v.w);
         }
         write_out(i, M, L, v);
     }
@@ -379,12 +552,12 @@ int pi_launch_attn_kv4(pi_ctx* c, int batch, const void* q, const void* pool, co
     p.scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(PI_HEAD_DIM));
     p.Hq = cfg.n_q_heads; p.Hkv = cfg.n_kv_heads; p.G = cfg.n_q_heads / cfg.n_kv_heads;
     p.B = cfg.block_tokens; p.K = cfg.budget_blocks; p.C = cfg.pool_slots;
-    // CTAs per item: as many as fill the GPU with two CTAs per SM, as long as every warp still has a tile
-    const long long items = static_cast<long long>(batch) * cfg.n_kv_heads, slots = 2ll * c->n_sms;
+    // CTAs per item: as many as fill the GPU with what fits an SM, as long as every warp still has a tile
+    const long long items = static_cast<long long>(batch) * cfg.n_kv_heads, slots = static_cast<long long>(a4_ctas_per_sm(p.G <= 8 ? 1 : 2)) * c->n_sms;
     const int tiles = cfg.budget_blocks * (cfg.block_tokens / 16);
     int split = 1;
     while (split < 8 && items * split * 2 <= slots && tiles >= split * 2 * A4_WARPS) split *= 2;
-    const size_t ring = static_cast<size_t>(A4_WARPS) * A4_STAGES * KV4_TILE_BYTES;
+    const size_t ring = static_cast<size_t>(A4_WARPS) * A4_STAGES * KV4_TILE_BYTES + (p.G <= 8 ? 1 : 2) * (4 * 32 * 16 + 3 * 32 * 4 + 8 * 4);
     const size_t merge = (static_cast<size_t>(A4_WARPS) * p.G * (PI_HEAD_DIM + 2) + 2 * p.G) * sizeof(float);
     const size_t smem = ring > merge ? ring : merge;
     auto launch = [&](auto kernel) -> int {
@@ -406,7 +579,6 @@ int pi_launch_attn_kv4(pi_ctx* c, int batch, const void* q, const void* pool, co
         PI_CUDA_TRY(cudaLaunchKernelEx(&lc, kernel, p));
         return PI_OK;
     };
-    if (p.G <= 4) return launch(attn_kv4_kernel<1, true>);
-    if (p.G <= 8) return launch(attn_kv4_kernel<1, false>);
-    return launch(attn_kv4_kernel<2, false>);
+    if (p.G <= 8) return launch(attn_kv4_kernel<1>);
+    return launch(attn_kv4_kernel<2>);
 }
