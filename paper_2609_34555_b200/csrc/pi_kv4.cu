@@ -16,7 +16,7 @@ struct StoreParams {
     unsigned char* store;
     pi_status_ref st;
     long long n_items, block_bytes, n_slots;
-    int inner, H, shift;                            // B = 1 << shift
+    int inner, log_h, shift;                        // Hkv = 1 << log_h, B = 1 << shift
 };
 
 // Half a warp takes the K row of a (token, head), the other half its V row; consecutive items are the heads of a token,
@@ -26,6 +26,7 @@ kv4_store_kernel(StoreParams p) {
     const int lane = threadIdx.x & 31, l = lane & 15;
     const bool is_v = lane >> 4;
     const long long first = (static_cast<long long>(blockIdx.x) * KV4_WARPS + (threadIdx.x >> 5)) * KV4_UNROLL;
+    const int heads = (1 << p.log_h) - 1, rows = (1 << p.shift) - 1;
     pi_grid_dependency_wait();
     pi_launch_dependents();
     uint4 x[KV4_UNROLL];
@@ -36,8 +37,9 @@ kv4_store_kernel(StoreParams p) {
         x[u] = make_uint4(0, 0, 0, 0);
         slot[u] = -1;
         if (item < p.n_items) {
-            const int t = static_cast<int>(item / p.H), h = static_cast<int>(item - static_cast<long long>(t) * p.H);
-            const long long outer = p.inner ? t / p.inner : 0, in = p.inner ? t % p.inner : t;
+            const int t = static_cast<int>(item >> p.log_h), h = static_cast<int>(item) & heads;
+            int outer = 0, in = t;
+            if (p.inner) { outer = t / p.inner; in = t - outer * p.inner; }
             slot[u] = p.slots ? p.slots[t] : t;
             const __nv_bfloat16* src = is_v ? p.v + outer * p.v_outer + in * p.v_tok + h * p.v_head
                                             : p.k + outer * p.k_outer + in * p.k_tok + h * p.k_head;
@@ -49,15 +51,15 @@ kv4_store_kernel(StoreParams p) {
         uint32_t codes, sz;
         kv4_quantise(x[u], codes, sz);
         const long long item = first + u;
+        const int h = static_cast<int>(item) & heads;
         bool write = slot[u] >= 0;
         if (write && slot[u] >= p.n_slots) {
-            if (lane == 0) pi_report(p.st, PI_ERR_INDEX_RANGE, PI_STAGE_KV4, static_cast<int>(item / p.H), static_cast<int>(item % p.H), static_cast<int>(min(slot[u], 0x7fffffffLL)));
+            if (lane == 0) pi_report(p.st, PI_ERR_INDEX_RANGE, PI_STAGE_KV4, static_cast<int>(item >> p.log_h), h, static_cast<int>(min(slot[u], 0x7fffffffLL)));
             write = false;
         }
         const long long s = write ? slot[u] : 0;
-        const int at = static_cast<int>(s & ((1 << p.shift) - 1)), h = static_cast<int>(item % p.H);
-        unsigned char* tile = p.store + (s >> p.shift) * p.block_bytes +
-                              (static_cast<long long>(h) << (p.shift - 4)) * KV4_TILE_BYTES + (at >> 4) * KV4_TILE_BYTES;
+        const int at = static_cast<int>(s) & rows;
+        unsigned char* tile = p.store + (s >> p.shift) * p.block_bytes + ((h << (p.shift - 4)) + (at >> 4)) * KV4_TILE_BYTES;
         kv4_write_row(tile, at & 15, is_v, l, codes, sz, write);
     }
 }
@@ -68,51 +70,66 @@ struct LoadParams {
     uint4* out;                                     // [n_out][Hkv][2][B][D] bf16, 16 uint4 a row
     pi_status_ref st;
     long long n_items, block_bytes, n_blocks;       // an item is a (block, head, tile)
-    int tiles, H, B;
+    int log_tiles, log_h, B;
 };
 
-// One warp a tile; lanes 0..15 take a K row, lanes 16..31 the V row of the same token, 16 bytes of output a lane.
+// Eight channels of a row: the codes of `w` (nibble i = channel i) times the scale plus the minimum of `sz`.  0x4300 | code
+// is the bf16 number 128 + code; a fused multiply-add of bf16 pairs rounds once, from the exact value.
+__device__ __forceinline__ uint4 kv4_eight(uint32_t w, uint32_t sz) {
+    const uint32_t s2 = __byte_perm(sz, sz, 0x1010), z2 = __byte_perm(sz, sz, 0x3232);
+    const __nv_bfloat162 less = __halves2bfloat162(__ushort_as_bfloat16(0xc300), __ushort_as_bfloat16(0xc300));     // -128
+    uint32_t p[4];                                  // channels (n, n + 4)
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        const uint32_t raised = ((w >> (4 * n)) & 0x000f000fu) | 0x43004300u;
+        const __nv_bfloat162 v = __hfma2(__hadd2(*reinterpret_cast<const __nv_bfloat162*>(&raised), less),
+                                         *reinterpret_cast<const __nv_bfloat162*>(&s2), *reinterpret_cast<const __nv_bfloat162*>(&z2));
+        p[n] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+    return make_uint4(__byte_perm(p[0], p[1], 0x5410), __byte_perm(p[2], p[3], 0x5410), __byte_perm(p[0], p[1], 0x7632), __byte_perm(p[2], p[3], 0x7632));
+}
+
+// One warp a tile: four lanes a row, each 16 bytes of codes (the same eight channels of all four groups), all loads of the
+// tile before the first store.
 __global__ void __launch_bounds__(KV4_THREADS)
 kv4_load_kernel(LoadParams p) {
-    const int lane = threadIdx.x & 31, l = lane & 15;
-    const bool is_v = lane >> 4;
+    const int lane = threadIdx.x & 31, row = lane >> 2, c = lane & 3;
     const long long item = static_cast<long long>(blockIdx.x) * KV4_WARPS + (threadIdx.x >> 5);
     pi_grid_dependency_wait();
     pi_launch_dependents();
     if (item >= p.n_items) return;
-    const int tile = static_cast<int>(item % p.tiles), h = static_cast<int>(item / p.tiles % p.H);
-    const long long i = item / p.tiles / p.H;
+    const int tile = static_cast<int>(item) & ((1 << p.log_tiles) - 1), h = static_cast<int>(item >> p.log_tiles) & ((1 << p.log_h) - 1);
+    const long long i = item >> (p.log_tiles + p.log_h);
     const long long block = p.blocks ? p.blocks[i] : i;
     if (block < 0 || block >= p.n_blocks) {
         if (lane == 0 && tile == 0 && h == 0) pi_report(p.st, PI_ERR_INDEX_RANGE, PI_STAGE_KV4, static_cast<int>(min(i, 0x7fffffffLL)), 0, static_cast<int>(block));
         return;
     }
-    const unsigned char* src = p.store + block * p.block_bytes + (static_cast<long long>(h) * p.tiles + tile) * KV4_TILE_BYTES;
-    uint4* dst = p.out + (((i * p.H + h) * 2 + (is_v ? 1 : 0)) * p.B + tile * 16) * 16 + l;
-    const int j = l >> 2, c = l & 3;
-    const unsigned char* codes = src + (is_v ? KV4_V_CODES + 16 * c + 2 * j : 16 * c + 4 * j);
-    const unsigned char* scales = src + (is_v ? KV4_V_SCALES : KV4_K_SCALES) + 4 * j;
-#pragma unroll 8
-    for (int t = 0; t < 16; ++t) {
-        uint32_t w;
-        if (is_v) {      // channels 8 c .. 8 c + 3 of group j sit at byte 16 c + 2 j, the next four 8 bytes further on
-            w = *reinterpret_cast<const uint16_t*>(codes + t * 64) |
-                (static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(codes + t * 64 + 8)) << 16);
-        } else {
-            w = *reinterpret_cast<const uint32_t*>(codes + t * 64);
-        }
-        const uint32_t sz = *reinterpret_cast<const uint32_t*>(scales + t * 16);
-        const float s = kv4_scale_of(sz), z = kv4_min_of(sz);
-        uint32_t o[4];
+    const unsigned char* src = p.store + block * p.block_bytes + ((h << p.log_tiles) + tile) * KV4_TILE_BYTES;
+    uint4* dst = p.out + (((((i << p.log_h) + h) * 2) * p.B + tile * 16 + row) * 16 + c);
+    uint4 codes[4], scales[4];                      // K rows 0..7, 8..15, then V
 #pragma unroll
-        for (int i2 = 0; i2 < 4; ++i2) {
-            // scale * code has at most 12 bits and is exact: one rounding in the sum, one to bf16
-            const float a = fmaf(s, static_cast<float>((w >> (8 * i2)) & 15u), z), b = fmaf(s, static_cast<float>((w >> (8 * i2 + 4)) & 15u), z);
-            const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-            o[i2] = *reinterpret_cast<const uint32_t*>(&v);
-        }
-        dst[t * 16] = make_uint4(o[0], o[1], o[2], o[3]);
+    for (int u = 0; u < 4; ++u) {
+        codes[u] = *reinterpret_cast<const uint4*>(src + (u >> 1) * KV4_V_CODES + ((u & 1) * 8 + row) * 64 + c * 16);
+        scales[u] = *reinterpret_cast<const uint4*>(src + KV4_K_SCALES + (u >> 1) * (KV4_V_SCALES - KV4_K_SCALES) + ((u & 1) * 8 + row) * 16);
     }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const uint32_t x[4] = {codes[u].x, codes[u].y, codes[u].z, codes[u].w}, sz[4] = {scales[u].x, scales[u].y, scales[u].z, scales[u].w};
+        uint4* to = dst + (static_cast<long long>(u >> 1) * p.B + (u & 1) * 8) * 16;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            // a K chunk is four words, one a group; a V chunk two runs of four halves, channels 0..3 and 4..7 of the eight
+            const uint32_t w = u < 2 ? x[j] : __byte_perm(x[j >> 1], x[2 + (j >> 1)], (j & 1) ? 0x7632 : 0x5410);
+            to[4 * j] = kv4_eight(w, sz[j]);
+        }
+    }
+}
+
+int log2_of(int x) {
+    int n = 0;
+    while ((1 << n) < x) ++n;
+    return n;
 }
 
 }  // namespace
@@ -126,12 +143,12 @@ int pi_launch_kv4_store(pi_ctx* c, int64_t n_tokens, const void* k, const int64_
     p.slots = slots;
     p.store = static_cast<unsigned char*>(store);
     p.st = pi_status_of(c);
-    p.H = c->cfg.n_kv_heads;
-    p.n_items = n_tokens * p.H;
+    p.log_h = log2_of(c->cfg.n_kv_heads);           // (a power of two: pi_create)
+    p.n_items = n_tokens * c->cfg.n_kv_heads;
     p.block_bytes = kv4_block_bytes(c->cfg.n_kv_heads, c->cfg.block_tokens);
     p.n_slots = n_blocks * c->cfg.block_tokens;
     p.inner = inner;
-    p.shift = c->cfg.block_tokens == 16 ? 4 : c->cfg.block_tokens == 32 ? 5 : 6;
+    p.shift = log2_of(c->cfg.block_tokens);
     const long long per_cta = KV4_WARPS * KV4_UNROLL;
     PI_CUDA_TRY(pi_launch_pdl(kv4_store_kernel, dim3(static_cast<unsigned>((p.n_items + per_cta - 1) / per_cta)), dim3(KV4_THREADS), 0, stream, p));
     return PI_OK;
@@ -143,8 +160,9 @@ int pi_launch_kv4_load(pi_ctx* c, int64_t n_out, const void* store, int64_t n_bl
     p.blocks = blocks;
     p.out = static_cast<uint4*>(out);
     p.st = pi_status_of(c);
-    p.H = c->cfg.n_kv_heads; p.B = c->cfg.block_tokens; p.tiles = p.B / 16;
-    p.n_items = n_out * p.H * p.tiles;
+    p.B = c->cfg.block_tokens;
+    p.log_h = log2_of(c->cfg.n_kv_heads); p.log_tiles = log2_of(p.B / 16);
+    p.n_items = n_out << (p.log_h + p.log_tiles);
     p.block_bytes = kv4_block_bytes(c->cfg.n_kv_heads, c->cfg.block_tokens);
     p.n_blocks = n_blocks;
     PI_CUDA_TRY(pi_launch_pdl(kv4_load_kernel, dim3(static_cast<unsigned>((p.n_items + KV4_WARPS - 1) / KV4_WARPS)), dim3(KV4_THREADS), 0, stream, p));

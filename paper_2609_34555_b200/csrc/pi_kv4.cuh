@@ -52,10 +52,26 @@ __device__ __forceinline__ void kv4_quantise(uint4 x, uint32_t& codes, uint32_t&
     const __nv_bfloat162 pair = __halves2bfloat162(sb, __low2bfloat16(mm));
     sz = *reinterpret_cast<const uint32_t*>(&pair);
     codes = 0;
+    if (__all_sync(0xffffffffu, s == 0.f || (s >= 0x1p-100f && s <= 0x1p100f))) {
+        // Correctly rounded quotients by one divisor, after Markstein (Computation of elementary functions on the IBM RISC
+        // System/6000 processor, 1990): q = d r with r = 1/s rounded, then q + (d - q s) r, the bracket being exact in a
+        // fused operation.  Seven operations a value where a division of its own takes three times as many; the sum with
+        // 1.5 * 2^23 rounds to the nearest whole number, ties to even, and leaves it in the low bits.
+        const float r = s > 0.f ? __frcp_rn(s) : 0.f;              // no spread: code 0
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float v = (i & 1) ? __high2float(h[i >> 1]) : __low2float(h[i >> 1]);
+            const float d = __fsub_rn(v, lo), q = __fmul_rn(d, r);
+            const float c = __fmaf_rn(__fmaf_rn(-q, s, d), r, q);  // at most 15 (1 + 2^-8): the scale is rounded to 8 bits
+            codes += __float_as_uint(__fadd_rn(c, 12582912.f)) << (4 * i);
+        }
+        codes -= 0x3f400000u;                                      // what 0x4b400000, shifted by 0, 4 and 8, adds up to
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float v = (i & 1) ? __high2float(h[i >> 1]) : __low2float(h[i >> 1]);
-        // a group without spread (scale 0) has code 0; fmaxf takes the 0 where the quotient is not a number
+        // fmaxf takes the 0 where the quotient is not a number
         const float c = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(v, lo), s)), 0.f), 15.f);
         codes |= static_cast<uint32_t>(s > 0.f ? c : 0.f) << (4 * i);
     }
