@@ -113,15 +113,19 @@ append_kernel(AppendParams p) {
     }
     if (tid == 0) slot_stamp[slot] = p.step_dev ? *p.step_dev : p.step;
     if (KV4) {
-        // half a warp a row: the K row of a head in lanes 0..15, its V row in lanes 16..31
-        const bool is_v = lane >> 4;
-        const int l = lane & 15;
-        for (int h = warp; h < p.Hkv; h += APPEND_WARPS) {
-            uint32_t codes, sz;
-            kv4_quantise((is_v ? p.v_new : p.k_new)[(static_cast<size_t>(seq) * p.Hkv + h) * 16 + l], codes, sz);
+        // eight lanes a row, a warp the K and V rows of two heads
+        const bool is_v = lane & 8;
+        const int l = lane & 7;
+        for (int h0 = 2 * warp; h0 < p.Hkv; h0 += 2 * APPEND_WARPS) {
+            const int h = min(h0 + (lane >> 4), p.Hkv - 1);
+            const uint4* src = (is_v ? p.v_new : p.k_new) + (static_cast<size_t>(seq) * p.Hkv + h) * 16 + 2 * l;
+            const uint4 x[2] = {src[0], src[1]};
+            uint32_t codes[2], sz;
+            kv4_quantise(x, codes, sz);
             const long long off = (static_cast<long long>(h) * (p.B >> 4) + (t >> 4)) * KV4_TILE_BYTES;
-            kv4_write_row(pool_blk + off, t & 15, is_v, l, codes, sz, true);
-            kv4_write_row(host_blk + off, t & 15, is_v, l, codes, sz, true);
+            const bool write = h0 + (lane >> 4) < p.Hkv;
+            kv4_write_row(pool_blk + off, t & 15, is_v, l, codes, sz, write);
+            kv4_write_row(host_blk + off, t & 15, is_v, l, codes, sz, write);
         }
     } else
     // rows: [Hkv][2][B][D]; one head row is 256 B = 16 uint4

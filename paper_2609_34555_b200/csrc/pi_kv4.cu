@@ -6,7 +6,8 @@ namespace {
 
 constexpr int KV4_THREADS = 256;
 constexpr int KV4_WARPS = KV4_THREADS / 32;
-constexpr int KV4_UNROLL = 4;                       // (token, head) items a warp has in flight: 2 KB of loads
+constexpr int KV4_UNROLL = 2;                       // pairs of (token, head) items a warp has in flight: 2 KB of loads
+constexpr int KV4_ITEMS = 2 * KV4_UNROLL;
 
 struct StoreParams {
     const __nv_bfloat16* k;
@@ -19,48 +20,74 @@ struct StoreParams {
     int inner, log_h, shift;                        // Hkv = 1 << log_h, B = 1 << shift
 };
 
-// Half a warp takes the K row of a (token, head), the other half its V row; consecutive items are the heads of a token,
-// whose rows lie next to each other in the projections.
+// Eight lanes take a row, a warp the K and V rows of two (token, head) items at a time, KV4_ITEMS consecutive items in all:
+// heads of one token (ONE_TOKEN: Hkv is a multiple of KV4_ITEMS), whose rows lie next to each other in the projections, or
+// of several.
+template <bool ONE_TOKEN>
 __global__ void __launch_bounds__(KV4_THREADS)
 kv4_store_kernel(StoreParams p) {
-    const int lane = threadIdx.x & 31, l = lane & 15;
-    const bool is_v = lane >> 4;
-    const long long first = (static_cast<long long>(blockIdx.x) * KV4_WARPS + (threadIdx.x >> 5)) * KV4_UNROLL;
+    const int lane = threadIdx.x & 31, l = lane & 7;
+    const bool is_v = lane & 8;
+    const long long first = (static_cast<long long>(blockIdx.x) * KV4_WARPS + (threadIdx.x >> 5)) * KV4_ITEMS;
     const int heads = (1 << p.log_h) - 1, rows = (1 << p.shift) - 1;
+    const __nv_bfloat16* base = (is_v ? p.v : p.k) + 16 * l;
+    const long long s_tok = is_v ? p.v_tok : p.k_tok, s_head = is_v ? p.v_head : p.k_head, s_outer = is_v ? p.v_outer : p.k_outer;
     pi_grid_dependency_wait();
     pi_launch_dependents();
-    uint4 x[KV4_UNROLL];
-    long long slot[KV4_UNROLL];
-#pragma unroll
-    for (int u = 0; u < KV4_UNROLL; ++u) {
-        const long long item = first + u;
-        x[u] = make_uint4(0, 0, 0, 0);
-        slot[u] = -1;
-        if (item < p.n_items) {
-            const int t = static_cast<int>(item >> p.log_h), h = static_cast<int>(item) & heads;
-            int outer = 0, in = t;
-            if (p.inner) { outer = t / p.inner; in = t - outer * p.inner; }
-            slot[u] = p.slots ? p.slots[t] : t;
-            const __nv_bfloat16* src = is_v ? p.v + outer * p.v_outer + in * p.v_tok + h * p.v_head
-                                            : p.k + outer * p.k_outer + in * p.k_tok + h * p.k_head;
-            x[u] = __ldg(reinterpret_cast<const uint4*>(src) + l);
+    auto row_of = [&](long long item) {
+        const int t = static_cast<int>(item >> p.log_h);
+        int outer = 0, in = t;
+        if (p.inner) { outer = t / p.inner; in = t - outer * p.inner; }
+        return base + outer * s_outer + in * s_tok + (static_cast<int>(item) & heads) * s_head;
+    };
+    auto slot_of = [&](long long item) -> long long { const int t = static_cast<int>(item >> p.log_h); return p.slots ? p.slots[t] : t; };
+    // the tile of a slot for head 0, nullptr where nothing is to be written
+    auto tile_of = [&](long long item, long long s) -> unsigned char* {
+        if (s < 0) return nullptr;
+        if (s >= p.n_slots) {
+            if (l == 0) pi_report(p.st, PI_ERR_INDEX_RANGE, PI_STAGE_KV4, static_cast<int>(item >> p.log_h), static_cast<int>(item) & heads, static_cast<int>(min(s, 0x7fffffffLL)));
+            return nullptr;
         }
-    }
+        return p.store + (s >> p.shift) * p.block_bytes + ((static_cast<int>(s) & rows) >> 4) * KV4_TILE_BYTES;
+    };
+    const int head_bytes = KV4_TILE_BYTES << (p.shift - 4);
+    const long long mine = first + (lane >> 4);                  // this lane's items: mine, mine + 2, ...
+    uint4 x[KV4_UNROLL][2];
+    if (ONE_TOKEN) {
+        if (first >= p.n_items) return;
+        const __nv_bfloat16* src = row_of(mine);
 #pragma unroll
-    for (int u = 0; u < KV4_UNROLL; ++u) {
-        uint32_t codes, sz;
-        kv4_quantise(x[u], codes, sz);
-        const long long item = first + u;
-        const int h = static_cast<int>(item) & heads;
-        bool write = slot[u] >= 0;
-        if (write && slot[u] >= p.n_slots) {
-            if (lane == 0) pi_report(p.st, PI_ERR_INDEX_RANGE, PI_STAGE_KV4, static_cast<int>(item >> p.log_h), h, static_cast<int>(min(slot[u], 0x7fffffffLL)));
-            write = false;
+        for (int u = 0; u < KV4_UNROLL; ++u) {
+            x[u][0] = __ldg(reinterpret_cast<const uint4*>(src + 2 * u * s_head));
+            x[u][1] = __ldg(reinterpret_cast<const uint4*>(src + 2 * u * s_head) + 1);
         }
-        const long long s = write ? slot[u] : 0;
-        const int at = static_cast<int>(s) & rows;
-        unsigned char* tile = p.store + (s >> p.shift) * p.block_bytes + ((h << (p.shift - 4)) + (at >> 4)) * KV4_TILE_BYTES;
-        kv4_write_row(tile, at & 15, is_v, l, codes, sz, write);
+        const long long slot = slot_of(first);
+        unsigned char* tile = tile_of(first, slot);
+        const bool write = tile != nullptr;
+        tile += (static_cast<int>(mine) & heads) * head_bytes;
+#pragma unroll
+        for (int u = 0; u < KV4_UNROLL; ++u) {
+            uint32_t codes[2], sz;
+            kv4_quantise(x[u], codes, sz);
+            kv4_write_row(tile + 2 * u * head_bytes, static_cast<int>(slot) & 15, is_v, l, codes, sz, write);
+        }
+    } else {
+        long long slot[KV4_UNROLL];
+#pragma unroll
+        for (int u = 0; u < KV4_UNROLL; ++u) {
+            const bool has = mine + 2 * u < p.n_items;
+            const uint4* src = has ? reinterpret_cast<const uint4*>(row_of(mine + 2 * u)) : nullptr;
+            x[u][0] = has ? __ldg(src) : make_uint4(0, 0, 0, 0);
+            x[u][1] = has ? __ldg(src + 1) : make_uint4(0, 0, 0, 0);
+            slot[u] = has ? slot_of(mine + 2 * u) : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < KV4_UNROLL; ++u) {
+            uint32_t codes[2], sz;
+            kv4_quantise(x[u], codes, sz);
+            unsigned char* tile = tile_of(mine + 2 * u, slot[u]);
+            kv4_write_row(tile + (static_cast<int>(mine + 2 * u) & heads) * head_bytes, static_cast<int>(slot[u]) & 15, is_v, l, codes, sz, tile != nullptr);
+        }
     }
 }
 
@@ -149,8 +176,8 @@ int pi_launch_kv4_store(pi_ctx* c, int64_t n_tokens, const void* k, const int64_
     p.n_slots = n_blocks * c->cfg.block_tokens;
     p.inner = inner;
     p.shift = log2_of(c->cfg.block_tokens);
-    const long long per_cta = KV4_WARPS * KV4_UNROLL;
-    PI_CUDA_TRY(pi_launch_pdl(kv4_store_kernel, dim3(static_cast<unsigned>((p.n_items + per_cta - 1) / per_cta)), dim3(KV4_THREADS), 0, stream, p));
+    const long long per_cta = KV4_WARPS * KV4_ITEMS;
+    PI_CUDA_TRY(pi_launch_pdl(c->cfg.n_kv_heads % KV4_ITEMS == 0 ? kv4_store_kernel<true> : kv4_store_kernel<false>, dim3(static_cast<unsigned>((p.n_items + per_cta - 1) / per_cta)), dim3(KV4_THREADS), 0, stream, p));
     return PI_OK;
 }
 

@@ -30,69 +30,82 @@ static inline int64_t kv4_block_bytes(int n_kv_heads, int block_tokens) {
 }
 
 #ifdef __CUDACC__
-// Codes and scale word of one row; 16 neighbouring lanes (aligned) hold the row, lane l of them channels 8 l .. 8 l + 7
-// in `x`.  codes: nibble i = channel 8 l + i.  sz: scale | minimum << 16 of the lane's group (lanes 4 j .. 4 j + 3).
-// All 32 lanes must call.
-__device__ __forceinline__ void kv4_quantise(uint4 x, uint32_t& codes, uint32_t& sz) {
-    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&x);
-    const __nv_bfloat162 mn2 = __hmin2_nan(__hmin2_nan(h[0], h[1]), __hmin2_nan(h[2], h[3]));
-    const __nv_bfloat162 mx2 = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
-    // {minimum, maximum} of the lane, then of the group's four lanes
-    __nv_bfloat162 mm = __halves2bfloat162(__hmin_nan(__low2bfloat16(mn2), __high2bfloat16(mn2)),
-                                           __hmax_nan(__low2bfloat16(mx2), __high2bfloat16(mx2)));
+// Codes and scale word of one row; 8 neighbouring lanes (aligned) hold the row, lane l of them channels 16 l .. 16 l + 15
+// in `x`.  codes: nibble i of word k = channel 16 l + 8 k + i.  sz: scale | minimum << 16 of the lane's group (lanes 2 j and
+// 2 j + 1).  All 32 lanes must call.
+__device__ __forceinline__ void kv4_quantise(const uint4 (&x)[2], uint32_t (&codes)[2], uint32_t& sz) {
+    const uint32_t xs[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(xs);
+    __nv_bfloat162 mn = __hmin2_nan(__hmin2_nan(__hmin2_nan(h[0], h[1]), __hmin2_nan(h[2], h[3])), __hmin2_nan(__hmin2_nan(h[4], h[5]), __hmin2_nan(h[6], h[7])));
+    __nv_bfloat162 mx = __hmax2_nan(__hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3])), __hmax2_nan(__hmax2_nan(h[4], h[5]), __hmax2_nan(h[6], h[7])));
+    mn = __hmin2_nan(mn, __lowhigh2highlow(mn));
+    mx = __hmax2_nan(mx, __lowhigh2highlow(mx));
+    // {minimum, -maximum} of the lane, then of the group's two lanes: one minimum of pairs
+    uint32_t pair = __byte_perm(*reinterpret_cast<uint32_t*>(&mn), *reinterpret_cast<uint32_t*>(&mx), 0x5410) ^ 0x80000000u;
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, pair, 1);
+    const __nv_bfloat162 m = __hmin2_nan(*reinterpret_cast<const __nv_bfloat162*>(&pair), *reinterpret_cast<const __nv_bfloat162*>(&other));
+    pair = *reinterpret_cast<const uint32_t*>(&m);
+    const float lo = __uint_as_float(pair << 16);
+    const float spread = __fsub_rn(-__uint_as_float(pair & 0xffff0000u), lo);
+    codes[0] = codes[1] = 0;
+    if (__all_sync(0xffffffffu, spread == 0.f || (spread >= 0x1p-96f && spread <= 0x1p96f))) {
+        // Quotients after Markstein (Computation of elementary functions on the IBM RISC System/6000 processor, 1990):
+        // q = d r with r about 1 / s, then q + (d - q s) r, the bracket being exact in a fused operation.  A quotient that is
+        // representable, as the borders between two codes are, comes out exactly.  The sum with 1.5 * 2^23 rounds to the
+        // nearest whole number, ties to even, and leaves it in the low bits.  Seven operations a value; a division of its
+        // own takes three times as many.
+        const float fifteenth = 0.066666670143604278564f;
+        const float q15 = __fmul_rn(spread, fifteenth);
+        const __nv_bfloat16 sb = __float2bfloat16_rn(__fmaf_rn(__fmaf_rn(-q15, 15.f, spread), fifteenth, q15));
+        const float s = __bfloat162float(sb);
+        sz = __byte_perm(__bfloat16_as_ushort(sb), pair, 0x5410);
+        const float r = spread > 0.f ? __fdividef(1.f, s) : 0.f;   // no spread: code 0
 #pragma unroll
-    for (int o = 1; o <= 2; o <<= 1) {
-        const __nv_bfloat162 other = __shfl_xor_sync(0xffffffffu, mm, o);
-        mm = __halves2bfloat162(__hmin_nan(__low2bfloat16(mm), __low2bfloat16(other)),
-                                __hmax_nan(__high2bfloat16(mm), __high2bfloat16(other)));
-    }
-    const float lo = __low2float(mm);
-    const __nv_bfloat16 sb = __float2bfloat16_rn(__fdiv_rn(__fsub_rn(__high2float(mm), lo), 15.f));
-    const float s = __bfloat162float(sb);
-    const __nv_bfloat162 pair = __halves2bfloat162(sb, __low2bfloat16(mm));
-    sz = *reinterpret_cast<const uint32_t*>(&pair);
-    codes = 0;
-    if (__all_sync(0xffffffffu, s == 0.f || (s >= 0x1p-100f && s <= 0x1p100f))) {
-        // Correctly rounded quotients by one divisor, after Markstein (Computation of elementary functions on the IBM RISC
-        // System/6000 processor, 1990): q = d r with r = 1/s rounded, then q + (d - q s) r, the bracket being exact in a
-        // fused operation.  Seven operations a value where a division of its own takes three times as many; the sum with
-        // 1.5 * 2^23 rounds to the nearest whole number, ties to even, and leaves it in the low bits.
-        const float r = s > 0.f ? __frcp_rn(s) : 0.f;              // no spread: code 0
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float v = (i & 1) ? __high2float(h[i >> 1]) : __low2float(h[i >> 1]);
+        for (int i = 0; i < 16; ++i) {
+            const float v = __uint_as_float((i & 1) ? xs[i >> 1] & 0xffff0000u : xs[i >> 1] << 16);
             const float d = __fsub_rn(v, lo), q = __fmul_rn(d, r);
             const float c = __fmaf_rn(__fmaf_rn(-q, s, d), r, q);  // at most 15 (1 + 2^-8): the scale is rounded to 8 bits
-            codes += __float_as_uint(__fadd_rn(c, 12582912.f)) << (4 * i);
+            codes[i >> 3] += __float_as_uint(__fadd_rn(c, 12582912.f)) << (4 * (i & 7));
         }
-        codes -= 0x3f400000u;                                      // what 0x4b400000, shifted by 0, 4 and 8, adds up to
+        codes[0] -= 0x3f400000u;                                   // what 0x4b400000, shifted by 0, 4 and 8, adds up to
+        codes[1] -= 0x3f400000u;
         return;
     }
+    const __nv_bfloat16 sb = __float2bfloat16_rn(__fdiv_rn(spread, 15.f));
+    const float s = __bfloat162float(sb);
+    sz = __byte_perm(__bfloat16_as_ushort(sb), pair, 0x5410);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float v = (i & 1) ? __high2float(h[i >> 1]) : __low2float(h[i >> 1]);
+    for (int i = 0; i < 16; ++i) {
+        const float v = __uint_as_float((i & 1) ? xs[i >> 1] & 0xffff0000u : xs[i >> 1] << 16);
         // fmaxf takes the 0 where the quotient is not a number
         const float c = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(v, lo), s)), 0.f), 15.f);
-        codes |= static_cast<uint32_t>(s > 0.f ? c : 0.f) << (4 * i);
+        codes[i >> 3] |= static_cast<uint32_t>(s > 0.f ? c : 0.f) << (4 * (i & 7));
     }
 }
 
-// Writes the row that 16 lanes hold (codes and scale words of kv4_quantise) to token `t` of the tile at `tile`.
-// is_v must be the same for the 16 lanes; all 32 lanes must call (`write` false: nothing is stored).
-__device__ __forceinline__ void kv4_write_row(unsigned char* tile, int t, bool is_v, int l, uint32_t codes, uint32_t sz, bool write) {
-    const int j = l >> 2, c = l & 3;
-    // a V row wants the 16-bit halves of lanes (j, c) and (j + 1, c) side by side: the even lane takes the low halves
-    // (channels 8 c .. 8 c + 3 of both groups), the odd one the high halves
-    const uint32_t other = __shfl_xor_sync(0xffffffffu, codes, 4);
-    uint32_t word = codes;
-    int at = 16 * c + 4 * j;
+// Where lane l of a row's eight puts its two words (the second kv4_step further on) and, for even l, its group's scales,
+// counted from the row's codes and scales.
+__device__ __forceinline__ int kv4_word_at(bool is_v, int l) { return is_v ? 32 * (l & 1) + 8 * (l & 2) + 4 * (l >> 2) : 32 * (l & 1) + 4 * (l >> 1); }
+__device__ __forceinline__ int kv4_step(bool is_v) { return is_v ? 8 : 16; }
+
+// Writes the row that eight lanes hold (codes and scale word of kv4_quantise) to token `t` of the tile at `tile`.  is_v
+// must be the same for the eight; all 32 lanes must call (`write` false: nothing is stored).
+__device__ __forceinline__ void kv4_write_row(unsigned char* tile, int t, bool is_v, int l, const uint32_t (&codes)[2], uint32_t sz, bool write) {
+    // a V row wants the 16-bit halves of two neighbouring groups (lanes l and l ^ 2) side by side: the lane of the even
+    // group takes the first word's, the other one the second's
+    const bool odd = l & 2;
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? codes[0] : codes[1], 2);
+    uint32_t w0 = codes[0], w1 = codes[1];
     if (is_v) {
-        word = (j & 1) ? __byte_perm(other, codes, 0x7632) : __byte_perm(codes, other, 0x5410);
-        at = 8 * (2 * c + (j & 1)) + 2 * (j & 2);
+        const uint32_t a = odd ? other : codes[0], b = odd ? codes[1] : other;
+        w0 = __byte_perm(a, b, 0x5410);
+        w1 = __byte_perm(a, b, 0x7632);
     }
     if (!write) return;
-    *reinterpret_cast<uint32_t*>(tile + (is_v ? KV4_V_CODES : 0) + t * 64 + at) = word;
-    if (c == 0) *reinterpret_cast<uint32_t*>(tile + (is_v ? KV4_V_SCALES : KV4_K_SCALES) + t * 16 + j * 4) = sz;
+    unsigned char* row = tile + (is_v ? KV4_V_CODES : 0) + t * 64 + kv4_word_at(is_v, l);
+    *reinterpret_cast<uint32_t*>(row) = w0;
+    *reinterpret_cast<uint32_t*>(row + kv4_step(is_v)) = w1;
+    if (!(l & 1)) *reinterpret_cast<uint32_t*>(tile + (is_v ? KV4_V_SCALES : KV4_K_SCALES) + t * 16 + 2 * l) = sz;
 }
 
 __device__ __forceinline__ float kv4_scale_of(uint32_t sz) { return __uint_as_float(sz << 16); }

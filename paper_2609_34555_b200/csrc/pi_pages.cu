@@ -29,26 +29,33 @@ struct PagesParams {
     int batch, n_pages, row_limit, shift;
 };
 
-// Block-wide exclusive scan, continued from `run`; all threads call.
-__device__ __forceinline__ long long scan_from(long long v, long long* warp_tot, long long& run) {
+// Block-wide exclusive scans of three values at once, continued from `run` (moved on); all threads call.
+__device__ __forceinline__ void scan_from(const long long (&v)[3], long long (&before)[3], long long (*warp_tot)[3], long long (&run)[3]) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    long long inc = v;
+    long long inc[3];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long t = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += t;
-    }
-    __syncthreads();
-    if (lane == 31) warp_tot[warp] = inc;
-    __syncthreads();
-    long long base = run, tot = 0;
+    for (int k = 0; k < 3; ++k) inc[k] = v[k];
 #pragma unroll
-    for (int i = 0; i < PAGES_WARPS; ++i) {
-        if (i < warp) base += warp_tot[i];
-        tot += warp_tot[i];
+    for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            const long long t = __shfl_up_sync(0xffffffffu, inc[k], o);
+            if (lane >= o) inc[k] += t;
+        }
+    __syncthreads();
+    if (lane == 31)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) warp_tot[warp][k] = inc[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        before[k] = run[k] + inc[k] - v[k];
+#pragma unroll
+        for (int i = 0; i < PAGES_WARPS; ++i) {
+            if (i < warp) before[k] += warp_tot[i][k];
+            run[k] += warp_tot[i][k];
+        }
     }
-    run += tot;
-    return base + inc - v;
 }
 
 // Last s with pref[s] <= i, for an ascending pref[0 .. n] with pref[0] = 0 and i < pref[n].
@@ -61,21 +68,21 @@ __device__ __forceinline__ int owner_of(const int* pref, int n, int i) {
     return lo;
 }
 
-__global__ void __launch_bounds__(PAGES_THREADS)
+__global__ void __launch_bounds__(PAGES_THREADS, 4)
 assign_pages_kernel(PagesParams p) {
     extern __shared__ int s_dyn[];
     int* s_old = s_dyn;                                  // [batch]
     int* s_tok = s_old + p.batch;                        // [batch + 1] new tokens before each sequence
     int* s_grow = s_tok + p.batch + 1;                   // [batch + 1] pages taken before it
     int* s_shrink = s_grow + p.batch + 1;                // [batch + 1] pages given back before it
-    __shared__ long long warp_tot[PAGES_WARPS];
+    __shared__ long long warp_tot[PAGES_WARPS][3];
     __shared__ int s_bad;
     const int tid = threadIdx.x, B = 1 << p.shift;
     if (tid == 0) s_bad = -1;
     pi_grid_dependency_wait();
     pi_launch_dependents();
     const long long head = *reinterpret_cast<volatile long long*>(p.state), tail = *reinterpret_cast<volatile long long*>(p.state + 1);
-    long long tokens = 0, grown = 0, shrunk = 0;
+    long long run[3] = {0, 0, 0};                        // new tokens, pages taken, pages given back
     for (int s0 = 0; s0 < p.batch; s0 += PAGES_THREADS) {
         const int s = s0 + tid;
         int add = 0, g = 0, r = 0, o = 0;
@@ -89,14 +96,17 @@ assign_pages_kernel(PagesParams p) {
                 add = max(n - o, 0); g = max(nb - ob, 0); r = max(ob - nb, 0);
             }
         }
-        const long long t0 = scan_from(add, warp_tot, tokens), g0 = scan_from(g, warp_tot, grown), r0 = scan_from(r, warp_tot, shrunk);
+        const long long v[3] = {add, g, r};
+        long long before[3];
+        scan_from(v, before, warp_tot, run);
         if (s < p.batch) {
             if (bad) atomicMax(&s_bad, s);
             s_old[s] = o;
             // (a total beyond 32 bits is refused below, before these are used)
-            s_tok[s] = static_cast<int>(t0); s_grow[s] = static_cast<int>(g0); s_shrink[s] = static_cast<int>(r0);
+            s_tok[s] = static_cast<int>(before[0]); s_grow[s] = static_cast<int>(before[1]); s_shrink[s] = static_cast<int>(before[2]);
         }
     }
+    long long tokens = run[0], grown = run[1], shrunk = run[2];
     if (tid == 0) { s_tok[p.batch] = static_cast<int>(tokens); s_grow[p.batch] = static_cast<int>(grown); s_shrink[p.batch] = static_cast<int>(shrunk); }
     __syncthreads();
 
@@ -139,12 +149,17 @@ assign_pages_kernel(PagesParams p) {
         p.ring[ring_at(tail_at, i)] = pg;
         *e = -1;
     }
-    // slot and position of every new token; four consecutive tokens a thread
+    // slot and position of every new token; a CTA takes one run of them, four consecutive tokens a thread at a time
     if (p.slots || p.positions) {
-        for (long long t0 = me * 4; t0 < p.n_tokens; t0 += all * 4) {
+        const long long each = ((p.n_tokens + gridDim.x - 1) / gridDim.x + 3) & ~3ll;
+        const long long end = min(p.n_tokens, (blockIdx.x + 1) * each);
+        int s = -1;
+        for (long long t0 = blockIdx.x * each + tid * 4; t0 < end; t0 += PAGES_THREADS * 4) {
             int64_t slot[4];
             int32_t pos[4];
-            int s = t0 < tokens ? owner_of(s_tok, p.batch, static_cast<int>(t0)) : p.batch;
+            // (most often the sequence is still the one before)
+            if (t0 >= tokens) s = p.batch;
+            else if (s < 0 || t0 >= s_tok[s + 1]) s = owner_of(s_tok, p.batch, static_cast<int>(t0));
             int block = -1, pg = -1;
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
@@ -204,10 +219,11 @@ int pi_launch_assign_pages(pi_ctx* c, int batch, const int32_t* old_len, const i
     p.batch = batch; p.n_pages = n_pages;
     p.row_limit = static_cast<int>(row_stride < c->cfg.max_blocks ? row_stride : c->cfg.max_blocks);
     p.shift = c->cfg.block_tokens == 16 ? 4 : c->cfg.block_tokens == 32 ? 5 : 6;
-    // enough CTAs for the token maps (four tokens a thread) and for a batch whose rows all change, at most two per SM
-    const long long work = (n_tokens + 3) / 4 > static_cast<long long>(batch) * p.row_limit / 8 ? (n_tokens + 3) / 4 : static_cast<long long>(batch) * p.row_limit / 8;
-    long long grid = (work + PAGES_THREADS - 1) / PAGES_THREADS;
-    grid = grid < 1 ? 1 : grid > 2ll * c->n_sms ? 2ll * c->n_sms : grid;
+    // enough CTAs for the token maps (four tokens a thread) and for a batch whose rows all change (two pages a thread),
+    // at most four per SM: each holds its own scan of the batch
+    const long long by_tokens = (n_tokens + 3) / 4, by_pages = static_cast<long long>(batch) * p.row_limit / 2;
+    long long grid = ((by_tokens > by_pages ? by_tokens : by_pages) + PAGES_THREADS - 1) / PAGES_THREADS;
+    grid = grid < 1 ? 1 : grid > 4ll * c->n_sms ? 4ll * c->n_sms : grid;
     const size_t smem = (4 * static_cast<size_t>(batch) + 3) * sizeof(int);
     if (smem > 40 * 1024) PI_CUDA_TRY(cudaFuncSetAttribute(assign_pages_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
     PI_CUDA_TRY(pi_launch_pdl(assign_pages_kernel, dim3(static_cast<unsigned>(grid)), dim3(PAGES_THREADS), smem, stream, p));

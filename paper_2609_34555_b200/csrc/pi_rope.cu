@@ -74,7 +74,7 @@ __device__ __forceinline__ uint4 narrow8(const float* f) {
 enum { PAIR_HALVES_FULL = 0, PAIR_NEIGHBOURS = 1, PAIR_HALVES_PART = 2 };
 
 template <typename T, int PAIR>
-__global__ void __launch_bounds__(ROPE_THREADS)
+__global__ void __launch_bounds__(ROPE_THREADS, 8)       // 64 registers: 32 warps an SM, 1 KB of loads each on their way
 qk_norm_rope_kernel(RopeParams p) {
     __shared__ float2 s_cs[ROPE_WARPS][64];                                    // cos, sin of the token's angles
     __shared__ float s_row[PAIR == PAIR_HALVES_PART ? ROPE_WARPS : 1][4][128];
@@ -84,8 +84,6 @@ qk_norm_rope_kernel(RopeParams p) {
     pi_launch_dependents();
     if (unit >= static_cast<long long>(p.n_tokens) * p.parts) return;
     const int t = static_cast<int>(unit / p.parts), part = static_cast<int>(unit - static_cast<long long>(t) * p.parts);
-    const int pos = p.pos[t];
-    if (pos < 0) return;                                                       // a padding token: its rows stay as they were
     const int H = p.Hq + p.Hkv, n_quads = (H + 3) >> 2;
     const T* q = static_cast<const T*>(p.q) + t * p.q_stride;
     const T* k = static_cast<const T*>(p.k) + t * p.k_stride;
@@ -95,12 +93,15 @@ qk_norm_rope_kernel(RopeParams p) {
     int quad = part;
     int row = quad * 4 + sub;
     if (row < H) { load8(src(row) + 8 * l, a); load8(src(row) + 64 + 8 * l, b); }
+    const float freq[2] = {lane < p.half ? __ldg(p.inv_freq + lane) : 0.f, lane + 32 < p.half ? __ldg(p.inv_freq + lane + 32) : 0.f};
+    const int pos = p.pos[t];
+    if (pos < 0) return;                                                       // a padding token: its rows stay as they were
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int f = lane + 32 * i;
         float2 cs = make_float2(1.f, 0.f);                                     // channels beyond rot_dim are not turned
         if (f < p.half) {
-            double turns = static_cast<double>(pos) * static_cast<double>(p.inv_freq[f]) * 0.15915494309189533577;   // 1 / (2 pi)
+            double turns = static_cast<double>(pos) * static_cast<double>(freq[i]) * 0.15915494309189533577;   // 1 / (2 pi)
             turns -= rint(turns);
             sincospif(2.f * static_cast<float>(turns), &cs.y, &cs.x);
         }
@@ -111,8 +112,6 @@ qk_norm_rope_kernel(RopeParams p) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) cs[e] = s_cs[warp][PAIR == PAIR_NEIGHBOURS ? (e < 4 ? 4 * l + e : 32 + 4 * l + e - 4) : 8 * l + e];
 
-    int have = -1;                                                             // whose weights are in w: 0 queries, 1 keys
-    float w[16];
     for (; quad < n_quads; quad += p.parts) {
         row = quad * 4 + sub;
         float x[16];
@@ -121,16 +120,11 @@ qk_norm_rope_kernel(RopeParams p) {
         const int next = row + 4 * p.parts;
         if (next < H) { load8(src(next) + 8 * l, a); load8(src(next) + 64 + 8 * l, b); }
         if (p.wq) {
-            const int is_k = row >= p.Hq;
-            if (is_k != have) {
-                have = is_k;
-                const float4* g = reinterpret_cast<const float4*>(is_k ? p.wk : p.wq);
+            // (the weights come out of L1 every time: kept in registers they would cost a quarter of the resident warps)
+            const float4* g = reinterpret_cast<const float4*>(row >= p.Hq ? p.wk : p.wq) + 2 * l;
+            float4 w[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float4 v = __ldg(g + (i < 2 ? 2 * l + i : 16 + 2 * l + i - 2));
-                    w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
-                }
-            }
+            for (int i = 0; i < 4; ++i) w[i] = __ldg(g + (i < 2 ? i : 14 + i));
             float ss = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) ss = fmaf(x[i], x[i], ss);
@@ -139,7 +133,9 @@ qk_norm_rope_kernel(RopeParams p) {
             ss += __shfl_xor_sync(0xffffffffu, ss, 4);
             const float r = rsqrtf(ss * (1.f / PI_HEAD_DIM) + p.eps);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] *= r * w[i];
+            for (int i = 0; i < 4; ++i) {
+                x[4 * i] *= r * w[i].x; x[4 * i + 1] *= r * w[i].y; x[4 * i + 2] *= r * w[i].z; x[4 * i + 3] *= r * w[i].w;
+            }
         }
         if (PAIR == PAIR_HALVES_FULL) {
 #pragma unroll
