@@ -361,7 +361,7 @@ int64_t pi_kv4_block_bytes(pi_ctx* ctx);
  *                    modulo n_pages: start with 0 and the number of free pages, entries in order from 0),
  *                    [2] must be 0 (used during the call), [3] unused
  *   token_start_dev  NULL or [batch + 1] int32 (out): new tokens before each sequence, the total last
- *   n_tokens         capacity of the two maps of the packed batch of new tokens (sequence after sequence, in
+ *   n_tokens         capacity (at most 2^30) of the two maps of the packed batch of new tokens (sequence after sequence, in
  *                    order of position):
  *   slot_map_dev     NULL or [n_tokens] int64 (out): page * B + position % B;  positions_dev NULL or [n_tokens]
  *                    int32 (out).  Entries behind the last new token become -1, which pi_kv4_store and

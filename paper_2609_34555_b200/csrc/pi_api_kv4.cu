@@ -54,7 +54,7 @@ extern "C" int pi_assign_pages(pi_ctx* ctx, int batch, const int32_t* old_len_de
                                int32_t* token_start_dev, int64_t n_tokens, int64_t* slot_map_dev, int32_t* positions_dev, void* stream) {
     if (!valid(ctx, 0, batch)) return PI_ERR_INVALID_ARG;
     if (!old_len_dev || !new_len_dev || !page_table_dev || !free_pages_dev || !free_state_dev) return PI_ERR_INVALID_ARG;
-    if (page_table_seq_stride < 1 || n_pages < 1 || n_tokens < 0 || n_tokens > INT32_MAX) return PI_ERR_INVALID_ARG;
+    if (page_table_seq_stride < 1 || n_pages < 1 || n_tokens < 0 || n_tokens > (1 << 30)) return PI_ERR_INVALID_ARG;
     if ((slot_map_dev && !pi_aligned16(slot_map_dev)) || (positions_dev && !pi_aligned16(positions_dev)) ||
         (reinterpret_cast<uintptr_t>(free_state_dev) & 7u))
         return PI_ERR_BAD_ALIGN;

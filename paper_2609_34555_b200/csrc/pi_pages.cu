@@ -123,7 +123,8 @@ assign_pages_kernel(PagesParams p) {
         if (blockIdx.x == 0 && tid == 0) pi_report(p.st, code, PI_STAGE_PAGES, ca, cb, cc);
         tokens = 0; grown = 0; shrunk = 0;
     }
-    const long long me = static_cast<long long>(blockIdx.x) * PAGES_THREADS + tid, all = static_cast<long long>(gridDim.x) * PAGES_THREADS;
+    // (the last threads of all begin with the pages, the first ones with the tokens: for a small batch the two run side by side)
+    const long long me = static_cast<long long>(gridDim.x - 1 - blockIdx.x) * PAGES_THREADS + (PAGES_THREADS - 1 - tid), all = static_cast<long long>(gridDim.x) * PAGES_THREADS;
     if (p.starts)
         for (long long s = me; s <= p.batch; s += all) p.starts[s] = ok ? s_tok[s] : 0;
 
@@ -149,53 +150,81 @@ assign_pages_kernel(PagesParams p) {
         p.ring[ring_at(tail_at, i)] = pg;
         *e = -1;
     }
-    // slot and position of every new token; a CTA takes one run of them, four consecutive tokens a thread at a time
+    // Slot and position of every new token: a CTA takes one run of them, a warp spans of 64, a lane a pair of neighbours (whole
+    // 16-byte stores side by side).  Four spans at a time, so that their page lookups are on their way together.  Most spans
+    // lie inside one sequence, which the warp then knows already.
     if (p.slots || p.positions) {
-        const long long each = ((p.n_tokens + gridDim.x - 1) / gridDim.x + 3) & ~3ll;
-        const long long end = min(p.n_tokens, (blockIdx.x + 1) * each);
-        int s = -1;
-        for (long long t0 = blockIdx.x * each + tid * 4; t0 < end; t0 += PAGES_THREADS * 4) {
-            int64_t slot[4];
-            int32_t pos[4];
-            // (most often the sequence is still the one before)
-            if (t0 >= tokens) s = p.batch;
-            else if (s < 0 || t0 >= s_tok[s + 1]) s = owner_of(s_tok, p.batch, static_cast<int>(t0));
-            int block = -1, pg = -1;
+        // (n_tokens is at most 2^30, and `tokens` not above it: 32 bits do)
+        const int n_tokens = static_cast<int>(p.n_tokens), total = static_cast<int>(tokens), lane = tid & 31;
+        const int each = ((n_tokens - 1) / static_cast<int>(gridDim.x) / 64 + 1) * 64;
+        const int from = static_cast<int>(min(static_cast<long long>(blockIdx.x) * each, p.n_tokens));
+        const int end = static_cast<int>(min(static_cast<long long>(from) + each, p.n_tokens));
+        auto lookup = [&](int s, int ob, int grow, int at) {
+            const int block = at >> p.shift;
+            return block < ob ? p.table[s * p.row_stride + block] : p.ring[ring_at(head_at, grow + (block - ob))];
+        };
+        int s = -1, first = 0, next = 0, old = 0, ob = 0, grow = 0;       // the warp's sequence: its tokens are first .. next - 1
+        for (int w0 = from + 64 * (tid >> 5); w0 < end; w0 += 64 * PAGES_WARPS * 4) {
+            int pos[4], pg[4][2];                                          // the pair's first position and the two pages, -1: none
+            bool apart[4];                                                 // the second token belongs to another sequence
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const long long t = t0 + u;
-                slot[u] = -1; pos[u] = -1;
-                if (t >= tokens) continue;
-                while (t >= s_tok[s + 1]) { ++s; block = -1; }
-                const int at = s_old[s] + static_cast<int>(t - s_tok[s]);
-                pos[u] = at;
-                if ((at >> p.shift) != block) {
-                    block = at >> p.shift;
-                    const int ob = (s_old[s] + B - 1) >> p.shift;
-                    pg = block < ob ? p.table[s * p.row_stride + block] : p.ring[ring_at(head_at, s_grow[s] + (block - ob))];
+            for (int k = 0; k < 4; ++k) {
+                const int w = w0 + 64 * PAGES_WARPS * k, t = w + 2 * lane;
+                pos[k] = pg[k][0] = pg[k][1] = -1;
+                apart[k] = false;
+                if (w >= end || w >= total) continue;
+                if (w >= next) {
+                    s = owner_of(s_tok, p.batch, w);
+                    first = s_tok[s]; next = s_tok[s + 1]; old = s_old[s]; grow = s_grow[s];
+                    ob = (old + B - 1) >> p.shift;
                 }
-                if (pg >= 0 && pg < p.n_pages) slot[u] = (static_cast<int64_t>(pg) << p.shift) + (at & (B - 1));
-                else pi_report(p.st, PI_ERR_INDEX_RANGE, PI_STAGE_PAGES, s, at, pg);
+                if (w + 64 <= next) {
+                    pos[k] = old + (t - first);
+                    pg[k][0] = lookup(s, ob, grow, pos[k]);
+                    pg[k][1] = ((pos[k] + 1) & (B - 1)) ? pg[k][0] : lookup(s, ob, grow, pos[k] + 1);
+                } else {
+                    // a span over a border: every lane looks for itself
+                    int s0 = -1;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        if (t + u >= total) continue;
+                        const int si = owner_of(s_tok, p.batch, t + u), at = s_old[si] + (t + u - s_tok[si]);
+                        if (u == 0) { s0 = si; pos[k] = at; } else apart[k] = si != s0;
+                        pg[k][u] = lookup(si, (s_old[si] + B - 1) >> p.shift, s_grow[si], at);
+                    }
+                }
             }
-            if (t0 + 4 <= p.n_tokens) {
-                if (p.slots) {
-                    reinterpret_cast<longlong2*>(p.slots + t0)[0] = make_longlong2(slot[0], slot[1]);
-                    reinterpret_cast<longlong2*>(p.slots + t0)[1] = make_longlong2(slot[2], slot[3]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int t = w0 + 64 * PAGES_WARPS * k + 2 * lane;
+                if (t >= end) continue;
+                int at[2] = {pos[k], pos[k] + 1};
+                if (apart[k]) { const int si = owner_of(s_tok, p.batch, t + 1); at[1] = s_old[si] + (t + 1 - s_tok[si]); }
+                int64_t slot[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    if (t + u >= total) { at[u] = -1; slot[u] = -1; continue; }
+                    slot[u] = (static_cast<int64_t>(pg[k][u]) << p.shift) + (at[u] & (B - 1));
+                    if (static_cast<unsigned>(pg[k][u]) >= static_cast<unsigned>(p.n_pages)) {
+                        slot[u] = -1;
+                        pi_report(p.st, PI_ERR_INDEX_RANGE, PI_STAGE_PAGES, -4, at[u], pg[k][u]);
+                    }
                 }
-                if (p.positions) *reinterpret_cast<int4*>(p.positions + t0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
-            } else {
-                for (int u = 0; u < 4 && t0 + u < p.n_tokens; ++u) {
-                    if (p.slots) p.slots[t0 + u] = slot[u];
-                    if (p.positions) p.positions[t0 + u] = pos[u];
+                if (t + 1 < n_tokens) {
+                    if (p.slots) *reinterpret_cast<longlong2*>(p.slots + t) = make_longlong2(slot[0], slot[1]);
+                    if (p.positions) *reinterpret_cast<int2*>(p.positions + t) = make_int2(at[0], at[1]);
+                } else {
+                    if (p.slots) p.slots[t] = slot[0];
+                    if (p.positions) p.positions[t] = at[0];
                 }
             }
         }
     }
-    // the last CTA moves the ring's counters: by then every CTA has read them
+    // the last CTA moves the ring's counters: by then every CTA has read them (and used what it read)
     __syncthreads();
     if (tid == 0) {
-        __threadfence();
-        const unsigned long long v = atomicAdd(reinterpret_cast<unsigned long long*>(p.state + 2), 1ull);
+        unsigned long long v = 0;
+        if (gridDim.x > 1) v = atomicAdd(reinterpret_cast<unsigned long long*>(p.state + 2), 1ull);
         if (v >= gridDim.x) pi_report(p.st, PI_ERR_INDEX_RANGE, PI_STAGE_PAGES, -3, static_cast<int>(v), static_cast<int>(gridDim.x));
         else if (v == gridDim.x - 1) {
             p.state[0] = head + grown;
@@ -219,10 +248,9 @@ int pi_launch_assign_pages(pi_ctx* c, int batch, const int32_t* old_len, const i
     p.batch = batch; p.n_pages = n_pages;
     p.row_limit = static_cast<int>(row_stride < c->cfg.max_blocks ? row_stride : c->cfg.max_blocks);
     p.shift = c->cfg.block_tokens == 16 ? 4 : c->cfg.block_tokens == 32 ? 5 : 6;
-    // enough CTAs for the token maps (four tokens a thread) and for a batch whose rows all change (two pages a thread),
-    // at most four per SM: each holds its own scan of the batch
-    const long long by_tokens = (n_tokens + 3) / 4, by_pages = static_cast<long long>(batch) * p.row_limit / 2;
-    long long grid = ((by_tokens > by_pages ? by_tokens : by_pages) + PAGES_THREADS - 1) / PAGES_THREADS;
+    // enough CTAs for the token maps (four tokens a thread; a page taken means a token), or, where there are none, for a batch
+    // whose rows all change (two pages a thread); at most four per SM: each makes its own scan of the batch
+    long long grid = ((n_tokens > 0 ? (n_tokens + 3) / 4 : static_cast<long long>(batch) * p.row_limit / 2) + PAGES_THREADS - 1) / PAGES_THREADS;
     grid = grid < 1 ? 1 : grid > 4ll * c->n_sms ? 4ll * c->n_sms : grid;
     const size_t smem = (4 * static_cast<size_t>(batch) + 3) * sizeof(int);
     if (smem > 40 * 1024) PI_CUDA_TRY(cudaFuncSetAttribute(assign_pages_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
