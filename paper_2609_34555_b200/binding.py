@@ -182,6 +182,7 @@ class PulseInfer:
         self.block_bytes = self.frag_bytes * n_kv_heads
         self.kv4_block_bytes = int(self._lib.pi_kv4_block_bytes(self._ctx))       # bytes of one block in 4 bits
         self.device = torch.device("cuda", torch.cuda.current_device())
+        self._remember_shape()
 
     @classmethod
     def from_workload(cls, cfg, max_batch: Optional[int] = None, **kw) -> "PulseInfer":
@@ -384,13 +385,20 @@ class PulseInfer:
             _dev(slot_stamp, torch.int32, "slot_stamp"), _dev(digest, torch.bfloat16, "digest"), _stream(stream)))
 
     # ------------------------------------------------------------------ the path on a cache in 4 bits, and what feeds it
+    def _remember_shape(self) -> None:
+        """Plain copies of what the calls below look at every time (a field of a ctypes structure costs as much as a check)."""
+        c = self.cfg
+        self._hq, self._hkv, self._d, self._b = c.n_q_heads, c.n_kv_heads, c.head_dim, c.block_tokens
+        self._slots, self._blocks, self._budget = c.pool_slots, c.max_blocks, c.budget_blocks
+        self._index = self.device.index
+
     def _on(self, t, dtype, name: str, shape=None, rows: Optional[int] = None) -> int:
         """Address of a contiguous tensor of `dtype` on the context's device; shape: exact, rows: at least so many values."""
-        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()):
+        if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_contiguous() or t.get_device() != self._index:
+            if isinstance(t, torch.Tensor) and t.is_cuda and t.device != self.device:
+                raise ValueError(f"{name}: on {t.device}, the context is on {self.device}")
             raise TypeError(f"{name}: expected a contiguous CUDA tensor of {dtype}")
-        if t.device != self.device:
-            raise ValueError(f"{name}: on {t.device}, the context is on {self.device}")
-        if shape is not None and tuple(t.shape) != shape:
+        if shape is not None and t.shape != shape:
             raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
         if rows is not None and t.numel() < rows:
             raise ValueError(f"{name}: expected at least {rows} values, got {t.numel()}")
@@ -398,15 +406,16 @@ class PulseInfer:
 
     def _stream4(self, stream) -> int:
         if stream is None:
-            return torch.cuda.current_stream(self.device).cuda_stream
+            return torch._C._cuda_getCurrentRawStream(self._index)
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
     def _blocks4(self, t, name: str, call: str, host: bool = False) -> tuple:
         """Address and number of 4-bit blocks of a contiguous uint8 tensor [..., kv4_block_bytes] (device; with `host` also pinned)."""
-        if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or not t.is_contiguous() or t.dim() < 2 or t.shape[-1] != self.kv4_block_bytes:
+        if not isinstance(t, torch.Tensor) or t.dtype is not torch.uint8 or not t.is_contiguous() or t.dim() < 2 or t.shape[-1] != self.kv4_block_bytes:
             raise TypeError(f"{name}: expected a contiguous uint8 tensor [..., {self.kv4_block_bytes}] of 4-bit blocks")
-        if t.is_cuda:
-            if t.device != self.device:
+        index = t.get_device()
+        if index >= 0:
+            if index != self._index:
                 raise ValueError(f"{name}: on {t.device}, the context is on {self.device}")
         elif not host:
             raise TypeError(f"{name}: expected a CUDA tensor")
@@ -443,62 +452,62 @@ class PulseInfer:
         """Per-head RMS norm (when weights are given) and rotation of q [T][Hq][D] and k [T][Hkv][D] (bf16, fp16 or fp32; may be
         slices of one fused projection) into q_out and k_out (bf16).  inv_freq: float32 [rot_dim / 2] (None: no rotation);
         tokens with a negative position are padding and leave their output rows alone."""
-        c = self.cfg
-        T = q.shape[0]
-        for t, heads, name in ((q, c.n_q_heads, "q"), (k, c.n_kv_heads, "k")):
-            if not (t.is_cuda and t.dtype in DTYPE_CODES and t.dtype == q.dtype):
+        T, hq, hkv, d = q.shape[0], self._hq, self._hkv, self._d
+        code = DTYPE_CODES.get(q.dtype)
+        for t, heads, name in ((q, hq, "q"), (k, hkv, "k")):
+            if code is None or t.dtype is not q.dtype or not t.is_cuda:
                 raise TypeError(f"{name}: expected a CUDA tensor of bfloat16, float16 or float32, both of one type")
-            if t.device != self.device:
+            if t.get_device() != self._index:
                 raise ValueError(f"{name}: on {t.device}, the context is on {self.device}")
-            if t.shape != (T, heads, c.head_dim):
-                raise ValueError(f"{name}: expected shape {(T, heads, c.head_dim)}, got {tuple(t.shape)}")
-            if T and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != c.head_dim)):
+            if t.shape != (T, heads, d):
+                raise ValueError(f"{name}: expected shape {(T, heads, d)}, got {tuple(t.shape)}")
+            strides = t.stride()
+            if T and (strides[2] != 1 or (heads > 1 and strides[1] != d)):
                 raise ValueError(f"{name}: the rows of a token must be contiguous")
         # (the token stride of a single token means nothing, and torch may report any)
-        qs, ks = (q.stride(0), k.stride(0)) if T > 1 else (c.n_q_heads * c.head_dim, c.n_kv_heads * c.head_dim)
-        rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+        qs, ks = (q.stride(0), k.stride(0)) if T > 1 else (hq * d, hkv * d)
         _check("pi_qk_norm_rope", self._lib.pi_qk_norm_rope(
-            self._ctx, T, DTYPE_CODES[q.dtype], q.data_ptr(), qs, k.data_ptr(), ks, self._on(positions, torch.int32, "positions", (T,)),
-            None if q_weight is None else self._on(q_weight, torch.float32, "q_weight", (c.head_dim,)),
-            None if k_weight is None else self._on(k_weight, torch.float32, "k_weight", (c.head_dim,)), eps,
-            None if inv_freq is None else self._on(inv_freq, torch.float32, "inv_freq"), rot, int(interleaved),
-            self._on(q_out, torch.bfloat16, "q_out", (T, c.n_q_heads, c.head_dim)),
-            self._on(k_out, torch.bfloat16, "k_out", (T, c.n_kv_heads, c.head_dim)), self._stream4(stream)))
+            self._ctx, T, code, q.data_ptr(), qs, k.data_ptr(), ks, self._on(positions, torch.int32, "positions", (T,)),
+            None if q_weight is None else self._on(q_weight, torch.float32, "q_weight", (d,)),
+            None if k_weight is None else self._on(k_weight, torch.float32, "k_weight", (d,)), eps,
+            None if inv_freq is None else self._on(inv_freq, torch.float32, "inv_freq"), 0 if inv_freq is None else 2 * inv_freq.numel(),
+            int(interleaved), self._on(q_out, torch.bfloat16, "q_out", (T, hq, d)), self._on(k_out, torch.bfloat16, "k_out", (T, hkv, d)),
+            self._stream4(stream)))
 
     def kv4_store(self, k, v, store, slot_map=None, stream=None) -> None:
         """Rounds the tokens k, v (bf16 [T][Hkv][D], or [N][M][Hkv][D] for N runs of M tokens; any strides with contiguous rows)
         to 4 bits and writes token t to slot slot_map[t] (int64; None: t) of `store` (uint8 [..., kv4_block_bytes], device or
         pinned).  Negative slots are skipped."""
-        c = self.cfg
         runs = k.dim() == 4
+        if k.dim() not in (3, 4):
+            raise ValueError("k: expected [tokens][heads][channels] or [runs][tokens][heads][channels]")
+        places = []
         for t, name in ((k, "k"), (v, "v")):
-            if not (t.is_cuda and t.dtype == torch.bfloat16):
+            if not t.is_cuda or t.dtype is not torch.bfloat16:
                 raise TypeError(f"{name}: expected a CUDA tensor of torch.bfloat16")
-            if t.device != self.device:
+            if t.get_device() != self._index:
                 raise ValueError(f"{name}: on {t.device}, the context is on {self.device}")
-            if t.dim() not in (3, 4) or t.shape != k.shape or tuple(t.shape[-2:]) != (c.n_kv_heads, c.head_dim):
-                raise ValueError(f"{name}: expected [tokens][{c.n_kv_heads}][{c.head_dim}] or [runs][tokens][{c.n_kv_heads}][{c.head_dim}], k and v alike")
-            if t.numel() and t.stride(-1) != 1:
+            shape, strides = t.shape, t.stride()
+            if shape != k.shape or shape[-2] != self._hkv or shape[-1] != self._d:
+                raise ValueError(f"{name}: expected [..., {self._hkv}, {self._d}], k and v alike, got {tuple(shape)}")
+            if strides[-1] != 1 and t.numel():
                 raise ValueError(f"{name}: rows must be contiguous")
+            # strides of token, head and run; of an axis of one entry the stride means nothing, and torch may report any
+            one = [0 if size <= 1 else st for size, st in zip(shape, strides)]
+            places += [t.data_ptr(), one[-3], one[-2], one[0] if runs else 0]
         n = k.shape[0] * k.shape[1] if runs else k.shape[0]
-
-        def strides(t):       # {token, head, run}; of an axis of one entry the stride means nothing, and torch may report any
-            one = [0 if size <= 1 else st for size, st in zip(t.shape, t.stride())]
-            return one[-3], one[-2], one[0] if runs else 0
-
         ptr, blocks = self._blocks4(store, "store", "pi_kv4_store", host=True)
         _check("pi_kv4_store", self._lib.pi_kv4_store(
-            self._ctx, n, k.data_ptr(), *strides(k), v.data_ptr(), *strides(v), k.shape[1] if runs else 0,
+            self._ctx, n, *places, k.shape[1] if runs else 0,
             None if slot_map is None else self._on(slot_map, torch.int64, "slot_map", (n,)), ptr, blocks, self._stream4(stream)))
 
     def kv4_load(self, store, out, blocks=None, stream=None) -> None:
         """Block blocks[i] (int32; None: i) of `store` as bf16 into out [n][Hkv][2][B][D]."""
-        c = self.cfg
         n = out.shape[0] if blocks is None else blocks.numel()
         ptr, held = self._blocks4(store, "store", "pi_kv4_load", host=True)
         _check("pi_kv4_load", self._lib.pi_kv4_load(
             self._ctx, n, ptr, held, None if blocks is None else self._on(blocks, torch.int32, "blocks"),
-            self._on(out, torch.bfloat16, "out", (n, c.n_kv_heads, 2, c.block_tokens, c.head_dim)), self._stream4(stream)))
+            self._on(out, torch.bfloat16, "out", (n, self._hkv, 2, self._b, self._d)), self._stream4(stream)))
 
     def _store4(self, host_kv4, page_table, batch: int, call: str) -> tuple:
         """(address, sequence stride, page table, its stride, pages) of a block-major or paged 4-bit store."""
@@ -507,29 +516,27 @@ class PulseInfer:
             if page_table.dim() != 2 or page_table.shape[0] < batch:
                 raise ValueError("page_table: expected [batch][blocks]")
             return ptr, 0, self._on(page_table, torch.int32, "page_table"), page_table.shape[1], blocks
-        if blocks < batch * self.cfg.max_blocks:
-            raise ValueError(f"host_kv4: expected [batch][{self.cfg.max_blocks}] blocks")
-        return ptr, self.cfg.max_blocks * self.kv4_block_bytes, None, 0, 0
+        if blocks < batch * self._blocks:
+            raise ValueError(f"host_kv4: expected [batch][{self._blocks}] blocks")
+        return ptr, self._blocks * self.kv4_block_bytes, None, 0, 0
 
     def _tables4(self, batch: int, block_table, slot_block, slot_stamp, digest) -> tuple:
-        c = self.cfg
-        return (self._on(block_table, torch.int32, "block_table", rows=batch * c.max_blocks),
-                self._on(slot_block, torch.int32, "slot_block", rows=batch * c.pool_slots),
-                self._on(slot_stamp, torch.int32, "slot_stamp", rows=batch * c.pool_slots),
-                self._on(digest, torch.bfloat16, "digest", rows=batch * c.max_blocks * 2 * c.head_dim))
+        return (self._on(block_table, torch.int32, "block_table", rows=batch * self._blocks),
+                self._on(slot_block, torch.int32, "slot_block", rows=batch * self._slots),
+                self._on(slot_stamp, torch.int32, "slot_stamp", rows=batch * self._slots),
+                self._on(digest, torch.bfloat16, "digest", rows=batch * self._blocks * 2 * self._d))
 
     def _pool4(self, pool4, batch: int, call: str) -> int:
         ptr, blocks = self._blocks4(pool4, "pool4", call)
-        if blocks < batch * self.cfg.pool_slots:
-            raise ValueError(f"pool4: expected [batch][{self.cfg.pool_slots}] blocks")
+        if blocks < batch * self._slots:
+            raise ValueError(f"pool4: expected [batch][{self._slots}] blocks")
         return ptr
 
     def append_kv4(self, layer: int, step, k_new, v_new, ctx_len, host_kv4, pool4, block_table, slot_block, slot_stamp, digest,
                    page_table=None, stream=None) -> None:
         """append_kv for a pool and a host store in 4 bits.  step: a positive int, or a one-element int32 CUDA tensor."""
-        c = self.cfg
         batch = ctx_len.shape[0]
-        shape = (batch, c.n_kv_heads, c.head_dim)
+        shape = (batch, self._hkv, self._d)
         dev_step = isinstance(step, torch.Tensor)
         _check("pi_append_kv4", self._lib.pi_append_kv4(
             self._ctx, layer, batch, 0 if dev_step else step, self._on(step, torch.int32, "step", rows=1) if dev_step else None,
@@ -550,15 +557,14 @@ class PulseInfer:
 
     def sparse_decode_attn_kv4(self, layer: int, q, pool4, sel_slots, sel_blocks, sel_count, ctx_len, out, lse=None, stream=None) -> None:
         """sparse_decode_attn over a pool of 4-bit blocks (uint8 [batch][C][kv4_block_bytes])."""
-        c = self.cfg
         batch = q.shape[0]
-        shape, lists = (batch, c.n_q_heads, c.head_dim), (batch, c.budget_blocks)
+        shape, lists = (batch, self._hq, self._d), (batch, self._budget)
         _check("pi_sparse_decode_attn_kv4", self._lib.pi_sparse_decode_attn_kv4(
             self._ctx, layer, batch, self._on(q, torch.bfloat16, "q", shape), self._pool4(pool4, batch, "pi_sparse_decode_attn_kv4"),
             self._on(sel_slots, torch.int32, "sel_slots", lists), self._on(sel_blocks, torch.int32, "sel_blocks", lists),
             self._on(sel_count, torch.int32, "sel_count", (batch,)), self._on(ctx_len, torch.int32, "ctx_len", (batch,)),
             self._on(out, torch.bfloat16, "out", shape),
-            None if lse is None else self._on(lse, torch.float32, "lse", (batch, c.n_q_heads)), self._stream4(stream)))
+            None if lse is None else self._on(lse, torch.float32, "lse", (batch, self._hq)), self._stream4(stream)))
 
     # ------------------------------------------------------------------ helpers
     def build_digests(self, layer: int, kv, ctx_len, digest, kv_seq_stride: Optional[int] = None, stream=None) -> None:

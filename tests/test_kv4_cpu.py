@@ -151,6 +151,7 @@ def test_the_front_end_refuses_what_is_not_on_the_gpu():
     ctx, keep = context()
     pi = object.__new__(pkg.PulseInfer)
     pi._lib, pi._ctx, pi.cfg, pi.device, pi.kv4_block_bytes = pkg.load_library(), ctx, keep[1], torch.device("cuda", 0), 20480
+    pi._remember_shape()
     pi.close = lambda: None                                     # (nothing was created)
     i32, bf = torch.zeros(4, dtype=torch.int32), torch.zeros((4, 8, 128), dtype=torch.bfloat16)
     blocks = torch.zeros((4, 20480), dtype=torch.uint8)
