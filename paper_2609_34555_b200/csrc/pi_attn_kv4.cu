@@ -30,8 +30,12 @@ using namespace pi_attn;
 
 constexpr int A4_WARPS = 4;
 constexpr int A4_THREADS = A4_WARPS * 32;
-constexpr int A4_STAGES = 4;
-constexpr int a4_ctas_per_sm(int NT) { return NT == 1 ? 4 : 2; }    // what the registers allow
+// Up to 8 query heads a KV head a warp works on two tiles at a time (the checks and the set-up of a step are shared, and the
+// second tile's products fill the waits of the first), with one step ahead on its way; 16 warps an SM have 160 KB in
+// flight or at work then.  More heads leave registers for one tile, with three ahead.
+__host__ __device__ constexpr int a4_tiles(int NT) { return NT == 1 ? 2 : 1; }
+__host__ __device__ constexpr int a4_steps(int NT) { return NT == 1 ? 2 : 4; }      // steps in the ring
+__host__ __device__ constexpr int a4_ctas_per_sm(int NT) { return NT == 1 ? 4 : 2; }    // what the registers allow
 constexpr float A4_NO_UNIT = 0x1p120f;             // before a group's first product: every product but 0 leaves fp16
 constexpr float A4_NO_MAX = -1e30f;                // stands for -infinity in the running maximum: differences stay numbers
 
@@ -94,7 +98,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-// 1 / x and 2^k for powers of two well inside the range
+// 1 / x of a power of two well inside the range
 __device__ __forceinline__ float inverse_power(float x) { return __uint_as_float(0x7f000000u - __float_as_uint(x)); }
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -140,6 +144,7 @@ attn_kv4_kernel(Attn4Params p) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
     const int S = static_cast<int>(cluster_nctarank()), rank = static_cast<int>(cluster_ctarank());
     const int item = blockIdx.x / S, seq = item / p.Hkv, h = item - seq * p.Hkv;
+    constexpr int TP = a4_tiles(NT), STEPS = a4_steps(NT), STAGES = STEPS * TP;
     const int SUB = p.B >> 4;
     pi_grid_dependency_wait();
     pi_launch_dependents();
@@ -177,27 +182,31 @@ attn_kv4_kernel(Attn4Params p) {
     unsigned some = __ballot_sync(0xffffffffu, meta.y != 0u), whole = __ballot_sync(0xffffffffu, meta.y == 16u), some_next = 0u;
 
     const unsigned char* head_base = p.pool + static_cast<long long>(seq) * p.C * p.block_bytes + static_cast<long long>(h) * SUB * KV4_TILE_BYTES + lane * 16;
-    const uint32_t ring = smem_u32(smem) + warp * (A4_STAGES * KV4_TILE_BYTES);
+    const uint32_t ring = smem_u32(smem) + warp * (STAGES * KV4_TILE_BYTES);
     const unsigned long long policy = pi_l2_stream_policy();
     uint32_t fill = 0u;                                  // stage of the next tile
-    auto issue = [&](bool has, uint32_t offset) {        // a tile into its stage; one commit per tile, also for what is skipped
-        if (has) {
-            const unsigned char* src = head_base + offset;
-            const uint32_t dst = ring + fill + lane * 16;
+    auto issue = [&](int i, unsigned mask, uint32_t offsets) {      // the step of tiles i .. of a batch of 32 into its stages, one commit
 #pragma unroll
-            for (int i = 0; i < KV4_TILE_BYTES / 512; ++i) copy16(dst + i * 512, src + i * 512, policy);
+        for (int k = 0; k < TP; ++k) {
+            const uint32_t offset = __shfl_sync(0xffffffffu, offsets, i + k);
+            if ((mask >> (i + k)) & 1u) {
+                const unsigned char* src = head_base + offset;
+                const uint32_t dst = ring + fill + lane * 16;
+#pragma unroll
+                for (int x = 0; x < KV4_TILE_BYTES / 512; ++x) copy16(dst + x * 512, src + x * 512, policy);
+            }
+            fill = fill == (STAGES - 1) * KV4_TILE_BYTES ? 0u : fill + KV4_TILE_BYTES;
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
-        fill = fill == (A4_STAGES - 1) * KV4_TILE_BYTES ? 0u : fill + KV4_TILE_BYTES;
     };
 #pragma unroll
-    for (int n = 0; n < A4_STAGES - 1; ++n) issue((some >> n) & 1u, __shfl_sync(0xffffffffu, meta.x, n));
+    for (int n = 0; n < STEPS - 1; ++n) issue(n * TP, some, meta.x);
 
     // ---- the queries as B operands, in the channel order of the K codes, as fp16 numbers: every head is scaled by a power of
     // two so that its largest channel lies in [1, 2); what is below 2^-14 of that is rounded at 2^-25 of it, less than the
     // sums below round.  With them, for the minima's own products, lane (r, c)'s {0, sum} of head r over the channels of
     // group c, as three bf16 numbers (2^-25 together).  One warp prepares a group of channels for all.
-    uint4* s_bq = reinterpret_cast<uint4*>(smem + A4_WARPS * A4_STAGES * KV4_TILE_BYTES);       // [NT][4 groups][32 lanes]
+    uint4* s_bq = reinterpret_cast<uint4*>(smem + A4_WARPS * STAGES * KV4_TILE_BYTES);       // [NT][4 groups][32 lanes]
     uint32_t* s_bz = reinterpret_cast<uint32_t*>(s_bq + NT * 4 * 32);                            // [NT][3][32]
     float* s_scale = reinterpret_cast<float*>(s_bz + NT * 3 * 32);                               // [NT][8 heads]
     for (int part = warp; part < 4 * NT; part += A4_WARPS) {
@@ -276,8 +285,8 @@ attn_kv4_kernel(Attn4Params p) {
     const int pr = (r >> 1) + 4 * (r & 1);
     const int pl = ((lane & 7) >> 1) + 4 * (lane & 1) + (lane & 8);     // the token whose scales this lane names to ldmatrix
 
-    uint32_t tile = ring;                                // stage of the tile at hand
-    for (int n = 0; n < n_mine; ++n, tile = tile == ring + (A4_STAGES - 1) * KV4_TILE_BYTES ? ring : tile + KV4_TILE_BYTES) {
+    uint32_t tile = ring;                                // first stage of the step at hand
+    for (int n = 0; n < n_mine; n += TP, tile = tile == ring + (STAGES - TP) * KV4_TILE_BYTES ? ring : tile + TP * KV4_TILE_BYTES) {
         const int i = n & 31;
         if (i == 0) {
             if (n) {
@@ -291,22 +300,25 @@ attn_kv4_kernel(Attn4Params p) {
                 some_next = __ballot_sync(0xffffffffu, meta_next.y != 0u);
             }
         }
-        asm volatile("cp.async.wait_group %0;" ::"n"(A4_STAGES - 2) : "memory");
-        __syncwarp();                                   // the stage is filled by all lanes, and the previous one read by all
-        if (i + A4_STAGES - 1 < 32) issue((some >> (i + A4_STAGES - 1)) & 1u, __shfl_sync(0xffffffffu, meta.x, i + A4_STAGES - 1));
-        else issue((some_next >> (i + A4_STAGES - 1 - 32)) & 1u, __shfl_sync(0xffffffffu, meta_next.x, i + A4_STAGES - 1 - 32));
-        if (!((some >> i) & 1u)) continue;
+        asm volatile("cp.async.wait_group %0;" ::"n"(STEPS - 2) : "memory");
+        __syncwarp();                                   // the step is filled by all lanes, and the previous one read by all
+        if (i + (STEPS - 1) * TP < 32) issue(i + (STEPS - 1) * TP, some, meta.x);
+        else issue(i + (STEPS - 1) * TP - 32, some_next, meta_next.x);
+        constexpr unsigned all_of = (1u << TP) - 1u;
+        if (!((some >> i) & all_of)) continue;
         // ---- S^T = K q^T: the minima's products first, then the codes' group by group
-        float s[NT][4];
-        {
-            const uint4 ka = lds128(tile + pr * 64 + c * 16), kb = lds128(tile + (pr + 8) * 64 + c * 16);
-            const uint4 za = lds128(tile + KV4_K_SCALES + pr * 16), zb = lds128(tile + KV4_K_SCALES + (pr + 8) * 16);
-            const uint32_t ya = lds32(tile + KV4_K_SCALES + pr * 16 + c * 4), yb = lds32(tile + KV4_K_SCALES + (pr + 8) * 16 + c * 4);
+        float s[TP][NT][4];
+#pragma unroll
+        for (int k = 0; k < TP; ++k) {
+            const uint32_t at = tile + k * KV4_TILE_BYTES;
+            const uint4 ka = lds128(at + pr * 64 + c * 16), kb = lds128(at + (pr + 8) * 64 + c * 16);
+            const uint4 za = lds128(at + KV4_K_SCALES + pr * 16), zb = lds128(at + KV4_K_SCALES + (pr + 8) * 16);
+            const uint32_t ya = lds32(at + KV4_K_SCALES + pr * 16 + c * 4), yb = lds32(at + KV4_K_SCALES + (pr + 8) * 16 + c * 4);
             const uint32_t az[4] = {ya, yb, ya, yb};    // {scale, minimum} of group c: places 2 c, 2 c + 1 (and + 8)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                mma_bf16_zero(s[nt], az, bz[nt][2], 0u);
-                mma_bf16(s[nt], az, bz[nt][0], bz[nt][1]);
+                mma_bf16_zero(s[k][nt], az, bz[nt][2], 0u);
+                mma_bf16(s[k][nt], az, bz[nt][0], bz[nt][1]);
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -319,37 +331,45 @@ attn_kv4_kernel(Attn4Params p) {
                     float x[4];
                     mma_f16_zero(x, a[0], b[0], a[1], b[1], bq[nt][j][0][0], bq[nt][j][0][1]);
                     mma_f16(x, a[2], b[2], a[3], b[3], bq[nt][j][1][0], bq[nt][j][1][1]);
-                    s[nt][0] = fmaf(sa, x[0], s[nt][0]); s[nt][1] = fmaf(sa, x[1], s[nt][1]);
-                    s[nt][2] = fmaf(sb, x[2], s[nt][2]); s[nt][3] = fmaf(sb, x[3], s[nt][3]);
+                    s[k][nt][0] = fmaf(sa, x[0], s[k][nt][0]); s[k][nt][1] = fmaf(sa, x[1], s[k][nt][1]);
+                    s[k][nt][2] = fmaf(sb, x[2], s[k][nt][2]); s[k][nt][3] = fmaf(sb, x[3], s[k][nt][3]);
                 }
             }
         }
-        if (!((whole >> i) & 1u)) {                     // what lies behind the last token may be anything, NaN among it
-            const int nvalid = static_cast<int>(__shfl_sync(0xffffffffu, meta.y, i));
-            if (lane < 16 && lane >= nvalid) sts128_zero(tile + KV4_V_SCALES + lane * 16);
-            __syncwarp();
+        if (((whole >> i) & all_of) != all_of) {        // what lies behind the last token may be anything, NaN among it
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                if (pr >= nvalid) s[nt][0] = s[nt][1] = -INFINITY;
-                if (pr + 8 >= nvalid) s[nt][2] = s[nt][3] = -INFINITY;
+            for (int k = 0; k < TP; ++k) {
+                const int nvalid = static_cast<int>(__shfl_sync(0xffffffffu, meta.y, i + k));
+                if (lane < 16 && lane >= nvalid) sts128_zero(tile + k * KV4_TILE_BYTES + KV4_V_SCALES + lane * 16);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    if (pr >= nvalid) s[k][nt][0] = s[k][nt][1] = -INFINITY;
+                    if (pr + 8 >= nvalid) s[k][nt][2] = s[k][nt][3] = -INFINITY;
+                }
             }
+            __syncwarp();
         }
-        // ---- online softmax over the tile's tokens.  The reference m moves only when a score exceeds it by 8 (a factor of
-        // 256, far from any overflow), so that most tiles neither reduce a maximum across lanes nor touch the sums.
-        float w[NT][4];
+        // ---- online softmax over the step's tokens.  The reference m moves only when a score exceeds it by 8 (a factor of
+        // 256, far from any overflow), so that most steps neither reduce a maximum across lanes nor touch the sums.
+        float w[TP][NT][4];
         bool over = false;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        for (int k = 0; k < TP; ++k)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[nt][e] = fmaf(s[nt][e], scale[nt][e & 1], -m[nt][e & 1]);
-            over |= max3(fmaxf(w[nt][0], w[nt][1]), w[nt][2], w[nt][3]) > 8.f;
-        }
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[k][nt][e] = fmaf(s[k][nt][e], scale[nt][e & 1], -m[nt][e & 1]);
+                over |= max3(fmaxf(w[k][nt][0], w[k][nt][1]), w[k][nt][2], w[k][nt][3]) > 8.f;
+            }
         if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float mx = fmaxf(s[nt][e], s[nt][2 + e]) * scale[nt][e];
+                    float mx = fmaxf(s[0][nt][e], s[0][nt][2 + e]);
+#pragma unroll
+                    for (int k = 1; k < TP; ++k) mx = max3(mx, s[k][nt][e], s[k][nt][2 + e]);
+                    mx *= scale[nt][e];
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
@@ -357,8 +377,11 @@ attn_kv4_kernel(Attn4Params p) {
                     m[nt][e] = m_new;
                     l[nt][e] *= alpha;
                     z[nt][e] *= alpha;
-                    w[nt][e] = fmaf(s[nt][e], scale[nt][e], -m_new);
-                    w[nt][2 + e] = fmaf(s[nt][2 + e], scale[nt][e], -m_new);
+#pragma unroll
+                    for (int k = 0; k < TP; ++k) {
+                        w[k][nt][e] = fmaf(s[k][nt][e], scale[nt][e], -m_new);
+                        w[k][nt][2 + e] = fmaf(s[k][nt][2 + e], scale[nt][e], -m_new);
+                    }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         o[nt][j][0][e] *= alpha; o[nt][j][0][2 + e] *= alpha;
@@ -368,38 +391,45 @@ attn_kv4_kernel(Attn4Params p) {
         }
         // ---- the weights; with them the minima's share of the result, for all four groups in one product.  Minima and
         // scales are bf16, so the weights take part as a bf16 head (the upper half of the number) and a bf16 remainder.
-        uint32_t az[4];
-        ldsm_x2_t(tile + KV4_V_SCALES + pl * 16, az[0], az[2]);
-        az[1] = az[3] = 0u;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            float rest[4];
+        for (int k = 0; k < TP; ++k) {
+            uint32_t az[4];
+            ldsm_x2_t(tile + k * KV4_TILE_BYTES + KV4_V_SCALES + pl * 16, az[0], az[2]);
+            az[1] = az[3] = 0u;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                w[nt][e] = ex2(w[nt][e]);
-                rest[e] = w[nt][e] - __uint_as_float(__float_as_uint(w[nt][e]) & 0xffff0000u);
+            for (int nt = 0; nt < NT; ++nt) {
+                float rest[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    w[k][nt][e] = ex2(w[k][nt][e]);
+                    rest[e] = w[k][nt][e] - __uint_as_float(__float_as_uint(w[k][nt][e]) & 0xffff0000u);
+                }
+                l[nt][0] += w[k][nt][0] + w[k][nt][2];
+                l[nt][1] += w[k][nt][1] + w[k][nt][3];
+                mma_bf16(z[nt], az, movm_t(pack_bf16(rest[0], rest[1])), movm_t(pack_bf16(rest[2], rest[3])));
+                mma_bf16(z[nt], az, movm_t(__byte_perm(__float_as_uint(w[k][nt][0]), __float_as_uint(w[k][nt][1]), 0x7632)),
+                         movm_t(__byte_perm(__float_as_uint(w[k][nt][2]), __float_as_uint(w[k][nt][3]), 0x7632)));
             }
-            l[nt][0] += w[nt][0] + w[nt][2];
-            l[nt][1] += w[nt][1] + w[nt][3];
-            mma_bf16(z[nt], az, movm_t(pack_bf16(rest[0], rest[1])), movm_t(pack_bf16(rest[2], rest[3])));
-            mma_bf16(z[nt], az, movm_t(__byte_perm(__float_as_uint(w[nt][0]), __float_as_uint(w[nt][1]), 0x7632)),
-                     movm_t(__byte_perm(__float_as_uint(w[nt][2]), __float_as_uint(w[nt][3]), 0x7632)));
         }
         // ---- weight times scale, one set per group, in fp16: 11 bits, where bf16 would need two numbers.  Its narrow range is
-        // covered by a power of two per group (`unit`), set by the first tile so that the largest product is about 2^8 and
+        // covered by a power of two per group (`unit`), set by the first step so that the largest product is about 2^8 and
         // moved when a later one leaves the range.
-        const uint4 va = lds128(tile + KV4_V_SCALES + pr * 16), vb = lds128(tile + KV4_V_SCALES + (pr + 8) * 16);
-        uint32_t pw[NT][4][2];
+        uint32_t pw[TP][NT][4][2];
         auto products = [&]() {
             uint32_t top = 0u;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float sa = kv4_scale_of(word_of(va, j)) * unit[j], sb = kv4_scale_of(word_of(vb, j)) * unit[j];
+            for (int k = 0; k < TP; ++k) {
+                const uint32_t at = tile + k * KV4_TILE_BYTES + KV4_V_SCALES;
+                const uint4 va = lds128(at + pr * 16), vb = lds128(at + (pr + 8) * 16);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    pw[nt][j][0] = pack_f16(w[nt][0] * sa, w[nt][1] * sa);
-                    pw[nt][j][1] = pack_f16(w[nt][2] * sb, w[nt][3] * sb);
-                    top = max_f16x2(top, max_f16x2(pw[nt][j][0], pw[nt][j][1]));
+                for (int j = 0; j < 4; ++j) {
+                    const float sa = kv4_scale_of(word_of(va, j)) * unit[j], sb = kv4_scale_of(word_of(vb, j)) * unit[j];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        pw[k][nt][j][0] = pack_f16(w[k][nt][0] * sa, w[k][nt][1] * sa);
+                        pw[k][nt][j][1] = pack_f16(w[k][nt][2] * sb, w[k][nt][3] * sb);
+                        top = max_f16x2(top, max_f16x2(pw[k][nt][j][0], pw[k][nt][j][1]));
+                    }
                 }
             }
             return top;
@@ -410,12 +440,16 @@ attn_kv4_kernel(Attn4Params p) {
             if (__any_sync(0xffffffffu, __hgt(__hmax(__low2half(t), __high2half(t)), __ushort_as_half(0x7800)))) {      // 2^15
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    // the largest product of the group in the tile (2^-20 of it: the product itself may leave fp32)
-                    const float sa = kv4_scale_of(word_of(va, j)) * 0x1p-20f, sb = kv4_scale_of(word_of(vb, j)) * 0x1p-20f;
+                    // the largest product of the group in the step (2^-20 of it: the product itself may leave fp32)
                     float mx = 0.f;
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-                        mx = fmaxf(mx, fmaxf(fmaxf(w[nt][0], w[nt][1]) * sa, fmaxf(w[nt][2], w[nt][3]) * sb));
+                    for (int k = 0; k < TP; ++k) {
+                        const uint32_t at = tile + k * KV4_TILE_BYTES + KV4_V_SCALES + j * 4;
+                        const float sa = kv4_scale_of(lds32(at + pr * 16)) * 0x1p-20f, sb = kv4_scale_of(lds32(at + (pr + 8) * 16)) * 0x1p-20f;
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+                            mx = fmaxf(mx, fmaxf(fmaxf(w[k][nt][0], w[k][nt][1]) * sa, fmaxf(w[k][nt][2], w[k][nt][3]) * sb));
+                    }
                     // exponents: of 2^8 / (2^20 mx), from which the product of the largest weight and scale is 2^8 and more
                     const int top_exp = min(static_cast<int>(__reduce_max_sync(0xffffffffu, __float_as_uint(mx)) >> 23), 239);
                     const int want = 242 - top_exp, have = static_cast<int>(__float_as_uint(unit[j]) >> 23);
@@ -432,20 +466,23 @@ attn_kv4_kernel(Attn4Params p) {
             }
         }
         // ---- O^T += V^T (weight scale), group by group
-        uint2 x[4];
 #pragma unroll
-        for (int a = 0; a < 4; ++a) x[a] = lds64(tile + KV4_V_CODES + (4 * a + c) * 64 + r * 8);
+        for (int k = 0; k < TP; ++k) {
+            uint2 x[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const unsigned sel = (j & 1) ? 0x7632u : 0x5410u;
-            uint32_t a[4], b[4];
-            code_pairs(__byte_perm(j < 2 ? x[0].x : x[0].y, j < 2 ? x[1].x : x[1].y, sel), a);
-            code_pairs(__byte_perm(j < 2 ? x[2].x : x[2].y, j < 2 ? x[3].x : x[3].y, sel), b);
+            for (int a = 0; a < 4; ++a) x[a] = lds64(tile + k * KV4_TILE_BYTES + KV4_V_CODES + (4 * a + c) * 64 + r * 8);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const uint32_t b0 = movm_t(pw[nt][j][0]), b1 = movm_t(pw[nt][j][1]);
-                mma_f16(o[nt][j][0], a[0], a[1], b[0], b[1], b0, b1);
-                mma_f16(o[nt][j][1], a[2], a[3], b[2], b[3], b0, b1);
+            for (int j = 0; j < 4; ++j) {
+                const unsigned sel = (j & 1) ? 0x7632u : 0x5410u;
+                uint32_t a[4], b[4];
+                code_pairs(__byte_perm(j < 2 ? x[0].x : x[0].y, j < 2 ? x[1].x : x[1].y, sel), a);
+                code_pairs(__byte_perm(j < 2 ? x[2].x : x[2].y, j < 2 ? x[3].x : x[3].y, sel), b);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const uint32_t b0 = movm_t(pw[k][nt][j][0]), b1 = movm_t(pw[k][nt][j][1]);
+                    mma_f16(o[nt][j][0], a[0], a[1], b[0], b[1], b0, b1);
+                    mma_f16(o[nt][j][1], a[2], a[3], b[2], b[3], b0, b1);
+                }
             }
         }
     }
@@ -557,7 +594,7 @@ int pi_launch_attn_kv4(pi_ctx* c, int batch, const void* q, const void* pool, co
     const int tiles = cfg.budget_blocks * (cfg.block_tokens / 16);
     int split = 1;
     while (split < 8 && items * split * 2 <= slots && tiles >= split * 2 * A4_WARPS) split *= 2;
-    const size_t ring = static_cast<size_t>(A4_WARPS) * A4_STAGES * KV4_TILE_BYTES + (p.G <= 8 ? 1 : 2) * (4 * 32 * 16 + 3 * 32 * 4 + 8 * 4);
+    const size_t ring = static_cast<size_t>(A4_WARPS) * a4_steps(p.G <= 8 ? 1 : 2) * a4_tiles(p.G <= 8 ? 1 : 2) * KV4_TILE_BYTES + (p.G <= 8 ? 1 : 2) * (4 * 32 * 16 + 3 * 32 * 4 + 8 * 4);
     const size_t merge = (static_cast<size_t>(A4_WARPS) * p.G * (PI_HEAD_DIM + 2) + 2 * p.G) * sizeof(float);
     const size_t smem = ring > merge ? ring : merge;
     auto launch = [&](auto kernel) -> int {
