@@ -51,6 +51,7 @@ struct Attn4Params {
     pi_status_ref st;
     long long block_bytes;
     float scale_log2;
+    uint32_t raise;                 // 0x64006400
     int Hq, Hkv, G, B, K, C;
 };
 
@@ -67,16 +68,22 @@ __device__ __forceinline__ uint2 lds64(uint32_t a) {
     asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
     return v;
 }
+// (v & mask) | raise in one operation: it takes one immediate, so `raise` comes in a register (a kernel argument -- seen as a
+// constant, it costs every pair a second operation: 218 instead of 159 of them a tile on the pipe that bounds this kernel)
+__device__ __forceinline__ uint32_t masked(uint32_t v, uint32_t mask, uint32_t raise) {
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(v), "r"(mask), "r"(raise));
+    return d;
+}
 // The four pairs of a word, nibbles n (low half) and n + 4 (high half), as fp16 numbers.  0x6400 | nibble is 1024 + nibble
-// and 0x6400 | 16 nibble is 1024 + 16 nibble, so two of the four need no shift; what brings them back to 0..15 is exact and
-// runs beside the logical operations, on the pipe that has room.
-__device__ __forceinline__ void code_pairs(uint32_t w, uint32_t (&p)[4]) {
+// and 0x6400 | 16 nibble is 1024 + 16 nibble, so two of the four need no shift; bringing them back to 0..15 is exact.
+__device__ __forceinline__ void code_pairs(uint32_t w, uint32_t raise, uint32_t (&p)[4]) {
     const __half2 low = __halves2half2(__ushort_as_half(0xe400), __ushort_as_half(0xe400));        // -1024
     const __half2 sixteenth = __halves2half2(__ushort_as_half(0x2c00), __ushort_as_half(0x2c00));  // 1 / 16
     const __half2 high = __halves2half2(__ushort_as_half(0xd400), __ushort_as_half(0xd400));       // -64
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const uint32_t v = i ? w >> 8 : w, a = (v & 0x000f000fu) | 0x64006400u, b = (v & 0x00f000f0u) | 0x64006400u;
+        const uint32_t v = i ? w >> 8 : w, a = masked(v, 0x000f000fu, raise), b = masked(v, 0x00f000f0u, raise);
         const __half2 x = __hadd2(*reinterpret_cast<const __half2*>(&a), low), y = __hfma2(*reinterpret_cast<const __half2*>(&b), sixteenth, high);
         p[2 * i] = *reinterpret_cast<const uint32_t*>(&x);
         p[2 * i + 1] = *reinterpret_cast<const uint32_t*>(&y);
@@ -285,6 +292,7 @@ attn_kv4_kernel(Attn4Params p) {
     const int pr = (r >> 1) + 4 * (r & 1);
     const int pl = ((lane & 7) >> 1) + 4 * (lane & 1) + (lane & 8);     // the token whose scales this lane names to ldmatrix
 
+    const uint32_t raise = p.raise;
     uint32_t tile = ring;                                // first stage of the step at hand
     for (int n = 0; n < n_mine; n += TP, tile = tile == ring + (STAGES - TP) * KV4_TILE_BYTES ? ring : tile + TP * KV4_TILE_BYTES) {
         const int i = n & 31;
@@ -323,8 +331,8 @@ attn_kv4_kernel(Attn4Params p) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 uint32_t a[4], b[4];
-                code_pairs(word_of(ka, j), a);
-                code_pairs(word_of(kb, j), b);
+                code_pairs(word_of(ka, j), raise, a);
+                code_pairs(word_of(kb, j), raise, b);
                 const float sa = kv4_scale_of(word_of(za, j)), sb = kv4_scale_of(word_of(zb, j));
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
@@ -475,8 +483,8 @@ attn_kv4_kernel(Attn4Params p) {
             for (int j = 0; j < 4; ++j) {
                 const unsigned sel = (j & 1) ? 0x7632u : 0x5410u;
                 uint32_t a[4], b[4];
-                code_pairs(__byte_perm(j < 2 ? x[0].x : x[0].y, j < 2 ? x[1].x : x[1].y, sel), a);
-                code_pairs(__byte_perm(j < 2 ? x[2].x : x[2].y, j < 2 ? x[3].x : x[3].y, sel), b);
+                code_pairs(__byte_perm(j < 2 ? x[0].x : x[0].y, j < 2 ? x[1].x : x[1].y, sel), raise, a);
+                code_pairs(__byte_perm(j < 2 ? x[2].x : x[2].y, j < 2 ? x[3].x : x[3].y, sel), raise, b);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     const uint32_t b0 = movm_t(pw[k][nt][j][0]), b1 = movm_t(pw[k][nt][j][1]);
@@ -587,6 +595,7 @@ int pi_launch_attn_kv4(pi_ctx* c, int batch, const void* q, const void* pool, co
     p.st = pi_status_of(c);
     p.block_bytes = kv4_block_bytes(cfg.n_kv_heads, cfg.block_tokens);
     p.scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(PI_HEAD_DIM));
+    p.raise = 0x64006400u;
     p.Hq = cfg.n_q_heads; p.Hkv = cfg.n_kv_heads; p.G = cfg.n_q_heads / cfg.n_kv_heads;
     p.B = cfg.block_tokens; p.K = cfg.budget_blocks; p.C = cfg.pool_slots;
     // CTAs per item: as many as fill the GPU with what fits an SM, as long as every warp still has a tile
