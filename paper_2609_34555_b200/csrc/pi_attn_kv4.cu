@@ -605,9 +605,8 @@ int pi_launch_attn_kv4(pi_ctx* c, int batch, const void* q, const void* pool, co
     while (split < 8 && items * split * 2 <= slots && tiles >= split * 2 * A4_WARPS) split *= 2;
     const size_t ring = static_cast<size_t>(A4_WARPS) * a4_steps(p.G <= 8 ? 1 : 2) * a4_tiles(p.G <= 8 ? 1 : 2) * KV4_TILE_BYTES + (p.G <= 8 ? 1 : 2) * (4 * 32 * 16 + 3 * 32 * 4 + 8 * 4);
     const size_t merge = (static_cast<size_t>(A4_WARPS) * p.G * (PI_HEAD_DIM + 2) + 2 * p.G) * sizeof(float);
-    const size_t smem = ring > merge ? ring : merge;
+    const size_t smem = ring > merge ? ring : merge;     // at most 46 KB: no attribute to set
     auto launch = [&](auto kernel) -> int {
-        PI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
         cudaLaunchConfig_t lc = {};
         lc.gridDim = dim3(static_cast<unsigned>(items * split));
         lc.blockDim = dim3(A4_THREADS);
