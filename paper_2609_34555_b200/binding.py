@@ -2,17 +2,19 @@
 
 Argument marshalling only: tensors are checked (dtype, device, contiguity) and handed
 over as raw pointers; every step of the path runs in the CUDA library.  There is no
-fallback: a missing library or a failing call raises.
+fallback: a missing library or a failing call raises.  The calls on the 4-bit path, some of which keep the
+GPU for a few microseconds only, have their tensors checked in native code (csrc/front.cpp).
 """
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 from ctypes import POINTER, c_char_p, c_float, c_int, c_int32, c_int64, c_uint32, c_void_p
 from typing import Optional, Sequence
 
 import torch
 
-from .build import LIB, build
+from .build import FRONT, LIB, build
 
 OK = 0
 ERR_NAMES = {
@@ -27,7 +29,7 @@ EXPORTS = ["pi_create", "pi_destroy", "pi_score_select", "pi_score_select_diff",
            "pi_get_status", "pi_get_stats", "pi_clear_status", "pi_strerror",
            "pi_kv4_block_bytes", "pi_assign_pages", "pi_qk_norm_rope", "pi_kv4_store", "pi_kv4_load", "pi_append_kv4", "pi_recall_kv4",
            "pi_sparse_decode_attn_kv4"]
-DTYPE_CODES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}      # PI_DTYPE_*
+FRONT_CALLS = ["pi_assign_pages", "pi_qk_norm_rope", "pi_kv4_store", "pi_kv4_load", "pi_append_kv4", "pi_recall_kv4", "pi_sparse_decode_attn_kv4"]
 
 
 class PiConfig(ctypes.Structure):
@@ -45,6 +47,7 @@ class PiError(RuntimeError):
 
 
 _lib = None
+_front = None
 
 
 def load_library(rebuild: bool = False) -> ctypes.CDLL:
@@ -106,6 +109,19 @@ def load_library(rebuild: bool = False) -> ctypes.CDLL:
     lib.pi_kv4_block_bytes.restype = c_int64
     _lib = lib
     return lib
+
+
+def load_front():
+    """The module that checks the tensors of the calls on the 4-bit path, connected to the CUDA library."""
+    global _front
+    if _front is None:
+        lib = load_library()
+        spec = importlib.util.spec_from_file_location("_front", FRONT)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        module.connect(*[ctypes.cast(getattr(lib, name), c_void_p).value for name in FRONT_CALLS])
+        _front = module
+    return _front
 
 
 def strerror(code: int) -> str:
@@ -196,6 +212,7 @@ class PulseInfer:
         if getattr(self, "_ctx", None) is not None and self._ctx.value:
             self._lib.pi_destroy(self._ctx)
             self._ctx = c_void_p()
+            self._remember_shape()
 
     def __del__(self):
         try:
@@ -386,61 +403,25 @@ class PulseInfer:
 
     # ------------------------------------------------------------------ the path on a cache in 4 bits, and what feeds it
     def _remember_shape(self) -> None:
-        """Plain copies of what the calls below look at every time (a field of a ctypes structure costs as much as a check)."""
+        """What the calls below check against, in native form."""
         c = self.cfg
-        self._hq, self._hkv, self._d, self._b = c.n_q_heads, c.n_kv_heads, c.head_dim, c.block_tokens
-        self._slots, self._blocks, self._budget = c.pool_slots, c.max_blocks, c.budget_blocks
+        self._front = load_front()
         self._index = self.device.index
-
-    def _on(self, t, dtype, name: str, shape=None, rows: Optional[int] = None) -> int:
-        """Address of a contiguous tensor of `dtype` on the context's device; shape: exact, rows: at least so many values."""
-        if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_contiguous() or t.get_device() != self._index:
-            if isinstance(t, torch.Tensor) and t.is_cuda and t.device != self.device:
-                raise ValueError(f"{name}: on {t.device}, the context is on {self.device}")
-            raise TypeError(f"{name}: expected a contiguous CUDA tensor of {dtype}")
-        if shape is not None and t.shape != shape:
-            raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
-        if rows is not None and t.numel() < rows:
-            raise ValueError(f"{name}: expected at least {rows} values, got {t.numel()}")
-        return t.data_ptr()
+        self._shape = self._front.shape(self._ctx.value or 0, self._index, c.n_q_heads, c.n_kv_heads, c.head_dim, c.block_tokens, c.pool_slots,
+                                        c.max_blocks, c.budget_blocks, self.kv4_block_bytes)
 
     def _stream4(self, stream) -> int:
         if stream is None:
             return torch._C._cuda_getCurrentRawStream(self._index)
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
-    def _blocks4(self, t, name: str, call: str, host: bool = False) -> tuple:
-        """Address and number of 4-bit blocks of a contiguous uint8 tensor [..., kv4_block_bytes] (device; with `host` also pinned)."""
-        if not isinstance(t, torch.Tensor) or t.dtype is not torch.uint8 or not t.is_contiguous() or t.dim() < 2 or t.shape[-1] != self.kv4_block_bytes:
-            raise TypeError(f"{name}: expected a contiguous uint8 tensor [..., {self.kv4_block_bytes}] of 4-bit blocks")
-        index = t.get_device()
-        if index >= 0:
-            if index != self._index:
-                raise ValueError(f"{name}: on {t.device}, the context is on {self.device}")
-        elif not host:
-            raise TypeError(f"{name}: expected a CUDA tensor")
-        elif not t.is_pinned():
-            raise PiError(call, -5, strerror(-5))
-        return t.data_ptr(), t.numel() // self.kv4_block_bytes
-
     def assign_pages(self, old_len, new_len, page_table, free_pages, free_state, token_start=None, slot_map=None, positions=None,
                      stream=None) -> None:
         """Takes pages for the sequences that grow from old_len to new_len tokens and gives back those of the sequences that
         shrink; writes slot and position of every new token (maps of one capacity, -1 behind the last token).
         page_table: int32 [batch][NB]; free_pages: int32 ring; free_state: int64 [4] (see free_page_ring)."""
-        batch = old_len.shape[0]
-        if page_table.dim() != 2 or page_table.shape[0] < batch:
-            raise ValueError("page_table: expected [batch][blocks]")
-        if slot_map is not None and positions is not None and slot_map.shape[0] != positions.shape[0]:
-            raise ValueError("slot_map and positions have different lengths")
-        n = slot_map.shape[0] if slot_map is not None else positions.shape[0] if positions is not None else 0
-        _check("pi_assign_pages", self._lib.pi_assign_pages(
-            self._ctx, batch, self._on(old_len, torch.int32, "old_len", (batch,)), self._on(new_len, torch.int32, "new_len", (batch,)),
-            self._on(page_table, torch.int32, "page_table"), page_table.shape[1], self._on(free_pages, torch.int32, "free_pages"),
-            free_pages.numel(), self._on(free_state, torch.int64, "free_state", (4,)),
-            None if token_start is None else self._on(token_start, torch.int32, "token_start", (batch + 1,)), n,
-            None if slot_map is None else self._on(slot_map, torch.int64, "slot_map", (n,)),
-            None if positions is None else self._on(positions, torch.int32, "positions", (n,)), self._stream4(stream)))
+        _check("pi_assign_pages", self._front.assign_pages(self._shape, old_len, new_len, page_table, free_pages, free_state, token_start,
+                                                           slot_map, positions, self._stream4(stream)))
 
     def free_page_ring(self, n_pages: int) -> tuple:
         """(free_pages, free_state) of an arena none of whose pages is taken."""
@@ -452,119 +433,33 @@ class PulseInfer:
         """Per-head RMS norm (when weights are given) and rotation of q [T][Hq][D] and k [T][Hkv][D] (bf16, fp16 or fp32; may be
         slices of one fused projection) into q_out and k_out (bf16).  inv_freq: float32 [rot_dim / 2] (None: no rotation);
         tokens with a negative position are padding and leave their output rows alone."""
-        T, hq, hkv, d = q.shape[0], self._hq, self._hkv, self._d
-        code = DTYPE_CODES.get(q.dtype)
-        for t, heads, name in ((q, hq, "q"), (k, hkv, "k")):
-            if code is None or t.dtype is not q.dtype or not t.is_cuda:
-                raise TypeError(f"{name}: expected a CUDA tensor of bfloat16, float16 or float32, both of one type")
-            if t.get_device() != self._index:
-                raise ValueError(f"{name}: on {t.device}, the context is on {self.device}")
-            if t.shape != (T, heads, d):
-                raise ValueError(f"{name}: expected shape {(T, heads, d)}, got {tuple(t.shape)}")
-            strides = t.stride()
-            if T and (strides[2] != 1 or (heads > 1 and strides[1] != d)):
-                raise ValueError(f"{name}: the rows of a token must be contiguous")
-        # (the token stride of a single token means nothing, and torch may report any)
-        qs, ks = (q.stride(0), k.stride(0)) if T > 1 else (hq * d, hkv * d)
-        _check("pi_qk_norm_rope", self._lib.pi_qk_norm_rope(
-            self._ctx, T, code, q.data_ptr(), qs, k.data_ptr(), ks, self._on(positions, torch.int32, "positions", (T,)),
-            None if q_weight is None else self._on(q_weight, torch.float32, "q_weight", (d,)),
-            None if k_weight is None else self._on(k_weight, torch.float32, "k_weight", (d,)), eps,
-            None if inv_freq is None else self._on(inv_freq, torch.float32, "inv_freq"), 0 if inv_freq is None else 2 * inv_freq.numel(),
-            int(interleaved), self._on(q_out, torch.bfloat16, "q_out", (T, hq, d)), self._on(k_out, torch.bfloat16, "k_out", (T, hkv, d)),
-            self._stream4(stream)))
+        _check("pi_qk_norm_rope", self._front.qk_norm_rope(self._shape, q, k, positions, inv_freq, q_out, k_out, q_weight, k_weight, eps,
+                                                           interleaved, self._stream4(stream)))
 
     def kv4_store(self, k, v, store, slot_map=None, stream=None) -> None:
         """Rounds the tokens k, v (bf16 [T][Hkv][D], or [N][M][Hkv][D] for N runs of M tokens; any strides with contiguous rows)
         to 4 bits and writes token t to slot slot_map[t] (int64; None: t) of `store` (uint8 [..., kv4_block_bytes], device or
         pinned).  Negative slots are skipped."""
-        runs = k.dim() == 4
-        if k.dim() not in (3, 4):
-            raise ValueError("k: expected [tokens][heads][channels] or [runs][tokens][heads][channels]")
-        places = []
-        for t, name in ((k, "k"), (v, "v")):
-            if not t.is_cuda or t.dtype is not torch.bfloat16:
-                raise TypeError(f"{name}: expected a CUDA tensor of torch.bfloat16")
-            if t.get_device() != self._index:
-                raise ValueError(f"{name}: on {t.device}, the context is on {self.device}")
-            shape, strides = t.shape, t.stride()
-            if shape != k.shape or shape[-2] != self._hkv or shape[-1] != self._d:
-                raise ValueError(f"{name}: expected [..., {self._hkv}, {self._d}], k and v alike, got {tuple(shape)}")
-            if strides[-1] != 1 and t.numel():
-                raise ValueError(f"{name}: rows must be contiguous")
-            # strides of token, head and run; of an axis of one entry the stride means nothing, and torch may report any
-            one = [0 if size <= 1 else st for size, st in zip(shape, strides)]
-            places += [t.data_ptr(), one[-3], one[-2], one[0] if runs else 0]
-        n = k.shape[0] * k.shape[1] if runs else k.shape[0]
-        ptr, blocks = self._blocks4(store, "store", "pi_kv4_store", host=True)
-        _check("pi_kv4_store", self._lib.pi_kv4_store(
-            self._ctx, n, *places, k.shape[1] if runs else 0,
-            None if slot_map is None else self._on(slot_map, torch.int64, "slot_map", (n,)), ptr, blocks, self._stream4(stream)))
+        _check("pi_kv4_store", self._front.kv4_store(self._shape, k, v, store, slot_map, self._stream4(stream)))
 
     def kv4_load(self, store, out, blocks=None, stream=None) -> None:
         """Block blocks[i] (int32; None: i) of `store` as bf16 into out [n][Hkv][2][B][D]."""
-        n = out.shape[0] if blocks is None else blocks.numel()
-        ptr, held = self._blocks4(store, "store", "pi_kv4_load", host=True)
-        _check("pi_kv4_load", self._lib.pi_kv4_load(
-            self._ctx, n, ptr, held, None if blocks is None else self._on(blocks, torch.int32, "blocks"),
-            self._on(out, torch.bfloat16, "out", (n, self._hkv, 2, self._b, self._d)), self._stream4(stream)))
-
-    def _store4(self, host_kv4, page_table, batch: int, call: str) -> tuple:
-        """(address, sequence stride, page table, its stride, pages) of a block-major or paged 4-bit store."""
-        ptr, blocks = self._blocks4(host_kv4, "host_kv4", call, host=True)
-        if page_table is not None:
-            if page_table.dim() != 2 or page_table.shape[0] < batch:
-                raise ValueError("page_table: expected [batch][blocks]")
-            return ptr, 0, self._on(page_table, torch.int32, "page_table"), page_table.shape[1], blocks
-        if blocks < batch * self._blocks:
-            raise ValueError(f"host_kv4: expected [batch][{self._blocks}] blocks")
-        return ptr, self._blocks * self.kv4_block_bytes, None, 0, 0
-
-    def _tables4(self, batch: int, block_table, slot_block, slot_stamp, digest) -> tuple:
-        return (self._on(block_table, torch.int32, "block_table", rows=batch * self._blocks),
-                self._on(slot_block, torch.int32, "slot_block", rows=batch * self._slots),
-                self._on(slot_stamp, torch.int32, "slot_stamp", rows=batch * self._slots),
-                self._on(digest, torch.bfloat16, "digest", rows=batch * self._blocks * 2 * self._d))
-
-    def _pool4(self, pool4, batch: int, call: str) -> int:
-        ptr, blocks = self._blocks4(pool4, "pool4", call)
-        if blocks < batch * self._slots:
-            raise ValueError(f"pool4: expected [batch][{self._slots}] blocks")
-        return ptr
+        _check("pi_kv4_load", self._front.kv4_load(self._shape, store, out, blocks, self._stream4(stream)))
 
     def append_kv4(self, layer: int, step, k_new, v_new, ctx_len, host_kv4, pool4, block_table, slot_block, slot_stamp, digest,
                    page_table=None, stream=None) -> None:
         """append_kv for a pool and a host store in 4 bits.  step: a positive int, or a one-element int32 CUDA tensor."""
-        batch = ctx_len.shape[0]
-        shape = (batch, self._hkv, self._d)
-        dev_step = isinstance(step, torch.Tensor)
-        _check("pi_append_kv4", self._lib.pi_append_kv4(
-            self._ctx, layer, batch, 0 if dev_step else step, self._on(step, torch.int32, "step", rows=1) if dev_step else None,
-            self._on(k_new, torch.bfloat16, "k_new", shape), self._on(v_new, torch.bfloat16, "v_new", shape),
-            self._on(ctx_len, torch.int32, "ctx_len"), *self._store4(host_kv4, page_table, batch, "pi_append_kv4"),
-            self._pool4(pool4, batch, "pi_append_kv4"), *self._tables4(batch, block_table, slot_block, slot_stamp, digest),
-            self._stream4(stream)))
+        _check("pi_append_kv4", self._front.append_kv4(self._shape, layer, step, k_new, v_new, ctx_len, host_kv4, pool4, block_table, slot_block,
+                                                       slot_stamp, digest, page_table, self._stream4(stream)))
 
     def recall_kv4(self, layer: int, host_kv4, pool4, recall_list, recall_count, page_table=None, stream=None) -> None:
         """recall_gather_scatter with a 4-bit block as the unit."""
-        batch = recall_count.shape[0]
-        if recall_list.dim() != 3 or recall_list.shape[0] != batch or recall_list.shape[2] != 4:
-            raise ValueError("recall_list: expected [batch][capacity][4]")
-        _check("pi_recall_kv4", self._lib.pi_recall_kv4(
-            self._ctx, layer, batch, *self._store4(host_kv4, page_table, batch, "pi_recall_kv4"), self._pool4(pool4, batch, "pi_recall_kv4"),
-            self._on(recall_list, EXTENT_DTYPE, "recall_list"), recall_list.shape[1], self._on(recall_count, torch.int32, "recall_count"),
-            self._stream4(stream)))
+        _check("pi_recall_kv4", self._front.recall_kv4(self._shape, layer, host_kv4, pool4, recall_list, recall_count, page_table, self._stream4(stream)))
 
     def sparse_decode_attn_kv4(self, layer: int, q, pool4, sel_slots, sel_blocks, sel_count, ctx_len, out, lse=None, stream=None) -> None:
         """sparse_decode_attn over a pool of 4-bit blocks (uint8 [batch][C][kv4_block_bytes])."""
-        batch = q.shape[0]
-        shape, lists = (batch, self._hq, self._d), (batch, self._budget)
-        _check("pi_sparse_decode_attn_kv4", self._lib.pi_sparse_decode_attn_kv4(
-            self._ctx, layer, batch, self._on(q, torch.bfloat16, "q", shape), self._pool4(pool4, batch, "pi_sparse_decode_attn_kv4"),
-            self._on(sel_slots, torch.int32, "sel_slots", lists), self._on(sel_blocks, torch.int32, "sel_blocks", lists),
-            self._on(sel_count, torch.int32, "sel_count", (batch,)), self._on(ctx_len, torch.int32, "ctx_len", (batch,)),
-            self._on(out, torch.bfloat16, "out", shape),
-            None if lse is None else self._on(lse, torch.float32, "lse", (batch, self._hq)), self._stream4(stream)))
+        _check("pi_sparse_decode_attn_kv4", self._front.sparse_decode_attn_kv4(self._shape, layer, q, pool4, sel_slots, sel_blocks, sel_count, ctx_len, out,
+                                                                               lse, self._stream4(stream)))
 
     # ------------------------------------------------------------------ helpers
     def build_digests(self, layer: int, kv, ctx_len, digest, kv_seq_stride: Optional[int] = None, stream=None) -> None:

@@ -1,4 +1,5 @@
-"""Builds libpulseinfer_b200.so (sm_100a only) in-tree with nvcc.
+"""Builds libpulseinfer_b200.so (sm_100a only) in-tree with nvcc, and _front.so, the Python module that checks
+the tensors of the calls on the 4-bit path, with g++ against the installed torch.
 
     python -m paper_2609_34555_b200.build [--force] [--verbose]
 """
@@ -7,12 +8,14 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import sysconfig
 from pathlib import Path
 
 PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 INCLUDE = PKG.parent / "include"
 LIB = PKG / "libpulseinfer_b200.so"
+FRONT = PKG / "_front.so"
 
 SOURCES = ["pi_api.cu", "pi_score_select.cu", "pi_select_diff.cu", "pi_diff_misses.cu", "pi_recall.cu", "pi_attn.cu", "pi_attn_headmajor.cu",
            "pi_helpers.cu", "pi_append.cu", "pi_api_kv4.cu", "pi_kv4.cu", "pi_rope.cu", "pi_pages.cu", "pi_attn_kv4.cu"]
@@ -30,7 +33,22 @@ def _stale() -> bool:
     return any(d.stat().st_mtime > t for d in deps)
 
 
+def build_front(force: bool = False) -> Path:
+    deps = [CSRC / "front.cpp"] + list(INCLUDE.glob("*.h"))
+    if not force and FRONT.exists() and all(d.stat().st_mtime <= FRONT.stat().st_mtime for d in deps):
+        return FRONT
+    import torch
+    root = Path(torch.__file__).resolve().parent
+    tmp = FRONT.with_suffix(f".tmp{os.getpid()}.so")
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                           f"-I{INCLUDE}", f"-I{sysconfig.get_paths()['include']}", f"-I{root / 'include'}", f"-I{root / 'include' / 'torch' / 'csrc' / 'api' / 'include'}",
+                           "-o", str(tmp), str(CSRC / "front.cpp"), f"-L{root / 'lib'}", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"])
+    os.replace(tmp, FRONT)
+    return FRONT
+
+
 def build(force: bool = False, verbose: bool = False) -> Path:
+    build_front(force)
     if not force and not _stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")

@@ -109,6 +109,61 @@ def test_store_of_runs_of_tokens_equals_store_token_by_token_and_a_pinned_store(
     pi.close()
 
 
+def test_the_front_end_checks_devices_types_and_shapes():
+    """Every tensor argument of the calls, one wrong at a time: refused before anything runs, and the call still works afterwards."""
+    import paper_2609_34555_b200 as pkg
+    pi = context()
+    n, H, B, C, NB, K = 4, 2, 16, 24, 256, 16
+    z = lambda *shape, dtype=torch.int32: torch.zeros(shape, dtype=dtype, device=DEV)          # noqa: E731
+    bfz = lambda *shape: z(*shape, dtype=torch.bfloat16)                                       # noqa: E731
+    pool, host = z(n, C, pi.kv4_block_bytes, dtype=torch.uint8), z(n, NB, pi.kv4_block_bytes, dtype=torch.uint8)
+    calls = {
+        "assign_pages": dict(old_len=z(n), new_len=z(n), page_table=z(n, NB), free_pages=z(50), free_state=torch.tensor([0, 50, 0, 0], device=DEV),
+                             token_start=z(n + 1), slot_map=z(8, dtype=torch.int64), positions=z(8)),
+        "qk_norm_rope": dict(q=bfz(n, 8, 128), k=bfz(n, H, 128), positions=z(n), inv_freq=z(64, dtype=torch.float32), q_out=bfz(n, 8, 128), k_out=bfz(n, H, 128),
+                             q_weight=z(128, dtype=torch.float32), k_weight=z(128, dtype=torch.float32)),
+        "kv4_store": dict(k=bfz(n, H, 128), v=bfz(n, H, 128), store=host, slot_map=z(n, dtype=torch.int64)),
+        "kv4_load": dict(store=host, out=bfz(n, H, 2, B, 128), blocks=z(n)),
+        "append_kv4": dict(layer=0, step=z(1) + 1, k_new=bfz(n, H, 128), v_new=bfz(n, H, 128), ctx_len=z(n), host_kv4=host, pool4=pool, block_table=z(n, NB) - 1,
+                           slot_block=z(n, C) - 1, slot_stamp=z(n, C), digest=bfz(n, NB, 2, 128), page_table=z(n, NB)),
+        "recall_kv4": dict(layer=0, host_kv4=host, pool4=pool, recall_list=z(n, K, 4), recall_count=z(n), page_table=z(n, NB)),
+        "sparse_decode_attn_kv4": dict(layer=0, q=bfz(n, 8, 128), pool4=pool, sel_slots=z(n, K), sel_blocks=z(n, K), sel_count=z(n), ctx_len=z(n), out=bfz(n, 8, 128),
+                                       lse=z(n, 8, dtype=torch.float32)),
+    }
+    for name, good in calls.items():
+        call = getattr(pi, name)
+        call(**good)
+        clean(pi)
+        for arg, t in good.items():
+            if not isinstance(t, torch.Tensor):
+                continue
+            wrong = [t.to(torch.float64), t.cpu() if arg not in ("host_kv4", "store") else t[..., 16:], t.repeat_interleave(2, -1)[..., ::2]]
+            if not (name, arg) in (("qk_norm_rope", "inv_freq"), ("kv4_load", "blocks"), ("assign_pages", "free_pages"), ("append_kv4", "step")):
+                # (of the tables only the number of values is asked for)
+                wrong.append(t[:1] if arg in ("block_table", "slot_block", "slot_stamp", "digest") else t[..., None].contiguous())
+            if (name, arg) in (("kv4_store", "k"), ("kv4_store", "v"), ("qk_norm_rope", "q"), ("qk_norm_rope", "k")):
+                wrong[2] = t.repeat_interleave(2, -1)[..., ::2]                                  # rows not contiguous
+            for bad in wrong:
+                if t.numel() == 1 and bad.is_cuda and bad.dtype == t.dtype:
+                    continue
+                with pytest.raises((TypeError, ValueError, pkg.PiError)):
+                    call(**dict(good, **{arg: bad}))
+        call(**good)
+        clean(pi)
+    with pytest.raises(pkg.PiError):
+        pi.append_kv4(**dict(calls["append_kv4"], step=0))
+    with pytest.raises(pkg.PiError):
+        pi.append_kv4(**dict(calls["append_kv4"], layer=1))
+    with pytest.raises(pkg.PiError):
+        pi.qk_norm_rope(**dict(calls["qk_norm_rope"], k_weight=None))
+    with pytest.raises(pkg.PiError) as e:
+        pi.kv4_load(torch.zeros((n, pi.kv4_block_bytes), dtype=torch.uint8), calls["kv4_load"]["out"])
+    assert e.value.code == -5                                                                    # not pinned
+    pi.close()
+    with pytest.raises(pkg.PiError):
+        pi.kv4_load(**calls["kv4_load"])                                                         # a closed context
+
+
 def test_store_skips_and_reports_a_slot_beyond_the_store():
     pi = context()
     rng = np.random.default_rng(6)

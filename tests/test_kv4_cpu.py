@@ -155,19 +155,27 @@ def test_the_front_end_refuses_what_is_not_on_the_gpu():
     pi.close = lambda: None                                     # (nothing was created)
     i32, bf = torch.zeros(4, dtype=torch.int32), torch.zeros((4, 8, 128), dtype=torch.bfloat16)
     blocks = torch.zeros((4, 20480), dtype=torch.uint8)
+    here = dict(stream=0)                                       # (the current stream of a device that is not there cannot be asked for)
+    with pytest.raises(TypeError, match="old_len"):
+        pi.assign_pages(i32, i32, torch.zeros((4, 512), dtype=torch.int32), i32, torch.zeros(4, dtype=torch.int64), **here)
+    with pytest.raises(TypeError, match="q: expected a CUDA tensor"):
+        pi.qk_norm_rope(torch.zeros((4, 32, 128), dtype=torch.bfloat16), bf, i32, None, bf, bf, **here)
+    with pytest.raises(TypeError, match="expected a tensor"):
+        pi.qk_norm_rope(None, bf, i32, None, bf, bf, **here)
+    with pytest.raises(TypeError, match="k: expected a CUDA tensor"):
+        pi.kv4_store(bf, bf, blocks, **here)
     with pytest.raises(TypeError):
-        pi.assign_pages(i32, i32, torch.zeros((4, 512), dtype=torch.int32), i32, torch.zeros(4, dtype=torch.int64))
+        pi.kv4_load(blocks.view(4, 2, 10240), bf, **here)       # not whole blocks
+    with pytest.raises(TypeError, match="out"):
+        pi.kv4_load(blocks, bf, **here)
     with pytest.raises(TypeError):
-        pi.qk_norm_rope(torch.zeros((4, 32, 128), dtype=torch.bfloat16), bf, i32, None, bf, bf)
+        pi.append_kv4(0, 1, bf, bf, i32, blocks, blocks, i32, i32, i32, bf, **here)
     with pytest.raises(TypeError):
-        pi.kv4_store(bf, bf, blocks)
+        pi.recall_kv4(0, blocks, blocks, torch.zeros((4, 8, 4), dtype=torch.int32), i32, **here)
+    with pytest.raises(TypeError, match="q"):
+        pi.sparse_decode_attn_kv4(0, torch.zeros((4, 32, 128), dtype=torch.bfloat16), blocks, i32, i32, i32, i32, bf, **here)
     with pytest.raises(TypeError):
-        pi.kv4_load(blocks.view(4, 2, 10240), bf)               # not whole blocks
-    with pytest.raises(pkg.PiError) as e:
-        pi.kv4_load(blocks, bf)                                 # neither on the GPU nor pinned
-    assert e.value.code == PINNED
-    with pytest.raises(TypeError):
-        pi.append_kv4(0, 1, bf, bf, i32, blocks, blocks, i32, i32, i32, bf)
-    with pytest.raises(TypeError):
-        pi.sparse_decode_attn_kv4(0, torch.zeros((4, 32, 128), dtype=torch.bfloat16), blocks, i32, i32, i32, i32, bf)
+        pi._front.kv4_load(pi._shape, blocks)                   # wrong number of arguments
+    with pytest.raises(ValueError):
+        pi._front.kv4_load(pi._ctx, blocks, bf, None, 0)        # not a shape
     pi._ctx = ctypes.c_void_p()
