@@ -165,6 +165,16 @@ void* stream_of(PyObject* o) {
 
 using Args = PyObject* const*;
 
+// The call itself, with the interpreter free for other threads (a launch may wait for room in the queue).  Arguments are
+// values: nothing of Python is touched inside.
+template <typename F, typename... A>
+int call(F function, A... arguments) {
+    PyThreadState* state = PyEval_SaveThread();
+    const int rc = function(arguments...);
+    PyEval_RestoreThread(state);
+    return rc;
+}
+
 int assign_pages(const Shape& s, Args a) {
     const at::Tensor& old_len = on(s, a[0], at::kInt, "old_len", {-1});
     const int batch = batch_of(old_len, "old_len");
@@ -177,7 +187,7 @@ int assign_pages(const Shape& s, Args a) {
     const int64_t n = a[6] != Py_None ? on(s, a[6], at::kLong, "slot_map", {-1}).size(0) : a[7] != Py_None ? on(s, a[7], at::kInt, "positions", {-1}).size(0) : 0;
     int64_t* slots = maybe<int64_t>(s, a[6], at::kLong, "slot_map", {n});
     int32_t* positions = maybe<int32_t>(s, a[7], at::kInt, "positions", {n});
-    return g_calls.assign_pages(s.ctx, batch, ptr<int32_t>(old_len), ptr<int32_t>(new_len), ptr<int32_t>(pages), pages.size(1), ptr<int32_t>(ring),
+    return call(g_calls.assign_pages, s.ctx, batch, ptr<int32_t>(old_len), ptr<int32_t>(new_len), ptr<int32_t>(pages), pages.size(1), ptr<int32_t>(ring),
                                 static_cast<int32_t>(ring.numel() < INT32_MAX ? ring.numel() : INT32_MAX), ptr<int64_t>(state), starts, n, slots, positions, stream_of(a[8]));
 }
 
@@ -200,7 +210,7 @@ int qk_norm_rope(const Shape& s, Args a) {
     const at::Tensor& positions = on(s, a[2], at::kInt, "positions", {T});
     const at::Tensor* freq = a[3] == Py_None ? nullptr : &on(s, a[3], at::kFloat, "inv_freq");
     const int64_t rot = freq ? 2 * freq->numel() : 0;
-    return g_calls.qk_norm_rope(s.ctx, T, dtype, q.data_ptr(), q_stride, k.data_ptr(), k_stride, ptr<int32_t>(positions),
+    return call(g_calls.qk_norm_rope, s.ctx, T, dtype, q.data_ptr(), q_stride, k.data_ptr(), k_stride, ptr<int32_t>(positions),
                                 maybe<float>(s, a[6], at::kFloat, "q_weight", {s.d}), maybe<float>(s, a[7], at::kFloat, "k_weight", {s.d}),
                                 static_cast<float>(number(a[8])), freq ? ptr<float>(*freq) : nullptr, rot > 256 ? 256 : static_cast<int>(rot), PyObject_IsTrue(a[9]) ? 1 : 0,
                                 on(s, a[4], at::kBFloat16, "q_out", {T, s.hq, s.d}).data_ptr(), on(s, a[5], at::kBFloat16, "k_out", {T, s.hkv, s.d}).data_ptr(), stream_of(a[10]));
@@ -228,7 +238,7 @@ int kv4_store(const Shape& s, Args a) {
     const int64_t* slots = maybe<int64_t>(s, a[3], at::kLong, "slot_map", {n});
     int64_t blocks = 0;
     void* store = blocks4(s, a[2], "store", true, &blocks).data_ptr();
-    return g_calls.kv4_store(s.ctx, n, k.data_ptr(), place[0][0], place[0][1], place[0][2], v.data_ptr(), place[1][0], place[1][1], place[1][2],
+    return call(g_calls.kv4_store, s.ctx, n, k.data_ptr(), place[0][0], place[0][1], place[0][2], v.data_ptr(), place[1][0], place[1][1], place[1][2],
                              dims == 4 ? k.size(1) : 0, slots, store, blocks, stream_of(a[4]));
 }
 
@@ -237,7 +247,7 @@ int kv4_load(const Shape& s, Args a) {
     const at::Tensor& out = on(s, a[1], at::kBFloat16, "out", {list ? list->numel() : -1, s.hkv, 2, s.b, s.d});
     int64_t blocks = 0;
     void* store = blocks4(s, a[0], "store", true, &blocks).data_ptr();
-    return g_calls.kv4_load(s.ctx, out.size(0), store, blocks, list ? ptr<int32_t>(*list) : nullptr, out.data_ptr(), stream_of(a[3]));
+    return call(g_calls.kv4_load, s.ctx, out.size(0), store, blocks, list ? ptr<int32_t>(*list) : nullptr, out.data_ptr(), stream_of(a[3]));
 }
 
 int append_kv4(const Shape& s, Args a) {
@@ -252,7 +262,7 @@ int append_kv4(const Shape& s, Args a) {
     }
     const at::Tensor &k = on(s, a[2], at::kBFloat16, "k_new", {batch, s.hkv, s.d}), &v = on(s, a[3], at::kBFloat16, "v_new", {batch, s.hkv, s.d});
     const Store4 st = store4(s, a[5], a[11], batch);
-    return g_calls.append_kv4(s.ctx, layer_of(a[0]), batch, step, step_dev, k.data_ptr(), v.data_ptr(), ptr<int32_t>(ctx_len), st.base, st.stride, st.pages, st.page_stride,
+    return call(g_calls.append_kv4, s.ctx, layer_of(a[0]), batch, step, step_dev, k.data_ptr(), v.data_ptr(), ptr<int32_t>(ctx_len), st.base, st.stride, st.pages, st.page_stride,
                               st.n_pages, pool4(s, a[6], batch), table<int32_t>(s, a[7], at::kInt, "block_table", batch * s.blocks),
                               table<int32_t>(s, a[8], at::kInt, "slot_block", batch * s.slots), table<uint32_t>(s, a[9], at::kInt, "slot_stamp", batch * s.slots),
                               table<void>(s, a[10], at::kBFloat16, "digest", batch * s.blocks * 2 * s.d), stream_of(a[12]));
@@ -263,7 +273,7 @@ int recall_kv4(const Shape& s, Args a) {
     const int batch = batch_of(count, "recall_count");
     const at::Tensor& lists = on(s, a[3], at::kInt, "recall_list", {batch, -1, 4});
     const Store4 st = store4(s, a[1], a[5], batch);
-    return g_calls.recall_kv4(s.ctx, layer_of(a[0]), batch, st.base, st.stride, st.pages, st.page_stride, st.n_pages, pool4(s, a[2], batch),
+    return call(g_calls.recall_kv4, s.ctx, layer_of(a[0]), batch, st.base, st.stride, st.pages, st.page_stride, st.n_pages, pool4(s, a[2], batch),
                               reinterpret_cast<const pi_extent*>(lists.data_ptr()), static_cast<int32_t>(lists.size(1) < INT32_MAX ? lists.size(1) : 0), ptr<int32_t>(count), stream_of(a[6]));
 }
 
@@ -271,7 +281,7 @@ int sparse_decode_attn_kv4(const Shape& s, Args a) {
     const at::Tensor& q = on(s, a[1], at::kBFloat16, "q", {-1, s.hq, s.d});
     const int batch = batch_of(q, "q");
     void* pool = pool4(s, a[2], batch);
-    return g_calls.sparse_decode_attn_kv4(s.ctx, layer_of(a[0]), batch, q.data_ptr(), pool, ptr<int32_t>(on(s, a[3], at::kInt, "sel_slots", {batch, s.budget})),
+    return call(g_calls.sparse_decode_attn_kv4, s.ctx, layer_of(a[0]), batch, q.data_ptr(), pool, ptr<int32_t>(on(s, a[3], at::kInt, "sel_slots", {batch, s.budget})),
                                           ptr<int32_t>(on(s, a[4], at::kInt, "sel_blocks", {batch, s.budget})), ptr<int32_t>(on(s, a[5], at::kInt, "sel_count", {batch})),
                                           ptr<int32_t>(on(s, a[6], at::kInt, "ctx_len", {batch})), on(s, a[7], at::kBFloat16, "out", {batch, s.hq, s.d}).data_ptr(),
                                           maybe<float>(s, a[8], at::kFloat, "lse", {batch, s.hq}), stream_of(a[9]));

@@ -152,7 +152,7 @@ assign_pages_kernel(PagesParams p) {
     }
     // Slot and position of every new token: a CTA takes one run of them, a warp spans of 64, a lane a pair of neighbours (whole
     // 16-byte stores side by side).  Four spans at a time, so that their page lookups are on their way together.  Most spans
-    // lie inside one sequence, which the warp then knows already.
+    // lie inside one sequence, which the warp then knows already; in the others every lane looks for itself.
     if (p.slots || p.positions) {
         // (n_tokens is at most 2^30, and `tokens` not above it: 32 bits do)
         const int n_tokens = static_cast<int>(p.n_tokens), total = static_cast<int>(tokens), lane = tid & 31;
@@ -165,57 +165,51 @@ assign_pages_kernel(PagesParams p) {
         };
         int s = -1, first = 0, next = 0, old = 0, ob = 0, grow = 0;       // the warp's sequence: its tokens are first .. next - 1
         for (int w0 = from + 64 * (tid >> 5); w0 < end; w0 += 64 * PAGES_WARPS * 4) {
-            int pos[4], pg[4][2];                                          // the pair's first position and the two pages, -1: none
-            bool apart[4];                                                 // the second token belongs to another sequence
+            int pos[4], pg[4][2];
+            unsigned rest = 0u;                                            // spans that every lane looks through for itself
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int w = w0 + 64 * PAGES_WARPS * k, t = w + 2 * lane;
-                pos[k] = pg[k][0] = pg[k][1] = -1;
-                apart[k] = false;
-                if (w >= end || w >= total) continue;
-                if (w >= next) {
+                const int w = w0 + 64 * PAGES_WARPS * k;
+                pg[k][0] = -1;
+                if (w >= end) continue;
+                if (w >= next && w < total) {
                     s = owner_of(s_tok, p.batch, w);
                     first = s_tok[s]; next = s_tok[s + 1]; old = s_old[s]; grow = s_grow[s];
                     ob = (old + B - 1) >> p.shift;
                 }
-                if (w + 64 <= next) {
-                    pos[k] = old + (t - first);
-                    pg[k][0] = lookup(s, ob, grow, pos[k]);
-                    pg[k][1] = ((pos[k] + 1) & (B - 1)) ? pg[k][0] : lookup(s, ob, grow, pos[k] + 1);
-                } else {
-                    // a span over a border: every lane looks for itself
-                    int s0 = -1;
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        if (t + u >= total) continue;
-                        const int si = owner_of(s_tok, p.batch, t + u), at = s_old[si] + (t + u - s_tok[si]);
-                        if (u == 0) { s0 = si; pos[k] = at; } else apart[k] = si != s0;
-                        pg[k][u] = lookup(si, (s_old[si] + B - 1) >> p.shift, s_grow[si], at);
-                    }
-                }
+                if (w + 64 > total || w + 64 > next) { rest |= 1u << k; continue; }
+                pos[k] = old + (w + 2 * lane - first);
+                pg[k][0] = pg[k][1] = lookup(s, ob, grow, pos[k]);
+                if (((pos[k] + 1) & (B - 1)) == 0) pg[k][1] = lookup(s, ob, grow, pos[k] + 1);
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int t = w0 + 64 * PAGES_WARPS * k + 2 * lane;
-                if (t >= end) continue;
-                int at[2] = {pos[k], pos[k] + 1};
-                if (apart[k]) { const int si = owner_of(s_tok, p.batch, t + 1); at[1] = s_old[si] + (t + 1 - s_tok[si]); }
-                int64_t slot[2];
+                const int w = w0 + 64 * PAGES_WARPS * k, t = w + 2 * lane;
+                if (w >= end || ((rest >> k) & 1u)) continue;
+                // (a page that is none is reported where every lane looks for itself)
+                if (!__all_sync(0xffffffffu, static_cast<unsigned>(pg[k][0]) < n && static_cast<unsigned>(pg[k][1]) < n)) { rest |= 1u << k; continue; }
+                const int64_t s0 = static_cast<int64_t>(pg[k][0]) * B + (pos[k] & (B - 1)), s1 = static_cast<int64_t>(pg[k][1]) * B + ((pos[k] + 1) & (B - 1));
+                if (p.slots) *reinterpret_cast<longlong2*>(p.slots + t) = make_longlong2(s0, s1);
+                if (p.positions) *reinterpret_cast<int2*>(p.positions + t) = make_int2(pos[k], pos[k] + 1);
+            }
+#pragma unroll 1
+            for (; rest; rest &= rest - 1) {
+                const int w = w0 + 64 * PAGES_WARPS * (__ffs(rest) - 1);
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    if (t + u >= total) { at[u] = -1; slot[u] = -1; continue; }
-                    slot[u] = (static_cast<int64_t>(pg[k][u]) << p.shift) + (at[u] & (B - 1));
-                    if (static_cast<unsigned>(pg[k][u]) >= static_cast<unsigned>(p.n_pages)) {
-                        slot[u] = -1;
-                        pi_report(p.st, PI_ERR_INDEX_RANGE, PI_STAGE_PAGES, -4, at[u], pg[k][u]);
+                    const int t = w + lane + 32 * u;
+                    if (t >= end) continue;
+                    int64_t slot = -1;
+                    int at = -1;
+                    if (t < total) {
+                        const int si = owner_of(s_tok, p.batch, t);
+                        at = s_old[si] + (t - s_tok[si]);
+                        const int pg1 = lookup(si, (s_old[si] + B - 1) >> p.shift, s_grow[si], at);
+                        if (static_cast<unsigned>(pg1) < n) slot = (static_cast<int64_t>(pg1) << p.shift) + (at & (B - 1));
+                        else pi_report(p.st, PI_ERR_INDEX_RANGE, PI_STAGE_PAGES, si, at, pg1);
                     }
-                }
-                if (t + 1 < n_tokens) {
-                    if (p.slots) *reinterpret_cast<longlong2*>(p.slots + t) = make_longlong2(slot[0], slot[1]);
-                    if (p.positions) *reinterpret_cast<int2*>(p.positions + t) = make_int2(at[0], at[1]);
-                } else {
-                    if (p.slots) p.slots[t] = slot[0];
-                    if (p.positions) p.positions[t] = at[0];
+                    if (p.slots) p.slots[t] = slot;
+                    if (p.positions) p.positions[t] = at;
                 }
             }
         }
