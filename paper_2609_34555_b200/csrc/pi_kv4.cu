@@ -1,5 +1,7 @@
 // Tokens into 4-bit blocks through a slot map, and 4-bit blocks back to bf16.  Both stream: 512 B of bf16 rows against
-// 160 B of codes and scales per (token, KV head), a handful of operations per value, bound by HBM.
+// 160 B of codes and scales per (token, KV head), a handful of operations per value.  Measured on a B200 at 65536 tokens of 8
+// KV heads (352 MB each way): load 54.6 us, 6.4 TB/s, bound by HBM; store 80 us, 4.4 TB/s, where issuing its 131
+// instructions per (token, head), 56 of them for the quotients, takes as long as the memory.
 #include "pi_kv4.cuh"
 
 namespace {
