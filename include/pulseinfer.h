@@ -342,7 +342,7 @@ int pi_append_kv_devstep(pi_ctx* ctx, int layer, int batch, const uint32_t* step
  *         2048..2303 K scales [16][4]{scale, minimum} bf16, 2304..2559 V scales likewise.
  * Each row of 128 channels is cut into 4 groups of 32: minimum = min x, scale = bf16((max x - min x) / 15)
  * computed in fp32, code = (x - minimum) / scale rounded half to even and clamped to 0..15 (0 where the
- * scale is 0); the value is scale * code + minimum.  K row: channel 32 j + 8 c + i is nibble i of the
+ * scale is 0; it is never negative); the value is scale * code + minimum.  K row: channel 32 j + 8 c + i is nibble i of the
  * little-endian 32-bit word at byte 16 c + 4 j; V row: channel 32 j + 4 r + i is nibble i of the 16-bit
  * word at byte 8 r + 2 j.  An infinite or NaN input, or a group whose spread overflows fp32, makes that
  * group of that row read back as NaN. */

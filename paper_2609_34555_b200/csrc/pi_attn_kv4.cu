@@ -21,7 +21,7 @@
 // across the cluster through distributed shared memory: one launch, no partials in global memory.
 //
 // Measured on a B200, back to back: 16 sequences x 128 blocks of 16 tokens, 8 KV heads, G = 4 (42 MB) 16.8 us; 64 x 64 blocks
-// of 32 tokens (165 MB) 44.6 us, 3.7 TB/s; one sequence x 64 blocks 6.2 us.  The copies alone take 10.9, 27.6 and 4.8 us:
+// of 32 tokens (165 MB) 44.6 us, 3.7 TB/s; one sequence x 64 blocks 5.9 us.  The copies alone take 10.9, 27.6 and 4.8 us:
 // what bounds the larger ones is the arithmetic, 405 instructions a tile and warp, of which 159 on the integer pipe and 64
 // packed fp16 ones at two cycles each (they do not overlap) and 20 matrix instructions at eight.
 // Tried and not taken: codes as 128 + code in bf16, or as 1024 + code with the offset taken off by a product with a constant
@@ -38,6 +38,7 @@ using namespace pi_attn;
 
 constexpr int A4_WARPS = 4;
 constexpr int A4_THREADS = A4_WARPS * 32;
+constexpr int A4_MAX_SPLIT = 8;                    // CTAs of a cluster that share an item
 // Up to 8 query heads a KV head a warp works on two tiles at a time (the checks and the set-up of a step are shared, and the
 // second tile's products fill the waits of the first), with one step ahead on its way; 16 warps an SM have 160 KB in
 // flight or at work then.  More heads leave registers for one tile, with three ahead.
@@ -574,14 +575,28 @@ attn_kv4_kernel(Attn4Params p) {
     const uint32_t at_o = smem_u32(s_o), at_m = smem_u32(s_l + A4_WARPS * p.G), at_l = at_m + 4 * p.G;
     for (int i = rank * A4_THREADS + tid; i < n_quads; i += S * A4_THREADS) {
         const int g = i >> 5;
+        // all of the others' numbers on their way at once: one after the other they would cost a round trip each
+        float mk[A4_MAX_SPLIT], lk[A4_MAX_SPLIT];
+        float4 x[A4_MAX_SPLIT];
+#pragma unroll
+        for (int k = 0; k < A4_MAX_SPLIT; ++k) {
+            mk[k] = A4_NO_MAX; lk[k] = 0.f;
+            x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (k < S) {
+                mk[k] = ld_shared_cluster_f32(map_shared_rank(at_m + 4 * g, k));
+                lk[k] = ld_shared_cluster_f32(map_shared_rank(at_l + 4 * g, k));
+                x[k] = ld_shared_cluster_f32x4(map_shared_rank(at_o + 16 * i, k));
+            }
+        }
         float M = A4_NO_MAX, L = 0.f;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = 0; k < S; ++k) M = fmaxf(M, ld_shared_cluster_f32(map_shared_rank(at_m + 4 * g, k)));
-        for (int k = 0; k < S; ++k) {
-            const float a = ex2(ld_shared_cluster_f32(map_shared_rank(at_m + 4 * g, k)) - M);
-            L = fmaf(ld_shared_cluster_f32(map_shared_rank(at_l + 4 * g, k)), a, L);
-            const float4 x = ld_shared_cluster_f32x4(map_shared_rank(at_o + 16 * i, k));
-            v.x = fmaf(x.x, a, v.x); v.y = fmaf(x.y, a, v.y); v.z = fmaf(x.z, a, v.z); v.w = fmaf(x.w, a, v.w);
+#pragma unroll
+        for (int k = 0; k < A4_MAX_SPLIT; ++k) M = fmaxf(M, mk[k]);
+#pragma unroll
+        for (int k = 0; k < A4_MAX_SPLIT; ++k) {
+            const float f = ex2(mk[k] - M);
+            L = fmaf(lk[k], f, L);
+            v.x = fmaf(x[k].x, f, v.x); v.y = fmaf(x[k].y, f, v.y); v.z = fmaf(x[k].z, f, v.z); v.w = fmaf(x[k].w, f, v.w);
         }
         write_out(i, M, L, v);
     }
@@ -610,7 +625,7 @@ int pi_launch_attn_kv4(pi_ctx* c, int batch, const void* q, const void* pool, co
     const long long items = static_cast<long long>(batch) * cfg.n_kv_heads, slots = static_cast<long long>(a4_ctas_per_sm(p.G <= 8 ? 1 : 2)) * c->n_sms;
     const int tiles = cfg.budget_blocks * (cfg.block_tokens / 16);
     int split = 1;
-    while (split < 8 && items * split * 2 <= slots && tiles >= split * 2 * A4_WARPS) split *= 2;
+    while (split < A4_MAX_SPLIT && items * split * 2 <= slots && tiles >= split * 2 * A4_WARPS) split *= 2;
     const size_t ring = static_cast<size_t>(A4_WARPS) * a4_steps(p.G <= 8 ? 1 : 2) * a4_tiles(p.G <= 8 ? 1 : 2) * KV4_TILE_BYTES + (p.G <= 8 ? 1 : 2) * (4 * 32 * 16 + 3 * 32 * 4 + 8 * 4);
     const size_t merge = (static_cast<size_t>(A4_WARPS) * p.G * (PI_HEAD_DIM + 2) + 2 * p.G) * sizeof(float);
     const size_t smem = ring > merge ? ring : merge;     // at most 46 KB: no attribute to set

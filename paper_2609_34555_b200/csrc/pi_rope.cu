@@ -5,7 +5,7 @@
 //   position * inv_freq[pair]; one rounding, to bf16, at the end.
 //
 // Streams each row once; bound by HBM from a few thousand tokens on, by latency below (B200, back to back: 32768 tokens of
-// 32 + 8 bf16 heads, 671 MB, 121 us, 5.5 TB/s; 2049 tokens of 64 + 8 fp16 heads 17.7 us; 16 tokens 2.0 us).  A warp works on one token, four
+// 32 + 8 bf16 heads, 671 MB, 120 us, 5.6 TB/s; 2049 tokens of 64 + 8 fp16 heads 17.4 us; 16 tokens 1.9 us).  A warp works on one token, four
 // rows at a time: eight lanes a row, 16 channels a lane (two runs of 8, 64 channels apart, so that both members of a
 // pair are in one lane for the usual pairing i / i + 64 and for neighbouring pairs alike).  The token's angles are
 // taken once per warp, two per lane, and shared through shared memory: the product position * inv_freq in 64 bits
@@ -17,7 +17,7 @@
 
 namespace {
 
-constexpr int ROPE_THREADS = 128;
+constexpr int ROPE_THREADS = 64;
 constexpr int ROPE_WARPS = ROPE_THREADS / 32;
 
 struct RopeParams {
@@ -39,10 +39,15 @@ template <> struct Raw<__nv_bfloat16> { uint4 a; };
 template <> struct Raw<__half> { uint4 a; };
 template <> struct Raw<float> { uint4 a, b; };
 
+__device__ __forceinline__ uint4 load_once(const uint4* p) {         // (L1 is left to the weights)
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
 template <typename T>
 __device__ __forceinline__ void load8(const T* p, Raw<T>& r) {
-    r.a = reinterpret_cast<const uint4*>(p)[0];
-    if constexpr (sizeof(T) == 4) r.b = reinterpret_cast<const uint4*>(p)[1];
+    r.a = load_once(reinterpret_cast<const uint4*>(p));
+    if constexpr (sizeof(T) == 4) r.b = load_once(reinterpret_cast<const uint4*>(p) + 1);
 }
 template <typename T>
 __device__ __forceinline__ void widen8(const Raw<T>& r, float* f) {
@@ -75,7 +80,7 @@ __device__ __forceinline__ uint4 narrow8(const float* f) {
 enum { PAIR_HALVES_FULL = 0, PAIR_NEIGHBOURS = 1, PAIR_HALVES_PART = 2 };
 
 template <typename T, int PAIR>
-__global__ void __launch_bounds__(ROPE_THREADS, 8)       // 64 registers: 32 warps an SM, 1 KB of loads each on their way
+__global__ void __launch_bounds__(ROPE_THREADS, 16)      // 64 registers: 32 warps an SM, 1 KB of loads each on their way
 qk_norm_rope_kernel(RopeParams p) {
     __shared__ float2 s_cs[ROPE_WARPS][64];                                    // cos, sin of the token's angles
     __shared__ float s_row[PAIR == PAIR_HALVES_PART ? ROPE_WARPS : 1][4][128];
