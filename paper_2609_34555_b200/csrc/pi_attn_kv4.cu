@@ -129,10 +129,11 @@ __device__ __forceinline__ uint32_t max_f16x2(uint32_t a, uint32_t b) {
     const __half2 v = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ float4 ld_shared_cluster_f32x4(uint32_t addr) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-    return v;
+__device__ __forceinline__ void st_cluster_f32x4(uint32_t addr, float4 v) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+__device__ __forceinline__ void st_cluster_f32x2(uint32_t addr, float a, float b) {
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1,%2};" ::"r"(addr), "f"(a), "f"(b) : "memory");
 }
 // The power of two at or below |x|, at least the smallest normal number.
 __device__ __forceinline__ float power_of(float x) { return __uint_as_float(max(__float_as_uint(x) & 0x7f800000u, 0x00800000u)); }
@@ -162,10 +163,20 @@ attn_kv4_kernel(Attn4Params p) {
     const int item = blockIdx.x / S, seq = item / p.Hkv, h = item - seq * p.Hkv;
     constexpr int TP = a4_tiles(NT), STEPS = a4_steps(NT), STAGES = STEPS * TP;
     const int SUB = p.B >> 4;
+    // (the other half of this barrier stands before the first store into another CTA's shared memory: by then it runs)
+    if (S > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     pi_grid_dependency_wait();
     pi_launch_dependents();
 
-    // the entries of the warp's first 32 tiles are fetched beside the list's length, whatever that turns out to be
+    // the queries, the entries of the warp's first 32 tiles and the list's length are fetched beside one another
+    uint4 query[NT][4];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int g = nt * 8 + r;
+        const __nv_bfloat16* qg = p.q + (static_cast<size_t>(seq) * p.Hq + static_cast<size_t>(h) * p.G + (g < p.G ? g : 0)) * PI_HEAD_DIM;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) query[nt][j] = g < p.G ? __ldg(reinterpret_cast<const uint4*>(qg + 32 * j + 8 * c)) : make_uint4(0, 0, 0, 0);
+    }
     const int first = rank * A4_WARPS + warp, stride = A4_WARPS * S, log_sub = 31 - __clz(SUB);
     const int32_t* slots = p.sel_slots + static_cast<size_t>(seq) * p.K;
     const int32_t* blocks = p.sel_blocks + static_cast<size_t>(seq) * p.K;
@@ -225,17 +236,17 @@ attn_kv4_kernel(Attn4Params p) {
     uint4* s_bq = reinterpret_cast<uint4*>(smem + A4_WARPS * STAGES * KV4_TILE_BYTES);       // [NT][4 groups][32 lanes]
     uint32_t* s_bz = reinterpret_cast<uint32_t*>(s_bq + NT * 4 * 32);                            // [NT][3][32]
     float* s_scale = reinterpret_cast<float*>(s_bz + NT * 3 * 32);                               // [NT][8 heads]
-    for (int part = warp; part < 4 * NT; part += A4_WARPS) {
-        const int nt = part >> 2, mine = part & 3, g = nt * 8 + r;
-        const bool real = g < p.G;
-        const __nv_bfloat16* qg = p.q + (static_cast<size_t>(seq) * p.Hq + static_cast<size_t>(h) * p.G + (real ? g : 0)) * PI_HEAD_DIM;
-        uint4 own = make_uint4(0, 0, 0, 0);
+    float4* s_in = reinterpret_cast<float4*>(s_scale + NT * 8);                                  // from the cluster: see the end
+    static_assert(A4_WARPS == 4, "one warp a group of channels");
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int mine = warp, part = nt * 4 + warp;
+        uint4 own = query[nt][0];
         __nv_bfloat162 top2 = __float2bfloat162_rn(0.f);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint4 x = real ? __ldg(reinterpret_cast<const uint4*>(qg + 32 * j + 8 * c)) : make_uint4(0, 0, 0, 0);
-            if (j == mine) own = x;
-            const __nv_bfloat162* y = reinterpret_cast<const __nv_bfloat162*>(&x);
+            if (j == mine) own = query[nt][j];
+            const __nv_bfloat162* y = reinterpret_cast<const __nv_bfloat162*>(&query[nt][j]);
             top2 = __hmax2(__hmax2(__hmax2(__habs2(y[0]), __habs2(y[1])), __hmax2(__habs2(y[2]), __habs2(y[3]))), top2);
         }
         float top = fmaxf(__low2float(top2), __high2float(top2));
@@ -529,10 +540,10 @@ attn_kv4_kernel(Attn4Params p) {
         }
     __syncthreads();
 
-    // ---- the warps' states into one: their factors first, once per head, then four channels a thread.  The result goes
-    // out, or, where a cluster shares the item, to s_o [0][G][128] (a thread's own places of warp 0's part, which nobody else
-    // reads) with the maximum and the sum in s_m / s_l behind the warps'.
-    const int n_quads = p.G * (PI_HEAD_DIM / 4);
+    // ---- the warps' states into one: their factors first, once per head, then four channels a thread.  The result goes out,
+    // or, where a cluster shares the item, to the CTA that concludes these channels: quads i of rank d's share into its
+    // s_in [from][share], with {maximum, sum} of every head behind them.
+    const int n_quads = p.G * (PI_HEAD_DIM / 4), share = (n_quads + S - 1) / S;
     for (int g = warp; g < p.G; g += A4_WARPS) {
         const float mk = lane < A4_WARPS ? s_m[lane * p.G + g] : A4_NO_MAX;
         float M = mk;
@@ -556,6 +567,7 @@ attn_kv4_kernel(Attn4Params p) {
         *reinterpret_cast<uint2*>(p.out + row * PI_HEAD_DIM + d) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
         if (p.lse && d == 0) p.lse[row] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : L == 0.f ? -INFINITY : L;
     };
+    if (S > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");        // every CTA of the cluster has begun
     for (int i = tid; i < n_quads; i += A4_THREADS) {
         const int g = i >> 5;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -566,42 +578,35 @@ attn_kv4_kernel(Attn4Params p) {
             v.x = fmaf(x.x, a, v.x); v.y = fmaf(x.y, a, v.y); v.z = fmaf(x.z, a, v.z); v.w = fmaf(x.w, a, v.w);
         }
         if (S == 1) write_out(i, s_l[A4_WARPS * p.G + g], s_l[A4_WARPS * p.G + p.G + g], v);
-        else reinterpret_cast<float4*>(s_o)[i] = v;
+        else {
+            const int to = i / share;
+            st_cluster_f32x4(map_shared_rank(smem_u32(s_in + rank * share + (i - to * share)), to), v);
+        }
     }
     if (S == 1) return;
     __syncwarp();
-    // ---- and the cluster's: every CTA concludes its share of the outputs, reading the others' shared memory
+    float2* s_ml = reinterpret_cast<float2*>(s_in + S * share);                   // [from][G]
+    for (int i = tid; i < S * p.G; i += A4_THREADS) {
+        const int to = i / p.G, g = i - to * p.G;
+        st_cluster_f32x2(map_shared_rank(smem_u32(s_ml + rank * p.G + g), to), s_l[A4_WARPS * p.G + g], s_l[A4_WARPS * p.G + p.G + g]);
+    }
+    __syncwarp();
     cluster_sync_all();
-    const uint32_t at_o = smem_u32(s_o), at_m = smem_u32(s_l + A4_WARPS * p.G), at_l = at_m + 4 * p.G;
-    for (int i = rank * A4_THREADS + tid; i < n_quads; i += S * A4_THREADS) {
-        const int g = i >> 5;
-        // all of the others' numbers on their way at once: one after the other they would cost a round trip each
-        float mk[A4_MAX_SPLIT], lk[A4_MAX_SPLIT];
-        float4 x[A4_MAX_SPLIT];
-#pragma unroll
-        for (int k = 0; k < A4_MAX_SPLIT; ++k) {
-            mk[k] = A4_NO_MAX; lk[k] = 0.f;
-            x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (k < S) {
-                mk[k] = ld_shared_cluster_f32(map_shared_rank(at_m + 4 * g, k));
-                lk[k] = ld_shared_cluster_f32(map_shared_rank(at_l + 4 * g, k));
-                x[k] = ld_shared_cluster_f32x4(map_shared_rank(at_o + 16 * i, k));
-            }
-        }
+    // ---- this CTA's share of the outputs, out of its own shared memory
+    for (int t = tid; t < share && rank * share + t < n_quads; t += A4_THREADS) {
+        const int i = rank * share + t, g = i >> 5;
         float M = A4_NO_MAX, L = 0.f;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int k = 0; k < A4_MAX_SPLIT; ++k) M = fmaxf(M, mk[k]);
-#pragma unroll
-        for (int k = 0; k < A4_MAX_SPLIT; ++k) {
-            const float f = ex2(mk[k] - M);
-            L = fmaf(lk[k], f, L);
-            v.x = fmaf(x[k].x, f, v.x); v.y = fmaf(x[k].y, f, v.y); v.z = fmaf(x[k].z, f, v.z); v.w = fmaf(x[k].w, f, v.w);
+        for (int k = 0; k < S; ++k) M = fmaxf(M, s_ml[k * p.G + g].x);
+        for (int k = 0; k < S; ++k) {
+            const float2 ml = s_ml[k * p.G + g];
+            const float4 x = s_in[k * share + t];
+            const float f = ex2(ml.x - M);
+            L = fmaf(ml.y, f, L);
+            v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
         }
         write_out(i, M, L, v);
     }
-    __syncwarp();
-    cluster_sync_all();                                 // nobody leaves while its state may still be read
 }
 
 }  // namespace
@@ -627,9 +632,11 @@ int pi_launch_attn_kv4(pi_ctx* c, int batch, const void* q, const void* pool, co
     int split = 1;
     while (split < A4_MAX_SPLIT && items * split * 2 <= slots && tiles >= split * 2 * A4_WARPS) split *= 2;
     const size_t ring = static_cast<size_t>(A4_WARPS) * a4_steps(p.G <= 8 ? 1 : 2) * a4_tiles(p.G <= 8 ? 1 : 2) * KV4_TILE_BYTES + (p.G <= 8 ? 1 : 2) * (4 * 32 * 16 + 3 * 32 * 4 + 8 * 4);
-    const size_t merge = (static_cast<size_t>(A4_WARPS) * p.G * (PI_HEAD_DIM + 2) + 2 * p.G) * sizeof(float);
-    const size_t smem = ring > merge ? ring : merge;     // at most 46 KB: no attribute to set
+    // (the merge of a CTA's warps, up to 33 KB, takes the ring's place; what the cluster sends lies behind)
+    const size_t share = (static_cast<size_t>(p.G) * (PI_HEAD_DIM / 4) + split - 1) / split;
+    const size_t smem = ring + (split > 1 ? split * (share * 16 + static_cast<size_t>(p.G) * 8) : 0);
     auto launch = [&](auto kernel) -> int {
+        if (smem > 48 * 1024) PI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
         cudaLaunchConfig_t lc = {};
         lc.gridDim = dim3(static_cast<unsigned>(items * split));
         lc.blockDim = dim3(A4_THREADS);
