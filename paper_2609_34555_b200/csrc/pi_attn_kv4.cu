@@ -20,14 +20,16 @@
 // end.  Every warp keeps its own running maximum and sum; the states are merged once, through shared memory, and
 // across the cluster through distributed shared memory: one launch, no partials in global memory.
 //
-// Measured on a B200, back to back: 16 sequences x 128 blocks of 16 tokens, 8 KV heads, G = 4 (42 MB) 16.8 us; 64 x 64 blocks
-// of 32 tokens (165 MB) 44.6 us, 3.7 TB/s; one sequence x 64 blocks 5.9 us.  The copies alone take 10.9, 27.6 and 4.8 us:
-// what bounds the larger ones is the arithmetic, 405 instructions a tile and warp, of which 159 on the integer pipe and 64
+// Measured on a B200, back to back: 16 sequences x 128 blocks of 16 tokens, 8 KV heads, G = 4 (42 MB) 15.8 us; 64 x 64 blocks
+// of 32 tokens (165 MB) 44.3 us, 3.7 TB/s; one sequence x 64 blocks 4.8 us.  The copies alone take 10.9 and 27.6 us of
+// the larger ones: what bounds them is the arithmetic, 405 instructions a tile and warp, of which 159 on the integer pipe and 64
 // packed fp16 ones at two cycles each (they do not overlap) and 20 matrix instructions at eight.
 // Tried and not taken: codes as 128 + code in bf16, or as 1024 + code with the offset taken off by a product with a constant
 // (one operation less a pair, paid back in matrix instructions); fp8 products (mma.sync turns the operands into fp16 first);
 // one CTA per item of 8 warps, and 3 CTAs of 168 registers an SM (slower by 5 to 10 %).
 #include <cuda_fp16.h>
+
+#include <type_traits>
 
 #include "pi_attn_core.cuh"
 #include "pi_kv4.cuh"
@@ -540,72 +542,64 @@ attn_kv4_kernel(Attn4Params p) {
         }
     __syncthreads();
 
-    // ---- the warps' states into one: their factors first, once per head, then four channels a thread.  The result goes out,
-    // or, where a cluster shares the item, to the CTA that concludes these channels: quads i of rank d's share into its
-    // s_in [from][share], with {maximum, sum} of every head behind them.
-    const int n_quads = p.G * (PI_HEAD_DIM / 4), share = (n_quads + S - 1) / S;
-    for (int g = warp; g < p.G; g += A4_WARPS) {
-        const float mk = lane < A4_WARPS ? s_m[lane * p.G + g] : A4_NO_MAX;
-        float M = mk;
-#pragma unroll
-        for (int d = A4_WARPS / 2; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-        const float a = lane < A4_WARPS ? ex2(mk - M) : 0.f;
-        float L = lane < A4_WARPS ? a * s_l[lane * p.G + g] : 0.f;
-#pragma unroll
-        for (int d = A4_WARPS / 2; d; d >>= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
-        __syncwarp();
-        if (lane < A4_WARPS) s_m[lane * p.G + g] = a;
-        if (lane == 0) { s_l[A4_WARPS * p.G + g] = M; s_l[A4_WARPS * p.G + p.G + g] = L; }
-    }
-    __syncthreads();
-    auto write_out = [&](int i, float M, float L, float4 v) {
-        const int g = i >> 5, d = 4 * (i & 31);
+    // ---- the warps' states into one, four channels (a quad) a thread.  The result goes out, or, where a cluster shares the
+    // item, to the CTA that concludes these channels: every head's 32 quads are cut into S runs, run d goes into rank d's
+    // s_in [from][head][quad of the run], with the {maximum, sum} of the head in s_ml [from][head].
+    const int n_quads = p.G * (PI_HEAD_DIM / 4), log_run = 5 - (31 - __clz(S)), run = 1 << log_run, share = p.G << log_run;
+    float2* s_ml = reinterpret_cast<float2*>(s_in + S * share);
+    auto write_out = [&](int g, int quad, float M, float L, float4 v) {
         const size_t row = static_cast<size_t>(seq) * p.Hq + static_cast<size_t>(h) * p.G + g;
         const float f = L > 0.f ? 1.f / L : 0.f;
         // (a NaN among the sums has to come through: 0 only where nothing was summed)
         const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x * f, v.y * f), hi = __floats2bfloat162_rn(v.z * f, v.w * f);
-        *reinterpret_cast<uint2*>(p.out + row * PI_HEAD_DIM + d) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-        if (p.lse && d == 0) p.lse[row] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : L == 0.f ? -INFINITY : L;
+        *reinterpret_cast<uint2*>(p.out + row * PI_HEAD_DIM + 4 * quad) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+        if (p.lse && quad == 0) p.lse[row] = L > 0.f ? (M + log2f(L)) * 0.6931471805599453f : L == 0.f ? -INFINITY : L;
+    };
+    // N states {maximum, sum, quad} into one
+    auto join = [&](auto number, const float* m_of, const float* l_of, int ml_step, const float4* v_of, int v_step, int n, float& M, float& L, float4& v) {
+        constexpr int N = decltype(number)::value;
+        float mk[N], lk[N];
+        float4 x[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const bool has = k < n;
+            mk[k] = has ? m_of[k * ml_step] : A4_NO_MAX;
+            lk[k] = has ? l_of[k * ml_step] : 0.f;
+            x[k] = has ? v_of[k * v_step] : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        M = A4_NO_MAX; L = 0.f;
+        v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < N; ++k) M = fmaxf(M, mk[k]);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float f = ex2(mk[k] - M);
+            L = fmaf(lk[k], f, L);
+            v.x = fmaf(x[k].x, f, v.x); v.y = fmaf(x[k].y, f, v.y); v.z = fmaf(x[k].z, f, v.z); v.w = fmaf(x[k].w, f, v.w);
+        }
     };
     if (S > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");        // every CTA of the cluster has begun
     for (int i = tid; i < n_quads; i += A4_THREADS) {
-        const int g = i >> 5;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int k = 0; k < A4_WARPS; ++k) {
-            const float a = s_m[k * p.G + g];
-            const float4 x = reinterpret_cast<const float4*>(s_o)[k * n_quads + i];
-            v.x = fmaf(x.x, a, v.x); v.y = fmaf(x.y, a, v.y); v.z = fmaf(x.z, a, v.z); v.w = fmaf(x.w, a, v.w);
-        }
-        if (S == 1) write_out(i, s_l[A4_WARPS * p.G + g], s_l[A4_WARPS * p.G + p.G + g], v);
-        else {
-            const int to = i / share;
-            st_cluster_f32x4(map_shared_rank(smem_u32(s_in + rank * share + (i - to * share)), to), v);
-        }
+        const int g = i >> 5, quad = i & 31;
+        float M, L;
+        float4 v;
+        join(std::integral_constant<int, A4_WARPS>(), s_m + g, s_l + g, p.G, reinterpret_cast<const float4*>(s_o) + i, n_quads, A4_WARPS, M, L, v);
+        if (S == 1) { write_out(g, quad, M, L, v); continue; }
+        const int to = quad >> log_run, at = quad & (run - 1);
+        st_cluster_f32x4(map_shared_rank(smem_u32(s_in + rank * share + (g << log_run) + at), to), v);
+        if (at == 0) st_cluster_f32x2(map_shared_rank(smem_u32(s_ml + rank * p.G + g), to), M, L);
     }
     if (S == 1) return;
     __syncwarp();
-    float2* s_ml = reinterpret_cast<float2*>(s_in + S * share);                   // [from][G]
-    for (int i = tid; i < S * p.G; i += A4_THREADS) {
-        const int to = i / p.G, g = i - to * p.G;
-        st_cluster_f32x2(map_shared_rank(smem_u32(s_ml + rank * p.G + g), to), s_l[A4_WARPS * p.G + g], s_l[A4_WARPS * p.G + p.G + g]);
-    }
-    __syncwarp();
     cluster_sync_all();
     // ---- this CTA's share of the outputs, out of its own shared memory
-    for (int t = tid; t < share && rank * share + t < n_quads; t += A4_THREADS) {
-        const int i = rank * share + t, g = i >> 5;
-        float M = A4_NO_MAX, L = 0.f;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = 0; k < S; ++k) M = fmaxf(M, s_ml[k * p.G + g].x);
-        for (int k = 0; k < S; ++k) {
-            const float2 ml = s_ml[k * p.G + g];
-            const float4 x = s_in[k * share + t];
-            const float f = ex2(ml.x - M);
-            L = fmaf(ml.y, f, L);
-            v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
-        }
-        write_out(i, M, L, v);
+    for (int t = tid; t < share; t += A4_THREADS) {
+        const int g = t >> log_run;
+        const float* ml = reinterpret_cast<const float*>(s_ml + g);
+        float M, L;
+        float4 v;
+        join(std::integral_constant<int, A4_MAX_SPLIT>(), ml, ml + 1, 2 * p.G, s_in + t, share, S, M, L, v);
+        write_out(g, (rank << log_run) + (t & (run - 1)), M, L, v);
     }
 }
 
@@ -633,8 +627,7 @@ int pi_launch_attn_kv4(pi_ctx* c, int batch, const void* q, const void* pool, co
     while (split < A4_MAX_SPLIT && items * split * 2 <= slots && tiles >= split * 2 * A4_WARPS) split *= 2;
     const size_t ring = static_cast<size_t>(A4_WARPS) * a4_steps(p.G <= 8 ? 1 : 2) * a4_tiles(p.G <= 8 ? 1 : 2) * KV4_TILE_BYTES + (p.G <= 8 ? 1 : 2) * (4 * 32 * 16 + 3 * 32 * 4 + 8 * 4);
     // (the merge of a CTA's warps, up to 33 KB, takes the ring's place; what the cluster sends lies behind)
-    const size_t share = (static_cast<size_t>(p.G) * (PI_HEAD_DIM / 4) + split - 1) / split;
-    const size_t smem = ring + (split > 1 ? split * (share * 16 + static_cast<size_t>(p.G) * 8) : 0);
+    const size_t smem = ring + (split > 1 ? static_cast<size_t>(p.G) * (PI_HEAD_DIM * 4 + split * 8) : 0);
     auto launch = [&](auto kernel) -> int {
         if (smem > 48 * 1024) PI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
         cudaLaunchConfig_t lc = {};
