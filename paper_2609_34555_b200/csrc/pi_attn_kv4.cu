@@ -20,8 +20,8 @@
 // end.  Every warp keeps its own running maximum and sum; the states are merged once, through shared memory, and
 // across the cluster through distributed shared memory: one launch, no partials in global memory.
 //
-// Measured on a B200, back to back: 16 sequences x 128 blocks of 16 tokens, 8 KV heads, G = 4 (42 MB) 15.8 us; 64 x 64 blocks
-// of 32 tokens (165 MB) 44.3 us, 3.7 TB/s; one sequence x 64 blocks 4.8 us.  The copies alone take 10.9 and 27.6 us of
+// Measured on a B200, back to back: 16 sequences x 128 blocks of 16 tokens, 8 KV heads, G = 4 (42 MB) 15.9 us; 64 x 64 blocks
+// of 32 tokens (165 MB) 44.8 us, 3.7 TB/s; one sequence x 64 blocks 4.8 us.  The copies alone take 10.9 and 27.6 us of
 // the larger ones: what bounds them is the arithmetic, 405 instructions a tile and warp, of which 159 on the integer pipe and 64
 // packed fp16 ones at two cycles each (they do not overlap) and 20 matrix instructions at eight.
 // Tried and not taken: codes as 128 + code in bf16, or as 1024 + code with the offset taken off by a product with a constant
@@ -48,7 +48,7 @@ __host__ __device__ constexpr int a4_tiles(int NT) { return NT == 1 ? 2 : 1; }
 __host__ __device__ constexpr int a4_steps(int NT) { return NT == 1 ? 2 : 4; }      // steps in the ring
 __host__ __device__ constexpr int a4_ctas_per_sm(int NT) { return NT == 1 ? 4 : 2; }    // what the registers allow
 constexpr float A4_NO_UNIT = 0x1p120f;             // before a group's first product: every product but 0 leaves fp16
-constexpr float A4_NO_MAX = -1e30f;                // stands for -infinity in the running maximum: differences stay numbers
+constexpr float A4_NO_MAX = -3.40282347e38f;       // the lowest number, for -infinity in the running maximum: differences are no NaN
 
 struct Attn4Params {
     const __nv_bfloat16* q;
@@ -381,6 +381,8 @@ attn_kv4_kernel(Attn4Params p) {
         }
         // ---- online softmax over the step's tokens.  The reference m moves only when a score exceeds it by 8 (a factor of
         // 256, far from any overflow), so that most steps neither reduce a maximum across lanes nor touch the sums.
+        // (The score is rounded before m is taken off: fused, the rounding of m would be left over in every weight, and for
+        // scores of 2^28 and more that alone leaves the range.  One operation a score, 1 % of the time.)
         float w[TP][NT][4];
         bool over = false;
 #pragma unroll
@@ -388,7 +390,10 @@ attn_kv4_kernel(Attn4Params p) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w[k][nt][e] = fmaf(s[k][nt][e], scale[nt][e & 1], -m[nt][e & 1]);
+                for (int e = 0; e < 4; ++e) {
+                    s[k][nt][e] = __fmul_rn(s[k][nt][e], scale[nt][e & 1]);
+                    w[k][nt][e] = s[k][nt][e] - m[nt][e & 1];
+                }
                 over |= max3(fmaxf(w[k][nt][0], w[k][nt][1]), w[k][nt][2], w[k][nt][3]) > 8.f;
             }
         if (__any_sync(0xffffffffu, over)) {
@@ -399,7 +404,6 @@ attn_kv4_kernel(Attn4Params p) {
                     float mx = fmaxf(s[0][nt][e], s[0][nt][2 + e]);
 #pragma unroll
                     for (int k = 1; k < TP; ++k) mx = max3(mx, s[k][nt][e], s[k][nt][2 + e]);
-                    mx *= scale[nt][e];
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
@@ -409,8 +413,8 @@ attn_kv4_kernel(Attn4Params p) {
                     z[nt][e] *= alpha;
 #pragma unroll
                     for (int k = 0; k < TP; ++k) {
-                        w[k][nt][e] = fmaf(s[k][nt][e], scale[nt][e], -m_new);
-                        w[k][nt][2 + e] = fmaf(s[k][nt][2 + e], scale[nt][e], -m_new);
+                        w[k][nt][e] = s[k][nt][e] - m_new;
+                        w[k][nt][2 + e] = s[k][nt][2 + e] - m_new;
                     }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {

@@ -638,6 +638,47 @@ def test_attention_with_small_and_large_values(spread):
     pi.close()
 
 
+@pytest.mark.parametrize("size", [1e4, 1e9, 1e20, 1e32])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_attention_with_scores_of_any_size(size, sign):
+    """Equal scores, then one that stands out, anywhere in the range of 32 bits."""
+    pi = context(budget_blocks=20)
+    c = pi.cfg
+    case = attention_case(pi, [300, 17], 5, garbage=False)
+    rng = np.random.default_rng(2)
+    kv = ref.bf16(rng.standard_normal((2 * c.pool_slots, 2, 2, 16, 128)))
+    key = float(ref.bf16(np.float32(1.37 * size ** 0.5)))
+    kv[:, :, 0] = key                                                                 # a constant row is stored exactly
+    q = float(ref.bf16(np.float32(sign * 1.71 * size ** 0.5)))
+    case["q"][:] = q
+    case["pool"] = ref.pack(kv, 16).reshape(case["pool"].shape)
+    score = 128 * q * key / 128 ** 0.5
+    out, lse = run_attention(pi, case)
+    held = ref.unpack(case["pool"].reshape(2 * c.pool_slots, -1), 2, 16).reshape(2, c.pool_slots, 2, 2, 16, 128)
+    pick = []
+    for s, n in enumerate((300, 17)):
+        v = np.concatenate([held[s, case["slots"][s, i], :, 1, :min(16, n - 16 * case["blocks"][s, i])] for i in range(case["count"][s])], axis=1)
+        assert v.shape[1] == n
+        want = np.repeat(v.mean(axis=1), 4, axis=0)
+        # weights are all alike up to the rounding of weight times scale (as in check_attention); the score carries at
+        # most nine cuts of 2^-23 in its one product that is not 0 and a few roundings of 2^-24 after it: below 2^-19 of itself
+        assert (np.abs(out[s].double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * np.abs(v).max()).all()
+        want_lse = score + np.log(n)
+        assert (np.abs(lse[s].double().cpu().numpy() - want_lse) <= 2.0 ** -19 * abs(score) + 2.0 ** -18).all()
+        pick.append(v[:, 0])
+    # the first token of each list half as far from 0 (scores below it) or twice as far (above it): the others' weights are nothing
+    for s in range(2):
+        kv.reshape(2, c.pool_slots, 2, 2, 16, 128)[s, case["slots"][s, 0], :, 0, 0] = key * (2.0 if sign > 0 else 0.5)
+    case["pool"] = ref.pack(kv, 16).reshape(case["pool"].shape)
+    out, lse = run_attention(pi, case)
+    for s in range(2):
+        want = np.repeat(pick[s], 4, axis=0)
+        assert (np.abs(out[s].double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * np.abs(want).max()).all()
+        top = score * (2.0 if sign > 0 else 0.5)
+        assert (np.abs(lse[s].double().cpu().numpy() - top) <= 2.0 ** -19 * abs(top) + 2.0 ** -18).all()
+    pi.close()
+
+
 def test_attention_reports_bad_lists_and_leaves_the_other_sequences_alone():
     pi = context(budget_blocks=16)
     case = attention_case(pi, [250, 250, 250, 250], 8)
