@@ -187,6 +187,10 @@ int assign_pages(const Shape& s, Args a) {
     const int64_t n = a[6] != Py_None ? on(s, a[6], at::kLong, "slot_map", {-1}).size(0) : a[7] != Py_None ? on(s, a[7], at::kInt, "positions", {-1}).size(0) : 0;
     int64_t* slots = maybe<int64_t>(s, a[6], at::kLong, "slot_map", {n});
     int32_t* positions = maybe<int32_t>(s, a[7], at::kInt, "positions", {n});
+    // (a map of no entries has no address, which would say that none is wanted; with one, new tokens are refused for it)
+    alignas(16) static int64_t none[2];
+    if (a[6] != Py_None && n == 0) slots = none;
+    if (a[7] != Py_None && n == 0) positions = reinterpret_cast<int32_t*>(none);
     return call(g_calls.assign_pages, s.ctx, batch, ptr<int32_t>(old_len), ptr<int32_t>(new_len), ptr<int32_t>(pages), pages.size(1), ptr<int32_t>(ring),
                                 static_cast<int32_t>(ring.numel() < INT32_MAX ? ring.numel() : INT32_MAX), ptr<int64_t>(state), starts, n, slots, positions, stream_of(a[8]));
 }

@@ -370,6 +370,24 @@ def test_pages_refuse_as_a_whole():
     pi.close()
 
 
+def test_pages_with_maps_of_no_entries():
+    """They hold nothing: new tokens are refused for them, and calls without new tokens run."""
+    pi = context(max_blocks=8)
+    table = torch.full((2, 8), -1, dtype=torch.int32, device=DEV)
+    ring, counters = pi.free_page_ring(10)
+    was = counters.clone(), table.clone()
+    slots, positions = torch.empty(0, dtype=torch.int64, device=DEV), torch.empty(0, dtype=torch.int32, device=DEV)
+    for maps in (dict(slot_map=slots), dict(positions=positions), dict(slot_map=slots, positions=positions)):
+        pi.assign_pages(i32([0, 0]), i32([0, 3]), table, ring, counters, **maps)
+        assert clean(pi, -9)[2] == -2
+        assert torch.equal(counters, was[0]) and torch.equal(table, was[1])
+    pi.assign_pages(i32([0, 0]), i32([20, 3]), table, ring, counters)
+    pi.assign_pages(i32([20, 3]), i32([16, 0]), table, ring, counters, slot_map=slots, positions=positions)
+    clean(pi)
+    assert counters.tolist()[:2] == [3, 12] and (table[0, 1:] == -1).all() and (table[1] == -1).all()
+    pi.close()
+
+
 def test_pages_of_the_largest_batch_and_a_long_prompt():
     pi = context(max_batch=4096, max_blocks=16384, block_tokens=16)
     batch = 4096
