@@ -20,9 +20,9 @@
 // end.  Every warp keeps its own running maximum and sum; the states are merged once, through shared memory, and
 // across the cluster through distributed shared memory: one launch, no partials in global memory.
 //
-// Measured on a B200, back to back: 16 sequences x 128 blocks of 16 tokens, 8 KV heads, G = 4 (42 MB) 15.9 us; 64 x 64 blocks
-// of 32 tokens (165 MB) 44.8 us, 3.7 TB/s; one sequence x 64 blocks 4.8 us.  The copies alone take 10.9 and 27.6 us of
-// the larger ones: what bounds them is the arithmetic, 405 instructions a tile and warp, of which 159 on the integer pipe and 64
+// Measured on a B200, back to back: 16 sequences x 128 blocks of 16 tokens, 8 KV heads, G = 4 (42 MB) 15.6 us; 64 x 64 blocks
+// of 32 tokens (165 MB) 43.8 us, 3.8 TB/s; one sequence x 64 blocks 4.8 us.  The copies alone take 10.9 and 27.6 us of
+// the larger ones: what bounds them is the arithmetic, 396 instructions a tile and warp, of which 159 on the integer pipe and 48
 // packed fp16 ones at two cycles each (they do not overlap) and 20 matrix instructions at eight.
 // Tried and not taken: codes as 128 + code in bf16, or as 1024 + code with the offset taken off by a product with a constant
 // (one operation less a pair, paid back in matrix instructions); fp8 products (mma.sync turns the operands into fp16 first);
@@ -62,7 +62,7 @@ struct Attn4Params {
     pi_status_ref st;
     long long block_bytes;
     float scale_log2;
-    uint32_t raise;                 // 0x64006400
+    uint32_t raise, raise64;        // 0x64006400, 0x54005400
     int Hq, Hkv, G, B, K, C;
 };
 
@@ -98,6 +98,18 @@ __device__ __forceinline__ void code_pairs(uint32_t w, uint32_t raise, uint32_t 
         const __half2 x = __hadd2(*reinterpret_cast<const __half2*>(&a), low), y = __hfma2(*reinterpret_cast<const __half2*>(&b), sixteenth, high);
         p[2 * i] = *reinterpret_cast<const uint32_t*>(&x);
         p[2 * i + 1] = *reinterpret_cast<const uint32_t*>(&y);
+    }
+}
+// The same, but with the second pair as 64 + code (0x5400 | 16 nibble): half the operations.  For K, where the offset's part
+// of the products is taken off with the minima's.
+__device__ __forceinline__ void code_pairs_k(uint32_t w, uint32_t raise, uint32_t raise64, uint32_t (&p)[4]) {
+    const __half2 low = __halves2half2(__ushort_as_half(0xe400), __ushort_as_half(0xe400));        // -1024
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t v = i ? w >> 8 : w, a = masked(v, 0x000f000fu, raise);
+        const __half2 x = __hadd2(*reinterpret_cast<const __half2*>(&a), low);
+        p[2 * i] = *reinterpret_cast<const uint32_t*>(&x);
+        p[2 * i + 1] = masked(v, 0x00f000f0u, raise64);
     }
 }
 // d = a b
@@ -233,8 +245,9 @@ attn_kv4_kernel(Attn4Params p) {
 
     // ---- the queries as B operands, in the channel order of the K codes, as fp16 numbers: every head is scaled by a power of
     // two so that its largest channel lies in [1, 2); what is below 2^-14 of that is rounded at 2^-25 of it, less than the
-    // sums below round.  With them, for the minima's own products, lane (r, c)'s {0, sum} of head r over the channels of
-    // group c, as three bf16 numbers (2^-25 together).  One warp prepares a group of channels for all.
+    // sums below round.  With them, for the minima's own products, lane (r, c)'s {-64 times the sum over every
+    // second pair, sum} of head r over the channels of group c, to meet {scale, minimum}, as three bf16 numbers (2^-25
+    // together).  One warp prepares a group of channels for all.
     uint4* s_bq = reinterpret_cast<uint4*>(smem + A4_WARPS * STAGES * KV4_TILE_BYTES);       // [NT][4 groups][32 lanes]
     uint32_t* s_bz = reinterpret_cast<uint32_t*>(s_bq + NT * 4 * 32);                            // [NT][3][32]
     float* s_scale = reinterpret_cast<float*>(s_bz + NT * 3 * 32);                               // [NT][8 heads]
@@ -266,14 +279,21 @@ attn_kv4_kernel(Attn4Params p) {
         }
         // pair n = channels (n, n + 4) of the eight
         s_bq[part * 32 + lane] = make_uint4(pack_f16(f[0], f[4]), pack_f16(f[1], f[5]), pack_f16(f[2], f[6]), pack_f16(f[3], f[7]));
+        float off = 0.f;                           // what 64 at every second pair adds, of the numbers as they are packed
+#pragma unroll
+        for (int i = 1; i < 8; i += 2) off -= 64.f * __half2float(__float2half_rn(f[i]));
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        off += __shfl_xor_sync(0xffffffffu, off, 1);
+        off += __shfl_xor_sync(0xffffffffu, off, 2);
         if (c == mine) {
 #pragma unroll
             for (int i = 0; i < 3; ++i) {
                 const float hi = __bfloat162float(__float2bfloat16_rn(sum));
-                s_bz[(nt * 3 + i) * 32 + lane] = pack_bf16(0.f, hi);
+                const float oh = __bfloat162float(__float2bfloat16_rn(off));
+                s_bz[(nt * 3 + i) * 32 + lane] = pack_bf16(oh, hi);
                 sum -= hi;
+                off -= oh;
             }
             if (mine == 0) s_scale[nt * 8 + r] = p.scale_log2 * top;
         }
@@ -314,7 +334,7 @@ attn_kv4_kernel(Attn4Params p) {
     const int pr = (r >> 1) + 4 * (r & 1);
     const int pl = ((lane & 7) >> 1) + 4 * (lane & 1) + (lane & 8);     // the token whose scales this lane names to ldmatrix
 
-    const uint32_t raise = p.raise;
+    const uint32_t raise = p.raise, raise64 = p.raise64;
     uint32_t tile = ring;                                // first stage of the step at hand
     for (int n = 0; n < n_mine; n += TP, tile = tile == ring + (STAGES - TP) * KV4_TILE_BYTES ? ring : tile + TP * KV4_TILE_BYTES) {
         const int i = n & 31;
@@ -353,8 +373,8 @@ attn_kv4_kernel(Attn4Params p) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 uint32_t a[4], b[4];
-                code_pairs(word_of(ka, j), raise, a);
-                code_pairs(word_of(kb, j), raise, b);
+                code_pairs_k(word_of(ka, j), raise, raise64, a);
+                code_pairs_k(word_of(kb, j), raise, raise64, b);
                 const float sa = kv4_scale_of(word_of(za, j)), sb = kv4_scale_of(word_of(zb, j));
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
@@ -622,6 +642,7 @@ int pi_launch_attn_kv4(pi_ctx* c, int batch, const void* q, const void* pool, co
     p.block_bytes = kv4_block_bytes(cfg.n_kv_heads, cfg.block_tokens);
     p.scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(PI_HEAD_DIM));
     p.raise = 0x64006400u;
+    p.raise64 = 0x54005400u;
     p.Hq = cfg.n_q_heads; p.Hkv = cfg.n_kv_heads; p.G = cfg.n_q_heads / cfg.n_kv_heads;
     p.B = cfg.block_tokens; p.K = cfg.budget_blocks; p.C = cfg.pool_slots;
     // CTAs per item: as many as fill the GPU with what fits an SM, as long as every warp still has a tile
