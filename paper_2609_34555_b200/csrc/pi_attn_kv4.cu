@@ -178,7 +178,7 @@ attn_kv4_kernel(Attn4Params p) {
     constexpr int TP = a4_tiles(NT), STEPS = a4_steps(NT), STAGES = STEPS * TP;
     const int SUB = p.B >> 4;
     // (the other half of this barrier stands before the first store into another CTA's shared memory: by then it runs)
-    if (S > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    if (S > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
     pi_grid_dependency_wait();
     pi_launch_dependents();
 
@@ -602,7 +602,7 @@ attn_kv4_kernel(Attn4Params p) {
             v.x = fmaf(x[k].x, f, v.x); v.y = fmaf(x[k].y, f, v.y); v.z = fmaf(x[k].z, f, v.z); v.w = fmaf(x[k].w, f, v.w);
         }
     };
-    if (S > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");        // every CTA of the cluster has begun
+    if (S > 1) asm volatile("barrier.cluster.wait;" ::: "memory");        // every CTA of the cluster has begun
     for (int i = tid; i < n_quads; i += A4_THREADS) {
         const int g = i >> 5, quad = i & 31;
         float M, L;
@@ -614,8 +614,7 @@ attn_kv4_kernel(Attn4Params p) {
         if (at == 0) st_cluster_f32x2(map_shared_rank(smem_u32(s_ml + rank * p.G + g), to), M, L);
     }
     if (S == 1) return;
-    __syncwarp();
-    cluster_sync_all();
+    asm volatile("barrier.cluster.arrive;\n\tbarrier.cluster.wait;" ::: "memory");      // (not .aligned: lanes leave the loop at different times)
     // ---- this CTA's share of the outputs, out of its own shared memory
     for (int t = tid; t < share; t += A4_THREADS) {
         const int g = t >> log_run;
