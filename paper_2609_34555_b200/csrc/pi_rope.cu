@@ -77,13 +77,19 @@ __device__ __forceinline__ uint4 narrow8(const float* f) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-enum { PAIR_HALVES_FULL = 0, PAIR_NEIGHBOURS = 1, PAIR_HALVES_PART = 2 };
+// How a pair's members lie: 64 channels apart, side by side, a multiple of 8 apart, any other distance.
+enum { PAIR_HALVES_FULL = 0, PAIR_NEIGHBOURS = 1, PAIR_HALVES_RUNS = 2, PAIR_HALVES_ANY = 3 };
+
+// What the registers are cut to.  16-bit inputs, pairs at a fixed distance: 64 registers, 32 warps an SM with 1 KB of loads each on
+// their way.  Other distances want 72 (8192 tokens of 40 heads, 64 channels turned: 34.8 us, 41.2 with 64); 32-bit inputs,
+// with twice the bytes a load, 96 (43.7 us; 45 with 80 and 74 with 64, where they no longer fit).
+constexpr int rope_ctas_per_sm(int bytes, int pair) { return bytes == 4 ? 10 : pair == PAIR_HALVES_FULL || pair == PAIR_NEIGHBOURS ? 16 : 14; }
 
 template <typename T, int PAIR>
-__global__ void __launch_bounds__(ROPE_THREADS, 16)      // 64 registers: 32 warps an SM, 1 KB of loads each on their way
+__global__ void __launch_bounds__(ROPE_THREADS, rope_ctas_per_sm(sizeof(T), PAIR))
 qk_norm_rope_kernel(RopeParams p) {
     __shared__ float2 s_cs[ROPE_WARPS][64];                                    // cos, sin of the token's angles
-    __shared__ float s_row[PAIR == PAIR_HALVES_PART ? ROPE_WARPS : 1][4][128];
+    __shared__ float s_row[PAIR == PAIR_HALVES_ANY ? ROPE_WARPS : 1][4][8 * 16 + 8];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane >> 3, l = lane & 7;
     const long long unit = static_cast<long long>(blockIdx.x) * ROPE_WARPS + warp;
     pi_grid_dependency_wait();
@@ -94,11 +100,16 @@ qk_norm_rope_kernel(RopeParams p) {
     const T* q = static_cast<const T*>(p.q) + t * p.q_stride;
     const T* k = static_cast<const T*>(p.k) + t * p.k_stride;
 
+    // The lane's two runs of 8 channels.  Pairs a multiple of 8 apart: run i and run i + half / 8, and of the channels that are not
+    // turned the rest, in order.
+    const int gap = p.half >> 3;
+    const bool turned = PAIR != PAIR_HALVES_RUNS || l < gap;
+    const int run_a = turned ? l : l + gap, run_b = PAIR == PAIR_HALVES_RUNS && turned ? l + gap : l + 8;
     auto src = [&](int row) { return row < p.Hq ? q + row * PI_HEAD_DIM : k + (row - p.Hq) * PI_HEAD_DIM; };
     Raw<T> a = {}, b = {};
     int quad = part;
     int row = quad * 4 + sub;
-    if (row < H) { load8(src(row) + 8 * l, a); load8(src(row) + 64 + 8 * l, b); }
+    if (row < H) { load8(src(row) + 8 * run_a, a); load8(src(row) + 8 * run_b, b); }
     const float freq[2] = {lane < p.half ? __ldg(p.inv_freq + lane) : 0.f, lane + 32 < p.half ? __ldg(p.inv_freq + lane + 32) : 0.f};
     const int pos = p.pos[t];
     if (pos < 0) return;                                                       // a padding token: its rows stay as they were
@@ -111,12 +122,20 @@ qk_norm_rope_kernel(RopeParams p) {
             turns -= rint(turns);
             sincospif(2.f * static_cast<float>(turns), &cs.y, &cs.x);
         }
-        s_cs[warp][f] = cs;
+        s_cs[warp][PAIR == PAIR_HALVES_ANY ? (f & 7) * 8 + (f >> 3) : f] = cs;
     }
     __syncwarp();
     float2 cs[8];                                                              // this lane's eight angles
 #pragma unroll
-    for (int e = 0; e < 8; ++e) cs[e] = s_cs[warp][PAIR == PAIR_NEIGHBOURS ? (e < 4 ? 4 * l + e : 32 + 4 * l + e - 4) : 8 * l + e];
+    for (int e = 0; e < 8; ++e) {
+        if (PAIR == PAIR_HALVES_ANY) {                                        // of the lane's first run; the sine with its sign
+            const int d = 8 * l + e, f = d < p.half ? d : d - p.half;          // (f < 64)
+            cs[e] = s_cs[warp][(f & 7) * 8 + (f >> 3)];
+            if (d < p.half) cs[e].y = -cs[e].y;
+        } else {
+            cs[e] = s_cs[warp][PAIR == PAIR_NEIGHBOURS ? (e < 4 ? 4 * l + e : 32 + 4 * l + e - 4) : 8 * l + e];
+        }
+    }
 
     for (; quad < n_quads; quad += p.parts) {
         row = quad * 4 + sub;
@@ -124,13 +143,13 @@ qk_norm_rope_kernel(RopeParams p) {
         widen8(a, x);
         widen8(b, x + 8);
         const int next = row + 4 * p.parts;
-        if (next < H) { load8(src(next) + 8 * l, a); load8(src(next) + 64 + 8 * l, b); }
+        if (next < H) { load8(src(next) + 8 * run_a, a); load8(src(next) + 8 * run_b, b); }
         if (p.wq) {
             // (the weights come out of L1 every time: kept in registers they would cost a quarter of the resident warps)
-            const float4* g = reinterpret_cast<const float4*>(row >= p.Hq ? p.wk : p.wq) + 2 * l;
+            const float4* g = reinterpret_cast<const float4*>(row >= p.Hq ? p.wk : p.wq);
             float4 w[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = __ldg(g + (i < 2 ? i : 14 + i));
+            for (int i = 0; i < 4; ++i) w[i] = __ldg(g + 2 * (i < 2 ? run_a : run_b) + (i & 1));
             float ss = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) ss = fmaf(x[i], x[i], ss);
@@ -143,9 +162,10 @@ qk_norm_rope_kernel(RopeParams p) {
                 x[4 * i] *= r * w[i].x; x[4 * i + 1] *= r * w[i].y; x[4 * i + 2] *= r * w[i].z; x[4 * i + 3] *= r * w[i].w;
             }
         }
-        if (PAIR == PAIR_HALVES_FULL) {
+        if (PAIR == PAIR_HALVES_FULL || PAIR == PAIR_HALVES_RUNS) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
+                if (!turned) continue;
                 const float u = x[e], v = x[8 + e];
                 x[e] = u * cs[e].x - v * cs[e].y;
                 x[8 + e] = v * cs[e].x + u * cs[e].y;
@@ -159,24 +179,33 @@ qk_norm_rope_kernel(RopeParams p) {
                 x[2 * e + 1] = v * cs[e].x + u * cs[e].y;
             }
         } else {
-            // the members of a pair are rot_dim / 2 channels apart, in whichever lanes: through shared memory
+            // The members of a pair are rot_dim / 2 channels apart, in whichever lanes: through shared memory, channel d at
+            // place 16 (d % 8) + d / 8, so that for any distance the lanes' places lie side by side.
             float* sr = s_row[warp][sub];
+            const bool both = p.half > 32;                                     // the second run is turned too
             __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sr[(i < 8 ? 0 : 56) + 8 * l + i] = x[i];
+            for (int e = 0; e < 8; ++e) {
+                sr[16 * e + l] = x[e];
+                if (both) sr[16 * e + 8 + l] = x[8 + e];
+            }
             __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int d = (i < 8 ? 0 : 56) + 8 * l + i;
-                if (d < p.half) { const float2 z = s_cs[warp][d]; x[i] = x[i] * z.x - sr[d + p.half] * z.y; }
-                else if (d < 2 * p.half) { const float2 z = s_cs[warp][d - p.half]; x[i] = x[i] * z.x + sr[d - p.half] * z.y; }
+            for (int e = 0; e < 8; ++e) {
+                const int d = 8 * l + e, o = d < p.half ? d + p.half : d - p.half;
+                if (d < 2 * p.half) x[e] = fmaf(x[e], cs[e].x, sr[16 * (o & 7) + (o >> 3)] * cs[e].y);
+                const int f = d + 64 - p.half;                                // (of the second run: always the second member of its pair)
+                if (both && f < p.half) {
+                    const float2 z = s_cs[warp][(f & 7) * 8 + (f >> 3)];
+                    x[8 + e] = fmaf(x[8 + e], z.x, sr[16 * (f & 7) + (f >> 3)] * z.y);
+                }
             }
         }
         if (row < H) {
             uint4* dst = reinterpret_cast<uint4*>(row < p.Hq ? p.q_out + (static_cast<size_t>(t) * p.Hq + row) * PI_HEAD_DIM
                                                              : p.k_out + (static_cast<size_t>(t) * p.Hkv + row - p.Hq) * PI_HEAD_DIM);
-            dst[l] = narrow8(x);
-            dst[8 + l] = narrow8(x + 8);
+            dst[run_a] = narrow8(x);
+            dst[run_b] = narrow8(x + 8);
         }
     }
 }
@@ -185,9 +214,10 @@ template <typename T>
 int launch(const RopeParams& p, int interleaved, cudaStream_t stream) {
     const long long units = static_cast<long long>(p.n_tokens) * p.parts;
     const dim3 grid(static_cast<unsigned>((units + ROPE_WARPS - 1) / ROPE_WARPS)), block(ROPE_THREADS);
-    if (interleaved) PI_CUDA_TRY(pi_launch_pdl(qk_norm_rope_kernel<T, PAIR_NEIGHBOURS>, grid, block, 0, stream, p));
+    if (interleaved || p.half == 0) PI_CUDA_TRY(pi_launch_pdl(qk_norm_rope_kernel<T, PAIR_NEIGHBOURS>, grid, block, 0, stream, p));
     else if (p.half == 64) PI_CUDA_TRY(pi_launch_pdl(qk_norm_rope_kernel<T, PAIR_HALVES_FULL>, grid, block, 0, stream, p));
-    else PI_CUDA_TRY(pi_launch_pdl(qk_norm_rope_kernel<T, PAIR_HALVES_PART>, grid, block, 0, stream, p));
+    else if (p.half % 8 == 0) PI_CUDA_TRY(pi_launch_pdl(qk_norm_rope_kernel<T, PAIR_HALVES_RUNS>, grid, block, 0, stream, p));
+    else PI_CUDA_TRY(pi_launch_pdl(qk_norm_rope_kernel<T, PAIR_HALVES_ANY>, grid, block, 0, stream, p));
     return PI_OK;
 }
 

@@ -249,6 +249,37 @@ def test_norm_and_rotation(T, Hq, Hkv, dtype, rot, inter, norm, fused):
     pi.close()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("inter", [False, True])
+def test_rotation_of_any_part_of_the_channels(dtype, inter):
+    """Every even rot_dim; infinities and NaN behind the turned channels stay where they are."""
+    pi = context(n_q_heads=6, n_kv_heads=2)
+    g = torch.Generator().manual_seed(17)
+    T = 9
+    q, k = [(torch.randn((T, h, 128), generator=g) * 2).to(dtype).to(DEV) for h in (6, 2)]
+    pos = np.random.default_rng(3).integers(0, 1 << 17, T).astype(np.int32)
+    for rot in range(0, 129, 2):
+        freq = (10000.0 ** (-np.arange(0, rot, 2) / max(rot, 1))).astype(np.float32)
+        a, b = q.clone(), k.clone()
+        if rot < 128:
+            a[1, :, rot:] = torch.inf
+            a[2, :, 127] = torch.nan
+            b[3, 0, rot] = -torch.inf
+        qo, ko = torch.full_like(q, 5.0, dtype=torch.bfloat16), torch.full_like(k, 5.0, dtype=torch.bfloat16)
+        pi.qk_norm_rope(a, b, i32(pos), dev(freq) if rot else None, qo, ko, interleaved=inter)
+        clean(pi)
+        for got, src, x in ((qo, a, q), (ko, b, k)):
+            got, src = got.double().cpu().numpy(), src.double().cpu().numpy()
+            want = ref.rope(x.double().cpu().numpy(), pos, freq, None, 0.0, inter)
+            want[..., rot:] = src[..., rot:]
+            # as above: one rounding to bf16, and under 2^-19 of the pair's length before it
+            tol = 2.0 ** -8 * np.abs(want) + 2.0 ** -19 * np.abs(x.double().cpu().numpy()).max() * np.sqrt(2)
+            same = (got == want) | (np.isnan(got) & np.isnan(want))
+            with np.errstate(invalid="ignore"):
+                assert (same | (np.abs(got - want) <= tol)).all(), rot
+    pi.close()
+
+
 def test_norm_and_rotation_in_place_and_far_rows_of_a_fused_projection():
     pi = context(n_q_heads=8, n_kv_heads=2)
     g = torch.Generator().manual_seed(3)
