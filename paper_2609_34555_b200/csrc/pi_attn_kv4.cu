@@ -14,7 +14,7 @@
 // Codes are exact in fp16, queries after a power of two per head; weights times scales are rounded to 11 bits, each an
 // eighth of the output's own rounding and of random sign; all sums are in 32 bits.
 //
-// One (sequence, KV head) per cluster of S CTAs of 4 warps (S = 1, 2, 4 or 8 by the launcher's rule).  The item's
+// One (sequence, KV head) per cluster of S CTAs of 4 or 8 warps (S = 1, 2, 4 or 8; both by the launcher's rule).  The item's
 // 16-token tiles are dealt out to its warps in turn; a warp streams its own tiles through its own ring of shared-memory
 // stages with 16-byte asynchronous copies (a tile is 2560 contiguous bytes), so no warp waits for another until the
 // end.  Every warp keeps its own running maximum and sum; the states are merged once, through shared memory, and
@@ -29,6 +29,7 @@
 // one CTA per item of 8 warps, and 3 CTAs of 168 registers an SM (slower by 5 to 10 %).
 #include <cuda_fp16.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "pi_attn_core.cuh"
@@ -38,15 +39,13 @@ namespace {
 
 using namespace pi_attn;
 
-constexpr int A4_WARPS = 4;
-constexpr int A4_THREADS = A4_WARPS * 32;
 constexpr int A4_MAX_SPLIT = 8;                    // CTAs of a cluster that share an item
 // Up to 8 query heads a KV head a warp works on two tiles at a time (the checks and the set-up of a step are shared, and the
 // second tile's products fill the waits of the first), with one step ahead on its way; 16 warps an SM have 160 KB in
 // flight or at work then.  More heads leave registers for one tile, with three ahead.
 __host__ __device__ constexpr int a4_tiles(int NT) { return NT == 1 ? 2 : 1; }
 __host__ __device__ constexpr int a4_steps(int NT) { return NT == 1 ? 2 : 4; }      // steps in the ring
-__host__ __device__ constexpr int a4_ctas_per_sm(int NT) { return NT == 1 ? 4 : 2; }    // what the registers allow
+__host__ __device__ constexpr int a4_warps_per_sm(int NT) { return NT == 1 ? 16 : 8; }  // what the registers allow
 constexpr float A4_NO_UNIT = 0x1p120f;             // before a group's first product: every product but 0 leaves fp16
 constexpr float A4_NO_MAX = -3.40282347e38f;       // the lowest number, for -infinity in the running maximum: differences are no NaN
 
@@ -167,9 +166,9 @@ __device__ __forceinline__ float ex2(float x) {
 }
 __device__ __forceinline__ uint32_t word_of(const uint4& v, int j) { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; }
 
-// NT: tiles of 8 query heads.
-template <int NT>
-__global__ void __launch_bounds__(A4_THREADS, a4_ctas_per_sm(NT))
+// NT: tiles of 8 query heads; WARPS of a CTA.
+template <int NT, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, a4_warps_per_sm(NT) / WARPS)
 attn_kv4_kernel(Attn4Params p) {
     extern __shared__ __align__(128) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, c = lane & 3;
@@ -191,7 +190,7 @@ attn_kv4_kernel(Attn4Params p) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) query[nt][j] = g < p.G ? __ldg(reinterpret_cast<const uint4*>(qg + 32 * j + 8 * c)) : make_uint4(0, 0, 0, 0);
     }
-    const int first = rank * A4_WARPS + warp, stride = A4_WARPS * S, log_sub = 31 - __clz(SUB);
+    const int first = rank * WARPS + warp, stride = WARPS * S, log_sub = 31 - __clz(SUB);
     const int32_t* slots = p.sel_slots + static_cast<size_t>(seq) * p.K;
     const int32_t* blocks = p.sel_blocks + static_cast<size_t>(seq) * p.K;
     auto entry_of = [&](int n) -> int2 {
@@ -248,13 +247,14 @@ attn_kv4_kernel(Attn4Params p) {
     // sums below round.  With them, for the minima's own products, lane (r, c)'s {-64 times the sum over every
     // second pair, sum} of head r over the channels of group c, to meet {scale, minimum}, as three bf16 numbers (2^-25
     // together).  One warp prepares a group of channels for all.
-    uint4* s_bq = reinterpret_cast<uint4*>(smem + A4_WARPS * STAGES * KV4_TILE_BYTES);       // [NT][4 groups][32 lanes]
+    uint4* s_bq = reinterpret_cast<uint4*>(smem + WARPS * STAGES * KV4_TILE_BYTES);       // [NT][4 groups][32 lanes]
     uint32_t* s_bz = reinterpret_cast<uint32_t*>(s_bq + NT * 4 * 32);                            // [NT][3][32]
     float* s_scale = reinterpret_cast<float*>(s_bz + NT * 3 * 32);                               // [NT][8 heads]
     float4* s_in = reinterpret_cast<float4*>(s_scale + NT * 8);                                  // from the cluster: see the end
-    static_assert(A4_WARPS == 4, "one warp a group of channels");
+    static_assert(WARPS >= 4, "one warp a group of channels");
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
+        if (WARPS > 4 && warp >= 4) break;
         const int mine = warp, part = nt * 4 + warp;
         uint4 own = query[nt][0];
         __nv_bfloat162 top2 = __float2bfloat162_rn(0.f);
@@ -545,8 +545,8 @@ attn_kv4_kernel(Attn4Params p) {
     // ---- the warp's state into shared memory: o [warp][G][128], then m and l [warp][G] (the ring is done with)
     __syncthreads();
     float* s_o = reinterpret_cast<float*>(smem);
-    float* s_m = s_o + A4_WARPS * p.G * PI_HEAD_DIM;
-    float* s_l = s_m + A4_WARPS * p.G;
+    float* s_m = s_o + WARPS * p.G * PI_HEAD_DIM;
+    float* s_l = s_m + WARPS * p.G;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -603,11 +603,11 @@ attn_kv4_kernel(Attn4Params p) {
         }
     };
     if (S > 1) asm volatile("barrier.cluster.wait;" ::: "memory");        // every CTA of the cluster has begun
-    for (int i = tid; i < n_quads; i += A4_THREADS) {
+    for (int i = tid; i < n_quads; i += WARPS * 32) {
         const int g = i >> 5, quad = i & 31;
         float M, L;
         float4 v;
-        join(std::integral_constant<int, A4_WARPS>(), s_m + g, s_l + g, p.G, reinterpret_cast<const float4*>(s_o) + i, n_quads, A4_WARPS, M, L, v);
+        join(std::integral_constant<int, WARPS>(), s_m + g, s_l + g, p.G, reinterpret_cast<const float4*>(s_o) + i, n_quads, WARPS, M, L, v);
         if (S == 1) { write_out(g, quad, M, L, v); continue; }
         const int to = quad >> log_run, at = quad & (run - 1);
         st_cluster_f32x4(map_shared_rank(smem_u32(s_in + rank * share + (g << log_run) + at), to), v);
@@ -616,7 +616,7 @@ attn_kv4_kernel(Attn4Params p) {
     if (S == 1) return;
     asm volatile("barrier.cluster.arrive;\n\tbarrier.cluster.wait;" ::: "memory");      // (not .aligned: lanes leave the loop at different times)
     // ---- this CTA's share of the outputs, out of its own shared memory
-    for (int t = tid; t < share; t += A4_THREADS) {
+    for (int t = tid; t < share; t += WARPS * 32) {
         const int g = t >> log_run;
         const float* ml = reinterpret_cast<const float*>(s_ml + g);
         float M, L;
@@ -645,18 +645,23 @@ int pi_launch_attn_kv4(pi_ctx* c, int batch, const void* q, const void* pool, co
     p.Hq = cfg.n_q_heads; p.Hkv = cfg.n_kv_heads; p.G = cfg.n_q_heads / cfg.n_kv_heads;
     p.B = cfg.block_tokens; p.K = cfg.budget_blocks; p.C = cfg.pool_slots;
     // CTAs per item: as many as fill the GPU with what fits an SM, as long as every warp still has a tile
-    const long long items = static_cast<long long>(batch) * cfg.n_kv_heads, slots = static_cast<long long>(a4_ctas_per_sm(p.G <= 8 ? 1 : 2)) * c->n_sms;
+    const int NT = p.G <= 8 ? 1 : 2;
+    const long long items = static_cast<long long>(batch) * cfg.n_kv_heads, room = static_cast<long long>(a4_warps_per_sm(NT)) * c->n_sms;
     const int tiles = cfg.budget_blocks * (cfg.block_tokens / 16);
-    int split = 1;
-    while (split < A4_MAX_SPLIT && items * split * 2 <= slots && tiles >= split * 2 * A4_WARPS) split *= 2;
-    const size_t ring = static_cast<size_t>(A4_WARPS) * a4_steps(p.G <= 8 ? 1 : 2) * a4_tiles(p.G <= 8 ? 1 : 2) * KV4_TILE_BYTES + (p.G <= 8 ? 1 : 2) * (4 * 32 * 16 + 3 * 32 * 4 + 8 * 4);
-    // (the merge of a CTA's warps, up to 33 KB, takes the ring's place; what the cluster sends lies behind)
+    int split = 1, warps = 4;
+    while (split < A4_MAX_SPLIT && items * split * 2 * warps <= room && tiles >= split * 2 * warps) split *= 2;
+    // Few items with long lists leave SMs with one CTA each, which 8 warps use better (8 items x 256 tiles 7.1 us, 8.0 with 4
+    // warps; x 1024 15.6, 20.8); a shorter list or more items pay for the larger merge (8 x 128 tiles gain 3 %, 16 x 256
+    // lose 2 to 8 %).
+    if (NT == 1 && split == A4_MAX_SPLIT && items * split * 8 <= room && tiles >= 32 * std::max(items, 8ll)) warps = 8;
+    const size_t ring = static_cast<size_t>(warps) * a4_steps(NT) * a4_tiles(NT) * KV4_TILE_BYTES + NT * (4 * 32 * 16 + 3 * 32 * 4 + 8 * 4);
+    // (the merge of a CTA's warps, up to 33 KB for four, takes the ring's place; what the cluster sends lies behind)
     const size_t smem = ring + (split > 1 ? static_cast<size_t>(p.G) * (PI_HEAD_DIM * 4 + split * 8) : 0);
     auto launch = [&](auto kernel) -> int {
         if (smem > 48 * 1024) PI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
         cudaLaunchConfig_t lc = {};
         lc.gridDim = dim3(static_cast<unsigned>(items * split));
-        lc.blockDim = dim3(A4_THREADS);
+        lc.blockDim = dim3(warps * 32);
         lc.dynamicSmemBytes = smem;
         lc.stream = stream;
         cudaLaunchAttribute attr[2];
@@ -671,6 +676,6 @@ int pi_launch_attn_kv4(pi_ctx* c, int batch, const void* q, const void* pool, co
         PI_CUDA_TRY(cudaLaunchKernelEx(&lc, kernel, p));
         return PI_OK;
     };
-    if (p.G <= 8) return launch(attn_kv4_kernel<1>);
-    return launch(attn_kv4_kernel<2>);
+    if (NT == 1) return warps == 4 ? launch(attn_kv4_kernel<1, 4>) : launch(attn_kv4_kernel<1, 8>);
+    return launch(attn_kv4_kernel<2, 4>);
 }

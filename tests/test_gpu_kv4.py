@@ -643,6 +643,17 @@ def test_attention(Hq, Hkv, B, K, ctx):
     pi.close()
 
 
+@pytest.mark.parametrize("Hq,Hkv,B,K", [(3, 1, 16, 256), (4, 1, 16, 300), (8, 2, 16, 257), (8, 1, 64, 70), (14, 2, 32, 150), (20, 2, 16, 300)])
+def test_attention_over_long_lists_of_few_sequences(Hq, Hkv, B, K):
+    """From 256 tiles on a few sequences take larger CTAs: lists of every length, empty ones among them."""
+    pi = context(n_q_heads=Hq, n_kv_heads=Hkv, block_tokens=B, budget_blocks=K, pool_slots=K + 3, max_batch=4, max_blocks=2 * K)
+    for ctx in ([K * B], [K * B - 3, 0], [37, 1, 2 * K * B - 9, 0], [B * K // 2, 17 * B + 1]):
+        case = attention_case(pi, ctx, len(ctx))
+        out, lse = run_attention(pi, case)
+        check_attention(pi, case, out, lse)
+    pi.close()
+
+
 @pytest.mark.parametrize("Hq,Hkv", [(4, 1), (8, 1), (16, 1)])
 def test_attention_over_a_long_list_of_one_sequence(Hq, Hkv):
     """4 096 blocks of 64 tokens, the largest budget: 2 048 tiles for each of eight CTAs."""
