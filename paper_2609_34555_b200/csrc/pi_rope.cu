@@ -5,9 +5,10 @@
 //   position * inv_freq[pair]; one rounding, to bf16, at the end.
 //
 // Streams each row once; bound by HBM from a few thousand tokens on, by latency below (B200, back to back: 32768 tokens of
-// 32 + 8 bf16 heads, 671 MB, 120 us, 5.6 TB/s; 2049 tokens of 64 + 8 fp16 heads 17.4 us; 16 tokens 1.9 us).  A warp works on one token, four
-// rows at a time: eight lanes a row, 16 channels a lane (two runs of 8, 64 channels apart, so that both members of a
-// pair are in one lane for the usual pairing i / i + 64 and for neighbouring pairs alike).  The token's angles are
+// 32 + 8 bf16 heads, 671 MB, 120 us, 5.6 TB/s; 2049 tokens of 64 + 8 fp16 heads 17.5 us; 16 tokens 1.9 us;
+// 8192 tokens of 32 + 8 heads 34 us in 16 bits, 44 us in 32).  A warp works on one token, four
+// rows at a time: eight lanes a row, 16 channels a lane: two runs of 8, chosen so that both members of a pair are
+// in one lane for neighbouring pairs and for pairs any multiple of 8 channels apart; other distances go through shared memory.  The token's angles are
 // taken once per warp, two per lane, and shared through shared memory: the product position * inv_freq in 64 bits
 // (32 lose a far position's angle: at 131072 radians their spacing is 2^-7), reduced to a fraction of a turn there,
 // the sine and cosine of the rest in 32.
