@@ -644,12 +644,23 @@ int pi_launch_attn_kv4(pi_ctx* c, int batch, const void* q, const void* pool, co
     p.raise64 = 0x54005400u;
     p.Hq = cfg.n_q_heads; p.Hkv = cfg.n_kv_heads; p.G = cfg.n_q_heads / cfg.n_kv_heads;
     p.B = cfg.block_tokens; p.K = cfg.budget_blocks; p.C = cfg.pool_slots;
-    // CTAs per item: as many as fill the GPU with what fits an SM, as long as every warp still has a tile
-    const int NT = p.G <= 8 ? 1 : 2;
+    const int NT = p.G <= 8 ? 1 : 2, tiles = cfg.budget_blocks * (cfg.block_tokens / 16);
     const long long items = static_cast<long long>(batch) * cfg.n_kv_heads, room = static_cast<long long>(a4_warps_per_sm(NT)) * c->n_sms;
-    const int tiles = cfg.budget_blocks * (cfg.block_tokens / 16);
+    // CTAs per item: what takes least by this estimate (microseconds, less what every call takes).  A cluster costs 1.0 more than
+    // a CTA by itself; a step of its warps 1.0, or with k CTAs on the SM 0.12 + 0.59 k, when they fill its pipes (more than 8
+    // heads: 0.8, or 0.5 k); the GPU starts 170 CTAs (85) in one, from three an SM on all in 3.0.  Measured, with S = 1 / 2 / 4 /
+    // 8: 64 items x 64 tiles 11.5 / 8.3 / 7.1 / 7.9 us, 144 x 16 tiles 5.3 / 5.9 / 10.8 / 16.5, 8 x 48 tiles 8.9 / 6.9 / 5.9 /
+    // 5.0, 128 x 128 tiles 20.2 / 16.0 / 15.8 / 19.9.  Clusters that would not all be on the GPU at once lose to smaller ones.
     int split = 1, warps = 4;
-    while (split < A4_MAX_SPLIT && items * split * 2 * warps <= room && tiles >= split * 2 * warps) split *= 2;
+    double least = 0.;
+    for (int s = 1; s <= A4_MAX_SPLIT; s *= 2) {
+        const long long ctas = items * s, per_sm = (ctas + c->n_sms - 1) / c->n_sms, per_step = s * warps * a4_tiles(NT), steps = (tiles + per_step - 1) / per_step;
+        if (s > 1 && ctas * warps > room * 7 / 8) break;
+        const double step = NT == 1 ? std::max(1., 0.12 + 0.59 * static_cast<double>(per_sm)) : std::max(0.8, 0.5 * static_cast<double>(per_sm));
+        const double start = NT == 2 ? static_cast<double>(ctas) / 85. : per_sm > 2 ? 3. : static_cast<double>(ctas) / 170.;
+        const double cost = (s > 1 ? 1. : 0.) + static_cast<double>(steps - 1) * step + start;
+        if (s == 1 || cost < least) { split = s; least = cost; }
+    }
     // Few items with long lists leave SMs with one CTA each, which 8 warps use better (8 items x 256 tiles 7.1 us, 8.0 with 4
     // warps; x 1024 15.6, 20.8); a shorter list or more items pay for the larger merge (8 x 128 tiles gain 3 %, 16 x 256
     // lose 2 to 8 %).
