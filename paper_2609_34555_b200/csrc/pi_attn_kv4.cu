@@ -46,7 +46,9 @@ constexpr int A4_MAX_SPLIT = 8;                    // CTAs of a cluster that sha
 __host__ __device__ constexpr int a4_tiles(int NT) { return NT == 1 ? 2 : 1; }
 __host__ __device__ constexpr int a4_steps(int NT) { return NT == 1 ? 2 : 4; }      // steps in the ring
 __host__ __device__ constexpr int a4_warps_per_sm(int NT) { return NT == 1 ? 16 : 8; }  // what the registers allow
-constexpr float A4_NO_UNIT = 0x1p120f;             // before a group's first product: every product but 0 leaves fp16
+// Power of two of a head and group before its first product: a weight (at most 2^8) times it stays a number, so that no weight
+// at all stays none, and whatever may be seen in the result (2^-133 and more) is above the smallest fp16 number.
+constexpr int A4_NO_UNIT = 246;                    // the exponent's bits: 2^119
 constexpr float A4_NO_MAX = -3.40282347e38f;       // the lowest number, for -infinity in the running maximum: differences are no NaN
 
 struct Attn4Params {
@@ -133,6 +135,13 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {          // both products in one operation
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
@@ -314,20 +323,20 @@ attn_kv4_kernel(Attn4Params p) {
         scale[nt][1] = s_scale[nt * 8 + 2 * c + 1];
     }
 
-    // ---- running state: o[j][mt] = channels 32 j + 4 r + 2 mt (+ 1 in the upper two) of heads 2 c, 2 c + 1, times unit[j];
+    // ---- running state: o[j][mt] = channels 32 j + 4 r + 2 mt (+ 1 in the upper two) of heads 2 c, 2 c + 1, times the head's unit[j];
     // z = row r of {scale, minimum} of the four groups, weighted, for the same heads; m (exp2 domain) and l as usual
-    float o[NT][4][2][4], z[NT][4], m[NT][2], l[NT][2], unit[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) unit[j] = A4_NO_UNIT;
+    float o[NT][4][2][4], z[NT][4], m[NT][2], l[NT][2], unit[NT][4][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         m[nt][0] = m[nt][1] = A4_NO_MAX;
         l[nt][0] = l[nt][1] = 0.f;
         z[nt][0] = z[nt][1] = z[nt][2] = z[nt][3] = 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 4; ++j) {
+            unit[nt][j][0] = unit[nt][j][1] = __uint_as_float(static_cast<uint32_t>(A4_NO_UNIT) << 23);
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[nt][j][0][e] = o[nt][j][1][e] = 0.f;
+        }
     }
     // Row r of a tile's products is token pr (row r + 8: pr + 8): then the four tokens that a lane needs of V, rows 2 c,
     // 2 c + 1, 2 c + 8, 2 c + 9, are c, c + 4, c + 8, c + 12, and the lanes of one load read neighbouring rows.
@@ -336,6 +345,7 @@ attn_kv4_kernel(Attn4Params p) {
 
     const uint32_t raise = p.raise, raise64 = p.raise64;
     uint32_t tile = ring;                                // first stage of the step at hand
+    bool begun = false;                                  // a step has been added up
     for (int n = 0; n < n_mine; n += TP, tile = tile == ring + (STAGES - TP) * KV4_TILE_BYTES ? ring : tile + TP * KV4_TILE_BYTES) {
         const int i = n & 31;
         if (i == 0) {
@@ -427,22 +437,30 @@ attn_kv4_kernel(Attn4Params p) {
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                    const float m_new = fmaxf(m[nt][e], mx), alpha = ex2(m[nt][e] - m_new);
-                    m[nt][e] = m_new;
-                    l[nt][e] *= alpha;
-                    z[nt][e] *= alpha;
+                    const float m_new = fmaxf(m[nt][e], mx), fall = m[nt][e] - m_new, alpha = ex2(fall);
 #pragma unroll
                     for (int k = 0; k < TP; ++k) {
                         w[k][nt][e] = s[k][nt][e] - m_new;
                         w[k][nt][2 + e] = s[k][nt][2 + e] - m_new;
                     }
+                    m[nt][e] = m_new;
+                    if (!begun) continue;                // the warp's first step: nothing has been summed yet
+                    l[nt][e] *= alpha;
+                    z[nt][e] *= alpha;
+                    // What the head has seen so far counts for 2^fall less from here on, and its units rise by the whole part of
+                    // that: tokens that have lost their weight take no bits from those that have it.
+                    const int rise = static_cast<int>(fminf(-fall, 255.f));
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        o[nt][j][0][e] *= alpha; o[nt][j][0][2 + e] *= alpha;
-                        o[nt][j][1][e] *= alpha; o[nt][j][1][2 + e] *= alpha;
+                        const int have = static_cast<int>(__float_as_uint(unit[nt][j][e]) >> 23), now = min(have + rise, A4_NO_UNIT);
+                        const float f = ex2(fall + static_cast<float>(now - have));
+                        unit[nt][j][e] = __uint_as_float(static_cast<uint32_t>(now) << 23);
+                        o[nt][j][0][e] *= f; o[nt][j][0][2 + e] *= f;
+                        o[nt][j][1][e] *= f; o[nt][j][1][2 + e] *= f;
                     }
                 }
         }
+        begun = true;
         // ---- the weights; with them the minima's share of the result, for all four groups in one product.  Minima and
         // scales are bf16, so the weights take part as a bf16 head (the upper half of the number) and a bf16 remainder.
 #pragma unroll
@@ -466,8 +484,10 @@ attn_kv4_kernel(Attn4Params p) {
             }
         }
         // ---- weight times scale, one set per group, in fp16: 11 bits, where bf16 would need two numbers.  Its narrow range is
-        // covered by a power of two per group (`unit`), set by the first step so that the largest product is about 2^8 and
-        // moved when a later one leaves the range.
+        // covered by a power of two per head and group (`unit`), set by the first step so that the largest product is about 2^8,
+        // lowered when a later one leaves the range and raised when the head's maximum moves.  A product that is 2^-22 of the
+        // largest of its head and group, and more, keeps its 11 bits; what a smaller one is off by is 2^-33 of the largest.
+        // Per head: weights that are everything for one are nothing for its neighbour, and columns without a head have weights too.
         uint32_t pw[TP][NT][4][2];
         auto products = [&]() {
             uint32_t top = 0u;
@@ -477,46 +497,63 @@ attn_kv4_kernel(Attn4Params p) {
                 const uint4 va = lds128(at + pr * 16), vb = lds128(at + (pr + 8) * 16);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float sa = kv4_scale_of(word_of(va, j)) * unit[j], sb = kv4_scale_of(word_of(vb, j)) * unit[j];
+                    const float sa = kv4_scale_of(word_of(va, j)), sb = kv4_scale_of(word_of(vb, j));
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        pw[k][nt][j][0] = pack_f16(w[k][nt][0] * sa, w[k][nt][1] * sa);
-                        pw[k][nt][j][1] = pack_f16(w[k][nt][2] * sb, w[k][nt][3] * sb);
+                        // (the weight first: scale times unit may leave 32 bits, and then no weight would be no number)
+                        const float2 u = make_float2(unit[nt][j][0], unit[nt][j][1]);
+                        const float2 pa = mul2(mul2(make_float2(w[k][nt][0], w[k][nt][1]), u), make_float2(sa, sa));
+                        const float2 pb = mul2(mul2(make_float2(w[k][nt][2], w[k][nt][3]), u), make_float2(sb, sb));
+                        pw[k][nt][j][0] = pack_f16(pa.x, pa.y);
+                        pw[k][nt][j][1] = pack_f16(pb.x, pb.y);
                         top = max_f16x2(top, max_f16x2(pw[k][nt][j][0], pw[k][nt][j][1]));
                     }
                 }
             }
             return top;
         };
-        {
+        // (a loop of two rounds at most, so that the products' code is there once)
+#pragma unroll 1
+        for (bool again = false;; again = true) {
             const uint32_t top = products();
             const __half2 t = *reinterpret_cast<const __half2*>(&top);
-            if (__any_sync(0xffffffffu, __hgt(__hmax(__low2half(t), __high2half(t)), __ushort_as_half(0x7800)))) {      // 2^15
+            if (again || !__any_sync(0xffffffffu, __hgt(__hmax(__low2half(t), __high2half(t)), __ushort_as_half(0x7800)))) break;      // 2^15
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    // the largest product of the group in the step (2^-20 of it: the product itself may leave fp32)
-                    float mx = 0.f;
+            for (int j = 0; j < 4; ++j) {
+                float sc[TP][2];                    // scales, 2^-20 of them: a product may leave fp32
 #pragma unroll
-                    for (int k = 0; k < TP; ++k) {
-                        const uint32_t at = tile + k * KV4_TILE_BYTES + KV4_V_SCALES + j * 4;
-                        const float sa = kv4_scale_of(lds32(at + pr * 16)) * 0x1p-20f, sb = kv4_scale_of(lds32(at + (pr + 8) * 16)) * 0x1p-20f;
+                for (int k = 0; k < TP; ++k) {
+                    const uint32_t at = tile + k * KV4_TILE_BYTES + KV4_V_SCALES + j * 4;
+                    sc[k][0] = kv4_scale_of(lds32(at + pr * 16)) * 0x1p-20f;
+                    sc[k][1] = kv4_scale_of(lds32(at + (pr + 8) * 16)) * 0x1p-20f;
+                }
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-                            mx = fmaxf(mx, fmaxf(fmaxf(w[k][nt][0], w[k][nt][1]) * sa, fmaxf(w[k][nt][2], w[k][nt][3]) * sb));
+                for (int nt = 0; nt < NT; ++nt) {
+                    // the two heads' largest products of the group in the step, cut to bf16: the exponent is all that counts.  (One
+                    // that leaves fp16 is above 2^-104, since a unit is at most 2^119, so 2^-20 of it is a normal number.)
+                    float mx[2] = {0.f, 0.f};
+#pragma unroll
+                    for (int k = 0; k < TP; ++k)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) mx[e] = max3(mx[e], w[k][nt][e] * sc[k][0], w[k][nt][2 + e] * sc[k][1]);
+                    uint32_t pair = __byte_perm(__float_as_uint(mx[0]), __float_as_uint(mx[1]), 0x7632);
+#pragma unroll
+                    for (int d = 4; d <= 16; d <<= 1) {
+                        const uint32_t other = __shfl_xor_sync(0xffffffffu, pair, d);
+                        const __nv_bfloat162 v = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&pair), *reinterpret_cast<const __nv_bfloat162*>(&other));
+                        pair = *reinterpret_cast<const uint32_t*>(&v);
                     }
-                    // exponents: of 2^8 / (2^20 mx), from which the product of the largest weight and scale is 2^8 and more
-                    const int top_exp = min(static_cast<int>(__reduce_max_sync(0xffffffffu, __float_as_uint(mx)) >> 23), 239);
-                    const int want = 242 - top_exp, have = static_cast<int>(__float_as_uint(unit[j]) >> 23);
-                    if (top_exp > 0 && want < have) {
-                        const float f = have - want < 127 ? __uint_as_float(static_cast<uint32_t>(127 + want - have) << 23) : 0.f;
-                        unit[j] = __uint_as_float(static_cast<uint32_t>(want) << 23);
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) { o[nt][j][0][e] *= f; o[nt][j][1][e] *= f; }
+                    for (int e = 0; e < 2; ++e) {
+                        // exponents: of 2^8 / (2^20 mx), from which the product of the largest weight and scale is 2^8 and more
+                        const int top_exp = min(static_cast<int>(e ? pair >> 23 : (pair >> 7) & 0xffu), 239);
+                        const int have = static_cast<int>(__float_as_uint(unit[nt][j][e]) >> 23), now = top_exp > 0 ? min(242 - top_exp, have) : have;
+                        const float f = __uint_as_float(static_cast<uint32_t>(max(127 + now - have, 0)) << 23);     // (2^-127 and less: 0)
+                        unit[nt][j][e] = __uint_as_float(static_cast<uint32_t>(now) << 23);
+                        o[nt][j][0][e] *= f; o[nt][j][0][2 + e] *= f;
+                        o[nt][j][1][e] *= f; o[nt][j][1][2 + e] *= f;
                     }
                 }
-                products();
             }
         }
         // ---- O^T += V^T (weight scale), group by group
@@ -558,7 +595,7 @@ attn_kv4_kernel(Attn4Params p) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 // the minima's share is in the lanes that hold row 2 j + 1
-                const float f = inverse_power(unit[j]), zj = __shfl_sync(0xffffffffu, z[nt][e], 8 * j + 4 + c);
+                const float f = inverse_power(unit[nt][j][e]), zj = __shfl_sync(0xffffffffu, z[nt][e], 8 * j + 4 + c);
                 const float4 v = make_float4(fmaf(o[nt][j][0][e], f, zj), fmaf(o[nt][j][0][2 + e], f, zj), fmaf(o[nt][j][1][e], f, zj), fmaf(o[nt][j][1][2 + e], f, zj));
                 if (g < p.G) *reinterpret_cast<float4*>(s_o + (warp * p.G + g) * PI_HEAD_DIM + 32 * j + 4 * r) = v;
             }

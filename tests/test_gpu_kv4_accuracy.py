@@ -1,0 +1,91 @@
+"""Attention over 4-bit blocks where its arithmetic is hardest put to it: tokens without any weight beside values of any size."""
+import numpy as np
+import pytest
+import torch
+
+from tests import kv4_reference as ref
+from tests.test_gpu_kv4 import bf, clean, context, dev, i32
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+
+
+def two_classes(pi, heavy, q_sign, v_heavy, v_light, key):
+    """One sequence of len(heavy) tokens.  Keys are constant rows (stored exactly): +key for the heavy tokens, -key for the light
+    ones; queries are q_sign * key.  Returns out and lse of the kernel, the 64-bit result, and per (head, channel) the sums of
+    weight * largest |value| of the channel's group over the tokens of the head's own class and over the others."""
+    c = pi.cfg
+    B, H, K, C, n = c.block_tokens, c.n_kv_heads, c.budget_blocks, c.pool_slots, len(heavy)
+    nb = -(-n // B)
+    kv = np.zeros((C, H, 2, B, 128), dtype=np.float32)
+    slots = np.random.default_rng(n).permutation(C)[:nb]
+    for t in range(n):
+        kv[slots[t // B], :, 0, t % B] = key if heavy[t] else -key
+        kv[slots[t // B], :, 1, t % B] = v_heavy[t] if heavy[t] else v_light[t]
+    pool = ref.pack(ref.bf16(kv), B)
+    held = ref.unpack(pool, H, B)
+    q = np.repeat(np.asarray(q_sign, dtype=np.float32)[:, None] * np.float32(key), 128, 1)
+    assert np.array_equal(q, ref.bf16(q)) and q.shape[0] == c.n_q_heads
+    blocks = np.full((1, K), -1, dtype=np.int32)
+    where = np.full((1, K), -1, dtype=np.int32)
+    blocks[0, :nb], where[0, :nb] = np.arange(nb), slots
+    out, lse = torch.zeros((1, c.n_q_heads, 128), dtype=torch.bfloat16, device=DEV), torch.zeros((1, c.n_q_heads), device=DEV)
+    pi.sparse_decode_attn_kv4(0, bf(q[None]), dev(pool[None]), dev(where), dev(blocks), i32([nb]), i32([n]), out, lse)
+    clean(pi)
+    want, own, other = [np.zeros((c.n_q_heads, 128)) for _ in range(3)]
+    want_lse = np.zeros(c.n_q_heads)
+    heavy = np.asarray(heavy)
+    for g in range(c.n_q_heads):
+        h = g // (c.n_q_heads // H)
+        k, v = [np.concatenate([held[s, h, i] for s in slots])[:n] for i in (0, 1)]
+        z = k @ q[g].astype(np.float64) / np.sqrt(128)
+        p = np.exp(z - z.max())
+        want_lse[g] = z.max() + np.log(p.sum())
+        p /= p.sum()
+        want[g] = p @ v
+        size = np.repeat(np.abs(v).reshape(n, 4, 32).max(2), 32, 1)
+        mine = heavy if q_sign[g] > 0 else ~heavy
+        own[g], other[g] = p[mine] @ size[mine], p[~mine] @ size[~mine]
+    return out[0].double().cpu().numpy(), lse[0].double().cpu().numpy(), want, want_lse, own, other
+
+
+PLACES = {
+    "side by side": [True, False],                                             # one step
+    "light ones behind": [True] * 2200 + [False] * 2200,                       # several steps of every warp each
+    "light ones first": [False] * 2200 + [True] * 2200,
+    "in turn": [True, False, False] * 1400,
+}
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(4, 1), (8, 1), (16, 2), (16, 1)])
+@pytest.mark.parametrize("place", PLACES)
+@pytest.mark.parametrize("heads", ["alike", "both ways"])
+def test_attention_with_tokens_of_no_weight_and_values_of_any_size(Hq, Hkv, place, heads):
+    """What the light tokens hold must not be seen in the heavy ones' result: keys of 3 put their scores 204 below (weights
+    of 2^-294, which are 0 in 32 bits), keys of 1.875 80 below (2^-115).  The other way round for the heads whose query is turned."""
+    pi = context(n_q_heads=Hq, n_kv_heads=Hkv, budget_blocks=300, pool_slots=300, max_batch=1, max_blocks=300, n_sink_blocks=0, n_local_blocks=1)
+    heavy, n = PLACES[place], len(PLACES[place])
+    rng = np.random.default_rng(n)
+    sign = np.ones(Hq) if heads == "alike" else np.where(np.arange(Hq) % 3 == 1, -1.0, 1.0)
+    for size in (4e3, 2.0 ** 24, 1e12, 1e30):
+        light = np.where(np.arange(128) % 2 == 0, 0.0, size)[None].repeat(n, 0)
+        for key in (3.0, 1.875):
+            for values in ("none", "constant", "any"):
+                v = {"none": np.zeros((n, 128)), "constant": np.full((n, 128), 2.5), "any": rng.standard_normal((n, 128))}[values]
+                out, lse, want, want_lse, own, other = two_classes(pi, heavy, sign, v, light, key)
+                # one rounding to bf16.  Tokens of one class have the same score to the bit, so only weight times scale is
+                # rounded for them: by at most 2^-11, at most 15 codes of it, and 15 scales are at most twice the
+                # largest |v| of the group.  The weights of the other class carry the scores' error as well: a constant
+                # row has one product, of the minimum and the query's sum, and no more than 32 roundings of 2^-23
+                score = 128 * key * key / np.sqrt(128)
+                eps = 2 * 32 * 2.0 ** -23 * score
+                tol = 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * own + (2.0 ** -10 + 2 * eps) * other + 1e-30
+                assert (np.abs(out - want) <= tol).all(), (size, key, values, np.abs(out - want).max(), int(np.isnan(out).sum()))
+                assert (np.abs(lse - want_lse) <= eps + 2.0 ** -18).all()
+    pi.close()
