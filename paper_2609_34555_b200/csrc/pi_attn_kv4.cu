@@ -11,8 +11,8 @@
 //     again one product, of the weights and the minima.
 // The contractions run on mma.sync (tokens or channels on M, up to 8 query heads on N): with G <= 16 query heads per
 // KV head a 128-row tcgen05 tile would be nearly empty, and the codes have to pass through registers anyway.
-// Codes are exact in fp16, queries after a power of two per head; weights times scales are rounded to 11 bits, each an
-// eighth of the output's own rounding and of random sign; all sums are in 32 bits.
+// Codes are exact in fp16, queries after a power of two per head; weights times scales are rounded to 11 bits, which in the mean
+// square adds an eighth of the output's own rounding (2 % to its square); all sums are in 32 bits.
 //
 // One (sequence, KV head) per cluster of S CTAs of 4 or 8 warps (S = 1, 2, 4 or 8; both by the launcher's rule).  The item's
 // 16-token tiles are dealt out to its warps in turn; a warp streams its own tiles through its own ring of shared-memory
@@ -87,12 +87,15 @@ __device__ __forceinline__ uint32_t masked(uint32_t v, uint32_t mask, uint32_t r
     asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(v), "r"(mask), "r"(raise));
     return d;
 }
-// The four pairs of a word, nibbles n (low half) and n + 4 (high half), as fp16 numbers.  0x6400 | nibble is 1024 + nibble
-// and 0x6400 | 16 nibble is 1024 + 16 nibble, so two of the four need no shift; bringing them back to 0..15 is exact.
+// The four pairs of a word, nibbles n (low half) and n + 4 (high half), as fp16 numbers, less 8: -8 .. 7.  0x6400 | nibble is
+// 1024 + nibble and 0x6400 | 16 nibble is 1024 + 16 nibble, so two of the four need no shift; bringing them back is exact.
+// (Bits placed below a large number's exponent, and the number taken off: Kim, Henry, Fahim and Hassan Awadalla, Who Says
+// Elephants Can't Run, 2022.)  Counted from the middle, since what a weight's rounding is worth is multiplied by the code: from 0 on, with
+// a mean of 7.5 that the minima have to cancel, it doubles the error (tests/test_kv4_accuracy_cpu.py).
 __device__ __forceinline__ void code_pairs(uint32_t w, uint32_t raise, uint32_t (&p)[4]) {
-    const __half2 low = __halves2half2(__ushort_as_half(0xe400), __ushort_as_half(0xe400));        // -1024
+    const __half2 low = __halves2half2(__ushort_as_half(0xe408), __ushort_as_half(0xe408));        // -1032
     const __half2 sixteenth = __halves2half2(__ushort_as_half(0x2c00), __ushort_as_half(0x2c00));  // 1 / 16
-    const __half2 high = __halves2half2(__ushort_as_half(0xd400), __ushort_as_half(0xd400));       // -64
+    const __half2 high = __halves2half2(__ushort_as_half(0xd480), __ushort_as_half(0xd480));       // -72
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const uint32_t v = i ? w >> 8 : w, a = masked(v, 0x000f000fu, raise), b = masked(v, 0x00f000f0u, raise);
@@ -101,8 +104,9 @@ __device__ __forceinline__ void code_pairs(uint32_t w, uint32_t raise, uint32_t 
         p[2 * i + 1] = *reinterpret_cast<const uint32_t*>(&y);
     }
 }
-// The same, but with the second pair as 64 + code (0x5400 | 16 nibble): half the operations.  For K, where the offset's part
-// of the products is taken off with the minima's.
+// For K: from 0 on, and the second pair as 64 + code (0x5400 | 16 nibble), which is half the operations (2 % of the call's time).
+// The offset's part of the products is taken off with the minima's; in 32 bits that leaves a score of ordinary keys off by
+// 9e-7 instead of 1e-7, and scores of some hundred by 3.5e-5: 2^-6 of the output's own rounding.
 __device__ __forceinline__ void code_pairs_k(uint32_t w, uint32_t raise, uint32_t raise64, uint32_t (&p)[4]) {
     const __half2 low = __halves2half2(__ushort_as_half(0xe400), __ushort_as_half(0xe400));        // -1024
 #pragma unroll
@@ -594,8 +598,8 @@ attn_kv4_kernel(Attn4Params p) {
             const int g = nt * 8 + 2 * c + e;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                // the minima's share is in the lanes that hold row 2 j + 1
-                const float f = inverse_power(unit[nt][j][e]), zj = __shfl_sync(0xffffffffu, z[nt][e], 8 * j + 4 + c);
+                // the minima's share is in the lanes that hold row 2 j + 1, the scales', of which the codes lack 8, in those of row 2 j
+                const float f = inverse_power(unit[nt][j][e]), zj = fmaf(8.f, __shfl_sync(0xffffffffu, z[nt][e], 8 * j + c), __shfl_sync(0xffffffffu, z[nt][e], 8 * j + 4 + c));
                 const float4 v = make_float4(fmaf(o[nt][j][0][e], f, zj), fmaf(o[nt][j][0][2 + e], f, zj), fmaf(o[nt][j][1][e], f, zj), fmaf(o[nt][j][1][2 + e], f, zj));
                 if (g < p.G) *reinterpret_cast<float4*>(s_o + (warp * p.G + g) * PI_HEAD_DIM + 32 * j + 4 * r) = v;
             }

@@ -3,8 +3,9 @@ import numpy as np
 import pytest
 import torch
 
+from tests import kv4_accuracy as acc
 from tests import kv4_reference as ref
-from tests.test_gpu_kv4 import bf, clean, context, dev, i32
+from tests.test_gpu_kv4 import attention_case, bf, clean, context, dev, i32, run_attention
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -88,4 +89,30 @@ def test_attention_with_tokens_of_no_weight_and_values_of_any_size(Hq, Hkv, plac
                 tol = 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * own + (2.0 ** -10 + 2 * eps) * other + 1e-30
                 assert (np.abs(out - want) <= tol).all(), (size, key, values, np.abs(out - want).max(), int(np.isnan(out).sum()))
                 assert (np.abs(lse - want_lse) <= eps + 2.0 ** -18).all()
+    pi.close()
+
+
+@pytest.mark.parametrize("Hq,Hkv,B,K,n", [(32, 8, 16, 64, 8), (64, 8, 32, 16, 4), (128, 8, 16, 40, 2), (8, 2, 64, 20, 32), (4, 1, 16, 300, 64)])
+def test_attention_is_as_near_as_its_bits_allow(Hq, Hkv, B, K, n):
+    """Ordinary keys and values; the outputs' error in the mean square, and the logarithms of the sums."""
+    pi = context(n_q_heads=Hq, n_kv_heads=Hkv, block_tokens=B, budget_blocks=K, pool_slots=K + 3, max_batch=n, max_blocks=2 * K, n_sink_blocks=0, n_local_blocks=1)
+    rng = np.random.default_rng(Hq * 1000 + K)
+    case = attention_case(pi, rng.integers(K * B // 2, 2 * K * B + 1, n), Hq + K, garbage=False)
+    kv = ref.bf16(rng.standard_normal((n * (K + 3), Hkv, 2, B, 128)))                # (means of 0: the outputs' last rounding hides least)
+    case["pool"] = ref.pack(kv, B).reshape(case["pool"].shape)
+    out, lse = run_attention(pi, case)
+    out, lse = out.double().cpu().numpy().reshape(n, Hkv, Hq // Hkv, 128), lse.double().cpu().numpy().reshape(n, Hkv, Hq // Hkv)
+    want, before = np.empty_like(out), np.empty_like(out)
+    for s in range(n):
+        codes, scales, lows = acc.tokens(case["pool"][s], case["slots"][s], case["blocks"][s], int(case["count"][s]), int(case["ctx"][s]), Hkv, B)
+        for h in range(Hkv):
+            q = case["q"][s].astype(np.float64).reshape(Hkv, Hq // Hkv, 128)[h]
+            p, want_lse = acc.softmax(q, codes[h, 0], scales[h, 0], lows[h, 0])
+            want[s, h], before[s, h] = acc.allowed(p, codes[h, 1], scales[h, 1], lows[h, 1])
+            # A score is the sum of four groups, each of two products that are added up in 32 bits and may be cut: by 2^-23 of
+            # a sum below 128 * 4 (every second code carries 64, queries are below 2, of either sign), times a scale of
+            # about 0.3, the queries' power of two (at most 4) and 1 / sqrt(D): 2 * 2 * 2^-23 * 512 * 0.3 * 0.35 = 2^-15.3 where
+            # all eight cuts of all tokens went the same way and were as large as they can be
+            assert (np.abs(lse[s, h] - want_lse) <= 2.0 ** -15).all()
+    acc.check(out, want, before)
     pi.close()
