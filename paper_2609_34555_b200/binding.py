@@ -220,6 +220,17 @@ class PulseInfer:
         except Exception:
             pass
 
+    def _bf16_blocks(self, t, name: str, n: int, blocks: int, stride: Optional[int] = None, instead: str = "", unit: Optional[int] = None):
+        """Refuses 4-bit blocks where blocks of bf16 are addressed, which would lead out of the tensor: n runs of `blocks` of them, `stride`
+        bytes apart (None: one behind the other).  A byte view of bf16 blocks is as large as they are, and passes; one of units other
+        than blocks may have rows of any length."""
+        if t.dtype != torch.uint8 or n < 1:
+            return
+        size = blocks * self.block_bytes
+        span = size + (n - 1) * (size if stride is None else stride)
+        if (unit in (None, 0, self.block_bytes) and t.dim() > 1 and t.shape[-1] == self.kv4_block_bytes) or (t.is_contiguous() and t.numel() < span):
+            raise TypeError(f"{name}: expected blocks of bf16, {span} bytes or more" + (f" (4-bit blocks: {instead})" if instead else ""))
+
     # ------------------------------------------------------------------ the four path calls
     def score_select(self, layer: int, q, digest, ctx_len, sel_blocks, sel_count, scores=None, stream=None) -> None:
         batch = q.shape[0]
@@ -261,6 +272,7 @@ class PulseInfer:
     def build_digests_all(self, kv, ctx_len, digest_all, kv_seq_stride: Optional[int] = None, stream=None) -> None:
         batch = ctx_len.shape[0]
         stride = kv_seq_stride if kv_seq_stride is not None else kv.stride(0) * kv.element_size()
+        self._bf16_blocks(kv, "kv", batch, self.cfg.max_blocks, stride)
         _check("pi_build_digests_all", self._lib.pi_build_digests_all(
             self._ctx, batch, kv.data_ptr(), stride, _dev(ctx_len, torch.int32, "ctx_len"),
             _dev(digest_all, torch.bfloat16, "digest_all"), _stream(stream)))
@@ -295,9 +307,17 @@ class PulseInfer:
         recall_list: int32 [n_lists][capacity][4].  With page_table (int32 CUDA tensor [batch][NB]) the
         host tensor is an arena of pages and block b of sequence s is page page_table[s][b]."""
         n_lists, cap = recall_list.shape[0], recall_list.shape[1]
+        n_seq = -(-n_lists // max(1, lists_per_seq))
+        ps = pool_seq_stride if pool_seq_stride is not None else pool.stride(0) * pool.element_size()
+        self._bf16_blocks(pool, "pool", n_seq, self.cfg.pool_slots, ps, "recall_kv4", unit_bytes)
+        hs = host_seq_stride if host_seq_stride is not None else host_kv.stride(0) * host_kv.element_size()
+        if page_table is None:
+            self._bf16_blocks(host_kv, "host_kv", n_seq, self.cfg.max_blocks, hs, "recall_kv4", unit_bytes)
+        else:
+            whole = unit_bytes in (None, 0, self.block_bytes) and unit_stride in (0, self.block_bytes)
+            self._bf16_blocks(host_kv, "host_kv", 1, (n_pages or 0) if whole else 0, None, "recall_kv4", unit_bytes)
         if not host_kv.is_cuda and not host_kv.is_pinned():
             raise PiError("pi_recall_gather_scatter", -5, strerror(-5))
-        ps = pool_seq_stride if pool_seq_stride is not None else pool.stride(0) * pool.element_size()
         if page_table is not None:
             ub = unit_bytes or self.block_bytes
             pages = n_pages if n_pages is not None else host_kv.numel() * host_kv.element_size() // (unit_stride or ub)
@@ -306,7 +326,6 @@ class PulseInfer:
                 page_table.stride(0), pages, pool.data_ptr(), ps, _dev(recall_list, EXTENT_DTYPE, "recall_list"), cap,
                 _dev(recall_count, torch.int32, "recall_count"), ub, unit_stride, list_offset, _stream(stream)))
             return
-        hs = host_seq_stride if host_seq_stride is not None else host_kv.stride(0) * host_kv.element_size()
         _check("pi_recall_gather_scatter", self._lib.pi_recall_gather_scatter(
             self._ctx, layer, n_lists, lists_per_seq, host_kv.data_ptr(), hs, pool.data_ptr(), ps,
             _dev(recall_list, EXTENT_DTYPE, "recall_list"), cap, _dev(recall_count, torch.int32, "recall_count"),
@@ -317,8 +336,9 @@ class PulseInfer:
         """headwise=True: sel_slots / sel_blocks are [batch][Hkv][K] (or [batch*Hkv][K]) and sel_count
         [batch][Hkv]: every KV head attends over its own selection."""
         batch = q.shape[0]
-        if not pool.is_cuda or not pool.is_contiguous() or pool.dtype == torch.uint8:
-            raise TypeError("pool: expected a contiguous CUDA tensor of bf16 blocks (4-bit blocks: sparse_decode_attn_kv4)")
+        self._bf16_blocks(pool, "pool", batch, self.cfg.pool_slots, None, "sparse_decode_attn_kv4")
+        if not pool.is_cuda or not pool.is_contiguous():
+            raise TypeError("pool: expected a contiguous CUDA tensor")
         fn = self._lib.pi_sparse_decode_attn_headwise if headwise else self._lib.pi_sparse_decode_attn
         _check("pi_sparse_decode_attn_headwise" if headwise else "pi_sparse_decode_attn", fn(
             self._ctx, layer, batch, _dev(q, torch.bfloat16, "q"), pool.data_ptr(),
@@ -339,8 +359,9 @@ class PulseInfer:
         """First half of the attention split around the recall: the selected blocks the step's recall list
         does not touch; may run beside recall_gather_scatter.  Leaves its softmax state in `state`."""
         batch = q.shape[0]
-        if not pool.is_cuda or not pool.is_contiguous() or pool.dtype == torch.uint8:
-            raise TypeError("pool: expected a contiguous CUDA tensor of bf16 blocks (4-bit blocks: sparse_decode_attn_kv4)")
+        self._bf16_blocks(pool, "pool", batch, self.cfg.pool_slots, None, "sparse_decode_attn_kv4")
+        if not pool.is_cuda or not pool.is_contiguous():
+            raise TypeError("pool: expected a contiguous CUDA tensor")
         _check("pi_sparse_decode_attn_resident", self._lib.pi_sparse_decode_attn_resident(
             self._ctx, layer, batch, _dev(q, torch.bfloat16, "q"), pool.data_ptr(),
             _dev(sel_slots, torch.int32, "sel_slots"), _dev(sel_blocks, torch.int32, "sel_blocks"),
@@ -353,8 +374,9 @@ class PulseInfer:
         """Second half: the blocks the recall brought in, merged with `state`; writes `out`.  The caller
         orders it after the first half and after the recall."""
         batch = q.shape[0]
-        if not pool.is_cuda or not pool.is_contiguous() or pool.dtype == torch.uint8:
-            raise TypeError("pool: expected a contiguous CUDA tensor of bf16 blocks (4-bit blocks: sparse_decode_attn_kv4)")
+        self._bf16_blocks(pool, "pool", batch, self.cfg.pool_slots, None, "sparse_decode_attn_kv4")
+        if not pool.is_cuda or not pool.is_contiguous():
+            raise TypeError("pool: expected a contiguous CUDA tensor")
         _check("pi_sparse_decode_attn_recalled", self._lib.pi_sparse_decode_attn_recalled(
             self._ctx, layer, batch, _dev(q, torch.bfloat16, "q"), pool.data_ptr(),
             _dev(sel_slots, torch.int32, "sel_slots"), _dev(sel_blocks, torch.int32, "sel_blocks"),
@@ -370,6 +392,12 @@ class PulseInfer:
         sequence: pool slot, host store, running digest; ctx_len is the length before the append.
         With page_table the host tensor is an arena of block-sized pages (see recall_gather_scatter)."""
         batch = ctx_len.shape[0]
+        self._bf16_blocks(pool, "pool", batch, self.cfg.pool_slots, None, "append_kv4")
+        if page_table is None:
+            hs = host_seq_stride if host_seq_stride is not None else host_kv.stride(0) * host_kv.element_size()
+            self._bf16_blocks(host_kv, "host_kv", batch, self.cfg.max_blocks, hs, "append_kv4")
+        else:
+            self._bf16_blocks(host_kv, "host_kv", 1, n_pages or 0, None, "append_kv4")
         if not host_kv.is_cuda and not host_kv.is_pinned():
             raise PiError("pi_append_kv", -5, strerror(-5))
         if isinstance(step, torch.Tensor):               # the step number lives on the device (graph replay)
@@ -465,6 +493,7 @@ class PulseInfer:
     def build_digests(self, layer: int, kv, ctx_len, digest, kv_seq_stride: Optional[int] = None, stream=None) -> None:
         batch = ctx_len.shape[0]
         stride = kv_seq_stride if kv_seq_stride is not None else kv.stride(0) * kv.element_size()
+        self._bf16_blocks(kv, "kv", batch, self.cfg.max_blocks, stride)
         _check("pi_build_digests", self._lib.pi_build_digests(
             self._ctx, layer, batch, kv.data_ptr(), stride, _dev(ctx_len, torch.int32, "ctx_len"),
             _dev(digest, torch.bfloat16, "digest"), _stream(stream)))

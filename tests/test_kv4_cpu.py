@@ -179,3 +179,67 @@ def test_the_front_end_refuses_what_is_not_on_the_gpu():
     with pytest.raises(ValueError):
         pi._front.kv4_load(pi._ctx, blocks, bf, None, 0)        # not a shape
     pi._ctx = ctypes.c_void_p()
+
+
+def a_front_end(**kw):
+    """A PulseInfer whose context is a zeroed buffer, for calls that must be refused; keep what it returns beside it."""
+    ctx, keep = context(**kw)
+    pi = object.__new__(pkg.PulseInfer)
+    pi._lib, pi._ctx, pi.cfg, pi.device = pkg.load_library(), ctx, keep[1], torch.device("cuda", 0)
+    pi.close = lambda: None                                     # (nothing was created)
+    pi.kv4_block_bytes = int(pi._lib.pi_kv4_block_bytes(ctx))
+    pi.block_bytes = pi.cfg.n_kv_heads * pi.cfg.block_tokens * 512
+    return pi, keep
+
+
+@pytest.mark.parametrize("heads,block", [(1, 16), (2, 16), (8, 32)])
+def test_calls_on_bf16_blocks_refuse_4_bit_blocks(heads, block):
+    """They address blocks 2 to 3.2 times as large, and would write or read behind the tensor.  Told by the last axis or by the size;
+    byte views of whole bf16 stores are taken, and fail here only for not being on a GPU or pinned."""
+    pi, keep = a_front_end(n_q_heads=heads, n_kv_heads=heads, block_tokens=block, max_blocks=12, pool_slots=6, budget_blocks=4, n_local_blocks=1, max_batch=2)
+    pool4, host4 = torch.zeros((2, 6, pi.kv4_block_bytes), dtype=torch.uint8), torch.zeros((2, 12, pi.kv4_block_bytes), dtype=torch.uint8)
+    pool, host = torch.zeros((2, 6, pi.block_bytes // 2), dtype=torch.bfloat16), torch.zeros((2, 12, pi.block_bytes // 2), dtype=torch.bfloat16)
+    i32, bf = torch.zeros((2, 4), dtype=torch.int32), torch.zeros((2, heads, 128), dtype=torch.bfloat16)
+    lists, count, table = torch.zeros((2, 4, 4), dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros((2, 12), dtype=torch.int32)
+
+    def attention(p):
+        return [lambda: pi.sparse_decode_attn(0, bf, p, i32, i32, count, count, bf),
+                lambda: pi.sparse_decode_attn_resident(0, bf, p, i32, i32, count, count, lists, count, pool),
+                lambda: pi.sparse_decode_attn_recalled(0, bf, p, i32, i32, count, count, lists, count, pool, bf)]
+
+    def writing(h, p):
+        calls = []
+        for kw in (dict(), dict(page_table=table), dict(page_table=table, n_pages=24)):
+            calls.append(lambda kw=kw: pi.recall_gather_scatter(0, h, p, lists, count, **kw))
+            calls += [lambda kw=kw, step=step: pi.append_kv(0, step, bf, bf, count, h, p, i32, i32, i32, bf, **kw) for step in (1, count[:1])]
+        return calls
+
+    for make in (lambda t: t, lambda t: t.view(2, -1), lambda t: t.view(2, t.shape[1], 2, -1)):
+        small_pool, small_host = make(pool4), make(host4)
+        for call in attention(small_pool) + writing(host, small_pool):
+            with pytest.raises(TypeError, match="pool: expected blocks of bf16"):
+                call()
+        for i, call in enumerate(writing(small_host, pool)):
+            if 3 <= i < 6 and small_host is not host4:
+                continue                                        # (an arena of so many bytes, read as fewer pages: nothing to tell it by)
+            with pytest.raises(TypeError, match="host_kv: expected blocks of bf16"):
+                call()
+        with pytest.raises(TypeError, match="kv: expected blocks of bf16"):
+            pi.build_digests(0, small_host, count, bf)
+        with pytest.raises(TypeError, match="kv: expected blocks of bf16"):
+            pi.build_digests_all(small_host, count, bf)
+    for view in (lambda t: t, lambda t: t.view(torch.uint8), lambda t: t.view(torch.uint8).view(2, -1)):
+        for call in attention(view(pool)):
+            with pytest.raises(TypeError, match="contiguous CUDA tensor"):
+                call()
+        for call in writing(view(host), view(pool)):
+            with pytest.raises(pkg.PiError) as e:
+                call()
+            assert e.value.code == PINNED
+    frag = block * 512                                          # units of one KV head: any rows, of as many bytes
+    if heads == 2:
+        assert frag == pi.kv4_block_bytes
+    with pytest.raises(pkg.PiError):
+        pi.recall_gather_scatter(0, host.view(torch.uint8).view(-1, frag), pool.view(torch.uint8).view(-1, frag), lists.repeat(heads, 1, 1), count.repeat(heads), lists_per_seq=heads,
+                                 unit_bytes=frag, unit_stride=frag, host_seq_stride=12 * pi.block_bytes, pool_seq_stride=6 * pi.block_bytes)
+    pi._ctx = ctypes.c_void_p()
