@@ -14,7 +14,7 @@ from typing import Optional, Sequence
 
 import torch
 
-from .build import FRONT, LIB, build
+from .build import LIB, build, build_front
 
 OK = 0
 ERR_NAMES = {
@@ -116,7 +116,7 @@ def load_front():
     global _front
     if _front is None:
         lib = load_library()
-        spec = importlib.util.spec_from_file_location("_front", FRONT)
+        spec = importlib.util.spec_from_file_location("_front", build_front())
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
         module.connect(*[ctypes.cast(getattr(lib, name), c_void_p).value for name in FRONT_CALLS])
@@ -198,7 +198,6 @@ class PulseInfer:
         self.block_bytes = self.frag_bytes * n_kv_heads
         self.kv4_block_bytes = int(self._lib.pi_kv4_block_bytes(self._ctx))       # bytes of one block in 4 bits
         self.device = torch.device("cuda", torch.cuda.current_device())
-        self._remember_shape()
 
     @classmethod
     def from_workload(cls, cfg, max_batch: Optional[int] = None, **kw) -> "PulseInfer":
@@ -212,7 +211,8 @@ class PulseInfer:
         if getattr(self, "_ctx", None) is not None and self._ctx.value:
             self._lib.pi_destroy(self._ctx)
             self._ctx = c_void_p()
-            self._remember_shape()
+            if "_shape" in self.__dict__:
+                self._remember_shape()
 
     def __del__(self):
         try:
@@ -430,6 +430,12 @@ class PulseInfer:
             _dev(slot_stamp, torch.int32, "slot_stamp"), _dev(digest, torch.bfloat16, "digest"), _stream(stream)))
 
     # ------------------------------------------------------------------ the path on a cache in 4 bits, and what feeds it
+    def __getattr__(self, name):
+        if name not in ("_front", "_shape", "_index"):
+            raise AttributeError(f"{type(self).__name__!r} object has no attribute {name!r}")
+        self._remember_shape()                           # the first of the calls below: until then nothing needs the module
+        return self.__dict__[name]
+
     def _remember_shape(self) -> None:
         """What the calls below check against, in native form."""
         c = self.cfg
