@@ -149,6 +149,11 @@ double number(PyObject* o) {
     if (v == -1.0 && PyErr_Occurred()) throw Raised();
     return v;
 }
+bool truth(PyObject* o) {
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw Raised();
+    return v != 0;
+}
 int layer_of(PyObject* o) {
     const int64_t v = whole(o);
     return v < INT32_MIN || v > INT32_MAX ? -1 : static_cast<int>(v);       // (-1 is refused by the call)
@@ -196,6 +201,8 @@ int assign_pages(const Shape& s, Args a) {
 }
 
 int qk_norm_rope(const Shape& s, Args a) {
+    const float eps = static_cast<float>(number(a[8]));
+    const int interleaved = truth(a[9]) ? 1 : 0;
     const at::Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k");
     const int64_t T = q.dim() ? q.size(0) : 0;
     const auto type = q.scalar_type();
@@ -216,7 +223,7 @@ int qk_norm_rope(const Shape& s, Args a) {
     const int64_t rot = freq ? 2 * freq->numel() : 0;
     return call(g_calls.qk_norm_rope, s.ctx, T, dtype, q.data_ptr(), q_stride, k.data_ptr(), k_stride, ptr<int32_t>(positions),
                                 maybe<float>(s, a[6], at::kFloat, "q_weight", {s.d}), maybe<float>(s, a[7], at::kFloat, "k_weight", {s.d}),
-                                static_cast<float>(number(a[8])), freq ? ptr<float>(*freq) : nullptr, rot > 256 ? 256 : static_cast<int>(rot), PyObject_IsTrue(a[9]) ? 1 : 0,
+                                eps, freq ? ptr<float>(*freq) : nullptr, rot > 256 ? 256 : static_cast<int>(rot), interleaved,
                                 on(s, a[4], at::kBFloat16, "q_out", {T, s.hq, s.d}).data_ptr(), on(s, a[5], at::kBFloat16, "k_out", {T, s.hkv, s.d}).data_ptr(), stream_of(a[10]));
 }
 

@@ -243,3 +243,19 @@ def test_calls_on_bf16_blocks_refuse_4_bit_blocks(heads, block):
         pi.recall_gather_scatter(0, host.view(torch.uint8).view(-1, frag), pool.view(torch.uint8).view(-1, frag), lists.repeat(heads, 1, 1), count.repeat(heads), lists_per_seq=heads,
                                  unit_bytes=frag, unit_stride=frag, host_seq_stride=12 * pi.block_bytes, pool_seq_stride=6 * pi.block_bytes)
     pi._ctx = ctypes.c_void_p()
+
+
+def test_a_flag_without_a_truth_value_is_an_error():
+    """Whatever asking for it raises is raised; it does not count as true."""
+    pi, keep = a_front_end()
+    bf, i32 = torch.zeros((4, 8, 128), dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32)
+
+    class Neither:
+        def __bool__(self):
+            raise ZeroDivisionError("neither")
+
+    with pytest.raises(ZeroDivisionError):
+        pi.qk_norm_rope(torch.zeros((4, 32, 128), dtype=torch.bfloat16), bf, i32, None, bf, bf, interleaved=Neither(), stream=0)
+    with pytest.raises(TypeError, match="CUDA tensor"):
+        pi.qk_norm_rope(torch.zeros((4, 32, 128), dtype=torch.bfloat16), bf, i32, None, bf, bf, interleaved=1, stream=0)
+    pi._ctx = ctypes.c_void_p()
