@@ -51,7 +51,7 @@ append_kernel(AppendParams p) {
     int32_t* table = p.table + static_cast<size_t>(seq) * p.max_blocks;
     int32_t* slot_block = p.slot_block + static_cast<size_t>(seq) * p.C;
     uint32_t* slot_stamp = p.slot_stamp + static_cast<size_t>(seq) * p.C;
-    const long long block_bytes = p.block_bytes;
+    const long long block_bytes = KV4 ? p.block_bytes : static_cast<long long>(p.Hkv) * 2 * p.B * PI_HEAD_DIM * 2;
     int slot = table[b];
     long long host_off = seq * p.host_stride + b * block_bytes;
     if (p.page) {

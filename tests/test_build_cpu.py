@@ -61,3 +61,13 @@ def test_the_module_is_built_anew_for_another_torch_or_python(monkeypatch, no_co
                 build.build_front()
             names.add(build.front_path())
     assert len(names) == 4
+
+
+def test_the_append_kernels_keep_their_state_in_registers(tmp_path):
+    """What the compiler says of both forms, bf16 and 4-bit blocks: nothing is spilled, and the bf16 form stays at 32 registers."""
+    import os
+    import re
+    said = subprocess.run([os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc"), "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-Xptxas=-v", f"-I{build.INCLUDE}",
+                           f"-I{build.CSRC}", "-c", "-o", str(tmp_path / "a.o"), str(build.CSRC / "pi_append.cu")], check=True, capture_output=True, text=True).stderr
+    assert re.findall(r"(\d+) bytes spill stores, (\d+) bytes spill loads", said) == [("0", "0")] * 2
+    assert min(int(n) for n in re.findall(r"Used (\d+) registers", said)) <= 32
