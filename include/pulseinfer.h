@@ -380,6 +380,7 @@ int pi_assign_pages(pi_ctx* ctx, int batch, const int32_t* old_len_dev, const in
 /* RMS norm of every query and key head and the rotation by position, from the projections to the q, k_new and
  * k that the other calls take (bf16), in one pass:
  *   y = x * rsqrt(mean(x^2) + eps) * weight    (both weights NULL: y = x)
+ *     (rows of any size: squares that leave 32 bits are taken of a scaled row)
  *   pair (a, b) of the first rot_dim channels -> (a cos - b sin, b cos + a sin) at positions[t] * inv_freq[pair],
  *   the angle computed in 64 bits;  pairs are (i, i + rot_dim/2), or (2i, 2i + 1) if interleaved.
  *   dtype             PI_DTYPE_* of q_dev and k_dev: [n_tokens][Hq][D] and [n_tokens][Hkv][D], rows of a token

@@ -151,13 +151,28 @@ qk_norm_rope_kernel(RopeParams p) {
             float4 w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[i] = __ldg(g + 2 * (i < 2 ? run_a : run_b) + (i & 1));
-            float ss = 0.f;
+            auto squares = [&]() {
+                float ss = 0.f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) ss = fmaf(x[i], x[i], ss);
-            ss += __shfl_xor_sync(0xffffffffu, ss, 1);
-            ss += __shfl_xor_sync(0xffffffffu, ss, 2);
-            ss += __shfl_xor_sync(0xffffffffu, ss, 4);
-            const float r = rsqrtf(ss * (1.f / PI_HEAD_DIM) + p.eps);
+                for (int i = 0; i < 16; ++i) ss = fmaf(x[i], x[i], ss);
+                ss += __shfl_xor_sync(0xffffffffu, ss, 1);
+                ss += __shfl_xor_sync(0xffffffffu, ss, 2);
+                return ss + __shfl_xor_sync(0xffffffffu, ss, 4);
+            };
+            float ss = squares(), eps = p.eps;
+            if (!std::is_same<T, __half>::value) {
+                // Rows whose squares leave 32 bits (2^60 and more, or 2^-50 and less where eps does not cover them) are taken 2^80 times
+                // smaller or larger, which the quotient does not show.
+                const bool large = ss > 0x1p126f, small = ss < 0x1p-100f && p.eps < 0x1p-70f;
+                if (__any_sync(0xffffffffu, large || small)) {
+                    const float f = large ? 0x1p-80f : small ? 0x1p80f : 1.f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] *= f;
+                    ss = squares();
+                    eps = p.eps * f * f;
+                }
+            }
+            const float r = rsqrtf(ss * (1.f / PI_HEAD_DIM) + eps);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 x[4 * i] *= r * w[i].x; x[4 * i + 1] *= r * w[i].y; x[4 * i + 2] *= r * w[i].z; x[4 * i + 3] *= r * w[i].w;

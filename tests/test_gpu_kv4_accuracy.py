@@ -116,3 +116,32 @@ def test_attention_is_as_near_as_its_bits_allow(Hq, Hkv, B, K, n):
             assert (np.abs(lse[s, h] - want_lse) <= 2.0 ** -15).all()
     acc.check(out, want, before)
     pi.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-6])
+@pytest.mark.parametrize("rot,inter", [(128, False), (64, False), (52, False), (128, True)])
+def test_norm_of_rows_of_any_size(dtype, eps, rot, inter):
+    """From numbers whose squares are lost below 32 bits to those whose squares are beyond, side by side."""
+    pi = context(n_q_heads=10, n_kv_heads=2)
+    sizes = np.asarray([1.0, 1e-38, 1e-30, 1e-22, 1e-15, 1e-3, 1e3, 1e17, 1e19, 1e22, 1e30, 5e37])
+    g = torch.Generator().manual_seed(4)
+    T = 24
+    x = torch.randn((T, 12, 128), generator=g, dtype=torch.float64)
+    for t in range(T):
+        x[t] *= torch.from_numpy(np.roll(sizes, t))[:, None]
+    x = x.to(dtype).to(DEV)
+    q, k = x[:, :10].contiguous(), x[:, 10:].contiguous()
+    pos = np.random.default_rng(0).integers(0, 1 << 17, T).astype(np.int32)
+    freq = (500000.0 ** (-np.arange(0, rot, 2) / rot)).astype(np.float32)
+    w = (1 + 0.3 * np.random.default_rng(9).standard_normal((2, 128))).astype(np.float32)
+    qo, ko = torch.empty_like(q, dtype=torch.bfloat16), torch.empty_like(k, dtype=torch.bfloat16)
+    pi.qk_norm_rope(q, k, i32(pos), dev(freq), qo, ko, q_weight=dev(w[0]), k_weight=dev(w[1]), eps=eps, interleaved=inter)
+    clean(pi)
+    for got, src, weight in ((qo, q, w[0]), (ko, k, w[1])):
+        want = ref.rope(src.double().cpu().numpy(), pos, freq, weight, float(np.float32(eps)), inter)
+        # one rounding to bf16; before it the norm and the turn in 32 bits, under 2^-19 of the row's largest pair
+        tol = 2.0 ** -8 * np.abs(want) + 2.0 ** -19 * np.abs(want).max(-1, keepdims=True) * np.sqrt(2) + 1e-37
+        bad = ~(np.abs(got.double().cpu().numpy() - want) <= tol)
+        assert not bad.any(), np.argwhere(bad.any(-1))[:5]
+    pi.close()
