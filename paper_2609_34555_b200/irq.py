@@ -180,7 +180,7 @@ class CudaOffload:
 
     def __init__(self, sess, q_all, ffn, split_attention: bool = False):
         import torch
-        if split_attention and sess.kv_bits != 16:
+        if split_attention and getattr(sess, "kv_bits", 16) != 16:
             raise ValueError("the attention is split around the recall for bf16 blocks only")
         self.torch, self.sess, self.q_all, self.ffn = torch, sess, q_all, ffn
         self.split = split_attention
@@ -250,8 +250,8 @@ class CudaNormal:
 
     def enqueue_attention(self, layer: int):
         b = self.buf
-        self.pi.sparse_decode_attn(0, self.q, b.pool, b.sel_slots, b.sel_blocks, b.sel_count, self.ctx, self.out, None,
-                                   stream=self.stream)
+        call = self.pi.sparse_decode_attn_kv4 if getattr(b, "kv_bits", 16) == 4 else self.pi.sparse_decode_attn
+        call(0, self.q, b.pool, b.sel_slots, b.sel_blocks, b.sel_count, self.ctx, self.out, None, stream=self.stream)
         ev = self.torch.cuda.Event(); ev.record(self.stream)
         return ev
 

@@ -52,13 +52,13 @@ class RecallPath:
     def recall(self, layer: int, buf: LayerBuffers, host_kv: torch.Tensor, recall_list, recall_count,
                page_table: Optional[torch.Tensor] = None, stream=None) -> None:
         """The lists' blocks from the host store into the pool, in whichever form the buffers keep them."""
-        call = self.pi.recall_kv4 if buf.kv_bits == 4 else self.pi.recall_gather_scatter
+        call = self.pi.recall_kv4 if getattr(buf, "kv_bits", 16) == 4 else self.pi.recall_gather_scatter
         call(layer, host_kv, buf.pool, recall_list, recall_count, page_table=page_table, stream=stream)
 
     def append(self, layer: int, step, buf: LayerBuffers, k_new, v_new, ctx_len, host_kv: torch.Tensor,
                page_table: Optional[torch.Tensor] = None, stream=None) -> None:
         """The step's token into pool, host store and digest."""
-        call = self.pi.append_kv4 if buf.kv_bits == 4 else self.pi.append_kv
+        call = self.pi.append_kv4 if getattr(buf, "kv_bits", 16) == 4 else self.pi.append_kv
         call(layer, step, k_new, v_new, ctx_len, host_kv, buf.pool, buf.block_table, buf.slot_block, buf.slot_stamp,
              buf.digest, page_table=page_table, stream=stream)
 
@@ -70,7 +70,7 @@ class RecallPath:
         host store needs kv_for_digest (the keys in logical block order)."""
         if page_table is not None and kv_for_digest is None:
             raise ValueError("a paged host store cannot be read in block order: pass kv_for_digest")
-        if buf.kv_bits == 4 and kv_for_digest is None:
+        if getattr(buf, "kv_bits", 16) == 4 and kv_for_digest is None:
             raise ValueError("digests are built from the keys in bf16: pass kv_for_digest")
         pi = self.pi
         pi.build_digests(layer, host_kv if kv_for_digest is None else kv_for_digest, ctx_len, buf.digest)
@@ -102,7 +102,7 @@ class RecallPath:
 
     def attention(self, layer: int, buf: LayerBuffers, q: torch.Tensor, ctx_len: torch.Tensor, out: torch.Tensor,
                   lse: Optional[torch.Tensor] = None, stream=None) -> None:
-        call = self.pi.sparse_decode_attn_kv4 if buf.kv_bits == 4 else self.pi.sparse_decode_attn
+        call = self.pi.sparse_decode_attn_kv4 if getattr(buf, "kv_bits", 16) == 4 else self.pi.sparse_decode_attn
         call(layer, q, buf.pool, buf.sel_slots, buf.sel_blocks, buf.sel_count, ctx_len, out, lse, stream=stream)
 
     def layer_step(self, layer: int, step: int, buf: LayerBuffers, q: torch.Tensor, ctx_len: torch.Tensor,
@@ -133,7 +133,7 @@ class RecallPath:
         stream, the resident blocks' share of the attention beside the recall on the side stream, the recalled
         blocks' share on the current stream once the recall has landed."""
         pi = self.pi
-        if buf.kv_bits != 16:
+        if getattr(buf, "kv_bits", 16) != 16:
             raise ValueError("the attention is split around the recall for bf16 blocks only")
         main = torch.cuda.current_stream()
         if fused:

@@ -109,3 +109,61 @@ def test_three_detection_modes_on_the_gpu_equal_the_serial_steps_and_order_as_de
     assert delays["semi"] < delays["async"], delays
     if not split:
         assert delays["semi"] < delays["sync"], delays
+
+
+def test_the_scheduler_on_4_bit_blocks_equals_the_serial_steps():
+    """The offload batch's pool and host store in 4-bit blocks: all three ways of noticing a recall end where the serial steps end."""
+    from paper_2609_34555_b200 import PulseInfer
+    from paper_2609_34555_b200.irq import MODES, CudaNormal, CudaOffload, IrqScheduler
+    from paper_2609_34555_b200.runner import DecodeSession, LayerBuffers
+    dev = torch.device("cuda:0")
+    cfg = tiny_config(batch=3, ctx=4000, n_layers=2, n_q_heads=16, n_kv_heads=4, budget_blocks=48, resident_frac=0.2)
+    steps = 4
+    q_all = torch.stack([gen.make_queries(cfg, l, steps, device=dev, ar1=0.8) for l in range(cfg.n_layers)], 1).contiguous()
+
+    def session(paged):
+        pi = PulseInfer.from_workload(cfg, recall_ctas=10)
+        sess = DecodeSession(pi, cfg.batch, cfg.n_layers, kv_bits=4, paged=paged)
+        sess.ctx_len.fill_(cfg.ctx)
+        for l in range(cfg.n_layers):
+            sess.load_layer(l, gen.make_kv(cfg, l, device=dev), torch.from_numpy(gen.initial_resident(cfg, l)).to(dev))
+        torch.cuda.synchronize()
+        return pi, sess
+
+    npi = PulseInfer.from_workload(tiny_config(batch=4, ctx=512, n_q_heads=16, n_kv_heads=4, budget_blocks=32, resident_frac=1.0, n_layers=1))
+    nbuf = LayerBuffers(npi, 4, dev, kv_bits=4)
+    kv = torch.randn((4 * npi.cfg.pool_slots, 4, 2, 16, 128), device=dev).to(torch.bfloat16)
+    rows = kv.transpose(1, 3)
+    npi.kv4_store(rows[:, :, 0], rows[:, :, 1], nbuf.pool)
+    ident = torch.arange(32, dtype=torch.int32, device=dev)[None, :].expand(4, -1).contiguous()
+    nbuf.sel_slots.copy_(ident); nbuf.sel_blocks.copy_(ident); nbuf.sel_count.fill_(32)
+    nq, nctx = torch.randn((4, 16, 128), device=dev).to(torch.bfloat16), torch.full((4,), 512, dtype=torch.int32, device=dev)
+    nout = torch.zeros_like(nq)
+    x = torch.randn((64, 1024), device=dev, dtype=torch.bfloat16)
+    w = torch.randn((1024, 1024), device=dev, dtype=torch.bfloat16) * 0.03
+    for paged in (False, True):
+        pi_r, want = session(paged)
+        for t in range(steps):
+            want.decode_step(q_all[t], overlapped=False)
+        torch.cuda.synchronize()
+        misses = pi_r.stats()["missing_blocks"]
+        assert pi_r.status()[0] == 0 and misses > 0
+        for mode in MODES:
+            pi, sess = session(paged)
+            off = CudaOffload(sess, q_all, lambda: torch.matmul(x, w))
+            nor = CudaNormal(npi, nbuf, nq, nctx, nout, lambda: torch.matmul(x, w), 4)
+            rep = IrqScheduler(off, nor, mode).run(steps * cfg.n_layers)
+            torch.cuda.synchronize()
+            assert pi.status()[0] == 0 and pi.stats()["missing_blocks"] == misses and rep.offload_layers == steps * cfg.n_layers
+            assert torch.equal(sess.out.view(torch.int16), want.out.view(torch.int16)), mode
+            for l, (got, ref) in enumerate(zip(_state(sess), _state(want))):
+                for g, r in zip(got, ref):
+                    assert torch.equal(g, r), f"{mode}: layer {l}"
+            pi.close()
+        with pytest.raises(ValueError):
+            CudaOffload(want, q_all, lambda: None, split_attention=True)
+        pi_r.close()
+    again = torch.zeros_like(nout)
+    npi.sparse_decode_attn_kv4(0, nq, nbuf.pool, nbuf.sel_slots, nbuf.sel_blocks, nbuf.sel_count, nctx, again)
+    assert torch.equal(nout, again) and bool((nout != 0).any()) and npi.status()[0] == 0
+    npi.close()
