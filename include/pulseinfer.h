@@ -359,7 +359,7 @@ int64_t pi_kv4_block_bytes(pi_ctx* ctx);
  *   free_pages_dev   [n_pages] int32 ring of free pages (in/out);  free_state_dev int64[4] (in/out): [0] pages
  *                    taken and [1] pages given back since the start (free pages are ring entries [0]..[1]-1
  *                    modulo n_pages: start with 0 and the number of free pages, entries in order from 0),
- *                    [2] must be 0 (used during the call), [3] unused
+ *                    [2] must be 0 (used during the call; not checked), [3] unused
  *   token_start_dev  NULL or [batch + 1] int32 (out): new tokens before each sequence, the total last
  *   n_tokens         capacity (at most 2^30) of the two maps of the packed batch of new tokens (sequence after sequence, in
  *                    order of position):
@@ -368,8 +368,8 @@ int64_t pi_kv4_block_bytes(pi_ctx* ctx);
  *                    pi_qk_norm_rope skip: a captured graph may keep one capacity.
  * All or nothing: a length that is negative or needs more blocks than the row or max_blocks holds
  * (PI_ERR_INDEX_RANGE: sequence, old, new), too few free pages (PI_ERR_POOL_TOO_SMALL: -1, wanted, free), more
- * pages given back than the ring has places or more tokens than n_tokens (PI_ERR_CAPACITY), or a damaged
- * free_state (PI_ERR_INDEX_RANGE) sets the status word with stage 7, changes no table, ring or counter, and
+ * pages given back than the ring has places or more tokens than n_tokens (PI_ERR_CAPACITY), or counters [0], [1]
+ * that cannot be (PI_ERR_INDEX_RANGE) sets the status word with stage 7, changes no table, ring or counter, and
  * fills the maps with -1 and token_start with 0.  A page outside [0, n_pages) found in the ring or the table
  * is reported likewise; its table entry and its tokens' slots become -1.
  * The caller orders calls that share a ring or a table; each sequence may appear in a batch once. */
@@ -427,7 +427,7 @@ int pi_recall_kv4(pi_ctx* ctx, int layer, int batch, const void* host_kv4_pinned
 
 /* pi_sparse_decode_attn over a pool of 4-bit blocks ([batch][C]); any Hkv and G of the context.  Bytes of tokens
  * beyond ctx_len in a selected block are ignored whatever they are.  A sequence without a single token to attend
- * to gets zeros, and lse -inf. */
+ * to gets zeros, and lse -inf.  Scores and sums are held in 32 bits: values below 2^100 stay within them for any list. */
 int pi_sparse_decode_attn_kv4(pi_ctx* ctx, int layer, int batch, const void* q_dev, const void* pool4_dev,
                               const int32_t* sel_slots_dev, const int32_t* sel_blocks_dev, const int32_t* sel_count_dev,
                               const int32_t* ctx_len_dev, void* out_dev, float* lse_dev, void* stream);

@@ -9,8 +9,9 @@
 //     contracted by themselves,  q.k = sum over groups  scale * (q . code) + minimum * (sum of q);  the minima's part is
 //     one more small product.  For V the scales are applied to the weights, one set per group, and the minima's part is
 //     again one product, of the weights and the minima.
-// The contractions run on mma.sync (tokens or channels on M, up to 8 query heads on N): with G <= 16 query heads per
-// KV head a 128-row tcgen05 tile would be nearly empty, and the codes have to pass through registers anyway.
+// The contractions run on mma.sync (tokens or channels on M, up to 8 query heads on N), whose operands are registers: the codes
+// are taken apart there. tcgen05 reads shared memory or TMEM, so every code would be written back first, two to four times as wide;
+// with 4 to 16 query heads on N the matrix pipe is a quarter busy as it is.
 // Codes are exact in fp16, queries after a power of two per head; weights times scales are rounded to 11 bits, which in the mean
 // square adds an eighth of the output's own rounding (2 % to its square); all sums are in 32 bits.
 //
@@ -20,10 +21,12 @@
 // end.  Every warp keeps its own running maximum and sum; the states are merged once, through shared memory, and
 // across the cluster through distributed shared memory: one launch, no partials in global memory.
 //
-// Measured on a B200, back to back: 16 sequences x 128 blocks of 16 tokens, 8 KV heads, G = 4 (42 MB) 15.6 us; 64 x 64 blocks
-// of 32 tokens (165 MB) 43.8 us, 3.8 TB/s; one sequence x 64 blocks 4.8 us.  The copies alone take 10.9 and 27.6 us of
-// the larger ones: what bounds them is the arithmetic, 396 instructions a tile and warp, of which 159 on the integer pipe and 48
-// packed fp16 ones at two cycles each (they do not overlap) and 20 matrix instructions at eight.
+// Measured on a B200, back to back: 16 sequences x 128 blocks of 16 tokens, 8 KV heads, G = 4 (42 MB) 15.8 us; 64 x 64 blocks
+// of 32 tokens (165 MB) 43.9 us, 3.8 TB/s; one sequence x 64 blocks 5.0 us; 64 x 64 blocks of 32 with G = 16 74 us.  The copies alone
+// take 10.9 and 27.6 us of the larger ones.  What bounds them is the length of a step's chain (load, unpack, product, vote,
+// exponential, transpose, product) with four warps a scheduler to cover it: about 400 instructions a tile and warp fill 62 % of the issue
+// slots with 3.1 of 4 warps present; the integer pipe and the packed fp16 operations, which do not overlap, take 65 % of the
+// cycles, the matrix pipe 25 %.
 // Tried and not taken: codes as 128 + code in bf16, or as 1024 + code with the offset taken off by a product with a constant
 // (one operation less a pair, paid back in matrix instructions); fp8 products (mma.sync turns the operands into fp16 first);
 // one CTA per item of 8 warps, and 3 CTAs of 168 registers an SM (slower by 5 to 10 %).
@@ -105,8 +108,9 @@ __device__ __forceinline__ void code_pairs(uint32_t w, uint32_t raise, uint32_t 
     }
 }
 // For K: from 0 on, and the second pair as 64 + code (0x5400 | 16 nibble), which is half the operations (2 % of the call's time).
-// The offset's part of the products is taken off with the minima's; in 32 bits that leaves a score of ordinary keys off by
-// 9e-7 instead of 1e-7, and scores of some hundred by 3.5e-5: 2^-6 of the output's own rounding.
+// The offset's part of the products is taken off with the minima's; cut to 32 bits on the way, that leaves scores about 1 off by
+// 8e-7 in the mean square and scores about 100 by 8e-5 (measured), some six times what codes from 0 would: 4 % of the output's
+// own rounding.
 __device__ __forceinline__ void code_pairs_k(uint32_t w, uint32_t raise, uint32_t raise64, uint32_t (&p)[4]) {
     const __half2 low = __halves2half2(__ushort_as_half(0xe400), __ushort_as_half(0xe400));        // -1024
 #pragma unroll
@@ -690,8 +694,8 @@ int pi_launch_attn_kv4(pi_ctx* c, int batch, const void* q, const void* pool, co
     // CTAs per item: what takes least by this estimate (microseconds, less what every call takes).  A cluster costs 1.0 more than
     // a CTA by itself; a step of its warps 1.0, or with k CTAs on the SM 0.12 + 0.59 k, when they fill its pipes (more than 8
     // heads: 0.8, or 0.5 k); the GPU starts 170 CTAs (85) in one, from three an SM on all in 3.0.  Measured, with S = 1 / 2 / 4 /
-    // 8: 64 items x 64 tiles 11.5 / 8.3 / 7.1 / 7.9 us, 144 x 16 tiles 5.3 / 5.9 / 10.8 / 16.5, 8 x 48 tiles 8.9 / 6.9 / 5.9 /
-    // 5.0, 128 x 128 tiles 20.2 / 16.0 / 15.8 / 19.9.  Clusters that would not all be on the GPU at once lose to smaller ones.
+    // 8: 64 items x 64 tiles 11.7 / 8.5 / 7.3 / 8.1 us, 144 x 16 tiles 5.2 / 5.9 / 10.7 / 16.1, 8 x 48 tiles 9.2 / 7.0 / 6.0 /
+    // 5.2, 128 x 128 tiles 20.7 / 16.1 / 16.0 / 20.4.  Clusters that would not all be on the GPU at once lose to smaller ones.
     int split = 1, warps = 4;
     double least = 0.;
     for (int s = 1; s <= A4_MAX_SPLIT; s *= 2) {
@@ -702,9 +706,9 @@ int pi_launch_attn_kv4(pi_ctx* c, int batch, const void* q, const void* pool, co
         const double cost = (s > 1 ? 1. : 0.) + static_cast<double>(steps - 1) * step + start;
         if (s == 1 || cost < least) { split = s; least = cost; }
     }
-    // Few items with long lists leave SMs with one CTA each, which 8 warps use better (8 items x 256 tiles 7.1 us, 8.0 with 4
-    // warps; x 1024 15.6, 20.8); a shorter list or more items pay for the larger merge (8 x 128 tiles gain 3 %, 16 x 256
-    // lose 2 to 8 %).
+    // Few items with long lists leave SMs with one CTA each, which 8 warps use better (8 items x 256 tiles 7.2 us, 8.4 with 4
+    // warps; x 1024 16.1, 21.4; one item x 1024 15.8, 20.7); a shorter list gains little (8 x 128 tiles 5.8, 6.2), more items nothing
+    // (16 x 256 9.9 both ways).
     if (NT == 1 && split == A4_MAX_SPLIT && items * split * 8 <= room && tiles >= 32 * std::max(items, 8ll)) warps = 8;
     const size_t ring = static_cast<size_t>(warps) * a4_steps(NT) * a4_tiles(NT) * KV4_TILE_BYTES + NT * (4 * 32 * 16 + 3 * 32 * 4 + 8 * 4);
     // (the merge of a CTA's warps, up to 33 KB for four, takes the ring's place; what the cluster sends lies behind)
