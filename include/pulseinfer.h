@@ -432,6 +432,26 @@ int pi_sparse_decode_attn_kv4(pi_ctx* ctx, int layer, int batch, const void* q_d
                               const int32_t* sel_slots_dev, const int32_t* sel_blocks_dev, const int32_t* sel_count_dev,
                               const int32_t* ctx_len_dev, void* out_dev, float* lse_dev, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------
+ * Attention over whole prompts, or chunks of them: what stands before the path.  (The paper takes a request up when its prompt is
+ * in the cache; this call exists for the library's users.)  A packed batch of sequences, one behind the other:
+ * sequence s has the queries q_start[s] .. q_start[s + 1] - 1 and the keys k_start[s] .. k_start[s + 1] - 1, and with n queries and
+ * m keys its query i sees the keys j <= i + m - n: the last query sees all, and where m > n the first m - n keys are those of
+ * earlier chunks.  out = softmax(q K^T / sqrt(D)) V for every query head over the keys of its KV head (head / G); lse its
+ * natural-log-sum-exp.  A query that sees no key (m < n) gets zeros, and lse -inf.  What a query does not see does not reach it,
+ * whatever it is (infinities and NaN too).
+ *   dtype            PI_DTYPE_BF16 or PI_DTYPE_FP16, of q, k, v and out
+ *   n_q, n_k         tokens of the tensors q_dev [n_q][Hq][D], k_dev and v_dev [n_k][Hkv][D]; rows contiguous, tokens and heads
+ *                    the given strides apart (in ELEMENTS, multiples of 8; so slices of one fused projection can be passed)
+ *   q_start_dev, k_start_dev  [n_seqs + 1] int32; k_start_dev NULL: the keys are packed as the queries are (m = n)
+ *   out_dev          [n_q][Hq][D], lse_dev NULL or [n_q][Hq] float; rows of tokens of no sequence stay as they were
+ * A sequence whose bounds decrease or leave the tensors is left out and sets PI_ERR_INDEX_RANGE (stage 8: sequence, its bounds).
+ * n_seqs at most max_batch.  Weights are rounded to the tensors' type before they meet V; all sums are in 32 bits. */
+int pi_prompt_attn(pi_ctx* ctx, int n_seqs, int dtype, int64_t n_q, const void* q_dev, int64_t q_token_stride, int64_t q_head_stride,
+                   int64_t n_k, const void* k_dev, int64_t k_token_stride, int64_t k_head_stride, const void* v_dev,
+                   int64_t v_token_stride, int64_t v_head_stride, const int32_t* q_start_dev, const int32_t* k_start_dev, void* out_dev,
+                   float* lse_dev, void* stream);
+
 /* Helpers around the path (input preparation and measurement; not hot calls).
  * pi_build_digests: channel-wise min / max of the keys of head solo_head[layer] over the
  *   valid tokens of each block; kv may be device memory or pinned host memory laid out
@@ -461,7 +481,8 @@ int pi_middle_attention_mass(pi_ctx* ctx, int batch, const float* lse_mid_dev, c
 int pi_empty_launch(int n_ctas, int n_threads, void* stream);
 
 /* Sticky device status.  out[0] = first PI_ERR_* code seen by a kernel (0 = none),
- * out[1] = stage (1 score/select, 2 diff, 3 recall, 4 attention, 5 append, 6 4-bit store / load, 7 page assignment), out[2..4] = sequence
+ * out[1] = stage (1 score/select, 2 diff, 3 recall, 4 attention, 5 append, 6 4-bit store / load, 7 page assignment,
+ * 8 prompt attention), out[2..4] = sequence
  * or list, position, offending value.  Reads a pinned mirror: call after the stream
  * has been synchronised.  pi_clear_status resets it. */
 int pi_get_status(pi_ctx* ctx, int32_t out[8]);

@@ -28,8 +28,9 @@ EXPORTS = ["pi_create", "pi_destroy", "pi_score_select", "pi_score_select_diff",
            "pi_recall_gather_scatter_paged", "pi_sparse_decode_attn", "pi_sparse_decode_attn_headwise", "pi_sparse_decode_attn_resident", "pi_sparse_decode_attn_recalled", "pi_attn_state_bytes", "pi_append_kv", "pi_append_kv_paged", "pi_append_kv_devstep", "pi_build_digests", "pi_build_digests_all", "pi_table_init", "pi_h2d_copy_ms", "pi_empty_launch", "pi_middle_attention_mass",
            "pi_get_status", "pi_get_stats", "pi_clear_status", "pi_strerror",
            "pi_kv4_block_bytes", "pi_assign_pages", "pi_qk_norm_rope", "pi_kv4_store", "pi_kv4_load", "pi_append_kv4", "pi_recall_kv4",
-           "pi_sparse_decode_attn_kv4"]
-FRONT_CALLS = ["pi_assign_pages", "pi_qk_norm_rope", "pi_kv4_store", "pi_kv4_load", "pi_append_kv4", "pi_recall_kv4", "pi_sparse_decode_attn_kv4"]
+           "pi_sparse_decode_attn_kv4", "pi_prompt_attn"]
+FRONT_CALLS = ["pi_assign_pages", "pi_qk_norm_rope", "pi_kv4_store", "pi_kv4_load", "pi_append_kv4", "pi_recall_kv4", "pi_sparse_decode_attn_kv4",
+               "pi_prompt_attn"]
 
 
 class PiConfig(ctypes.Structure):
@@ -100,6 +101,7 @@ def load_library(rebuild: bool = False) -> ctypes.CDLL:
                                   i32p, u32p, vp, vp]
     lib.pi_recall_kv4.argtypes = [c_void_p, c_int, c_int, vp, c_int64, i32p, c_int64, c_int32, vp, vp, c_int32, i32p, vp]
     lib.pi_sparse_decode_attn_kv4.argtypes = [c_void_p, c_int, c_int, vp, vp, i32p, i32p, i32p, i32p, vp, vp, vp]
+    lib.pi_prompt_attn.argtypes = [c_void_p, c_int, c_int, c_int64, vp, c_int64, c_int64, c_int64, vp, c_int64, c_int64, vp, c_int64, c_int64, i32p, i32p, vp, vp, vp]
     lib.pi_strerror.argtypes = [c_int]
     lib.pi_strerror.restype = c_char_p
     for name in EXPORTS:
@@ -494,6 +496,13 @@ class PulseInfer:
         """sparse_decode_attn over a pool of 4-bit blocks (uint8 [batch][C][kv4_block_bytes])."""
         _check("pi_sparse_decode_attn_kv4", self._front.sparse_decode_attn_kv4(self._shape, layer, q, pool4, sel_slots, sel_blocks, sel_count, ctx_len, out,
                                                                                lse, self._stream4(stream)))
+
+    def prompt_attn(self, q, k, v, q_start, out, k_start=None, lse=None, stream=None) -> None:
+        """Causal attention over a packed batch of prompts or prompt chunks: q [T][Hq][D], k, v [Tk][Hkv][D] (bf16 or fp16, any strides with
+        contiguous rows, so slices of one fused projection can be passed), out [T][Hq][D] of the same type, lse float32 [T][Hq].
+        q_start, k_start: int32 [sequences + 1] (k_start None: as q_start); the last query of a sequence sees all of its keys, each
+        one before it a key less.  Rows of tokens of no sequence stay as they were."""
+        _check("pi_prompt_attn", self._front.prompt_attn(self._shape, q, k, v, q_start, out, k_start, lse, self._stream4(stream)))
 
     # ------------------------------------------------------------------ helpers
     def build_digests(self, layer: int, kv, ctx_len, digest, kv_seq_stride: Optional[int] = None, stream=None) -> None:

@@ -7,6 +7,7 @@
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cstring>
 #include <initializer_list>
 #include <string>
 
@@ -22,6 +23,7 @@ struct Calls {
     decltype(&pi_append_kv4) append_kv4;
     decltype(&pi_recall_kv4) recall_kv4;
     decltype(&pi_sparse_decode_attn_kv4) sparse_decode_attn_kv4;
+    decltype(&pi_prompt_attn) prompt_attn;
 } g_calls;
 
 // What a context's calls look at: its address, device and shape.
@@ -48,6 +50,7 @@ const char* name_of(at::ScalarType t) {
         case at::kInt: return "torch.int32";
         case at::kLong: return "torch.int64";
         case at::kBFloat16: return "torch.bfloat16";
+        case at::kHalf: return "torch.float16";
         case at::kFloat: return "torch.float32";
         default: return "torch.uint8";
     }
@@ -298,6 +301,37 @@ int sparse_decode_attn_kv4(const Shape& s, Args a) {
                                           maybe<float>(s, a[8], at::kFloat, "lse", {batch, s.hq}), stream_of(a[9]));
 }
 
+int prompt_attn(const Shape& s, Args a) {
+    const at::Tensor& q = tensor(a[0], "q");
+    const auto type = q.scalar_type();
+    const int dtype = type == at::kBFloat16 ? PI_DTYPE_BF16 : type == at::kHalf ? PI_DTYPE_FP16 : -1;
+    int64_t place[3][2];                           // strides of token and head
+    auto rows = [&](PyObject* o, const char* name, int64_t tokens, int64_t heads, int64_t (&to)[2]) -> const at::Tensor& {
+        const at::Tensor& t = tensor(o, name);
+        if (dtype < 0 || t.scalar_type() != type || !t.is_cuda()) refuse(PyExc_TypeError, std::string(name) + ": expected a CUDA tensor of bfloat16 or float16, all of one type");
+        same_device(s, t, name);
+        if (t.dim() != 3 || (tokens >= 0 && t.size(0) != tokens) || t.size(1) != heads || t.size(2) != s.d) {
+            const int64_t want[3] = {tokens, heads, s.d};
+            refuse(PyExc_ValueError, std::string(name) + ": expected shape " + text_of(want) + ", got " + text_of(t.sizes()));
+        }
+        if (t.numel() && t.stride(2) != 1) refuse(PyExc_ValueError, std::string(name) + ": rows must be contiguous");
+        // (of an axis of one entry the stride means nothing, and torch may report any)
+        to[0] = t.size(0) > 1 ? t.stride(0) : heads * s.d;
+        to[1] = heads > 1 ? t.stride(1) : s.d;
+        return t;
+    };
+    rows(a[0], "q", -1, s.hq, place[0]);
+    const at::Tensor& k = rows(a[1], "k", -1, s.hkv, place[1]);
+    const at::Tensor& v = rows(a[2], "v", k.size(0), s.hkv, place[2]);
+    const at::Tensor& q_start = on(s, a[3], at::kInt, "q_start", {-1});
+    if (q_start.size(0) < 2) refuse(PyExc_ValueError, "q_start: expected at least two entries");
+    const int64_t n_seqs = q_start.size(0) - 1;
+    return call(g_calls.prompt_attn, s.ctx, n_seqs > INT32_MAX ? -1 : static_cast<int>(n_seqs), dtype, q.size(0), static_cast<const void*>(q.data_ptr()), place[0][0], place[0][1], k.size(0),
+                static_cast<const void*>(k.data_ptr()), place[1][0], place[1][1], static_cast<const void*>(v.data_ptr()), place[2][0], place[2][1], ptr<const int32_t>(q_start),
+                maybe<const int32_t>(s, a[5], at::kInt, "k_start", {n_seqs + 1}), on(s, a[4], type, "out", {q.size(0), s.hq, s.d}).data_ptr(),
+                maybe<float>(s, a[6], at::kFloat, "lse", {q.size(0), s.hq}), stream_of(a[7]));
+}
+
 // module function: (shape, arguments...) -> the C call's return code
 template <int (*CALL)(const Shape&, Args), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -332,22 +366,17 @@ PyObject* make_shape(PyObject*, PyObject* const* args, Py_ssize_t n) {
     }
 }
 
-// connect(addresses of the seven calls, in the order of Calls)
+// connect(addresses of the calls, in the order of Calls)
 PyObject* connect(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    static_assert(sizeof(Calls) == 7 * sizeof(void*), "seven calls");
-    if (n != 7) { PyErr_SetString(PyExc_TypeError, "connect: expected seven addresses"); return nullptr; }
-    void* p[7];
-    for (int i = 0; i < 7; ++i) {
+    constexpr Py_ssize_t count = sizeof(Calls) / sizeof(void*);
+    if (n != count) { PyErr_SetString(PyExc_TypeError, ("connect: expected " + std::to_string(count) + " addresses").c_str()); return nullptr; }
+    void* p[count];
+    for (Py_ssize_t i = 0; i < count; ++i) {
         p[i] = PyLong_AsVoidPtr(args[i]);
         if (!p[i]) { if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "connect: a null address"); return nullptr; }
     }
-    g_calls.assign_pages = reinterpret_cast<decltype(g_calls.assign_pages)>(p[0]);
-    g_calls.qk_norm_rope = reinterpret_cast<decltype(g_calls.qk_norm_rope)>(p[1]);
-    g_calls.kv4_store = reinterpret_cast<decltype(g_calls.kv4_store)>(p[2]);
-    g_calls.kv4_load = reinterpret_cast<decltype(g_calls.kv4_load)>(p[3]);
-    g_calls.append_kv4 = reinterpret_cast<decltype(g_calls.append_kv4)>(p[4]);
-    g_calls.recall_kv4 = reinterpret_cast<decltype(g_calls.recall_kv4)>(p[5]);
-    g_calls.sparse_decode_attn_kv4 = reinterpret_cast<decltype(g_calls.sparse_decode_attn_kv4)>(p[6]);
+    static_assert(sizeof p == sizeof g_calls, "addresses only");
+    std::memcpy(&g_calls, p, sizeof p);
     Py_RETURN_NONE;
 }
 
@@ -362,6 +391,7 @@ PyMethodDef methods[] = {
     METHOD("append_kv4", (&entry<append_kv4, 13>)),
     METHOD("recall_kv4", (&entry<recall_kv4, 7>)),
     METHOD("sparse_decode_attn_kv4", (&entry<sparse_decode_attn_kv4, 10>)),
+    METHOD("prompt_attn", (&entry<prompt_attn, 8>)),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_front", "Tensor checks and calls of the 4-bit path.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -15,6 +15,7 @@
 #define PI_STAGE_APPEND 5
 #define PI_STAGE_KV4    6
 #define PI_STAGE_PAGES  7
+#define PI_STAGE_PROMPT 8
 
 // Programmatic dependent launch.  Every kernel of the path is launched with programmatic stream
 // serialization: its grid may be scheduled while the kernel before it in the stream is still
@@ -182,3 +183,7 @@ int pi_launch_kv4_store(pi_ctx*, int64_t n_tokens, const void* k, const int64_t 
 int pi_launch_kv4_load(pi_ctx*, int64_t n_out, const void* store, int64_t n_blocks, const int32_t* blocks, void* out, cudaStream_t);
 int pi_launch_attn_kv4(pi_ctx*, int batch, const void* q, const void* pool, const int32_t* sel_slots, const int32_t* sel_blocks,
                        const int32_t* sel_count, const int32_t* ctx_len, void* out, float* lse, cudaStream_t);
+// strides in elements; n_q, n_k: tokens of the tensors
+int pi_launch_prompt_attn(pi_ctx*, int n_seqs, int dtype, int n_q, int n_k, const void* q, int64_t q_tok, int64_t q_head, const void* k,
+                          int64_t k_tok, int64_t k_head, const void* v, int64_t v_tok, int64_t v_head, const int32_t* q_start,
+                          const int32_t* k_start, void* out, float* lse, cudaStream_t);
