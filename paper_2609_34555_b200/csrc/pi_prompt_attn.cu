@@ -24,12 +24,16 @@ namespace {
 
 using namespace pi_attn;
 
-constexpr int PA_THREADS = 320;
+constexpr int PA_THREADS = 384;                  // three warpgroups: softmax of A, softmax of B, the rest (two of its warps have nothing to do)
+// registers of a softmax thread and of the others: 256 x 208 + 128 x 80 of the 384 x 168 that the block is launched with
+constexpr int PA_SOFTMAX_REGS = 208, PA_OTHER_REGS = 80;
+static_assert(256 * PA_SOFTMAX_REGS + 128 * PA_OTHER_REGS <= PA_THREADS * 168, "more than the block has");
 constexpr int PA_ROWS = 128;                        // rows of a query tile, and tokens of a K or V tile
 constexpr int PA_STAGES = 5;
 constexpr int PA_HALF = PA_ROWS * 128;              // 64 channels of 128 rows
 constexpr int PA_TILE = 2 * PA_HALF;
 constexpr float PA_NO_MAX = -3.40282347e38f;        // the lowest number, for -infinity in the running maximum: differences are no NaN
+constexpr float PA_FAR = 1024.f;
 constexpr uint32_t PA_TMEM_S = 0, PA_TMEM_O = 256;  // columns: S (and P) of A and B, O of A and B
 
 struct PromptParams {
@@ -98,10 +102,10 @@ __device__ __forceinline__ float pa_max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-// (a + b) c, a pair in two operations
-__device__ __forceinline__ float2 pa_add_mul(float2 a, float2 b, float2 c) {
+// a b + c, a pair in one operation
+__device__ __forceinline__ float2 pa_fma(float2 a, float2 b, float2 c) {
     float2 d;
-    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tadd.rn.f32x2 x, x, y;\n\tmul.rn.f32x2 x, x, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
         : "=f"(d.x), "=f"(d.y)
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
     return d;
@@ -230,114 +234,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const uint32_t tmem = s_tmem;
     volatile int* abort = &s_abort;
 
-    if (warp == 9) {
-        // ---- TMA: K0 V0 K1 V1 ...; the whole warp waits, one lane issues.  Three loads behind, a V tile that some row must not
-        // see all of is looked through: rows behind the sequence's end become 0, and so does every value that is no number
-        // (its weight would be 0 where it is masked, and 0 times it is none); those are put back at the end, row by row.
-        const int loads = 2 * n_tiles;
-        auto look = [&](int n) -> bool {            // load n is in the ring: is it such a V tile?
-            const int j = n >> 1;
-            if (!(n & 1) || j < odd_from) return true;
-            if (!mbar_wait(kv_full + 8 * (n % PA_STAGES), (n / PA_STAGES) & 1, abort, p.wait_cycles)) return false;
-            const uint32_t tile = ring + (n % PA_STAGES) * PA_TILE;
-            const int real = me.m - j * PA_ROWS;    // rows of the sequence
-            bool odd = false;
-#pragma unroll 4
-            for (int i = lane; i < PA_TILE / 16; i += 32) {
-                const int row = (i >> 3) & (PA_ROWS - 1);
-                uint32_t w[4];
-                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(tile + i * 16));
-                const uint32_t bad = not_finite<T>(w[0]) | not_finite<T>(w[1]) | not_finite<T>(w[2]) | not_finite<T>(w[3]);
-                if (row >= real) w[0] = w[1] = w[2] = w[3] = 0u;
-                else if (bad) {
-                    odd = true;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) w[k] &= ~((not_finite<T>(w[k]) >> 15) * 0xffffu);
-                }
-                if (row >= real || bad) asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(tile + i * 16), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-            }
-            if (odd) s_odd = 1;
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(v_good + 8 * (n % PA_STAGES));
-            return true;
-        };
-        if (n_tiles > 0 && lane == 0) {
-            const uint32_t bytes = static_cast<uint32_t>(p.tq) * p.G * 128u;
-            mbar_expect_tx(q_full, bytes * (n_b ? 4u : 2u));
-            for (int t = 0; t < (n_b ? 2 : 1); ++t)
-                for (int x = 0; x < 2; ++x) tma_load_q(smem + t * PA_TILE + x * PA_HALF, &map_q, q_full, 64 * x, 0, h, me.q0 + first + t * p.tq);
-        }
-        int n = 0;
-        bool alive = true;
-        for (; n < loads && alive; ++n) {
-            const int stage = n % PA_STAGES;
-            if (n >= PA_STAGES && !mbar_wait(kv_empty + 8 * stage, (n / PA_STAGES - 1) & 1, abort, p.wait_cycles)) break;
-            if (lane == 0) {
-                const CUtensorMap* map = (n & 1) ? &map_v : &map_k;
-                mbar_expect_tx(kv_full + 8 * stage, PA_TILE);
-                for (int x = 0; x < 2; ++x) tma_load_3d(ring + stage * PA_TILE + x * PA_HALF, map, kv_full + 8 * stage, 64 * x, h, me.k0 + (n >> 1) * PA_ROWS);
-            }
-            __syncwarp();
-            if (n >= 3) alive = look(n - 3);
-        }
-        for (int i = max(0, n - 3); i < n && alive; ++i) alive = look(i);
-        if (*abort) {                               // copies in flight end before the CTA does
-            volatile int none = 0;
-            if (n_tiles > 0) mbar_wait(q_full, 0, &none, p.wait_cycles);
-            for (int i = max(0, n - PA_STAGES); i < n; ++i) mbar_wait(kv_full + 8 * (i % PA_STAGES), (i / PA_STAGES) & 1, &none, p.wait_cycles);
-        }
-    } else if (warp == 8) {
-        if (lane == 0 && n_tiles > 0) {
-            constexpr uint32_t base = (1u << 4) | (Form<T>::code << 7) | (Form<T>::code << 10) | (static_cast<uint32_t>(PA_ROWS >> 3) << 17) | (static_cast<uint32_t>(PA_ROWS >> 4) << 24);
-            constexpr uint32_t idesc_s = base, idesc_o = base | (1u << 16);      // V: channels run along its rows
-            auto product_s = [&](int t, int n) {
-                const uint64_t a = desc_k_major(smem + t * PA_TILE), b = desc_k_major(ring + (n % PA_STAGES) * PA_TILE);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const uint64_t step = static_cast<uint64_t>(((k >> 2) * PA_HALF + (k & 3) * 32) >> 4);
-                    tc_mma_ss(tmem + PA_TMEM_S + 128 * t, a + step, b + step, idesc_s, k > 0);
-                }
-                tc_commit(s_full + 8 * t);
-            };
-            auto product_o = [&](int t, int n, bool add) {
-                const uint64_t b = desc_mn_major(ring + (n % PA_STAGES) * PA_TILE);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) tc_mma_ts(tmem + PA_TMEM_O + 128 * t, tmem + PA_TMEM_S + 128 * t + 8 * k, b + static_cast<uint64_t>((k * 2048) >> 4), idesc_o, add || k > 0);
-            };
-            const int tiles[2] = {tiles_a, tiles_b};
-            bool alive = mbar_wait(q_full, 0, abort, p.wait_cycles) && mbar_wait(kv_full, 0, abort, p.wait_cycles);
-            if (alive) {
-                tc_fence_after();
-                for (int t = 0; t < 2; ++t)
-                    if (tiles[t] > 0) product_s(t, 0);
-                tc_commit(kv_empty);
-            }
-            for (int j = 0; j < n_tiles && alive; ++j) {
-                const int nv = 2 * j + 1, nk = 2 * j + 2;
-                if (j < odd_from) alive = mbar_wait(kv_full + 8 * (nv % PA_STAGES), (nv / PA_STAGES) & 1, abort, p.wait_cycles);
-                else alive = mbar_wait(v_good + 8 * (nv % PA_STAGES), ((j - odd_from) / PA_STAGES) & 1, abort, p.wait_cycles);     // (a V tile meets its stage again five tiles on)
-                if (alive && j + 1 < n_tiles) alive = mbar_wait(kv_full + 8 * (nk % PA_STAGES), (nk / PA_STAGES) & 1, abort, p.wait_cycles);
-                for (int t = 0; t < 2 && alive; ++t) {
-                    if (j >= tiles[t]) continue;
-                    alive = mbar_wait(p_full + 8 * t, j & 1, abort, p.wait_cycles);
-                    if (!alive) break;
-                    tc_fence_after();
-                    product_o(t, nv, j > 0);
-                    if (j + 1 < tiles[t]) product_s(t, nk);
-                    else tc_commit(o_full + 8 * t);
-                }
-                if (!alive) break;
-                tc_commit(kv_empty + 8 * (nv % PA_STAGES));
-                if (j + 1 < n_tiles) tc_commit(kv_empty + 8 * (nk % PA_STAGES));
-            }
-            // products in flight end before the CTA does
-            volatile int none = 0;
-            tc_commit(drained);
-            mbar_wait(drained, 0, &none, p.wait_cycles);
-        }
-        __syncwarp();
-    } else {
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PA_SOFTMAX_REGS));
         // ---- softmax: thread = row r of tile t, token r / G, head r % G
         const int t = warp >> 2, r = tid & 127, tok = r / p.G, g = r - tok * p.G;
         const int n_tok = t ? n_b : n_a, tiles = t ? tiles_b : tiles_a;
@@ -348,7 +246,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;      // the warp's 32 lanes of tensor memory
         const uint32_t at_s = tmem + lanes + PA_TMEM_S + 128 * t, at_o = tmem + lanes + PA_TMEM_O + 128 * t;
         const float c = p.scale_log2;
-        float m = PA_NO_MAX, l = 0.f;
+        float m = PA_NO_MAX, mc = PA_NO_MAX, l = 0.f;      // the reference of the row's weights, as a score and times c; their sum
+        bool far = false;
         bool alive = true;
         for (int j = 0; j < tiles; ++j) {
             if (!mbar_wait(s_full + 8 * t, j & 1, abort, p.wait_cycles)) { alive = false; break; }
@@ -362,13 +261,21 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
                 for (int x = 0; x < 128; ++x) s[x] = x < left ? s[x] : -INFINITY;
             }
-            float mx = pa_max3(s[0], s[1], s[2]);
+            float mx4[4];
 #pragma unroll
-            for (int x = 3; x < 127; x += 2) mx = pa_max3(mx, s[x], s[x + 1]);
-            mx = fmaxf(mx, s[127]);
-            if (__any_sync(0xffffffffu, (mx - m) * c > 8.f)) {
-                const float m_new = fmaxf(m, mx), alpha = pa_ex2((m - m_new) * c);
+            for (int x = 0; x < 4; ++x) {
+                mx4[x] = fmaxf(s[x], s[x + 4]);
+#pragma unroll
+                for (int y = 8; y < 128; y += 8) mx4[x] = pa_max3(mx4[x], s[x + y], s[x + y + 4]);
+            }
+            const float mx = fmaxf(pa_max3(mx4[0], mx4[1], mx4[2]), mx4[3]);
+            if (__any_sync(0xffffffffu, mx * c - mc > 8.f)) {
+                const float m_new = fmaxf(m, mx), mc_new = m_new * c;
+                // (far from 0 the reference's own rounding counts: see below)
+                const float alpha = pa_ex2(fabsf(mc_new) > PA_FAR ? (m - m_new) * c : mc - mc_new);
                 m = m_new;
+                mc = mc_new;
+                far = __any_sync(0xffffffffu, fabsf(mc) > PA_FAR);
                 l *= alpha;
                 if (j > 0) {
 #pragma unroll 1
@@ -383,15 +290,23 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     tc_wait_st();
                 }
             }
-            // (the maximum is taken off before the scale: scores of any size keep their differences)
-            const float2 less = make_float2(-m, -m), cc = make_float2(c, c);
+            // The weight is 2^(s c - mc), one fused operation and the exponential: mc is what the row's weights are counted from, and its
+            // rounding is in all of them alike.  Where it is large that rounding would leave the range of the weights, so there the
+            // maximum is taken off before the scale.
+            float2 less = make_float2(-mc, -mc);
+            if (far) {
+#pragma unroll
+                for (int x = 0; x < 128; ++x) s[x] -= m;
+                less = make_float2(0.f, 0.f);
+            }
+            const float2 cc = make_float2(c, c);
             float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 uint32_t w[32];
 #pragma unroll
                 for (int y = 0; y < 32; ++y) {
-                    float2 v = pa_add_mul(make_float2(s[64 * x + 2 * y], s[64 * x + 2 * y + 1]), less, cc);
+                    float2 v = pa_fma(make_float2(s[64 * x + 2 * y], s[64 * x + 2 * y + 1]), cc, less);
                     v.x = pa_ex2(v.x);
                     v.y = pa_ex2(v.y);
                     sum = pa_add(sum, v);
@@ -441,9 +356,119 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     to[y] = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
-            if (real && p.lse) p.lse[row] = none ? -INFINITY : (m * c + log2f(l)) * 0.6931471805599453f;
+            if (real && p.lse) p.lse[row] = none ? -INFINITY : (mc + log2f(l)) * 0.6931471805599453f;
         }
         tc_fence_before();
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PA_OTHER_REGS));
+        if (warp == 9) {
+            // ---- TMA: K0 V0 K1 V1 ...; the whole warp waits, one lane issues.  Three loads behind, a V tile that some row must not
+            // see all of is looked through: rows behind the sequence's end become 0, and so does every value that is no number
+            // (its weight would be 0 where it is masked, and 0 times it is none); those are put back at the end, row by row.
+            const int loads = 2 * n_tiles;
+            auto look = [&](int n) -> bool {            // load n is in the ring: is it such a V tile?
+                const int j = n >> 1;
+                if (!(n & 1) || j < odd_from) return true;
+                if (!mbar_wait(kv_full + 8 * (n % PA_STAGES), (n / PA_STAGES) & 1, abort, p.wait_cycles)) return false;
+                const uint32_t tile = ring + (n % PA_STAGES) * PA_TILE;
+                const int real = me.m - j * PA_ROWS;    // rows of the sequence
+                bool odd = false;
+#pragma unroll 4
+                for (int i = lane; i < PA_TILE / 16; i += 32) {
+                    const int row = (i >> 3) & (PA_ROWS - 1);
+                    uint32_t w[4];
+                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(tile + i * 16));
+                    const uint32_t bad = not_finite<T>(w[0]) | not_finite<T>(w[1]) | not_finite<T>(w[2]) | not_finite<T>(w[3]);
+                    if (row >= real) w[0] = w[1] = w[2] = w[3] = 0u;
+                    else if (bad) {
+                        odd = true;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) w[k] &= ~((not_finite<T>(w[k]) >> 15) * 0xffffu);
+                    }
+                    if (row >= real || bad) asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(tile + i * 16), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                }
+                if (odd) s_odd = 1;
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(v_good + 8 * (n % PA_STAGES));
+                return true;
+            };
+            if (n_tiles > 0 && lane == 0) {
+                const uint32_t bytes = static_cast<uint32_t>(p.tq) * p.G * 128u;
+                mbar_expect_tx(q_full, bytes * (n_b ? 4u : 2u));
+                for (int t = 0; t < (n_b ? 2 : 1); ++t)
+                    for (int x = 0; x < 2; ++x) tma_load_q(smem + t * PA_TILE + x * PA_HALF, &map_q, q_full, 64 * x, 0, h, me.q0 + first + t * p.tq);
+            }
+            int n = 0;
+            bool alive = true;
+            for (; n < loads && alive; ++n) {
+                const int stage = n % PA_STAGES;
+                if (n >= PA_STAGES && !mbar_wait(kv_empty + 8 * stage, (n / PA_STAGES - 1) & 1, abort, p.wait_cycles)) break;
+                if (lane == 0) {
+                    const CUtensorMap* map = (n & 1) ? &map_v : &map_k;
+                    mbar_expect_tx(kv_full + 8 * stage, PA_TILE);
+                    for (int x = 0; x < 2; ++x) tma_load_3d(ring + stage * PA_TILE + x * PA_HALF, map, kv_full + 8 * stage, 64 * x, h, me.k0 + (n >> 1) * PA_ROWS);
+                }
+                __syncwarp();
+                if (n >= 3) alive = look(n - 3);
+            }
+            for (int i = max(0, n - 3); i < n && alive; ++i) alive = look(i);
+            if (*abort) {                               // copies in flight end before the CTA does
+                volatile int none = 0;
+                if (n_tiles > 0) mbar_wait(q_full, 0, &none, p.wait_cycles);
+                for (int i = max(0, n - PA_STAGES); i < n; ++i) mbar_wait(kv_full + 8 * (i % PA_STAGES), (i / PA_STAGES) & 1, &none, p.wait_cycles);
+            }
+        } else if (warp == 8) {
+            if (lane == 0 && n_tiles > 0) {
+                constexpr uint32_t base = (1u << 4) | (Form<T>::code << 7) | (Form<T>::code << 10) | (static_cast<uint32_t>(PA_ROWS >> 3) << 17) | (static_cast<uint32_t>(PA_ROWS >> 4) << 24);
+                constexpr uint32_t idesc_s = base, idesc_o = base | (1u << 16);      // V: channels run along its rows
+                auto product_s = [&](int t, int n) {
+                    const uint64_t a = desc_k_major(smem + t * PA_TILE), b = desc_k_major(ring + (n % PA_STAGES) * PA_TILE);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const uint64_t step = static_cast<uint64_t>(((k >> 2) * PA_HALF + (k & 3) * 32) >> 4);
+                        tc_mma_ss(tmem + PA_TMEM_S + 128 * t, a + step, b + step, idesc_s, k > 0);
+                    }
+                    tc_commit(s_full + 8 * t);
+                };
+                auto product_o = [&](int t, int n, bool add) {
+                    const uint64_t b = desc_mn_major(ring + (n % PA_STAGES) * PA_TILE);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) tc_mma_ts(tmem + PA_TMEM_O + 128 * t, tmem + PA_TMEM_S + 128 * t + 8 * k, b + static_cast<uint64_t>((k * 2048) >> 4), idesc_o, add || k > 0);
+                };
+                const int tiles[2] = {tiles_a, tiles_b};
+                bool alive = mbar_wait(q_full, 0, abort, p.wait_cycles) && mbar_wait(kv_full, 0, abort, p.wait_cycles);
+                if (alive) {
+                    tc_fence_after();
+                    for (int t = 0; t < 2; ++t)
+                        if (tiles[t] > 0) product_s(t, 0);
+                    tc_commit(kv_empty);
+                }
+                for (int j = 0; j < n_tiles && alive; ++j) {
+                    const int nv = 2 * j + 1, nk = 2 * j + 2;
+                    if (j < odd_from) alive = mbar_wait(kv_full + 8 * (nv % PA_STAGES), (nv / PA_STAGES) & 1, abort, p.wait_cycles);
+                    else alive = mbar_wait(v_good + 8 * (nv % PA_STAGES), ((j - odd_from) / PA_STAGES) & 1, abort, p.wait_cycles);     // (a V tile meets its stage again five tiles on)
+                    if (alive && j + 1 < n_tiles) alive = mbar_wait(kv_full + 8 * (nk % PA_STAGES), (nk / PA_STAGES) & 1, abort, p.wait_cycles);
+                    for (int t = 0; t < 2 && alive; ++t) {
+                        if (j >= tiles[t]) continue;
+                        alive = mbar_wait(p_full + 8 * t, j & 1, abort, p.wait_cycles);
+                        if (!alive) break;
+                        tc_fence_after();
+                        product_o(t, nv, j > 0);
+                        if (j + 1 < tiles[t]) product_s(t, nk);
+                        else tc_commit(o_full + 8 * t);
+                    }
+                    if (!alive) break;
+                    tc_commit(kv_empty + 8 * (nv % PA_STAGES));
+                    if (j + 1 < n_tiles) tc_commit(kv_empty + 8 * (nk % PA_STAGES));
+                }
+                // products in flight end before the CTA does
+                volatile int none = 0;
+                tc_commit(drained);
+                mbar_wait(drained, 0, &none, p.wait_cycles);
+            }
+            __syncwarp();
+        }
     }
     __syncthreads();
     if (warp == 8) {
