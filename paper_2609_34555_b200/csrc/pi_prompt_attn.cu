@@ -17,6 +17,7 @@
 // The maximum that is taken off moves only when a score exceeds it by a factor of 2^8 after the exponential, so that O is seldom
 // rescaled; then the softmax warps do it themselves, between their S and their P, when no product of their tile is in flight.
 #include <cuda_fp16.h>
+#include <cstdlib>
 
 #include "pi_attn_core.cuh"
 
@@ -30,6 +31,7 @@ constexpr int PA_SOFTMAX_REGS = 208, PA_OTHER_REGS = 80;
 static_assert(256 * PA_SOFTMAX_REGS + 128 * PA_OTHER_REGS <= PA_THREADS * 168, "more than the block has");
 constexpr int PA_ROWS = 128;                        // rows of a query tile, and tokens of a K or V tile
 constexpr int PA_STAGES = 5;
+constexpr int PA_MAX_SPLIT = 8;                     // CTAs of a cluster that share an item
 constexpr int PA_HALF = PA_ROWS * 128;              // 64 channels of 128 rows
 constexpr int PA_TILE = 2 * PA_HALF;
 constexpr float PA_NO_MAX = -3.40282347e38f;        // the lowest number, for -infinity in the running maximum: differences are no NaN
@@ -46,6 +48,7 @@ struct PromptParams {
     long long wait_cycles, v_tok, v_head;
     float scale_log2;                               // log2(e) / sqrt(D)
     int n_seqs, Hq, Hkv, G, tq, n_q, n_k;           // tq: tokens of a query tile
+    int hold_last;                                  // test only: an item's last V tile is never fetched
 };
 
 // ---------------------------------------------------------------- PTX wrappers
@@ -164,318 +167,562 @@ __device__ __forceinline__ Span span_of(const PromptParams& p, int s, bool tell)
     return x;
 }
 
-template <typename T>
+// One piece of work: a block of up to 2 tq tokens of a sequence and a KV head.
+struct Item {
+    int q0, n, k0, m;                               // the sequence
+    int first, h;                                   // the block's first token, its KV head; h < 0: there is no more work
+};
+
+// What follows from an item, for every role alike.
+struct Plan {
+    int off, n_a, n_b, lo, hi, tiles_a, tiles_b, odd_from;
+    bool pair;
+    __device__ __forceinline__ Plan(const PromptParams& p, const Item& w, int rank, int split) {
+        off = w.m - w.n;                            // token i sees the keys j < i + off + 1
+        n_a = min(p.tq, w.n - w.first);
+        n_b = min(p.tq, max(0, w.n - w.first - p.tq));
+        auto upto = [&](int i) { return (seen(w, i) + PA_ROWS - 1) / PA_ROWS; };
+        tiles_a = upto(w.first + n_a - 1);
+        tiles_b = n_b ? upto(w.first + p.tq + n_b - 1) : tiles_a;
+        pair = n_b == 0;                            // one query tile: the softmax groups take every second K/V tile each
+        const int all = max(tiles_a, tiles_b);
+        lo = static_cast<int>(static_cast<long long>(all) * rank / split);
+        hi = static_cast<int>(static_cast<long long>(all) * (rank + 1) / split);
+        tiles_a = min(tiles_a, hi);
+        tiles_b = min(tiles_b, hi);
+        odd_from = seen(w, w.first) / PA_ROWS;      // from this tile on, some row of the block does not see all of a tile
+    }
+    __device__ __forceinline__ int seen(const Item& w, int i) const { return min(max(i + off + 1, 0), w.m); }
+    // group t's first K/V tile, and how far it is to the next
+    __device__ __forceinline__ int begin(int t) const { return pair ? lo + t : lo; }
+    __device__ __forceinline__ int step() const { return pair ? 2 : 1; }
+    __device__ __forceinline__ int end(int t) const { return t ? tiles_b : tiles_a; }
+};
+
+__device__ __forceinline__ float ld_cluster(uint32_t addr) { return ld_shared_cluster_f32(addr); }
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
+// Barriers, in 8-byte places.
+enum : uint32_t {
+    B_Q_FULL = 0, B_Q_EMPTY = 1, B_DRAINED = 2, B_MERGED = 3, B_HALF = 4, B_NEXT = 5, B_ITEM_FULL = 6, B_ITEM_EMPTY = 8, B_S_FULL = 10, B_P_FULL = 12, B_O_FULL = 14,
+    B_ALL = 16, B_KV_FULL = 17, B_KV_EMPTY = B_KV_FULL + PA_STAGES, B_V_GOOD = B_KV_EMPTY + PA_STAGES, B_COUNT = B_V_GOOD + PA_STAGES
+};
+
+constexpr uint32_t PA_ML_AT = 2 * PA_ROWS * 512;    // a cluster's shares: [256 rows][128] in 32 bits, then every row's reference and sum
+
+// SPLIT: a cluster of CTAs shares an item, each with a run of its K/V tiles.  Else a CTA takes one item after the other: it begins with its own
+// place in the grid and then takes over CTAs that have not begun yet, so that loads, barriers and tensor memory run on.
+template <typename T, bool SPLIT>
 __global__ void __launch_bounds__(PA_THREADS, 1)
 prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, PromptParams p) {
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t s_bar[2 + 3 * PA_STAGES + 6];
+    __shared__ __align__(16) uint32_t s_next[4];    // what came of taking over a CTA
+    __shared__ __align__(8) uint64_t s_bar[B_COUNT];
+    __shared__ Item s_item[2];
+    __shared__ float2 s_ml[PA_ROWS];                // tile A alone: reference and sum of group B's rows
     __shared__ uint32_t s_tmem;
-    __shared__ int s_abort, s_odd;                  // s_odd: values that are no numbers were taken out of a tile
+    __shared__ int s_abort, s_odd[2];               // s_odd: values that are no numbers were taken out of a tile
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    pi_grid_dependency_wait();
-    pi_launch_dependents();
-
-    // ---- the CTA's work: blocks of 2 tq tokens, counted from the last one of the last sequence (the longest come first), heads innermost
-    const int h = static_cast<int>(blockIdx.x % static_cast<unsigned>(p.Hkv)), item = static_cast<int>(blockIdx.x / static_cast<unsigned>(p.Hkv));
-    const int per_block = 2 * p.tq;
-    int total = 0;
-    for (int s0 = 0; s0 < p.n_seqs; s0 += 32) total += (span_of(p, s0 + lane, blockIdx.x == 0 && warp == 0).n + per_block - 1) / per_block;
-    total = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(total)));
-    if (item >= total) return;
-    int at = total - 1 - item, block = 0;
-    Span me = {0, 0, 0, 0};
-    for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
-        const Span x = span_of(p, s0 + lane, false);
-        const int nb = (x.n + per_block - 1) / per_block;
-        int upto = nb;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, upto, d);
-            if (lane >= d) upto += y;
-        }
-        const unsigned found = __ballot_sync(0xffffffffu, at < upto);
-        if (found) {
-            const int from = __ffs(static_cast<int>(found)) - 1;
-            block = at - __shfl_sync(0xffffffffu, upto - nb, from);
-            me.q0 = __shfl_sync(0xffffffffu, x.q0, from); me.n = __shfl_sync(0xffffffffu, x.n, from);
-            me.k0 = __shfl_sync(0xffffffffu, x.k0, from); me.m = __shfl_sync(0xffffffffu, x.m, from);
-            break;
-        }
-        at -= __shfl_sync(0xffffffffu, upto, 31);
-    }
-    const int first = block * per_block;            // the block's first token
-    const int off = me.m - me.n;                    // token i sees the keys j < i + off + 1
-    const int n_a = min(p.tq, me.n - first), n_b = min(p.tq, max(0, me.n - first - p.tq));
-    auto seen_by = [&](int i) { return min(max(i + off + 1, 0), me.m); };
-    const int tiles_a = (seen_by(first + n_a - 1) + PA_ROWS - 1) / PA_ROWS, tiles_b = n_b ? (seen_by(first + p.tq + n_b - 1) + PA_ROWS - 1) / PA_ROWS : 0;
-    const int n_tiles = max(tiles_a, tiles_b);
-    const int odd_from = seen_by(first) / PA_ROWS;  // from this tile on, some row of the block does not see all of a tile
-
+    const int split = SPLIT ? static_cast<int>(cluster_nctarank()) : 1, rank = SPLIT ? static_cast<int>(cluster_ctarank()) : 0;
     const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = smem + 2 * PA_TILE;
     const uint32_t bars = smem_u32(s_bar);
-    const uint32_t q_full = bars, drained = bars + 8, kv_full = bars + 16, kv_empty = kv_full + 8 * PA_STAGES, s_full = kv_empty + 8 * PA_STAGES, p_full = s_full + 16,
-                   o_full = p_full + 16, v_good = o_full + 16;
+    auto bar = [&](uint32_t place) { return bars + 8 * place; };
     if (tid == 0) {
-        mbar_init(q_full, 1);
-        mbar_init(drained, 1);
-        for (int i = 0; i < PA_STAGES; ++i) { mbar_init(kv_full + 8 * i, 1); mbar_init(kv_empty + 8 * i, 1); mbar_init(v_good + 8 * i, 1); }
-        for (int t = 0; t < 2; ++t) { mbar_init(s_full + 8 * t, 1); mbar_init(p_full + 8 * t, 4); mbar_init(o_full + 8 * t, 1); }
+        for (uint32_t i = 0; i < B_COUNT; ++i) {
+            const bool by_warps = i == B_P_FULL || i == B_P_FULL + 1 || i == B_MERGED || i == B_HALF;
+            mbar_init(bar(i), by_warps ? 4 : i == B_ALL ? 8 : i == B_ITEM_EMPTY || i == B_ITEM_EMPTY + 1 ? 11 : 1);
+        }
         s_abort = 0;
-        s_odd = 0;
+        s_odd[0] = s_odd[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 8) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    if (warp == 9 && lane < 3) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &map_q : lane == 1 ? &map_k : &map_v));
+    pi_grid_dependency_wait();
+    pi_launch_dependents();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = s_tmem;
     volatile int* abort = &s_abort;
+    // item number `it` of this CTA, for the roles that are told
+    auto item_of = [&](int it, Item& w) -> bool {
+        if (!mbar_wait(bar(B_ITEM_FULL + (it & 1)), (it >> 1) & 1, abort, p.wait_cycles)) return false;
+        w = s_item[it & 1];
+        return w.h >= 0;
+    };
+    auto done_with = [&](int it) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(B_ITEM_EMPTY + (it & 1)));
+    };
 
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PA_SOFTMAX_REGS));
-        // ---- softmax: thread = row r of tile t, token r / G, head r % G
+        // ---- softmax: thread = row r of tile t (of tile A where that is alone), token r / G, head r % G
         const int t = warp >> 2, r = tid & 127, tok = r / p.G, g = r - tok * p.G;
-        const int n_tok = t ? n_b : n_a, tiles = t ? tiles_b : tiles_a;
-        const bool real = tok < n_tok && tok < p.tq;
-        const int i = first + t * p.tq + tok;
-        const int seen = real ? seen_by(i) : INT32_MAX;      // (rows of no query may be anything: none is looked at)
-        const int all_see = __reduce_min_sync(0xffffffffu, seen);
         const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;      // the warp's 32 lanes of tensor memory
         const uint32_t at_s = tmem + lanes + PA_TMEM_S + 128 * t, at_o = tmem + lanes + PA_TMEM_O + 128 * t;
         const float c = p.scale_log2;
-        float m = PA_NO_MAX, mc = PA_NO_MAX, l = 0.f;      // the reference of the row's weights, as a score and times c; their sum
-        bool far = false;
+        auto far_off = [](float x) { return fabsf(x) > PA_FAR && x != PA_NO_MAX; };
+        uint32_t steps = 0u, results = 0u, merges = 0u;      // so far: S of this tile, O of this tile, items of one query tile
         bool alive = true;
-        for (int j = 0; j < tiles; ++j) {
-            if (!mbar_wait(s_full + 8 * t, j & 1, abort, p.wait_cycles)) { alive = false; break; }
-            tc_fence_after();
-            float s[128];
+        Item w;
+        for (int it = 0; alive && item_of(it, w); ++it) {
+            const Plan plan(p, w, rank, split);
+            const int n_tok = t && !plan.pair ? plan.n_b : plan.n_a, i = w.first + (t && !plan.pair ? p.tq : 0) + tok;
+            const bool real = tok < n_tok;
+            const int seen = real ? plan.seen(w, i) : INT32_MAX;     // (rows of no query may be anything: none is looked at)
+            const int all_see = __reduce_min_sync(0xffffffffu, seen);
+            const int begin = plan.begin(t), end = plan.end(t);
+            float m = PA_NO_MAX, mc = PA_NO_MAX, l = 0.f;            // the reference of the row's weights, as a score and times c; their sum
+            bool far = false;
+            for (int j = begin; j < end; j += plan.step(), ++steps) {
+                if (!mbar_wait(bar(B_S_FULL + t), steps & 1u, abort, p.wait_cycles)) { alive = false; break; }
+                tc_fence_after();
+                float s[128];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) tc_ld32(at_s + 32 * x, s + 32 * x);
-            tc_wait_ld();
-            if ((j + 1) * PA_ROWS > all_see) {
-                const int left = seen - j * PA_ROWS;
+                for (int x = 0; x < 4; ++x) tc_ld32(at_s + 32 * x, s + 32 * x);
+                tc_wait_ld();
+                if ((j + 1) * PA_ROWS > all_see) {
+                    const int left = seen - j * PA_ROWS;
 #pragma unroll
-                for (int x = 0; x < 128; ++x) s[x] = x < left ? s[x] : -INFINITY;
-            }
-            float mx4[4];
+                    for (int x = 0; x < 128; ++x) s[x] = x < left ? s[x] : -INFINITY;
+                }
+                float mx4[4];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                mx4[x] = fmaxf(s[x], s[x + 4]);
+                for (int x = 0; x < 4; ++x) {
+                    mx4[x] = fmaxf(s[x], s[x + 4]);
 #pragma unroll
-                for (int y = 8; y < 128; y += 8) mx4[x] = pa_max3(mx4[x], s[x + y], s[x + y + 4]);
-            }
-            const float mx = fmaxf(pa_max3(mx4[0], mx4[1], mx4[2]), mx4[3]);
-            if (__any_sync(0xffffffffu, mx * c - mc > 8.f)) {
-                const float m_new = fmaxf(m, mx), mc_new = m_new * c;
-                // (far from 0 the reference's own rounding counts: see below)
-                const float alpha = pa_ex2(fabsf(mc_new) > PA_FAR ? (m - m_new) * c : mc - mc_new);
-                m = m_new;
-                mc = mc_new;
-                far = __any_sync(0xffffffffu, fabsf(mc) > PA_FAR);
-                l *= alpha;
-                if (j > 0) {
+                    for (int y = 8; y < 128; y += 8) mx4[x] = pa_max3(mx4[x], s[x + y], s[x + y + 4]);
+                }
+                const float mx = fmaxf(pa_max3(mx4[0], mx4[1], mx4[2]), mx4[3]);
+                if (__any_sync(0xffffffffu, mx * c - mc > 8.f)) {
+                    const float m_new = fmaxf(m, mx), mc_new = m_new == PA_NO_MAX ? PA_NO_MAX : m_new * c;
+                    // (far from 0 the reference's own rounding counts: see below)
+                    const float alpha = pa_ex2(far_off(mc_new) ? (m - m_new) * c : mc - mc_new);
+                    m = m_new;
+                    mc = mc_new;
+                    far = __any_sync(0xffffffffu, far_off(mc));
+                    l *= alpha;
+                    if (j > begin) {
 #pragma unroll 1
-                    for (int x = 0; x < 4; ++x) {
-                        float o[32];
-                        tc_ld32(at_o + 32 * x, o);
-                        tc_wait_ld();
+                        for (int x = 0; x < 4; ++x) {
+                            float o[32];
+                            tc_ld32(at_o + 32 * x, o);
+                            tc_wait_ld();
 #pragma unroll
-                        for (int y = 0; y < 32; ++y) o[y] *= alpha;
-                        tc_st32(at_o + 32 * x, reinterpret_cast<const uint32_t*>(o));
+                            for (int y = 0; y < 32; ++y) o[y] *= alpha;
+                            tc_st32(at_o + 32 * x, reinterpret_cast<const uint32_t*>(o));
+                        }
+                        tc_wait_st();
                     }
-                    tc_wait_st();
                 }
-            }
-            // The weight is 2^(s c - mc), one fused operation and the exponential: mc is what the row's weights are counted from, and its
-            // rounding is in all of them alike.  Where it is large that rounding would leave the range of the weights, so there the
-            // maximum is taken off before the scale.
-            float2 less = make_float2(-mc, -mc);
-            if (far) {
+                // The weight is 2^(s c - mc), one fused operation and the exponential: mc is what the row's weights are counted from, and its
+                // rounding is in all of them alike.  Where it is large that rounding would leave the range of the weights, so there the
+                // maximum is taken off before the scale.
+                float2 less = make_float2(-mc, -mc);
+                if (far) {
 #pragma unroll
-                for (int x = 0; x < 128; ++x) s[x] -= m;
-                less = make_float2(0.f, 0.f);
-            }
-            const float2 cc = make_float2(c, c);
-            float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                uint32_t w[32];
-#pragma unroll
-                for (int y = 0; y < 32; ++y) {
-                    float2 v = pa_fma(make_float2(s[64 * x + 2 * y], s[64 * x + 2 * y + 1]), cc, less);
-                    v.x = pa_ex2(v.x);
-                    v.y = pa_ex2(v.y);
-                    sum = pa_add(sum, v);
-                    w[y] = Form<T>::pack(v.x, v.y);
+                    for (int x = 0; x < 128; ++x) s[x] -= m;
+                    less = make_float2(0.f, 0.f);
                 }
-                tc_st32(at_s + 32 * x, w);
+                const float2 cc = make_float2(c, c);
+                float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    uint32_t u[32];
+#pragma unroll
+                    for (int y = 0; y < 32; ++y) {
+                        float2 v = pa_fma(make_float2(s[64 * x + 2 * y], s[64 * x + 2 * y + 1]), cc, less);
+                        v.x = pa_ex2(v.x);
+                        v.y = pa_ex2(v.y);
+                        sum = pa_add(sum, v);
+                        u[y] = Form<T>::pack(v.x, v.y);
+                    }
+                    tc_st32(at_s + 32 * x, u);
+                }
+                l += sum.x + sum.y;
+                tc_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(B_P_FULL + t));
             }
-            l += sum.x + sum.y;
-            tc_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_full + 8 * t);
-        }
-        // ---- the row's result
-        if (alive && tiles > 0) alive = mbar_wait(o_full + 8 * t, 0, abort, p.wait_cycles);
-        if (alive && n_tok > 0) {
+            // ---- the row's result
+            if (alive && end > begin) alive = mbar_wait(bar(B_O_FULL + t), results++ & 1u, abort, p.wait_cycles);
+            if (!alive) break;
             tc_fence_after();
+            bool some = end > begin;                // there is an O of this group
+            bool other_some = false;
+            float f = 1.f, f_other = 0.f;
+            if (plan.pair) {
+                // tile A's rows twice, with every second K/V tile each: group A takes both, out of the same lanes of tensor memory
+                if (t == 1) {
+                    s_ml[r] = make_float2(mc, l);
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(B_HALF));
+                } else {
+                    if (!mbar_wait(bar(B_HALF), merges & 1u, abort, p.wait_cycles)) { alive = false; break; }
+                    tc_fence_after();
+                    const float2 ml = s_ml[r];
+                    other_some = plan.end(1) > plan.begin(1);
+                    const float top = fmaxf(mc, ml.x);
+                    f = pa_ex2(mc - top);
+                    f_other = pa_ex2(ml.x - top);
+                    l = l * f + ml.y * f_other;
+                    mc = top;
+                }
+            }
+            if (SPLIT) {                            // Q's and the ring's place is free when both groups have their O
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(B_ALL));
+                if (!mbar_wait(bar(B_ALL), 0, abort, p.wait_cycles)) { alive = false; break; }
+            }
             const bool none = l == 0.f;             // (a NaN among the sums has to come through)
             const float inv = none ? 0.f : 1.f / l;
-            const size_t row = static_cast<size_t>(me.q0 + i) * p.Hq + static_cast<size_t>(h) * p.G + g;
-            const bool odd = s_odd != 0;
+            const bool odd = s_odd[it & 1] != 0;
+            const size_t row = static_cast<size_t>(w.q0 + i) * p.Hq + static_cast<size_t>(w.h) * p.G + g;
+            if (!(plan.pair && t == 1)) {
 #pragma unroll 1
-            for (int x = 0; x < 4; ++x) {
-                float o[32];
-                if (tiles > 0) {
-                    tc_ld32(at_o + 32 * x, o);
-                    tc_wait_ld();
-                }
-                if (odd && real) {                  // what was taken out of the values: infinities and NaN that the row does see
-                    for (int k = odd_from * PA_ROWS; k < seen; ++k) {
-                        const uint32_t* v = reinterpret_cast<const uint32_t*>(static_cast<const T*>(p.v) + (me.k0 + k) * p.v_tok + h * p.v_head + 32 * x);
+                for (int x = 0; x < 4; ++x) {
+                    float o[32];
+                    if (some) {
+                        tc_ld32(at_o + 32 * x, o);
+                        tc_wait_ld();
+                    } else {
 #pragma unroll
-                        for (int y = 0; y < 16; ++y) {
-                            const uint32_t w = v[y], bad = not_finite<T>(w);
-                            if (bad & 0x8000u) o[2 * y] += Form<T>::value(w & 0xffffu);
-                            if (bad & 0x80000000u) o[2 * y + 1] += Form<T>::value(w >> 16);
+                        for (int y = 0; y < 32; ++y) o[y] = 0.f;
+                    }
+                    if (other_some) {
+                        float o2[32];
+                        tc_ld32(at_o + 128 + 32 * x, o2);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int y = 0; y < 32; ++y) o[y] = o[y] * f + o2[y] * f_other;
+                    }
+                    if (!real) continue;
+                    if (odd) {                      // what was taken out of the values: infinities and NaN that the row does see
+                        for (int k = max(plan.odd_from, plan.lo) * PA_ROWS; k < min(seen, plan.hi * PA_ROWS); ++k) {
+                            const uint32_t* v = reinterpret_cast<const uint32_t*>(static_cast<const T*>(p.v) + (w.k0 + k) * p.v_tok + w.h * p.v_head + 32 * x);
+#pragma unroll
+                            for (int y = 0; y < 16; ++y) {
+                                const uint32_t u = v[y], bad = not_finite<T>(u);
+                                if (bad & 0x8000u) o[2 * y] += Form<T>::value(u & 0xffffu);
+                                if (bad & 0x80000000u) o[2 * y + 1] += Form<T>::value(u >> 16);
+                            }
+                        }
+                    }
+                    if (SPLIT) {                    // the CTA's share of the row, in 32 bits, where the cluster finds it (the ring is done with)
+                        const uint32_t at = smem + static_cast<uint32_t>(128 * t + r) * 512u;
+#pragma unroll
+                        for (int y = 0; y < 8; ++y)
+                            asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(at + (((8 * x + y) ^ (r & 31)) << 4)), "f"(o[4 * y]), "f"(o[4 * y + 1]), "f"(o[4 * y + 2]), "f"(o[4 * y + 3]) : "memory");
+                    } else {
+                        uint4* to = reinterpret_cast<uint4*>(static_cast<T*>(p.out) + row * PI_HEAD_DIM + 32 * x);
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            uint32_t u[4];
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) u[z] = none ? 0u : Form<T>::pack(o[8 * y + 2 * z] * inv, o[8 * y + 2 * z + 1] * inv);
+                            to[y] = make_uint4(u[0], u[1], u[2], u[3]);
                         }
                     }
                 }
-                if (!real) continue;
-                uint4* to = reinterpret_cast<uint4*>(static_cast<T*>(p.out) + row * PI_HEAD_DIM + 32 * x);
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int z = 0; z < 4; ++z) w[z] = none ? 0u : Form<T>::pack(o[8 * y + 2 * z] * inv, o[8 * y + 2 * z + 1] * inv);
-                    to[y] = make_uint4(w[0], w[1], w[2], w[3]);
-                }
+                if (SPLIT) asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(smem + PA_ML_AT + static_cast<uint32_t>(128 * t + r) * 8u), "f"(mc), "f"(l) : "memory");
+                else if (real && p.lse) p.lse[row] = none ? -INFINITY : (mc + log2f(l)) * 0.6931471805599453f;
             }
-            if (real && p.lse) p.lse[row] = none ? -INFINITY : (mc + log2f(l)) * 0.6931471805599453f;
+            tc_fence_before();
+            if (plan.pair) {                        // B's O may be written anew when A has read it
+                __syncwarp();
+                if (t == 0) {
+                    if (lane == 0) mbar_arrive(bar(B_MERGED));
+                } else if (!mbar_wait(bar(B_MERGED), merges & 1u, abort, p.wait_cycles)) {
+                    alive = false;
+                    break;
+                }
+                ++merges;
+            }
+            done_with(it);
         }
-        tc_fence_before();
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PA_OTHER_REGS));
         if (warp == 9) {
-            // ---- TMA: K0 V0 K1 V1 ...; the whole warp waits, one lane issues.  Three loads behind, a V tile that some row must not
-            // see all of is looked through: rows behind the sequence's end become 0, and so does every value that is no number
-            // (its weight would be 0 where it is masked, and 0 times it is none); those are put back at the end, row by row.
-            const int loads = 2 * n_tiles;
-            auto look = [&](int n) -> bool {            // load n is in the ring: is it such a V tile?
-                const int j = n >> 1;
-                if (!(n & 1) || j < odd_from) return true;
-                if (!mbar_wait(kv_full + 8 * (n % PA_STAGES), (n / PA_STAGES) & 1, abort, p.wait_cycles)) return false;
-                const uint32_t tile = ring + (n % PA_STAGES) * PA_TILE;
-                const int real = me.m - j * PA_ROWS;    // rows of the sequence
-                bool odd = false;
-#pragma unroll 4
-                for (int i = lane; i < PA_TILE / 16; i += 32) {
-                    const int row = (i >> 3) & (PA_ROWS - 1);
-                    uint32_t w[4];
-                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(tile + i * 16));
-                    const uint32_t bad = not_finite<T>(w[0]) | not_finite<T>(w[1]) | not_finite<T>(w[2]) | not_finite<T>(w[3]);
-                    if (row >= real) w[0] = w[1] = w[2] = w[3] = 0u;
-                    else if (bad) {
-                        odd = true;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) w[k] &= ~((not_finite<T>(w[k]) >> 15) * 0xffffu);
-                    }
-                    if (row >= real || bad) asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(tile + i * 16), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-                }
-                if (odd) s_odd = 1;
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(v_good + 8 * (n % PA_STAGES));
-                return true;
-            };
-            if (n_tiles > 0 && lane == 0) {
-                const uint32_t bytes = static_cast<uint32_t>(p.tq) * p.G * 128u;
-                mbar_expect_tx(q_full, bytes * (n_b ? 4u : 2u));
-                for (int t = 0; t < (n_b ? 2 : 1); ++t)
-                    for (int x = 0; x < 2; ++x) tma_load_q(smem + t * PA_TILE + x * PA_HALF, &map_q, q_full, 64 * x, 0, h, me.q0 + first + t * p.tq);
-            }
-            int n = 0;
-            bool alive = true;
-            for (; n < loads && alive; ++n) {
-                const int stage = n % PA_STAGES;
-                if (n >= PA_STAGES && !mbar_wait(kv_empty + 8 * stage, (n / PA_STAGES - 1) & 1, abort, p.wait_cycles)) break;
+            // ---- TMA: Q, then K0 V0 K1 V1 ...
+            uint32_t n = 0u, items = 0u;            // loads, and items with any, so far
+            bool alive = true, q_issued = false;
+            Item w;
+            for (int it = 0; alive && item_of(it, w); ++it) {
+                const Plan plan(p, w, rank, split);
+                done_with(it);
+                if (plan.hi <= plan.lo) continue;
+                if (items && !mbar_wait(bar(B_Q_EMPTY), (items - 1) & 1u, abort, p.wait_cycles)) { alive = false; break; }
                 if (lane == 0) {
-                    const CUtensorMap* map = (n & 1) ? &map_v : &map_k;
-                    mbar_expect_tx(kv_full + 8 * stage, PA_TILE);
-                    for (int x = 0; x < 2; ++x) tma_load_3d(ring + stage * PA_TILE + x * PA_HALF, map, kv_full + 8 * stage, 64 * x, h, me.k0 + (n >> 1) * PA_ROWS);
+                    const uint32_t bytes = static_cast<uint32_t>(p.tq) * p.G * 128u;
+                    mbar_expect_tx(bar(B_Q_FULL), bytes * (plan.n_b ? 4u : 2u));
+                    for (int t = 0; t < (plan.n_b ? 2 : 1); ++t)
+                        for (int x = 0; x < 2; ++x) tma_load_q(smem + t * PA_TILE + x * PA_HALF, &map_q, bar(B_Q_FULL), 64 * x, 0, w.h, w.q0 + w.first + t * p.tq);
                 }
-                __syncwarp();
-                if (n >= 3) alive = look(n - 3);
+                q_issued = true;
+                ++items;
+                for (int i = 2 * plan.lo; i < 2 * plan.hi; ++i, ++n) {
+                    const uint32_t stage = n % PA_STAGES;
+                    if (n >= PA_STAGES && !mbar_wait(bar(B_KV_EMPTY + stage), (n / PA_STAGES - 1) & 1u, abort, p.wait_cycles)) { alive = false; break; }
+                    if (p.hold_last && i == 2 * plan.hi - 1) { alive = false; break; }
+                    if (lane == 0) {
+                        const CUtensorMap* map = (i & 1) ? &map_v : &map_k;
+                        mbar_expect_tx(bar(B_KV_FULL + stage), PA_TILE);
+                        for (int x = 0; x < 2; ++x) tma_load_3d(ring + stage * PA_TILE + x * PA_HALF, map, bar(B_KV_FULL + stage), 64 * x, w.h, w.k0 + (i >> 1) * PA_ROWS);
+                    }
+                    __syncwarp();
+                }
             }
-            for (int i = max(0, n - 3); i < n && alive; ++i) alive = look(i);
-            if (*abort) {                               // copies in flight end before the CTA does
+            if (!alive || *abort) {                 // copies in flight end before the CTA does
                 volatile int none = 0;
-                if (n_tiles > 0) mbar_wait(q_full, 0, &none, p.wait_cycles);
-                for (int i = max(0, n - PA_STAGES); i < n; ++i) mbar_wait(kv_full + 8 * (i % PA_STAGES), (i / PA_STAGES) & 1, &none, p.wait_cycles);
+                if (q_issued) mbar_wait(bar(B_Q_FULL), (items - 1) & 1u, &none, p.wait_cycles);
+                for (uint32_t i = n < PA_STAGES ? 0u : n - PA_STAGES; i < n; ++i) mbar_wait(bar(B_KV_FULL + i % PA_STAGES), (i / PA_STAGES) & 1u, &none, p.wait_cycles);
             }
         } else if (warp == 8) {
-            if (lane == 0 && n_tiles > 0) {
-                constexpr uint32_t base = (1u << 4) | (Form<T>::code << 7) | (Form<T>::code << 10) | (static_cast<uint32_t>(PA_ROWS >> 3) << 17) | (static_cast<uint32_t>(PA_ROWS >> 4) << 24);
-                constexpr uint32_t idesc_s = base, idesc_o = base | (1u << 16);      // V: channels run along its rows
-                auto product_s = [&](int t, int n) {
-                    const uint64_t a = desc_k_major(smem + t * PA_TILE), b = desc_k_major(ring + (n % PA_STAGES) * PA_TILE);
+            // ---- the products, by one lane
+            constexpr uint32_t base = (1u << 4) | (Form<T>::code << 7) | (Form<T>::code << 10) | (static_cast<uint32_t>(PA_ROWS >> 3) << 17) | (static_cast<uint32_t>(PA_ROWS >> 4) << 24);
+            constexpr uint32_t idesc_s = base, idesc_o = base | (1u << 16);      // V: channels run along its rows
+            uint32_t n0 = 0u, items = 0u, steps[2] = {0u, 0u}, good = 0u;       // good: bit = which phase of a stage's V_GOOD comes next
+            bool alive = true;
+            Item w;
+            for (int it = 0; alive && item_of(it, w); ++it) {
+                const Plan plan(p, w, rank, split);
+                done_with(it);
+                if (plan.hi <= plan.lo) continue;
+                auto product_s = [&](int t, int j) {
+                    const uint32_t n = n0 + 2 * (j - plan.lo);
+                    const uint64_t a = desc_k_major(smem + (plan.pair ? 0 : t) * PA_TILE), b = desc_k_major(ring + (n % PA_STAGES) * PA_TILE);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         const uint64_t step = static_cast<uint64_t>(((k >> 2) * PA_HALF + (k & 3) * 32) >> 4);
                         tc_mma_ss(tmem + PA_TMEM_S + 128 * t, a + step, b + step, idesc_s, k > 0);
                     }
-                    tc_commit(s_full + 8 * t);
+                    tc_commit(bar(B_S_FULL + t));
                 };
-                auto product_o = [&](int t, int n, bool add) {
+                auto product_o = [&](int t, uint32_t n, bool add) {
                     const uint64_t b = desc_mn_major(ring + (n % PA_STAGES) * PA_TILE);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) tc_mma_ts(tmem + PA_TMEM_O + 128 * t, tmem + PA_TMEM_S + 128 * t + 8 * k, b + static_cast<uint64_t>((k * 2048) >> 4), idesc_o, add || k > 0);
                 };
-                const int tiles[2] = {tiles_a, tiles_b};
-                bool alive = mbar_wait(q_full, 0, abort, p.wait_cycles) && mbar_wait(kv_full, 0, abort, p.wait_cycles);
-                if (alive) {
+                auto wait_k = [&](int j) {
+                    const uint32_t n = n0 + 2 * (j - plan.lo);
+                    return mbar_wait(bar(B_KV_FULL + n % PA_STAGES), (n / PA_STAGES) & 1u, abort, p.wait_cycles);
+                };
+                // all lanes wait, one issues
+                alive = mbar_wait(bar(B_Q_FULL), items++ & 1u, abort, p.wait_cycles);
+                const int step = plan.step();
+                for (int j = plan.lo; j < min(plan.lo + step, plan.hi) && alive; ++j) {
+                    alive = wait_k(j);
+                    if (!alive) break;
                     tc_fence_after();
-                    for (int t = 0; t < 2; ++t)
-                        if (tiles[t] > 0) product_s(t, 0);
-                    tc_commit(kv_empty);
+                    if (lane == 0) {
+                        for (int t = 0; t < 2; ++t)
+                            if (plan.pair ? t == j - plan.lo : j < plan.end(t)) product_s(t, j);
+                        tc_commit(bar(B_KV_EMPTY + (n0 + 2 * (j - plan.lo)) % PA_STAGES));
+                        if (j + 1 == plan.hi) tc_commit(bar(B_Q_EMPTY));
+                    }
+                    __syncwarp();
                 }
-                for (int j = 0; j < n_tiles && alive; ++j) {
-                    const int nv = 2 * j + 1, nk = 2 * j + 2;
-                    if (j < odd_from) alive = mbar_wait(kv_full + 8 * (nv % PA_STAGES), (nv / PA_STAGES) & 1, abort, p.wait_cycles);
-                    else alive = mbar_wait(v_good + 8 * (nv % PA_STAGES), ((j - odd_from) / PA_STAGES) & 1, abort, p.wait_cycles);     // (a V tile meets its stage again five tiles on)
-                    if (alive && j + 1 < n_tiles) alive = mbar_wait(kv_full + 8 * (nk % PA_STAGES), (nk / PA_STAGES) & 1, abort, p.wait_cycles);
+                for (int j = plan.lo; j < plan.hi && alive; ++j) {
+                    const uint32_t nv = n0 + 2 * (j - plan.lo) + 1, stage = nv % PA_STAGES;
+                    const int next = j + step;
+                    if (j < plan.odd_from) alive = mbar_wait(bar(B_KV_FULL + stage), (nv / PA_STAGES) & 1u, abort, p.wait_cycles);
+                    else {
+                        alive = mbar_wait(bar(B_V_GOOD + stage), (good >> stage) & 1u, abort, p.wait_cycles);
+                        good ^= 1u << stage;
+                    }
+                    if (alive && next < plan.hi) alive = wait_k(next);
                     for (int t = 0; t < 2 && alive; ++t) {
-                        if (j >= tiles[t]) continue;
-                        alive = mbar_wait(p_full + 8 * t, j & 1, abort, p.wait_cycles);
+                        if (plan.pair ? t != ((j - plan.lo) & 1) : j >= plan.end(t)) continue;
+                        alive = mbar_wait(bar(B_P_FULL + t), steps[t] & 1u, abort, p.wait_cycles);
+                        ++steps[t];
                         if (!alive) break;
                         tc_fence_after();
-                        product_o(t, nv, j > 0);
-                        if (j + 1 < tiles[t]) product_s(t, nk);
-                        else tc_commit(o_full + 8 * t);
+                        if (lane == 0) {
+                            product_o(t, nv, j >= plan.lo + step);
+                            if (next < plan.end(t)) product_s(t, next);
+                            else tc_commit(bar(B_O_FULL + t));
+                        }
+                        __syncwarp();
                     }
                     if (!alive) break;
-                    tc_commit(kv_empty + 8 * (nv % PA_STAGES));
-                    if (j + 1 < n_tiles) tc_commit(kv_empty + 8 * (nk % PA_STAGES));
+                    if (lane == 0) {
+                        tc_commit(bar(B_KV_EMPTY + stage));
+                        if (next < plan.hi) tc_commit(bar(B_KV_EMPTY + (nv - 1 + 2 * step) % PA_STAGES));
+                        if (next + 1 == plan.hi) tc_commit(bar(B_Q_EMPTY));
+                    }
+                    __syncwarp();
                 }
-                // products in flight end before the CTA does
-                volatile int none = 0;
-                tc_commit(drained);
-                mbar_wait(drained, 0, &none, p.wait_cycles);
+                n0 += 2 * (plan.hi - plan.lo);
+            }
+            // products in flight end before the CTA does
+            volatile int none = 0;
+            if (lane == 0) {
+                tc_commit(bar(B_DRAINED));
+                mbar_wait(bar(B_DRAINED), 0, &none, p.wait_cycles);
             }
             __syncwarp();
+        } else if (warp == 11) {
+            // ---- a V tile that some row must not see all of is looked through: rows behind the sequence's end become 0, and so does every
+            // value that is no number (its weight would be 0 where it is masked, and 0 times it is none); those are put back at the
+            // end, row by row
+            uint32_t n = 0u;
+            bool alive = true;
+            Item w;
+            for (int it = 0; alive && item_of(it, w); ++it) {
+                const Plan plan(p, w, rank, split);
+                bool odd = false;
+                for (int i = 2 * plan.lo; i < 2 * plan.hi; ++i, ++n) {         // (every load is waited for: a phase is told from the one before the last by the order alone)
+                    const uint32_t stage = n % PA_STAGES, tile = ring + stage * PA_TILE;
+                    if (!mbar_wait(bar(B_KV_FULL + stage), (n / PA_STAGES) & 1u, abort, p.wait_cycles)) { alive = false; break; }
+                    const int j = i >> 1;
+                    if (!(i & 1) || j < plan.odd_from) continue;
+                    const int rows = w.m - j * PA_ROWS;              // of the sequence
+#pragma unroll 8
+                    for (int x = lane; x < PA_TILE / 16; x += 32) {
+                        const int row = (x >> 3) & (PA_ROWS - 1);
+                        uint32_t u[4];
+                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]) : "r"(tile + x * 16));
+                        const uint32_t bad = not_finite<T>(u[0]) | not_finite<T>(u[1]) | not_finite<T>(u[2]) | not_finite<T>(u[3]);
+                        if (row < rows && !bad) continue;
+                        odd |= row < rows;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) u[k] = row < rows ? u[k] & ~((not_finite<T>(u[k]) >> 15) * 0xffffu) : 0u;
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(tile + x * 16), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]) : "memory");
+                    }
+                    if (odd) s_odd[it & 1] = 1;
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(B_V_GOOD + stage));
+                }
+                done_with(it);
+            }
+        } else {
+            // ---- warp 10: which items are this CTA's.  Blocks are counted from the last one of the last sequence, so that the longest of a
+            // sequence come first; KV heads innermost.
+            const int per_block = 2 * p.tq;
+            const Span mine = span_of(p, lane, blockIdx.x == 0);
+            int total = (mine.n + per_block - 1) / per_block;
+            for (int s0 = 32; s0 < p.n_seqs; s0 += 32) total += (span_of(p, s0 + lane, blockIdx.x == 0).n + per_block - 1) / per_block;
+            total = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(total)));
+            unsigned place = blockIdx.x / static_cast<unsigned>(split);
+            uint32_t asked = 0u;
+            bool more = true;
+            for (int it = 0;; ++it) {
+                Item w = {0, 0, 0, 0, 0, -1};
+                const int item = static_cast<int>(place / static_cast<unsigned>(p.Hkv));
+                const bool has = more && item < total;
+                if (has) {
+                    int at = total - 1 - item;
+                    for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
+                        const Span x = s0 ? span_of(p, s0 + lane, false) : mine;
+                        const int nb = (x.n + per_block - 1) / per_block;
+                        int upto = nb;
+#pragma unroll
+                        for (int d = 1; d < 32; d <<= 1) {
+                            const int y = __shfl_up_sync(0xffffffffu, upto, d);
+                            if (lane >= d) upto += y;
+                        }
+                        const unsigned found = __ballot_sync(0xffffffffu, at < upto);
+                        if (found) {
+                            const int from = __ffs(static_cast<int>(found)) - 1;
+                            w.first = (at - __shfl_sync(0xffffffffu, upto - nb, from)) * per_block;
+                            w.q0 = __shfl_sync(0xffffffffu, x.q0, from); w.n = __shfl_sync(0xffffffffu, x.n, from);
+                            w.k0 = __shfl_sync(0xffffffffu, x.k0, from); w.m = __shfl_sync(0xffffffffu, x.m, from);
+                            w.h = static_cast<int>(place % static_cast<unsigned>(p.Hkv));
+                            break;
+                        }
+                        at -= __shfl_sync(0xffffffffu, upto, 31);
+                    }
+                }
+                if (it >= 2 && !mbar_wait(bar(B_ITEM_EMPTY + (it & 1)), ((it >> 1) - 1) & 1, abort, p.wait_cycles)) break;
+                if (lane == 0) {
+                    s_item[it & 1] = w;
+                    s_odd[it & 1] = 0;
+                    mbar_arrive(bar(B_ITEM_FULL + (it & 1)));
+                }
+                __syncwarp();
+                if (!has) break;
+                if (SPLIT) { more = false; continue; }
+                // a CTA that has not begun gives its place up, if there is one (a place behind the last item too, and then the next)
+                uint32_t got = 0u;
+                do {
+                    if (lane == 0) {
+                        mbar_expect_tx(bar(B_NEXT), 16);
+                        asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_u32(s_next)), "r"(bar(B_NEXT)) : "memory");
+                    }
+                    __syncwarp();
+                    volatile int none = 0;          // (the answer is written into this CTA's memory, so it is waited for in any case)
+                    if (!mbar_wait(bar(B_NEXT), asked++ & 1u, &none, p.wait_cycles)) { *abort = 1; got = 0u; break; }
+                    asm volatile(
+                        "{\n .reg .b128 r;\n .reg .pred c;\n ld.shared.b128 r, [%2];\n clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 c, r;\n selp.u32 %0, 1, 0, c;\n mov.u32 %1, 0;\n"
+                        " @c clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n}"
+                        : "=r"(got), "=r"(place) : "r"(smem_u32(s_next)) : "memory");
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // (read before the next answer is written)
+                    __syncwarp();
+                } while (got && static_cast<int>(place / static_cast<unsigned>(p.Hkv)) >= total);
+                more = got != 0u;
+            }
         }
     }
+    __syncwarp();
     __syncthreads();
+    if (SPLIT) {
+        // ---- the cluster's shares of every row into one: rank r concludes every `split`-th row; four channels a thread
+        cluster_sync_all();
+        const Item w = s_item[0];
+        if (w.h >= 0 && !s_abort) {
+            const Plan plan(p, w, rank, split);
+            const int rows = plan.pair ? PA_ROWS : 2 * PA_ROWS;
+            for (int x = tid; x < rows / split * 32; x += PA_THREADS) {
+                const int rr = (x >> 5) * split + rank, quad = x & 31, t = rr >> 7, r = rr & 127, tok = r / p.G, g = r - tok * p.G;
+                if (tok >= (t ? plan.n_b : plan.n_a)) continue;
+                float2 ml[PA_MAX_SPLIT];
+                float4 v[PA_MAX_SPLIT];
+#pragma unroll
+                for (int k = 0; k < PA_MAX_SPLIT; ++k)
+                    if (k < split) {
+                        const uint32_t at = map_shared_rank(smem + PA_ML_AT + static_cast<uint32_t>(rr) * 8u, k);
+                        ml[k] = make_float2(ld_cluster(at), ld_cluster(at + 4));
+                        v[k] = ld_cluster4(map_shared_rank(smem + static_cast<uint32_t>(rr) * 512u + ((quad ^ (r & 31)) << 4), k));
+                    }
+                float top = PA_NO_MAX, l = 0.f;
+                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int k = 0; k < PA_MAX_SPLIT; ++k)
+                    if (k < split) top = fmaxf(top, ml[k].x);
+#pragma unroll
+                for (int k = 0; k < PA_MAX_SPLIT; ++k)
+                    if (k < split) {
+                        const float f = pa_ex2(ml[k].x - top);
+                        l = fmaf(ml[k].y, f, l);
+                        o.x = fmaf(v[k].x, f, o.x); o.y = fmaf(v[k].y, f, o.y); o.z = fmaf(v[k].z, f, o.z); o.w = fmaf(v[k].w, f, o.w);
+                    }
+                const bool none = l == 0.f;
+                const float inv = none ? 0.f : 1.f / l;
+                const size_t row = static_cast<size_t>(w.q0 + w.first + t * p.tq + tok) * p.Hq + static_cast<size_t>(w.h) * p.G + g;
+                *reinterpret_cast<uint2*>(static_cast<T*>(p.out) + row * PI_HEAD_DIM + 4 * quad) =
+                    none ? make_uint2(0u, 0u) : make_uint2(Form<T>::pack(o.x * inv, o.y * inv), Form<T>::pack(o.z * inv, o.w * inv));
+                if (p.lse && quad == 0) p.lse[row] = none ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
+            }
+        }
+        cluster_sync_all();                         // no CTA ends while another reads its share
+    }
     if (warp == 8) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
     }
-    if (tid == 0 && s_abort) pi_report(p.st, PI_ERR_TIMEOUT, PI_STAGE_PROMPT, static_cast<int>(blockIdx.x), block, n_tiles);
+    if (tid == 0 && s_abort) pi_report(p.st, PI_ERR_TIMEOUT, PI_STAGE_PROMPT, static_cast<int>(blockIdx.x), s_item[0].first, s_item[0].h);
 }
 
 typedef CUresult (*encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
@@ -518,13 +765,33 @@ int pi_launch_prompt_attn(pi_ctx* c, int n_seqs, int dtype, int n_q, int n_k, co
         const int rc = make_map(c, i ? &map_v : &map_k, type, 3, n_k ? (i ? v : k) : q, dims, strides, box);
         if (rc != PI_OK) return rc;
     }
-    const long long blocks = n_q / (2 * p.tq) + static_cast<long long>(n_seqs < n_q ? n_seqs : n_q), grid = blocks * p.Hkv;
+    p.hold_last = cfg.test_hold_producer;
+    const long long blocks = n_q / (2 * p.tq) + static_cast<long long>(n_seqs < n_q ? n_seqs : n_q), items = blocks * p.Hkv;
+    int split = 1;
+    const char* e = getenv("PA_SPLIT");
+    if (e) split = atoi(e);
+    const long long grid = items * split;
     if (grid > INT32_MAX) return PI_ERR_UNSUPPORTED_DIM;
     const size_t smem = 2 * PA_TILE + PA_STAGES * PA_TILE + 1024;
     auto launch = [&](auto kernel) -> int {
         PI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
-        PI_CUDA_TRY(pi_launch_pdl(kernel, dim3(static_cast<unsigned>(grid)), dim3(PA_THREADS), smem, stream, map_q, map_k, map_v, p));
+        cudaLaunchConfig_t lc = {};
+        lc.gridDim = dim3(static_cast<unsigned>(grid));
+        lc.blockDim = dim3(PA_THREADS);
+        lc.dynamicSmemBytes = smem;
+        lc.stream = stream;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = split;
+        attr[1].val.clusterDim.y = 1;
+        attr[1].val.clusterDim.z = 1;
+        lc.attrs = attr;
+        lc.numAttrs = split > 1 ? 2 : 1;
+        PI_CUDA_TRY(cudaLaunchKernelEx(&lc, kernel, map_q, map_k, map_v, p));
         return PI_OK;
     };
-    return dtype == PI_DTYPE_BF16 ? launch(prompt_attn_kernel<__nv_bfloat16>) : launch(prompt_attn_kernel<__half>);
+    if (dtype == PI_DTYPE_BF16) return split > 1 ? launch(prompt_attn_kernel<__nv_bfloat16, true>) : launch(prompt_attn_kernel<__nv_bfloat16, false>);
+    return split > 1 ? launch(prompt_attn_kernel<__half, true>) : launch(prompt_attn_kernel<__half, false>);
 }
