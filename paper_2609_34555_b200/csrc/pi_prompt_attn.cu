@@ -26,8 +26,8 @@ namespace {
 using namespace pi_attn;
 
 constexpr int PA_THREADS = 384;                  // three warpgroups: softmax of A, softmax of B, the rest (two of its warps have nothing to do)
-// registers of a softmax thread and of the others: 256 x 208 + 128 x 80 of the 384 x 168 that the block is launched with
-constexpr int PA_SOFTMAX_REGS = 208, PA_OTHER_REGS = 80;
+// registers of a softmax thread and of the others: 256 x 200 + 128 x 104 of the 384 x 168 that the block is launched with
+constexpr int PA_SOFTMAX_REGS = 200, PA_OTHER_REGS = 104;
 static_assert(256 * PA_SOFTMAX_REGS + 128 * PA_OTHER_REGS <= PA_THREADS * 168, "more than the block has");
 constexpr int PA_ROWS = 128;                        // rows of a query tile, and tokens of a K or V tile
 constexpr int PA_STAGES = 5;
@@ -75,6 +75,11 @@ __device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, ui
     asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
                  ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(add ? 1u : 0u) : "memory");
 }
+__device__ __forceinline__ bool elect_one() {
+    uint32_t one;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(one));
+    return one != 0u;
+}
 // 32 columns of this warp's 32 lanes
 __device__ __forceinline__ void tc_ld32(uint32_t addr, float* r) {
     uint32_t* u = reinterpret_cast<uint32_t*>(r);
@@ -94,6 +99,13 @@ __device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t* u) {
         : "memory");
 }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// (nothing that is made of what a load brings may be moved in front of the wait)
+template <int N>
+__device__ __forceinline__ void tc_wait_ld(float (&r)[N]) {
+    tc_wait_ld();
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+f"(r[i]));
+}
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float pa_ex2(float x) {
     float y;
@@ -175,7 +187,7 @@ struct Item {
 
 // What follows from an item, for every role alike.
 struct Plan {
-    int off, n_a, n_b, lo, hi, tiles_a, tiles_b, odd_from;
+    int off, n_a, n_b, lo, hi, tiles_a, tiles_b, seen_first, odd_from;
     bool pair;
     __device__ __forceinline__ Plan(const PromptParams& p, const Item& w, int rank, int split) {
         off = w.m - w.n;                            // token i sees the keys j < i + off + 1
@@ -190,7 +202,8 @@ struct Plan {
         hi = static_cast<int>(static_cast<long long>(all) * (rank + 1) / split);
         tiles_a = min(tiles_a, hi);
         tiles_b = min(tiles_b, hi);
-        odd_from = seen(w, w.first) / PA_ROWS;      // from this tile on, some row of the block does not see all of a tile
+        seen_first = seen(w, w.first);
+        odd_from = seen_first / PA_ROWS;            // from this tile on, some row of the block does not see all of a tile
     }
     __device__ __forceinline__ int seen(const Item& w, int i) const { return min(max(i + off + 1, 0), w.m); }
     // group t's first K/V tile, and how far it is to the next
@@ -199,7 +212,11 @@ struct Plan {
     __device__ __forceinline__ int end(int t) const { return t ? tiles_b : tiles_a; }
 };
 
-__device__ __forceinline__ float ld_cluster(uint32_t addr) { return ld_shared_cluster_f32(addr); }
+__device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+    return v;
+}
 __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
     float4 v;
     asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
@@ -289,7 +306,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 float s[128];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) tc_ld32(at_s + 32 * x, s + 32 * x);
-                tc_wait_ld();
+                tc_wait_ld(s);
                 if ((j + 1) * PA_ROWS > all_see) {
                     const int left = seen - j * PA_ROWS;
 #pragma unroll
@@ -316,7 +333,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         for (int x = 0; x < 4; ++x) {
                             float o[32];
                             tc_ld32(at_o + 32 * x, o);
-                            tc_wait_ld();
+                            tc_wait_ld(o);
 #pragma unroll
                             for (int y = 0; y < 32; ++y) o[y] *= alpha;
                             tc_st32(at_o + 32 * x, reinterpret_cast<const uint32_t*>(o));
@@ -395,7 +412,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     float o[32];
                     if (some) {
                         tc_ld32(at_o + 32 * x, o);
-                        tc_wait_ld();
+                        tc_wait_ld(o);
                     } else {
 #pragma unroll
                         for (int y = 0; y < 32; ++y) o[y] = 0.f;
@@ -403,13 +420,13 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     if (other_some) {
                         float o2[32];
                         tc_ld32(at_o + 128 + 32 * x, o2);
-                        tc_wait_ld();
+                        tc_wait_ld(o2);
 #pragma unroll
                         for (int y = 0; y < 32; ++y) o[y] = o[y] * f + o2[y] * f_other;
                     }
                     if (!real) continue;
                     if (odd) {                      // what was taken out of the values: infinities and NaN that the row does see
-                        for (int k = max(plan.odd_from, plan.lo) * PA_ROWS; k < min(seen, plan.hi * PA_ROWS); ++k) {
+                        for (int k = max(plan.seen_first, plan.lo * PA_ROWS); k < min(seen, plan.hi * PA_ROWS); ++k) {
                             const uint32_t* v = reinterpret_cast<const uint32_t*>(static_cast<const T*>(p.v) + (w.k0 + k) * p.v_tok + w.h * p.v_head + 32 * x);
 #pragma unroll
                             for (int y = 0; y < 16; ++y) {
@@ -489,88 +506,118 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 for (uint32_t i = n < PA_STAGES ? 0u : n - PA_STAGES; i < n; ++i) mbar_wait(bar(B_KV_FULL + i % PA_STAGES), (i / PA_STAGES) & 1u, &none, p.wait_cycles);
             }
         } else if (warp == 8) {
-            // ---- the products, by one lane
+            // ---- the products.  One lane issues them, but everything they are made of is kept the same in all lanes, and plainly so (values from
+            // lane 0, votes): their operands are uniform registers, and moving each of them there took longer than the products
+            // themselves (8192 tokens 520 us instead of 433).
             constexpr uint32_t base = (1u << 4) | (Form<T>::code << 7) | (Form<T>::code << 10) | (static_cast<uint32_t>(PA_ROWS >> 3) << 17) | (static_cast<uint32_t>(PA_ROWS >> 4) << 24);
             constexpr uint32_t idesc_s = base, idesc_o = base | (1u << 16);      // V: channels run along its rows
-            uint32_t n0 = 0u, items = 0u, steps[2] = {0u, 0u}, good = 0u;       // good: bit = which phase of a stage's V_GOOD comes next
+            const uint32_t utmem = __shfl_sync(0xffffffffu, tmem, 0), usmem = __shfl_sync(0xffffffffu, smem, 0), uring = usmem + 2 * PA_TILE;
+            uint32_t n0 = 0u, items = 0u, steps0 = 0u, steps1 = 0u, good = 0u;  // good: bit = which phase of a stage's V_GOOD comes next
             bool alive = true;
             Item w;
-            for (int it = 0; alive && item_of(it, w); ++it) {
+            auto wait = [&](uint32_t place, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar(place), parity, abort, p.wait_cycles)) != 0; };
+            auto full = [&](uint32_t n) { return wait(B_KV_FULL + n % PA_STAGES, (n / PA_STAGES) & 1u); };
+            for (int it = 0; alive && __all_sync(0xffffffffu, item_of(it, w)); ++it) {
+                w.q0 = __shfl_sync(0xffffffffu, w.q0, 0); w.n = __shfl_sync(0xffffffffu, w.n, 0);
+                w.k0 = __shfl_sync(0xffffffffu, w.k0, 0); w.m = __shfl_sync(0xffffffffu, w.m, 0);
+                w.first = __shfl_sync(0xffffffffu, w.first, 0); w.h = __shfl_sync(0xffffffffu, w.h, 0);
                 const Plan plan(p, w, rank, split);
                 done_with(it);
                 if (plan.hi <= plan.lo) continue;
-                auto product_s = [&](int t, int j) {
-                    const uint32_t n = n0 + 2 * (j - plan.lo);
-                    const uint64_t a = desc_k_major(smem + (plan.pair ? 0 : t) * PA_TILE), b = desc_k_major(ring + (n % PA_STAGES) * PA_TILE);
+                auto product_s = [&](int t, uint32_t n) {
+                    const uint64_t a = desc_k_major(usmem + (plan.pair ? 0 : t) * PA_TILE), b = desc_k_major(uring + (n % PA_STAGES) * PA_TILE);
+                    if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const uint64_t step = static_cast<uint64_t>(((k >> 2) * PA_HALF + (k & 3) * 32) >> 4);
-                        tc_mma_ss(tmem + PA_TMEM_S + 128 * t, a + step, b + step, idesc_s, k > 0);
+                        for (int k = 0; k < 8; ++k) {
+                            const uint64_t step = static_cast<uint64_t>(((k >> 2) * PA_HALF + (k & 3) * 32) >> 4);
+                            tc_mma_ss(utmem + PA_TMEM_S + 128 * t, a + step, b + step, idesc_s, k > 0);
+                        }
+                        tc_commit(bar(B_S_FULL + t));
                     }
-                    tc_commit(bar(B_S_FULL + t));
                 };
                 auto product_o = [&](int t, uint32_t n, bool add) {
-                    const uint64_t b = desc_mn_major(ring + (n % PA_STAGES) * PA_TILE);
+                    const uint64_t b = desc_mn_major(uring + (n % PA_STAGES) * PA_TILE);
+                    if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) tc_mma_ts(tmem + PA_TMEM_O + 128 * t, tmem + PA_TMEM_S + 128 * t + 8 * k, b + static_cast<uint64_t>((k * 2048) >> 4), idesc_o, add || k > 0);
+                        for (int k = 0; k < 8; ++k) tc_mma_ts(utmem + PA_TMEM_O + 128 * t, utmem + PA_TMEM_S + 128 * t + 8 * k, b + static_cast<uint64_t>((k * 2048) >> 4), idesc_o, add || k > 0);
+                    }
                 };
-                auto wait_k = [&](int j) {
-                    const uint32_t n = n0 + 2 * (j - plan.lo);
-                    return mbar_wait(bar(B_KV_FULL + n % PA_STAGES), (n / PA_STAGES) & 1u, abort, p.wait_cycles);
+                auto signal = [&](uint32_t place) {
+                    if (elect_one()) tc_commit(bar(place));
                 };
-                // all lanes wait, one issues
-                alive = mbar_wait(bar(B_Q_FULL), items++ & 1u, abort, p.wait_cycles);
-                const int step = plan.step();
-                for (int j = plan.lo; j < min(plan.lo + step, plan.hi) && alive; ++j) {
-                    alive = wait_k(j);
+                alive = wait(B_Q_FULL, items++ & 1u);
+                if (!alive) break;
+                const int count = plan.hi - plan.lo, step = plan.step();
+                // the first S of either group
+                alive = full(n0);
+                if (!alive) break;
+                tc_fence_after();
+                if (plan.pair || plan.lo < plan.tiles_a) product_s(0, n0);
+                if (!plan.pair && plan.lo < plan.tiles_b) product_s(1, n0);
+                signal(B_KV_EMPTY + n0 % PA_STAGES);
+                if (plan.pair && count > 1) {
+                    alive = full(n0 + 2);
                     if (!alive) break;
                     tc_fence_after();
-                    if (lane == 0) {
-                        for (int t = 0; t < 2; ++t)
-                            if (plan.pair ? t == j - plan.lo : j < plan.end(t)) product_s(t, j);
-                        tc_commit(bar(B_KV_EMPTY + (n0 + 2 * (j - plan.lo)) % PA_STAGES));
-                        if (j + 1 == plan.hi) tc_commit(bar(B_Q_EMPTY));
-                    }
-                    __syncwarp();
+                    product_s(1, n0 + 2);
+                    signal(B_KV_EMPTY + (n0 + 2) % PA_STAGES);
                 }
-                for (int j = plan.lo; j < plan.hi && alive; ++j) {
-                    const uint32_t nv = n0 + 2 * (j - plan.lo) + 1, stage = nv % PA_STAGES;
-                    const int next = j + step;
-                    if (j < plan.odd_from) alive = mbar_wait(bar(B_KV_FULL + stage), (nv / PA_STAGES) & 1u, abort, p.wait_cycles);
+                if (count <= step) signal(B_Q_EMPTY);
+                for (int x = 0; x < count; ++x) {
+                    const int j = plan.lo + x;
+                    const uint32_t nv = n0 + 2 * x + 1, nk = nv - 1 + 2 * step, stage = nv % PA_STAGES;
+                    const bool next = x + step < count;
+                    if (j < plan.odd_from) alive = full(nv);
                     else {
-                        alive = mbar_wait(bar(B_V_GOOD + stage), (good >> stage) & 1u, abort, p.wait_cycles);
+                        alive = wait(B_V_GOOD + stage, (good >> stage) & 1u);
                         good ^= 1u << stage;
                     }
-                    if (alive && next < plan.hi) alive = wait_k(next);
-                    for (int t = 0; t < 2 && alive; ++t) {
-                        if (plan.pair ? t != ((j - plan.lo) & 1) : j >= plan.end(t)) continue;
-                        alive = mbar_wait(bar(B_P_FULL + t), steps[t] & 1u, abort, p.wait_cycles);
-                        ++steps[t];
+                    if (!alive) break;
+                    if (plan.pair) {
+                        // the group's next K is two tiles on, and is waited for behind the product with V, which frees a place for the loads
+                        if (x & 1) alive = wait(B_P_FULL + 1, steps1++ & 1u);
+                        else alive = wait(B_P_FULL, steps0++ & 1u);
                         if (!alive) break;
                         tc_fence_after();
-                        if (lane == 0) {
-                            product_o(t, nv, j >= plan.lo + step);
-                            if (next < plan.end(t)) product_s(t, next);
-                            else tc_commit(bar(B_O_FULL + t));
+                        product_o(x & 1, nv, x >= 2);
+                        signal(B_KV_EMPTY + stage);
+                        if (next) {
+                            alive = full(nk);
+                            if (!alive) break;
+                            tc_fence_after();
+                            product_s(x & 1, nk);
+                            signal(B_KV_EMPTY + nk % PA_STAGES);
+                        } else signal(B_O_FULL + (x & 1));
+                    } else {
+                        if (next) alive = full(nk);
+                        if (!alive) break;
+                        if (j < plan.tiles_a) {
+                            alive = wait(B_P_FULL, steps0++ & 1u);
+                            if (!alive) break;
+                            tc_fence_after();
+                            product_o(0, nv, x > 0);
+                            if (j + 1 < plan.tiles_a) product_s(0, nk);
+                            else signal(B_O_FULL);
                         }
-                        __syncwarp();
+                        if (j < plan.tiles_b) {
+                            alive = wait(B_P_FULL + 1, steps1++ & 1u);
+                            if (!alive) break;
+                            tc_fence_after();
+                            product_o(1, nv, x > 0);
+                            if (j + 1 < plan.tiles_b) product_s(1, nk);
+                            else signal(B_O_FULL + 1);
+                        }
+                        signal(B_KV_EMPTY + stage);
+                        if (next) signal(B_KV_EMPTY + nk % PA_STAGES);
                     }
-                    if (!alive) break;
-                    if (lane == 0) {
-                        tc_commit(bar(B_KV_EMPTY + stage));
-                        if (next < plan.hi) tc_commit(bar(B_KV_EMPTY + (nv - 1 + 2 * step) % PA_STAGES));
-                        if (next + 1 == plan.hi) tc_commit(bar(B_Q_EMPTY));
-                    }
-                    __syncwarp();
+                    if (x + step + 1 == count) signal(B_Q_EMPTY);
                 }
-                n0 += 2 * (plan.hi - plan.lo);
+                n0 += 2 * count;
             }
             // products in flight end before the CTA does
             volatile int none = 0;
-            if (lane == 0) {
-                tc_commit(bar(B_DRAINED));
-                mbar_wait(bar(B_DRAINED), 0, &none, p.wait_cycles);
-            }
+            if (elect_one()) tc_commit(bar(B_DRAINED));
+            mbar_wait(bar(B_DRAINED), 0, &none, p.wait_cycles);
             __syncwarp();
         } else if (warp == 11) {
             // ---- a V tile that some row must not see all of is looked through: rows behind the sequence's end become 0, and so does every
@@ -587,18 +634,34 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     if (!mbar_wait(bar(B_KV_FULL + stage), (n / PA_STAGES) & 1u, abort, p.wait_cycles)) { alive = false; break; }
                     const int j = i >> 1;
                     if (!(i & 1) || j < plan.odd_from) continue;
-                    const int rows = w.m - j * PA_ROWS;              // of the sequence
-#pragma unroll 8
-                    for (int x = lane; x < PA_TILE / 16; x += 32) {
-                        const int row = (x >> 3) & (PA_ROWS - 1);
-                        uint32_t u[4];
-                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]) : "r"(tile + x * 16));
-                        const uint32_t bad = not_finite<T>(u[0]) | not_finite<T>(u[1]) | not_finite<T>(u[2]) | not_finite<T>(u[3]);
-                        if (row < rows && !bad) continue;
-                        odd |= row < rows;
+                    const int rows = min(w.m - j * PA_ROWS, PA_ROWS), from = max(plan.seen_first - j * PA_ROWS, 0);      // of the sequence; not seen by all
+                    for (int half = 0; half < 2; ++half) {
+                        const uint32_t at = tile + half * PA_HALF + lane * 16;
+#pragma unroll 4
+                        for (int x = rows * 128; x < PA_HALF; x += 512)
+                            if (x + lane * 16 < PA_HALF) asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(at + x), "r"(0u) : "memory");
+                        for (int x0 = from * 128; x0 < rows * 128; x0 += 8 * 512) {
+                            uint32_t u[8][4], most = 0u;     // the largest exponent and fraction, in either half of a word
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) u[k] = row < rows ? u[k] & ~((not_finite<T>(u[k]) >> 15) * 0xffffu) : 0u;
-                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(tile + x * 16), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]) : "memory");
+                            for (int k = 0; k < 8; ++k) {
+                                const int x = x0 + 512 * k;
+                                if (x + lane * 16 < rows * 128) asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(u[k][0]), "=r"(u[k][1]), "=r"(u[k][2]), "=r"(u[k][3]) : "r"(at + x));
+                                else u[k][0] = u[k][1] = u[k][2] = u[k][3] = 0u;
+                            }
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+#pragma unroll
+                                for (int y = 0; y < 4; ++y) most = __vmaxu2(most, u[k][y] & 0x7fff7fffu);
+                            if (!not_finite<T>(most)) continue;
+                            odd = true;
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                if (x0 + 512 * k + lane * 16 >= rows * 128) continue;
+#pragma unroll
+                                for (int y = 0; y < 4; ++y) u[k][y] &= ~((not_finite<T>(u[k][y]) >> 15) * 0xffffu);
+                                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at + x0 + 512 * k), "r"(u[k][0]), "r"(u[k][1]), "r"(u[k][2]), "r"(u[k][3]) : "memory");
+                            }
+                        }
                     }
                     if (odd) s_odd[it & 1] = 1;
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -684,36 +747,53 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         if (w.h >= 0 && !s_abort) {
             const Plan plan(p, w, rank, split);
             const int rows = plan.pair ? PA_ROWS : 2 * PA_ROWS;
-            for (int x = tid; x < rows / split * 32; x += PA_THREADS) {
-                const int rr = (x >> 5) * split + rank, quad = x & 31, t = rr >> 7, r = rr & 127, tok = r / p.G, g = r - tok * p.G;
-                if (tok >= (t ? plan.n_b : plan.n_a)) continue;
-                float2 ml[PA_MAX_SPLIT];
-                float4 v[PA_MAX_SPLIT];
+            // (four quads a round: what comes from the other CTAs takes about a microsecond)
+            constexpr int AT_ONCE = 4;
+            for (int x0 = tid; x0 < rows / split * 32; x0 += AT_ONCE * PA_THREADS) {
+                float4 o[AT_ONCE];
+                float top[AT_ONCE], l[AT_ONCE];
+                size_t row[AT_ONCE];
+                bool real[AT_ONCE];
 #pragma unroll
-                for (int k = 0; k < PA_MAX_SPLIT; ++k)
-                    if (k < split) {
-                        const uint32_t at = map_shared_rank(smem + PA_ML_AT + static_cast<uint32_t>(rr) * 8u, k);
-                        ml[k] = make_float2(ld_cluster(at), ld_cluster(at + 4));
-                        v[k] = ld_cluster4(map_shared_rank(smem + static_cast<uint32_t>(rr) * 512u + ((quad ^ (r & 31)) << 4), k));
+                for (int u = 0; u < AT_ONCE; ++u) {
+                    const int x = x0 + u * PA_THREADS, rr = (x >> 5) * split + rank, t = rr >> 7, r = rr & 127, tok = r / p.G, g = r - tok * p.G;
+                    real[u] = x < rows / split * 32 && tok < (t ? plan.n_b : plan.n_a);
+                    row[u] = static_cast<size_t>(w.q0 + w.first + t * p.tq + tok) * p.Hq + static_cast<size_t>(w.h) * p.G + g;
+                    o[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    top[u] = PA_NO_MAX;
+                    l[u] = 0.f;
+                }
+#pragma unroll 2
+                for (int k = 0; k < split; ++k) {
+                    float2 ml[AT_ONCE];
+                    float4 v[AT_ONCE];
+#pragma unroll
+                    for (int u = 0; u < AT_ONCE; ++u) {
+                        const int x = x0 + u * PA_THREADS, rr = (x >> 5) * split + rank;
+                        if (!real[u]) continue;
+                        ml[u] = ld_cluster2(map_shared_rank(smem + PA_ML_AT + static_cast<uint32_t>(rr) * 8u, k));
+                        v[u] = ld_cluster4(map_shared_rank(smem + static_cast<uint32_t>(rr) * 512u + (((x & 31) ^ (rr & 31)) << 4), k));
                     }
-                float top = PA_NO_MAX, l = 0.f;
-                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int k = 0; k < PA_MAX_SPLIT; ++k)
-                    if (k < split) top = fmaxf(top, ml[k].x);
-#pragma unroll
-                for (int k = 0; k < PA_MAX_SPLIT; ++k)
-                    if (k < split) {
-                        const float f = pa_ex2(ml[k].x - top);
-                        l = fmaf(ml[k].y, f, l);
-                        o.x = fmaf(v[k].x, f, o.x); o.y = fmaf(v[k].y, f, o.y); o.z = fmaf(v[k].z, f, o.z); o.w = fmaf(v[k].w, f, o.w);
+                    for (int u = 0; u < AT_ONCE; ++u) {
+                        if (!real[u]) continue;
+                        const float most = fmaxf(top[u], ml[u].x), f = pa_ex2(ml[u].x - most), was = pa_ex2(top[u] - most);
+                        l[u] = l[u] * was + ml[u].y * f;
+                        o[u].x = o[u].x * was + v[u].x * f; o[u].y = o[u].y * was + v[u].y * f;
+                        o[u].z = o[u].z * was + v[u].z * f; o[u].w = o[u].w * was + v[u].w * f;
+                        top[u] = most;
                     }
-                const bool none = l == 0.f;
-                const float inv = none ? 0.f : 1.f / l;
-                const size_t row = static_cast<size_t>(w.q0 + w.first + t * p.tq + tok) * p.Hq + static_cast<size_t>(w.h) * p.G + g;
-                *reinterpret_cast<uint2*>(static_cast<T*>(p.out) + row * PI_HEAD_DIM + 4 * quad) =
-                    none ? make_uint2(0u, 0u) : make_uint2(Form<T>::pack(o.x * inv, o.y * inv), Form<T>::pack(o.z * inv, o.w * inv));
-                if (p.lse && quad == 0) p.lse[row] = none ? -INFINITY : (top + log2f(l)) * 0.6931471805599453f;
+                }
+#pragma unroll
+                for (int u = 0; u < AT_ONCE; ++u) {
+                    if (!real[u]) continue;
+                    const int quad = (x0 + u * PA_THREADS) & 31;
+                    const bool none = l[u] == 0.f;
+                    const float inv = none ? 0.f : 1.f / l[u];
+                    *reinterpret_cast<uint2*>(static_cast<T*>(p.out) + row[u] * PI_HEAD_DIM + 4 * quad) =
+                        none ? make_uint2(0u, 0u) : make_uint2(Form<T>::pack(o[u].x * inv, o[u].y * inv), Form<T>::pack(o[u].z * inv, o[u].w * inv));
+                    if (p.lse && quad == 0) p.lse[row[u]] = none ? -INFINITY : (top[u] + log2f(l[u])) * 0.6931471805599453f;
+                }
             }
         }
         cluster_sync_all();                         // no CTA ends while another reads its share
