@@ -17,7 +17,6 @@
 // The maximum that is taken off moves only when a score exceeds it by a factor of 2^8 after the exponential, so that O is seldom
 // rescaled; then the softmax warps do it themselves, between their S and their P, when no product of their tile is in flight.
 #include <cuda_fp16.h>
-#include <cstdlib>
 
 #include "pi_attn_core.cuh"
 
@@ -846,28 +845,37 @@ int pi_launch_prompt_attn(pi_ctx* c, int n_seqs, int dtype, int n_q, int n_k, co
         if (rc != PI_OK) return rc;
     }
     p.hold_last = cfg.test_hold_producer;
-    const long long blocks = n_q / (2 * p.tq) + static_cast<long long>(n_seqs < n_q ? n_seqs : n_q), items = blocks * p.Hkv;
+    const long long per_block = 2 * p.tq, seqs = n_seqs < n_q ? n_seqs : n_q, blocks = (n_q + seqs * (per_block - 1)) / per_block, items = blocks * p.Hkv;
+    // CTAs that share an item: where the items leave SMs without work and the keys are many, a cluster for each, up to a power of two that fits the
+    // GPU once (and eight: fewer than eight clusters of 16 are resident at a time).  A cluster costs 3 to 5 us more than a CTA, and a K/V tile 1 to 2 us:
+    // 8 items of one token and 4 / 8 / 32 / 128 tiles take 9.9 / 13.6 / 36 / 130 us with 1 CTA each, 10.7 / 12.8 / 24 / 73 with 2,
+    // 9.8 / 11.0 / 17 / 42 with 4, 11.3 / 11.3 / 14.5 / 28 with 8.
+    // (How long each sequence is, only the kernel sees: the rule goes by the mean.)
+    const long long tiles = (n_k / seqs + PA_ROWS - 1) / PA_ROWS;
     int split = 1;
-    const char* e = getenv("PA_SPLIT");
-    if (e) split = atoi(e);
+    while (split < PA_MAX_SPLIT && items * split * 2 <= c->n_sms && tiles >= 4 * split && tiles >= 8) split *= 2;
+    // Items that leave less than half of the SMs without work, with keys for a long time: two each.  Sequences of like length take longer
+    // for it (16 of one token and 16 384 keys 199 us instead of 166), but one that is twice the mean would hold up the others (of 0 to
+    // 16 384 keys 126 us instead of 157).
+    if (split == 1 && items <= c->n_sms && per_block / 2 * seqs >= n_q && tiles >= 32) split = 2;
     const long long grid = items * split;
     if (grid > INT32_MAX) return PI_ERR_UNSUPPORTED_DIM;
     const size_t smem = 2 * PA_TILE + PA_STAGES * PA_TILE + 1024;
     auto launch = [&](auto kernel) -> int {
         PI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
         cudaLaunchConfig_t lc = {};
-        lc.gridDim = dim3(static_cast<unsigned>(grid));
+        lc.gridDim = dim3(static_cast<unsigned>(items * split));
         lc.blockDim = dim3(PA_THREADS);
         lc.dynamicSmemBytes = smem;
         lc.stream = stream;
         cudaLaunchAttribute attr[2];
-        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[0].val.programmaticStreamSerializationAllowed = 1;
-        attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = split;
-        attr[1].val.clusterDim.y = 1;
-        attr[1].val.clusterDim.z = 1;
-        lc.attrs = attr;
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = split;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
+        lc.attrs = split > 1 ? attr : attr + 1;
         lc.numAttrs = split > 1 ? 2 : 1;
         PI_CUDA_TRY(cudaLaunchKernelEx(&lc, kernel, map_q, map_k, map_v, p));
         return PI_OK;
