@@ -433,6 +433,52 @@ int pi_sparse_decode_attn_kv4(pi_ctx* ctx, int layer, int batch, const void* q_d
                               const int32_t* ctx_len_dev, void* out_dev, float* lse_dev, void* stream);
 
 /* ---------------------------------------------------------------------------------------------------
+ * The path on a cache in 8 bits.  (The paper keeps its cache in 16 bits; these calls exist for the library's users.)  Half of the bf16
+ * block's bytes cross the host link, and values are off by 2^-4 of their own size at most, however they differ between channels: for caches
+ * that 4 bits are too few for.  Used as the 4-bit calls are: score_select_diff -> pi_recall_kv8 -> pi_sparse_decode_attn_kv8,
+ * with pi_append_kv8 before them; pages from pi_assign_pages.  The context's device is current for the launch.
+ *
+ * 8-bit block: [Hkv][2 = K,V][B][D] e4m3 numbers (1 + 4 + 3 bits, no infinities), then [Hkv][2 = K,V] float scales, rounded up to a multiple of
+ * 128 bytes (pi_kv8_block_bytes; the padding is never read as data).  The value is scale * number.  All tokens of a block share the scale
+ * of their head and of K or V: 2^-7 of the power of two at or below the largest magnitude among them (infinities and NaN do not
+ * count), at least 2^-117.  Numbers are rounded to nearest, ties to even.  A token that joins a block keeps the block's scale where that
+ * is enough; where it is not, the scale grows, and the numbers of the block's other tokens are rounded again under it (exactly, but for
+ * those below 2^-13 of the new largest magnitude).  Storing a block's first token begins the block anew: its scales are of what is stored, and
+ * its other tokens become zero.  An infinite or NaN input reads back as NaN, and no other value does; magnitudes of 1.9375 * 2^127
+ * and more read back as infinite. */
+
+/* Bytes of an 8-bit block of this context's shape (> 0), or a negative PI_ERR_* code. */
+int64_t pi_kv8_block_bytes(pi_ctx* ctx);
+
+/* Tokens into 8-bit blocks; arguments, skipped tokens and errors as pi_kv4_store.  The tokens of one call that go to the same block stand
+ * one behind the other (as in the maps of pi_assign_pages), and no two of them name the same slot.  Bytes of blocks that no token
+ * goes to stay as they are. */
+int pi_kv8_store(pi_ctx* ctx, int64_t n_tokens, const void* k_dev, int64_t k_token_stride, int64_t k_head_stride,
+                 int64_t k_outer_stride, const void* v_dev, int64_t v_token_stride, int64_t v_head_stride,
+                 int64_t v_outer_stride, int64_t inner_tokens, const int64_t* slot_map_dev, void* store, int64_t n_blocks,
+                 void* stream);
+/* 8-bit blocks back to bf16 (the products are exact there); arguments and errors as pi_kv4_load. */
+int pi_kv8_load(pi_ctx* ctx, int64_t n_out, const void* store, int64_t n_blocks, const int32_t* blocks_dev, void* kv_dev, void* stream);
+
+/* pi_append_kv4 for pool and host store in 8 bits.  Where the token makes a scale grow, the host store's copy of that head's K or V is
+ * written anew from the pool's. */
+int pi_append_kv8(pi_ctx* ctx, int layer, int batch, uint32_t step, const uint32_t* step_dev, const void* k_new_dev,
+                  const void* v_new_dev, const int32_t* ctx_len_dev, void* host_kv8_pinned, int64_t host_seq_stride_bytes,
+                  const int32_t* page_table_dev, int64_t page_table_seq_stride, int32_t n_pages, void* pool8_dev,
+                  int32_t* block_table_dev, int32_t* slot_block_dev, uint32_t* slot_stamp_dev, void* digest_dev, void* stream);
+
+/* pi_recall_kv4 with an 8-bit block as the unit. */
+int pi_recall_kv8(pi_ctx* ctx, int layer, int batch, const void* host_kv8_pinned, int64_t host_seq_stride_bytes,
+                  const int32_t* page_table_dev, int64_t page_table_seq_stride, int32_t n_pages, void* pool8_dev,
+                  const pi_extent* recall_list_dev, int32_t list_capacity, const int32_t* recall_count_dev, void* stream);
+
+/* pi_sparse_decode_attn_kv4 over a pool of 8-bit blocks ([batch][C]): the same arguments, masks, empty sequences and errors.  Scores and
+ * sums are held in 32 bits: values below 2^100 stay within them for any list. */
+int pi_sparse_decode_attn_kv8(pi_ctx* ctx, int layer, int batch, const void* q_dev, const void* pool8_dev,
+                              const int32_t* sel_slots_dev, const int32_t* sel_blocks_dev, const int32_t* sel_count_dev,
+                              const int32_t* ctx_len_dev, void* out_dev, float* lse_dev, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------
  * Attention over whole prompts, or chunks of them: what stands before the path.  (The paper takes a request up when its prompt is
  * in the cache; this call exists for the library's users.)  A packed batch of sequences, one behind the other:
  * sequence s has the queries q_start[s] .. q_start[s + 1] - 1 and the keys k_start[s] .. k_start[s + 1] - 1, and with n queries and
@@ -481,7 +527,7 @@ int pi_middle_attention_mass(pi_ctx* ctx, int batch, const float* lse_mid_dev, c
 int pi_empty_launch(int n_ctas, int n_threads, void* stream);
 
 /* Sticky device status.  out[0] = first PI_ERR_* code seen by a kernel (0 = none),
- * out[1] = stage (1 score/select, 2 diff, 3 recall, 4 attention, 5 append, 6 4-bit store / load, 7 page assignment,
+ * out[1] = stage (1 score/select, 2 diff, 3 recall, 4 attention, 5 append, 6 4-bit or 8-bit store / load, 7 page assignment,
  * 8 prompt attention), out[2..4] = sequence
  * or list, position, offending value.  Reads a pinned mirror: call after the stream
  * has been synchronised.  pi_clear_status resets it. */

@@ -28,9 +28,10 @@ EXPORTS = ["pi_create", "pi_destroy", "pi_score_select", "pi_score_select_diff",
            "pi_recall_gather_scatter_paged", "pi_sparse_decode_attn", "pi_sparse_decode_attn_headwise", "pi_sparse_decode_attn_resident", "pi_sparse_decode_attn_recalled", "pi_attn_state_bytes", "pi_append_kv", "pi_append_kv_paged", "pi_append_kv_devstep", "pi_build_digests", "pi_build_digests_all", "pi_table_init", "pi_h2d_copy_ms", "pi_empty_launch", "pi_middle_attention_mass",
            "pi_get_status", "pi_get_stats", "pi_clear_status", "pi_strerror",
            "pi_kv4_block_bytes", "pi_assign_pages", "pi_qk_norm_rope", "pi_kv4_store", "pi_kv4_load", "pi_append_kv4", "pi_recall_kv4",
-           "pi_sparse_decode_attn_kv4", "pi_prompt_attn"]
+           "pi_sparse_decode_attn_kv4", "pi_prompt_attn",
+           "pi_kv8_block_bytes", "pi_kv8_store", "pi_kv8_load", "pi_append_kv8", "pi_recall_kv8", "pi_sparse_decode_attn_kv8"]
 FRONT_CALLS = ["pi_assign_pages", "pi_qk_norm_rope", "pi_kv4_store", "pi_kv4_load", "pi_append_kv4", "pi_recall_kv4", "pi_sparse_decode_attn_kv4",
-               "pi_prompt_attn"]
+               "pi_prompt_attn", "pi_kv8_store", "pi_kv8_load", "pi_append_kv8", "pi_recall_kv8", "pi_sparse_decode_attn_kv8"]
 
 
 class PiConfig(ctypes.Structure):
@@ -101,6 +102,9 @@ def load_library(rebuild: bool = False) -> ctypes.CDLL:
                                   i32p, u32p, vp, vp]
     lib.pi_recall_kv4.argtypes = [c_void_p, c_int, c_int, vp, c_int64, i32p, c_int64, c_int32, vp, vp, c_int32, i32p, vp]
     lib.pi_sparse_decode_attn_kv4.argtypes = [c_void_p, c_int, c_int, vp, vp, i32p, i32p, i32p, i32p, vp, vp, vp]
+    lib.pi_kv8_block_bytes.argtypes = [c_void_p]
+    for name in ("kv%d_store", "kv%d_load", "append_kv%d", "recall_kv%d", "sparse_decode_attn_kv%d"):
+        getattr(lib, "pi_" + name % 8).argtypes = getattr(lib, "pi_" + name % 4).argtypes
     lib.pi_prompt_attn.argtypes = [c_void_p, c_int, c_int, c_int64, vp, c_int64, c_int64, c_int64, vp, c_int64, c_int64, vp, c_int64, c_int64, i32p, i32p, vp, vp, vp]
     lib.pi_strerror.argtypes = [c_int]
     lib.pi_strerror.restype = c_char_p
@@ -109,6 +113,7 @@ def load_library(rebuild: bool = False) -> ctypes.CDLL:
             getattr(lib, name).restype = c_int
     lib.pi_attn_state_bytes.restype = c_int64
     lib.pi_kv4_block_bytes.restype = c_int64
+    lib.pi_kv8_block_bytes.restype = c_int64
     _lib = lib
     return lib
 
@@ -223,15 +228,15 @@ class PulseInfer:
             pass
 
     def _bf16_blocks(self, t, name: str, n: int, blocks: int, stride: Optional[int] = None, instead: str = "", unit: Optional[int] = None):
-        """Refuses 4-bit blocks where blocks of bf16 are addressed, which would lead out of the tensor: n runs of `blocks` of them, `stride`
+        """Refuses 4-bit or 8-bit blocks where blocks of bf16 are addressed, which would lead out of the tensor: n runs of `blocks` of them, `stride`
         bytes apart (None: one behind the other).  A byte view of bf16 blocks is as large as they are, and passes; one of units other
         than blocks may have rows of any length."""
         if t.dtype != torch.uint8 or n < 1:
             return
         size = blocks * self.block_bytes
         span = size + (n - 1) * (size if stride is None else stride)
-        if (unit in (None, 0, self.block_bytes) and t.dim() > 1 and t.shape[-1] == self.kv4_block_bytes) or (t.is_contiguous() and t.numel() < span):
-            raise TypeError(f"{name}: expected blocks of bf16, {span} bytes or more" + (f" (4-bit blocks: {instead})" if instead else ""))
+        if (unit in (None, 0, self.block_bytes) and t.dim() > 1 and t.shape[-1] in (self.kv4_block_bytes, self.kv8_block_bytes)) or (t.is_contiguous() and t.numel() < span):
+            raise TypeError(f"{name}: expected blocks of bf16, {span} bytes or more" + (f" (4-bit blocks: {instead}4, 8-bit blocks: {instead}8)" if instead else ""))
 
     # ------------------------------------------------------------------ the four path calls
     def score_select(self, layer: int, q, digest, ctx_len, sel_blocks, sel_count, scores=None, stream=None) -> None:
@@ -311,13 +316,13 @@ class PulseInfer:
         n_lists, cap = recall_list.shape[0], recall_list.shape[1]
         n_seq = -(-n_lists // max(1, lists_per_seq))
         ps = pool_seq_stride if pool_seq_stride is not None else pool.stride(0) * pool.element_size()
-        self._bf16_blocks(pool, "pool", n_seq, self.cfg.pool_slots, ps, "recall_kv4", unit_bytes)
+        self._bf16_blocks(pool, "pool", n_seq, self.cfg.pool_slots, ps, "recall_kv", unit_bytes)
         hs = host_seq_stride if host_seq_stride is not None else host_kv.stride(0) * host_kv.element_size()
         if page_table is None:
-            self._bf16_blocks(host_kv, "host_kv", n_seq, self.cfg.max_blocks, hs, "recall_kv4", unit_bytes)
+            self._bf16_blocks(host_kv, "host_kv", n_seq, self.cfg.max_blocks, hs, "recall_kv", unit_bytes)
         else:
             whole = unit_bytes in (None, 0, self.block_bytes) and unit_stride in (0, self.block_bytes)
-            self._bf16_blocks(host_kv, "host_kv", 1, (n_pages or 0) if whole else 0, None, "recall_kv4", unit_bytes)
+            self._bf16_blocks(host_kv, "host_kv", 1, (n_pages or 0) if whole else 0, None, "recall_kv", unit_bytes)
         if not host_kv.is_cuda and not host_kv.is_pinned():
             raise PiError("pi_recall_gather_scatter", -5, strerror(-5))
         if page_table is not None:
@@ -338,7 +343,7 @@ class PulseInfer:
         """headwise=True: sel_slots / sel_blocks are [batch][Hkv][K] (or [batch*Hkv][K]) and sel_count
         [batch][Hkv]: every KV head attends over its own selection."""
         batch = q.shape[0]
-        self._bf16_blocks(pool, "pool", batch, self.cfg.pool_slots, None, "sparse_decode_attn_kv4")
+        self._bf16_blocks(pool, "pool", batch, self.cfg.pool_slots, None, "sparse_decode_attn_kv")
         if not pool.is_cuda or not pool.is_contiguous():
             raise TypeError("pool: expected a contiguous CUDA tensor")
         fn = self._lib.pi_sparse_decode_attn_headwise if headwise else self._lib.pi_sparse_decode_attn
@@ -361,7 +366,7 @@ class PulseInfer:
         """First half of the attention split around the recall: the selected blocks the step's recall list
         does not touch; may run beside recall_gather_scatter.  Leaves its softmax state in `state`."""
         batch = q.shape[0]
-        self._bf16_blocks(pool, "pool", batch, self.cfg.pool_slots, None, "sparse_decode_attn_kv4")
+        self._bf16_blocks(pool, "pool", batch, self.cfg.pool_slots, None, "sparse_decode_attn_kv")
         if not pool.is_cuda or not pool.is_contiguous():
             raise TypeError("pool: expected a contiguous CUDA tensor")
         _check("pi_sparse_decode_attn_resident", self._lib.pi_sparse_decode_attn_resident(
@@ -376,7 +381,7 @@ class PulseInfer:
         """Second half: the blocks the recall brought in, merged with `state`; writes `out`.  The caller
         orders it after the first half and after the recall."""
         batch = q.shape[0]
-        self._bf16_blocks(pool, "pool", batch, self.cfg.pool_slots, None, "sparse_decode_attn_kv4")
+        self._bf16_blocks(pool, "pool", batch, self.cfg.pool_slots, None, "sparse_decode_attn_kv")
         if not pool.is_cuda or not pool.is_contiguous():
             raise TypeError("pool: expected a contiguous CUDA tensor")
         _check("pi_sparse_decode_attn_recalled", self._lib.pi_sparse_decode_attn_recalled(
@@ -394,12 +399,12 @@ class PulseInfer:
         sequence: pool slot, host store, running digest; ctx_len is the length before the append.
         With page_table the host tensor is an arena of block-sized pages (see recall_gather_scatter)."""
         batch = ctx_len.shape[0]
-        self._bf16_blocks(pool, "pool", batch, self.cfg.pool_slots, None, "append_kv4")
+        self._bf16_blocks(pool, "pool", batch, self.cfg.pool_slots, None, "append_kv")
         if page_table is None:
             hs = host_seq_stride if host_seq_stride is not None else host_kv.stride(0) * host_kv.element_size()
-            self._bf16_blocks(host_kv, "host_kv", batch, self.cfg.max_blocks, hs, "append_kv4")
+            self._bf16_blocks(host_kv, "host_kv", batch, self.cfg.max_blocks, hs, "append_kv")
         else:
-            self._bf16_blocks(host_kv, "host_kv", 1, n_pages or 0, None, "append_kv4")
+            self._bf16_blocks(host_kv, "host_kv", 1, n_pages or 0, None, "append_kv")
         if not host_kv.is_cuda and not host_kv.is_pinned():
             raise PiError("pi_append_kv", -5, strerror(-5))
         if isinstance(step, torch.Tensor):               # the step number lives on the device (graph replay)
@@ -444,7 +449,12 @@ class PulseInfer:
         self._front = load_front()
         self._index = self.device.index
         self._shape = self._front.shape(self._ctx.value or 0, self._index, c.n_q_heads, c.n_kv_heads, c.head_dim, c.block_tokens, c.pool_slots,
-                                        c.max_blocks, c.budget_blocks, self.kv4_block_bytes)
+                                        c.max_blocks, c.budget_blocks, self.kv4_block_bytes, self.kv8_block_bytes)
+
+    @property
+    def kv8_block_bytes(self) -> int:
+        """Bytes of one block in 8 bits."""
+        return self.cfg.n_kv_heads * self.cfg.block_tokens * 2 * self.cfg.head_dim + (self.cfg.n_kv_heads * 8 + 127) // 128 * 128
 
     def _stream4(self, stream) -> int:
         if stream is None:
@@ -495,6 +505,30 @@ class PulseInfer:
     def sparse_decode_attn_kv4(self, layer: int, q, pool4, sel_slots, sel_blocks, sel_count, ctx_len, out, lse=None, stream=None) -> None:
         """sparse_decode_attn over a pool of 4-bit blocks (uint8 [batch][C][kv4_block_bytes])."""
         _check("pi_sparse_decode_attn_kv4", self._front.sparse_decode_attn_kv4(self._shape, layer, q, pool4, sel_slots, sel_blocks, sel_count, ctx_len, out,
+                                                                               lse, self._stream4(stream)))
+
+    def kv8_store(self, k, v, store, slot_map=None, stream=None) -> None:
+        """kv4_store for blocks in 8 bits (uint8 [..., kv8_block_bytes]).  Tokens of one block, which share its scales, stand one behind the
+        other; a block's first token begins it anew."""
+        _check("pi_kv8_store", self._front.kv8_store(self._shape, k, v, store, slot_map, self._stream4(stream)))
+
+    def kv8_load(self, store, out, blocks=None, stream=None) -> None:
+        """Block blocks[i] (int32; None: i) of `store` as bf16 into out [n][Hkv][2][B][D]."""
+        _check("pi_kv8_load", self._front.kv8_load(self._shape, store, out, blocks, self._stream4(stream)))
+
+    def append_kv8(self, layer: int, step, k_new, v_new, ctx_len, host_kv8, pool8, block_table, slot_block, slot_stamp, digest,
+                   page_table=None, stream=None) -> None:
+        """append_kv for a pool and a host store in 8 bits.  step: a positive int, or a one-element int32 CUDA tensor."""
+        _check("pi_append_kv8", self._front.append_kv8(self._shape, layer, step, k_new, v_new, ctx_len, host_kv8, pool8, block_table, slot_block,
+                                                       slot_stamp, digest, page_table, self._stream4(stream)))
+
+    def recall_kv8(self, layer: int, host_kv8, pool8, recall_list, recall_count, page_table=None, stream=None) -> None:
+        """recall_gather_scatter with an 8-bit block as the unit."""
+        _check("pi_recall_kv8", self._front.recall_kv8(self._shape, layer, host_kv8, pool8, recall_list, recall_count, page_table, self._stream4(stream)))
+
+    def sparse_decode_attn_kv8(self, layer: int, q, pool8, sel_slots, sel_blocks, sel_count, ctx_len, out, lse=None, stream=None) -> None:
+        """sparse_decode_attn over a pool of 8-bit blocks (uint8 [batch][C][kv8_block_bytes])."""
+        _check("pi_sparse_decode_attn_kv8", self._front.sparse_decode_attn_kv8(self._shape, layer, q, pool8, sel_slots, sel_blocks, sel_count, ctx_len, out,
                                                                                lse, self._stream4(stream)))
 
     def prompt_attn(self, q, k, v, q_start, out, k_start=None, lse=None, stream=None) -> None:

@@ -18,7 +18,7 @@ LIB = PKG / "libpulseinfer_b200.so"
 
 SOURCES = ["pi_api.cu", "pi_score_select.cu", "pi_select_diff.cu", "pi_diff_misses.cu", "pi_recall.cu", "pi_attn.cu", "pi_attn_headmajor.cu",
            "pi_helpers.cu", "pi_append.cu", "pi_api_kv4.cu", "pi_kv4.cu", "pi_rope.cu", "pi_pages.cu", "pi_attn_kv4.cu",
-           "pi_api_prompt.cu", "pi_prompt_attn.cu"]
+           "pi_api_prompt.cu", "pi_prompt_attn.cu", "pi_api_kv8.cu", "pi_kv8.cu", "pi_append_kv8.cu", "pi_attn_kv8.cu"]
 
 
 def sources() -> list[Path]:

@@ -1,4 +1,5 @@
-// Checks of the tensors that the calls on the 4-bit path are given, and the calls themselves, for binding.py.
+// Checks of the tensors that the calls on the 4-bit and the 8-bit path and the attention over prompts are given, and the calls
+// themselves, for binding.py.
 //
 // The calls are small: a decode step's rotation or attention of one sequence keeps the GPU for a few microseconds, and the
 // same checks written in Python took longer than the launch.  This module does what binding._dev and the methods beside
@@ -24,12 +25,18 @@ struct Calls {
     decltype(&pi_recall_kv4) recall_kv4;
     decltype(&pi_sparse_decode_attn_kv4) sparse_decode_attn_kv4;
     decltype(&pi_prompt_attn) prompt_attn;
+    decltype(&pi_kv8_store) kv8_store;
+    decltype(&pi_kv8_load) kv8_load;
+    decltype(&pi_append_kv8) append_kv8;
+    decltype(&pi_recall_kv8) recall_kv8;
+    decltype(&pi_sparse_decode_attn_kv8) sparse_decode_attn_kv8;
 } g_calls;
 
 // What a context's calls look at: its address, device and shape.
 struct Shape {
     pi_ctx* ctx;
-    int64_t device, hq, hkv, d, b, slots, blocks, budget, block4;
+    int64_t device, hq, hkv, d, b, slots, blocks, budget, block4, block8;
+    template <int BITS> int64_t block() const { return BITS == 4 ? block4 : block8; }
 };
 
 struct Raised {};                                  // a Python error is set
@@ -100,35 +107,41 @@ T* table(const Shape& s, PyObject* o, at::ScalarType type, const char* name, int
 
 struct NotPinned {};                               // PI_ERR_NOT_PINNED, as the C call would say
 
-// A contiguous uint8 tensor [..., block4] of 4-bit blocks, on the device or (host) in pinned memory.
-const at::Tensor& blocks4(const Shape& s, PyObject* o, const char* name, bool host, int64_t* blocks) {
+// A contiguous uint8 tensor [..., bytes of a block] of 4-bit or 8-bit blocks, on the device or (host) in pinned memory.
+template <int BITS>
+const at::Tensor& small_blocks(const Shape& s, PyObject* o, const char* name, bool host, int64_t* blocks) {
     const at::Tensor& t = tensor(o, name);
-    if (t.scalar_type() != at::kByte || !t.is_contiguous() || t.dim() < 2 || t.size(-1) != s.block4)
-        refuse(PyExc_TypeError, std::string(name) + ": expected a contiguous uint8 tensor [..., " + std::to_string(s.block4) + "] of 4-bit blocks");
+    const int64_t bytes = s.block<BITS>();
+    if (t.scalar_type() != at::kByte || !t.is_contiguous() || t.dim() < 2 || t.size(-1) != bytes)
+        refuse(PyExc_TypeError, std::string(name) + ": expected a contiguous uint8 tensor [..., " + std::to_string(bytes) + "] of " + std::to_string(BITS) + "-bit blocks");
     if (t.is_cuda()) same_device(s, t, name);
     else if (!host) refuse(PyExc_TypeError, std::string(name) + ": expected a CUDA tensor");
     else if (!t.is_pinned()) throw NotPinned();
-    *blocks = t.numel() / s.block4;
+    *blocks = t.numel() / bytes;
     return t;
 }
 
-void* pool4(const Shape& s, PyObject* o, int64_t batch) {
+template <int BITS>
+void* small_pool(const Shape& s, PyObject* o, int64_t batch) {
     int64_t n = 0;
-    const at::Tensor& t = blocks4(s, o, "pool4", false, &n);
-    if (n < batch * s.slots) refuse(PyExc_ValueError, "pool4: expected [batch][" + std::to_string(s.slots) + "] blocks");
+    const char* name = BITS == 4 ? "pool4" : "pool8";
+    const at::Tensor& t = small_blocks<BITS>(s, o, name, false, &n);
+    if (n < batch * s.slots) refuse(PyExc_ValueError, std::string(name) + ": expected [batch][" + std::to_string(s.slots) + "] blocks");
     return t.data_ptr();
 }
 
-// A block-major or paged 4-bit store.
-struct Store4 {
+// A block-major or paged store of such blocks.
+struct SmallStore {
     void* base;
     int64_t stride, page_stride;
     const int32_t* pages;
     int32_t n_pages;
 };
-Store4 store4(const Shape& s, PyObject* store, PyObject* page_table, int64_t batch) {
+template <int BITS>
+SmallStore small_store(const Shape& s, PyObject* store, PyObject* page_table, int64_t batch) {
     int64_t n = 0;
-    Store4 r = {blocks4(s, store, "host_kv4", true, &n).data_ptr(), s.blocks * s.block4, 0, nullptr, 0};
+    const char* name = BITS == 4 ? "host_kv4" : "host_kv8";
+    SmallStore r = {small_blocks<BITS>(s, store, name, true, &n).data_ptr(), s.blocks * s.block<BITS>(), 0, nullptr, 0};
     if (page_table != Py_None) {
         const at::Tensor& t = on(s, page_table, at::kInt, "page_table");
         if (t.dim() != 2 || t.size(0) < batch) refuse(PyExc_ValueError, "page_table: expected [batch][blocks]");
@@ -137,7 +150,7 @@ Store4 store4(const Shape& s, PyObject* store, PyObject* page_table, int64_t bat
         r.pages = ptr<int32_t>(t);
         r.n_pages = static_cast<int32_t>(n < INT32_MAX ? n : INT32_MAX);
     } else if (n < batch * s.blocks) {
-        refuse(PyExc_ValueError, "host_kv4: expected [batch][" + std::to_string(s.blocks) + "] blocks");
+        refuse(PyExc_ValueError, std::string(name) + ": expected [batch][" + std::to_string(s.blocks) + "] blocks");
     }
     return r;
 }
@@ -230,7 +243,8 @@ int qk_norm_rope(const Shape& s, Args a) {
                                 on(s, a[4], at::kBFloat16, "q_out", {T, s.hq, s.d}).data_ptr(), on(s, a[5], at::kBFloat16, "k_out", {T, s.hkv, s.d}).data_ptr(), stream_of(a[10]));
 }
 
-int kv4_store(const Shape& s, Args a) {
+template <int BITS>
+int small_store_tokens(const Shape& s, Args a) {
     const at::Tensor &k = tensor(a[0], "k"), &v = tensor(a[1], "v");
     const int64_t dims = k.dim();
     if (dims != 3 && dims != 4) refuse(PyExc_ValueError, "k: expected [tokens][heads][channels] or [runs][tokens][heads][channels]");
@@ -251,20 +265,22 @@ int kv4_store(const Shape& s, Args a) {
     const int64_t n = dims == 4 ? k.size(0) * k.size(1) : k.size(0);
     const int64_t* slots = maybe<int64_t>(s, a[3], at::kLong, "slot_map", {n});
     int64_t blocks = 0;
-    void* store = blocks4(s, a[2], "store", true, &blocks).data_ptr();
-    return call(g_calls.kv4_store, s.ctx, n, k.data_ptr(), place[0][0], place[0][1], place[0][2], v.data_ptr(), place[1][0], place[1][1], place[1][2],
+    void* store = small_blocks<BITS>(s, a[2], "store", true, &blocks).data_ptr();
+    return call(BITS == 4 ? g_calls.kv4_store : g_calls.kv8_store, s.ctx, n, k.data_ptr(), place[0][0], place[0][1], place[0][2], v.data_ptr(), place[1][0], place[1][1], place[1][2],
                              dims == 4 ? k.size(1) : 0, slots, store, blocks, stream_of(a[4]));
 }
 
-int kv4_load(const Shape& s, Args a) {
+template <int BITS>
+int small_load(const Shape& s, Args a) {
     const at::Tensor* list = a[2] == Py_None ? nullptr : &on(s, a[2], at::kInt, "blocks");
     const at::Tensor& out = on(s, a[1], at::kBFloat16, "out", {list ? list->numel() : -1, s.hkv, 2, s.b, s.d});
     int64_t blocks = 0;
-    void* store = blocks4(s, a[0], "store", true, &blocks).data_ptr();
-    return call(g_calls.kv4_load, s.ctx, out.size(0), store, blocks, list ? ptr<int32_t>(*list) : nullptr, out.data_ptr(), stream_of(a[3]));
+    void* store = small_blocks<BITS>(s, a[0], "store", true, &blocks).data_ptr();
+    return call(BITS == 4 ? g_calls.kv4_load : g_calls.kv8_load, s.ctx, out.size(0), store, blocks, list ? ptr<int32_t>(*list) : nullptr, out.data_ptr(), stream_of(a[3]));
 }
 
-int append_kv4(const Shape& s, Args a) {
+template <int BITS>
+int small_append(const Shape& s, Args a) {
     const at::Tensor& ctx_len = on(s, a[4], at::kInt, "ctx_len", {-1});
     const int batch = batch_of(ctx_len, "ctx_len");
     uint32_t step = 0;
@@ -275,27 +291,29 @@ int append_kv4(const Shape& s, Args a) {
         step = v < 1 || v > UINT32_MAX ? 0u : static_cast<uint32_t>(v);     // (0 is refused by the call)
     }
     const at::Tensor &k = on(s, a[2], at::kBFloat16, "k_new", {batch, s.hkv, s.d}), &v = on(s, a[3], at::kBFloat16, "v_new", {batch, s.hkv, s.d});
-    const Store4 st = store4(s, a[5], a[11], batch);
-    return call(g_calls.append_kv4, s.ctx, layer_of(a[0]), batch, step, step_dev, k.data_ptr(), v.data_ptr(), ptr<int32_t>(ctx_len), st.base, st.stride, st.pages, st.page_stride,
-                              st.n_pages, pool4(s, a[6], batch), table<int32_t>(s, a[7], at::kInt, "block_table", batch * s.blocks),
+    const SmallStore st = small_store<BITS>(s, a[5], a[11], batch);
+    return call(BITS == 4 ? g_calls.append_kv4 : g_calls.append_kv8, s.ctx, layer_of(a[0]), batch, step, step_dev, k.data_ptr(), v.data_ptr(), ptr<int32_t>(ctx_len), st.base, st.stride, st.pages, st.page_stride,
+                              st.n_pages, small_pool<BITS>(s, a[6], batch), table<int32_t>(s, a[7], at::kInt, "block_table", batch * s.blocks),
                               table<int32_t>(s, a[8], at::kInt, "slot_block", batch * s.slots), table<uint32_t>(s, a[9], at::kInt, "slot_stamp", batch * s.slots),
                               table<void>(s, a[10], at::kBFloat16, "digest", batch * s.blocks * 2 * s.d), stream_of(a[12]));
 }
 
-int recall_kv4(const Shape& s, Args a) {
+template <int BITS>
+int small_recall(const Shape& s, Args a) {
     const at::Tensor& count = on(s, a[4], at::kInt, "recall_count", {-1});
     const int batch = batch_of(count, "recall_count");
     const at::Tensor& lists = on(s, a[3], at::kInt, "recall_list", {batch, -1, 4});
-    const Store4 st = store4(s, a[1], a[5], batch);
-    return call(g_calls.recall_kv4, s.ctx, layer_of(a[0]), batch, st.base, st.stride, st.pages, st.page_stride, st.n_pages, pool4(s, a[2], batch),
+    const SmallStore st = small_store<BITS>(s, a[1], a[5], batch);
+    return call(BITS == 4 ? g_calls.recall_kv4 : g_calls.recall_kv8, s.ctx, layer_of(a[0]), batch, st.base, st.stride, st.pages, st.page_stride, st.n_pages, small_pool<BITS>(s, a[2], batch),
                               reinterpret_cast<const pi_extent*>(lists.data_ptr()), static_cast<int32_t>(lists.size(1) < INT32_MAX ? lists.size(1) : 0), ptr<int32_t>(count), stream_of(a[6]));
 }
 
-int sparse_decode_attn_kv4(const Shape& s, Args a) {
+template <int BITS>
+int small_attn(const Shape& s, Args a) {
     const at::Tensor& q = on(s, a[1], at::kBFloat16, "q", {-1, s.hq, s.d});
     const int batch = batch_of(q, "q");
-    void* pool = pool4(s, a[2], batch);
-    return call(g_calls.sparse_decode_attn_kv4, s.ctx, layer_of(a[0]), batch, q.data_ptr(), pool, ptr<int32_t>(on(s, a[3], at::kInt, "sel_slots", {batch, s.budget})),
+    void* pool = small_pool<BITS>(s, a[2], batch);
+    return call(BITS == 4 ? g_calls.sparse_decode_attn_kv4 : g_calls.sparse_decode_attn_kv8, s.ctx, layer_of(a[0]), batch, q.data_ptr(), pool, ptr<int32_t>(on(s, a[3], at::kInt, "sel_slots", {batch, s.budget})),
                                           ptr<int32_t>(on(s, a[4], at::kInt, "sel_blocks", {batch, s.budget})), ptr<int32_t>(on(s, a[5], at::kInt, "sel_count", {batch})),
                                           ptr<int32_t>(on(s, a[6], at::kInt, "ctx_len", {batch})), on(s, a[7], at::kBFloat16, "out", {batch, s.hq, s.d}).data_ptr(),
                                           maybe<float>(s, a[8], at::kFloat, "lse", {batch, s.hq}), stream_of(a[9]));
@@ -350,13 +368,13 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     }
 }
 
-// shape(context address, device, Hq, Hkv, D, B, C, NB, K, bytes of a 4-bit block)
+// shape(context address, device, Hq, Hkv, D, B, C, NB, K, bytes of a 4-bit block, bytes of an 8-bit block)
 PyObject* make_shape(PyObject*, PyObject* const* args, Py_ssize_t n) {
     try {
-        if (n != 10) refuse(PyExc_TypeError, "shape: wrong number of arguments");
-        int64_t v[10];
-        for (int i = 0; i < 10; ++i) v[i] = whole(args[i]);
-        Shape* s = new Shape{reinterpret_cast<pi_ctx*>(v[0]), v[1], v[2], v[3], v[4], v[5], v[6], v[7], v[8], v[9]};
+        if (n != 11) refuse(PyExc_TypeError, "shape: wrong number of arguments");
+        int64_t v[11];
+        for (int i = 0; i < 11; ++i) v[i] = whole(args[i]);
+        Shape* s = new Shape{reinterpret_cast<pi_ctx*>(v[0]), v[1], v[2], v[3], v[4], v[5], v[6], v[7], v[8], v[9], v[10]};
         return PyCapsule_New(s, "pulseinfer.shape", [](PyObject* c) { delete static_cast<Shape*>(PyCapsule_GetPointer(c, "pulseinfer.shape")); });
     } catch (const Raised&) {
         return nullptr;
@@ -386,14 +404,19 @@ PyMethodDef methods[] = {
     METHOD("shape", make_shape),
     METHOD("assign_pages", (&entry<assign_pages, 9>)),
     METHOD("qk_norm_rope", (&entry<qk_norm_rope, 11>)),
-    METHOD("kv4_store", (&entry<kv4_store, 5>)),
-    METHOD("kv4_load", (&entry<kv4_load, 4>)),
-    METHOD("append_kv4", (&entry<append_kv4, 13>)),
-    METHOD("recall_kv4", (&entry<recall_kv4, 7>)),
-    METHOD("sparse_decode_attn_kv4", (&entry<sparse_decode_attn_kv4, 10>)),
+    METHOD("kv4_store", (&entry<small_store_tokens<4>, 5>)),
+    METHOD("kv4_load", (&entry<small_load<4>, 4>)),
+    METHOD("append_kv4", (&entry<small_append<4>, 13>)),
+    METHOD("recall_kv4", (&entry<small_recall<4>, 7>)),
+    METHOD("sparse_decode_attn_kv4", (&entry<small_attn<4>, 10>)),
+    METHOD("kv8_store", (&entry<small_store_tokens<8>, 5>)),
+    METHOD("kv8_load", (&entry<small_load<8>, 4>)),
+    METHOD("append_kv8", (&entry<small_append<8>, 13>)),
+    METHOD("recall_kv8", (&entry<small_recall<8>, 7>)),
+    METHOD("sparse_decode_attn_kv8", (&entry<small_attn<8>, 10>)),
     METHOD("prompt_attn", (&entry<prompt_attn, 8>)),
     {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_front", "Tensor checks and calls of the 4-bit path.", -1, methods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_front", "Tensor checks and calls of the 4-bit and 8-bit paths and of the attention over prompts.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 

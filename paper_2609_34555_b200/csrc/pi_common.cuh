@@ -187,3 +187,12 @@ int pi_launch_attn_kv4(pi_ctx*, int batch, const void* q, const void* pool, cons
 int pi_launch_prompt_attn(pi_ctx*, int n_seqs, int dtype, int n_q, int n_k, const void* q, int64_t q_tok, int64_t q_head, const void* k,
                           int64_t k_tok, int64_t k_head, const void* v, int64_t v_tok, int64_t v_head, const int32_t* q_start,
                           const int32_t* k_start, void* out, float* lse, cudaStream_t);
+// the 8-bit form: as the 4-bit one's
+int pi_launch_kv8_store(pi_ctx*, int64_t n_tokens, const void* k, const int64_t (&k_strides)[3], const void* v,
+                        const int64_t (&v_strides)[3], int inner, const int64_t* slots, void* store, int64_t n_blocks, cudaStream_t);
+int pi_launch_kv8_load(pi_ctx*, int64_t n_out, const void* store, int64_t n_blocks, const int32_t* blocks, void* out, cudaStream_t);
+int pi_launch_append_kv8(pi_ctx*, int h_star, int batch, uint32_t step, const uint32_t* step_dev, const void* k_new, const void* v_new,
+                         const int32_t* ctx_len, void* host_kv, int64_t host_stride, void* pool, int32_t* table, int32_t* slot_block,
+                         uint32_t* slot_stamp, void* digest, const int32_t* page_table, int64_t page_stride, int32_t n_pages, cudaStream_t);
+int pi_launch_attn_kv8(pi_ctx*, int batch, const void* q, const void* pool, const int32_t* sel_slots, const int32_t* sel_blocks,
+                       const int32_t* sel_count, const int32_t* ctx_len, void* out, float* lse, cudaStream_t);

@@ -29,6 +29,7 @@ struct RecallParams {
     const int32_t* count;
     pi_status_ref st;
     long long host_stride, pool_stride, unit_bytes;
+    int tail;                                      // bytes of a unit behind its last whole piece: they go with that piece
     long long unit_stride, list_offset;            // distance between consecutive units; byte offset of list (l % lists_per_seq)
     int n_lists, lists_per_seq, cap, cache_cap;
     long long pool_units, host_units;              // units one sequence's pool region / host region holds
@@ -68,7 +69,8 @@ __device__ __forceinline__ long long block_scan_add(long long v, long long* warp
     return base + inc - v;
 }
 
-template <bool PAGED>
+// TAIL: units are not a whole number of pieces (8-bit blocks: numbers, and 128 bytes of scales); the last piece of a unit takes the rest along.
+template <bool PAGED, bool TAIL>
 __global__ void __launch_bounds__(RECALL_THREADS)
 recall_kernel(RecallParams p) {
     extern __shared__ long long s_dyn[];
@@ -144,11 +146,12 @@ recall_kernel(RecallParams p) {
     const long long stride = static_cast<long long>(gridDim.x) * RECALL_WARPS;
 
     // piece -> (source, destination) of this lane's 16-byte column; src == nullptr: skip the piece
-    auto resolve = [&](long long piece, const unsigned char*& src, unsigned char*& dst) {
-        src = nullptr; dst = nullptr;
+    auto resolve = [&](long long piece, const unsigned char*& src, unsigned char*& dst, bool& last) {
+        src = nullptr; dst = nullptr; last = false;
         if (piece >= total) return;
         const long long unit = piece / pieces_per_unit;
         const long long in_unit = (piece - unit * pieces_per_unit) * PIECE_BYTES;
+        if (TAIL) last = in_unit == (pieces_per_unit - 1) * PIECE_BYTES && lane * 16 < p.tail;
         // list that holds this unit: last l with s_pref[l] <= unit
         int lo = 0, hi = p.n_lists;
         while (hi - lo > 1) {
@@ -201,22 +204,26 @@ recall_kernel(RecallParams p) {
     long long piece = static_cast<long long>(warp) * gridDim.x + blockIdx.x;
     const unsigned char* src;
     unsigned char* dst;
-    resolve(piece, src, dst);
+    bool last;
+    resolve(piece, src, dst, last);
     while (piece < total) {
-        uint4 v[LOADS_PER_LANE];
+        uint4 v[LOADS_PER_LANE], rest;
         if (src) {
 #pragma unroll
             for (int i = 0; i < LOADS_PER_LANE; ++i) v[i] = ld_host16(src + i * 512);
+            if (TAIL && last) rest = ld_host16(src + PIECE_BYTES);
         }
         const unsigned char* nsrc;
         unsigned char* ndst;
+        bool nlast;
         piece += stride;
-        resolve(piece, nsrc, ndst);
+        resolve(piece, nsrc, ndst, nlast);
         if (src) {
 #pragma unroll
             for (int i = 0; i < LOADS_PER_LANE; ++i) *reinterpret_cast<uint4*>(dst + i * 512) = v[i];
+            if (TAIL && last) *reinterpret_cast<uint4*>(dst + PIECE_BYTES) = rest;
         }
-        src = nsrc; dst = ndst;
+        src = nsrc; dst = ndst; last = nlast;
     }
 }
 
@@ -234,6 +241,8 @@ int pi_launch_recall(pi_ctx* c, int n_lists, int lists_per_seq, const void* host
     p.st = pi_status_of(c);
     p.host_stride = host_stride; p.pool_stride = pool_stride; p.unit_bytes = unit_bytes;
     p.unit_stride = unit_stride > 0 ? unit_stride : unit_bytes;
+    p.tail = static_cast<int>(unit_bytes % PIECE_BYTES);
+    if (p.tail > 512 || p.tail % 16 || unit_bytes < PIECE_BYTES) return PI_ERR_INVALID_ARG;      // (one more load a lane)
     p.list_offset = list_offset;
     p.n_lists = n_lists; p.lists_per_seq = lists_per_seq; p.cap = cap;
     // capacities of one sequence's regions in units (pool: C blocks, host: NB blocks of block_bytes)
@@ -245,7 +254,7 @@ int pi_launch_recall(pi_ctx* c, int n_lists, int lists_per_seq, const void* host
     const size_t smem = (static_cast<size_t>(n_lists) + 1) * sizeof(long long) +
                         ((static_cast<size_t>(n_lists) + 2) / 2) * sizeof(long long) +
                         static_cast<size_t>(p.cache_cap) * sizeof(pi_extent);
-    auto kernel = page_table ? recall_kernel<true> : recall_kernel<false>;
+    auto kernel = p.tail ? (page_table ? recall_kernel<true, true> : recall_kernel<false, true>) : page_table ? recall_kernel<true, false> : recall_kernel<false, false>;
     if (smem > 40 * 1024)
         PI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
     // ask for the largest shared-memory carve-out although this kernel hardly uses any: an SM

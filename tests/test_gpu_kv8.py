@@ -1,0 +1,531 @@
+"""The 8-bit cache on the GPU, against the plain references of kv8_reference."""
+import numpy as np
+import pytest
+import torch
+
+from tests import kv8_reference as ref
+from tests.test_gpu_kv4 import bf, clean, context, dev, i32
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+
+
+def tokens_of(rng, T, heads, spread=2.0):
+    """k, v as bf16 numbers, sizes that differ from token to token."""
+    kv = ref.bf16(rng.standard_normal((T, 2, heads, 128)) * np.exp(rng.standard_normal((T, 2, heads, 1)) * spread))
+    return kv[:, 0], kv[:, 1]
+
+
+def slots_of(rng, T, B, pages, at=0):
+    """Runs of tokens in order through scattered pages, the first from place `at` on."""
+    order = rng.permutation(pages)
+    t = np.arange(T) + at
+    return (order[t // B] * B + t % B).astype(np.int64)
+
+
+# ------------------------------------------------------------------ store and load
+@pytest.mark.parametrize("heads,block", [(1, 16), (2, 32), (4, 16), (8, 16), (8, 64), (16, 32)])
+@pytest.mark.parametrize("tokens,at", [(1, 0), (1, 15), (7, 3), (130, 0), (333, 9)])
+def test_store_writes_the_reference_bytes_and_nothing_else(heads, block, tokens, at):
+    pi = context(n_q_heads=heads, n_kv_heads=heads, block_tokens=block)
+    rng = np.random.default_rng(heads * 1000 + block + tokens)
+    pages = -(-(tokens + at) // block) + 2
+    k, v = tokens_of(rng, tokens, heads)
+    if tokens > 5:
+        k, v = k.copy(), v.copy()
+        k[0], v[1] = 0, np.float32(1e-39)                                              # nothing, subnormal
+        k[3, 0, 5], v[4, 0, 7], v[4, 0, 8] = np.nan, np.inf, -np.inf
+    slots = slots_of(rng, tokens, block, pages, at)
+    if tokens > 8:
+        slots[-3:] = -1                                                                # padding
+    before = ref.pack(ref.bf16(rng.standard_normal((pages, heads, 2, block, 128)) * np.exp(rng.standard_normal((pages, heads, 2, 1, 1)) * 3)), block)
+    want = before.copy()
+    ref.store(want, k, v, slots, block)
+    store = dev(before)
+    pi.kv8_store(bf(k), bf(v), store, dev(slots))
+    clean(pi)
+    got = store.cpu().numpy()
+    assert got.shape[1] == pi.kv8_block_bytes == ref.block_bytes(heads, block)
+    assert np.array_equal(got, want), np.argwhere(got != want)[:5]
+    out = torch.full((pages, heads, 2, block, 128), 5.0, dtype=torch.bfloat16, device=DEV)
+    pi.kv8_load(store, out)
+    clean(pi)
+    assert np.array_equal(out.double().cpu().numpy(), ref.unpack(want, heads, block), equal_nan=True)       # products are exact
+    pi.close()
+
+
+def test_store_in_two_calls_raises_scales_and_begins_blocks_anew():
+    """A block filled by several calls: small tokens, then large ones (scales grow, old tokens are rounded again), then small ones (scales
+    stay); then its first token again."""
+    pi = context(n_q_heads=2, n_kv_heads=2, block_tokens=32)
+    rng = np.random.default_rng(3)
+    store = torch.full((3, pi.kv8_block_bytes), 255, dtype=torch.uint8, device=DEV)    # never written: NaN all over
+    want = store.cpu().numpy()
+    for places, size in ((range(0, 5), 1e-3), (range(5, 9), 1.0), (range(9, 12), 1e-30), (range(12, 13), 2.0 ** 100), (range(13, 32), 3.0), ([0, 1], 1e-6), (range(2, 6), 0.0)):
+        n = len(places)
+        k, v = ref.bf16(rng.standard_normal((2, n, 2, 128)) * np.float64(size))
+        slots = np.asarray(places, dtype=np.int64) + 32
+        pi.kv8_store(bf(k), bf(v), store, dev(slots))
+        clean(pi)
+        ref.store(want, k, v, slots, 32)
+        assert np.array_equal(store.cpu().numpy(), want), size
+    pi.close()
+
+
+def test_store_of_the_largest_and_smallest_values():
+    pi = context(n_q_heads=1, n_kv_heads=1, block_tokens=16)
+    top = np.float32(3.3895313892515355e38)                                            # the largest bf16 number
+    k = np.zeros((3, 1, 128), dtype=np.float32)
+    k[0, 0, :4] = top, -top, top / 2, 2.0 ** 127
+    k[1, 0, :4] = 2.0 ** -126, 2.0 ** -110, -(2.0 ** -118), 2.0 ** -133
+    k[2, 0, :4] = 1.0, 2.0 ** -60, np.inf, -1.75
+    slots = np.asarray([0, 16, 32], dtype=np.int64)
+    store = torch.zeros((3, pi.kv8_block_bytes), dtype=torch.uint8, device=DEV)
+    want = store.cpu().numpy()
+    pi.kv8_store(bf(k), bf(-k), store, dev(slots))
+    clean(pi)
+    ref.store(want, k, -k, slots, 16)
+    assert np.array_equal(store.cpu().numpy(), want)
+    out = torch.zeros((3, 1, 2, 16, 128), dtype=torch.bfloat16, device=DEV)
+    pi.kv8_load(store, out)
+    clean(pi)
+    o = out.double().cpu().numpy()
+    assert np.isinf(o[0, 0, 0, 0, :2]).all() and o[0, 0, 0, 0, 3] == 2.0 ** 127 and o[1, 0, 0, 0, 1] == 2.0 ** -110 and np.isnan(o[2, 0, 0, 0, 2]) and o[2, 0, 1, 0, 3] == 1.75
+    pi.close()
+
+
+def test_store_of_runs_of_tokens_equals_store_token_by_token_and_a_pinned_store():
+    pi = context(n_q_heads=4, n_kv_heads=4, block_tokens=16)
+    rng = np.random.default_rng(7)
+    for N, M in ((3, 16), (5, 7), (40, 1), (1, 100)):
+        kv = bf(rng.standard_normal((N, 4, 2, M, 128)))
+        k, v = kv[:, :, 0].transpose(1, 2), kv[:, :, 1].transpose(1, 2)                # [N][M][head][128]
+        pages = N * M // 16 + 1
+        whole, pinned = torch.zeros((pages, pi.kv8_block_bytes), dtype=torch.uint8, device=DEV), torch.zeros((pages, pi.kv8_block_bytes), dtype=torch.uint8).pin_memory()
+        pi.kv8_store(k, v, whole)
+        pi.kv8_store(k.reshape(N * M, 4, 128), v.reshape(N * M, 4, 128), pinned, torch.arange(N * M, device=DEV))
+        clean(pi)
+        assert torch.equal(whole.cpu(), pinned)
+        want = np.zeros((pages, pi.kv8_block_bytes), dtype=np.uint8)
+        ref.store(want, k.float().cpu().numpy().reshape(N * M, 4, 128), v.float().cpu().numpy().reshape(N * M, 4, 128), range(N * M), 16)
+        assert np.array_equal(pinned.numpy(), want)
+        out = [torch.zeros((pages, 4, 2, 16, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+        pi.kv8_load(whole, out[0])
+        pi.kv8_load(pinned, out[1])
+        clean(pi)
+        assert torch.equal(*out)
+    pi.close()
+
+
+def test_store_and_load_skip_and_report_what_lies_beyond_the_store():
+    pi = context(n_q_heads=2, n_kv_heads=2, block_tokens=16)
+    rng = np.random.default_rng(5)
+    k, v = tokens_of(rng, 6, 2)
+    slots = np.asarray([0, 1, 48, 1 << 40, -(1 << 50), 17], dtype=np.int64)
+    store = torch.zeros((3, pi.kv8_block_bytes), dtype=torch.uint8, device=DEV)
+    want = store.cpu().numpy()
+    ref.store(want, k, v, slots, 16)
+    pi.kv8_store(bf(k), bf(v), store, dev(slots))
+    got = clean(pi, -8)
+    assert got[1] == 6 and got[2] in (2, 3) and np.array_equal(store.cpu().numpy(), want)
+    out = torch.full((3, 2, 2, 16, 128), 4.0, dtype=torch.bfloat16, device=DEV)
+    pi.kv8_load(store, out, i32([1, 3, 0]))
+    assert clean(pi, -8)[1] == 6
+    held = ref.unpack(want, 2, 16)
+    o = out.double().cpu().numpy()
+    assert np.array_equal(o[0], held[1]) and (o[1] == 4).all() and np.array_equal(o[2], held[0])
+    pi.kv8_store(bf(k)[:0], bf(v)[:0], store)                                          # no token: nothing happens
+    pi.kv8_load(store, out[:0], i32([]))
+    clean(pi)
+    assert np.array_equal(store.cpu().numpy(), want)
+    pi.close()
+
+
+def test_the_front_end_checks_devices_types_and_shapes():
+    pi = context()
+    n = pi.kv8_block_bytes
+    k = torch.zeros((4, 2, 128), dtype=torch.bfloat16, device=DEV)
+    store, pool, small = torch.zeros((4, n), dtype=torch.uint8, device=DEV), torch.zeros((1, 24, n), dtype=torch.uint8, device=DEV), torch.zeros((4, pi.kv4_block_bytes), dtype=torch.uint8, device=DEV)
+    with pytest.raises(TypeError):
+        pi.kv8_store(k, k, small)                                                      # 4-bit blocks
+    with pytest.raises(TypeError):
+        pi.kv4_store(k, k, store)                                                      # 8-bit blocks
+    with pytest.raises(TypeError):
+        pi.kv8_store(k.float(), k.float(), store)
+    with pytest.raises(ValueError):
+        pi.kv8_store(k, k[:3], store)
+    with pytest.raises(Exception) as e:
+        pi.kv8_store(k, k, torch.zeros((4, n), dtype=torch.uint8))                     # pageable
+    assert getattr(e.value, "code", None) == -5
+    with pytest.raises(ValueError):
+        pi.kv8_load(store, torch.zeros((4, 2, 2, 32, 128), dtype=torch.bfloat16, device=DEV))
+    q, sel, one = torch.zeros((1, 8, 128), dtype=torch.bfloat16, device=DEV), torch.zeros((1, 16), dtype=torch.int32, device=DEV), i32([1])
+    with pytest.raises(ValueError):
+        pi.sparse_decode_attn_kv8(0, q, pool[:, :20].contiguous(), sel, sel, one, one, torch.zeros_like(q))
+    with pytest.raises(TypeError):
+        pi.sparse_decode_attn(0, q, pool, sel, sel, one, one, torch.zeros_like(q))     # the bf16 call
+    with pytest.raises(Exception) as e:
+        pi.sparse_decode_attn_kv8(3, q, pool, sel, sel, one, one, torch.zeros_like(q))
+    assert getattr(e.value, "code", None) == -1
+    clean(pi)
+    pi.close()
+
+
+# ------------------------------------------------------------------ append and recall
+@pytest.mark.parametrize("heads,block,paged,dev_step", [(2, 16, False, False), (8, 16, True, True), (1, 64, False, True), (4, 32, True, False)])
+def test_append_over_block_borders(heads, block, paged, dev_step):
+    pi = context(n_q_heads=heads, n_kv_heads=heads, block_tokens=block, pool_slots=20, max_blocks=40, solo_head=[heads - 1])
+    rng = np.random.default_rng(heads + block)
+    n, NB, C = 3, 40, 20
+    ctx = np.asarray([12 * block + block - 2, 25 * block, 5 * block + 1])
+    table, slot_block = np.full((n, NB), -1, dtype=np.int32), np.full((n, C), -1, dtype=np.int32)
+    stamp = rng.integers(0, 50, (n, C)).astype(np.int32)
+    for s in range(n):
+        cur = -(-int(ctx[s]) // block)
+        must = sorted({0} | set(range(max(0, cur - 2), cur)))
+        other = [b for b in rng.permutation(cur) if b not in must][:C - len(must) - (2 if s == 0 else 0)]
+        for slot, b in zip(rng.permutation(C), must + other):
+            table[s, b], slot_block[s, slot] = slot, b
+    digest = ref.bf16(np.stack((rng.standard_normal((n, NB, 128)) - 1, rng.standard_normal((n, NB, 128)) + 1), 2))
+    pool = np.empty((n, C, pi.kv8_block_bytes), dtype=np.uint8)
+    pages = rng.permutation(n * NB).astype(np.int32).reshape(n, NB) if paged else None
+    store = ref.pack(ref.bf16(rng.standard_normal((n * NB, heads, 2, block, 128)) * np.exp(2 * rng.standard_normal((n * NB, heads, 2, 1, 1)))), block)
+    for s in range(n):                                                                 # pool and store hold the same
+        for slot in range(C):
+            b = slot_block[s, slot]
+            pool[s, slot] = 77 if b < 0 else store[pages[s, b] if paged else s * NB + b]
+    if not paged:
+        store = store.reshape(n, NB, -1)
+    sim = ref.Appender(table, slot_block, stamp, digest, pool, store, pi.cfg, heads - 1)
+    d = [dev(table), dev(slot_block), dev(stamp), bf(digest)]
+    pool_d, store_d = dev(pool), torch.from_numpy(store.copy()).pin_memory()
+    pt = dev(pages) if paged else None
+    for step in range(100, 106):
+        k, v = ref.bf16(rng.standard_normal((2, n, heads, 128)) * np.exp(2.5 * rng.standard_normal((2, n, heads, 1))))
+        if step == 104:
+            k[0, 0, 3], v[1, heads - 1, 4] = np.nan, np.inf
+            k[0, heads - 1], v[2] = ref.bf16(np.nan_to_num(k[0, heads - 1])), 0
+        st = i32([step]) if dev_step else step
+        pi.append_kv8(0, st, bf(k), bf(v), i32(ctx), store_d, pool_d, d[0], d[1], d[2], d[3], page_table=pt)
+        clean(pi)
+        sim.step(ctx, k, v, step, pages)
+        assert np.array_equal(d[0].cpu().numpy(), sim.table) and np.array_equal(d[1].cpu().numpy(), sim.slot_block)
+        assert np.array_equal(d[2].cpu().numpy(), sim.stamp) and np.array_equal(d[3].float().cpu().numpy(), sim.digest)
+        assert np.array_equal(pool_d.cpu().numpy(), sim.pool) and np.array_equal(store_d.numpy(), sim.store), step
+        ctx = ctx + 1
+    pi.close()
+
+
+def test_append_reports_what_cannot_be_appended():
+    pi = context(pool_slots=16, max_blocks=10)
+    store = torch.zeros((2, 10, pi.kv8_block_bytes), dtype=torch.uint8, device=DEV)
+    pool = torch.zeros((2, 16, pi.kv8_block_bytes), dtype=torch.uint8, device=DEV)
+    k = torch.ones((2, 2, 128), dtype=torch.bfloat16, device=DEV)
+
+    def tables():
+        return (torch.full((2, 10), -1, dtype=torch.int32, device=DEV), torch.full((2, 16), -1, dtype=torch.int32, device=DEV),
+                torch.zeros((2, 16), dtype=torch.int32, device=DEV), torch.zeros((2, 10, 2, 128), dtype=torch.bfloat16, device=DEV))
+
+    pi.append_kv8(0, 1, k, k, i32([160, 0]), store, pool, *tables())                   # block 10 of ten
+    assert clean(pi, -9)[1] == 5
+    pi.append_kv8(0, 1, k, k, i32([5, 0]), store, pool, *tables())                     # the block being filled is not resident
+    assert clean(pi, -8)[1] == 5
+    pages = torch.full((2, 10), 20, dtype=torch.int32, device=DEV)
+    pi.append_kv8(0, 1, k, k, i32([0, 0]), store, pool, *tables(), page_table=pages)   # page 20 of twenty
+    assert clean(pi, -8)[1] == 5
+    assert int(store[:, 1:].sum()) == 0 and int(pool[:, 2:].sum()) == 0
+    pi.close()
+
+
+@pytest.mark.parametrize("heads,block,paged", [(1, 16, False), (2, 16, True), (8, 16, True), (16, 64, False)])
+def test_recall_moves_whole_blocks_and_skips_what_leaves_the_pool(heads, block, paged):
+    pi = context(n_q_heads=heads, n_kv_heads=heads, block_tokens=block, pool_slots=16, max_blocks=30)
+    rng = np.random.default_rng(heads)
+    n, NB, C, size = 3, 30, 16, pi.kv8_block_bytes
+    host = torch.from_numpy(rng.integers(0, 256, (n, NB, size), dtype=np.uint8)).pin_memory()
+    pages = rng.permutation(n * NB).astype(np.int32).reshape(n, NB) if paged else None
+    logical = host.numpy() if not paged else host.numpy().reshape(n * NB, -1)[pages]
+    lists = np.zeros((n, 16, 4), dtype=np.int32)
+    lists[0, :3] = [[2, 0, 3, 0], [9, 5, 1, 3], [20, 12, 4, 4]]
+    lists[2, :1] = [[29, 15, 1, 0]]
+    pool = torch.full((n, C, size), 3, dtype=torch.uint8, device=DEV)
+    want = np.full((n, C, size), 3, dtype=np.uint8)
+    for s, cnt in ((0, 3), (2, 1)):
+        for src, dst, m, _ in lists[s, :cnt]:
+            want[s, dst:dst + m] = logical[s, src:src + m]
+    pi.recall_kv8(0, host, pool, dev(lists), i32([3, 0, 1]), page_table=None if pages is None else dev(pages))
+    clean(pi)
+    assert np.array_equal(pool.cpu().numpy(), want)
+    lists[1, :1] = [[0, 15, 2, 0]]                                                     # its second block would land behind the pool's sequence
+    pi.recall_kv8(0, host, pool, dev(lists), i32([0, 1, 0]), page_table=None if pages is None else dev(pages))
+    got = clean(pi, -8)
+    want[1, 15] = logical[1, 0]
+    assert got[1] == 3 and np.array_equal(pool.cpu().numpy(), want)
+    lists[1, :1] = [[29, 2, 2, 0]]                                                     # and one that leaves the store
+    pi.recall_kv8(0, host, pool, dev(lists), i32([0, 1, 0]), page_table=None if pages is None else dev(pages))
+    got = clean(pi, -8)
+    want[1, 2] = logical[1, 29]
+    assert got[1] == 3 and np.array_equal(pool.cpu().numpy(), want)
+    pi.close()
+
+
+# ------------------------------------------------------------------ attention
+def attention_case(pi, ctx, seed, garbage=True, spread=1.0):
+    """Pool, lists and queries for the given lengths: the newest block and others, in scattered slots; blocks of different sizes."""
+    c = pi.cfg
+    rng = np.random.default_rng(seed)
+    n, K, C, B, H = len(ctx), c.budget_blocks, c.pool_slots, c.block_tokens, c.n_kv_heads
+    kv = rng.standard_normal((n * C, H, 2, B, 128)) * np.exp(spread * rng.standard_normal((n * C, H, 2, 1, 1)) * np.asarray([0.3, 2.0])[:, None, None])
+    kv[..., [3, 90]] *= 8
+    pool = ref.pack(ref.bf16(kv), B).reshape(n, C, -1)
+    blocks, slots = np.full((n, K), -1, dtype=np.int32), np.full((n, K), -1, dtype=np.int32)
+    count = np.zeros(n, dtype=np.int32)
+    for s in range(n):
+        nb = -(-int(ctx[s]) // B)
+        count[s] = min(nb, K)
+        if nb:
+            rest = rng.permutation(nb - 1)[:count[s] - 1] if nb > 1 else []
+            blocks[s, :count[s]] = np.sort(np.append(rest, nb - 1))
+            slots[s, :count[s]] = rng.permutation(C)[:count[s]]
+        last = int(ctx[s]) % B
+        if nb and last and garbage:                                                    # behind the last token: NaN
+            ref.parts(pool[s, slots[s, count[s] - 1]], H, B)[0][:, :, last:] = 255
+    q = ref.bf16(rng.standard_normal((n, c.n_q_heads, 128)))
+    return dict(pool=pool, blocks=blocks, slots=slots, count=count, ctx=np.asarray(ctx), q=q)
+
+
+def check_attention(pi, case, out, lse):
+    c = pi.cfg
+    out, lse = out.double().cpu().numpy(), None if lse is None else lse.double().cpu().numpy()
+    for s in range(len(case["ctx"])):
+        def kv_of(slot):
+            return ref.unpack(case["pool"][s, slot][None], c.n_kv_heads, c.block_tokens)[0]
+        want, want_lse, tol, eps = ref.attention(case["q"][s].astype(np.float64), kv_of, case["blocks"][s], case["slots"][s], int(case["count"][s]), int(case["ctx"][s]), c.block_tokens)
+        assert (np.abs(out[s] - want) <= tol).all(), (s, (np.abs(out[s] - want) / tol).max())
+        if lse is not None:
+            if np.isinf(want_lse).any():
+                assert (lse[s] == -np.inf).all() and (out[s] == 0).all()
+            else:
+                assert (np.abs(lse[s] - want_lse) <= eps + 2.0 ** -20 * np.abs(want_lse) + 2.0 ** -18).all()
+
+
+def run_attention(pi, case, lse=True, stream=None):
+    n, c = len(case["ctx"]), pi.cfg
+    out = torch.full((n + 1, c.n_q_heads, 128), 9.0, dtype=torch.bfloat16, device=DEV)
+    l = torch.full((n + 1, c.n_q_heads), 9.0, dtype=torch.float32, device=DEV)
+    pi.sparse_decode_attn_kv8(0, bf(case["q"]), dev(case["pool"]), dev(case["slots"]), dev(case["blocks"]), dev(case["count"]), i32(case["ctx"]),
+                              out[:n], l[:n] if lse else None, stream=stream)
+    clean(pi)
+    assert (out[n] == 9).all() and (l[n] == 9).all()                                   # rows behind the last sequence
+    return out[:n], l[:n] if lse else None
+
+
+@pytest.mark.parametrize("Hq,Hkv,B,K,ctx", [
+    (8, 2, 16, 16, [1, 0, 250, 256]),
+    (1, 1, 16, 1, [1, 16, 700]),
+    (2, 2, 64, 3, [63, 64, 65, 5]),
+    (3, 1, 32, 24, [700, 31, 33]),                    # three query heads per KV head
+    (16, 4, 16, 40, [640, 641, 3999]),
+    (5, 1, 16, 9, [100, 7]),                          # five
+    (64, 8, 16, 64, [1024, 500]),                     # eight
+    (12, 1, 16, 9, [100, 7]),                         # twelve
+    (32, 2, 32, 8, [255, 256, 0]),                    # sixteen
+    (16, 16, 64, 5, [320, 1]),                        # sixteen KV heads
+    (32, 8, 16, 64, [8192]),                          # one sequence: a cluster an item
+    (8, 8, 16, 3, [40] * 40),                         # many items: one CTA each
+    (4, 1, 16, 300, [4795, 16, 4800]),                # more than 32 tiles a warp
+    (20, 2, 16, 300, [4800, 3]),
+    (8, 1, 64, 70, [4480, 0, 77]),
+])
+def test_attention(Hq, Hkv, B, K, ctx):
+    pi = context(n_q_heads=Hq, n_kv_heads=Hkv, block_tokens=B, budget_blocks=K, pool_slots=K + 3, max_batch=max(8, len(ctx)), max_blocks=max(256, 2 * K), n_sink_blocks=0, n_local_blocks=1)
+    case = attention_case(pi, ctx, Hq * 100 + K)
+    out, lse = run_attention(pi, case)
+    check_attention(pi, case, out, lse)
+    again, _ = run_attention(pi, case, lse=False)
+    assert torch.equal(out, again)
+    pi.close()
+
+
+@pytest.mark.parametrize("Hq,Hkv,B", [(8, 1, 64), (32, 8, 16), (48, 4, 32)])
+def test_attention_random_shapes(Hq, Hkv, B):
+    rng = np.random.default_rng(Hq + B)
+    for _ in range(6):
+        K, batch = int(rng.integers(1, 80)), int(rng.integers(1, 12))
+        pi = context(n_q_heads=Hq, n_kv_heads=Hkv, block_tokens=B, budget_blocks=K, pool_slots=K + int(rng.integers(0, 9)), max_batch=batch,
+                     max_blocks=2 * K, n_sink_blocks=0, n_local_blocks=1)
+        case = attention_case(pi, rng.integers(0, 2 * K * B + 1, batch), int(rng.integers(1 << 30)))
+        out, lse = run_attention(pi, case)
+        check_attention(pi, case, out, lse)
+        pi.close()
+
+
+@pytest.mark.parametrize("spread", [6.0, 12.0])
+def test_attention_over_blocks_of_very_different_sizes(spread):
+    """V's scales differ by many powers of two between blocks, and scores are in the hundreds: what has the weight keeps its bits, however
+    small its values are next to a block's that has none."""
+    pi = context(budget_blocks=20)
+    case = attention_case(pi, [300, 17], 3, spread=spread)
+    for factor in (1.0, 30.0):
+        case["q"] = ref.bf16(case["q"] * np.float32(factor))
+        out, lse = run_attention(pi, case)
+        check_attention(pi, case, out, lse)
+    pi.close()
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-3, 1e4, 1e30])
+def test_attention_with_small_and_large_values(size):
+    pi = context(budget_blocks=20)
+    case = attention_case(pi, [300, 17], 4)
+    rng = np.random.default_rng(1)
+    kv = ref.bf16(rng.standard_normal((2 * pi.cfg.pool_slots, 2, 2, 16, 128)))
+    kv[:, :, 1] = ref.bf16(kv[:, :, 1] * np.float32(size))                             # V; scores stay ordinary
+    case["pool"] = ref.pack(kv, 16).reshape(case["pool"].shape)
+    out, lse = run_attention(pi, case)
+    check_attention(pi, case, out, lse)
+    kv = ref.bf16(rng.standard_normal((2 * pi.cfg.pool_slots, 2, 2, 16, 128)))
+    kv[:, :, 0] = ref.bf16(kv[:, :, 0] * np.float32(size))                             # K, and queries as much the other way
+    case["q"] = ref.bf16(case["q"] / np.float32(size))
+    case["pool"] = ref.pack(kv, 16).reshape(case["pool"].shape)
+    out, lse = run_attention(pi, case)
+    check_attention(pi, case, out, lse)
+    pi.close()
+
+
+@pytest.mark.parametrize("size", [1e4, 1e9, 1e20, 1e32])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_attention_with_scores_of_any_size(size, sign):
+    """Equal scores, then one that stands out, anywhere in the range of 32 bits."""
+    pi = context(budget_blocks=20)
+    c = pi.cfg
+    case = attention_case(pi, [300, 17], 5, garbage=False)
+    rng = np.random.default_rng(2)
+    kv = ref.bf16(rng.standard_normal((2 * c.pool_slots, 2, 2, 16, 128)))
+    key = float(np.float32(2.0 ** round(np.log2(size ** 0.5))))
+    kv[:, :, 0] = key
+    q = float(ref.bf16(np.float32(sign * 1.71 * size ** 0.5)))
+    case["q"][:] = q
+    case["pool"] = ref.pack(kv, 16).reshape(case["pool"].shape)
+    score = 128 * q * key / 128 ** 0.5
+    out, lse = run_attention(pi, case)
+    held = ref.unpack(case["pool"].reshape(2 * c.pool_slots, -1), 2, 16).reshape(2, c.pool_slots, 2, 2, 16, 128)
+    pick = []
+    for s, n in enumerate((300, 17)):
+        v = np.concatenate([held[s, case["slots"][s, i], :, 1, :min(16, n - 16 * case["blocks"][s, i])] for i in range(case["count"][s])], axis=1)
+        assert v.shape[1] == n
+        want, spread = np.repeat(v.mean(axis=1), 4, axis=0), np.repeat(np.abs(v).mean(axis=1), 4, axis=0)
+        # weights are all alike but for their rounding to fp16; the score carries eight cuts of 2^-23 and four roundings of 2^-24: below 2^-19 of itself
+        assert (np.abs(out[s].double().cpu().numpy() - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * spread).all()
+        assert (np.abs(lse[s].double().cpu().numpy() - (score + np.log(n))) <= 2.0 ** -19 * abs(score) + 2.0 ** -18).all()
+        pick.append(v[:, 0])
+    # the first token of each list half as far from 0 (scores below it) or twice as far (above it): the others' weights are nothing
+    for s in range(2):
+        kv.reshape(2, c.pool_slots, 2, 2, 16, 128)[s, case["slots"][s, 0], :, 0, 0] = key * (2.0 if sign > 0 else 0.5)
+    case["pool"] = ref.pack(kv, 16).reshape(case["pool"].shape)
+    out, lse = run_attention(pi, case)
+    for s in range(2):
+        want = np.repeat(pick[s], 4, axis=0)
+        assert (np.abs(out[s].double().cpu().numpy() - want) <= (2.0 ** -8 + 2.0 ** -10) * np.abs(want) + 1e-30).all()
+        top = score * (2.0 if sign > 0 else 0.5)
+        assert (np.abs(lse[s].double().cpu().numpy() - top) <= 2.0 ** -19 * abs(top) + 2.0 ** -18).all()
+    pi.close()
+
+
+def test_attention_reports_bad_lists_and_leaves_the_other_sequences_alone():
+    pi = context(budget_blocks=16)
+    case = attention_case(pi, [250, 250, 250, 250], 8)
+    good, _ = run_attention(pi, case)
+    case["count"][1] = 17
+    case["slots"][2, 3] = 24
+    case["slots"][3, 2], case["blocks"][3, 2] = -1, -1                                 # an entry that names nothing is skipped silently
+    out = torch.zeros((4, 8, 128), dtype=torch.bfloat16, device=DEV)
+    lse = torch.zeros((4, 8), dtype=torch.float32, device=DEV)
+    pi.sparse_decode_attn_kv8(0, bf(case["q"]), dev(case["pool"]), dev(case["slots"]), dev(case["blocks"]), dev(case["count"]), i32(case["ctx"]), out, lse)
+    torch.cuda.synchronize()
+    assert pi.status()[0] in (-8, -9) and pi.status()[1] == 4
+    pi.clear_status()
+    assert torch.equal(out[0], good[0]) and (out[1] == 0).all() and (lse[1] == -float("inf")).all()
+    case["count"][1] = 0
+    case["blocks"][2, 3] = -1                                                          # what the kernel skipped, the reference skips
+    check_attention(pi, case, out, lse)
+    # NaN in one sequence's cache stays in that sequence, and in V in its channel
+    case = attention_case(pi, [250, 250], 9)
+    ref.parts(case["pool"][1, case["slots"][1, 0]], 2, 16)[0][0, 1, 0, 77] = 127
+    out, _ = run_attention(pi, case)
+    bad = torch.isnan(out.float())
+    assert not bad[0].any() and bad[1, :4, 77].all() and int(bad[1].sum()) == 4
+    pi.close()
+
+
+def test_attention_takes_a_list_as_it_is():
+    """Entries behind the count are not looked at, a block named twice counts twice, a block behind the context not at all;
+    a head whose query is not a number leaves the others alone."""
+    pi = context(n_q_heads=8, n_kv_heads=2, budget_blocks=16)
+    case = attention_case(pi, [250, 250, 100, 250], 21)
+    case["blocks"][0, 3], case["slots"][0, 3] = case["blocks"][0, 4], case["slots"][0, 4]
+    case["blocks"][1, 2] = 200                                                         # far behind the context
+    case["count"][3] = 5
+    case["blocks"][3, 5:], case["slots"][3, 5:] = 123456, -77
+    out, lse = run_attention(pi, case)
+    check_attention(pi, case, out, lse)
+    before = out.clone()
+    q = case["q"].copy()
+    case["q"][:, 5, 17] = np.nan
+    out, lse = run_attention(pi, case)
+    keep = [g for g in range(8) if g != 5]
+    assert torch.equal(out[:, keep], before[:, keep]) and torch.isnan(out[:, 5].float()).all() and torch.isnan(lse[:, 5]).all()
+    case["q"] = q
+    case["pool"][:] = 0                                                                # a pool that was never written: all values zero
+    out, lse = run_attention(pi, case)
+    check_attention(pi, case, out, lse)
+    assert (out == 0).all()
+    pi.close()
+
+
+def test_attention_with_pool_offsets_beyond_32_bits():
+    pi = context(n_q_heads=16, n_kv_heads=16, block_tokens=64, budget_blocks=4, pool_slots=8192, max_batch=4)
+    small = attention_case(context(n_q_heads=16, n_kv_heads=16, block_tokens=64, budget_blocks=4, pool_slots=8, max_batch=4), [250, 3, 256, 200], 4)
+    pool = torch.zeros((4, 8192, pi.kv8_block_bytes), dtype=torch.uint8, device=DEV)   # 8.6 GB
+    far = np.asarray([8191, 5000, 8000, 1, 8190, 4096, 77, 3000])
+    pool[:, torch.from_numpy(far).to(DEV)] = dev(small["pool"])
+    slots = np.where(small["slots"] >= 0, far[np.maximum(small["slots"], 0)], -1).astype(np.int32)
+    out, lse = torch.zeros((4, 16, 128), dtype=torch.bfloat16, device=DEV), torch.zeros((4, 16), device=DEV)
+    pi.sparse_decode_attn_kv8(0, bf(small["q"]), pool, dev(slots), dev(small["blocks"]), dev(small["count"]), i32(small["ctx"]), out, lse)
+    clean(pi)
+    check_attention(pi, small, out, lse)
+    pi.close()
+
+
+def test_attention_on_two_streams_at_once_and_in_a_replayed_graph():
+    pi = context(n_q_heads=32, n_kv_heads=8, budget_blocks=64, pool_slots=70, max_batch=4)
+    cases = [attention_case(pi, [1000, 37, 1024], s) for s in (1, 2)]
+    want = [run_attention(pi, c)[0].clone() for c in cases]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    args = [[bf(c["q"]), dev(c["pool"]), dev(c["slots"]), dev(c["blocks"]), dev(c["count"]), i32(c["ctx"])] for c in cases]
+    outs = [torch.zeros((3, 32, 128), dtype=torch.bfloat16, device=DEV) for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for a, o, s in zip(args, outs, streams):
+            pi.sparse_decode_attn_kv8(0, *a, o, stream=s)
+    clean(pi)
+    for o, w in zip(outs, want):
+        assert torch.equal(o, w)
+    static = [t.clone() for t in args[0]]
+    out = torch.zeros_like(outs[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pi.sparse_decode_attn_kv8(0, *static, out)
+    for a, w in zip(args, want):
+        for s, t in zip(static, a):
+            s.copy_(t)
+        graph.replay()
+        clean(pi)
+        assert torch.equal(out, w)
+    pi.close()
