@@ -249,8 +249,9 @@ class CudaNormal:
         self.stream = torch.cuda.current_stream()
 
     def enqueue_attention(self, layer: int):
+        from .runner import call_for
         b = self.buf
-        call = self.pi.sparse_decode_attn_kv4 if getattr(b, "kv_bits", 16) == 4 else self.pi.sparse_decode_attn
+        call = call_for(self.pi, b, "sparse_decode_attn", "sparse_decode_attn_kv")
         call(0, self.q, b.pool, b.sel_slots, b.sel_blocks, b.sel_count, self.ctx, self.out, None, stream=self.stream)
         ev = self.torch.cuda.Event(); ev.record(self.stream)
         return ev

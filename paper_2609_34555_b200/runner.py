@@ -12,14 +12,20 @@ import torch
 from .binding import PulseInfer
 
 
+def call_for(pi: PulseInfer, buf, whole: str, small: str):
+    """The call on the form of blocks that the buffers keep: `whole` for bf16 blocks (buffers that do not say), else `small` with the bits behind it."""
+    bits = getattr(buf, "kv_bits", 16)
+    return getattr(pi, whole if bits == 16 else f"{small}{bits}")
+
+
 class LayerBuffers:
-    """Everything one layer keeps on the device for a batch of offloaded sequences.  kv_bits: 16, or 4 for a
-    pool of 4-bit blocks (uint8 [batch][C][pi.kv4_block_bytes])."""
+    """Everything one layer keeps on the device for a batch of offloaded sequences.  kv_bits: 16, or 8 or 4 for a
+    pool of 8-bit or 4-bit blocks (uint8 [batch][C][pi.kv8_block_bytes or pi.kv4_block_bytes])."""
 
     def __init__(self, pi: PulseInfer, batch: int, device="cuda", keep_scores: bool = False, kv_bits: int = 16):
         c = pi.cfg
-        if kv_bits not in (4, 16):
-            raise ValueError("kv_bits: 16 or 4")
+        if kv_bits not in (4, 8, 16):
+            raise ValueError("kv_bits: 16, 8 or 4")
         self.kv_bits = kv_bits
         i32 = dict(dtype=torch.int32, device=device)
         self.batch = batch
@@ -27,8 +33,8 @@ class LayerBuffers:
         self.block_table = torch.full((batch, c.max_blocks), -1, **i32)
         self.slot_block = torch.full((batch, c.pool_slots), -1, **i32)
         self.slot_stamp = torch.zeros((batch, c.pool_slots), **i32)
-        if kv_bits == 4:
-            self.pool = torch.zeros((batch, c.pool_slots, pi.kv4_block_bytes), dtype=torch.uint8, device=device)
+        if kv_bits != 16:
+            self.pool = torch.zeros((batch, c.pool_slots, getattr(pi, f"kv{kv_bits}_block_bytes")), dtype=torch.uint8, device=device)
         else:
             self.pool = torch.zeros((batch, c.pool_slots, c.n_kv_heads, 2, c.block_tokens, c.head_dim),
                                     dtype=torch.bfloat16, device=device)
@@ -52,13 +58,12 @@ class RecallPath:
     def recall(self, layer: int, buf: LayerBuffers, host_kv: torch.Tensor, recall_list, recall_count,
                page_table: Optional[torch.Tensor] = None, stream=None) -> None:
         """The lists' blocks from the host store into the pool, in whichever form the buffers keep them."""
-        call = self.pi.recall_kv4 if getattr(buf, "kv_bits", 16) == 4 else self.pi.recall_gather_scatter
-        call(layer, host_kv, buf.pool, recall_list, recall_count, page_table=page_table, stream=stream)
+        call_for(self.pi, buf, "recall_gather_scatter", "recall_kv")(layer, host_kv, buf.pool, recall_list, recall_count, page_table=page_table, stream=stream)
 
     def append(self, layer: int, step, buf: LayerBuffers, k_new, v_new, ctx_len, host_kv: torch.Tensor,
                page_table: Optional[torch.Tensor] = None, stream=None) -> None:
         """The step's token into pool, host store and digest."""
-        call = self.pi.append_kv4 if getattr(buf, "kv_bits", 16) == 4 else self.pi.append_kv
+        call = call_for(self.pi, buf, "append_kv", "append_kv")
         call(layer, step, k_new, v_new, ctx_len, host_kv, buf.pool, buf.block_table, buf.slot_block, buf.slot_stamp,
              buf.digest, page_table=page_table, stream=stream)
 
@@ -70,7 +75,7 @@ class RecallPath:
         host store needs kv_for_digest (the keys in logical block order)."""
         if page_table is not None and kv_for_digest is None:
             raise ValueError("a paged host store cannot be read in block order: pass kv_for_digest")
-        if getattr(buf, "kv_bits", 16) == 4 and kv_for_digest is None:
+        if getattr(buf, "kv_bits", 16) != 16 and kv_for_digest is None:
             raise ValueError("digests are built from the keys in bf16: pass kv_for_digest")
         pi = self.pi
         pi.build_digests(layer, host_kv if kv_for_digest is None else kv_for_digest, ctx_len, buf.digest)
@@ -102,7 +107,7 @@ class RecallPath:
 
     def attention(self, layer: int, buf: LayerBuffers, q: torch.Tensor, ctx_len: torch.Tensor, out: torch.Tensor,
                   lse: Optional[torch.Tensor] = None, stream=None) -> None:
-        call = self.pi.sparse_decode_attn_kv4 if getattr(buf, "kv_bits", 16) == 4 else self.pi.sparse_decode_attn
+        call = call_for(self.pi, buf, "sparse_decode_attn", "sparse_decode_attn_kv")
         call(layer, q, buf.pool, buf.sel_slots, buf.sel_blocks, buf.sel_count, ctx_len, out, lse, stream=stream)
 
     def layer_step(self, layer: int, step: int, buf: LayerBuffers, q: torch.Tensor, ctx_len: torch.Tensor,
@@ -264,8 +269,8 @@ class DecodeSession:
     the fixed cost of one launch (launch gap, list scan, first round trip over the host link,
     drain) is covered by the transfer of the next.
 
-    `kv_bits=4` keeps the host store and the pools in 4-bit blocks (pi.kv4_block_bytes each): load_layer rounds the
-    layer's keys and values, appended tokens are rounded as they come, the recall moves 4-bit blocks and the
+    `kv_bits=4` or `8` keeps the host store and the pools in 4-bit or 8-bit blocks (pi.kv4_block_bytes, pi.kv8_block_bytes each): load_layer rounds the
+    layer's keys and values, appended tokens are rounded as they come, the recall moves such blocks and the
     attention reads them.  Digests, and with them the selection, are built from the keys as given."""
 
     def __init__(self, pi: PulseInfer, batch: int, n_layers: int, host_layers: Optional[int] = None,
@@ -273,7 +278,7 @@ class DecodeSession:
                  recall_streams: int = 2, fused_select_diff: bool = True, split_attention: bool = False,
                  kv_bits: int = 16):
         c = pi.cfg
-        if kv_bits == 4 and split_attention:
+        if kv_bits != 16 and split_attention:
             raise ValueError("the attention is split around the recall for bf16 blocks only")
         self.kv_bits = kv_bits
         # attention split around the recall: the resident blocks' share runs beside the recall (in the serial
@@ -285,9 +290,9 @@ class DecodeSession:
         self.device = torch.device(device)
         self.bufs = [LayerBuffers(pi, batch, device, keep_scores, kv_bits) for _ in range(n_layers)]
         shape = (batch, c.max_blocks, c.n_kv_heads, 2, c.block_tokens, c.head_dim)
-        if kv_bits == 4:
-            shape = (batch, c.max_blocks, pi.kv4_block_bytes)
-        self.host_kv = [torch.empty(shape, dtype=torch.uint8 if kv_bits == 4 else torch.bfloat16, pin_memory=True)
+        if kv_bits != 16:
+            shape = (batch, c.max_blocks, getattr(pi, f"kv{kv_bits}_block_bytes"))
+        self.host_kv = [torch.empty(shape, dtype=torch.bfloat16 if kv_bits == 16 else torch.uint8, pin_memory=True)
                         for _ in range(self.host_layers)]
         self.page_tables = None
         if paged:
@@ -337,7 +342,7 @@ class DecodeSession:
         host = self.host_region(layer)
         pt = self.page_table(layer)
         if kv_dev is not None and store:
-            blocks = self.pack_blocks(kv_dev) if self.kv_bits == 4 else kv_dev
+            blocks = kv_dev if self.kv_bits == 16 else self.pack_blocks(kv_dev)
             if pt is None:
                 host.copy_(blocks, non_blocking=False)
             else:
@@ -350,12 +355,43 @@ class DecodeSession:
                                  kv_for_digest=kv_dev, page_table=pt)
 
     def pack_blocks(self, kv_dev: torch.Tensor) -> torch.Tensor:
-        """Whole blocks [batch][NB][Hkv][2][B][D] bf16 -> 4-bit blocks [batch][NB][kv4_block_bytes] uint8."""
+        """Whole blocks [batch][NB][Hkv][2][B][D] bf16 -> blocks of the session's bits [batch][NB][kv4_block_bytes or kv8_block_bytes] uint8."""
+        bits = 8 if self.kv_bits == 8 else 4
         n = kv_dev.shape[0] * kv_dev.shape[1]
         rows = kv_dev.reshape((n,) + tuple(kv_dev.shape[2:])).transpose(1, 3)          # [block][token][K, V][head][D]
-        out = torch.zeros((kv_dev.shape[0], kv_dev.shape[1], self.pi.kv4_block_bytes), dtype=torch.uint8, device=kv_dev.device)
-        self.pi.kv4_store(rows[:, :, 0], rows[:, :, 1], out)
+        out = torch.zeros((kv_dev.shape[0], kv_dev.shape[1], getattr(self.pi, f"kv{bits}_block_bytes")), dtype=torch.uint8, device=kv_dev.device)
+        getattr(self.pi, f"kv{bits}_store")(rows[:, :, 0], rows[:, :, 1], out)
         return out
+
+    def load_prompts(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, out: torch.Tensor,
+                     lse: Optional[torch.Tensor] = None, resident: Optional[torch.Tensor] = None) -> None:
+        """One layer's prompts, from its (normed and rotated) queries, keys and values: q [T][Hq][D], k, v [T][Hkv][D] bf16, the sequences one behind
+        the other, sequence s from token starts[s] on (int32 [batch + 1] on the device).  Their attention goes to `out` [T][Hq][D]; the
+        keys and values go where load_layer puts them, with the lengths as the context.  resident: int32 [batch][C], the blocks of
+        the hot set (None: sink blocks and as many of the newest as the pool holds)."""
+        c = self.pi.cfg
+        if k.shape[0] != v.shape[0] or starts.shape != (self.batch + 1,):
+            raise ValueError("load_prompts: expected keys and values of the same tokens, and batch + 1 starts")
+        self.pi.prompt_attn(q, k, v, starts, out, lse=lse)
+        begin = starts.long()
+        lens = begin.diff()
+        if int(lens.max()) > c.max_blocks * c.block_tokens:
+            raise ValueError("load_prompts: a prompt is longer than max_blocks blocks")
+        self.ctx_len.copy_(lens)
+        t = torch.arange(k.shape[0], device=self.device)
+        seq = (torch.searchsorted(begin, t, right=True) - 1).clamp(0, self.batch - 1)
+        mine = (t >= begin[0]) & (t < begin[-1])
+        t, seq = t[mine], seq[mine]
+        pos = t - begin[seq]
+        blocks = torch.zeros((self.batch, c.max_blocks, c.n_kv_heads, 2, c.block_tokens, c.head_dim), dtype=torch.bfloat16, device=self.device)
+        for i, x in enumerate((k, v)):
+            blocks[seq, pos // c.block_tokens, :, i, pos % c.block_tokens] = x[t]
+        if resident is None:
+            n = (lens + c.block_tokens - 1) // c.block_tokens
+            slot = torch.arange(c.pool_slots, device=self.device)[None]
+            newest = torch.where(slot < c.n_sink_blocks, slot, torch.maximum(n[:, None] - c.pool_slots, torch.zeros_like(slot)) + slot)
+            resident = torch.where(newest < n[:, None], newest, -1).to(torch.int32).contiguous()
+        self.load_layer(layer, blocks, resident)
 
     def decode_step(self, q: torch.Tensor, overlapped: bool = True, timer: Optional[StageTimer] = None,
                     resident_script: Optional[torch.Tensor] = None, new_kv=None,

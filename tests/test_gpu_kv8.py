@@ -529,3 +529,141 @@ def test_attention_on_two_streams_at_once_and_in_a_replayed_graph():
         clean(pi)
         assert torch.equal(out, w)
     pi.close()
+
+
+# ------------------------------------------------------------------ together
+@pytest.mark.parametrize("paged", [False, True])
+def test_a_session_in_8_bits_with_appends_eager_and_replayed(paged):
+    """Two layers, four steps with appends: eager and graph-replayed sessions agree bit for bit, every layer's attention is
+    what the reference makes of the session's own lists and pool, and pool and host store agree on every resident block."""
+    from paper_2609_34555_b200 import PulseInfer
+    from paper_2609_34555_b200.runner import DecodeSession
+    from workloads import generate as gen, tiny_config
+    cfg = tiny_config(batch=3, ctx=1200, n_layers=2, n_q_heads=16, n_kv_heads=4, budget_blocks=24, resident_frac=0.4)
+    lens = [1150, 700, 433]
+    sessions = []
+    for _ in range(2):
+        pi = PulseInfer.from_workload(cfg)
+        sess = DecodeSession(pi, cfg.batch, cfg.n_layers, paged=paged, kv_bits=8)
+        sess.ctx_len.copy_(i32(lens))
+        for l in range(cfg.n_layers):
+            res = np.stack([np.pad(gen.initial_resident(cfg.replace(ctx=n, batch=1), l)[0][:cfg.pool_slots],
+                                   (0, max(0, cfg.pool_slots - len(gen.initial_resident(cfg.replace(ctx=n, batch=1), l)[0]))), constant_values=-1) for n in lens])
+            sess.load_layer(l, gen.make_kv(cfg, l, device=torch.device(DEV)), i32(res))
+        torch.cuda.synchronize()
+        sessions.append((pi, sess))
+    g = torch.Generator().manual_seed(1)
+    qs = [torch.randn((2, 3, 16, 128), generator=g).to(torch.bfloat16).to(DEV) for _ in range(4)]
+    new = [tuple((torch.randn((2, 3, 4, 128), generator=g) * 4 ** i).to(torch.bfloat16).to(DEV) for _ in range(2)) for i in range(4)]
+    (pi, sess), (pi2, sess2) = sessions
+    q_static, kv_static = torch.empty_like(qs[0]), tuple(torch.empty_like(t) for t in new[0])
+    graph = sess2.capture_step(q_static, new_kv_static=kv_static)
+    misses = 0
+    for step in range(4):
+        out = sess.decode_step(qs[step], new_kv=new[step]).clone()
+        q_static.copy_(qs[step]); kv_static[0].copy_(new[step][0]); kv_static[1].copy_(new[step][1])
+        sess2.replay_step(graph)
+        clean(pi)
+        clean(pi2)
+        assert torch.equal(out, sess2.out)
+        misses += sess.miss_blocks()
+        for l in range(2):
+            b = sess.bufs[l]
+            case = dict(pool=b.pool.cpu().numpy(), blocks=b.sel_blocks.cpu().numpy(), slots=b.sel_slots.cpu().numpy(), count=b.sel_count.cpu().numpy(),
+                        ctx=sess.ctx_len.cpu().numpy(), q=qs[step][l].float().cpu().numpy())
+            check_attention(pi, case, out[l], None)
+            host = sess.logical_host(l).numpy()
+            table = b.block_table.cpu().numpy()
+            for s in range(3):
+                for blk in np.nonzero(table[s] >= 0)[0]:
+                    assert np.array_equal(case["pool"][s, table[s, blk]], host[s, blk]), (step, l, s, blk)
+    assert misses > 0
+    with pytest.raises(ValueError):
+        DecodeSession(pi, 3, 2, kv_bits=8, split_attention=True)
+    with pytest.raises(ValueError):
+        DecodeSession(pi, 3, 2, kv_bits=6)
+    pi.close()
+    pi2.close()
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+def test_prompts_into_a_session_and_a_decode_step_over_them(bits):
+    """Prompts of different lengths (none, a token, more than the pool holds): their attention, the cache that they leave, and the next token's
+    attention over the whole of it, which is one more row of the prompt's attention but for the cache's rounding."""
+    from paper_2609_34555_b200.runner import DecodeSession
+    lens = [70, 0, 1, 130]
+    pi = context(n_q_heads=8, n_kv_heads=2, budget_blocks=10, pool_slots=10, max_blocks=12, max_batch=4, n_sink_blocks=1, n_local_blocks=2, n_layers=2)
+    sess = DecodeSession(pi, 4, 2, kv_bits=bits)
+    g = torch.Generator().manual_seed(bits)
+    T = sum(lens) + 4                                                                  # and padding behind the last prompt
+    starts = i32(np.concatenate(([0], np.cumsum(lens))))
+    layers = []
+    for l in range(2):
+        q, k, v = ((torch.randn((T, h, 128), generator=g) * s).to(torch.bfloat16).to(DEV) for h, s in ((8, 1.0), (2, 1.0), (2, 3.0)))
+        out, lse = torch.full((T, 8, 128), 3.0, dtype=torch.bfloat16, device=DEV), torch.zeros((T, 8), device=DEV)
+        sess.load_prompts(l, q, k, v, starts, out, lse)
+        clean(pi)
+        assert (out[-4:] == 3).all() and sess.ctx_len.tolist() == lens
+        layers.append((q, k, v, out, lse))
+    step_q = torch.stack([torch.stack([q[max(0, int(e) - 1)] for e in starts[1:]]) for q, *_ in layers])      # the last token's query once more
+    got = sess.decode_step(step_q)
+    clean(pi)
+    for l, (q, k, v, out, lse) in enumerate(layers):
+        for s, n in enumerate(lens):
+            if n == 0:
+                assert (got[l, s] == 0).all()
+                continue
+            last = out[int(starts[s + 1]) - 1].float()
+            # (weights of a cache in few bits are off by the keys' rounding: 2^-5 of a score of a few units, and half a step of 4 bits, 1 / 30 of a spread of about 6)
+            tol = {16: 0.05, 8: 0.5, 4: 1.0}[bits]
+            assert float((got[l, s].float() - last).abs().max()) <= tol, (l, s)
+        b = sess.bufs[l]
+        assert b.slot_block[0].tolist()[:5] == [0, 1, 2, 3, 4] and b.slot_block[3].tolist() == [0, 1, 2, 3, 4, 5, 6, 7, 8, -1]
+    with pytest.raises(ValueError):
+        sess.load_prompts(0, q, k, v, starts[:-1], out)
+    pi.close()
+
+
+def test_prompt_to_attention_through_pages_rotation_prompt_attention_store_recall():
+    """A ragged batch of prompts: pages, norm + rotation, attention over the prompts, store into an arena, recall into a pool, attention of
+    the last token over everything, against the chain in 64 bits."""
+    from tests.prompt_reference import check, reference
+    pi = context(n_q_heads=8, n_kv_heads=2, budget_blocks=16, pool_slots=16, max_blocks=16, max_batch=4, n_sink_blocks=1, n_local_blocks=1)
+    lens = np.asarray([100, 1, 0, 256])
+    rng = np.random.default_rng(12)
+    cap = int(lens.sum()) + 11
+    table = torch.full((4, 16), -1, dtype=torch.int32, device=DEV)
+    ring, counters = pi.free_page_ring(40)
+    ring.copy_(dev(rng.permutation(40).astype(np.int32)))
+    slots, pos, starts = torch.empty(cap, dtype=torch.int64, device=DEV), torch.empty(cap, dtype=torch.int32, device=DEV), torch.empty(5, dtype=torch.int32, device=DEV)
+    pi.assign_pages(i32([0] * 4), i32(lens), table, ring, counters, token_start=starts, slot_map=slots, positions=pos)
+    qkv = bf(rng.standard_normal((cap, 12 * 128)))
+    q, k, v = qkv[:, :1024].unflatten(1, (8, 128)), qkv[:, 1024:1280].unflatten(1, (2, 128)), qkv[:, 1280:].unflatten(1, (2, 128))
+    freq = (1e4 ** (-np.arange(0, 128, 2) / 128)).astype(np.float32)
+    qo, ko = torch.zeros((cap, 8, 128), dtype=torch.bfloat16, device=DEV), torch.zeros((cap, 2, 128), dtype=torch.bfloat16, device=DEV)
+    pi.qk_norm_rope(q, k, pos, dev(freq), qo, ko)
+    out, lse = torch.full((cap, 8, 128), 3.0, dtype=torch.bfloat16, device=DEV), torch.zeros((cap, 8), device=DEV)
+    pi.prompt_attn(qo, ko, v, starts, out, lse=lse)                                    # the starts that the pages came with
+    arena = torch.zeros((40, pi.kv8_block_bytes), dtype=torch.uint8).pin_memory()
+    pi.kv8_store(ko, v, arena, slots)
+    nb = -(-lens // 16)
+    lists = np.zeros((4, 16, 4), dtype=np.int32)
+    for s in range(4):
+        lists[s, 0] = [0, 0, nb[s], 0]
+    pool = torch.zeros((4, 16, pi.kv8_block_bytes), dtype=torch.uint8, device=DEV)
+    pi.recall_kv8(0, arena, pool, dev(lists), i32((nb > 0).astype(np.int32)), page_table=table)
+    sel = np.where(np.arange(16)[None] < nb[:, None], np.arange(16)[None], -1).astype(np.int32)
+    begin = np.concatenate(([0], np.cumsum(lens)))
+    qd = qo[torch.from_numpy(np.maximum(begin[1:] - 1, 0)).to(DEV)].contiguous()
+    o1, l1 = torch.zeros((4, 8, 128), dtype=torch.bfloat16, device=DEV), torch.zeros((4, 8), device=DEV)
+    pi.sparse_decode_attn_kv8(0, qd, pool, dev(sel), dev(sel), i32(nb), i32(lens), o1, l1)
+    clean(pi)
+    assert starts.tolist() == begin.tolist() and (out[int(begin[-1]):] == 3).all()
+    check(torch.bfloat16, out, lse, reference(qo, ko, v, begin.tolist(), begin.tolist()))
+    kb, vb = ko.float().cpu().numpy(), v.float().cpu().numpy()
+    pools = np.zeros((4, 16, pi.kv8_block_bytes), dtype=np.uint8)
+    for s in range(4):
+        ref.store(pools[s], kb[begin[s]:begin[s + 1]], vb[begin[s]:begin[s + 1]], range(lens[s]), 16)
+    assert np.array_equal(pool.cpu().numpy(), pools)
+    check_attention(pi, dict(pool=pools, blocks=sel, slots=sel, count=nb, ctx=lens, q=qd.float().cpu().numpy()), o1, l1)
+    pi.close()
