@@ -319,8 +319,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     for (int y = 8; y < 128; y += 8) mx4[x] = pa_max3(mx4[x], s[x + y], s[x + y + 4]);
                 }
                 const float mx = fmaxf(pa_max3(mx4[0], mx4[1], mx4[2]), mx4[3]);
-                if (__any_sync(0xffffffffu, mx * c - mc > 8.f)) {
-                    const float m_new = fmaxf(m, mx), mc_new = m_new == PA_NO_MAX ? PA_NO_MAX : m_new * c;
+                const bool over = real && mx * c - mc > 8.f;         // (each row by itself: what its neighbours are does not change its bits)
+                if (__any_sync(0xffffffffu, over)) {
+                    const float m_new = over ? mx : m, mc_new = over ? mx * c : mc;
                     // (far from 0 the reference's own rounding counts: see below)
                     const float alpha = pa_ex2(far_off(mc_new) ? (m - m_new) * c : mc - mc_new);
                     m = m_new;

@@ -75,3 +75,271 @@ def test_fp16(Hq, Hkv, n, m):
     out, lse = run(pi, q, k, v, qs, ks)
     check(q.dtype, out, lse, reference(q, k, v, qs, ks))
     untouched(out, lse, qs)
+
+
+@pytest.mark.parametrize("Hq,Hkv,n,m", [(8, 1, 1, 9000), (8, 2, 5, 4200), (32, 8, 40, 2300), (4, 4, 130, 3000), (16, 1, 17, 1030), (2, 1, 1, 130000)])
+def test_few_queries_over_many_keys(Hq, Hkv, n, m):
+    """Keys shared out over clusters and over both softmax groups."""
+    pi = context(Hq, Hkv)
+    for batch in (1, 3):
+        if batch * m > 140000:
+            continue
+        q, k, v, qs, ks = case(Hq, Hkv, [n] * batch, [m - 37 * i for i in range(batch)], seed=n)
+        out, lse = run(pi, q, k, v, qs, ks)
+        check(q.dtype, out, lse, reference(q, k, v, qs, ks))
+        untouched(out, lse, qs)
+
+
+def test_a_prompt_of_many_blocks_and_a_large_batch():
+    pi = context(4, 1, max_batch=300)
+    for lens in ([1900], [1 + 7 * (i % 29) for i in range(300)]):
+        q, k, v, qs, ks = case(4, 1, lens, lens, seed=len(lens))
+        out, lse = run(pi, q, k, v, qs, None)
+        check(q.dtype, out, lse, reference(q, k, v, qs, ks))
+        untouched(out, lse, qs)
+
+
+def test_random_shapes():
+    r = torch.Generator().manual_seed(11)
+    pick = lambda lo, hi: int(torch.randint(lo, hi + 1, (1,), generator=r))  # noqa: E731
+    for i in range(40):
+        Hkv = (1, 2, 4, 8, 16)[pick(0, 4)]
+        Hq = Hkv * pick(1, 16)
+        batch = pick(1, 9)
+        n = [pick(0, (3, 70, 300)[pick(0, 2)]) for _ in range(batch)]
+        m = [max(0, a + (pick(0, 500) if pick(0, 1) else pick(-40, 10))) for a in n]
+        dtype = torch.bfloat16 if pick(0, 2) else torch.float16
+        pi = context(Hq, Hkv)
+        q, k, v, qs, ks = case(Hq, Hkv, n, m, dtype, seed=i, pad=pick(1, 5))
+        out, lse = run(pi, q, k, v, qs, ks)
+        check(dtype, out, lse, reference(q, k, v, qs, ks))
+        untouched(out, lse, qs)
+        pi.close()
+
+
+def test_strides_and_no_lse():
+    """Slices of a fused projection, heads before tokens, every second token; the first sequence not at the first token."""
+    pi = context(8, 2)
+    g = torch.Generator().manual_seed(3)
+    qs = [5, 90, 200]
+    want = None
+    x = torch.randn((220, 12 * 128), generator=g).to(torch.bfloat16).cuda()
+    q, k, v = x[:, :1024].unflatten(1, (8, 128)), x[:, 1024:1280].unflatten(1, (2, 128)), x[:, 1280:].unflatten(1, (2, 128))
+    heads_first = lambda t: t.transpose(0, 1).contiguous().transpose(0, 1)  # noqa: E731
+    spaced = lambda t: t.repeat_interleave(2, 0)[::2]  # noqa: E731
+    for form in (lambda t: t, lambda t: t.contiguous(), heads_first, spaced):
+        out, lse = torch.full((220, 8, 128), 7.0, dtype=torch.bfloat16, device="cuda"), None
+        pi.prompt_attn(form(q), form(k), form(v), i32(qs), out)
+        torch.cuda.synchronize()
+        assert pi.status()[0] == 0
+        if want is None:
+            check(out.dtype, out, lse, reference(q, k, v, qs, qs))
+            untouched(out, None, qs)
+            want = out
+        assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("n,m", [([200, 61, 3], [200, 61, 3]), ([2, 70], [300, 1000])])
+def test_what_is_not_seen_does_not_reach_a_row(dtype, n, m):
+    """Infinities and NaN in keys and values: rows that see them are what the sums make of them, all others are as without them.  In the
+    tokens behind a sequence, in its neighbours, and in its own future."""
+    pi = context(8, 2)
+    q, k, v, qs, ks = case(8, 2, n, m, dtype, seed=5, pad=40)
+    base, base_lse = run(pi, q, k, v, qs, ks)
+    bad_v = [(ks[1] - 1, 0, 3, float("nan")), (ks[1] - min(m[0], 30), 1, 9, float("inf")), (ks[1], 0, 70, float("-inf")), (ks[-1] + 2, 0, 5, float("nan")), (ks[-1] + 39, 1, 127, float("inf"))]
+    bad_k = [(ks[-1] - 1, 1, 2, float("nan")), (ks[-1] + 1, 0, 0, float("inf"))]
+    for t, h, d, x in bad_v:
+        v[t, h, d] = x
+    for t, h, d, x in bad_k:
+        k[t, h, d] = x
+    out, lse = run(pi, q, k, v, qs, ks)
+    for s in range(len(n)):
+        for i in range(n[s]):
+            row, seen = qs[s] + i, ks[s] + i + m[s] - n[s] + 1
+            for h in range(2):
+                heads = slice(4 * h, 4 * h + 4)
+                if any(kh == h and ks[s] <= t < seen for t, kh, _, _ in bad_k):
+                    assert torch.isnan(out[row, heads].float()).all()
+                    continue
+                assert torch.equal(lse[row, heads], base_lse[row, heads])
+                hit = {d: x for t, vh, d, x in bad_v if vh == h and ks[s] <= t < seen}
+                for d in range(128):
+                    got = out[row, heads, d].float()
+                    if d in hit:
+                        assert torch.equal(got, torch.full_like(got, hit[d])) or (hit[d] != hit[d] and torch.isnan(got).all()), (s, i, h, d)
+                keep = [d for d in range(128) if d not in hit]
+                assert torch.equal(out[row, heads][:, keep], base[row, heads][:, keep]), (s, i, h)
+
+
+@pytest.mark.parametrize("dtype,scale", [(torch.bfloat16, 30.0), (torch.bfloat16, 1e5), (torch.bfloat16, 1e9), (torch.bfloat16, 1e15), (torch.float16, 100.0)])
+def test_scores_of_any_size(dtype, scale):
+    """Queries and keys so large that one key takes all the weight: the output is its value, the log-sum-exp its score."""
+    pi = context(4, 2)
+    q, k, v, qs, ks = case(4, 2, [150, 7], [400, 7], dtype, seed=9, scale=scale if dtype == torch.bfloat16 else 1.0)
+    k = (k * scale).to(dtype)
+    out, lse = run(pi, q, k, v, qs, ks)
+    o, l, _, _, owned = reference(q, k, v, qs, ks)
+    out, lse = out.cpu().double(), lse.cpu().double()
+    # a score is a sum of 128 products in 32 bits, off by at most 128 cuts of 2^-23 of the sum of magnitudes
+    size = (q.abs().float().amax(-1).cpu().double() * k.abs().float().amax().cpu().double() * 128 / 128 ** 0.5)
+    off = 128 * 2.0 ** -23 * size
+    assert bool(((lse - l).abs() <= off + 2.0 ** -16 * (1 + l.abs()))[owned].all())
+    # rows whose two largest scores are further apart than that: the weights are known
+    for s in range(2):
+        for i in range(qs[s], qs[s + 1]):
+            for h in range(4):
+                seen = ks[s + 1] - (qs[s + 1] - 1 - i)
+                z = k[ks[s]:seen, h // 2].cpu().double() @ q[i, h].cpu().double() / 128 ** 0.5
+                top = torch.topk(z, min(2, len(z)))
+                if len(z) == 1 or float(top.values[0] - top.values[1]) > 2 * float(off[i, h]) + 20:
+                    want = v[ks[s] + int(top.indices[0]), h // 2].cpu().double()
+                    assert bool(((out[i, h] - want).abs() <= torch.finfo(dtype).eps * want.abs() + 2.0 ** -20).all())
+
+
+def test_scores_that_rise_from_key_to_key():
+    """Every tile's largest score is above the last one's by more than a factor of 2^8 after the exponential: the reference moves each time."""
+    pi = context(4, 1)
+    n = 700
+    q, k, v, qs, ks = case(4, 1, [n], [n], seed=2)
+    q[:], k[:] = 0, 0
+    q[..., 0] = 1.0
+    k[..., 0] = (torch.arange(k.shape[0]) * 0.5).to(torch.bfloat16).cuda()[:, None]
+    k[:, :, 1:] = torch.randn(k[:, :, 1:].shape, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+    q[..., 1:] = 0.1
+    out, lse = run(pi, q, k, v, qs, ks)
+    check(q.dtype, out, lse, reference(q, k, v, qs, ks))
+
+
+def test_heads_whose_query_is_no_number_leave_the_others_alone():
+    pi = context(8, 2)
+    q, k, v, qs, ks = case(8, 2, [90, 1], [90, 500], seed=4)
+    base, base_lse = run(pi, q, k, v, qs, ks)
+    q[17, 5, 3] = float("nan")
+    q[60, 0] = float("inf")
+    q[90, 7, 127] = float("nan")
+    out, lse = run(pi, q, k, v, qs, ks)
+    hit = torch.zeros(q.shape[:2], dtype=torch.bool)
+    hit[17, 5] = hit[60, 0] = hit[90, 7] = True
+    assert torch.equal(out.cpu()[~hit], base.cpu()[~hit]) and torch.equal(lse.cpu()[~hit], base_lse.cpu()[~hit])
+    assert bool(torch.isnan(out.cpu()[hit].float()).all())
+
+
+def test_bounds_that_make_no_sense_are_reported_and_left_out():
+    pi = context(8, 2)
+    q, k, v, qs, ks = case(8, 2, [20, 30, 10], [50, 30, 60], pad=0)
+    good, good_lse = run(pi, q, k, v, qs, ks)
+    for bad_q, bad_k, which in (([0, 20, 10, 60], ks, 1), (qs, [0, 50, 80, 141], 2), ([-1, 20, 50, 60], ks, 0), (qs, [0, 50, 40, 140], 1)):
+        out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+        pi.prompt_attn(q, k, v, i32(bad_q), out, k_start=i32(bad_k), lse=lse)
+        torch.cuda.synchronize()
+        got = pi.status()
+        assert got[0] == -8 and got[1] == 8 and got[2] == which, got
+        pi.clear_status()
+        # (the sequence behind one whose bounds decrease may name tokens of an earlier one too: those rows are either's)
+        spans = [range(x, y) for x, y in zip(bad_q, bad_q[1:]) if 0 <= x <= y <= 60]
+        for s in range(3):
+            if bad_q[s:s + 2] == qs[s:s + 2] and bad_k[s:s + 2] == ks[s:s + 2]:
+                rows = [t for t in range(qs[s], qs[s + 1]) if sum(t in x for x in spans) == 1]
+                assert len(rows) >= 10 and torch.equal(out[rows], good[rows]) and torch.equal(lse[rows], good_lse[rows])
+
+
+def test_no_queries_no_keys():
+    pi = context(8, 2)
+    q, k, v, qs, ks = case(8, 2, [3, 4], [0, 0], pad=0)
+    assert k.shape[0] == 0
+    out, lse = run(pi, q, k, v, qs, ks)
+    assert bool((out == 0).all()) and bool((lse == -float("inf")).all())
+    out, lse = torch.zeros((0, 8, 128), dtype=torch.bfloat16, device="cuda"), torch.zeros((0, 8), device="cuda")
+    pi.prompt_attn(q[:0], k, v, i32([0, 0]), out, lse=lse)
+    torch.cuda.synchronize()
+    assert pi.status()[0] == 0
+
+
+def test_the_front_end_checks_devices_types_and_shapes():
+    pi = context(8, 2, max_batch=2)
+    q, k, v, qs, ks = case(8, 2, [9], [9], pad=0)
+    out, s = torch.zeros_like(q), i32([0, 9])
+    for change, error in (
+            (lambda: pi.prompt_attn(q.float(), k, v, s, out), TypeError), (lambda: pi.prompt_attn(q, k.half(), v, s, out), TypeError),
+            (lambda: pi.prompt_attn(q.cpu(), k, v, s, out), TypeError), (lambda: pi.prompt_attn(q, k, v[:5], s, out), ValueError),
+            (lambda: pi.prompt_attn(q[:, :6], k, v, s, out), ValueError), (lambda: pi.prompt_attn(q, k, v, s.long(), out), TypeError),
+            (lambda: pi.prompt_attn(q, k, v, s[:1], out), ValueError), (lambda: pi.prompt_attn(q, k, v, s, out.half()), TypeError),
+            (lambda: pi.prompt_attn(q, k, v, s, out[:5]), ValueError), (lambda: pi.prompt_attn(q, k, v, s, out, k_start=i32([0, 1, 9])), ValueError),
+            (lambda: pi.prompt_attn(q, k, v, s, out, lse=torch.zeros((9, 2), device="cuda")), ValueError),
+            (lambda: pi.prompt_attn(q.transpose(1, 2).contiguous().transpose(1, 2), k, v, s, out), ValueError)):
+        with pytest.raises(error):
+            change()
+    x = torch.zeros((9, 12 * 128 + 4), dtype=torch.bfloat16, device="cuda")
+    for change, code in ((lambda: pi.prompt_attn(q, k, v, i32([0, 3, 6, 9]), out), -1),                      # more sequences than the context has
+                         (lambda: pi.prompt_attn(x[:, :1024].unflatten(1, (8, 128)), k, v, s, out), -2),     # tokens 8 bytes off
+                         (lambda: pi.prompt_attn(q, k[:1].expand(9, 2, 128), v, s, out), -1)):               # one key for all tokens
+        with pytest.raises(pkg.binding.PiError) as e:
+            change()
+        assert e.value.code == code
+    torch.cuda.synchronize()
+    assert pi.status()[0] == 0 and bool((out == 0).all())
+
+
+def test_on_two_streams_at_once_and_in_a_replayed_graph():
+    pi = context(32, 8)
+    cases = [case(32, 8, [100, 1, 300], [100, 700, 900], seed=s) for s in (1, 2)]
+    want = [run(pi, *c) for c in cases]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    bounds = [(i32(c[3]), i32(c[4])) for c in cases]
+    outs = [(torch.full_like(c[0], 7.0), torch.full(c[0].shape[:2], 7.0, device="cuda")) for c in cases]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for (q, k, v, *_), (qs, ks), (o, l), st in zip(cases, bounds, outs, streams):
+            pi.prompt_attn(q, k, v, qs, o, k_start=ks, lse=l, stream=st)
+    torch.cuda.synchronize()
+    for (o, l), (wo, wl) in zip(outs, want):
+        assert torch.equal(o, wo) and torch.equal(l, wl)
+    # captured once for a capacity; replayed for other sequences, among them fewer tokens than the capacity
+    q, k, v = torch.zeros((500, 32, 128), dtype=torch.bfloat16, device="cuda"), *(torch.zeros((2000, 8, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    qs, ks = i32([0] * 4), i32([0] * 4)
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        pi.prompt_attn(q, k, v, qs, out, k_start=ks, lse=lse)
+    for n, m in (([100, 1, 300], [100, 700, 900]), ([0, 0, 0], [0, 0, 0]), ([5, 495, 0], [5, 600, 3])):
+        cq, ck, cv, a, b = case(32, 8, n, m, seed=sum(n), pad=0)
+        q[:a[-1]], k[:b[-1]], v[:b[-1]] = cq, ck, cv
+        q[a[-1]:], k[b[-1]:], v[b[-1]:] = float("nan"), float("nan"), float("nan")
+        qs.copy_(i32(a)); ks.copy_(i32(b))
+        out.fill_(7.0); lse.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert pi.status()[0] == 0
+        check(q.dtype, out[:a[-1]], lse[:a[-1]], reference(cq, ck, cv, a, b))
+        untouched(out, lse, a)
+
+
+def test_a_wait_that_runs_out_is_reported_and_the_next_call_works():
+    """The last values of every piece of work never arrive (a test's switch): every CTA gives up after a millisecond, says so and ends."""
+    held = context(8, 2, wait_limit_us=1000, test_hold_producer=1)
+    q, k, v, qs, ks = case(8, 2, [300, 2], [300, 1000])
+    out = torch.zeros_like(q)
+    held.prompt_attn(q, k, v, i32(qs), out, k_start=i32(ks))
+    torch.cuda.synchronize()
+    assert held.status()[0] == -7 and held.status()[1] == 8
+    held.close()
+    pi = context(8, 2)
+    out, lse = run(pi, q, k, v, qs, ks)
+    check(q.dtype, out, lse, reference(q, k, v, qs, ks))
+
+
+def test_keys_beyond_32_bits_of_an_address():
+    """Keys 5 GB apart in one tensor: the sequences at its two ends."""
+    pi = context(16, 16)
+    q, k, v, qs, ks = case(16, 16, [30, 40], [300, 70], pad=0)
+    rows = 1300000                                                                     # x 16 heads x 256 bytes
+    far = [torch.zeros((rows, 16, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for f, x in zip(far, (k, v)):
+        f[:300], f[rows - 70:] = x[:300], x[300:]
+    out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+    pi.prompt_attn(q, *far, i32([0, 30, 30, 70]), out, k_start=i32([0, 300, rows - 70, rows]), lse=lse)
+    torch.cuda.synchronize()
+    assert pi.status()[0] == 0
+    check(q.dtype, out, lse, reference(q, k, v, qs, ks))
