@@ -51,6 +51,18 @@ __device__ __forceinline__ uint32_t kv8_round4(uint32_t x0, uint32_t x1, float i
     }
     return got[0] | got[1] << 16;
 }
+// The same where everything is known to be a finite number, in a third of the operations.
+__device__ __forceinline__ uint32_t kv8_round4_finite(uint32_t x0, uint32_t x1, float inverse) {
+    const uint32_t a = kv8_pair(__uint_as_float(x0 << 16) * inverse, __uint_as_float(x0 & 0xffff0000u) * inverse);
+    const uint32_t b = kv8_pair(__uint_as_float(x1 << 16) * inverse, __uint_as_float(x1 & 0xffff0000u) * inverse);
+    return a | b << 16;
+}
+// The larger magnitudes of two pairs; NaN where either is NaN.  (One operation with the absolute value in it.)
+__device__ __forceinline__ uint32_t kv8_larger(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a), __habs2(*reinterpret_cast<const __nv_bfloat162*>(&b)));
+    return *reinterpret_cast<const uint32_t*>(&m);
+}
+__device__ __forceinline__ bool kv8_odd(uint32_t w) { return ((w & 0x7fff7fffu) + 0x00800080u) & 0x80008000u; }      // infinite or NaN, either half
 __device__ __forceinline__ float2 kv8_values(uint32_t pair) {
     uint32_t h;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<unsigned short>(pair)));
