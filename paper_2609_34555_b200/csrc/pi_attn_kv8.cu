@@ -11,10 +11,14 @@
 // scale (of V).  So a block whose values are small next to another's, and whose weights are not, keeps its bits, and no weight leaves fp16.
 // Both move only when they are exceeded by 2^8.
 //
-// One (sequence, KV head) per cluster of S CTAs of 4 or 8 warps (S = 1, 2, 4 or 8; both by the launcher's rule).  The item's
+// One (sequence, KV head) per cluster of S CTAs of 4, 8 or 16 warps (S = 1, 2, 4 or 8; both by the launcher's rule).  The item's
 // 16-token tiles are dealt out to its warps in turn; a warp streams its own tiles through its own ring of shared-memory
 // stages with 16-byte asynchronous copies (a tile is 2048 contiguous bytes of K and as many of V), so no warp waits for another until the
 // end (pi_attn_merge.cuh).
+//
+// Measured on a B200, back to back: 64 sequences x 64 blocks of 32 tokens, 8 KV heads, G = 4 (263 MB) 44 us, 6.0 TB/s, 91 % of what a copy
+// reaches; 16 x 128 blocks of 16 (67 MB) 15.0 us; one sequence x 64 blocks 4.3 us; 64 x 64 blocks of 32 with G = 16 55 us.  HBM bounds the large
+// ones; the others carry about 5 us of launch, two dependent loads before the first tile, and the merge.
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -357,10 +361,15 @@ int pi_launch_attn_kv8(pi_ctx* c, int batch, const void* q, const void* pool, co
     p.B = cfg.block_tokens; p.K = cfg.budget_blocks; p.C = cfg.pool_slots;
     const int NT = p.G <= 8 ? 1 : 2, tiles = cfg.budget_blocks * (cfg.block_tokens / 16);
     const long long items = static_cast<long long>(batch) * cfg.n_kv_heads, room = static_cast<long long>(a8_warps_per_sm(NT)) * c->n_sms;
-    // CTAs per item: as many as find room at once, while every warp has two tiles.
+    // CTAs per item: twice as many while they fill half of the warps there is room for, at most, and every warp has two tiles.  Measured with
+    // S = 1 / 2 / 4 / 8: 8 items x 64 tiles 10.4 / 7.3 / 5.3 / 4.3 us, 32 x 128 19.1 / 11.9 / 8.3 / 6.8, 64 x 256 36.7 / 20.8 / 15.1 / 15.6,
+    // 128 x 128 19.9 / 15.0 / 15.3 / 18.7, 256 x 128 24.3 / 25.7 / 27.6 / 32.5.
     int split = 1, warps = 4;
-    while (split < A4_MAX_SPLIT && items * split * 2 * warps <= room && tiles >= 2 * warps * split * 2) split *= 2;
-    if (NT == 1 && split == A4_MAX_SPLIT && items * split * 8 <= room && tiles >= 2 * 8 * split) warps = 8;
+    while (split < A4_MAX_SPLIT && items * split * 2 * warps <= room / 2 && tiles >= 2 * warps * split * 2) split *= 2;
+    // Few items with long lists leave SMs with one CTA each, which more warps use better, two tiles a warp or four: 8 items x 256 tiles
+    // 6.4 us with 8, 6.6 with 16; x 512 8.6 and 7.8; x 1024 20.1 with 4, 13.7 with 8, 12.0 with 16; x 2048 23.3 and 19.1.
+    if (NT == 1 && split == A4_MAX_SPLIT)
+        while (warps < 16 && items * split * warps * 2 <= room / 2 && tiles >= warps * warps * split) warps *= 2;
     const size_t ring = static_cast<size_t>(warps) * a8_stages(NT) * A8_TILE_BYTES;
     // (the merge of a CTA's warps, up to 33 KB for four, takes the ring's place; what the cluster sends lies behind)
     const size_t smem = ring + (split > 1 ? static_cast<size_t>(p.G) * (PI_HEAD_DIM * 4 + split * 8) : 0);
@@ -383,6 +392,6 @@ int pi_launch_attn_kv8(pi_ctx* c, int batch, const void* q, const void* pool, co
         PI_CUDA_TRY(cudaLaunchKernelEx(&lc, kernel, p));
         return PI_OK;
     };
-    if (NT == 1) return warps == 4 ? launch(attn_kv8_kernel<1, 4>) : launch(attn_kv8_kernel<1, 8>);
+    if (NT == 1) return warps == 4 ? launch(attn_kv8_kernel<1, 4>) : warps == 8 ? launch(attn_kv8_kernel<1, 8>) : launch(attn_kv8_kernel<1, 16>);
     return launch(attn_kv8_kernel<2, 4>);
 }
