@@ -47,6 +47,7 @@ struct PromptParams {
     long long wait_cycles, v_tok, v_head;
     float scale_log2;                               // log2(e) / sqrt(D)
     int n_seqs, Hq, Hkv, G, tq, n_q, n_k;           // tq: tokens of a query tile
+    bool wide;                                      // out is aligned to 32 bytes
     int hold_last;                                  // test only: an item's last V tile is never fetched
 };
 
@@ -442,13 +443,18 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         for (int y = 0; y < 8; ++y)
                             asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(at + (((8 * x + y) ^ (r & 31)) << 4)), "f"(o[4 * y]), "f"(o[4 * y + 1]), "f"(o[4 * y + 2]), "f"(o[4 * y + 3]) : "memory");
                     } else {
+                        // (32 bytes a store where the output allows it: a lane's stores go to a row of its own, one line each)
                         uint4* to = reinterpret_cast<uint4*>(static_cast<T*>(p.out) + row * PI_HEAD_DIM + 32 * x);
+                        uint32_t u[16];
 #pragma unroll
-                        for (int y = 0; y < 4; ++y) {
-                            uint32_t u[4];
+                        for (int y = 0; y < 16; ++y) u[y] = none ? 0u : Form<T>::pack(o[2 * y] * inv, o[2 * y + 1] * inv);
+                        if (p.wide) {
 #pragma unroll
-                            for (int z = 0; z < 4; ++z) u[z] = none ? 0u : Form<T>::pack(o[8 * y + 2 * z] * inv, o[8 * y + 2 * z + 1] * inv);
-                            to[y] = make_uint4(u[0], u[1], u[2], u[3]);
+                            for (int y = 0; y < 16; y += 8)
+                                asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to + y / 4), "r"(u[y]), "r"(u[y + 1]), "r"(u[y + 2]), "r"(u[y + 3]), "r"(u[y + 4]), "r"(u[y + 5]), "r"(u[y + 6]), "r"(u[y + 7]) : "memory");
+                        } else {
+#pragma unroll
+                            for (int y = 0; y < 16; y += 4) to[y / 4] = make_uint4(u[y], u[y + 1], u[y + 2], u[y + 3]);
                         }
                     }
                 }
@@ -846,6 +852,7 @@ int pi_launch_prompt_attn(pi_ctx* c, int n_seqs, int dtype, int n_q, int n_k, co
         if (rc != PI_OK) return rc;
     }
     p.hold_last = cfg.test_hold_producer;
+    p.wide = (reinterpret_cast<uintptr_t>(out) & 31u) == 0;
     const long long per_block = 2 * p.tq, seqs = n_seqs < n_q ? n_seqs : n_q, blocks = (n_q + seqs * (per_block - 1)) / per_block, items = blocks * p.Hkv;
     // CTAs that share an item: where the items leave SMs without work and the keys are many, a cluster for each, up to a power of two that fits the
     // GPU once (and eight: fewer than eight clusters of 16 are resident at a time).  A cluster costs 3 to 5 us more than a CTA, and a K/V tile 1 to 2 us:
