@@ -25,9 +25,10 @@ namespace {
 using namespace pi_attn;
 
 constexpr int PA_THREADS = 384;                  // three warpgroups: softmax of A, softmax of B, the rest (two of its warps have nothing to do)
-// registers of a softmax thread and of the others: 256 x 200 + 128 x 104 of the 384 x 168 that the block is launched with
-constexpr int PA_SOFTMAX_REGS = 200, PA_OTHER_REGS = 104;
+// registers of a softmax thread and of the others: 256 x 208 + 128 x 88 of the 384 x 168 that the block is launched with
+constexpr int PA_SOFTMAX_REGS = 208, PA_OTHER_REGS = 88;
 static_assert(256 * PA_SOFTMAX_REGS + 128 * PA_OTHER_REGS <= PA_THREADS * 168, "more than the block has");
+constexpr int PA_SOFTMAX = 256;                     // threads of the softmax warps
 constexpr int PA_ROWS = 128;                        // rows of a query tile, and tokens of a K or V tile
 constexpr int PA_STAGES = 5;
 constexpr int PA_MAX_SPLIT = 8;                     // CTAs of a cluster that share an item
@@ -212,6 +213,23 @@ struct Plan {
     __device__ __forceinline__ int end(int t) const { return t ? tiles_b : tiles_a; }
 };
 
+// The waits and arrivals across a cluster: what was written before the arrival is seen behind the wait.
+__device__ __forceinline__ bool mbar_try_cluster(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort, long long limit) {
+    const long long t0 = clock64();
+    while (!mbar_try_cluster(bar, parity)) {
+        if (*abort) return false;
+        if (clock64() - t0 > limit) { *abort = 1; return false; }
+    }
+    return true;
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+}
 __device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
     float2 v;
     asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
@@ -226,13 +244,14 @@ __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
 // Barriers, in 8-byte places.
 enum : uint32_t {
     B_Q_FULL = 0, B_Q_EMPTY = 1, B_DRAINED = 2, B_MERGED = 3, B_HALF = 4, B_NEXT = 5, B_ITEM_FULL = 6, B_ITEM_EMPTY = 8, B_S_FULL = 10, B_P_FULL = 12, B_O_FULL = 14,
-    B_ALL = 16, B_KV_FULL = 17, B_KV_EMPTY = B_KV_FULL + PA_STAGES, B_V_GOOD = B_KV_EMPTY + PA_STAGES, B_COUNT = B_V_GOOD + PA_STAGES
+    B_ALL = 16, B_SHARE_FULL = 17, B_SHARE_EMPTY = 18, B_WANTED = 19, B_KV_FULL = 20, B_KV_EMPTY = B_KV_FULL + PA_STAGES, B_V_GOOD = B_KV_EMPTY + PA_STAGES, B_COUNT = B_V_GOOD + PA_STAGES
 };
 
 constexpr uint32_t PA_ML_AT = 2 * PA_ROWS * 512;    // a cluster's shares: [256 rows][128] in 32 bits, then every row's reference and sum
+constexpr int PA_FEW = 64;                          // so many rows have their shares in query tile B's place, which such an item leaves free
 
-// SPLIT: a cluster of CTAs shares an item, each with a run of its K/V tiles.  Else a CTA takes one item after the other: it begins with its own
-// place in the grid and then takes over CTAs that have not begun yet, so that loads, barriers and tensor memory run on.
+// A CTA takes one item after the other: it begins with its own place in the grid and then takes over CTAs that have not begun yet, so that loads,
+// barriers and tensor memory run on.  SPLIT: a cluster of CTAs does so, and shares every item, each with a run of its K/V tiles.
 template <typename T, bool SPLIT>
 __global__ void __launch_bounds__(PA_THREADS, 1)
 prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, PromptParams p) {
@@ -241,6 +260,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     __shared__ __align__(8) uint64_t s_bar[B_COUNT];
     __shared__ Item s_item[2];
     __shared__ float2 s_ml[PA_ROWS];                // tile A alone: reference and sum of group B's rows
+    __shared__ float2 s_share[PA_FEW];              // SPLIT, few rows: reference and sum of the CTA's share
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort, s_odd[2];               // s_odd: values that are no numbers were taken out of a tile
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -251,7 +271,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     if (tid == 0) {
         for (uint32_t i = 0; i < B_COUNT; ++i) {
             const bool by_warps = i == B_P_FULL || i == B_P_FULL + 1 || i == B_MERGED || i == B_HALF;
-            mbar_init(bar(i), by_warps ? 4 : i == B_ALL ? 8 : i == B_ITEM_EMPTY || i == B_ITEM_EMPTY + 1 ? 11 : 1);
+            mbar_init(bar(i), by_warps ? 4 : i == B_ALL ? 8 : i == B_SHARE_FULL || i == B_SHARE_EMPTY ? 8 * split : i == B_ITEM_EMPTY || i == B_ITEM_EMPTY + 1 ? 11 * split : 1);
         }
         s_abort = 0;
         s_odd[0] = s_odd[1] = 0;
@@ -265,19 +285,29 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     pi_grid_dependency_wait();
     pi_launch_dependents();
     tc_fence_before();
-    __syncthreads();
+    if (SPLIT) cluster_sync_all();                  // (the others' barriers are there too)
+    else __syncthreads();
     tc_fence_after();
     const uint32_t tmem = s_tmem;
     volatile int* abort = &s_abort;
+    // a wait for what this CTA, or with SPLIT another of the cluster, has written
+    auto wait_here = [&](uint32_t place, uint32_t parity) { return SPLIT ? mbar_wait_cluster(bar(place), parity, abort, p.wait_cycles) : mbar_wait(bar(place), parity, abort, p.wait_cycles); };
     // item number `it` of this CTA, for the roles that are told
     auto item_of = [&](int it, Item& w) -> bool {
-        if (!mbar_wait(bar(B_ITEM_FULL + (it & 1)), (it >> 1) & 1, abort, p.wait_cycles)) return false;
+        if (!wait_here(B_ITEM_FULL + (it & 1), (it >> 1) & 1)) return false;
         w = s_item[it & 1];
         return w.h >= 0;
     };
     auto done_with = [&](int it) {
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_ITEM_EMPTY + (it & 1)));
+        if (lane != 0) return;
+        if (SPLIT) mbar_arrive_cluster(map_shared_rank(bar(B_ITEM_EMPTY + (it & 1)), 0));      // rank 0 tells the cluster its items
+        else mbar_arrive(bar(B_ITEM_EMPTY + (it & 1)));
+    };
+    // one arrival of this warp at the same barrier of every CTA of the cluster
+    auto arrive_at_all = [&](uint32_t place) {
+        __syncwarp();
+        if (lane < split) mbar_arrive_cluster(map_shared_rank(bar(place), lane));
     };
 
     if (warp < 8) {
@@ -398,10 +428,13 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     mc = top;
                 }
             }
-            if (SPLIT) {                            // Q's and the ring's place is free when both groups have their O
+            const bool few = plan.pair && plan.n_a * p.G <= PA_FEW;
+            const uint32_t share = smem + (few ? PA_TILE : 0), share_ml = few ? smem_u32(s_share) : smem + PA_ML_AT;
+            if (SPLIT) {
+                // the last item's shares have been read by all; Q's and the ring's place is free when both groups have their O
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(B_ALL));
-                if (!mbar_wait(bar(B_ALL), 0, abort, p.wait_cycles)) { alive = false; break; }
+                if (!mbar_wait(bar(B_ALL), it & 1, abort, p.wait_cycles) || (it > 0 && !mbar_wait_cluster(bar(B_SHARE_EMPTY), (it - 1) & 1, abort, p.wait_cycles))) { alive = false; break; }
             }
             const bool none = l == 0.f;             // (a NaN among the sums has to come through)
             const float inv = none ? 0.f : 1.f / l;
@@ -438,7 +471,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         }
                     }
                     if (SPLIT) {                    // the CTA's share of the row, in 32 bits, where the cluster finds it (the ring is done with)
-                        const uint32_t at = smem + static_cast<uint32_t>(128 * t + r) * 512u;
+                        const uint32_t at = share + static_cast<uint32_t>(128 * t + r) * 512u;
 #pragma unroll
                         for (int y = 0; y < 8; ++y)
                             asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(at + (((8 * x + y) ^ (r & 31)) << 4)), "f"(o[4 * y]), "f"(o[4 * y + 1]), "f"(o[4 * y + 2]), "f"(o[4 * y + 3]) : "memory");
@@ -458,10 +491,66 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         }
                     }
                 }
-                if (SPLIT) asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(smem + PA_ML_AT + static_cast<uint32_t>(128 * t + r) * 8u), "f"(mc), "f"(l) : "memory");
-                else if (real && p.lse) p.lse[row] = none ? -INFINITY : (mc + log2f(l)) * 0.6931471805599453f;
+                if (SPLIT) {
+                    if (real) asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(share_ml + static_cast<uint32_t>(128 * t + r) * 8u), "f"(mc), "f"(l) : "memory");
+                } else if (real && p.lse) p.lse[row] = none ? -INFINITY : (mc + log2f(l)) * 0.6931471805599453f;
             }
             tc_fence_before();
+            if (SPLIT) {
+                // ---- the cluster's shares of every row into one: rank r concludes every `split`-th row; four channels a thread
+                arrive_at_all(B_SHARE_FULL);
+                if (!mbar_wait_cluster(bar(B_SHARE_FULL), it & 1, abort, p.wait_cycles)) { alive = false; break; }
+                const int rows = few ? PA_FEW : plan.pair ? PA_ROWS : 2 * PA_ROWS;
+                // (two quads a round, from two CTAs at a time: what comes from them takes about a microsecond)
+                constexpr int AT_ONCE = 2;
+                for (int x0 = tid; x0 < rows / split * 32; x0 += AT_ONCE * PA_SOFTMAX) {
+                    float4 o[AT_ONCE];
+                    float top[AT_ONCE], sum_of[AT_ONCE];
+                    size_t row_of[AT_ONCE];
+                    bool real_of[AT_ONCE];
+#pragma unroll
+                    for (int u = 0; u < AT_ONCE; ++u) {
+                        const int x = x0 + u * PA_SOFTMAX, rr = (x >> 5) * split + rank, of = rr >> 7, in = rr & 127, to = in / p.G;
+                        real_of[u] = x < rows / split * 32 && to < (of ? plan.n_b : plan.n_a);
+                        row_of[u] = static_cast<size_t>(w.q0 + w.first + of * p.tq + to) * p.Hq + static_cast<size_t>(w.h) * p.G + (in - to * p.G);
+                        o[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        top[u] = PA_NO_MAX;
+                        sum_of[u] = 0.f;
+                    }
+#pragma unroll 2
+                    for (int k = 0; k < split; ++k) {
+                        float2 ml[AT_ONCE];
+                        float4 v[AT_ONCE];
+#pragma unroll
+                        for (int u = 0; u < AT_ONCE; ++u) {
+                            const int x = x0 + u * PA_SOFTMAX, rr = (x >> 5) * split + rank;
+                            if (!real_of[u]) continue;
+                            ml[u] = ld_cluster2(map_shared_rank(share_ml + static_cast<uint32_t>(rr) * 8u, k));
+                            v[u] = ld_cluster4(map_shared_rank(share + static_cast<uint32_t>(rr) * 512u + (((x & 31) ^ (rr & 31)) << 4), k));
+                        }
+#pragma unroll
+                        for (int u = 0; u < AT_ONCE; ++u) {
+                            if (!real_of[u]) continue;
+                            const float most = fmaxf(top[u], ml[u].x), f = pa_ex2(ml[u].x - most), was = pa_ex2(top[u] - most);
+                            sum_of[u] = sum_of[u] * was + ml[u].y * f;
+                            o[u].x = o[u].x * was + v[u].x * f; o[u].y = o[u].y * was + v[u].y * f;
+                            o[u].z = o[u].z * was + v[u].z * f; o[u].w = o[u].w * was + v[u].w * f;
+                            top[u] = most;
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < AT_ONCE; ++u) {
+                        if (!real_of[u]) continue;
+                        const int quad = (x0 + u * PA_SOFTMAX) & 31;
+                        const bool nothing = sum_of[u] == 0.f;
+                        const float by = nothing ? 0.f : 1.f / sum_of[u];
+                        *reinterpret_cast<uint2*>(static_cast<T*>(p.out) + row_of[u] * PI_HEAD_DIM + 4 * quad) =
+                            nothing ? make_uint2(0u, 0u) : make_uint2(Form<T>::pack(o[u].x * by, o[u].y * by), Form<T>::pack(o[u].z * by, o[u].w * by));
+                        if (p.lse && quad == 0) p.lse[row_of[u]] = nothing ? -INFINITY : (top[u] + log2f(sum_of[u])) * 0.6931471805599453f;
+                    }
+                }
+                arrive_at_all(B_SHARE_EMPTY);
+            }
             if (plan.pair) {                        // B's O may be written anew when A has read it
                 __syncwarp();
                 if (t == 0) {
@@ -479,12 +568,26 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         if (warp == 9) {
             // ---- TMA: Q, then K0 V0 K1 V1 ...
             uint32_t n = 0u, items = 0u;            // loads, and items with any, so far
-            bool alive = true, q_issued = false;
+            bool alive = true, q_issued = false, few_before = true;
+            int read = 0;                           // items whose shares have been read, as far as this warp has waited for it
             Item w;
             for (int it = 0; alive && item_of(it, w); ++it) {
                 const Plan plan(p, w, rank, split);
                 done_with(it);
-                if (plan.hi <= plan.lo) continue;
+                if (SPLIT) {
+                    // Where the last item's shares lie in the way of this one's loads, they have to have been read; those of the one before
+                    // that have been, or will be in a moment (and every phase of the barrier is waited for once).
+                    const bool in_the_way = it > 0 && (!few_before || plan.n_b);
+                    for (; read < (in_the_way ? it : it - 1); ++read)
+                        if (!mbar_wait_cluster(bar(B_SHARE_EMPTY), read & 1, abort, p.wait_cycles)) { alive = false; break; }
+                    if (!alive) break;
+                    if (in_the_way) asm volatile("fence.proxy.async;" ::: "memory");
+                    few_before = plan.pair && plan.n_a * p.G <= PA_FEW;
+                }
+                if (plan.hi <= plan.lo) {
+                    if (rank == 0 && lane == 0) mbar_arrive(bar(B_WANTED));
+                    continue;
+                }
                 if (items && !mbar_wait(bar(B_Q_EMPTY), (items - 1) & 1u, abort, p.wait_cycles)) { alive = false; break; }
                 if (lane == 0) {
                     const uint32_t bytes = static_cast<uint32_t>(p.tq) * p.G * 128u;
@@ -505,6 +608,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     }
                     __syncwarp();
                 }
+                // (what comes next is asked for when this item's loads have all been issued, and no sooner: until then others may come to it first)
+                if (rank == 0 && lane == 0) mbar_arrive(bar(B_WANTED));
             }
             if (!alive || *abort) {                 // copies in flight end before the CTA does
                 volatile int none = 0;
@@ -711,15 +816,15 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 }
                 done_with(it);
             }
-        } else {
-            // ---- warp 10: which items are this CTA's.  Blocks are counted from the last one of the last sequence, so that the longest of a
+        } else if (rank == 0) {
+            // ---- warp 10: which items are this CTA's, or its cluster's.  Blocks are counted from the last one of the last sequence, so that the longest of a
             // sequence come first; KV heads innermost.
             const int per_block = 2 * p.tq;
             const Span mine = span_of(p, lane, blockIdx.x == 0);
             int total = (mine.n + per_block - 1) / per_block;
             for (int s0 = 32; s0 < p.n_seqs; s0 += 32) total += (span_of(p, s0 + lane, blockIdx.x == 0).n + per_block - 1) / per_block;
             total = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(total)));
-            unsigned place = blockIdx.x / static_cast<unsigned>(split);
+            unsigned place = blockIdx.x / static_cast<unsigned>(split);      // (of a cluster: its first CTA's)
             uint32_t asked = 0u;
             bool more = true;
             for (int it = 0;; ++it) {
@@ -749,15 +854,24 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         at -= __shfl_sync(0xffffffffu, upto, 31);
                     }
                 }
-                if (it >= 2 && !mbar_wait(bar(B_ITEM_EMPTY + (it & 1)), ((it >> 1) - 1) & 1, abort, p.wait_cycles)) break;
-                if (lane == 0) {
+                if (it >= 2 && !wait_here(B_ITEM_EMPTY + (it & 1), ((it >> 1) - 1) & 1)) break;
+                if (SPLIT) {                        // lane k tells rank k
+                    if (lane < split) {
+                        const uint32_t at = map_shared_rank(smem_u32(&s_item[it & 1]), lane), odd = map_shared_rank(smem_u32(&s_odd[it & 1]), lane);
+                        const int v[6] = {w.q0, w.n, w.k0, w.m, w.first, w.h};
+#pragma unroll
+                        for (int k = 0; k < 6; ++k) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at + 4 * k), "r"(v[k]) : "memory");
+                        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(odd), "r"(0) : "memory");
+                        mbar_arrive_cluster(map_shared_rank(bar(B_ITEM_FULL + (it & 1)), lane));
+                    }
+                } else if (lane == 0) {
                     s_item[it & 1] = w;
                     s_odd[it & 1] = 0;
                     mbar_arrive(bar(B_ITEM_FULL + (it & 1)));
                 }
                 __syncwarp();
                 if (!has) break;
-                if (SPLIT) { more = false; continue; }
+                if (!mbar_wait(bar(B_WANTED), it & 1, abort, p.wait_cycles)) break;
                 // a CTA that has not begun gives its place up, if there is one (a place behind the last item too, and then the next)
                 uint32_t got = 0u;
                 do {
@@ -774,6 +888,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         : "=r"(got), "=r"(place) : "r"(smem_u32(s_next)) : "memory");
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // (read before the next answer is written)
                     __syncwarp();
+                    place /= static_cast<unsigned>(split);
                 } while (got && static_cast<int>(place / static_cast<unsigned>(p.Hkv)) >= total);
                 more = got != 0u;
             }
@@ -781,64 +896,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     }
     __syncwarp();
     __syncthreads();
-    if (SPLIT) {
-        // ---- the cluster's shares of every row into one: rank r concludes every `split`-th row; four channels a thread
-        cluster_sync_all();
-        const Item w = s_item[0];
-        if (w.h >= 0 && !s_abort) {
-            const Plan plan(p, w, rank, split);
-            const int rows = plan.pair ? PA_ROWS : 2 * PA_ROWS;
-            // (four quads a round: what comes from the other CTAs takes about a microsecond)
-            constexpr int AT_ONCE = 4;
-            for (int x0 = tid; x0 < rows / split * 32; x0 += AT_ONCE * PA_THREADS) {
-                float4 o[AT_ONCE];
-                float top[AT_ONCE], l[AT_ONCE];
-                size_t row[AT_ONCE];
-                bool real[AT_ONCE];
-#pragma unroll
-                for (int u = 0; u < AT_ONCE; ++u) {
-                    const int x = x0 + u * PA_THREADS, rr = (x >> 5) * split + rank, t = rr >> 7, r = rr & 127, tok = r / p.G, g = r - tok * p.G;
-                    real[u] = x < rows / split * 32 && tok < (t ? plan.n_b : plan.n_a);
-                    row[u] = static_cast<size_t>(w.q0 + w.first + t * p.tq + tok) * p.Hq + static_cast<size_t>(w.h) * p.G + g;
-                    o[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    top[u] = PA_NO_MAX;
-                    l[u] = 0.f;
-                }
-#pragma unroll 2
-                for (int k = 0; k < split; ++k) {
-                    float2 ml[AT_ONCE];
-                    float4 v[AT_ONCE];
-#pragma unroll
-                    for (int u = 0; u < AT_ONCE; ++u) {
-                        const int x = x0 + u * PA_THREADS, rr = (x >> 5) * split + rank;
-                        if (!real[u]) continue;
-                        ml[u] = ld_cluster2(map_shared_rank(smem + PA_ML_AT + static_cast<uint32_t>(rr) * 8u, k));
-                        v[u] = ld_cluster4(map_shared_rank(smem + static_cast<uint32_t>(rr) * 512u + (((x & 31) ^ (rr & 31)) << 4), k));
-                    }
-#pragma unroll
-                    for (int u = 0; u < AT_ONCE; ++u) {
-                        if (!real[u]) continue;
-                        const float most = fmaxf(top[u], ml[u].x), f = pa_ex2(ml[u].x - most), was = pa_ex2(top[u] - most);
-                        l[u] = l[u] * was + ml[u].y * f;
-                        o[u].x = o[u].x * was + v[u].x * f; o[u].y = o[u].y * was + v[u].y * f;
-                        o[u].z = o[u].z * was + v[u].z * f; o[u].w = o[u].w * was + v[u].w * f;
-                        top[u] = most;
-                    }
-                }
-#pragma unroll
-                for (int u = 0; u < AT_ONCE; ++u) {
-                    if (!real[u]) continue;
-                    const int quad = (x0 + u * PA_THREADS) & 31;
-                    const bool none = l[u] == 0.f;
-                    const float inv = none ? 0.f : 1.f / l[u];
-                    *reinterpret_cast<uint2*>(static_cast<T*>(p.out) + row[u] * PI_HEAD_DIM + 4 * quad) =
-                        none ? make_uint2(0u, 0u) : make_uint2(Form<T>::pack(o[u].x * inv, o[u].y * inv), Form<T>::pack(o[u].z * inv, o[u].w * inv));
-                    if (p.lse && quad == 0) p.lse[row[u]] = none ? -INFINITY : (top[u] + log2f(l[u])) * 0.6931471805599453f;
-                }
-            }
-        }
-        cluster_sync_all();                         // no CTA ends while another reads its share
-    }
+    if (SPLIT) cluster_sync_all();                  // no CTA ends while another reads its share or arrives at its barriers
     if (warp == 8) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
