@@ -43,6 +43,28 @@ append_kernel(AppendParams p) {
     pi_grid_dependency_wait();
     pi_launch_dependents();
     const int pos = p.ctx_len[seq];
+    // What hangs on no other load is asked for with the context's length: a load that has to come from memory takes most of a microsecond,
+    // and the call is little else than a chain of them.
+    int32_t* slot_block = p.slot_block + static_cast<size_t>(seq) * p.C;
+    uint32_t* slot_stamp = p.slot_stamp + static_cast<size_t>(seq) * p.C;
+    constexpr int AHEAD = 2;                               // slots of a thread
+    int ahead_block[AHEAD];
+    uint32_t ahead_stamp[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+        const int s = tid + i * APPEND_THREADS;
+        ahead_block[i] = s < p.C ? slot_block[s] : 0;
+        ahead_stamp[i] = s < p.C ? slot_stamp[s] : 0u;
+    }
+    uint2 ahead_row[AHEAD];                                // 8 bits: rows of a warp
+    if (FORM == 8) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int r = warp + i * APPEND_WARPS;
+            if (r < 2 * p.Hkv) ahead_row[i] = reinterpret_cast<const uint2*>(r & 1 ? p.v_new : p.k_new)[(static_cast<size_t>(seq) * p.Hkv + (r >> 1)) * 32 + lane];
+        }
+    }
+    const __nv_bfloat16 key = reinterpret_cast<const __nv_bfloat16*>(p.k_new)[(static_cast<size_t>(seq) * p.Hkv + p.h_star) * PI_HEAD_DIM + (tid & (PI_HEAD_DIM - 1))];
     if (pos < 0) return;
     const int b = pos / p.B, t = pos - b * p.B;
     if (b >= p.max_blocks) {
@@ -50,10 +72,10 @@ append_kernel(AppendParams p) {
         return;
     }
     int32_t* table = p.table + static_cast<size_t>(seq) * p.max_blocks;
-    int32_t* slot_block = p.slot_block + static_cast<size_t>(seq) * p.C;
-    uint32_t* slot_stamp = p.slot_stamp + static_cast<size_t>(seq) * p.C;
     const long long block_bytes = FORM != 16 ? p.block_bytes : static_cast<long long>(p.Hkv) * 2 * p.B * PI_HEAD_DIM * 2;
     int slot = table[b];
+    __nv_bfloat16* digest = p.digest + (static_cast<size_t>(seq) * p.max_blocks + b) * 2 * PI_HEAD_DIM + (tid & (PI_HEAD_DIM - 1));
+    const __nv_bfloat16 lowest = digest[0], highest = digest[PI_HEAD_DIM];      // (of a block that is open)
     long long host_off = seq * p.host_stride + b * block_bytes;
     if (p.page) {
         // a block index beyond the sequence's row of the table is not followed (rows are page_stride long)
@@ -70,11 +92,14 @@ append_kernel(AppendParams p) {
         // slot whose block is neither sink nor local under the new length (free slots first)
         const int nb_new = b + 1;
         unsigned long long best = ~0ull;
-        for (int s = tid; s < p.C; s += APPEND_THREADS) {
-            const int ob = slot_block[s];
+        auto look = [&](int s, int ob, uint32_t stamp) {
             const bool pinned = ob >= 0 && (ob < p.n_sink || ob >= nb_new - p.n_local);
-            if (!pinned) best = min(best, (static_cast<unsigned long long>(slot_stamp[s]) << 32) | static_cast<unsigned>(s));
-        }
+            if (!pinned) best = min(best, (static_cast<unsigned long long>(stamp) << 32) | static_cast<unsigned>(s));
+        };
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (tid + i * APPEND_THREADS < p.C) look(tid + i * APPEND_THREADS, ahead_block[i], ahead_stamp[i]);
+        for (int s = tid + AHEAD * APPEND_THREADS; s < p.C; s += APPEND_THREADS) look(s, slot_block[s], slot_stamp[s]);
 #pragma unroll
         for (int o = 16; o; o >>= 1) best = min(best, __shfl_xor_sync(0xffffffffu, best, o));
         if (lane == 0) warp_min[warp] = best;
@@ -133,8 +158,8 @@ append_kernel(AppendParams p) {
         // A warp a row of 128 channels, four a lane.  A row whose scale suffices is 128 bytes into the block; one that is larger takes the other
         // rows of its head and K or V with it: they are rounded again, and the store's copy is written anew from the pool's.
         for (int i = warp; i < 2 * p.Hkv; i += APPEND_WARPS) {
-            const int h = i >> 1, is_v = i & 1;
-            const uint2 x = reinterpret_cast<const uint2*>(is_v ? p.v_new : p.k_new)[(static_cast<size_t>(seq) * p.Hkv + h) * 32 + lane];
+            const uint2 x = i == warp ? ahead_row[0] : i == warp + APPEND_WARPS ? ahead_row[1]
+                          : reinterpret_cast<const uint2*>(i & 1 ? p.v_new : p.k_new)[(static_cast<size_t>(seq) * p.Hkv + (i >> 1)) * 32 + lane];
             const long long scales = static_cast<long long>(p.Hkv) * 2 * p.B * PI_HEAD_DIM + 4 * i, rows = static_cast<long long>(i) * p.B * PI_HEAD_DIM;
             uint32_t* scale = reinterpret_cast<uint32_t*>(pool_blk + scales);
             const int had = t == 0 ? 0 : kv8_field_of(*scale);
@@ -174,14 +199,8 @@ append_kernel(AppendParams p) {
     }
     // running min / max of the retrieval head's keys in this block (exact: bf16 values only)
     if (tid < PI_HEAD_DIM) {
-        const __nv_bfloat16 x = reinterpret_cast<const __nv_bfloat16*>(p.k_new)[(static_cast<size_t>(seq) * p.Hkv + p.h_star) * PI_HEAD_DIM + tid];
-        __nv_bfloat16* lo = p.digest + (static_cast<size_t>(seq) * p.max_blocks + b) * 2 * PI_HEAD_DIM + tid;
-        __nv_bfloat16* hi = lo + PI_HEAD_DIM;
-        if (t == 0) { *lo = x; *hi = x; }
-        else {
-            if (__bfloat162float(x) < __bfloat162float(*lo)) *lo = x;
-            if (__bfloat162float(x) > __bfloat162float(*hi)) *hi = x;
-        }
+        if (t == 0 || __bfloat162float(key) < __bfloat162float(lowest)) digest[0] = key;
+        if (t == 0 || __bfloat162float(key) > __bfloat162float(highest)) digest[PI_HEAD_DIM] = key;
     }
 }
 
