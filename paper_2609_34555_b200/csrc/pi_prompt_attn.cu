@@ -290,8 +290,14 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     tc_fence_after();
     const uint32_t tmem = s_tmem;
     volatile int* abort = &s_abort;
-    // a wait for what this CTA, or with SPLIT another of the cluster, has written
-    auto wait_here = [&](uint32_t place, uint32_t parity) { return SPLIT ? mbar_wait_cluster(bar(place), parity, abort, p.wait_cycles) : mbar_wait(bar(place), parity, abort, p.wait_cycles); };
+    // A warp's waits, for what this CTA or (`_cluster`) another has written.  A wait that is given up is given up by all lanes: a warp
+    // whose lanes went different ways would stand at its next vote for good.
+    auto wait = [&](uint32_t place, uint32_t parity) {
+        if (__all_sync(0xffffffffu, mbar_try(bar(place), parity))) return true;
+        return __all_sync(0xffffffffu, mbar_wait(bar(place), parity, abort, p.wait_cycles)) != 0;
+    };
+    auto wait_cluster = [&](uint32_t place, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait_cluster(bar(place), parity, abort, p.wait_cycles)) != 0; };
+    auto wait_here = [&](uint32_t place, uint32_t parity) { return SPLIT ? wait_cluster(place, parity) : wait(place, parity); };
     // item number `it` of this CTA, for the roles that are told
     auto item_of = [&](int it, Item& w) -> bool {
         if (!wait_here(B_ITEM_FULL + (it & 1), (it >> 1) & 1)) return false;
@@ -331,7 +337,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             float m = PA_NO_MAX, mc = PA_NO_MAX, l = 0.f;            // the reference of the row's weights, as a score and times c; their sum
             bool far = false;
             for (int j = begin; j < end; j += plan.step(), ++steps) {
-                if (!mbar_wait(bar(B_S_FULL + t), steps & 1u, abort, p.wait_cycles)) { alive = false; break; }
+                if (!wait(B_S_FULL + t, steps & 1u)) { alive = false; break; }
                 tc_fence_after();
                 float s[128];
 #pragma unroll
@@ -403,7 +409,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 if (lane == 0) mbar_arrive(bar(B_P_FULL + t));
             }
             // ---- the row's result
-            if (alive && end > begin) alive = mbar_wait(bar(B_O_FULL + t), results++ & 1u, abort, p.wait_cycles);
+            if (alive && end > begin) alive = wait(B_O_FULL + t, results++ & 1u);
             if (!alive) break;
             tc_fence_after();
             bool some = end > begin;                // there is an O of this group
@@ -417,7 +423,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(B_HALF));
                 } else {
-                    if (!mbar_wait(bar(B_HALF), merges & 1u, abort, p.wait_cycles)) { alive = false; break; }
+                    if (!wait(B_HALF, merges & 1u)) { alive = false; break; }
                     tc_fence_after();
                     const float2 ml = s_ml[r];
                     other_some = plan.end(1) > plan.begin(1);
@@ -434,7 +440,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 // the last item's shares have been read by all; Q's and the ring's place is free when both groups have their O
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(B_ALL));
-                if (!mbar_wait(bar(B_ALL), it & 1, abort, p.wait_cycles) || (it > 0 && !mbar_wait_cluster(bar(B_SHARE_EMPTY), (it - 1) & 1, abort, p.wait_cycles))) { alive = false; break; }
+                if (!wait(B_ALL, it & 1) || (it > 0 && !wait_cluster(B_SHARE_EMPTY, (it - 1) & 1))) { alive = false; break; }
             }
             const bool none = l == 0.f;             // (a NaN among the sums has to come through)
             const float inv = none ? 0.f : 1.f / l;
@@ -499,7 +505,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             if (SPLIT) {
                 // ---- the cluster's shares of every row into one: rank r concludes every `split`-th row; four channels a thread
                 arrive_at_all(B_SHARE_FULL);
-                if (!mbar_wait_cluster(bar(B_SHARE_FULL), it & 1, abort, p.wait_cycles)) { alive = false; break; }
+                if (!wait_cluster(B_SHARE_FULL, it & 1)) { alive = false; break; }
                 const int rows = few ? PA_FEW : plan.pair ? PA_ROWS : 2 * PA_ROWS;
                 // (two quads a round, from two CTAs at a time: what comes from them takes about a microsecond)
                 constexpr int AT_ONCE = 2;
@@ -555,7 +561,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 __syncwarp();
                 if (t == 0) {
                     if (lane == 0) mbar_arrive(bar(B_MERGED));
-                } else if (!mbar_wait(bar(B_MERGED), merges & 1u, abort, p.wait_cycles)) {
+                } else if (!wait(B_MERGED, merges & 1u)) {
                     alive = false;
                     break;
                 }
@@ -579,7 +585,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     // that have been, or will be in a moment (and every phase of the barrier is waited for once).
                     const bool in_the_way = it > 0 && (!few_before || plan.n_b);
                     for (; read < (in_the_way ? it : it - 1); ++read)
-                        if (!mbar_wait_cluster(bar(B_SHARE_EMPTY), read & 1, abort, p.wait_cycles)) { alive = false; break; }
+                        if (!wait_cluster(B_SHARE_EMPTY, read & 1)) { alive = false; break; }
                     if (!alive) break;
                     if (in_the_way) asm volatile("fence.proxy.async;" ::: "memory");
                     few_before = plan.pair && plan.n_a * p.G <= PA_FEW;
@@ -588,7 +594,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     if (rank == 0 && lane == 0) mbar_arrive(bar(B_WANTED));
                     continue;
                 }
-                if (items && !mbar_wait(bar(B_Q_EMPTY), (items - 1) & 1u, abort, p.wait_cycles)) { alive = false; break; }
+                if (items && !wait(B_Q_EMPTY, (items - 1) & 1u)) { alive = false; break; }
                 if (lane == 0) {
                     const uint32_t bytes = static_cast<uint32_t>(p.tq) * p.G * 128u;
                     mbar_expect_tx(bar(B_Q_FULL), bytes * (plan.n_b ? 4u : 2u));
@@ -599,7 +605,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 ++items;
                 for (int i = 2 * plan.lo; i < 2 * plan.hi; ++i, ++n) {
                     const uint32_t stage = n % PA_STAGES;
-                    if (n >= PA_STAGES && !mbar_wait(bar(B_KV_EMPTY + stage), (n / PA_STAGES - 1) & 1u, abort, p.wait_cycles)) { alive = false; break; }
+                    if (n >= PA_STAGES && !wait(B_KV_EMPTY + stage, (n / PA_STAGES - 1) & 1u)) { alive = false; break; }
                     if (p.hold_last && i == 2 * plan.hi - 1) { alive = false; break; }
                     if (lane == 0) {
                         const CUtensorMap* map = (i & 1) ? &map_v : &map_k;
@@ -632,10 +638,6 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             uint32_t items = 0u, made = 0u;                  // bit t of `made`: which phase of tile t's P_FULL comes next
             bool alive = true;
             Item w;
-            auto wait = [&](uint32_t place, uint32_t parity) {
-                if (__all_sync(0xffffffffu, mbar_try(bar(place), parity))) return true;
-                return __all_sync(0xffffffffu, mbar_wait(bar(place), parity, abort, p.wait_cycles)) != 0;
-            };
             auto after = [](uint32_t at) { return at == PA_STAGES - 1 ? 0u : at + 1; };
             auto full = [&](uint32_t at) {
                 const uint32_t phase = (filled >> at) & 1u;
@@ -676,7 +678,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             auto signal = [&](uint32_t place) {
                 if (elect_one()) tc_commit(bar(place));
             };
-            for (int it = 0; alive && __all_sync(0xffffffffu, item_of(it, w)); ++it) {
+            for (int it = 0; alive && item_of(it, w); ++it) {
                 w.q0 = __shfl_sync(0xffffffffu, w.q0, 0); w.n = __shfl_sync(0xffffffffu, w.n, 0);
                 w.k0 = __shfl_sync(0xffffffffu, w.k0, 0); w.m = __shfl_sync(0xffffffffu, w.m, 0);
                 w.first = __shfl_sync(0xffffffffu, w.first, 0); w.h = __shfl_sync(0xffffffffu, w.h, 0);
@@ -777,7 +779,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 bool odd = false;
                 for (int i = 2 * plan.lo; i < 2 * plan.hi; ++i, ++n) {         // (every load is waited for: a phase is told from the one before the last by the order alone)
                     const uint32_t stage = n % PA_STAGES, tile = ring + stage * PA_TILE;
-                    if (!mbar_wait(bar(B_KV_FULL + stage), (n / PA_STAGES) & 1u, abort, p.wait_cycles)) { alive = false; break; }
+                    if (!wait(B_KV_FULL + stage, (n / PA_STAGES) & 1u)) { alive = false; break; }
                     const int j = i >> 1;
                     if (!(i & 1) || j < plan.odd_from) continue;
                     const int rows = min(w.m - j * PA_ROWS, PA_ROWS), from = max(plan.seen_first - j * PA_ROWS, 0);      // of the sequence; not seen by all
@@ -871,7 +873,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 }
                 __syncwarp();
                 if (!has) break;
-                if (!mbar_wait(bar(B_WANTED), it & 1, abort, p.wait_cycles)) break;
+                if (!wait(B_WANTED, it & 1)) break;
                 // a CTA that has not begun gives its place up, if there is one (a place behind the last item too, and then the next)
                 uint32_t got = 0u;
                 do {
@@ -881,7 +883,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     }
                     __syncwarp();
                     volatile int none = 0;          // (the answer is written into this CTA's memory, so it is waited for in any case)
-                    if (!mbar_wait(bar(B_NEXT), asked++ & 1u, &none, p.wait_cycles)) { *abort = 1; got = 0u; break; }
+                    if (!__all_sync(0xffffffffu, mbar_wait(bar(B_NEXT), asked++ & 1u, &none, p.wait_cycles))) { *abort = 1; got = 0u; break; }
                     asm volatile(
                         "{\n .reg .b128 r;\n .reg .pred c;\n ld.shared.b128 r, [%2];\n clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 c, r;\n selp.u32 %0, 1, 0, c;\n mov.u32 %1, 0;\n"
                         " @c clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n}"
@@ -948,17 +950,18 @@ int pi_launch_prompt_attn(pi_ctx* c, int n_seqs, int dtype, int n_q, int n_k, co
     p.wide = (reinterpret_cast<uintptr_t>(out) & 31u) == 0;
     const long long per_block = 2 * p.tq, seqs = n_seqs < n_q ? n_seqs : n_q, blocks = (n_q + seqs * (per_block - 1)) / per_block, items = blocks * p.Hkv;
     // CTAs that share an item: where the items leave SMs without work and the keys are many, a cluster for each, up to a power of two that fits the
-    // GPU once (and eight: fewer than eight clusters of 16 are resident at a time).  A cluster costs 3 to 5 us more than a CTA, and a K/V tile 1 to 2 us:
-    // 8 items of one token and 4 / 8 / 32 / 128 tiles take 9.9 / 13.6 / 36 / 130 us with 1 CTA each, 10.7 / 12.8 / 24 / 73 with 2,
-    // 9.8 / 11.0 / 17 / 42 with 4, 11.3 / 11.3 / 14.5 / 28 with 8.
-    // (How long each sequence is, only the kernel sees: the rule goes by the mean.)
+    // GPU once (and eight: fewer than eight clusters of 16 are resident at a time).  A cluster costs 2 to 4 us more than a CTA, and a K/V tile 1 us:
+    // 8 items of one token and 4 / 8 / 32 / 128 tiles take 10.2 / 13.4 / 33 / 120 us with 1 CTA each, 12.5 / 14.1 / 24 / 68 with 2,
+    // 11.4 / 12.4 / 18 / 40 with 4, 12.6 / 12.6 / 16 / 28 with 8.
     const long long tiles = (n_k / seqs + PA_ROWS - 1) / PA_ROWS;
     int split = 1;
     while (split < PA_MAX_SPLIT && items * split * 2 <= c->n_sms && tiles >= 4 * split && tiles >= 8) split *= 2;
-    // Items that leave less than half of the SMs without work, with keys for a long time: two each.  Sequences of like length take longer
-    // for it (16 of one token and 16 384 keys 199 us instead of 166), but one that is twice the mean would hold up the others (of 0 to
-    // 16 384 keys 126 us instead of 157).
-    if (split == 1 && items <= c->n_sms && per_block / 2 * seqs >= n_q && tiles >= 32) split = 2;
+    // How long each sequence is, only the kernel sees; the rule goes by the mean.  Where several of them make up to two items an SM and keep it busy
+    // for a while, one that is longer than the others would be what the call waits for, so there two CTAs share each item.  Sequences of
+    // like length lose by it what the others gain: 16 of one token after 16 384 take 176 us instead of 166, after 0 to 16 384
+    // 106 instead of 130; 12 of 4 tokens after 16 000 161 instead of 143, after 0 to 16 000 88 instead of 130; 5 of 256 after 8 000
+    // 223 instead of 249.  With fewer keys it does not pay: 16 of one token after 4 096 57 instead of 46, after 0 to 4 096 44 instead of 42.
+    if (split == 1 && seqs > 1 && items <= 2 * c->n_sms && tiles >= 40) split = 2;
     const long long grid = items * split;
     if (grid > INT32_MAX) return PI_ERR_UNSUPPORTED_DIM;
     const size_t smem = 2 * PA_TILE + PA_STAGES * PA_TILE + 1024;

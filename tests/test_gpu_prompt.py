@@ -1,4 +1,6 @@
 """Attention over packed prompts against the definition in 64 bits."""
+import random
+
 import pytest
 import torch
 
@@ -328,6 +330,25 @@ def test_a_wait_that_runs_out_is_reported_and_the_next_call_works():
     pi = context(8, 2)
     out, lse = run(pi, q, k, v, qs, ks)
     check(q.dtype, out, lse, reference(q, k, v, qs, ks))
+
+
+@pytest.mark.parametrize("n,longest", [(1, 3000), (1, 7000), (3, 500), (90, 2000)])
+def test_call_after_call_gives_the_same_bits(n, longest):
+    """Hundreds of calls without a pause, of uneven sequences, more of them than fit the GPU at once or few that are shared."""
+    r = random.Random(n * longest)
+    for batch in (21, 5):
+        lens = [r.randrange(1, n + 1) for _ in range(batch)]
+        q, k, v, qs, ks = case(32, 8, lens, [a + r.randrange(0, longest) for a in lens], seed=n)
+        pi = context(32, 8, wait_limit_us=100000)
+        out, lse = run(pi, q, k, v, qs, ks)
+        check(q.dtype, out, lse, reference(q, k, v, qs, ks))
+        a, b, others = i32(qs), i32(ks), [(torch.full_like(out, 7.0), torch.full_like(lse, 7.0)) for _ in range(3)]
+        for i in range(300):
+            pi.prompt_attn(q, k, v, a, others[i % 3][0], k_start=b, lse=others[i % 3][1])
+        torch.cuda.synchronize()
+        assert pi.status()[0] == 0, pi.status()
+        for o, l in others:
+            assert torch.equal(o, out) and torch.equal(l, lse)
 
 
 def test_keys_beyond_32_bits_of_an_address():
