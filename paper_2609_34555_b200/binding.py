@@ -2,8 +2,8 @@
 
 Argument marshalling only: tensors are checked (dtype, device, contiguity) and handed
 over as raw pointers; every step of the path runs in the CUDA library.  There is no
-fallback: a missing library or a failing call raises.  The calls on the 4-bit path, some of which keep the
-GPU for a few microseconds only, have their tensors checked in native code (csrc/front.cpp).
+fallback: a missing library or a failing call raises.  The calls on the 4-bit and 8-bit paths and the attention over
+prompts, some of which keep the GPU for a few microseconds only, have their tensors checked in native code (csrc/front.cpp).
 """
 from __future__ import annotations
 
@@ -119,7 +119,7 @@ def load_library(rebuild: bool = False) -> ctypes.CDLL:
 
 
 def load_front():
-    """The module that checks the tensors of the calls on the 4-bit path, connected to the CUDA library."""
+    """The module that checks the tensors of the calls on the 4-bit and 8-bit paths and over prompts, connected to the CUDA library."""
     global _front
     if _front is None:
         lib = load_library()

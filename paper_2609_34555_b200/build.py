@@ -1,5 +1,6 @@
 """Builds libpulseinfer_b200.so (sm_100a only) in-tree with nvcc, and _front, the Python module that checks
-the tensors of the calls on the 4-bit path, with g++ against the installed torch.  Only those calls need the module.
+the tensors of the calls on the 4-bit and 8-bit paths and of the attention over prompts, with g++ against the installed
+torch.  Only those calls need the module.
 
     python -m paper_2609_34555_b200.build [--force] [--verbose]
 """

@@ -31,9 +31,10 @@ struct AppendParams {
 };
 
 // FORM: bits of a number in pool and store, 16, 8 or 4; the token's rows are rounded on their way there (the digest takes the
-// key as it came).  Latency-bound like the other form.  B200, 16 sequences of 256 slots, one launch between two events (an empty
+// key as it came).  Latency-bound in every form.  B200, 4 bits, 16 sequences of 256 slots, one launch between two events (an empty
 // one 6.1 us): into an open block 12.3 us with the store in pinned memory and 8.2 with it on the device, opening a
-// block (the choice of a slot, a fresh block cleared in pool and store) 18.4 and 10.2.
+// block (the choice of a slot, a fresh block cleared in pool and store) 18.4 and 10.2.  8 bits, blocks of 16 and 8 heads, store on the device, 4 of 16
+// sequences opening a block: 3.8 us back to back, 8.2 with cold caches (an empty one 2.6); 64 sequences, blocks of 32: 5.1 and 10.2.
 template <int FORM>
 __global__ void __launch_bounds__(APPEND_THREADS)
 append_kernel(AppendParams p) {

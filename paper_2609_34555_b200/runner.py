@@ -372,11 +372,12 @@ class DecodeSession:
         c = self.pi.cfg
         if k.shape[0] != v.shape[0] or starts.shape != (self.batch + 1,):
             raise ValueError("load_prompts: expected keys and values of the same tokens, and batch + 1 starts")
-        self.pi.prompt_attn(q, k, v, starts, out, lse=lse)
         begin = starts.long()
         lens = begin.diff()
-        if int(lens.max()) > c.max_blocks * c.block_tokens:
-            raise ValueError("load_prompts: a prompt is longer than max_blocks blocks")
+        least, longest = lens.aminmax()
+        if int(least) < 0 or int(longest) > c.max_blocks * c.block_tokens or int(begin[0]) < 0 or int(begin[-1]) > k.shape[0]:
+            raise ValueError("load_prompts: starts have to rise within the tokens given, by max_blocks blocks at most")
+        self.pi.prompt_attn(q, k, v, starts, out, lse=lse)
         self.ctx_len.copy_(lens)
         t = torch.arange(k.shape[0], device=self.device)
         seq = (torch.searchsorted(begin, t, right=True) - 1).clamp(0, self.batch - 1)
