@@ -451,7 +451,7 @@ int pi_sparse_decode_attn_kv4(pi_ctx* ctx, int layer, int batch, const void* q_d
 int64_t pi_kv8_block_bytes(pi_ctx* ctx);
 
 /* Tokens into 8-bit blocks; arguments, skipped tokens and errors as pi_kv4_store.  The tokens of one call that go to the same block stand
- * one behind the other (as in the maps of pi_assign_pages), and no two of them name the same slot.  Bytes of blocks that no token
+ * one behind the other with none skipped between them (as in the maps of pi_assign_pages), and no two of them name the same slot.  Bytes of blocks that no token
  * goes to stay as they are. */
 int pi_kv8_store(pi_ctx* ctx, int64_t n_tokens, const void* k_dev, int64_t k_token_stride, int64_t k_head_stride,
                  int64_t k_outer_stride, const void* v_dev, int64_t v_token_stride, int64_t v_head_stride,

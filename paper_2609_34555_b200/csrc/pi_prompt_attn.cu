@@ -17,8 +17,8 @@
 // call).  The sum of the weights, the maxima and all products' sums are in 32 bits.
 //
 // An item is a block of up to 2 tq tokens (tq = 128 / G) of a sequence and a KV head.  Where a block has one query tile, the two softmax groups
-// take every second K/V tile of it and are joined at the end.  CTAs stay and take over the places of CTAs that have not begun, the longest items
-// first, so that the next item's loads and first product run under the last one's end; few items with many keys are shared by
+// take every second K/V tile of it and are joined at the end.  CTAs stay and take over the places of CTAs that have not begun, the longest
+// sequences first, so that the next item's loads and first product run under the last one's end; few items with many keys are shared by
 // clusters of two to eight CTAs (the launcher's rule).
 //
 // The maximum that is taken off moves only when a score exceeds it by a factor of 2^8 after the exponential, so that O is seldom
@@ -27,7 +27,7 @@
 // Measured on a B200 (32 query heads, 8 KV heads, bf16; 1 643 TFLOP/s is what a library product reaches in a short run, 1 394 for seconds):
 // one prompt of 8 192 tokens 436 us, 1 260 TFLOP/s, in a run of a few milliseconds, 510 us for longer, where the power limit takes the
 // clock from 1.7 to 1.45 GHz; 23 prompts of 0 to 1 500 tokens 175 us; 77 tokens 9.3 us; 16 sequences of one token after 16 384
-// 174 us, 6.2 TB/s, after 0 to 16 384 105 us; 500 tokens after 65 536 with 64 heads in fp16 930 us.  An iteration (two query tiles, one K/V tile) takes 3 270 cycles,
+// 174 us, 6.2 TB/s, after 0 to 16 384 89 us (105 before the longest sequences came first); 500 tokens after 65 536 with 64 heads in fp16 930 us.  An iteration (two query tiles, one K/V tile) takes 3 270 cycles,
 // of which the tensor pipe and the exponentials are busy for 2 048 each.
 // Tried and not taken: a share of the exponentials as polynomials (3 % fewer cycles, the same time), P handed over in two halves, a
 // reference without each tile's maximum, clusters of 16.
@@ -276,6 +276,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     __shared__ Item s_item[2];
     __shared__ float2 s_ml[PA_ROWS];                // tile A alone: reference and sum of group B's rows
     __shared__ float2 s_share[PA_FEW];              // SPLIT, few rows: reference and sum of the CTA's share
+    __shared__ unsigned char s_order[32];           // of 32 sequences, by their keys
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort, s_odd[2];               // s_odd: values that are no numbers were taken out of a tile
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -835,9 +836,30 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             }
         } else if (rank == 0) {
             // ---- warp 10: which items are this CTA's, or its cluster's.  Blocks are counted from the last one of the last sequence, so that the longest of a
-            // sequence come first; KV heads innermost.
+            // sequence come first; KV heads innermost.  32 sequences at a time are put in the order of their keys, so that the longest of them come first
+            // too, and what is short fills the end.
             const int per_block = 2 * p.tq;
-            const Span mine = span_of(p, lane, blockIdx.x == 0);
+            auto spans_from = [&](int s0, bool tell) {
+                Span x = span_of(p, s0 + lane, tell);
+                const int count = min(p.n_seqs - s0, 32);
+                if (count > 1) {
+                    const int key = x.n > 0 ? x.m : -1;
+                    int before = 0;
+#pragma unroll 8
+                    for (int k = 0; k < count; ++k) {
+                        const int other = __shfl_sync(0xffffffffu, key, k);
+                        before += other < key || (other == key && k < lane);
+                    }
+                    if (lane < count) s_order[before] = static_cast<unsigned char>(lane);
+                    __syncwarp();
+                    const int from = lane < count ? s_order[lane] : lane;
+                    __syncwarp();
+                    x.q0 = __shfl_sync(0xffffffffu, x.q0, from); x.n = __shfl_sync(0xffffffffu, x.n, from);
+                    x.k0 = __shfl_sync(0xffffffffu, x.k0, from); x.m = __shfl_sync(0xffffffffu, x.m, from);
+                }
+                return x;
+            };
+            const Span mine = spans_from(0, blockIdx.x == 0);
             int total = (mine.n + per_block - 1) / per_block;
             for (int s0 = 32; s0 < p.n_seqs; s0 += 32) total += (span_of(p, s0 + lane, blockIdx.x == 0).n + per_block - 1) / per_block;
             total = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(total)));
@@ -851,7 +873,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 if (has) {
                     int at = total - 1 - item;
                     for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
-                        const Span x = s0 ? span_of(p, s0 + lane, false) : mine;
+                        const Span x = s0 ? spans_from(s0, false) : mine;
                         const int nb = (x.n + per_block - 1) / per_block;
                         int upto = nb;
 #pragma unroll
@@ -973,10 +995,11 @@ int pi_launch_prompt_attn(pi_ctx* c, int n_seqs, int dtype, int n_q, int n_k, co
     while (split < PA_MAX_SPLIT && items * split * 2 <= c->n_sms && tiles >= 4 * split && tiles >= 8) split *= 2;
     // How long each sequence is, only the kernel sees; the rule goes by the mean.  Where several of them make up to two items an SM and keep it busy
     // for a while, one that is longer than the others would be what the call waits for, so there two CTAs share each item.  Sequences of
-    // like length lose by it what the others gain: 16 of one token after 16 384 take 176 us instead of 166, after 0 to 16 384
-    // 106 instead of 130; 12 of 4 tokens after 16 000 161 instead of 143, after 0 to 16 000 88 instead of 130; 5 of 256 after 8 000
-    // 223 instead of 249.  With fewer keys it does not pay: 16 of one token after 4 096 57 instead of 46, after 0 to 4 096 44 instead of 42.
-    if (split == 1 && seqs > 1 && items <= 2 * c->n_sms && tiles >= 40) split = 2;
+    // like length lose less by it than the others gain: 16 of one token after 16 384 take 175 us instead of 166, after 0 to 16 384
+    // 89 instead of 132; 12 of 4 after 16 000 159 instead of 142, after 0 to 16 000 81 instead of 127; 8 of 200 after 8 000 262 instead of 266, of 1 to 200
+    // after 0 to 8 000 87 instead of 143; of the others only 32 of one token after 0 to 8 192 loses, 107 instead of 95.  With fewer keys it does
+    // not pay: 16 of one token after 4 096 57 instead of 46, 6 of 100 after 3 000 75 instead of 53 (of 1 to 100 after 0 to 3 000 41 instead of 50).
+    if (split == 1 && seqs > 1 && items <= 2 * c->n_sms && tiles > 32) split = 2;
     const long long grid = items * split;
     if (grid > INT32_MAX) return PI_ERR_UNSUPPORTED_DIM;
     const size_t smem = 2 * PA_TILE + PA_STAGES * PA_TILE + 1024;
