@@ -17,7 +17,7 @@
 // end (pi_attn_merge.cuh).
 //
 // Measured on a B200, back to back: 64 sequences x 64 blocks of 32 tokens, 8 KV heads, G = 4 (263 MB) 44 us, 6.0 TB/s, 91 % of what a copy
-// reaches; 16 x 128 blocks of 16 (67 MB) 15.0 us; one sequence x 64 blocks 4.3 us; 64 x 64 blocks of 32 with G = 16 55 us.  HBM bounds the large
+// reaches; 16 x 128 blocks of 16 (67 MB) 14.6 us; one sequence x 64 blocks 4.3 us; 64 x 64 blocks of 32 with G = 16 55 us.  HBM bounds the large
 // ones; the others carry about 5 us of launch, two dependent loads before the first tile, and the merge.
 #include <cuda_fp16.h>
 
@@ -361,15 +361,21 @@ int pi_launch_attn_kv8(pi_ctx* c, int batch, const void* q, const void* pool, co
     p.B = cfg.block_tokens; p.K = cfg.budget_blocks; p.C = cfg.pool_slots;
     const int NT = p.G <= 8 ? 1 : 2, tiles = cfg.budget_blocks * (cfg.block_tokens / 16);
     const long long items = static_cast<long long>(batch) * cfg.n_kv_heads, room = static_cast<long long>(a8_warps_per_sm(NT)) * c->n_sms;
-    // CTAs per item: twice as many while they fill half of the warps there is room for, at most, and every warp has two tiles.  Measured with
-    // S = 1 / 2 / 4 / 8: 8 items x 64 tiles 10.4 / 7.3 / 5.3 / 4.3 us, 32 x 128 19.1 / 11.9 / 8.3 / 6.8, 64 x 256 36.7 / 20.8 / 15.1 / 15.6,
-    // 128 x 128 19.9 / 15.0 / 15.3 / 18.7, 256 x 128 24.3 / 25.7 / 27.6 / 32.5.
     int split = 1, warps = 4;
-    while (split < A4_MAX_SPLIT && items * split * 2 * warps <= room / 2 && tiles >= 2 * warps * split * 2) split *= 2;
-    // Few items with long lists leave SMs with one CTA each, which more warps use better, two tiles a warp or four: 8 items x 256 tiles
-    // 6.4 us with 8, 6.6 with 16; x 512 8.6 and 7.8; x 1024 20.1 with 4, 13.7 with 8, 12.0 with 16; x 2048 23.3 and 19.1.
-    if (NT == 1 && split == A4_MAX_SPLIT)
-        while (warps < 16 && items * split * warps * 2 <= room / 2 && tiles >= warps * warps * split) warps *= 2;
+    if (NT == 1 && items * 8 >= 5 * c->n_sms) {
+        // Items enough for most of the SMs: a CTA each, of as many warps as fill seven tenths of the room at most, with four tiles a warp.  4 / 8 / 16 warps:
+        // 96 items x 128 tiles 19.5 / 13.6 / 12.7 us, 128 x 128 19.9 / 14.6 / 14.9 (two CTAs of 4 warps 15.2), 192 x 128 23.0 / 19.8 / 25.8,
+        // 256 x 128 24.6 / 24.8 / 27.6, 384 x 64 19.3 / 24.4 / 26.8.
+        while (warps < 16 && items * warps * 2 * 10 <= room * 7 && tiles >= 4 * warps) warps *= 2;
+    } else {
+        // CTAs per item: twice as many while they fill half of the warps there is room for, at most, and every warp has two tiles.  Measured with
+        // S = 1 / 2 / 4 / 8: 8 items x 64 tiles 10.4 / 7.3 / 5.3 / 4.3 us, 32 x 128 19.1 / 11.9 / 8.3 / 6.8, 64 x 256 36.7 / 20.8 / 15.1 / 15.6.
+        while (split < A4_MAX_SPLIT && items * split * 2 * warps <= room / 2 && tiles >= 2 * warps * split * 2) split *= 2;
+        // Few items with long lists leave SMs with one CTA each, which more warps use better, two tiles a warp or four: 8 items x 256 tiles
+        // 6.4 us with 8, 6.6 with 16; x 512 8.6 and 7.8; x 1024 20.1 with 4, 13.7 with 8, 12.0 with 16; x 2048 23.3 and 19.1.
+        if (NT == 1 && split == A4_MAX_SPLIT)
+            while (warps < 16 && items * split * warps * 2 <= room / 2 && tiles >= warps * warps * split) warps *= 2;
+    }
     const size_t ring = static_cast<size_t>(warps) * a8_stages(NT) * A8_TILE_BYTES;
     // (the merge of a CTA's warps, up to 33 KB for four, takes the ring's place; what the cluster sends lies behind)
     const size_t smem = ring + (split > 1 ? static_cast<size_t>(p.G) * (PI_HEAD_DIM * 4 + split * 8) : 0);

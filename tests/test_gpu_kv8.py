@@ -366,6 +366,19 @@ def test_attention_random_shapes(Hq, Hkv, B):
         pi.close()
 
 
+@pytest.mark.parametrize("batch,B,K", [(12, 16, 64), (12, 16, 33), (12, 32, 9), (13, 64, 4), (21, 16, 40), (30, 32, 5), (40, 16, 17)])
+def test_attention_of_many_sequences(batch, B, K):
+    """A CTA for each (sequence, KV head), of 4, 8 or 16 warps; ragged, some sequences empty."""
+    rng = np.random.default_rng(batch + K)
+    pi = context(n_q_heads=32, n_kv_heads=8, block_tokens=B, budget_blocks=K, pool_slots=K + 2, max_batch=batch, max_blocks=2 * K, n_sink_blocks=0, n_local_blocks=1)
+    ctx = rng.integers(1, 2 * K * B + 1, batch)
+    ctx[[1, batch - 1]] = 0, 2 * K * B
+    case = attention_case(pi, ctx, batch)
+    out, lse = run_attention(pi, case)
+    check_attention(pi, case, out, lse)
+    pi.close()
+
+
 @pytest.mark.parametrize("spread", [6.0, 12.0])
 def test_attention_over_blocks_of_very_different_sizes(spread):
     """V's scales differ by many powers of two between blocks, and scores are in the hundreds: what has the weight keeps its bits, however
