@@ -164,6 +164,11 @@ template <> struct Form<__nv_bfloat16> {
     static constexpr uint32_t code = 1u;            // of the instruction descriptor
     static constexpr uint32_t exponent = 0x7f807f80u, one = 0x00800080u;
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack_bf16(lo, hi); }
+    // the larger magnitudes of two pairs, NaN where either is NaN (one operation)
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+        const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a), __habs2(*reinterpret_cast<const __nv_bfloat162*>(&b)));
+        return *reinterpret_cast<const uint32_t*>(&m);
+    }
     static __device__ __forceinline__ float value(uint32_t half) { return __uint_as_float(half << 16); }
 };
 template <> struct Form<__half> {
@@ -172,6 +177,10 @@ template <> struct Form<__half> {
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
         const __half2 v = __floats2half2_rn(lo, hi);
         return *reinterpret_cast<const uint32_t*>(&v);
+    }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+        const __half2 m = __hmax2_nan(*reinterpret_cast<const __half2*>(&a), __habs2(*reinterpret_cast<const __half2*>(&b)));
+        return *reinterpret_cast<const uint32_t*>(&m);
     }
     static __device__ __forceinline__ float value(uint32_t half) { return __half2float(__ushort_as_half(static_cast<unsigned short>(half))); }
 };
@@ -498,7 +507,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         for (int y = 0; y < 8; ++y)
                             asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(at + (((8 * x + y) ^ (r & 31)) << 4)), "f"(o[4 * y]), "f"(o[4 * y + 1]), "f"(o[4 * y + 2]), "f"(o[4 * y + 3]) : "memory");
                     } else {
-                        // (32 bytes a store where the output allows it: a lane's stores go to a row of its own, one line each)
+                        // (32 bytes a store where the output allows it, past L1: a lane's stores go to a row of its own, one line each.  23 ragged prompts 188 us,
+                        // 196 through L1; with neighbours exchanging halves, for 64 bytes a row, 191)
                         uint4* to = reinterpret_cast<uint4*>(static_cast<T*>(p.out) + row * PI_HEAD_DIM + 32 * x);
                         uint32_t u[16];
 #pragma unroll
@@ -506,7 +516,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         if (p.wide) {
 #pragma unroll
                             for (int y = 0; y < 16; y += 8)
-                                asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to + y / 4), "r"(u[y]), "r"(u[y + 1]), "r"(u[y + 2]), "r"(u[y + 3]), "r"(u[y + 4]), "r"(u[y + 5]), "r"(u[y + 6]), "r"(u[y + 7]) : "memory");
+                                asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to + y / 4), "r"(u[y]), "r"(u[y + 1]), "r"(u[y + 2]), "r"(u[y + 3]), "r"(u[y + 4]), "r"(u[y + 5]), "r"(u[y + 6]), "r"(u[y + 7]) : "memory");
                         } else {
 #pragma unroll
                             for (int y = 0; y < 16; y += 4) to[y / 4] = make_uint4(u[y], u[y + 1], u[y + 2], u[y + 3]);
@@ -805,7 +815,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         for (int x = rows * 128; x < PA_HALF; x += 512)
                             if (x + lane * 16 < PA_HALF) asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(at + x), "r"(0u) : "memory");
                         for (int x0 = from * 128; x0 < rows * 128; x0 += 8 * 512) {
-                            uint32_t u[8][4], most = 0u;     // the largest exponent and fraction, in either half of a word
+                            uint32_t u[8][4], most = 0u;     // the largest magnitudes
 #pragma unroll
                             for (int k = 0; k < 8; ++k) {
                                 const int x = x0 + 512 * k;
@@ -815,7 +825,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
                             for (int k = 0; k < 8; ++k)
 #pragma unroll
-                                for (int y = 0; y < 4; ++y) most = __vmaxu2(most, u[k][y] & 0x7fff7fffu);
+                                for (int y = 0; y < 4; ++y) most = Form<T>::larger(most, u[k][y]);
                             if (!not_finite<T>(most)) continue;
                             odd = true;
 #pragma unroll
