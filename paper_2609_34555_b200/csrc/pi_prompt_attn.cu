@@ -26,11 +26,12 @@
 //
 // Measured on a B200 (32 query heads, 8 KV heads, bf16; 1 643 TFLOP/s is what a library product reaches in a short run, 1 394 for seconds):
 // one prompt of 8 192 tokens 436 us, 1 260 TFLOP/s, in a run of a few milliseconds, 510 us for longer, where the power limit takes the
-// clock from 1.7 to 1.45 GHz; 23 prompts of 0 to 1 500 tokens 175 us; 77 tokens 9.3 us; 16 sequences of one token after 16 384
+// clock from 1.7 to 1.45 GHz; 23 prompts of 0 to 1 500 tokens 172 us; 77 tokens 8.5 us; 16 sequences of one token after 16 384
 // 174 us, 6.2 TB/s, after 0 to 16 384 89 us (105 before the longest sequences came first); 500 tokens after 65 536 with 64 heads in fp16 930 us.  An iteration (two query tiles, one K/V tile) takes 3 270 cycles,
 // of which the tensor pipe and the exponentials are busy for 2 048 each.
 // Tried and not taken: a share of the exponentials as polynomials (3 % fewer cycles, the same time), P handed over in two halves, a
-// reference without each tile's maximum, clusters of 16.
+// reference without each tile's maximum, clusters of 16; the next item's first product ahead of this one's last, weights of masked keys left
+// out 32 at a time (both cost the steady state more than they gave); a ring of four stages to make room for whole-line stores.
 #include <cuda_fp16.h>
 
 #include "pi_attn_core.cuh"
