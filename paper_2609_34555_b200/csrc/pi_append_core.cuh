@@ -44,28 +44,28 @@ append_kernel(AppendParams p) {
     pi_grid_dependency_wait();
     pi_launch_dependents();
     const int pos = p.ctx_len[seq];
-    // What hangs on no other load is asked for with the context's length: a load that has to come from memory takes most of a microsecond,
-    // and the call is little else than a chain of them.
+    // 8 bits: what hangs on no other load is asked for with the context's length.  A load that has to come from memory takes most of a microsecond, and
+    // the call is little else than a chain of them (cold, 16 sequences: 8.2 us, 10.2 one after the other).  The other forms keep their registers.
     int32_t* slot_block = p.slot_block + static_cast<size_t>(seq) * p.C;
     uint32_t* slot_stamp = p.slot_stamp + static_cast<size_t>(seq) * p.C;
-    constexpr int AHEAD = 2;                               // slots of a thread
-    int ahead_block[AHEAD];
-    uint32_t ahead_stamp[AHEAD];
+    constexpr int AHEAD = FORM == 8 ? 2 : 0;               // slots of a thread, rows of a warp
+    int ahead_block[AHEAD + 1];
+    uint32_t ahead_stamp[AHEAD + 1];
+    uint2 ahead_row[AHEAD + 1];
+    __nv_bfloat16 key, lowest, highest;                    // of the digest
+    const __nv_bfloat16* keys = reinterpret_cast<const __nv_bfloat16*>(p.k_new) + (static_cast<size_t>(seq) * p.Hkv + p.h_star) * PI_HEAD_DIM;
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
         const int s = tid + i * APPEND_THREADS;
         ahead_block[i] = s < p.C ? slot_block[s] : 0;
         ahead_stamp[i] = s < p.C ? slot_stamp[s] : 0u;
     }
-    uint2 ahead_row[AHEAD];                                // 8 bits: rows of a warp
-    if (FORM == 8) {
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const int r = warp + i * APPEND_WARPS;
-            if (r < 2 * p.Hkv) ahead_row[i] = reinterpret_cast<const uint2*>(r & 1 ? p.v_new : p.k_new)[(static_cast<size_t>(seq) * p.Hkv + (r >> 1)) * 32 + lane];
-        }
+    for (int i = 0; i < AHEAD; ++i) {
+        const int r = warp + i * APPEND_WARPS;
+        if (r < 2 * p.Hkv) ahead_row[i] = reinterpret_cast<const uint2*>(r & 1 ? p.v_new : p.k_new)[(static_cast<size_t>(seq) * p.Hkv + (r >> 1)) * 32 + lane];
     }
-    const __nv_bfloat16 key = reinterpret_cast<const __nv_bfloat16*>(p.k_new)[(static_cast<size_t>(seq) * p.Hkv + p.h_star) * PI_HEAD_DIM + (tid & (PI_HEAD_DIM - 1))];
+    if (FORM == 8) key = keys[tid & (PI_HEAD_DIM - 1)];
     if (pos < 0) return;
     const int b = pos / p.B, t = pos - b * p.B;
     if (b >= p.max_blocks) {
@@ -75,8 +75,11 @@ append_kernel(AppendParams p) {
     int32_t* table = p.table + static_cast<size_t>(seq) * p.max_blocks;
     const long long block_bytes = FORM != 16 ? p.block_bytes : static_cast<long long>(p.Hkv) * 2 * p.B * PI_HEAD_DIM * 2;
     int slot = table[b];
-    __nv_bfloat16* digest = p.digest + (static_cast<size_t>(seq) * p.max_blocks + b) * 2 * PI_HEAD_DIM + (tid & (PI_HEAD_DIM - 1));
-    const __nv_bfloat16 lowest = digest[0], highest = digest[PI_HEAD_DIM];      // (of a block that is open)
+    if (FORM == 8) {
+        const __nv_bfloat16* digest = p.digest + (static_cast<size_t>(seq) * p.max_blocks + b) * 2 * PI_HEAD_DIM + (tid & (PI_HEAD_DIM - 1));
+        lowest = digest[0];
+        highest = digest[PI_HEAD_DIM];
+    }
     long long host_off = seq * p.host_stride + b * block_bytes;
     if (p.page) {
         // a block index beyond the sequence's row of the table is not followed (rows are page_stride long)
@@ -200,8 +203,16 @@ append_kernel(AppendParams p) {
     }
     // running min / max of the retrieval head's keys in this block (exact: bf16 values only)
     if (tid < PI_HEAD_DIM) {
-        if (t == 0 || __bfloat162float(key) < __bfloat162float(lowest)) digest[0] = key;
-        if (t == 0 || __bfloat162float(key) > __bfloat162float(highest)) digest[PI_HEAD_DIM] = key;
+        __nv_bfloat16* lo = p.digest + (static_cast<size_t>(seq) * p.max_blocks + b) * 2 * PI_HEAD_DIM + tid;
+        __nv_bfloat16* hi = lo + PI_HEAD_DIM;
+        if (FORM != 8) key = keys[tid];
+        if (t == 0) { *lo = key; *hi = key; }
+        else {
+            if (FORM != 8) lowest = *lo;
+            if (__bfloat162float(key) < __bfloat162float(lowest)) *lo = key;
+            if (FORM != 8) highest = *hi;
+            if (__bfloat162float(key) > __bfloat162float(highest)) *hi = key;
+        }
     }
 }
 
