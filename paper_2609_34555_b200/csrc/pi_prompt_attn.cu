@@ -26,7 +26,7 @@
 //
 // Measured on a B200 (32 query heads, 8 KV heads, bf16; 1 643 TFLOP/s is what a library product reaches in a short run, 1 394 for seconds):
 // one prompt of 8 192 tokens 436 us, 1 260 TFLOP/s, in a run of a few milliseconds, 510 us for longer, where the power limit takes the
-// clock from 1.7 to 1.45 GHz; 23 prompts of 0 to 1 500 tokens 172 us; 77 tokens 8.5 us; 16 sequences of one token after 16 384
+// clock from 1.7 to 1.45 GHz; 23 prompts of 0 to 1 500 tokens 172 us; 77 tokens 8.1 us; 16 sequences of one token after 16 384
 // 174 us, 6.2 TB/s, after 0 to 16 384 89 us (105 before the longest sequences came first); 500 tokens after 65 536 with 64 heads in fp16 930 us.  An iteration (two query tiles, one K/V tile) takes 3 270 cycles,
 // of which the tensor pipe and the exponentials are busy for 2 048 each.
 // Tried and not taken: a share of the exponentials as polynomials (3 % fewer cycles, the same time), P handed over in two halves, a
@@ -64,6 +64,8 @@ struct PromptParams {
     long long wait_cycles, v_tok, v_head;
     float scale_log2;                               // log2(e) / sqrt(D)
     int n_seqs, Hq, Hkv, G, tq, n_q, n_k;           // tq: tokens of a query tile
+    uint32_t per_block;                             // 2^32 / (2 tq), rounded up
+    int log_hkv;
     bool wide;                                      // out is aligned to 32 bytes
     int hold_last;                                  // test only: an item's last V tile is never fetched
 };
@@ -856,6 +858,11 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             // sequence come first; KV heads innermost.  32 sequences at a time are put in the order of their keys, so that the longest of them come first
             // too, and what is short fills the end.
             const int per_block = 2 * p.tq;
+            // (quotients by multiplication: a lone warp takes 200 cycles for a division, and the first item waits for five of them)
+            auto blocks_of = [&](int n) {
+                const unsigned x = static_cast<unsigned>(n + per_block - 1), q = __umulhi(x, p.per_block);
+                return static_cast<int>(q - (q * per_block > x));
+            };
             auto spans_from = [&](int s0, bool tell) {
                 Span x = span_of(p, s0 + lane, tell);
                 const int count = min(p.n_seqs - s0, 32);
@@ -877,21 +884,21 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 return x;
             };
             const Span mine = spans_from(0, blockIdx.x == 0);
-            int total = (mine.n + per_block - 1) / per_block;
-            for (int s0 = 32; s0 < p.n_seqs; s0 += 32) total += (span_of(p, s0 + lane, blockIdx.x == 0).n + per_block - 1) / per_block;
+            int total = blocks_of(mine.n);
+            for (int s0 = 32; s0 < p.n_seqs; s0 += 32) total += blocks_of(span_of(p, s0 + lane, blockIdx.x == 0).n);
             total = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(total)));
             unsigned place = blockIdx.x / static_cast<unsigned>(split);      // (of a cluster: its first CTA's)
             uint32_t asked = 0u;
             bool more = true;
             for (int it = 0;; ++it) {
                 Item w = {0, 0, 0, 0, 0, -1};
-                const int item = static_cast<int>(place / static_cast<unsigned>(p.Hkv));
+                const int item = static_cast<int>(place >> p.log_hkv);
                 const bool has = more && item < total;
                 if (has) {
                     int at = total - 1 - item;
                     for (int s0 = 0; s0 < p.n_seqs; s0 += 32) {
                         const Span x = s0 ? spans_from(s0, false) : mine;
-                        const int nb = (x.n + per_block - 1) / per_block;
+                        const int nb = blocks_of(x.n);
                         int upto = nb;
 #pragma unroll
                         for (int d = 1; d < 32; d <<= 1) {
@@ -904,7 +911,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                             w.first = (at - __shfl_sync(0xffffffffu, upto - nb, from)) * per_block;
                             w.q0 = __shfl_sync(0xffffffffu, x.q0, from); w.n = __shfl_sync(0xffffffffu, x.n, from);
                             w.k0 = __shfl_sync(0xffffffffu, x.k0, from); w.m = __shfl_sync(0xffffffffu, x.m, from);
-                            w.h = static_cast<int>(place % static_cast<unsigned>(p.Hkv));
+                            w.h = static_cast<int>(place) & (p.Hkv - 1);
                             break;
                         }
                         at -= __shfl_sync(0xffffffffu, upto, 31);
@@ -945,7 +952,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // (read before the next answer is written)
                     __syncwarp();
                     place /= static_cast<unsigned>(split);
-                } while (got && static_cast<int>(place / static_cast<unsigned>(p.Hkv)) >= total);
+                } while (got && static_cast<int>(place >> p.log_hkv) >= total);
                 more = got != 0u;
             }
         }
@@ -975,7 +982,7 @@ int make_map(pi_ctx* c, CUtensorMap* map, CUtensorMapDataType type, int rank, co
 int pi_launch_prompt_attn(pi_ctx* c, int n_seqs, int dtype, int n_q, int n_k, const void* q, int64_t q_tok, int64_t q_head, const void* k, int64_t k_tok, int64_t k_head,
                           const void* v, int64_t v_tok, int64_t v_head, const int32_t* q_start, const int32_t* k_start, void* out, float* lse, cudaStream_t stream) {
     const pi_config& cfg = c->cfg;
-    PromptParams p;
+    PromptParams p = {};
     p.q_start = q_start; p.k_start = k_start;
     p.out = out; p.lse = lse; p.v = v; p.v_tok = v_tok; p.v_head = v_head;
     p.st = pi_status_of(c);
@@ -983,6 +990,8 @@ int pi_launch_prompt_attn(pi_ctx* c, int n_seqs, int dtype, int n_q, int n_k, co
     p.scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(PI_HEAD_DIM));
     p.n_seqs = n_seqs; p.Hq = cfg.n_q_heads; p.Hkv = cfg.n_kv_heads; p.G = cfg.n_q_heads / cfg.n_kv_heads; p.n_q = n_q; p.n_k = n_k;
     p.tq = PA_ROWS / p.G;
+    p.per_block = static_cast<uint32_t>(0xffffffffu / (2 * p.tq) + 1);
+    while ((1 << p.log_hkv) < p.Hkv) ++p.log_hkv;  // (a power of two: pi_create)
     const CUtensorMapDataType type = dtype == PI_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     CUtensorMap map_q, map_k, map_v;
     {
