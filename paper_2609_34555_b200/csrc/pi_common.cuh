@@ -89,6 +89,7 @@ struct pi_ctx {
     void* encode_tiled_fn;
     // clusters of 2^i CTAs of the selection kernel that are resident at once, [plain | fused][i]; -1 = not asked yet
     int sd_resident_clusters[2][5];
+    int pa_resident_clusters[4]; // the same of the attention over prompts
 };
 
 struct pi_status_ref {

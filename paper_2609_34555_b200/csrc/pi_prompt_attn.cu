@@ -16,7 +16,7 @@
 // tensor core wants both operands of one type; weights in two halves would cost half as much again on the pipe that bounds the
 // call).  The sum of the weights, the maxima and all products' sums are in 32 bits.
 //
-// An item is a block of up to 2 tq tokens (tq = 128 / G) of a sequence and a KV head.  Where a block has one query tile, the two softmax groups
+// An item is a block of up to 2 tq tokens (tq = 128 / G; of tq where SMs would be idle) of a sequence and a KV head.  Where a block has one query tile, the two softmax groups
 // take every second K/V tile of it and are joined at the end.  CTAs stay and take over the places of CTAs that have not begun, the longest
 // sequences first, so that the next item's loads and first product run under the last one's end; few items with many keys are shared by
 // clusters of two to eight CTAs (the launcher's rule).
@@ -26,7 +26,7 @@
 //
 // Measured on a B200 (32 query heads, 8 KV heads, bf16; 1 643 TFLOP/s is what a library product reaches in a short run, 1 394 for seconds):
 // one prompt of 8 192 tokens 436 us, 1 260 TFLOP/s, in a run of a few milliseconds, 510 us for longer, where the power limit takes the
-// clock from 1.7 to 1.45 GHz; 23 prompts of 0 to 1 500 tokens 172 us; 77 tokens 8.1 us; 16 sequences of one token after 16 384
+// clock from 1.7 to 1.45 GHz; 23 prompts of 0 to 1 500 tokens 172 us; 77 tokens 7.2 us; 16 sequences of one token after 16 384
 // 174 us, 6.2 TB/s, after 0 to 16 384 89 us (105 before the longest sequences came first); 500 tokens after 65 536 with 64 heads in fp16 930 us.  An iteration (two query tiles, one K/V tile) takes 3 270 cycles,
 // of which the tensor pipe and the exponentials are busy for 2 048 each.
 // Tried and not taken: a share of the exponentials as polynomials (3 % fewer cycles, the same time), P handed over in two halves, a
@@ -47,7 +47,6 @@ static_assert(256 * PA_SOFTMAX_REGS + 128 * PA_OTHER_REGS <= PA_THREADS * 168, "
 constexpr int PA_SOFTMAX = 256;                     // threads of the softmax warps
 constexpr int PA_ROWS = 128;                        // rows of a query tile, and tokens of a K or V tile
 constexpr int PA_STAGES = 5;
-constexpr int PA_MAX_SPLIT = 8;                     // CTAs of a cluster that share an item
 constexpr int PA_HALF = PA_ROWS * 128;              // 64 channels of 128 rows
 constexpr int PA_TILE = 2 * PA_HALF;
 constexpr float PA_NO_MAX = -3.40282347e38f;        // the lowest number, for -infinity in the running maximum: differences are no NaN
@@ -64,7 +63,8 @@ struct PromptParams {
     long long wait_cycles, v_tok, v_head;
     float scale_log2;                               // log2(e) / sqrt(D)
     int n_seqs, Hq, Hkv, G, tq, n_q, n_k;           // tq: tokens of a query tile
-    uint32_t per_block;                             // 2^32 / (2 tq), rounded up
+    int per_block;                                  // tokens of an item: 2 tq, or tq
+    uint32_t by_block;                              // 2^32 / per_block, rounded up
     int log_hkv;
     bool wide;                                      // out is aligned to 32 bytes
     int hold_last;                                  // test only: an item's last V tile is never fetched
@@ -220,7 +220,7 @@ struct Plan {
     __device__ __forceinline__ Plan(const PromptParams& p, const Item& w, int rank, int split) {
         off = w.m - w.n;                            // token i sees the keys j < i + off + 1
         n_a = min(p.tq, w.n - w.first);
-        n_b = min(p.tq, max(0, w.n - w.first - p.tq));
+        n_b = min(p.per_block - p.tq, max(0, w.n - w.first - p.tq));
         auto upto = [&](int i) { return (seen(w, i) + PA_ROWS - 1) / PA_ROWS; };
         tiles_a = upto(w.first + n_a - 1);
         tiles_b = n_b ? upto(w.first + p.tq + n_b - 1) : tiles_a;
@@ -857,10 +857,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             // ---- warp 10: which items are this CTA's, or its cluster's.  Blocks are counted from the last one of the last sequence, so that the longest of a
             // sequence come first; KV heads innermost.  32 sequences at a time are put in the order of their keys, so that the longest of them come first
             // too, and what is short fills the end.
-            const int per_block = 2 * p.tq;
+            const int per_block = p.per_block;
             // (quotients by multiplication: a lone warp takes 200 cycles for a division, and the first item waits for five of them)
             auto blocks_of = [&](int n) {
-                const unsigned x = static_cast<unsigned>(n + per_block - 1), q = __umulhi(x, p.per_block);
+                const unsigned x = static_cast<unsigned>(n + per_block - 1), q = __umulhi(x, p.by_block);
                 return static_cast<int>(q - (q * per_block > x));
             };
             auto spans_from = [&](int s0, bool tell) {
@@ -990,7 +990,6 @@ int pi_launch_prompt_attn(pi_ctx* c, int n_seqs, int dtype, int n_q, int n_k, co
     p.scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(PI_HEAD_DIM));
     p.n_seqs = n_seqs; p.Hq = cfg.n_q_heads; p.Hkv = cfg.n_kv_heads; p.G = cfg.n_q_heads / cfg.n_kv_heads; p.n_q = n_q; p.n_k = n_k;
     p.tq = PA_ROWS / p.G;
-    p.per_block = static_cast<uint32_t>(0xffffffffu / (2 * p.tq) + 1);
     while ((1 << p.log_hkv) < p.Hkv) ++p.log_hkv;  // (a power of two: pi_create)
     const CUtensorMapDataType type = dtype == PI_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     CUtensorMap map_q, map_k, map_v;
@@ -1011,14 +1010,50 @@ int pi_launch_prompt_attn(pi_ctx* c, int n_seqs, int dtype, int n_q, int n_k, co
     }
     p.hold_last = cfg.test_hold_producer;
     p.wide = (reinterpret_cast<uintptr_t>(out) & 31u) == 0;
-    const long long per_block = 2 * p.tq, seqs = n_seqs < n_q ? n_seqs : n_q, blocks = (n_q + seqs * (per_block - 1)) / per_block, items = blocks * p.Hkv;
-    // CTAs that share an item: where the items leave SMs without work and the keys are many, a cluster for each, up to a power of two that fits the
-    // GPU once (and eight: fewer than eight clusters of 16 are resident at a time).  A cluster costs 2 to 4 us more than a CTA, and a K/V tile 1 us:
-    // 8 items of one token and 4 / 8 / 32 / 128 tiles take 10.2 / 13.4 / 33 / 120 us with 1 CTA each, 12.5 / 14.1 / 24 / 68 with 2,
-    // 11.4 / 12.4 / 18 / 40 with 4, 12.6 / 12.6 / 16 / 28 with 8.
+    const long long seqs = n_seqs < n_q ? n_seqs : n_q;
+    auto items_of = [&](int block) { return (n_q + seqs * (block - 1)) / block * p.Hkv; };
+    // Items of one query tile where each has an SM to itself: the two groups then share its K/V tiles.  77 tokens 7.2 us instead of 8.1, 512 11.1
+    // instead of 13.6, 100 after 4 000 20.7 instead of 29.7, 6 of 1 to 90 after 0 to 1 000 15.6 instead of 22.3.
+    p.per_block = items_of(p.tq) <= c->n_sms ? p.tq : 2 * p.tq;
+    p.by_block = 0xffffffffu / static_cast<uint32_t>(p.per_block) + 1;
+    const long long items = items_of(p.per_block);
+    const size_t smem = 2 * PA_TILE + PA_STAGES * PA_TILE + 1024;
+    cudaLaunchConfig_t lc = {};
+    lc.blockDim = dim3(PA_THREADS);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    // how many clusters of 2^power CTAs are resident at a time, asked once
+    auto resident = [&](int power) {
+        int& n = c->pa_resident_clusters[power];
+        if (n < 0) {
+            auto kernel = prompt_attn_kernel<__nv_bfloat16, true>;
+            cudaLaunchConfig_t one = lc;
+            attr[0].val.clusterDim.x = 1 << power;
+            one.gridDim = dim3(1 << power);
+            one.stream = nullptr;
+            one.attrs = attr;
+            one.numAttrs = 1;
+            if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess ||
+                cudaOccupancyMaxActiveClusters(&n, kernel, &one) != cudaSuccess) {
+                (void)cudaGetLastError();
+                n = 0;
+            }
+        }
+        return n;
+    };
+    // CTAs that share an item: where the items leave SMs without work and the keys are many, a cluster for each, of a power of two of CTAs up to
+    // eight, as long as all clusters are resident at once (16 of eight are not: 2 of 20 tokens after 8 000 37.9 us instead of 28.1 with four; of clusters
+    // of 16 fewer than eight are).  A cluster costs 2 to 4 us more than a CTA, and a K/V tile 1 us: 8 items of one token and 4 / 8 / 32 / 128 tiles take
+    // 10.2 / 13.4 / 33 / 120 us with 1 CTA each, 12.5 / 14.1 / 24 / 68 with 2, 11.4 / 12.4 / 18 / 40 with 4, 12.6 / 12.6 / 16 / 28 with 8.
     const long long tiles = (n_k / seqs + PA_ROWS - 1) / PA_ROWS;
     int split = 1;
-    while (split < PA_MAX_SPLIT && items * split * 2 <= c->n_sms && tiles >= 4 * split && tiles >= 8) split *= 2;
+    for (int power = 1; power <= 3 && tiles >= 4 * split && tiles >= 8 && items <= resident(power); ++power) split *= 2;
     // How long each sequence is, only the kernel sees; the rule goes by the mean.  Where several of them make up to two items an SM and keep it busy
     // for a while, one that is longer than the others would be what the call waits for, so there two CTAs share each item.  Sequences of
     // like length lose less by it than the others gain: 16 of one token after 16 384 take 175 us instead of 166, after 0 to 16 384
@@ -1028,23 +1063,12 @@ int pi_launch_prompt_attn(pi_ctx* c, int n_seqs, int dtype, int n_q, int n_k, co
     if (split == 1 && seqs > 1 && items <= 2 * c->n_sms && tiles > 32) split = 2;
     const long long grid = items * split;
     if (grid > INT32_MAX) return PI_ERR_UNSUPPORTED_DIM;
-    const size_t smem = 2 * PA_TILE + PA_STAGES * PA_TILE + 1024;
+    lc.gridDim = dim3(static_cast<unsigned>(grid));
+    attr[0].val.clusterDim.x = split;
+    lc.attrs = split > 1 ? attr : attr + 1;
+    lc.numAttrs = split > 1 ? 2 : 1;
     auto launch = [&](auto kernel) -> int {
         PI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
-        cudaLaunchConfig_t lc = {};
-        lc.gridDim = dim3(static_cast<unsigned>(items * split));
-        lc.blockDim = dim3(PA_THREADS);
-        lc.dynamicSmemBytes = smem;
-        lc.stream = stream;
-        cudaLaunchAttribute attr[2];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = split;
-        attr[0].val.clusterDim.y = 1;
-        attr[0].val.clusterDim.z = 1;
-        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[1].val.programmaticStreamSerializationAllowed = 1;
-        lc.attrs = split > 1 ? attr : attr + 1;
-        lc.numAttrs = split > 1 ? 2 : 1;
         PI_CUDA_TRY(cudaLaunchKernelEx(&lc, kernel, map_q, map_k, map_v, p));
         return PI_OK;
     };

@@ -318,6 +318,22 @@ def test_on_two_streams_at_once_and_in_a_replayed_graph():
         untouched(out, lse, a)
 
 
+@pytest.mark.parametrize("n,m", [([1], [2000]), ([40, 9], [900, 2500]), ([77], [77]), ([300] * 9, [300] * 9)])
+def test_the_first_call_of_a_context_may_be_captured(n, m):
+    pi = context(32, 8)
+    q, k, v, a, b = case(32, 8, n, m, seed=9)
+    qs, ks, out, lse = i32(a), i32(b), torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        pi.prompt_attn(q, k, v, qs, out, k_start=ks, lse=lse)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert pi.status()[0] == 0
+    check(q.dtype, out, lse, reference(q, k, v, a, b))
+    untouched(out, lse, a)
+
+
 def test_a_wait_that_runs_out_is_reported_and_the_next_call_works():
     """The last values of every piece of work never arrive (a test's switch): every CTA gives up after a millisecond, says so and ends."""
     held = context(8, 2, wait_limit_us=1000, test_hold_producer=1)
