@@ -25,8 +25,8 @@
 // rescaled; then the softmax warps do it themselves, between their S and their P, when no product of their tile is in flight.
 //
 // Measured on a B200 (32 query heads, 8 KV heads, bf16; 1 643 TFLOP/s is what a library product reaches in a short run, 1 394 for seconds):
-// one prompt of 8 192 tokens 436 us, 1 260 TFLOP/s, in a run of a few milliseconds, 510 us for longer, where the power limit takes the
-// clock from 1.7 to 1.45 GHz; 23 prompts of 0 to 1 500 tokens 172 us; 77 tokens 7.2 us; 16 sequences of one token after 16 384
+// one prompt of 8 192 tokens 434 us, 1 267 TFLOP/s, in a run of a few milliseconds, 505 us for longer, where the power limit takes the
+// clock from 1.7 to 1.45 GHz; 23 prompts of 0 to 1 500 tokens 172 us, 219 for longer; 77 tokens 7.1 us; 16 sequences of one token after 16 384
 // 174 us, 6.2 TB/s, after 0 to 16 384 89 us (105 before the longest sequences came first); 500 tokens after 65 536 with 64 heads in fp16 930 us.  An iteration (two query tiles, one K/V tile) takes 3 270 cycles,
 // of which the tensor pipe and the exponentials are busy for 2 048 each.
 // Tried and not taken: a share of the exponentials as polynomials (3 % fewer cycles, the same time), P handed over in two halves, a
@@ -215,15 +215,16 @@ struct Item {
 
 // What follows from an item, for every role alike.
 struct Plan {
-    int off, n_a, n_b, lo, hi, tiles_a, tiles_b, seen_first, odd_from;
+    int off, n_a, n_b, lo, hi, tiles_a, tiles_b, seen_first, odd_from, last_a, last_b;      // last_: keys that the last token of tile A, B sees
     bool pair;
     __device__ __forceinline__ Plan(const PromptParams& p, const Item& w, int rank, int split) {
         off = w.m - w.n;                            // token i sees the keys j < i + off + 1
         n_a = min(p.tq, w.n - w.first);
         n_b = min(p.per_block - p.tq, max(0, w.n - w.first - p.tq));
-        auto upto = [&](int i) { return (seen(w, i) + PA_ROWS - 1) / PA_ROWS; };
-        tiles_a = upto(w.first + n_a - 1);
-        tiles_b = n_b ? upto(w.first + p.tq + n_b - 1) : tiles_a;
+        last_a = seen(w, w.first + n_a - 1);
+        last_b = n_b ? seen(w, w.first + p.tq + n_b - 1) : last_a;
+        tiles_a = (last_a + PA_ROWS - 1) / PA_ROWS;
+        tiles_b = (last_b + PA_ROWS - 1) / PA_ROWS;
         pair = n_b == 0;                            // one query tile: the softmax groups take every second K/V tile each
         const int all = max(tiles_a, tiles_b);
         lo = static_cast<int>(static_cast<long long>(all) * rank / split);
@@ -692,22 +693,29 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 made ^= 1u << t;
                 return wait(B_P_FULL + t, phase);
             };
-            auto product_s = [&](int t, uint32_t q_step, uint32_t at) {
+            // (`half`: no row sees the upper 64 of a tile's keys, and they are left out of both products; the softmax masks what stands in their scores' place.
+            // 16 prompts of 1 024 tokens 159 us instead of 162)
+            auto product_s = [&](int t, uint32_t q_step, uint32_t at, bool half) {
                 const uint64_t qa = desc_q + q_step, kb = desc_k + at * tile_step;
+                const uint32_t idesc = half ? idesc_s - (static_cast<uint32_t>(PA_ROWS >> 4) << 17) : idesc_s;
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         const uint64_t step = static_cast<uint64_t>(((k >> 2) * PA_HALF + (k & 3) * 32) >> 4);
-                        tc_mma_ss(utmem + PA_TMEM_S + 128 * t, qa + step, kb + step, idesc_s, k > 0);
+                        tc_mma_ss(utmem + PA_TMEM_S + 128 * t, qa + step, kb + step, idesc, k > 0);
                     }
                     tc_commit(bar(B_S_FULL + t));
                 }
             };
-            auto product_o = [&](int t, uint32_t at, bool add) {
+            auto product_o = [&](int t, uint32_t at, bool add, bool half) {
                 const uint64_t vb = desc_v + at * tile_step;
                 if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) tc_mma_ts(utmem + PA_TMEM_O + 128 * t, utmem + PA_TMEM_S + 128 * t + 8 * k, vb + static_cast<uint64_t>((k * 2048) >> 4), idesc_o, add || k > 0);
+                    for (int k = 0; k < 4; ++k) tc_mma_ts(utmem + PA_TMEM_O + 128 * t, utmem + PA_TMEM_S + 128 * t + 8 * k, vb + static_cast<uint64_t>((k * 2048) >> 4), idesc_o, add || k > 0);
+                    if (!half) {
+#pragma unroll
+                        for (int k = 4; k < 8; ++k) tc_mma_ts(utmem + PA_TMEM_O + 128 * t, utmem + PA_TMEM_S + 128 * t + 8 * k, vb + static_cast<uint64_t>((k * 2048) >> 4), idesc_o, true);
+                    }
                 }
             };
             auto signal = [&](uint32_t place) {
@@ -723,16 +731,17 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 if (!wait(B_Q_FULL, items++ & 1u) || !full(stage)) { alive = false; break; }
                 tc_fence_after();
                 const int count = plan.hi - plan.lo;
+                auto half = [&](int t, int j) { return (t ? plan.last_b : plan.last_a) <= j * PA_ROWS + PA_ROWS / 2; };
                 if (plan.pair) {
                     // one query tile: S of the first two K tiles, then V after V; a group's next K is two tiles on, and is waited for behind the product
                     // with V, which frees a place for the loads
-                    product_s(0, 0u, stage);
+                    product_s(0, 0u, stage, half(0, plan.lo));
                     signal(B_KV_EMPTY + stage);
                     uint32_t sv = after(stage), sk = after(sv);
                     if (count > 1) {
                         if (!full(sk)) { alive = false; break; }
                         tc_fence_after();
-                        product_s(1, 0u, sk);
+                        product_s(1, 0u, sk, half(1, plan.lo + 1));
                         signal(B_KV_EMPTY + sk);
                     }
                     if (count <= 2) signal(B_Q_EMPTY);
@@ -743,13 +752,13 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         alive = full_v(sv, plan.lo + x >= plan.odd_from) && weights(t);
                         if (!alive) break;
                         tc_fence_after();
-                        product_o(t, sv, x >= 2);
+                        product_o(t, sv, x >= 2, half(t, plan.lo + x));
                         signal(B_KV_EMPTY + sv);
                         if (next) {
                             alive = full(sk);
                             if (!alive) break;
                             tc_fence_after();
-                            product_s(t, 0u, sk);
+                            product_s(t, 0u, sk, half(t, plan.lo + x + 2));
                             signal(B_KV_EMPTY + sk);
                             if (x + 3 == count) signal(B_Q_EMPTY);
                         } else signal(B_O_FULL + t);
@@ -758,8 +767,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     stage = after(sv);
                 } else {
                     const bool a_some = plan.lo < plan.tiles_a;
-                    if (a_some) product_s(0, 0u, stage);
-                    product_s(1, tile_step, stage);          // (tile B sees as many tiles as the item has)
+                    if (a_some) product_s(0, 0u, stage, half(0, plan.lo));
+                    product_s(1, tile_step, stage, half(1, plan.lo));          // (tile B sees as many tiles as the item has)
                     signal(B_KV_EMPTY + stage);
                     if (count == 1) signal(B_Q_EMPTY);
                     uint32_t sv = after(stage);
@@ -771,24 +780,24 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         if (j < plan.tiles_a) {
                             if (!weights(0)) { alive = false; break; }
                             tc_fence_after();
-                            product_o(0, sv, x > 0);
+                            product_o(0, sv, x > 0, half(0, j));
                         }
                         if (next && !full(sk)) { alive = false; break; }
                         if (j < plan.tiles_a) {
                             if (j + 1 < plan.tiles_a) {
                                 tc_fence_after();
-                                product_s(0, 0u, sk);
+                                product_s(0, 0u, sk, half(0, j + 1));
                             } else signal(B_O_FULL);
                         }
                         if (!weights(1)) { alive = false; break; }
                         tc_fence_after();
-                        product_o(1, sv, x > 0);
+                        product_o(1, sv, x > 0, half(1, j));
                         signal(B_KV_EMPTY + sv);
                         if (next) {
                             alive = full_v(sv_next, j + 1 >= plan.odd_from);
                             if (!alive) break;
                             tc_fence_after();
-                            product_s(1, tile_step, sk);
+                            product_s(1, tile_step, sk, half(1, j + 1));
                             signal(B_KV_EMPTY + sk);
                             if (x + 2 == count) signal(B_Q_EMPTY);
                         } else signal(B_O_FULL + 1);
