@@ -92,6 +92,33 @@ def test_few_queries_over_many_keys(Hq, Hkv, n, m):
         untouched(out, lse, qs)
 
 
+# so many sequences of one token beside the others that the items are of two query tiles, whatever the GPU's SMs
+ONES = [1] * 250
+
+
+@pytest.mark.parametrize("Hq,Hkv,dtype", [(1, 1, torch.bfloat16), (4, 1, torch.float16), (8, 2, torch.bfloat16), (10, 2, torch.bfloat16), (16, 1, torch.bfloat16), (7, 1, torch.float16)])
+@pytest.mark.parametrize("n,m", LENGTHS + [([64, 65, 63], [64, 192, 255]), ([256, 129], [320, 130])])
+def test_two_query_tiles_an_item(Hq, Hkv, dtype, n, m):
+    pi = context(Hq, Hkv, max_batch=300)
+    n, m = n + ONES, m + ONES
+    q, k, v, qs, ks = case(Hq, Hkv, n, m, dtype, seed=sum(n) + Hq)
+    out, lse = run(pi, q, k, v, qs, ks)
+    check(q.dtype, out, lse, reference(q, k, v, qs, ks))
+    untouched(out, lse, qs)
+
+
+@pytest.mark.parametrize("Hq,Hkv,batch,n,m,dtype", [(8, 8, 10, 200, 5000, torch.bfloat16), (16, 4, 20, 50, 4400, torch.float16), (12, 4, 20, 70, 4300, torch.bfloat16)])
+def test_two_ctas_share_items_of_two_query_tiles(Hq, Hkv, batch, n, m, dtype):
+    r = random.Random(batch + n)
+    lens = [n] + [r.randrange(n // 2, n + 1) for _ in range(batch - 3)] + [0, 1]
+    keys = [m + 700 + r.randrange(0, 600) for _ in range(batch - 2)] + [9, 300]
+    q, k, v, qs, ks = case(Hq, Hkv, lens, keys, dtype, seed=n)
+    pi = context(Hq, Hkv)
+    out, lse = run(pi, q, k, v, qs, ks)
+    check(q.dtype, out, lse, reference(q, k, v, qs, ks))
+    untouched(out, lse, qs)
+
+
 def test_a_prompt_of_many_blocks_and_a_large_batch():
     pi = context(4, 1, max_batch=300)
     for lens in ([1900], [1 + 7 * (i % 29) for i in range(300)]):
@@ -142,11 +169,11 @@ def test_strides_and_no_lse():
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
-@pytest.mark.parametrize("n,m", [([200, 61, 3], [200, 61, 3]), ([2, 70], [300, 1000])])
+@pytest.mark.parametrize("n,m", [([200, 61, 3], [200, 61, 3]), ([2, 70], [300, 1000]), ([200, 61, 3] + ONES, [200, 61, 3] + ONES), ([2, 70] + ONES, [300, 1000] + ONES)])
 def test_what_is_not_seen_does_not_reach_a_row(dtype, n, m):
     """Infinities and NaN in keys and values: rows that see them are what the sums make of them, all others are as without them.  In the
     tokens behind a sequence, in its neighbours, and in its own future."""
-    pi = context(8, 2)
+    pi = context(8, 2, max_batch=300)
     q, k, v, qs, ks = case(8, 2, n, m, dtype, seed=5, pad=40)
     base, base_lse = run(pi, q, k, v, qs, ks)
     bad_v = [(ks[1] - 1, 0, 3, float("nan")), (ks[1] - min(m[0], 30), 1, 9, float("inf")), (ks[1], 0, 70, float("-inf")), (ks[-1] + 2, 0, 5, float("nan")), (ks[-1] + 39, 1, 127, float("inf"))]
@@ -199,11 +226,12 @@ def test_scores_of_any_size(dtype, scale):
                     assert bool(((out[i, h] - want).abs() <= torch.finfo(dtype).eps * want.abs() + 2.0 ** -20).all())
 
 
-def test_scores_that_rise_from_key_to_key():
+@pytest.mark.parametrize("others", [[], ONES])
+def test_scores_that_rise_from_key_to_key(others):
     """Every tile's largest score is above the last one's by more than a factor of 2^8 after the exponential: the reference moves each time."""
-    pi = context(4, 1)
+    pi = context(4, 1, max_batch=300)
     n = 700
-    q, k, v, qs, ks = case(4, 1, [n], [n], seed=2)
+    q, k, v, qs, ks = case(4, 1, [n] + others, [n] + others, seed=2)
     q[:], k[:] = 0, 0
     q[..., 0] = 1.0
     k[..., 0] = (torch.arange(k.shape[0]) * 0.5).to(torch.bfloat16).cuda()[:, None]
