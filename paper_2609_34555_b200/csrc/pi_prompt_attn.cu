@@ -610,25 +610,24 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         if (warp == 9) {
             // ---- TMA: Q, then K0 V0 K1 V1 ...
             uint32_t n = 0u, items = 0u;            // loads, and items with any, so far
-            bool alive = true, q_issued = false, few_before = true;
-            int read = 0;                           // items whose shares have been read, as far as this warp has waited for it
+            bool alive = true, q_issued = false, shares = false;     // shares: those of an earlier item lie where loads go
             Item w;
             for (int it = 0; alive && item_of(it, w); ++it) {
                 const Plan plan(p, w, rank, split);
                 done_with(it);
-                if (SPLIT) {
-                    // Where the last item's shares lie in the way of this one's loads, they have to have been read; those of the one before
-                    // that have been, or will be in a moment (and every phase of the barrier is waited for once).
-                    const bool in_the_way = it > 0 && (!few_before || plan.n_b);
-                    for (; read < (in_the_way ? it : it - 1); ++read)
-                        if (!wait_cluster(B_SHARE_EMPTY, read & 1)) { alive = false; break; }
-                    if (!alive) break;
-                    if (in_the_way) asm volatile("fence.proxy.async;" ::: "memory");
-                    few_before = plan.pair && plan.n_a * p.G <= PA_FEW;
-                }
+                const bool in_the_way = SPLIT && it > 0 && (shares || plan.n_b), few = plan.pair && plan.n_a * p.G <= PA_FEW;
+                shares |= SPLIT && !few;
                 if (plan.hi <= plan.lo) {
                     if (rank == 0 && lane == 0) mbar_arrive(bar(B_WANTED));
                     continue;
+                }
+                if (in_the_way) {
+                    // The shares of the last item have to have been read, and with them all before it (an item is told when the cluster is done
+                    // with the one before the last).  This phase and no other can be told by its parity: the one before it is over, and the next ends
+                    // behind the loads that this warp is about to issue.
+                    if (!wait_cluster(B_SHARE_EMPTY, (it - 1) & 1)) { alive = false; break; }
+                    asm volatile("fence.proxy.async;" ::: "memory");
+                    shares = !few;
                 }
                 if (items && !wait(B_Q_EMPTY, (items - 1) & 1u)) { alive = false; break; }
                 if (lane == 0) {

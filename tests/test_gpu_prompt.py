@@ -408,3 +408,41 @@ def test_keys_beyond_32_bits_of_an_address():
     torch.cuda.synchronize()
     assert pi.status()[0] == 0
     check(q.dtype, out, lse, reference(q, k, v, qs, ks))
+
+
+# ------------------------------------------------------------------ clusters that share items, and many sequences
+MANY = [(4, 1, [1] * 256, [4500] * 256),
+        (8, 8, [0] * 2016 + [1] * 32, [0] * 2016 + [8000] * 32),
+        (8, 8, ([0] * 31 + [1]) * 32, ([0] * 31 + [8000]) * 32)]
+
+
+@pytest.mark.parametrize("Hq,Hkv,n,m", MANY, ids=["256 of one token", "the last 32 of 2048", "every 32nd of 1024"])
+def test_shared_items_of_few_rows_among_many_sequences(Hq, Hkv, n, m):
+    """Three items and more a cluster, each of which is told late: the looking through hundreds of sequences comes before it."""
+    pi = context(Hq, Hkv, max_batch=2048, wait_limit_us=20000)
+    q, k, v, qs, ks = case(Hq, Hkv, n, m, seed=len(n), pad=0)
+    out, lse = run(pi, q, k, v, qs, ks)
+    check(q.dtype, out, lse, reference(q, k, v, qs, ks))
+    a, b, o, l = i32(qs), i32(ks), torch.empty_like(out), torch.empty_like(lse)
+    for _ in range(20):
+        pi.prompt_attn(q, k, v, a, o, k_start=b, lse=l)
+    torch.cuda.synchronize()
+    assert pi.status()[0] == 0 and torch.equal(o, out) and torch.equal(l, lse)
+
+
+def test_shared_items_with_and_without_rows_of_the_second_tile_and_with_empty_ranges():
+    """Clusters whose items follow each other in every order: few rows and many, one query tile and two, keys for every CTA, for one, for none."""
+    r = random.Random(8)
+    n = [r.choice([0, 1, 1, 30, 70, 128, 140, 250]) for _ in range(100)]
+    m = [r.choice([0, 1, 9, 128, 129, 300]) if i % 5 == 1 else 5600 + r.randrange(0, 900) for i in range(100)]
+    pi = context(2, 2, max_batch=100, wait_limit_us=20000)
+    q, k, v, qs, ks = case(2, 2, n, m, seed=8)
+    assert 2 * (q.shape[0] + 100 * 255) // 256 <= 296 and sum(m) // 100 > 33 * 128       # up to two items an SM, keys enough: two CTAs each
+    out, lse = run(pi, q, k, v, qs, ks)
+    check(q.dtype, out, lse, reference(q, k, v, qs, ks))
+    untouched(out, lse, qs)
+    a, b, o, l = i32(qs), i32(ks), torch.full_like(out, 7.0), torch.full_like(lse, 7.0)
+    for _ in range(20):
+        pi.prompt_attn(q, k, v, a, o, k_start=b, lse=l)
+    torch.cuda.synchronize()
+    assert pi.status()[0] == 0 and torch.equal(o, out) and torch.equal(l, lse)
