@@ -300,7 +300,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     if (tid == 0) {
         for (uint32_t i = 0; i < B_COUNT; ++i) {
             const bool by_warps = i == B_P_FULL || i == B_P_FULL + 1 || i == B_MERGED || i == B_HALF;
-            mbar_init(bar(i), by_warps ? 4 : i == B_ALL ? 8 : i == B_SHARE_FULL || i == B_SHARE_EMPTY ? 8 * split : i == B_ITEM_EMPTY || i == B_ITEM_EMPTY + 1 ? 11 * split : 1);
+            mbar_init(bar(i), by_warps ? 4 : i == B_ALL ? 8 : i == B_SHARE_FULL || i == B_SHARE_EMPTY ? 8 * split : i == B_ITEM_EMPTY || i == B_ITEM_EMPTY + 1 ? 11 * split : i >= B_KV_EMPTY && i < B_KV_EMPTY + PA_STAGES ? 2 : 1);
         }
         s_abort = 0;
         s_odd[0] = s_odd[1] = 0;
@@ -813,18 +813,22 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         } else if (warp == 11) {
             // ---- a V tile that some row must not see all of is looked through: rows behind the sequence's end become 0, and so does every
             // value that is no number (its weight would be 0 where it is masked, and 0 times it is none); those are put back at the
-            // end, row by row
+            // end, row by row.  A stage is given back by this warp as well as by the products, whether it is looked through or not: the phases
+            // of its loads are told by parity, and none may go by meanwhile.
             uint32_t n = 0u;
             bool alive = true;
             Item w;
             for (int it = 0; alive && item_of(it, w); ++it) {
                 const Plan plan(p, w, rank, split);
                 bool odd = false;
-                for (int i = 2 * plan.lo; i < 2 * plan.hi; ++i, ++n) {         // (every load is waited for: a phase is told from the one before the last by the order alone)
+                for (int i = 2 * plan.lo; i < 2 * plan.hi; ++i, ++n) {
                     const uint32_t stage = n % PA_STAGES, tile = ring + stage * PA_TILE;
                     if (!wait(B_KV_FULL + stage, (n / PA_STAGES) & 1u)) { alive = false; break; }
                     const int j = i >> 1;
-                    if (!(i & 1) || j < plan.odd_from) continue;
+                    if (!(i & 1) || j < plan.odd_from) {
+                        if (lane == 0) mbar_arrive(bar(B_KV_EMPTY + stage));
+                        continue;
+                    }
                     const int rows = min(w.m - j * PA_ROWS, PA_ROWS), from = max(plan.seen_first - j * PA_ROWS, 0);      // of the sequence; not seen by all
                     for (int half = 0; half < 2; ++half) {
                         const uint32_t at = tile + half * PA_HALF + lane * 16;
@@ -857,7 +861,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     if (odd) s_odd[it & 1] = 1;
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(B_V_GOOD + stage));
+                    if (lane == 0) {
+                        mbar_arrive(bar(B_V_GOOD + stage));
+                        mbar_arrive(bar(B_KV_EMPTY + stage));
+                    }
                 }
                 done_with(it);
             }

@@ -446,3 +446,31 @@ def test_shared_items_with_and_without_rows_of_the_second_tile_and_with_empty_ra
         pi.prompt_attn(q, k, v, a, o, k_start=b, lse=l)
     torch.cuda.synchronize()
     assert pi.status()[0] == 0 and torch.equal(o, out) and torch.equal(l, lse)
+
+
+@pytest.mark.parametrize("Hq,Hkv,batch", [(8, 8, 24), (4, 1, 12), (8, 1, 3)])
+def test_tiles_that_take_long_to_look_through_between_others(Hq, Hkv, batch):
+    """Prompts whose last tiles are full of infinities, so that each is rewritten, between sequences that see all of theirs: every load of either
+    kind is followed, and the result is there within a short limit of the waits."""
+    n = [1 if i % 2 else 129 for i in range(batch)]
+    m = [1280 if i % 2 else 900 + 128 * (i % 3) for i in range(batch)]
+    q, k, v, qs, ks = case(Hq, Hkv, n, m, seed=batch)
+    pi = context(Hq, Hkv, wait_limit_us=20000)
+    want, want_lse = run(pi, q, k, v, qs, ks)
+    check(q.dtype, want, want_lse, reference(q, k, v, qs, ks))
+    for i in range(0, batch, 2):
+        v[ks[i + 1] - 128:ks[i + 1], :, ::3] = float("inf")                            # seen by all rows but the first, from one key on
+    a, b, out, lse = i32(qs), i32(ks), torch.full_like(want, 7.0), torch.full_like(want_lse, 7.0)
+    for _ in range(50):
+        pi.prompt_attn(q, k, v, a, out, k_start=b, lse=lse)
+    torch.cuda.synchronize()
+    assert pi.status()[0] == 0, pi.status()
+    assert torch.equal(lse, want_lse)
+    keep = [d for d in range(128) if d % 3]
+    assert torch.equal(out[..., keep], want[..., keep])
+    for i in range(batch):
+        rows = out[qs[i]:qs[i + 1], :, ::3].float()
+        if i % 2:
+            assert torch.equal(rows, want[qs[i]:qs[i + 1], :, ::3].float())
+        else:
+            assert torch.equal(rows[0], want[qs[i], :, ::3].float()) and bool((rows[1:] == float("inf")).all())
