@@ -485,6 +485,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll 1
                 for (int x = 0; x < 4; ++x) {
                     float o[32];
+                    __syncwarp();                   // (rows of no query, and rows that see different numbers of odd values, come here at different times)
                     if (some) {
                         tc_ld32(at_o + 32 * x, o);
                         tc_wait_ld(o);

@@ -474,3 +474,25 @@ def test_tiles_that_take_long_to_look_through_between_others(Hq, Hkv, batch):
             assert torch.equal(rows, want[qs[i]:qs[i + 1], :, ::3].float())
         else:
             assert torch.equal(rows[0], want[qs[i], :, ::3].float()) and bool((rows[1:] == float("inf")).all())
+
+
+@pytest.mark.parametrize("Hq,Hkv,n,m", [(4, 4, [50], [70]), (8, 1, [5], [2500]), (4, 4, [40, 129] + [1] * 80, [60, 300] + [1] * 80), (2, 2, [30] * 30, [4700] * 30)])
+def test_rows_of_a_warp_that_see_different_numbers_of_infinite_values(Hq, Hkv, n, m):
+    """Every key of the last ones has an infinity of its own: a warp's rows look at different numbers of them, and some of its rows are of no query."""
+    q, k, v, qs, ks = case(Hq, Hkv, n, m, seed=3)
+    pi = context(Hq, Hkv, max_batch=100, wait_limit_us=20000)
+    want, want_lse = run(pi, q, k, v, qs, ks)
+    put = []
+    for s, e in enumerate(ks[1:]):
+        for x in range(min(n[s], 40)):                                                 # key e - 1 - x: channel 3 x + 1 of every head
+            v[e - 1 - x, :, 3 * x + 1] = float("inf") if x % 2 else -float("inf")
+            put.append((s, x))
+    out, lse = run(pi, q, k, v, qs, ks)
+    assert torch.equal(lse, want_lse)
+    expect = want.float()
+    for s, x in put:                                                                   # the last x + 1 queries see it
+        expect[qs[s + 1] - 1 - x:qs[s + 1], :, 3 * x + 1] = float("inf") if x % 2 else -float("inf")
+    got = out.float()
+    assert torch.equal(torch.isinf(got), torch.isinf(expect)) and torch.equal(got[torch.isinf(got)], expect[torch.isinf(expect)])
+    assert torch.equal(got[~torch.isinf(got)], expect[~torch.isinf(expect)])
+    untouched(out, lse, qs)
