@@ -14,7 +14,9 @@
 // While one tile's softmax runs, the tensor pipe works on the other tile's products.  P takes S's place in tensor memory, in 16 bits: a
 // weight is rounded to the type of V, which adds to a result in the mean square about what the rounding of the output itself does (the
 // tensor core wants both operands of one type; weights in two halves would cost half as much again on the pipe that bounds the
-// call).  The sum of the weights, the maxima and all products' sums are in 32 bits.
+// call).  In fp16 they are counted 2^7 times as large, up to 2^15, so that they keep 11 bits down to 2^-21 of the row's reference and are off
+// by 2^-32 of it at most below that: a long tail under one large score keeps its share.  The sum of the weights, the maxima and all
+// products' sums are in 32 bits.
 //
 // An item is a block of up to 2 tq tokens (tq = 128 / G; of tq where SMs would be idle) of a sequence and a KV head.  Where a block has one query tile, the two softmax groups
 // take every second K/V tile of it and are joined at the end.  CTAs stay and take over the places of CTAs that have not begun, the longest
@@ -165,6 +167,7 @@ __device__ __forceinline__ uint64_t desc_mn_major(uint32_t addr) {
 template <typename T> struct Form;
 template <> struct Form<__nv_bfloat16> {
     static constexpr uint32_t code = 1u;            // of the instruction descriptor
+    static constexpr float lift = 0.f;              // weights are 2^lift times as large: a weight is at most 2^8 before
     static constexpr uint32_t exponent = 0x7f807f80u, one = 0x00800080u;
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack_bf16(lo, hi); }
     // the larger magnitudes of two pairs, NaN where either is NaN (one operation)
@@ -176,6 +179,7 @@ template <> struct Form<__nv_bfloat16> {
 };
 template <> struct Form<__half> {
     static constexpr uint32_t code = 0u;
+    static constexpr float lift = 7.f;
     static constexpr uint32_t exponent = 0x7c007c00u, one = 0x04000400u;
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
         const __half2 v = __floats2half2_rn(lo, hi);
@@ -416,11 +420,12 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 // The weight is 2^(s c - mc), one fused operation and the exponential: mc is what the row's weights are counted from, and its
                 // rounding is in all of them alike.  Where it is large that rounding would leave the range of the weights, so there the
                 // maximum is taken off before the scale.
-                float2 less = make_float2(-mc, -mc);
+                constexpr float lift = Form<T>::lift;
+                float2 less = make_float2(lift - mc, lift - mc);
                 if (far) {
 #pragma unroll
                     for (int x = 0; x < 128; ++x) s[x] -= m;
-                    less = make_float2(0.f, 0.f);
+                    less = make_float2(lift, lift);
                 }
                 const float2 cc = make_float2(c, c);
                 float2 sum = make_float2(0.f, 0.f);
@@ -536,7 +541,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 }
                 if (SPLIT) {
                     if (real) asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(share_ml + static_cast<uint32_t>(128 * t + r) * 8u), "f"(mc), "f"(l) : "memory");
-                } else if (real && p.lse) p.lse[row] = none ? -INFINITY : (mc + log2f(l)) * 0.6931471805599453f;
+                } else if (real && p.lse) p.lse[row] = none ? -INFINITY : (mc + (log2f(l) - Form<T>::lift)) * 0.6931471805599453f;
             }
             tc_fence_before();
             if (SPLIT) {
@@ -589,7 +594,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         const float by = nothing ? 0.f : 1.f / sum_of[u];
                         *reinterpret_cast<uint2*>(static_cast<T*>(p.out) + row_of[u] * PI_HEAD_DIM + 4 * quad) =
                             nothing ? make_uint2(0u, 0u) : make_uint2(Form<T>::pack(o[u].x * by, o[u].y * by), Form<T>::pack(o[u].z * by, o[u].w * by));
-                        if (p.lse && quad == 0) p.lse[row_of[u]] = nothing ? -INFINITY : (top[u] + log2f(sum_of[u])) * 0.6931471805599453f;
+                        if (p.lse && quad == 0) p.lse[row_of[u]] = nothing ? -INFINITY : (top[u] + (log2f(sum_of[u]) - Form<T>::lift)) * 0.6931471805599453f;
                     }
                 }
                 arrive_at_all(B_SHARE_EMPTY);

@@ -496,3 +496,26 @@ def test_rows_of_a_warp_that_see_different_numbers_of_infinite_values(Hq, Hkv, n
     assert torch.equal(torch.isinf(got), torch.isinf(expect)) and torch.equal(got[torch.isinf(got)], expect[torch.isinf(expect)])
     assert torch.equal(got[~torch.isinf(got)], expect[~torch.isinf(expect)])
     untouched(out, lse, qs)
+
+
+@pytest.mark.parametrize("nats", [5.0, 14.0, 17.0])
+@pytest.mark.parametrize("Hq,Hkv,n,m,at", [(4, 1, 1, 65537, 0), (4, 1, 1, 65537, 40000), (2, 2, 40, 20000, 0), (16, 16, 1200, 6000, 3), (16, 16, 1200, 6000, 5000)])
+def test_a_long_tail_under_one_large_score_in_fp16(Hq, Hkv, n, m, at, nats):
+    """One key far above all others, of value 0: the result is what the others' small weights make of it.  Weights are counted 2^7 times as
+    large as under the reference, which the largest is never below, so they are off by half a step (2^-11 of themselves) or by 2^-25-7
+    of the largest."""
+    q, k, v, qs, ks = case(Hq, Hkv, [n], [m], torch.float16, seed=m, pad=0)
+    q[..., 0] = 128 ** 0.5
+    k *= 0.1
+    k[..., 0] = 0
+    k[at, :, 0] = nats
+    v += 2
+    v[at] = 0
+    pi = context(Hq, Hkv)
+    out, lse = run(pi, q, k, v, qs, ks)
+    ref = reference(q, k, v, qs, ks)
+    check(q.dtype, out, lse, ref)
+    want, want_lse, spread, thin, _ = ref
+    tol = 2.0 ** -11 * want.abs() + (2.0 ** -11 + 2.0 ** -15) * spread + 2.0 ** -32 * thin + 2.0 ** -25
+    over = float(((out.cpu().double() - want).abs() / tol).max())
+    assert over <= 1.0, over
