@@ -5,11 +5,13 @@
 // conversion a pair, exactly, and the scales never meet them: K's multiplies the products, V's the weights.  The contractions run on
 // mma.sync (tokens or channels on M, up to 8 query heads on N), whose operands are registers, where the numbers are converted; with 4
 // to 16 query heads on N the matrix pipe is far from busy.  Queries are exact in fp16 after a power of two per head.  A weight times V's scale
-// is rounded to 11 bits (an eighth of the output's own rounding in the mean square); all sums are in 32 bits.
+// is rounded to 11 bits (an eighth of the output's own rounding in the mean square), below 2^-21 of its reference to a multiple of 2^-31
+// of it; all sums are in 32 bits.
 //
 // Weights are counted from two references a head: the sum from the largest score, the products with V from the largest score times
 // scale (of V).  So a block whose values are small next to another's, and whose weights are not, keeps its bits, and no weight leaves fp16.
-// Both move only when they are exceeded by 2^8.
+// Both move only when they are exceeded by 2^8; the products' weights are 2^7 times as large, up to 2^15, so that a long tail under one large
+// score keeps its bits too.
 //
 // One (sequence, KV head) per cluster of S CTAs of 4, 8 or 16 warps (S = 1, 2, 4 or 8; both by the launcher's rule).  The item's
 // 16-token tiles are dealt out to its warps in turn; a warp streams its own tiles through its own ring of shared-memory
@@ -31,6 +33,7 @@ namespace {
 using namespace pi_attn;
 
 constexpr int A8_TILE_BYTES = 4096;                // 16 tokens: K, then V
+constexpr float A8_LIFT = 7.f;                     // log2 of the factor of the products' weights
 __host__ __device__ constexpr int a8_stages(int NT) { return NT == 1 ? 3 : 6; }          // tiles in the ring
 __host__ __device__ constexpr int a8_warps_per_sm(int NT) { return NT == 1 ? 16 : 8; }   // what the registers allow
 
@@ -292,7 +295,7 @@ attn_kv8_kernel(Attn8Params p) {
             float w[4];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const float t0 = s[nt][e] - m[nt][e], t1 = s[nt][2 + e] - m[nt][e], by = v_log - d[nt][e];
+                const float t0 = s[nt][e] - m[nt][e], t1 = s[nt][2 + e] - m[nt][e], by = v_log - d[nt][e] + A8_LIFT;
                 l[nt][e] += ex2(t0) + ex2(t1);
                 w[e] = ex2(t0 + by);
                 w[2 + e] = ex2(t1 + by);
@@ -329,8 +332,8 @@ attn_kv8_kernel(Attn8Params p) {
 #pragma unroll
             for (int x = 4; x <= 16; x <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
             const int g = nt * 8 + 2 * c + e;
-            // 2^d, in two steps: scales reach from 2^-117 to 2^120
-            const float f = m[nt][e] == A4_NO_MAX ? 0.f : ex2(0.5f * d[nt][e]);
+            // 2^d without the factor, in two steps: scales reach from 2^-117 to 2^120
+            const float f = m[nt][e] == A4_NO_MAX ? 0.f : ex2(0.5f * (d[nt][e] - A8_LIFT));
             if (g >= p.G) continue;
 #pragma unroll
             for (int x = 0; x < 8; ++x) {

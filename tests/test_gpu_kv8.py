@@ -680,3 +680,69 @@ def test_prompt_to_attention_through_pages_rotation_prompt_attention_store_recal
     assert np.array_equal(pool.cpu().numpy(), pools)
     check_attention(pi, dict(pool=pools, blocks=sel, slots=sel, count=nb, ctx=lens, q=qd.float().cpu().numpy()), o1, l1)
     pi.close()
+
+
+@pytest.mark.parametrize("nats", [5.0, 14.0, 17.0])
+@pytest.mark.parametrize("Hq,B,K,at", [(4, 64, 1024, 0), (4, 64, 1024, 40000), (16, 64, 1024, 70), (8, 32, 1000, 31999)])
+def test_a_long_tail_under_one_large_score(Hq, B, K, at, nats):
+    """One key far above all others, of value 0: the result is what the others' small weights make of it.  The products' weights are counted 2^7
+    times as large as under their reference, the largest weight times scale at most: each is off by half a step (2^-11 of itself) or by
+    2^-25-7 of the reference, times a number of up to 2^8 that is twice its block's largest value over its scale at most."""
+    pi = context(n_q_heads=Hq, n_kv_heads=1, block_tokens=B, budget_blocks=K, pool_slots=K, max_blocks=K, max_batch=1)
+    rng = np.random.default_rng(Hq + B)
+    kv = rng.standard_normal((K, 1, 2, B, 128)) * np.asarray([0.1, 1.0])[:, None, None]
+    kv[:, :, 1] += 2
+    kv[:, :, 0, :, 0] = 0
+    kv[at // B, 0, 0, at % B, 0], kv[at // B, 0, 1, at % B] = nats, 0
+    pool = ref.pack(ref.bf16(kv), B)[None]
+    q = ref.bf16(rng.standard_normal((1, Hq, 128)))
+    q[..., 0] = ref.bf16(np.float64(128 ** 0.5))
+    order = np.arange(K, dtype=np.int32)[None]
+    case = dict(pool=pool, blocks=order, slots=order, count=np.asarray([K], dtype=np.int32), ctx=np.asarray([K * B]), q=q)
+    out, lse = run_attention(pi, case)
+    check_attention(pi, case, out, lse)
+    k, v = (x.reshape(K * B, 128) for x in np.moveaxis(ref.unpack(pool[0], 1, B)[:, 0], 1, 0))
+    top = np.repeat(np.abs(v).reshape(K, B * 128).max(1), B)
+    for g in range(Hq):
+        z = k @ q[0, g].astype(np.float64) / np.sqrt(128)
+        w = np.exp(z - z.max())
+        w /= w.sum()
+        eps = (8 * 2.0 ** -23 * (np.abs(k) @ np.abs(q[0, g].astype(np.float64))).max() + 4 * 2.0 ** -24 * np.abs(z).max() * np.sqrt(128)) / np.sqrt(128)
+        want, spread = w @ v, w @ np.abs(v)
+        tol = 2.0 ** -8 * np.abs(want) + (2 * eps + 2.0 ** -11 + 2.0 ** -20) * spread + K * B * 2.0 ** -31 * (w * top).max()
+        over = (np.abs(out[0, g].double().cpu().numpy() - want) / tol).max()
+        assert over <= 1, over
+    pi.close()
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(64, 16), (128, 8)])
+@pytest.mark.parametrize("nats", [14.0, 17.0])
+def test_a_long_tail_under_one_large_score_in_many_sequences(Hq, Hkv, nats):
+    """As above, with so many sequences that four warps have all tokens of one: a fourth of the tail is counted from the large score's reference."""
+    n, K, B = 13, 16, 64
+    pi = context(n_q_heads=Hq, n_kv_heads=Hkv, block_tokens=B, budget_blocks=K, pool_slots=K, max_blocks=K, max_batch=n)
+    rng = np.random.default_rng(Hq)
+    kv = rng.standard_normal((K, Hkv, 2, B, 128)) * np.asarray([0.1, 1.0])[:, None, None]
+    kv[:, :, 1] += 2
+    kv[:, :, 0, :, 0] = 0
+    kv[3, :, 0, 20, 0], kv[3, :, 1, 20] = nats, 0
+    pool = ref.pack(ref.bf16(kv), B)
+    q = ref.bf16(rng.standard_normal((1, Hq, 128)))
+    q[..., 0] = ref.bf16(np.float64(128 ** 0.5))
+    order = np.tile(np.arange(K, dtype=np.int32), (n, 1))
+    case = dict(pool=np.tile(pool, (n, 1, 1)), blocks=order, slots=order, count=np.full(n, K, dtype=np.int32), ctx=np.full(n, K * B), q=np.tile(q, (n, 1, 1)))
+    out, lse = run_attention(pi, case)
+    assert torch.equal(out, out[:1].expand_as(out)) and torch.equal(lse, lse[:1].expand_as(lse))
+    values = ref.unpack(pool, Hkv, B)
+    for g in range(Hq):
+        k, v = (values[:, g * Hkv // Hq, i].reshape(K * B, 128) for i in (0, 1))
+        top = np.repeat(np.abs(v).reshape(K, B * 128).max(1), B)
+        z = k @ q[0, g].astype(np.float64) / np.sqrt(128)
+        w = np.exp(z - z.max())
+        w /= w.sum()
+        eps = (8 * 2.0 ** -23 * (np.abs(k) @ np.abs(q[0, g].astype(np.float64))).max() + 4 * 2.0 ** -24 * np.abs(z).max() * np.sqrt(128)) / np.sqrt(128)
+        want, spread = w @ v, w @ np.abs(v)
+        tol = 2.0 ** -8 * np.abs(want) + (2 * eps + 2.0 ** -11 + 2.0 ** -20) * spread + K * B * 2.0 ** -31 * (w * top).max()
+        over = (np.abs(out[0, g].double().cpu().numpy() - want) / tol).max()
+        assert over <= 1, over
+    pi.close()
