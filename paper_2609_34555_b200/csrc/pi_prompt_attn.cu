@@ -402,7 +402,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     const float alpha = pa_ex2(far_off(mc_new) ? (m - m_new) * c : mc - mc_new);
                     m = m_new;
                     mc = mc_new;
-                    far = __any_sync(0xffffffffu, far_off(mc));
+                    far = far_off(mc);
                     l *= alpha;
                     if (j > begin) {
 #pragma unroll 1
@@ -422,10 +422,11 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 // maximum is taken off before the scale.
                 constexpr float lift = Form<T>::lift;
                 float2 less = make_float2(lift - mc, lift - mc);
-                if (far) {
+                if (__any_sync(0xffffffffu, far)) {
+                    const float off = far ? m : 0.f;             // (a row's bits do not hang on the rows beside it)
 #pragma unroll
-                    for (int x = 0; x < 128; ++x) s[x] -= m;
-                    less = make_float2(lift, lift);
+                    for (int x = 0; x < 128; ++x) s[x] -= off;
+                    if (far) less = make_float2(lift, lift);
                 }
                 const float2 cc = make_float2(c, c);
                 float2 sum = make_float2(0.f, 0.f);

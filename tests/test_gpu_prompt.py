@@ -519,3 +519,18 @@ def test_a_long_tail_under_one_large_score_in_fp16(Hq, Hkv, n, m, at, nats):
     tol = 2.0 ** -11 * want.abs() + (2.0 ** -11 + 2.0 ** -15) * spread + 2.0 ** -32 * thin + 2.0 ** -25
     over = float(((out.cpu().double() - want).abs() / tol).max())
     assert over <= 1.0, over
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("n,m", [([90], [400]), ([90] + ONES, [400] + ONES), ([3], [3000])])
+def test_a_row_with_scores_far_from_zero_leaves_the_bits_of_its_neighbours(dtype, n, m):
+    pi = context(8, 2, max_batch=300)
+    q, k, v, qs, ks = case(8, 2, n, m, dtype, seed=6)
+    base, base_lse = run(pi, q, k, v, qs, ks)
+    large = torch.zeros(q.shape[:2], dtype=torch.bool)
+    for row, head in ((0, 5), (n[0] // 2, 0), (n[0] - 1, 7)):
+        large[row, head] = True
+    q[large.cuda()] *= 2000.0
+    out, lse = run(pi, q, k, v, qs, ks)
+    assert torch.equal(out.cpu()[~large], base.cpu()[~large]) and torch.equal(lse.cpu()[~large], base_lse.cpu()[~large])
+    assert bool((lse.cpu()[large].abs() > 1024).all())
