@@ -395,7 +395,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     for (int y = 8; y < 128; y += 8) mx4[x] = pa_max3(mx4[x], s[x + y], s[x + y + 4]);
                 }
                 const float mx = fmaxf(pa_max3(mx4[0], mx4[1], mx4[2]), mx4[3]);
-                const bool over = real && mx * c - mc > 8.f;         // (each row by itself: what its neighbours are does not change its bits)
+                // (each row by itself: what its neighbours are does not change its bits.  Far from 0 as the weights are counted there: with the reference
+                // rounded in both, scores that are far apart might seem equal, and a weight leave its range)
+                const bool over = real && (far ? (mx - m) * c : mx * c - mc) > 8.f;
                 if (__any_sync(0xffffffffu, over)) {
                     const float m_new = over ? mx : m, mc_new = over ? mx * c : mc;
                     // (far from 0 the reference's own rounding counts: see below)

@@ -534,3 +534,24 @@ def test_a_row_with_scores_far_from_zero_leaves_the_bits_of_its_neighbours(dtype
     out, lse = run(pi, q, k, v, qs, ks)
     assert torch.equal(out.cpu()[~large], base.cpu()[~large]) and torch.equal(lse.cpu()[~large], base_lse.cpu()[~large])
     assert bool((lse.cpu()[large].abs() > 1024).all())
+
+
+# two scores a step of fp32 apart, whose logarithms under base 2 round to the same number although the weights differ by 2^16 and 2^261
+@pytest.mark.parametrize("dtype,q0,k0,step", [(torch.float16, 32768.0, 64288.0, 128.0), (torch.bfloat16, 221184.0, 153600.0, 2048.0)])
+@pytest.mark.parametrize("others", [[], ONES])
+def test_scores_so_large_that_a_step_is_more_than_a_weights_range(dtype, q0, k0, step, others):
+    pi = context(4, 1, max_batch=300)
+    q, k, v, qs, ks = case(4, 1, [1] + others, [700] + others, dtype, seed=13)
+    q[0], k[:700] = 0, 0
+    q[0, :, 0], q[0, :, 1] = q0, 1.0
+    k[5, 0, 0] = k0
+    k[300, 0, 0], k[300, 0, 1] = k0, step
+    out, lse = run(pi, q, k, v, qs, ks)
+    a, b = v[5, 0].double().cpu(), v[300, 0].double().cpu()
+    # (a score is off by more than the two differ, so the result may be either value or any in between)
+    got = out[0].double().cpu()
+    slack = torch.finfo(dtype).eps * torch.maximum(a.abs(), b.abs()) + 2.0 ** -14
+    assert bool(((got >= torch.minimum(a, b) - slack) & (got <= torch.maximum(a, b) + slack)).all())
+    assert bool(((lse[0].double().cpu() - q0 * k0 / 128 ** 0.5).abs() <= 2.0 ** -20 * q0 * k0 / 128 ** 0.5).all())
+    for s in range(1, len(qs) - 1):
+        assert torch.allclose(out[qs[s]].float(), v[ks[s]].float().expand(4, 128))
