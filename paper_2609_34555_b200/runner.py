@@ -368,14 +368,19 @@ class DecodeSession:
         """One layer's prompts, from its (normed and rotated) queries, keys and values: q [T][Hq][D], k, v [T][Hkv][D] bf16, the sequences one behind
         the other, sequence s from token starts[s] on (int32 [batch + 1] on the device).  Their attention goes to `out` [T][Hq][D]; the
         keys and values go where load_layer puts them, with the lengths as the context.  resident: int32 [batch][C], the blocks of
-        the hot set (None: sink blocks and as many of the newest as the pool holds)."""
+        the hot set (None: sink blocks and as many of the newest as the pool holds).  As load_layer it writes all of the layer's blocks, of every
+        sequence, whatever the prompts' lengths: for the start of a batch.  What does not fit is refused before anything is written."""
         c = self.pi.cfg
+        if any(x.dtype != torch.bfloat16 for x in (q, k, v)):
+            raise TypeError("load_prompts: expected queries, keys and values in bfloat16")
         if k.shape[0] != v.shape[0] or starts.shape != (self.batch + 1,):
             raise ValueError("load_prompts: expected keys and values of the same tokens, and batch + 1 starts")
+        if resident is not None and resident.shape != (self.batch, c.pool_slots):
+            raise ValueError("load_prompts: expected resident blocks [batch][pool_slots]")
         begin = starts.long()
         lens = begin.diff()
         least, longest = lens.aminmax()
-        if int(least) < 0 or int(longest) > c.max_blocks * c.block_tokens or int(begin[0]) < 0 or int(begin[-1]) > k.shape[0]:
+        if int(least) < 0 or int(longest) > c.max_blocks * c.block_tokens or int(begin[0]) < 0 or int(begin[-1]) > min(q.shape[0], k.shape[0]):
             raise ValueError("load_prompts: starts have to rise within the tokens given, by max_blocks blocks at most")
         self.pi.prompt_attn(q, k, v, starts, out, lse=lse)
         self.ctx_len.copy_(lens)

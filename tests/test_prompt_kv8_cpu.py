@@ -169,3 +169,17 @@ def test_the_front_end_refuses_what_is_not_on_the_gpu():
         pi.recall_kv8(0, blocks, blocks, torch.zeros((4, 8, 4), dtype=torch.int32), i32[:4], **here)
     with pytest.raises(TypeError, match="q"):
         pi.sparse_decode_attn_kv8(0, bf, blocks, i32, i32, i32, i32, bf, **here)
+
+
+def test_prompts_that_do_not_fit_are_refused_before_anything_is_written():
+    sess = object.__new__(DecodeSession)
+    made = []
+    sess.pi = types.SimpleNamespace(cfg=types.SimpleNamespace(max_blocks=4, block_tokens=16, pool_slots=4), prompt_attn=lambda *a, **k: made.append(a))
+    sess.batch, sess.kv_bits, sess.device, sess.ctx_len = 2, 8, torch.device("cpu"), torch.full((2,), 9, dtype=torch.int32)
+    q, k, starts = torch.zeros((20, 4, 128), dtype=torch.bfloat16), torch.zeros((20, 2, 128), dtype=torch.bfloat16), torch.tensor([0, 5, 20], dtype=torch.int32)
+    for args, kw, error in (((q[:19], k, k, starts), {}, ValueError), ((q, k[:19], k[:19], starts), {}, ValueError), ((q, k, k[:19], starts), {}, ValueError),
+                            ((q.half(), k.half(), k.half(), starts), {}, TypeError), ((q, k, k.float(), starts), {}, TypeError), ((q, k, k, starts[:2]), {}, ValueError),
+                            ((q, k, k, starts.flip(0)), {}, ValueError), ((q, k, k, starts), dict(resident=torch.zeros((2, 3), dtype=torch.int32)), ValueError)):
+        with pytest.raises(error, match="load_prompts"):
+            sess.load_prompts(0, *args, torch.zeros_like(args[0]), **kw)
+    assert made == [] and sess.ctx_len.tolist() == [9, 9]
