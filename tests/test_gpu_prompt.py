@@ -555,3 +555,39 @@ def test_scores_so_large_that_a_step_is_more_than_a_weights_range(dtype, q0, k0,
     assert bool(((lse[0].double().cpu() - q0 * k0 / 128 ** 0.5).abs() <= 2.0 ** -20 * q0 * k0 / 128 ** 0.5).all())
     for s in range(1, len(qs) - 1):
         assert torch.allclose(out[qs[s]].float(), v[ks[s]].float().expand(4, 128))
+
+
+@pytest.mark.parametrize("batch,longest", [(33, 300), (64, 200), (1024, 9), (1025, 40), (1057, 3), (4096, 5)])
+def test_many_sequences_of_any_length(batch, longest):
+    """More sequences than are looked at at once, some without queries, some without keys, among them a few long ones."""
+    r = random.Random(batch)
+    n = [r.choice([0, 0, 1, r.randrange(longest + 1)]) for _ in range(batch)]
+    m = [max(0, a + r.choice([0, 0, 7, 130, -2])) for a in n]
+    for s in (0, 31, 32, batch // 2, batch - 1):
+        n[s], m[s] = 270 + s % 7, 500
+    pi = context(2, 2, max_batch=4096)
+    q, k, v, qs, ks = case(2, 2, n, m, seed=batch)
+    out, lse = run(pi, q, k, v, qs, ks)
+    check(q.dtype, out, lse, reference(q, k, v, qs, ks))
+    untouched(out, lse, qs)
+
+
+@pytest.mark.parametrize("batch,at", [(40, 35), (1500, 1499), (1500, 700), (4096, 1024)])
+def test_bounds_that_make_no_sense_among_many_sequences(batch, at):
+    n = [3] * batch
+    pi = context(2, 2, max_batch=4096)
+    q, k, v, qs, ks = case(2, 2, n, n, seed=1, pad=0)
+    good, good_lse = run(pi, q, k, v, qs, ks)
+    bad = list(ks)
+    bad[at + 1] = ks[-1] + 1 if at + 1 == batch else ks[at] - 1                        # behind the tensor, or falling
+    out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+    pi.prompt_attn(q, k, v, i32(qs), out, k_start=i32(bad), lse=lse)
+    torch.cuda.synchronize()
+    got = pi.status()
+    assert got[0] == -8 and got[1] == 8 and got[2] == at, got
+    rows = torch.ones(q.shape[0], dtype=torch.bool)
+    rows[qs[at]:qs[at + 1]] = False
+    assert bool((out.cpu()[~rows] == 7).all())
+    if at + 1 < batch:
+        rows[qs[at + 1]:qs[at + 2]] = False                                            # the next one has other keys than before
+    assert torch.equal(out.cpu()[rows], good.cpu()[rows]) and torch.equal(lse.cpu()[rows], good_lse.cpu()[rows])
