@@ -451,8 +451,10 @@ int pi_sparse_decode_attn_kv4(pi_ctx* ctx, int layer, int batch, const void* q_d
 int64_t pi_kv8_block_bytes(pi_ctx* ctx);
 
 /* Tokens into 8-bit blocks; arguments, skipped tokens and errors as pi_kv4_store.  The tokens of one call that go to the same block stand
- * one behind the other with none skipped between them (as in the maps of pi_assign_pages), and no two of them name the same slot.  Bytes of blocks that no token
- * goes to stay as they are. */
+ * one behind the other with none skipped between them (as in the maps of pi_assign_pages), and no two of them name the same slot: where they
+ * do not, that block's bytes may be any.  A slot named twice by neighbours, and a block that comes back within 16 tokens of where its run begins (32
+ * for blocks of 32, 64 for blocks of 64), set PI_ERR_INDEX_RANGE (stage 6: the run's first token, its length, the block).  Bytes of blocks that no
+ * token goes to stay as they are. */
 int pi_kv8_store(pi_ctx* ctx, int64_t n_tokens, const void* k_dev, int64_t k_token_stride, int64_t k_head_stride,
                  int64_t k_outer_stride, const void* v_dev, int64_t v_token_stride, int64_t v_head_stride,
                  int64_t v_outer_stride, int64_t inner_tokens, const int64_t* slot_map_dev, void* store, int64_t n_blocks,

@@ -509,7 +509,8 @@ class PulseInfer:
 
     def kv8_store(self, k, v, store, slot_map=None, stream=None) -> None:
         """kv4_store for blocks in 8 bits (uint8 [..., kv8_block_bytes]).  Tokens of one block, which share its scales, stand one behind the
-        other; a block's first token begins it anew."""
+        other with none skipped between them, or the block may hold anything (and status() says so where the block comes back within a few
+        tokens); a block's first token begins it anew."""
         _check("pi_kv8_store", self._front.kv8_store(self._shape, k, v, store, slot_map, self._stream4(stream)))
 
     def kv8_load(self, store, out, blocks=None, stream=None) -> None:

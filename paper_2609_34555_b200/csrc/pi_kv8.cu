@@ -66,6 +66,10 @@ kv8_store_kernel(StoreParams p) {
         unsigned long long fills = lane < n ? 1ull << at0 : 0ull;
         if (B > 32 && 32 + lane < n) fills |= 1ull << at1;
         const unsigned f0 = __reduce_or_sync(0xffffffffu, static_cast<unsigned>(fills)), f1 = B > 32 ? __reduce_or_sync(0xffffffffu, static_cast<unsigned>(fills >> 32)) : 0u;
+        // a block that comes back behind its run, as far as can be seen from here, or a slot named twice: what the block holds then is chance, which is said
+        const unsigned long long in = in0 | static_cast<unsigned long long>(in1) << 32;
+        if (!is_v && h == 0 && lane == 0 && ((n < 64 && in >> n) || __popc(f0) + __popc(f1) != n))
+            pi_report(p.st, PI_ERR_INDEX_RANGE, PI_STAGE_KV4, static_cast<int>(first), n, static_cast<int>(block));
         // (token t is row t % inner of the outer index t / inner: one division a run, then a step at a time)
         const long long o0 = p.inner ? first / p.inner : 0, r0 = (p.inner ? first - o0 * p.inner : first) + quarter;
         // rows from the i0-th four on, KEEP fours of them: eight lanes a row, 32 bytes a lane

@@ -746,3 +746,40 @@ def test_a_long_tail_under_one_large_score_in_many_sequences(Hq, Hkv, nats):
         over = (np.abs(out[0, g].double().cpu().numpy() - want) / tol).max()
         assert over <= 1, over
     pi.close()
+
+
+@pytest.mark.parametrize("slots,first,run,block", [
+    (list(range(10)) + [-1] + list(range(11, 20)), 0, 10, 0),                          # a token skipped inside a block
+    ([64, 65, 0, 1, 66], 0, 2, 2),                                                     # a block that comes back behind another one
+    ([32, 33, 34, 34, 34, 35] + [36] * 30, 0, 32, 1),                                  # more tokens than a block has
+])
+def test_store_reports_a_block_that_comes_back(slots, first, run, block):
+    pi = context(n_q_heads=2, n_kv_heads=2, block_tokens=32)
+    rng = np.random.default_rng(9)
+    k, v = tokens_of(rng, len(slots), 2)
+    store = torch.zeros((4, pi.kv8_block_bytes), dtype=torch.uint8, device=DEV)
+    pi.kv8_store(bf(k), bf(v), store, dev(np.asarray(slots, dtype=np.int64)))
+    assert clean(pi, -8)[1:5] == [6, first, run, block]
+    rest = [b for b in range(4) if b not in {s // 32 for s in slots if s >= 0}]
+    assert int(store[rest].sum()) == 0
+    pi.close()
+
+
+@pytest.mark.parametrize("block", [16, 32, 64])
+def test_store_reports_nothing_of_maps_in_order(block):
+    """Runs that begin and end anywhere, skipped tokens between blocks, single tokens of many blocks."""
+    pi = context(n_q_heads=2, n_kv_heads=2, block_tokens=block)
+    rng = np.random.default_rng(block)
+    for _ in range(30):
+        order, slots = rng.permutation(40), []
+        for b in order[:rng.integers(1, 40)]:
+            a = rng.integers(0, block)
+            slots += list(b * block + np.arange(a, a + rng.integers(1, block - a + 1)) % block) + [-1] * rng.integers(0, 3)
+        k, v = tokens_of(rng, len(slots), 2)
+        store = torch.zeros((40, pi.kv8_block_bytes), dtype=torch.uint8, device=DEV)
+        want = store.cpu().numpy()
+        pi.kv8_store(bf(k), bf(v), store, dev(np.asarray(slots, dtype=np.int64)))
+        clean(pi)
+        ref.store(want, k, v, np.asarray(slots, dtype=np.int64), block)
+        assert np.array_equal(store.cpu().numpy(), want)
+    pi.close()
