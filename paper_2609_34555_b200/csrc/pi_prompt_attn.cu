@@ -369,7 +369,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             const int seen = real ? plan.seen(w, i) : INT32_MAX;     // (rows of no query may be anything: none is looked at)
             const int all_see = __reduce_min_sync(0xffffffffu, seen);
             const int begin = plan.begin(t), end = plan.end(t);
-            float m = PA_NO_MAX, mc = PA_NO_MAX, l = 0.f;            // the reference of the row's weights, as a score and times c; their sum
+            float m = PA_NO_MAX, mc = PA_NO_MAX, l = 0.f;            // the reference of the row's weights, as a score, and times c less the lift; their sum
             bool far = false;
             for (int j = begin; j < end; j += plan.step(), ++steps) {
                 if (!wait(B_S_FULL + t, steps & 1u)) { alive = false; break; }
@@ -399,9 +399,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const float mx = fmaxf(pa_max3(mx4[0], mx4[1], mx4[2]), mx4[3]);
                 // (each row by itself: what its neighbours are does not change its bits.  Far from 0 as the weights are counted there: with the reference
                 // rounded in both, scores that are far apart might seem equal, and a weight leave its range)
-                const bool over = real && (far ? (mx - m) * c : mx * c - mc) > 8.f;
+                const bool over = real && (far ? (mx - m) * c > 8.f : mx * c - mc > 8.f + Form<T>::lift);
                 if (__any_sync(0xffffffffu, over)) {
-                    const float m_new = over ? mx : m, mc_new = over ? mx * c : mc;
+                    const float m_new = over ? mx : m, mc_new = over ? mx * c - Form<T>::lift : mc;
                     // (far from 0 the reference's own rounding counts: see below)
                     const float alpha = pa_ex2(far_off(mc_new) ? (m - m_new) * c : mc - mc_new);
                     m = m_new;
@@ -424,13 +424,12 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 // The weight is 2^(s c - mc), one fused operation and the exponential: mc is what the row's weights are counted from, and its
                 // rounding is in all of them alike.  Where it is large that rounding would leave the range of the weights, so there the
                 // maximum is taken off before the scale.
-                constexpr float lift = Form<T>::lift;
-                float2 less = make_float2(lift - mc, lift - mc);
+                float2 less = make_float2(-mc, -mc);
                 if (__any_sync(0xffffffffu, far)) {
                     const float off = far ? m : 0.f;             // (a row's bits do not hang on the rows beside it)
 #pragma unroll
                     for (int x = 0; x < 128; ++x) s[x] -= off;
-                    if (far) less = make_float2(lift, lift);
+                    if (far) less = make_float2(Form<T>::lift, Form<T>::lift);
                 }
                 const float2 cc = make_float2(c, c);
                 float2 sum = make_float2(0.f, 0.f);
@@ -546,7 +545,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 }
                 if (SPLIT) {
                     if (real) asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(share_ml + static_cast<uint32_t>(128 * t + r) * 8u), "f"(mc), "f"(l) : "memory");
-                } else if (real && p.lse) p.lse[row] = none ? -INFINITY : (mc + (log2f(l) - Form<T>::lift)) * 0.6931471805599453f;
+                } else if (real && p.lse) p.lse[row] = none ? -INFINITY : (mc + log2f(l)) * 0.6931471805599453f;
             }
             tc_fence_before();
             if (SPLIT) {
@@ -599,7 +598,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         const float by = nothing ? 0.f : 1.f / sum_of[u];
                         *reinterpret_cast<uint2*>(static_cast<T*>(p.out) + row_of[u] * PI_HEAD_DIM + 4 * quad) =
                             nothing ? make_uint2(0u, 0u) : make_uint2(Form<T>::pack(o[u].x * by, o[u].y * by), Form<T>::pack(o[u].z * by, o[u].w * by));
-                        if (p.lse && quad == 0) p.lse[row_of[u]] = nothing ? -INFINITY : (top[u] + (log2f(sum_of[u]) - Form<T>::lift)) * 0.6931471805599453f;
+                        if (p.lse && quad == 0) p.lse[row_of[u]] = nothing ? -INFINITY : (top[u] + log2f(sum_of[u])) * 0.6931471805599453f;
                     }
                 }
                 arrive_at_all(B_SHARE_EMPTY);
