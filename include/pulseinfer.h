@@ -61,9 +61,10 @@ typedef struct {
     int32_t attn_mode;                        /* split of the attention work: 0 = chosen per call, 1 = flat (all KV heads of a block
                                                  per tile, sequences cut across CTAs, partials merged by a second kernel),
                                                  2 = head-major (one (sequence, KV head) per CTA, merged inside the CTA) */
-    int32_t wait_limit_us;                    /* bound of every device-side wait of the attention kernel in microseconds,
+    int32_t wait_limit_us;                    /* bound of every device-side wait of the attention kernels in microseconds,
                                                  0 = default (2 000 000); when it runs out the kernel gives up, returns and
-                                                 the status word says PI_ERR_TIMEOUT (stage 4: CTA, first unit, last unit) */
+                                                 the status word says PI_ERR_TIMEOUT (stage 4: CTA, first unit, last unit;
+                                                 stage 8: CTA, first token, KV head of its first item) */
     int32_t test_hold_producer;               /* TEST ONLY, keep 0: when 1 the loads of every CTA's last tile are never
                                                  issued, so that the bounded wait above can be seen to run out */
     const int32_t* solo_head;                 /* host [n_layers]: retrieval KV head per layer (copied) */

@@ -944,6 +944,11 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             unsigned place = blockIdx.x / static_cast<unsigned>(split);      // (of a cluster: its first CTA's)
             uint32_t asked = 0u;
             bool more = true;
+            // This warp's waits last as long as an item does, so their limit grows with the longest item told so far: 2^15 cycles a K/V tile, ten times what one takes.
+            long long patience = p.wait_cycles;
+            auto wait_item = [&](uint32_t place, uint32_t parity) {
+                return __all_sync(0xffffffffu, SPLIT ? mbar_wait_cluster(bar(place), parity, abort, patience) : mbar_wait(bar(place), parity, abort, patience)) != 0;
+            };
             for (int it = 0;; ++it) {
                 Item w = {0, 0, 0, 0, 0, -1};
                 const int item = static_cast<int>(place >> p.log_hkv);
@@ -981,7 +986,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         w.h = static_cast<int>(place) & (p.Hkv - 1);
                     }
                 }
-                if (it >= 2 && !wait_here(B_ITEM_EMPTY + (it & 1), ((it >> 1) - 1) & 1)) break;
+                if (it >= 2 && !wait_item(B_ITEM_EMPTY + (it & 1), ((it >> 1) - 1) & 1)) break;
+                patience = max(patience, p.wait_cycles + (static_cast<long long>(w.m / PA_ROWS + 1) << 15));
                 if (SPLIT) {                        // lane k tells rank k
                     if (lane < split) {
                         const uint32_t at = map_shared_rank(smem_u32(&s_item[it & 1]), lane), odd = map_shared_rank(smem_u32(&s_odd[it & 1]), lane);
@@ -998,7 +1004,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 }
                 __syncwarp();
                 if (!has) break;
-                if (!wait(B_WANTED, it & 1)) break;
+                if (!wait_item(B_WANTED, it & 1)) break;
                 // a CTA that has not begun gives its place up, if there is one (a place behind the last item too, and then the next)
                 uint32_t got = 0u;
                 do {

@@ -591,3 +591,15 @@ def test_bounds_that_make_no_sense_among_many_sequences(batch, at):
     if at + 1 < batch:
         rows[qs[at + 1]:qs[at + 2]] = False                                            # the next one has other keys than before
     assert torch.equal(out.cpu()[rows], good.cpu()[rows]) and torch.equal(lse.cpu()[rows], good_lse.cpu()[rows])
+
+
+def test_a_short_limit_of_the_waits_does_not_end_a_long_item():
+    """Items of 938 K/V tiles, which take longer than the limit of a single wait: nothing stands still, so nothing is given up."""
+    pi, short = context(16, 16), context(16, 16, wait_limit_us=500)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    q, k, v = (torch.randn((t, 16, 128), generator=g, device="cuda", dtype=torch.bfloat16) for t in (1200, 120000, 120000))
+    want, want_lse = run(pi, q, k, v, [0, 1200], [0, 120000])
+    out, lse = run(short, q, k, v, [0, 1200], [0, 120000])
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    heads = [0, 15]
+    check(q.dtype, out[-3:, heads], lse[-3:, heads], reference(q[-3:, heads], k[:, heads], v[:, heads], [0, 3], [0, 120000]))
