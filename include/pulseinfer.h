@@ -495,7 +495,8 @@ int pi_sparse_decode_attn_kv8(pi_ctx* ctx, int layer, int batch, const void* q_d
  *   q_start_dev, k_start_dev  [n_seqs + 1] int32; k_start_dev NULL: the keys are packed as the queries are (m = n)
  *   out_dev          [n_q][Hq][D], lse_dev NULL or [n_q][Hq] float; rows of tokens of no sequence stay as they were
  * A sequence whose bounds decrease or leave the tensors is left out and sets PI_ERR_INDEX_RANGE (stage 8: sequence, its bounds).
- * n_seqs at most max_batch.  Weights are rounded to the tensors' type before they meet V; all sums are in 32 bits. */
+ * n_seqs at most max_batch.  Weights are rounded to the tensors' type before they meet V (by half a step; in fp16 those below 2^-21 of a row's
+ * largest by up to 2^-32 of it); all sums are in 32 bits. */
 int pi_prompt_attn(pi_ctx* ctx, int n_seqs, int dtype, int64_t n_q, const void* q_dev, int64_t q_token_stride, int64_t q_head_stride,
                    int64_t n_k, const void* k_dev, int64_t k_token_stride, int64_t k_head_stride, const void* v_dev,
                    int64_t v_token_stride, int64_t v_head_stride, const int32_t* q_start_dev, const int32_t* k_start_dev, void* out_dev,

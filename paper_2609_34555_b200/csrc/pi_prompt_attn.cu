@@ -27,9 +27,9 @@
 // rescaled; then the softmax warps do it themselves, between their S and their P, when no product of their tile is in flight.
 //
 // Measured on a B200 (32 query heads, 8 KV heads, bf16; 1 643 TFLOP/s is what a library product reaches in a short run, 1 394 for seconds):
-// one prompt of 8 192 tokens 434 us, 1 267 TFLOP/s, in a run of a few milliseconds, 505 us for longer, where the power limit takes the
-// clock from 1.7 to 1.45 GHz; 23 prompts of 0 to 1 500 tokens 172 us, 219 for longer; 77 tokens 7.1 us; 16 sequences of one token after 16 384
-// 174 us, 6.2 TB/s, after 0 to 16 384 89 us (105 before the longest sequences came first); 500 tokens after 65 536 with 64 heads in fp16 930 us.  An iteration (two query tiles, one K/V tile) takes 3 270 cycles,
+// one prompt of 8 192 tokens 434 us, 1 267 TFLOP/s, in a run of a few milliseconds, 496 us for longer, where the power limit takes the
+// clock from 1.7 to 1.45 GHz; 23 prompts of 0 to 1 500 tokens 173 us, 214 for longer; 77 tokens 7.0 us; 16 sequences of one token after 16 384
+// 171 us, 6.3 TB/s, after 0 to 16 384 87 us (105 before the longest sequences came first); 500 tokens after 65 536 with 64 heads in fp16 920 to 950 us.  An iteration (two query tiles, one K/V tile) takes 3 270 cycles,
 // of which the tensor pipe and the exponentials are busy for 2 048 each.
 // Tried and not taken: a share of the exponentials as polynomials (3 % fewer cycles, the same time), P handed over in two halves, a
 // reference without each tile's maximum, clusters of 16; the next item's first product ahead of this one's last, weights of masked keys left
